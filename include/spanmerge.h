@@ -31,6 +31,15 @@
  *   sm_kv_project       the K/V state of an input row (surrogate or token) at
  *                       its compressed position; sm_kv_append_projected
  *                       appends it
+ *   sm_kv_reserve       block tables, positions and slots of a step's rows,
+ *                       for all layers at once
+ *   sm_rotary           rotary positions of rows of heads
+ *   sm_kv_write_rotary  one layer's q, K and V rows: q and K turned, K and V
+ *                       into the reserved slots
+ *   sm_block_norm       residual sum with the norms after one block and
+ *                       before the next
+ *   sm_token_logprobs   log probabilities, entropy and top alternatives of
+ *                       rows of logits
  *
  * General rules for every call
  * ----------------------------
@@ -674,6 +683,217 @@ sm_status sm_kv_project(const sm_paged_cache *c, const int32_t *seq_ids, int n,
 sm_status sm_kv_append_projected(const sm_paged_cache *c, const int32_t *seq_ids,
                                  int n, const void *x, const sm_kv_proj_params *p,
                                  void *ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * Rows that a backbone's layers write (every layer of a step at the same
+ * positions: "Compressed-position convention"; "Decoding-time Integration").
+ *
+ * sm_kv_reserve -- the block tables, positions and slots of the rows that
+ * the requests of a step (or of a prompt batch) are about to write, once for
+ * all layers whose caches share the tables: request i first drops its last
+ * crop[i] cached entries (the raw tokens of a span that just completed, or
+ * draft tokens that were rejected), then room for rows[i] entries is taken.
+ * The state is the one that
+ *   sm_kv_rollback(c, seq_ids, crop, n), then the bookkeeping of
+ *   sm_kv_append(c, seq_ids, row_offsets, n, sum of rows, ...)
+ * leave, with lengths advanced to include the rows; no K or V is touched
+ * (sm_kv_write_rotary writes them).  It is made whole or not at all.
+ *
+ *  seq_ids      [n] distinct sequence ids, n <= min(max_seqs, SM_MAX_REQUESTS)
+ *  crop         [n] 0 <= crop[i] <= lengths[seq_ids[i]], or null for none
+ *  rows         [n] rows[i] >= 0
+ *  max_rows     (host) room in pos and slots
+ *  row_offsets  [n + 1] out: request i's rows are [row_offsets[i],
+ *               row_offsets[i+1]) of every layer's K and V
+ *  pos          [max_rows] out: each row's position in its sequence
+ *  slots        [max_rows] out: physical block x block_size + slot in the
+ *               page.  Entries past the last row are -1 (position 0), so a
+ *               batch padded to max_rows writes its own rows only.
+ * num_blocks x block_size must be below 2^31.  Device errors (into c->err):
+ * EINVAL (bad or repeated id, negative count, more than max_rows rows,
+ * corrupt free stack or block table), ERANGE (crop longer than the cache,
+ * length above the capacity, no room on the free stack), ENOMEM (not enough
+ * free blocks).  When the call fails, or the error word was set before it,
+ * the cache is left as it was, every slot is -1, and every position and
+ * every row offset is 0.
+ */
+sm_status sm_kv_reserve(const sm_paged_cache *c, const int32_t *seq_ids,
+                        const int32_t *crop, const int32_t *rows, int n,
+                        int max_rows, int32_t *row_offsets, int32_t *pos,
+                        int32_t *slots, hipStream_t stream);
+
+/*
+ * Rotary positions.  Feature pair j < rot_dim / 2 of a head (features j and
+ * j + rot_dim / 2 in the half layout, 2 j and 2 j + 1 in the interleaved
+ * one) is turned by the angle p w'_j and scaled by attn_scale:
+ *   (a, b) -> attn_scale (a cos - b sin, a sin + b cos),
+ *   w_j = theta^(-2 j / rot_dim)
+ * and w' is w, or for contexts beyond the trained one
+ *   LINEAR  w / factor
+ *   BANDS   u w + (1 - u) w / factor, u = (context w / 2 pi - low) /
+ *           (high - low) clamped to [0, 1]: pairs that turn more than `high`
+ *           times over the trained context keep their frequency, those
+ *           below `low` turns are stretched (Llama 3: 1 and 4)
+ *   RAMP    v w / factor + (1 - v) w, v = (j - j0) / max(j1 - j0, 0.001)
+ *           clamped to [0, 1], between the pairs that turn `high` and `low`
+ *           times, J(t) = rot_dim ln(context / (2 pi t)) / (2 ln theta):
+ *           j0 = max(floor J(high), 0), j1 = min(ceil J(low), rot_dim - 1)
+ * Features from rot_dim on are copied.  Angles are formed and reduced in
+ * double precision; positions may be any int32.
+ */
+typedef enum { SM_ROPE_HALF = 0, SM_ROPE_INTERLEAVED = 1 } sm_rope_layout;
+typedef enum {
+  SM_ROPE_PLAIN = 0,
+  SM_ROPE_LINEAR = 1,
+  SM_ROPE_BANDS = 2,
+  SM_ROPE_RAMP = 3
+} sm_rope_scaling;
+
+typedef struct {
+  int rot_dim;      /* even, 2 <= rot_dim <= head_dim */
+  int layout;       /* sm_rope_layout */
+  int scaling;      /* sm_rope_scaling */
+  float theta;      /* > 0 (RAMP: > 1) */
+  float attn_scale; /* factor of the turned features, finite (1 for none) */
+  float factor;     /* LINEAR, BANDS, RAMP: > 0 */
+  float low, high;  /* BANDS, RAMP: 0 < low < high (turns over the context) */
+  float context;    /* BANDS, RAMP: trained context length, > 0 */
+} sm_rope_params;
+
+/*
+ * sm_rotary -- out[r, h] = x[r, h] turned by position pos[r].
+ *
+ *  x, x_stride  row r, head h, feature i at x[r x_stride + h head_dim + i]
+ *               (a column range of a packed projection, say); x_stride >=
+ *               heads x head_dim, in elements
+ *  pos          [rows]
+ *  heads, head_dim  (host) 1 <= heads <= 1024, 2 <= head_dim <= 256
+ *  p            (host)
+ *  transpose    (host) 1: the transposed map (angles negated): the gradient
+ *               of the forward call with respect to x, and its inverse
+ *               where attn_scale is 1; 0: the forward map
+ *  out, out_stride  as x; x itself (same address and stride) or no overlap
+ * Any element-aligned address; 16-byte aligned rows with rot_dim a multiple
+ * of 16 (fp32: 8) take the wide path.  No device errors.
+ */
+sm_status sm_rotary(const void *x, int64_t x_stride, const int32_t *pos,
+                    int rows, int heads, int head_dim, const sm_rope_params *p,
+                    int transpose, sm_dtype dt, void *out, int64_t out_stride,
+                    hipStream_t stream);
+
+/*
+ * sm_kv_write_rotary -- one layer's rows after its projection, in one launch:
+ *   q_out[r, h] = q[r, h] turned by pos[r]
+ *   k[r], turned by pos[r], and v[r] go to slot slots[r] of the cache's pages
+ *
+ *  c            (host) the layer's pools, their sizes and err (its tables and
+ *               lengths are not read)
+ *  pos, slots   [rows] from sm_kv_reserve; a row of slot -1 is not written
+ *               to the pages; the other slots are distinct
+ *  q, q_stride  [rows][num_q_heads][head_dim], row stride in elements as in
+ *               sm_rotary; null with num_q_heads = 0 for K and V alone
+ *  k, v         [rows][num_kv_heads][head_dim] with their row strides (the
+ *               three may be column ranges of one packed buffer)
+ *  num_q_heads  (host) 0 <= num_q_heads <= 1024 (any multiple or none of
+ *               num_kv_heads)
+ *  q_out        as q (every row is written); q itself or no overlap
+ * Values are in the cache's dtype; num_blocks x block_size must be below
+ * 2^31.  Device errors (into c->err): EINVAL for a slot outside
+ * [-1, num_blocks x block_size); that row is not written to the pages, the
+ * others are.  The call goes by its slots alone and does not look at the
+ * error word (a reserve that failed gives no slots).
+ */
+sm_status sm_kv_write_rotary(const sm_paged_cache *c, const int32_t *pos,
+                             const int32_t *slots, int rows, const void *q,
+                             int64_t q_stride, int num_q_heads, const void *k,
+                             int64_t k_stride, const void *v, int64_t v_stride,
+                             const sm_rope_params *p, void *q_out,
+                             int64_t q_out_stride, hipStream_t stream);
+
+/*
+ * The norms around a block of the backbone:
+ *   RMS    x / sqrt(mean(x^2) + eps) gain (+ bias)
+ *   LAYER  (x - mean(x)) / sqrt(var(x) + eps) gain (+ bias), biased variance
+ */
+typedef enum { SM_NORM_RMS = 0, SM_NORM_LAYER = 1 } sm_norm_kind;
+
+typedef struct {
+  int kind;         /* sm_norm_kind */
+  float eps;        /* >= 0 */
+  const void *gain; /* [d] (dtype dt), or null for 1 (folded into a weight) */
+  const void *bias; /* [d], or null for 0 */
+} sm_norm;
+
+/*
+ * sm_block_norm -- the residual stream past one block and the next block's
+ * input, in one pass:
+ *   t     = norm_post(y)              (y itself without post)
+ *   h_out = h + scale gate t          (h alone without y)
+ *   n_out = norm_pre(h + scale gate t)
+ * The norms' statistics and the sum are fp32; n_out is taken of the sum
+ * before it is rounded into h_out.
+ *
+ *  h, h_stride  [rows][d], row stride in elements (>= d)
+ *  y, y_stride  the block's output, or null
+ *  rows, d      (host) 1 <= d <= 16384
+ *  post, pre    (host) or null; pre null only without n_out
+ *  gate         [d] with gate_stride 0, or a row each (gate_stride >= d), or
+ *               null for 1
+ *  scale        (host) finite
+ *  h_out, n_out row strides as h; either may be null, not both.  Each may
+ *               be an input itself (same address and stride) or overlaps
+ *               nothing
+ * Any element-aligned address; 16-byte aligned rows with d a multiple of 8
+ * (fp32: 4) take the wide path.  No device errors.
+ */
+sm_status sm_block_norm(const void *h, int64_t h_stride, const void *y,
+                        int64_t y_stride, int rows, int d, const sm_norm *post,
+                        const void *gate, int64_t gate_stride, float scale,
+                        const sm_norm *pre, sm_dtype dt, void *h_out,
+                        int64_t h_out_stride, void *n_out, int64_t n_out_stride,
+                        hipStream_t stream);
+
+/* Largest number of alternatives per row. */
+#define SM_MAX_TOP 64
+
+/* Bytes of workspace sm_token_logprobs needs for these sizes. */
+size_t sm_token_logprobs_workspace_bytes(int rows, int vocab, int k);
+
+/*
+ * sm_token_logprobs -- from the logits of a row to probabilities: with
+ * z = scale x and lse = log sum_v exp(z_v),
+ *   logprob[r]  = z[tokens[r]] - lse            (0 for tokens[r] = -1)
+ *   entropy[r]  = lse - sum_v p_v z_v,  p = exp(z - lse)
+ *   top_ids[r], top_logprobs[r]: the k largest x, the largest first, the
+ *   lower index first among equal ones, and their z - lse
+ * The first alternative is the greedy token, ready for sm_match_decode; a
+ * prompt is scored with its positions as rows.
+ *
+ *  logits, stride  [rows][vocab] (dtype dt), row stride in elements (>= vocab)
+ *  rows, vocab  (host) vocab >= 1
+ *  scale        (host) 1 / temperature: > 0, at most 2e38
+ *  tokens       [rows] -1 or an id in [0, vocab); null with logprob
+ *  logprob, entropy  [rows] fp32 out; each may be null
+ *  k            (host) 0 <= k <= min(SM_MAX_TOP, vocab)
+ *  top_ids      [rows][k] int32 out, top_logprobs [rows][k] fp32 out; null
+ *               for k = 0 (top_logprobs may be null with top_ids)
+ *  ws, ws_bytes at least sm_token_logprobs_workspace_bytes(rows, vocab, k),
+ *               16-byte aligned.  Its first 64 KiB hold arrival counters:
+ *               zero-fill them once before the first call; every call
+ *               leaves them zero again.  Calls that may run concurrently
+ *               must not share a workspace
+ * A logit of -infinity has probability 0 and adds nothing to the entropy.
+ * A row of nothing else has log probabilities of -infinity and entropy 0;
+ * a row with NaN or +infinity has NaN for both (its alternatives are still
+ * in order, NaN below everything).  Device errors (into err, unless it is
+ * null): EINVAL for a token id out of range; its log probability is 0.
+ */
+sm_status sm_token_logprobs(const void *logits, int64_t stride, int rows,
+                            int vocab, sm_dtype dt, float scale,
+                            const int32_t *tokens, float *logprob,
+                            float *entropy, int k, int32_t *top_ids,
+                            float *top_logprobs, void *ws, size_t ws_bytes,
+                            int32_t *err, hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -19,7 +19,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libspanmerge.so")
-SOURCES = ["decode_attn.hip", "kv_paged.hip", "kvproj.hip", "lut.hip", "merge_spans.hip", "prefill_attn.hip", "rules.hip"]
+SOURCES = ["block_norm.hip", "decode_attn.hip", "kv_paged.hip", "kvproj.hip", "logprobs.hip", "lut.hip", "merge_spans.hip",
+           "prefill_attn.hip", "reserve.hip", "rotary.hip", "rules.hip"]
 BINDING = os.path.join(HERE, "_binding" + sysconfig.get_config_var("EXT_SUFFIX"))
 ARCH = "gfx950"
 

@@ -6,8 +6,10 @@
 // four calls, 30 us of kernels).  Every entry here takes the C call's
 // arguments in order: a tensor (or None) for a device pointer, the ctypes
 // structure for a cache or a rule table, the bytes that merge_params or
-// kv_proj_params gave for parameters, an int (or None) for a stream handle,
-// plain numbers for the rest; it returns the status.  Values are taken and
+// kv_proj_params gave (or a structure's own bytes) for parameters, an int (or
+// None) for a stream handle, plain numbers for the rest; it returns the
+// status.  A tensor in a tuple of its own is taken by its address alone: rows
+// with a stride, which the caller has looked at.  Values are taken and
 // refused as ctypes does for the same prototypes: integers wrap to the C
 // type's width, a ctypes number of the argument's own type counts as its
 // value, and what does not fit raises ctypes.ArgumentError.
@@ -29,7 +31,8 @@ namespace {
   X(sm_merge_spans) X(sm_merge_token_table) X(sm_merge_spans_tabled) X(sm_pack_spans) X(sm_kv_rollback)       \
   X(sm_kv_append) X(sm_decode_attention) X(sm_decode_step) X(sm_decode_merge_step)                            \
   X(sm_decode_step_noalloc) X(sm_prefill_attention) X(sm_rules_build) X(sm_rules_lookup) X(sm_match_prompt)   \
-  X(sm_match_decode) X(sm_gather_surrogates) X(sm_span_dedupe) X(sm_kv_project) X(sm_kv_append_projected)
+  X(sm_match_decode) X(sm_gather_surrogates) X(sm_span_dedupe) X(sm_kv_project) X(sm_kv_append_projected)     \
+  X(sm_kv_reserve) X(sm_rotary) X(sm_kv_write_rotary) X(sm_block_norm) X(sm_token_logprobs)
 #define SM_SLOT(name) decltype(&::name) p_##name;
 SM_ENTRIES(SM_SLOT)
 
@@ -51,8 +54,10 @@ bool is_true(PyObject *r, const char *otherwise) {
 bool tensor_address(PyObject *t, void **p) {
   *p = nullptr;
   if (t == Py_None) return true;
+  const bool strided = PyTuple_CheckExact(t) && PyTuple_GET_SIZE(t) == 1;
+  if (strided) t = PyTuple_GET_ITEM(t, 0);
   if (!is_true(PyObject_GetAttr(t, g_is_cuda), "expected a GPU tensor")) return false;
-  if (!is_true(PyObject_CallMethodNoArgs(t, g_is_contiguous), "expected a contiguous tensor")) return false;
+  if (!strided && !is_true(PyObject_CallMethodNoArgs(t, g_is_contiguous), "expected a contiguous tensor")) return false;
   PyObject *r = PyObject_CallMethodNoArgs(t, g_data_ptr);
   if (!r) return false;
   *p = PyLong_AsVoidPtr(r);
@@ -62,7 +67,8 @@ bool tensor_address(PyObject *t, void **p) {
 
 template <class T>
 constexpr bool is_host_struct = std::is_same_v<T, sm_paged_cache> || std::is_same_v<T, sm_rule_table> ||
-                                std::is_same_v<T, sm_merge_params> || std::is_same_v<T, sm_kv_proj_params>;
+                                std::is_same_v<T, sm_merge_params> || std::is_same_v<T, sm_kv_proj_params> ||
+                                std::is_same_v<T, sm_rope_params> || std::is_same_v<T, sm_norm>;
 
 // the C type that a plain argument (or a stream handle) has in the prototypes
 template <class A>

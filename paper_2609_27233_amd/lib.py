@@ -23,6 +23,10 @@ SM_F32, SM_BF16 = 0, 1
 SM_OK, SM_EINVAL, SM_ERANGE, SM_ENOMEM, SM_EHIP = 0, 1, 2, 3, 4
 ERR_EINVAL, ERR_ERANGE, ERR_ENOMEM = 1, 2, 4
 MAX_REQUESTS = 1024
+MAX_TOP = 64
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {None: 0, "linear": 1, "bands": 2, "ramp": 3}
+NORM_KINDS = {"rms": 0, "layer": 1}
 
 _P, _I, _L, _F, _Z = C.c_void_p, C.c_int, C.c_int64, C.c_float, C.c_size_t
 
@@ -34,7 +38,9 @@ EXPORTED = ("sm_status_string", "sm_merge_workspace_bytes", "sm_merge_spans",
             "sm_prefill_attention", "sm_rules_build_workspace_bytes", "sm_rules_build",
             "sm_rules_lookup", "sm_match_prompt_workspace_bytes", "sm_match_prompt",
             "sm_match_decode", "sm_gather_surrogates", "sm_span_dedupe_workspace_bytes", "sm_span_dedupe",
-            "sm_kv_project_workspace_bytes", "sm_kv_project", "sm_kv_append_projected")
+            "sm_kv_project_workspace_bytes", "sm_kv_project", "sm_kv_append_projected",
+            "sm_kv_reserve", "sm_rotary", "sm_kv_write_rotary", "sm_block_norm",
+            "sm_token_logprobs_workspace_bytes", "sm_token_logprobs")
 
 
 class MergeParams(C.Structure):
@@ -57,6 +63,15 @@ class RuleTableDesc(C.Structure):
 
 class KVProjParams(C.Structure):
     _fields_ = [("d", _I), ("W_k", _P), ("W_v", _P), ("rope_theta", _F), ("rms_eps", _F)]
+
+
+class RopeParams(C.Structure):
+    _fields_ = [("rot_dim", _I), ("layout", _I), ("scaling", _I), ("theta", _F), ("attn_scale", _F), ("factor", _F),
+                ("low", _F), ("high", _F), ("context", _F)]
+
+
+class NormParams(C.Structure):
+    _fields_ = [("kind", _I), ("eps", _F), ("gain", _P), ("bias", _P)]
 
 
 class SpanMergeError(RuntimeError):
@@ -139,6 +154,20 @@ def load(path: str = LIB_PATH):
     L.sm_kv_project.restype = _I
     L.sm_kv_append_projected.argtypes = [C.POINTER(PagedCacheDesc), _P, _I, _P, C.POINTER(KVProjParams), _P, _Z, _P]
     L.sm_kv_append_projected.restype = _I
+    L.sm_kv_reserve.argtypes = [C.POINTER(PagedCacheDesc), _P, _P, _P, _I, _I, _P, _P, _P, _P]
+    L.sm_kv_reserve.restype = _I
+    L.sm_rotary.argtypes = [_P, _L, _P, _I, _I, _I, C.POINTER(RopeParams), _I, _I, _P, _L, _P]
+    L.sm_rotary.restype = _I
+    L.sm_kv_write_rotary.argtypes = [C.POINTER(PagedCacheDesc), _P, _P, _I, _P, _L, _I, _P, _L, _P, _L,
+                                     C.POINTER(RopeParams), _P, _L, _P]
+    L.sm_kv_write_rotary.restype = _I
+    L.sm_block_norm.argtypes = [_P, _L, _P, _L, _I, _I, C.POINTER(NormParams), _P, _L, _F, C.POINTER(NormParams), _I,
+                                _P, _L, _P, _L, _P]
+    L.sm_block_norm.restype = _I
+    L.sm_token_logprobs_workspace_bytes.argtypes = [_I, _I, _I]
+    L.sm_token_logprobs_workspace_bytes.restype = _Z
+    L.sm_token_logprobs.argtypes = [_P, _L, _I, _I, _I, _F, _P, _P, _P, _I, _P, _P, _P, _Z, _P, _P]
+    L.sm_token_logprobs.restype = _I
     try:
         fast = importlib.import_module("._binding", __package__)
     except ImportError as e:
@@ -256,24 +285,36 @@ def pack_spans(seq_offsets, span_start, span_len, seq_span_offsets, pi,
 
 class PagedCache:
     """Device buffers of one paged KV cache (allocated with torch) and the
-    descriptor the C calls take.  Pools: K [NB, Hkv, bs, D], V [NB, Hkv, D, bs]."""
+    descriptor the C calls take.  Pools: K [NB, Hkv, bs, D], V [NB, Hkv, D, bs].
+    ``tables``: another cache of the same sizes, a layer's neighbour, whose
+    block table, lengths, free stack and error word this one shares (kv_reserve
+    keeps them for all layers; only the pools are this one's own)."""
 
     def __init__(self, *, dtype: torch.dtype, num_kv_heads: int, head_dim: int,
                  block_size: int, num_blocks: int, max_seqs: int,
-                 max_blocks_per_seq: int, device="cuda", free_order=None):
+                 max_blocks_per_seq: int, device="cuda", free_order=None,
+                 tables: Optional["PagedCache"] = None):
         self.dtype = dtype
         self.H, self.D, self.bs = num_kv_heads, head_dim, block_size
         self.num_blocks, self.max_seqs, self.max_blocks = num_blocks, max_seqs, max_blocks_per_seq
         self.k_pool = torch.zeros((num_blocks, num_kv_heads, block_size, head_dim), dtype=dtype, device=device)
         self.v_pool = torch.zeros((num_blocks, num_kv_heads, head_dim, block_size), dtype=dtype, device=device)
-        self.block_table = torch.full((max_seqs, max_blocks_per_seq), -1, dtype=torch.int32, device=device)
-        self.lengths = torch.zeros(max_seqs, dtype=torch.int32, device=device)
-        order = (torch.arange(num_blocks, dtype=torch.int32) if free_order is None
-                 else torch.as_tensor(free_order, dtype=torch.int32))
-        # the top of the stack (last element) is handed out first
-        self.free_stack = order.flip(0).contiguous().to(device)
-        self.free_top = torch.tensor([num_blocks], dtype=torch.int32, device=device)
-        self.err = torch.zeros(1, dtype=torch.int32, device=device)
+        if tables is not None:
+            if ((tables.bs, tables.num_blocks, tables.max_seqs, tables.max_blocks) !=
+                    (block_size, num_blocks, max_seqs, max_blocks_per_seq) or free_order is not None
+                    or tables.k_pool.device != self.k_pool.device):
+                raise SpanMergeError("caches that share their tables have the same blocks, sequences and device")
+            self.block_table, self.lengths = tables.block_table, tables.lengths
+            self.free_stack, self.free_top, self.err = tables.free_stack, tables.free_top, tables.err
+        else:
+            self.block_table = torch.full((max_seqs, max_blocks_per_seq), -1, dtype=torch.int32, device=device)
+            self.lengths = torch.zeros(max_seqs, dtype=torch.int32, device=device)
+            order = (torch.arange(num_blocks, dtype=torch.int32) if free_order is None
+                     else torch.as_tensor(free_order, dtype=torch.int32))
+            # the top of the stack (last element) is handed out first
+            self.free_stack = order.flip(0).contiguous().to(device)
+            self.free_top = torch.tensor([num_blocks], dtype=torch.int32, device=device)
+            self.err = torch.zeros(1, dtype=torch.int32, device=device)
         self.desc = PagedCacheDesc(dtype_code(dtype), num_kv_heads, head_dim, block_size,
                                    num_blocks, max_seqs, max_blocks_per_seq,
                                    _ptr(self.k_pool), _ptr(self.v_pool), _ptr(self.block_table),
@@ -474,3 +515,180 @@ def kv_append_projected(cache: PagedCache, seq_ids, x, W_k, W_v, ws=None, rope_t
     p = _proj_params(W_k, W_v, rope_theta, rms_eps)
     st = _calls().sm_kv_append_projected(cache.desc, seq_ids, n, x, p, ws, ws.nbytes, _stream(stream))
     _check(st, "sm_kv_append_projected")
+
+
+# --------------------------------------------------------------------------
+# rows of a backbone's layers: reserved, normed, turned, written, scored
+#
+# These calls look at their tensors before anything is enqueued: a wrong
+# type, device or size raises SpanMergeError.
+
+def _here(stream, *tensors):
+    """The stream's handle; every tensor has to be on the current device, and the stream one of its."""
+    now = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != now:
+            raise SpanMergeError(f"expected tensors on the current device cuda:{now}, got one on {t.device}")
+    if stream is not None and stream.device_index != now:
+        raise SpanMergeError(f"expected a stream of the current device cuda:{now}")
+    return _stream(stream)
+
+
+def _need(t, dtype, count: int, name: str):
+    if t.dtype is not dtype or t.numel() < count:
+        raise SpanMergeError(f"{name}: expected {count} values of {dtype}, got {t.numel()} of {t.dtype}")
+
+
+def _row_stride(t, dtype, rows: int, inner, name: str) -> int:
+    """The row stride of a [rows, *inner] tensor whose rows are contiguous."""
+    shape, st = t.shape, t.stride()
+    if t.dtype is not dtype or len(shape) != 1 + len(inner) or shape[0] != rows or shape[1:] != inner:
+        raise SpanMergeError(f"{name}: expected {dtype} of shape {(rows, *inner)}, got {t.dtype} of {tuple(shape)}")
+    width = 1
+    for size, s in zip(reversed(inner), reversed(st[1:])):
+        if size != 1 and s != width:
+            raise SpanMergeError(f"{name}: expected contiguous rows, got strides {st}")
+        width *= size
+    return st[0] if rows > 1 else width
+
+
+def kv_reserve(cache: PagedCache, seq_ids, rows, row_offsets, pos, slots, crop=None, stream=None):
+    """Drop crop[i] entries of each listed sequence, then take room for rows[i]
+    more: block tables and lengths, and for each row its position and slot.
+    pos and slots (their size is the room for rows) get 0 and -1 past the last."""
+    n, most, i32 = seq_ids.numel(), pos.numel(), torch.int32
+    _need(seq_ids, i32, n, "seq_ids")
+    _need(rows, i32, n, "rows")
+    _need(row_offsets, i32, n + 1, "row_offsets")
+    _need(pos, i32, most, "pos")
+    _need(slots, i32, most, "slots")
+    if crop is not None:
+        _need(crop, i32, n, "crop")
+    st = _calls().sm_kv_reserve(cache.desc, seq_ids, crop, rows, n, most, row_offsets, pos, slots,
+                                _here(stream, cache.err, seq_ids, crop, rows, row_offsets, pos, slots))
+    _check(st, "sm_kv_reserve")
+
+
+def rope_params(rot_dim: int, theta: float = 500000.0, layout: str = "half", scaling: Optional[str] = None,
+                factor: float = 1.0, low: float = 1.0, high: float = 4.0, context: float = 8192,
+                attn_scale: float = 1.0) -> bytes:
+    """A rotation for rotary and kv_write_rotary; layout "half" or
+    "interleaved", scaling None, "linear", "bands" or "ramp"."""
+    if layout not in ROPE_LAYOUTS or scaling not in ROPE_SCALINGS:
+        raise SpanMergeError(f"unknown rotary layout or scaling: {layout!r}, {scaling!r}")
+    return bytes(RopeParams(rot_dim, ROPE_LAYOUTS[layout], ROPE_SCALINGS[scaling], theta, attn_scale, factor, low, high,
+                            context))
+
+
+def rotary(x, pos, rope: bytes, out, transpose: bool = False, stream=None):
+    """out[r, h] = x[r, h] turned by pos[r]; x, out [rows, heads, D], each row
+    contiguous; out may be x.  transpose: the gradient of that with respect to x."""
+    rows, heads, D = x.shape
+    dt = x.dtype
+    _need(pos, torch.int32, rows, "pos")
+    sx = _row_stride(x, dt, rows, (heads, D), "x")
+    so = _row_stride(out, dt, rows, (heads, D), "out")
+    st = _calls().sm_rotary((x,), sx, pos, rows, heads, D, rope, int(transpose), dtype_code(dt), (out,), so,
+                            _here(stream, x, pos, out))
+    _check(st, "sm_rotary")
+
+
+def kv_write_rotary(cache: PagedCache, pos, slots, q, k, v, rope: bytes, q_out, stream=None):
+    """q_out = q turned by pos; K (turned) and V rows into the slots of the
+    cache's pages (-1: not written).  q, q_out [rows, Hq, D] or both None; k, v
+    [rows, Hkv, D]; each row contiguous, so the three may be views of one buffer."""
+    rows, dt, kv = k.shape[0], cache.dtype, (cache.H, cache.D)
+    _need(pos, torch.int32, rows, "pos")
+    _need(slots, torch.int32, rows, "slots")
+    sk, sv = _row_stride(k, dt, rows, kv, "k"), _row_stride(v, dt, rows, kv, "v")
+    hq = sq = so = 0
+    if (q is None) != (q_out is None):
+        raise SpanMergeError("q and q_out go together")
+    if q is not None:
+        hq = q.shape[1]
+        sq, so = _row_stride(q, dt, rows, (hq, cache.D), "q"), _row_stride(q_out, dt, rows, (hq, cache.D), "q_out")
+    st = _calls().sm_kv_write_rotary(cache.desc, pos, slots, rows, q if q is None else (q,), sq, hq, (k,), sk, (v,), sv,
+                                     rope, q_out if q is None else (q_out,), so,
+                                     _here(stream, cache.err, pos, slots, q, k, v, q_out))
+    _check(st, "sm_kv_write_rotary")
+
+
+class Norm:
+    """A norm for block_norm: its kind ("rms" or "layer"), epsilon and [d]
+    tensors (None: 1, 0), which it keeps."""
+
+    def __init__(self, kind: str = "rms", gain=None, bias=None, eps: float = 1e-5):
+        if kind not in NORM_KINDS:
+            raise SpanMergeError(f"unknown norm: {kind!r}")
+        self.gain, self.bias = gain, bias
+        self.packed = bytes(NormParams(NORM_KINDS[kind], eps, _ptr(gain), _ptr(bias)))
+
+    def look(self, dtype, d: int, name: str):
+        for t in (self.gain, self.bias):
+            if t is not None and (t.dtype is not dtype or t.numel() != d):
+                raise SpanMergeError(f"{name}: expected {d} values of {dtype}, got {t.numel()} of {t.dtype}")
+
+
+def norm_params(kind: str = "rms", gain=None, bias=None, eps: float = 1e-5) -> Norm:
+    return Norm(kind, gain, bias, eps)
+
+
+def block_norm(h, y, h_out, n_out, post: Optional[Norm] = None, gate=None, scale: float = 1.0,
+               pre: Optional[Norm] = None, stream=None):
+    """h_out = h + scale * gate * post(y), n_out = pre(h_out) of the unrounded
+    sum; [rows, d] with contiguous rows.  y None: h alone; gate [d] or
+    [rows, d]; h_out or n_out may be None, or an input itself."""
+    (rows, d), dt = h.shape, h.dtype
+    sh = _row_stride(h, dt, rows, (d,), "h")
+    sy = 0 if y is None else _row_stride(y, dt, rows, (d,), "y")
+    sho = 0 if h_out is None else _row_stride(h_out, dt, rows, (d,), "h_out")
+    sno = 0 if n_out is None else _row_stride(n_out, dt, rows, (d,), "n_out")
+    sg = 0
+    if gate is not None:
+        if gate.dim() == 1:
+            _row_stride(gate.unsqueeze(0), dt, 1, (d,), "gate")
+        else:
+            sg = _row_stride(gate, dt, rows, (d,), "gate")
+    at = [h, y, gate, h_out, n_out]
+    for norm, name in ((post, "post"), (pre, "pre")):
+        if norm is not None:
+            norm.look(dt, d, name)
+            at += (norm.gain, norm.bias)
+    one = lambda t: None if t is None else (t,)   # noqa: E731
+    st = _calls().sm_block_norm((h,), sh, one(y), sy, rows, d, None if post is None else post.packed, one(gate), sg, scale,
+                                None if pre is None else pre.packed, dtype_code(dt), one(h_out), sho, one(n_out), sno,
+                                _here(stream, *at))
+    _check(st, "sm_block_norm")
+
+
+def token_logprobs_workspace_bytes(rows: int, vocab: int, k: int) -> int:
+    return load().sm_token_logprobs_workspace_bytes(rows, vocab, k)
+
+
+def token_logprobs(logits, tokens, logprob, entropy, top_ids, top_logprobs, ws, scale: float = 1.0, err=None, stream=None):
+    """Log probability of tokens[r], entropy and the k = top_ids.shape[1]
+    largest logits of each row of logits [rows, vocab] (contiguous rows);
+    scale = 1 / temperature.  Each output may be None."""
+    rows, vocab = logits.shape
+    dt, f32, i32 = logits.dtype, torch.float32, torch.int32
+    sl = _row_stride(logits, dt, rows, (vocab,), "logits")
+    k = 0
+    if tokens is not None:
+        _need(tokens, i32, rows, "tokens")
+    if logprob is not None:
+        _need(logprob, f32, rows, "logprob")
+    if entropy is not None:
+        _need(entropy, f32, rows, "entropy")
+    if top_ids is not None:
+        k = top_ids.shape[-1] if top_ids.dim() > 1 else 1
+        _need(top_ids, i32, rows * k, "top_ids")
+        if top_logprobs is not None:
+            _need(top_logprobs, f32, rows * k, "top_logprobs")
+    elif top_logprobs is not None and top_logprobs.numel():
+        raise SpanMergeError("top_logprobs without top_ids")
+    if err is not None:
+        _need(err, i32, 1, "err")
+    st = _calls().sm_token_logprobs((logits,), sl, rows, vocab, dtype_code(dt), scale, tokens, logprob, entropy, k,
+                                    top_ids, top_logprobs, ws, ws.nbytes, err,
+                                    _here(stream, logits, tokens, logprob, entropy, top_ids, top_logprobs, ws, err))
+    _check(st, "sm_token_logprobs")

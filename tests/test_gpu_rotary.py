@@ -1,0 +1,320 @@
+"""Rotary positions, and the rotated K/V write, against the formula in 64 bits."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from gpu_util import dev, i32, say
+from paper_2609_27233_amd import lib as sm
+
+pytestmark = pytest.mark.gpu
+
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def frequencies(R, theta=500000.0, scaling=None, factor=1.0, low=1.0, high=4.0, context=8192, **_):
+    j = torch.arange(R // 2, dtype=torch.float64)
+    w = theta ** (-2 * j / R)
+    if scaling == "linear":
+        return w / factor
+    if scaling == "bands":
+        u = ((context * w / (2 * math.pi) - low) / (high - low)).clamp(0, 1)
+        return u * w + (1 - u) * w / factor
+    if scaling == "ramp":
+        at = lambda t: R * math.log(context / (2 * math.pi * t)) / (2 * math.log(theta))     # noqa: E731
+        j0, j1 = max(math.floor(at(high)), 0), min(math.ceil(at(low)), R - 1)
+        v = ((j - j0) / max(j1 - j0, 0.001)).clamp(0, 1)
+        return v * w / factor + (1 - v) * w
+    return w
+
+
+def turned(x, pos, a, transpose=False):
+    """(the rotation of x [rows, H, D] in 64 bits, what rounding to fp32 may move it by)"""
+    # (theta and the other numbers reach the library as floats)
+    a = {k: float(np.float32(v)) if isinstance(v, float) else v for k, v in a.items()}
+    R, f = a["rot_dim"], a.get("attn_scale", 1.0)
+    ang = pos.double().cpu()[:, None, None] * frequencies(R, **{k: v for k, v in a.items() if k != "rot_dim"})
+    c, s = f * ang.cos(), f * ang.sin() * (-1 if transpose else 1)
+    x = x.double().cpu()
+    out, slack = x.clone(), torch.zeros_like(x)
+    if a.get("layout", "half") == "half":
+        i0, i1 = slice(0, R // 2), slice(R // 2, R)
+    else:
+        i0, i1 = slice(0, R, 2), slice(1, R, 2)
+    u, v = x[..., i0], x[..., i1]
+    out[..., i0], out[..., i1] = u * c - v * s, u * s + v * c
+    # The angle in turns is rounded to fp32 once reduced to half a turn (off by
+    # 2^-25 x pi), its sine and cosine to 2 ulp (2^-23): 2.2e-7; scaling them,
+    # two products and a sum add 4 x 2^-24 of the terms.  In all below 5e-7 (|u| + |v|) f.
+    slack[..., i0] = slack[..., i1] = 5e-7 * (u.abs() + v.abs()) * abs(f)
+    return out, slack
+
+
+def assert_near(got, ref, slack, dt):
+    got = got.double().cpu()
+    # rounding to the type: half a step of the value
+    tol = slack + torch.finfo(dt).eps / 2 * (ref.abs() + slack)
+    over = (got - ref).abs() - tol
+    assert not got.isnan().any() and float(over.max()) <= 0, (float(over.max()), int((over > 0).sum()))
+
+
+def _rand(shape, dt, seed):
+    g = torch.Generator().manual_seed(seed)
+    return torch.randn(shape, generator=g).to(dt).to(dev())
+
+
+ROTATIONS = [
+    dict(),
+    dict(layout="interleaved"),
+    dict(scaling="linear", factor=4.0),
+    dict(scaling="bands", factor=8.0, low=1.0, high=4.0, context=8192),
+    dict(scaling="ramp", factor=16.0, low=1.0, high=32.0, context=4096, theta=10000.0, attn_scale=1.277, layout="interleaved"),
+    dict(scaling="ramp", factor=2.0, low=1.0, high=1.0001, context=1e9, theta=10.0),     # an empty ramp
+    dict(theta=1.0),
+    dict(attn_scale=-0.5),
+]
+SHAPES = [
+    # rows, heads, D, R
+    (1, 1, 2, 2), (1, 32, 128, 128), (3, 8, 128, 64), (17, 5, 64, 64), (16, 4, 80, 32), (15, 3, 72, 18), (130, 2, 256, 256),
+    (5, 7, 96, 96), (33, 1, 128, 2), (2, 1024, 64, 64), (1000, 3, 33, 20),
+]
+
+
+@pytest.mark.parametrize("dt", [BF, F32], ids=str)
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_rotary_matches_formula(dt, shape):
+    rows, heads, D, R = shape
+    for k, rot in enumerate(ROTATIONS):
+        a = dict(rot_dim=R, **rot)
+        x = _rand((rows, heads, D), dt, 10 * rows + k)
+        pos = torch.randint(0, 9000, (rows,), generator=torch.Generator().manual_seed(k)).int()
+        out = torch.full_like(x, float("nan"))
+        say("rotary", dt, shape, rot)
+        sm.rotary(x, pos.to(dev()), sm.rope_params(**a), out, transpose=k % 2 == 1)
+        assert_near(out, *turned(x, pos, a, k % 2 == 1), dt)
+        rest = out[..., R:]
+        assert torch.equal(rest, x[..., R:])
+
+
+@pytest.mark.parametrize("dt", [BF, F32], ids=str)
+def test_far_and_negative_positions(dt):
+    pos = torch.tensor([0, 1, -1, 131071, 1 << 20, -(1 << 20), 2 ** 31 - 1, -2 ** 31], dtype=torch.int32)
+    for layout in ("half", "interleaved"):
+        a = dict(rot_dim=64, layout=layout, theta=10000.0)
+        x = _rand((8, 3, 128), dt, 5)
+        out = torch.full_like(x, float("nan"))
+        say("rotary far", dt, layout)
+        sm.rotary(x, pos.to(dev()), sm.rope_params(**a), out)
+        ref, slack = turned(x, pos, a)
+        # In units of 2^-53 x 2^31 rad = 2^-22 at the farthest position: the library's frequency exp(-a) / 2 pi with
+        # a = 2 j ln(theta) / rot_dim is off by 2.5 a exp(-a) < 1 (a's roundings), 2 (exp) and 2 (2 pi and the division),
+        # its product with the position by 1; here the power and the product are off by 1 each.  8 in all, of a pair whose
+        # length is at most sqrt(2) times the largest feature: 12.
+        assert_near(out, ref, slack + 12 * 2.0 ** -22 * x.double().cpu().abs().amax(), dt)
+
+
+def test_transposed_is_the_gradient():
+    """<G, d out> = <transposed(G), d x> for the linear map: by the formula's autograd and by differences."""
+    a = dict(rot_dim=48, layout="half", scaling="linear", factor=2.0, attn_scale=1.3)
+    x, G = _rand((9, 2, 64), F32, 1), _rand((9, 2, 64), F32, 2)
+    pos = torch.arange(9, dtype=torch.int32) * 37
+    back = torch.empty_like(G)
+    p = sm.rope_params(**a)
+    sm.rotary(G, pos.to(dev()), p, back, transpose=True)
+    xr = x.double().cpu().requires_grad_()
+    R = 48
+    ang = pos.double()[:, None, None] * frequencies(R, scaling="linear", factor=2.0)
+    u, v = xr[..., :24], xr[..., 24:48]
+    f = float(np.float32(1.3))
+    out = torch.cat([f * (u * ang.cos() - v * ang.sin()), f * (u * ang.sin() + v * ang.cos()), xr[..., 48:]], -1)
+    (out * G.double().cpu()).sum().backward()
+    _, slack = turned(G, pos, a, True)
+    assert_near(back, xr.grad, slack, F32)
+    # differences: the map is linear, so any step gives the slope exactly up to rounding
+    d = _rand((9, 2, 64), F32, 3)
+    fwd = [torch.empty_like(x) for _ in range(2)]
+    for t, o in zip((x, x + d), fwd):
+        sm.rotary(t, pos.to(dev()), p, o)
+    lhs = float((G.double() * (fwd[1].double() - fwd[0].double())).sum())
+    rhs = float((back.double() * ((x + d).double() - x.double())).sum())
+    # each of 9 x 2 x 64 terms off by at most 1e-6 (|x| + |x + d|) |G| < 1e-6 x 12 x 5
+    assert abs(lhs - rhs) <= 1152 * 6e-5
+
+
+@pytest.mark.parametrize("dt", [BF, F32], ids=str)
+@pytest.mark.parametrize("shift", [0, 8, 1, 3])
+def test_strides_alignment_and_in_place(dt, shift):
+    """Column ranges of a wider buffer at any element, in place; nothing beside them is touched."""
+    rows, heads, D = 21, 3, 64
+    a = dict(rot_dim=32, layout="interleaved" if shift & 1 else "half")
+    buf = _rand((rows, 304), dt, shift)
+    before = buf.clone()
+    x = buf[:, 40 + shift:40 + shift + heads * D].view(rows, heads, D)
+    pos = torch.arange(rows, dtype=torch.int32).flip(0)
+    ref, slack = turned(x, pos, a)
+    sm.rotary(x, pos.to(dev()), sm.rope_params(**a), x)
+    assert_near(x, ref, slack, dt)
+    keep = torch.ones(304, dtype=torch.bool)
+    keep[40 + shift:40 + shift + heads * D] = False
+    assert torch.equal(buf[:, keep], before[:, keep])
+
+
+def test_nothing_to_turn_and_special_values():
+    x = torch.empty((0, 4, 64), device=dev())
+    sm.rotary(x, i32([]), sm.rope_params(64), torch.empty_like(x))
+    y = torch.zeros((2, 1, 64), device=dev())
+    y[0, 0, 3], y[1, 0, 63] = float("inf"), float("nan")
+    out = torch.zeros_like(y)
+    sm.rotary(y, i32([5, 5]), sm.rope_params(32), out)
+    torch.cuda.synchronize()
+    bad = ~out.isfinite()
+    assert bad[0].nonzero()[:, 1].tolist() == [3, 19]            # the pair of feature 3, nothing else
+    assert bad[1].nonzero()[:, 1].tolist() == [63]               # behind the turned part: copied
+    assert out[1, 0, 63].isnan()
+
+
+# --------------------------------------------------------------------------
+# the rotated K/V write
+
+def _cache(dt, H, D, bs, nb):
+    c = sm.PagedCache(dtype=dt, num_kv_heads=H, head_dim=D, block_size=bs, num_blocks=nb, max_seqs=4, max_blocks_per_seq=nb)
+    c.k_pool.copy_(_rand(c.k_pool.shape, dt, 100))
+    c.v_pool.copy_(_rand(c.v_pool.shape, dt, 101))
+    return c
+
+
+def _runs(rng, total, bs, lens):
+    """Slots of sequences that start anywhere in their pages and run over pages in any order."""
+    pages = rng.permutation(total)
+    slots, at = [], 0
+    for n in lens:
+        off = int(rng.randint(bs))
+        need = -(-(off + n) // bs)
+        p = off + np.arange(n)
+        slots.append(pages[at + p // bs] * bs + p % bs)
+        at += need
+    assert at <= total
+    return np.concatenate(slots) if slots else np.zeros(0, int)
+
+
+WRITES = [
+    # dtype, Hq, Hkv, D, bs, rows of each sequence, padded rows, kind of slots
+    (BF, 32, 8, 128, 16, [1] * 16, 0, "runs"),
+    (BF, 28, 4, 128, 16, [1], 0, "runs"),
+    (BF, 32, 8, 128, 16, [100, 3, 17, 64], 5, "runs"),
+    (BF, 4, 1, 64, 64, [200, 1, 1, 90], 0, "runs"),
+    (BF, 0, 2, 64, 32, [33, 40], 3, "runs"),                    # K and V alone
+    (BF, 8, 8, 128, 512, [600, 30], 0, "runs"),
+    (F32, 4, 4, 64, 16, [77, 5, 1, 16], 9, "runs"),
+    (F32, 3, 2, 128, 32, [50], 0, "runs"),                      # heads that no group divides
+    (BF, 4, 2, 64, 16, [90], 0, "any"),                         # slots in any order
+    (BF, 4, 2, 64, 16, [90], 0, "down"),                        # counted down
+    (F32, 4, 2, 64, 16, [50], 20, "holes"),                     # padded rows between the others
+    (BF, 2, 2, 64, 16, [300], 40, "holes"),
+    (BF, 2, 1, 128, 16, [700], 0, "runs"),
+    (BF, 32, 8, 128, 16, [2000, 2001, 1999], 0, "runs"),
+]
+
+
+@pytest.mark.parametrize("packed", [True, False])
+@pytest.mark.parametrize("case", range(len(WRITES)))
+def test_write_matches_formula(case, packed):
+    dt, Hq, Hkv, D, bs, lens, pad, kind = WRITES[case]
+    rng = np.random.RandomState(case)
+    nb = sum(-(-x // bs) + 1 for x in lens) + 2
+    c = _cache(dt, Hkv, D, bs, nb)
+    n = sum(lens)
+    slots = _runs(rng, nb, bs, lens)
+    if kind == "any":
+        slots = rng.permutation(nb * bs)[:n]
+    if kind == "down":
+        slots = nb * bs - 1 - np.arange(n)
+    slots = np.concatenate([slots, np.full(pad, -1)])
+    if kind == "holes":
+        order = np.sort(np.concatenate([np.arange(n), rng.choice(n, pad)]), kind="stable")
+        slots = slots[:n][order]
+        slots[1:][order[1:] == order[:-1]] = -1                  # each repeat becomes a hole
+    rows = len(slots)
+    pos = torch.from_numpy(rng.randint(0, 40000, rows).astype(np.int32))
+    a = dict(rot_dim=D if case % 3 else D // 2, layout="interleaved" if case % 2 else "half", scaling="bands", factor=8.0)
+    if packed:
+        buf = _rand((rows, (Hq + 2 * Hkv) * D), dt, case)
+        q, k, v = (t.unflatten(1, (-1, D)) for t in buf.split([Hq * D, Hkv * D, Hkv * D], 1))
+    else:
+        q, k, v = (_rand((rows, h, D), dt, 3 * case + i) for i, h in enumerate((Hq, Hkv, Hkv)))
+    k0, v0 = c.k_pool.double().cpu(), c.v_pool.double().cpu()
+    say("write", case, "packed", packed, "rows", rows)
+    q_out = torch.full((rows, Hq, D), float("nan"), dtype=dt, device=dev()) if Hq else None
+    sm.kv_write_rotary(c, pos.to(dev()), i32(slots), q if Hq else None, k, v, sm.rope_params(**a), q_out)
+    torch.cuda.synchronize()
+    assert c.error_bits() == 0
+    if Hq:
+        assert_near(q_out, *turned(q, pos, a), dt)
+    ref, slack = turned(k, pos, a)
+    sk = torch.zeros_like(k0)
+    for r, s in enumerate(slots):
+        if s >= 0:
+            k0[s // bs, :, s % bs], sk[s // bs, :, s % bs] = ref[r], slack[r]
+            v0[s // bs, :, :, s % bs] = v[r].double().cpu()
+    written = torch.zeros(nb * bs, dtype=torch.bool)
+    written[torch.from_numpy(slots[slots >= 0].astype(np.int64))] = True
+    untouched = ~written.view(nb, 1, bs, 1).expand_as(k0)
+    assert torch.equal(c.k_pool.double().cpu()[untouched], k0[untouched])
+    assert torch.equal(c.v_pool.double().cpu(), v0)
+    assert_near(c.k_pool, k0, sk, dt)
+
+
+def test_write_unaligned_columns_and_in_place_q():
+    dt, Hq, Hkv, D, bs = BF, 2, 1, 64, 16
+    c = _cache(dt, Hkv, D, bs, 4)
+    buf = _rand((37, 400), dt, 8)
+    q, k, v = buf[:, 1:129].view(37, 2, D), buf[:, 131:195].view(37, 1, D), buf[:, 203:267].view(37, 1, D)
+    pos = torch.arange(37, dtype=torch.int32)
+    a = dict(rot_dim=64)
+    want_q, want_k = turned(q, pos, a), turned(k, pos, a)
+    sm.kv_write_rotary(c, pos.to(dev()), i32(np.arange(37) + 5), q, k, v, sm.rope_params(**a), q)
+    torch.cuda.synchronize()
+    assert_near(q, *want_q, dt)
+    flat = c.k_pool.permute(0, 2, 1, 3).reshape(64, 1, D)[5:42]
+    assert_near(flat, *want_k, dt)
+    assert torch.equal(c.v_pool.permute(0, 3, 1, 2).reshape(64, 1, D)[5:42], v)
+
+
+def test_slots_out_of_range_are_refused_alone():
+    c = _cache(BF, 2, 64, 16, 4)
+    before = c.k_pool.clone(), c.v_pool.clone()
+    n = 20
+    q, k, v = (_rand((n, 2, 64), BF, i) for i in range(3))
+    pos, slots = torch.zeros(n, dtype=torch.int32), np.arange(n) + 8
+    slots[[2, 11, 19]] = [64, -2, 2 ** 31 - 1]
+    q_out = torch.zeros_like(q)
+    sm.kv_write_rotary(c, pos.to(dev()), i32(slots), q, k, v, sm.rope_params(64), q_out)
+    torch.cuda.synchronize()
+    assert c.error_bits() == sm.ERR_EINVAL
+    assert torch.equal(q_out, q)                                 # position 0: q as it is
+    kf, vf = before[0].permute(0, 2, 1, 3).reshape(64, 2, 64), before[1].permute(0, 3, 1, 2).reshape(64, 2, 64)
+    for r, s in enumerate(slots):
+        if 0 <= s < 64:
+            kf[s], vf[s] = k[r], v[r]
+    assert torch.equal(c.k_pool.permute(0, 2, 1, 3).reshape(64, 2, 64), kf)
+    assert torch.equal(c.v_pool.permute(0, 3, 1, 2).reshape(64, 2, 64), vf)
+
+
+def test_write_equals_append():
+    """Rows written by reserved slots without rotation (position 0 turns nothing): kv_append's pages."""
+    rng = np.random.RandomState(4)
+    kw = dict(dtype=BF, num_kv_heads=2, head_dim=64, block_size=16, num_blocks=40, max_seqs=3, max_blocks_per_seq=20,
+              free_order=rng.permutation(40))
+    a, b = sm.PagedCache(**kw), sm.PagedCache(**kw)
+    for rows in ([5, 100, 0], [30, 1, 17], [1, 1, 1]):
+        n = sum(rows)
+        k, v = _rand((n, 2, 64), BF, n), _rand((n, 2, 64), BF, n + 1)
+        ro, pos, slots = (torch.empty(m, dtype=torch.int32, device=dev()) for m in (4, n, n))
+        sm.kv_reserve(a, i32([2, 0, 1]), i32(rows), ro, pos, slots)
+        sm.kv_write_rotary(a, torch.zeros_like(pos), slots, None, k, v, sm.rope_params(64), None)
+        sm.kv_append(b, i32([2, 0, 1]), ro, k, v, total_rows=n)
+    torch.cuda.synchronize()
+    assert a.error_bits() == 0 and b.error_bits() == 0
+    for name in ("k_pool", "v_pool", "block_table", "lengths", "free_top"):
+        assert torch.equal(getattr(a, name), getattr(b, name)), name
