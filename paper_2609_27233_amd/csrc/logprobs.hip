@@ -1,18 +1,40 @@
 // Log probabilities of given tokens, entropy and top alternatives of rows of
-// logits (gfx950).
+// logits (gfx950), in one pass over the logits.
 //
-// With z = scale x, m = max z and S = sum exp(z - m):
-//   log p_v = z_v - m - log S,   entropy = log S - sum (z - m) exp(z - m) / S.
+// With a reference r and d = x - r:
+//   S = sum exp(scale d), E = sum d exp(scale d),
+//   log p_v = scale d_v - log S,   entropy = log S - scale E / S.
+// r is the maximum of the workgroup's first chunk, and moves only when a later
+// logit is 2^kLift times as probable, so that the loop rescales nothing: 5
+// instructions and one exponential a logit.  A logit of -infinity would make
+// E NaN (0 x infinity).  A chunk of either kind is added again, with r moved
+// and d clamped.
+//
 // Alternatives are ordered by one 64-bit key per logit: the value's bits made
 // to ascend with it, then the index counted down, so that no two are equal.
+// The first chunk gives a bound below the k-th largest (a count over the
+// lanes' maxima, bit by bit); a wave keeps what lies above its bound in LDS,
+// and reduces that to its k largest, with a new bound, when it is full.
+//
+// A row is one workgroup's, or for few rows its slices are several ones',
+// joined by the last to arrive at the row's counter.
 #include <cmath>
 
-#include "common.hpp"
+#include "vec16.hpp"
 
 namespace sm {
 
 constexpr int kLpThreads = 256;
+constexpr int kLpWaves = kLpThreads / 64;
+constexpr int kLpUnroll = 4;                                  // 16-byte vectors that a thread holds at a time
+constexpr int kLpChunk = kLpThreads * kLpUnroll;              // vectors of a chunk
+constexpr int kKeep = 640;                                    // keys a wave keeps: SM_MAX_TOP and one vector of each lane
+constexpr int kMostSlices = 64;                               // (one wave reads their sums)
+constexpr int kMostKeys = kLpWaves * kKeep;                   // of all slices of a row
+constexpr int kCounters = 65536 / 4;
 constexpr float kLn2 = 0.69314718055994531f;
+constexpr float kLowest = -3.4028234663852886e38f;
+constexpr float kLift = 4.f;
 
 struct LogprobArgs {
   const void *logits;
@@ -24,55 +46,169 @@ struct LogprobArgs {
   int32_t *top_ids;
   float *top_logprobs;
   int32_t *err;
+  int slices, per_slice;  // per_slice: vectors
+  int *counters;
+  float4 *part_sums;    // [row][slice] {r, S, E}
+  uint64_t *part_keys;  // [row][slice][k], 0 behind the last
 };
 
 // Ascends with x; -0 counts as 0, NaN is below everything.
 __device__ __forceinline__ uint32_t order_of(float x) {
-  if (x != x) return 0;
   const uint32_t b = __float_as_uint(x + 0.f);
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
+__device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o); }
+__device__ __forceinline__ uint64_t key_of(float x, int v) { return (uint64_t)order_of(x) << 32 | (uint32_t)~v; }
 
-__device__ __forceinline__ uint64_t wave_max64(uint64_t v) {
+__device__ __forceinline__ int lanes_below(uint64_t mask) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
+
+// Sums over logits relative to r.
+struct Sums {
+  float r, S, E;
+};
+
+// s relative to another reference
+__device__ __forceinline__ void move_to(Sums &s, float r, float c) {
+  const float d = s.r - r, f = __builtin_amdgcn_exp2f(d * c);
+  s.E = f == 0.f ? 0.f : f * fmaf(s.S, d, s.E);
+  s.S *= f;
+  s.r = r;
+}
+
+// One wave's sums of its lanes'.
+__device__ __forceinline__ Sums wave_sums(Sums s, float c) {
+  move_to(s, wave_max(s.r), c);
+  s.S = wave_sum(s.S);
+  s.E = wave_sum(s.E);
+  return s;
+}
+
+// Largest x in steps of 2^LOW for which at least k of the counted values are x or more.
+template <int LOW, class Count>
+__device__ __forceinline__ uint32_t kth(Count count, int k) {
+  uint32_t x = 0;
+  for (int b = 31; b >= LOW; --b) {
+    const uint32_t y = x | 1u << b;
+    if (count(y) >= k) x = y;
+  }
+  return x;
+}
+
+__device__ __forceinline__ void wave_order() {  // LDS accesses of the wave's lanes, in program order
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
+// The k largest of a wave's n keys (n <= kKeep) to the front of buf, in any
+// order; returns how many there are.  Values below 2^LOW are all alike.
+template <int LOW>
+__device__ __forceinline__ int keep_largest(uint64_t *buf, int n, int k) {
+  if (n <= k) return n;
+  constexpr int NR = kKeep / 64;
+  const int lane = threadIdx.x & 63;
+  wave_order();
+  if (n <= 64) {  // by their ranks: n reads, where the search takes up to 64 counts
+    const uint64_t key = lane < n ? buf[lane] : 0;
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += buf[j] > key;
+    wave_order();
+    if (lane < n && rank < k) buf[rank] = key;
+    wave_order();
+    return k;
+  }
+  uint32_t hi[NR], lo[NR];
+#pragma unroll
+  for (int i = 0; i < NR; ++i) {
+    const uint64_t key = lane + 64 * i < n ? buf[lane + 64 * i] : 0;
+    hi[i] = (uint32_t)(key >> 32);
+    lo[i] = (uint32_t)key;
+  }
+  wave_order();
+  const auto count = [&](auto f) {
+    int cnt = 0;
+#pragma unroll
+    for (int i = 0; i < NR; ++i)
+      if (64 * i < n) cnt += __popcll(__ballot(f(i)));
+    return cnt;
+  };
+  const uint32_t v = kth<LOW>([&](uint32_t x) { return count([&](int i) { return hi[i] >= x; }); }, k);
+  const int above = count([&](int i) { return hi[i] >> LOW > v >> LOW; });
+  const int alike = count([&](int i) { return hi[i] >> LOW == v >> LOW; });
+  uint32_t from = 0;
+  if (above + alike > k)  // the lower indices among the equal ones
+    from = kth<0>([&](uint32_t x) { return count([&](int i) { return hi[i] >> LOW == v >> LOW && lo[i] >= x; }); }, k - above);
+  int at = 0;
+#pragma unroll
+  for (int i = 0; i < NR; ++i)
+    if (64 * i < n) {
+      const bool keep = hi[i] >> LOW > v >> LOW || (hi[i] >> LOW == v >> LOW && lo[i] >= from);
+      const uint64_t mask = __ballot(keep);
+      if (keep) buf[at + lanes_below(mask)] = (uint64_t)hi[i] << 32 | lo[i];
+      at += __popcll(mask);
+    }
+  wave_order();
+  return at;
+}
+
+__device__ __forceinline__ uint64_t wave_min64(uint64_t v) {
 #pragma unroll
   for (int off = 32; off; off >>= 1) {
     const uint64_t u = __shfl_xor(v, off, kWave);
-    v = u > v ? u : v;
+    v = u < v ? u : v;
   }
   return v;
 }
 
+// A wave's candidates and the bound that they lie above.
 template <typename T>
-__global__ __launch_bounds__(kLpThreads) void logprobs_kernel(LogprobArgs a) {
-  __shared__ float red[kLpThreads / 64];
-  __shared__ uint64_t best[kLpThreads / 64];
-  const int t = threadIdx.x;
-  const int64_t r = blockIdx.x;
-  const T *x = (const T *)a.logits + r * a.stride;
-  float m = -INFINITY, odd = 0.f;
-  for (int v = t; v < a.vocab; v += kLpThreads) {
-    const float f = Elem<T>::load(x + v);
-    m = fmaxf(m, f);
-    if (!(f < INFINITY)) odd = 1.f;  // NaN or +infinity
-  }
-  m = block_max(m, red);
-  odd = block_max(odd, red);
-  float S = 0.f, E = 0.f;
-  if (m > -INFINITY)
-    for (int v = t; v < a.vocab; v += kLpThreads) {
-      const float d = (Elem<T>::load(x + v) - m) * a.c, e = __builtin_amdgcn_exp2f(d);
-      S += e;
-      if (e > 0.f) E += e * d;
+struct Candidates {
+  static constexpr int LOW = sizeof(T) == 2 ? 16 : 0;
+  uint64_t *buf;
+  int n, k;
+  uint64_t bound;  // keys above it are wanted
+  float least;     // its value
+
+  // Room for `more` keys (more <= kKeep - SM_MAX_TOP).
+  __device__ __forceinline__ void make_room(int more) {
+    if (n + more <= kKeep) return;
+    n = keep_largest<LOW>(buf, n, k);
+    const int lane = threadIdx.x & 63;
+    const uint64_t b = wave_min64(lane < n ? buf[lane] : ~0ull);
+    if (n == k && b > bound) {
+      bound = b;
+      least = value_of((uint32_t)(b >> 32));
     }
-  S = block_sum(S, red);
-  E = block_sum(E, red);
-  const float log_s = __builtin_amdgcn_logf(S);  // base 2
-  const float nan = __uint_as_float(0x7fc00000u);
+  }
+  __device__ __forceinline__ void offer(float x, int v, bool valid) {
+    bool want = valid && x >= least;  // (no NaN)
+    if (!__ballot(want)) return;
+    const uint64_t key = key_of(x, v);
+    want = want && key > bound;
+    const uint64_t mask = __ballot(want);
+    if (want) buf[n + lanes_below(mask)] = key;
+    n += __popcll(mask);
+  }
+};
+
+// Results of a row by one wave: its sums, and its m best keys in buf.
+template <typename T, bool TOP>
+__device__ void put_row(const LogprobArgs &a, int64_t r, Sums s, const uint64_t *buf, int m) {
+  const int lane = threadIdx.x & 63;
+  const T *x = (const T *)a.logits + r * a.stride;
+  const float log_s = __builtin_amdgcn_logf(s.S) * kLn2;
   auto logprob = [&](float f) {
-    return odd != 0.f ? nan : f == -INFINITY ? -INFINITY : fmaf(f - m, a.scale, -log_s * kLn2);
+    if (s.S == 0.f) return -INFINITY;  // nothing but -infinity
+    const float lp = fmaf(f - s.r, a.scale, -log_s);
+    return lp > 0.f ? 0.f : lp;
   };
-  if (t == 0) {
-    if (a.entropy) a.entropy[r] = odd != 0.f ? nan : S > 0.f ? (log_s - E / S) * kLn2 : 0.f;
+  if (lane == 0) {
+    if (a.entropy) {
+      const float h = s.S == 0.f ? 0.f : fmaf(-a.scale, s.E / s.S, log_s);
+      a.entropy[r] = h < 0.f ? 0.f : h;
+    }
     if (a.logprob) {
       const int tok = a.tokens[r];
       float lp = 0.f;
@@ -81,25 +217,244 @@ __global__ __launch_bounds__(kLpThreads) void logprobs_kernel(LogprobArgs a) {
       a.logprob[r] = lp;
     }
   }
-  uint64_t below = ~0ull;
-  for (int i = 0; i < a.k; ++i) {
-    uint64_t top = 0;
-    for (int v = t; v < a.vocab; v += kLpThreads) {
-      const uint64_t key = (uint64_t)order_of(Elem<T>::load(x + v)) << 32 | (uint32_t)~v;
-      if (key < below && key > top) top = key;
+  if constexpr (TOP) {
+    wave_order();
+    const uint64_t key = lane < m ? buf[lane] : 0;
+    int rank = 0;
+    for (int j = 0; j < m; ++j) rank += buf[j] > key;
+    if (lane < m) {
+      a.top_ids[r * a.k + rank] = (int)~(uint32_t)key;
+      if (a.top_logprobs) a.top_logprobs[r * a.k + rank] = logprob(value_of((uint32_t)(key >> 32)));
     }
-    top = wave_max64(top);
-    __syncthreads();
-    if ((t & 63) == 0) best[t >> 6] = top;
-    __syncthreads();
-    for (int w = 0; w < kLpThreads / 64; ++w) top = best[w] > top ? best[w] : top;
-    below = top;
-    if (t == 0) {
-      const int v = (int)~(uint32_t)top;
-      a.top_ids[r * a.k + i] = v;
-      if (a.top_logprobs) a.top_logprobs[r * a.k + i] = logprob(Elem<T>::load(x + v));
+    for (int v0 = 0; m < a.k && v0 < a.vocab; v0 += 64) {  // fewer numbers than alternatives: NaN follow
+      const float f = v0 + lane < a.vocab ? Elem<T>::load(x + v0 + lane) : 0.f;
+      const uint64_t mask = __ballot(f != f);
+      const int at = m + lanes_below(mask);
+      if (f != f && at < a.k) {
+        a.top_ids[r * a.k + at] = v0 + lane;
+        if (a.top_logprobs) a.top_logprobs[r * a.k + at] = f;
+      }
+      m += __popcll(mask);
     }
   }
+}
+
+template <class V>
+__device__ __forceinline__ void put_shared(V *p, V v) {
+  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <class V>
+__device__ __forceinline__ V get_shared(V *p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+template <typename T, bool TOP>
+__global__ __launch_bounds__(kLpThreads) void logprobs_kernel(LogprobArgs a) {
+  constexpr int N = Vec16<T>::N, LOW = Candidates<T>::LOW;
+  __shared__ uint64_t keys[TOP ? kLpWaves : 1][TOP ? kKeep : 1];
+  __shared__ float w_max[kLpWaves], w_r[kLpWaves], w_S[kLpWaves], w_E[kLpWaves];
+  __shared__ uint32_t w_bound[kLpWaves];
+  __shared__ int w_n[kLpWaves], last;
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+  const int64_t r = blockIdx.x / a.slices;
+  const int slice = blockIdx.x - (int)r * a.slices;
+  const T *x = (const T *)a.logits + r * a.stride;
+  // aligned vectors, and the few logits before and behind them
+  const int head = min((int)((16 - (uintptr_t)x % 16) % 16 / sizeof(T)), a.vocab);
+  const int nvec = (a.vocab - head) / N;
+  const u32x4_t *xv = (const u32x4_t *)(x + head);
+  const int begin = min(slice * a.per_slice, nvec), end = min(begin + a.per_slice, nvec);
+  u32x4_t raw[kLpUnroll];
+  auto load = [&](int v0) {
+#pragma unroll
+    for (int u = 0; u < kLpUnroll; ++u) {
+      const int v = v0 + u * kLpThreads + t;
+      raw[u] = u32x4_t{Vec16<T>::kMinusInf, Vec16<T>::kMinusInf, Vec16<T>::kMinusInf, Vec16<T>::kMinusInf};
+      if (v < end) raw[u] = __builtin_nontemporal_load(xv + v);
+    }
+  };
+  auto largest = [&](const float *f) {
+    float m = f[0];
+#pragma unroll
+    for (int e = 1; e < N; ++e) m = fmaxf(m, f[e]);
+    return m;
+  };
+  Sums s{kLowest, 0.f, 0.f};
+  Candidates<T> top{keys[TOP ? w : 0], 0, a.k, 0, -INFINITY};
+  if (begin < end) {
+    load(begin);
+    float m = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < kLpUnroll; ++u) {
+      float f[N];
+      Vec16<T>::open(raw[u], f);
+      m = fmaxf(m, largest(f));
+    }
+    const float mw = wave_max(m);
+    uint32_t b = 0;
+    if constexpr (TOP) {
+      // k / 4 of each wave's lanes hold a logit of this or more, so k of the row's do
+      const uint32_t o = order_of(m);
+      b = kth<16>([&](uint32_t y) { return __popcll(__ballot(o >= y)); }, (a.k + kLpWaves - 1) / kLpWaves);
+    }
+    if (lane == 0) {
+      w_max[w] = mw;
+      w_bound[w] = b;
+    }
+    __syncthreads();
+    b = w_bound[0];
+#pragma unroll
+    for (int i = 0; i < kLpWaves; ++i) {
+      s.r = fmaxf(s.r, w_max[i]);
+      b = min(b, w_bound[i]);
+    }
+    if constexpr (TOP) {
+      b = max(b, 0x007fffffu);  // (-infinity's)
+      top.bound = (uint64_t)b << 32;
+      top.least = value_of(b);
+    }
+  }
+  auto add = [&](const float *f, bool clamp) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const float d = f[e] - s.r, p = __builtin_amdgcn_exp2f(d * a.c);
+      s.S += p;
+      s.E = fmaf(p, clamp ? fmaxf(d, kLowest) : d, s.E);
+    }
+  };
+  if (slice == 0 && w == 0) {
+    const int rest = a.vocab - head - nvec * N;  // (under two vectors with the head's)
+    const int v = lane < head ? lane : a.vocab - rest + lane - head;
+    float f[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) f[e] = -INFINITY;
+    if (lane < head + rest) f[0] = Elem<T>::load(x + v);
+    const float m = wave_max(f[0]);
+    if ((m - s.r) * a.c > kLift) move_to(s, m, a.c);
+    add(f, true);
+    if constexpr (TOP) {
+      top.offer(f[0], v, lane < head + rest);
+    }
+  }
+  for (int v0 = begin; v0 < end; v0 += kLpChunk) {
+    u32x4_t cur[kLpUnroll];
+#pragma unroll
+    for (int u = 0; u < kLpUnroll; ++u) cur[u] = raw[u];
+    if (v0 + kLpChunk < end) load(v0 + kLpChunk);
+    const Sums before = s;
+    float m[kLpUnroll], all = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < kLpUnroll; ++u) {
+      float f[N];
+      Vec16<T>::open(cur[u], f);
+      m[u] = largest(f);
+      all = fmaxf(all, m[u]);
+      add(f, false);
+    }
+    if (__ballot((all - s.r) * a.c > kLift || s.E != s.E)) {
+      s = before;
+      move_to(s, fmaxf(s.r, wave_max(all)), a.c);
+#pragma unroll 1
+      for (int u = 0; u < kLpUnroll; ++u) {
+        float f[N];
+        Vec16<T>::open(u == 0 ? cur[0] : u == 1 ? cur[1] : u == 2 ? cur[2] : cur[3], f);
+        add(f, true);
+      }
+    }
+    if constexpr (TOP) {
+      if (__ballot(all >= top.least)) {
+#pragma unroll 1
+        for (int u = 0; u < kLpUnroll; ++u) {  // (rolled: the code below once)
+          if (!__ballot((u == 0 ? m[0] : u == 1 ? m[1] : u == 2 ? m[2] : m[3]) >= top.least)) continue;
+          float f[N];
+          Vec16<T>::open(u == 0 ? cur[0] : u == 1 ? cur[1] : u == 2 ? cur[2] : cur[3], f);
+          top.make_room(64 * N);
+          const int v = v0 + u * kLpThreads + t;
+#pragma unroll
+          for (int e = 0; e < N; ++e) top.offer(f[e], head + v * N + e, v < end);
+        }
+      }
+    }
+  }
+  // Each wave's results, then the first one's of all waves; for a row of
+  // several slices that twice, the second time of the slices' results.
+#pragma unroll 1
+  for (int stage = 0;; ++stage) {
+    if (w == 0 || !(stage & 1)) {
+      s = wave_sums(s, a.c);
+      if constexpr (TOP) top.n = keep_largest<LOW>(top.buf, top.n, a.k);
+    }
+    if (!(stage & 1)) {
+      if (lane == 0) {
+        w_r[w] = s.r;
+        w_S[w] = s.S;
+        w_E[w] = s.E;
+        w_n[w] = top.n;
+      }
+      __syncthreads();
+      if (w == 0) {
+        s = Sums{lane < kLpWaves ? w_r[lane] : kLowest, lane < kLpWaves ? w_S[lane] : 0.f,
+                 lane < kLpWaves ? w_E[lane] : 0.f};
+        if constexpr (TOP)
+          for (int i = 1; i < kLpWaves; ++i) {
+            const int n = w_n[i];
+            if (lane < n) top.buf[top.n + lane] = keys[i][lane];
+            top.n += n;
+          }
+      }
+      continue;
+    }
+    if (stage == 3 || a.slices == 1) {
+      if (w == 0) put_row<T, TOP>(a, r, s, top.buf, top.n);
+      return;
+    }
+    if (w == 0) {
+      float *ps = (float *)(a.part_sums + r * a.slices + slice);
+      if (lane < 3) put_shared(ps + lane, lane == 0 ? s.r : lane == 1 ? s.S : s.E);
+      if constexpr (TOP) {
+        if (lane < a.k) put_shared(a.part_keys + (r * a.slices + slice) * a.k + lane, lane < top.n ? top.buf[lane] : 0);
+      }
+      __builtin_amdgcn_s_waitcnt(0);  // in before the arrival counts
+      if (lane == 0)
+        last = __hip_atomic_fetch_add(a.counters + r, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.slices - 1;
+    }
+    __syncthreads();
+    if (!last) return;
+    if (t == 0) put_shared(a.counters + r, 0);
+    s = Sums{kLowest, 0.f, 0.f};
+    top.n = 0;
+    if (t < a.slices) {
+      float *ps = (float *)(a.part_sums + r * a.slices + t);
+      s = Sums{get_shared(ps), get_shared(ps + 1), get_shared(ps + 2)};
+    }
+    if constexpr (TOP) {
+      uint64_t *pk = a.part_keys + r * a.slices * a.k;
+      for (int i = t - lane; i < a.slices * a.k; i += kLpThreads) {  // (kMostKeys: they fit)
+        const uint64_t key = i + lane < a.slices * a.k ? get_shared(pk + i + lane) : 0;
+        const uint64_t mask = __ballot(key != 0);
+        if (key != 0) top.buf[top.n + lanes_below(mask)] = key;
+        top.n += __popcll(mask);
+      }
+    }
+  }
+}
+
+struct LogprobPlan {
+  int slices, per_slice;
+};
+
+// Slices of a row: while there are fewer workgroups than kLpFill, a row is
+// cut into chunks.
+constexpr int kLpFill = 1024;
+
+static LogprobPlan plan_logprobs(int rows, int vocab, int k) {
+  const int nvec = (vocab + 3) / 4;  // (of fp32; bf16 rows have half as many)
+  int slices = rows > 0 && rows < kLpFill && rows <= kCounters ? (kLpFill + rows - 1) / rows : 1;
+  const int chunks = (nvec + kLpChunk - 1) / kLpChunk;
+  slices = slices < chunks ? slices : chunks;
+  slices = slices < kMostSlices ? slices : kMostSlices;
+  if (k > 0 && slices > kMostKeys / k) slices = kMostKeys / k;
+  return LogprobPlan{slices < 1 ? 1 : slices, 0};
 }
 
 }  // namespace sm
@@ -108,7 +463,8 @@ using namespace sm;
 
 SM_API size_t sm_token_logprobs_workspace_bytes(int rows, int vocab, int k) {
   if (rows < 0 || vocab < 1 || k < 0 || k > SM_MAX_TOP || k > vocab) return 0;
-  return 65536;
+  const LogprobPlan p = plan_logprobs(rows, vocab, k);
+  return 65536 + (p.slices > 1 ? (size_t)rows * p.slices * (16 + 8 * (size_t)k) : 0);
 }
 
 SM_API sm_status sm_token_logprobs(const void *logits, int64_t stride, int rows, int vocab, sm_dtype dt, float scale,
@@ -120,11 +476,17 @@ SM_API sm_status sm_token_logprobs(const void *logits, int64_t stride, int rows,
   if (rows == 0) return SM_OK;
   if (!logits || (logprob && !tokens) || (k > 0 && !top_ids) || (uintptr_t)ws % 16 != 0) return SM_EINVAL;
   if (!ws || ws_bytes < sm_token_logprobs_workspace_bytes(rows, vocab, k)) return SM_EINVAL;
-  const LogprobArgs a{logits, stride, rows, vocab, k, scale, c, tokens, logprob, entropy, top_ids,
-                      top_logprobs, err};
-  if (dt == SM_BF16)
-    hipLaunchKernelGGL(logprobs_kernel<uint16_t>, dim3(rows), dim3(kLpThreads), 0, stream, a);
-  else
-    hipLaunchKernelGGL(logprobs_kernel<float>, dim3(rows), dim3(kLpThreads), 0, stream, a);
+  const int n = dt == SM_BF16 ? 8 : 4;
+  LogprobPlan p = plan_logprobs(rows, vocab, k);
+  const int nvec = (vocab + n - 1) / n, chunks = (nvec + kLpChunk - 1) / kLpChunk;
+  p.per_slice = (chunks + p.slices - 1) / p.slices * kLpChunk;
+  p.slices = (nvec + p.per_slice - 1) / p.per_slice;
+  float4 *sums = (float4 *)((char *)ws + 65536);
+  const LogprobArgs a{logits, stride, rows, vocab, k, scale, c, tokens, logprob, entropy, top_ids, top_logprobs, err,
+                      p.slices, p.per_slice, (int *)ws, sums, (uint64_t *)(sums + (size_t)rows * p.slices)};
+  const dim3 grid((unsigned)((int64_t)rows * p.slices));
+  const auto kernel = dt == SM_BF16 ? (k ? logprobs_kernel<uint16_t, true> : logprobs_kernel<uint16_t, false>)
+                                    : (k ? logprobs_kernel<float, true> : logprobs_kernel<float, false>);
+  hipLaunchKernelGGL(kernel, grid, dim3(kLpThreads), 0, stream, a);
   return hipGetLastError() == hipSuccess ? SM_OK : SM_EHIP;
 }
