@@ -12,23 +12,26 @@
 //
 // Alternatives are ordered by one 64-bit key per logit: the value's bits made
 // to ascend with it, then the index counted down, so that no two are equal.
-// The first chunk gives a bound below the k-th largest (a count over the
-// lanes' maxima, bit by bit); a wave keeps what lies above its bound in LDS,
-// and reduces that to its k largest, with a new bound, when it is full.
+// Lanes' maxima give a bound below the k-th largest (a count over them, bit by
+// bit), after the first chunk and whenever the chunks seen have doubled.  A
+// wave notes which 16-byte vectors reach the bound, and looks at their logits
+// 64 vectors at a time: keys above the bound go to LDS, where they are reduced
+// to the k largest, with a bound of the wave's own, when there is no room.
 //
-// A row is one workgroup's, or for few rows its slices are several ones',
-// joined by the last to arrive at the row's counter.
+// A row is one workgroup's (of one wave where it is short), or for few rows
+// its slices are several ones', joined by the last to arrive at the row's
+// counter.
 #include <cmath>
 
 #include "vec16.hpp"
 
 namespace sm {
 
-constexpr int kLpThreads = 256;
-constexpr int kLpWaves = kLpThreads / 64;
+constexpr int kLpWaves = 4;                                   // waves of a workgroup, but for short rows
 constexpr int kLpUnroll = 4;                                  // 16-byte vectors that a thread holds at a time
-constexpr int kLpChunk = kLpThreads * kLpUnroll;              // vectors of a chunk
-constexpr int kKeep = 640;                                    // keys a wave keeps: SM_MAX_TOP and one vector of each lane
+constexpr int kLpChunk = 64 * kLpWaves * kLpUnroll;           // vectors that they hold
+constexpr int kKeep = 256;                                    // keys that a wave keeps: SM_MAX_TOP and one of each lane at least
+constexpr int kNoted = 64 + 64 * kLpUnroll;                   // vectors that it has noted: a chunk's, and those before
 constexpr int kMostSlices = 64;                               // (one wave reads their sums)
 constexpr int kMostKeys = kLpWaves * kKeep;                   // of all slices of a row
 constexpr int kCounters = 65536 / 4;
@@ -167,35 +170,69 @@ template <typename T>
 struct Candidates {
   static constexpr int LOW = sizeof(T) == 2 ? 16 : 0;
   uint64_t *buf;
-  int n, k;
+  int *noted;
+  int n, vectors, k;
+  int ordered;     // a bound of an index below this is the lowest index of its value to come
   uint64_t bound;  // keys above it are wanted
-  float least;     // its value
+  float least;     // vectors whose largest is this or more may hold one
 
-  // Room for `more` keys (more <= kKeep - SM_MAX_TOP).
-  __device__ __forceinline__ void make_room(int more) {
-    if (n + more <= kKeep) return;
-    n = keep_largest<LOW>(buf, n, k);
-    const int lane = threadIdx.x & 63;
-    const uint64_t b = wave_min64(lane < n ? buf[lane] : ~0ull);
-    if (n == k && b > bound) {
-      bound = b;
-      least = value_of((uint32_t)(b >> 32));
-    }
+  __device__ __forceinline__ void raise(uint64_t b) {
+    if (b <= bound) return;
+    bound = b;
+    const uint32_t hi = (uint32_t)(b >> 32), lo = (uint32_t)b;
+    least = value_of(lo != 0 && (int)~lo < ordered ? hi + 1 : hi);
   }
-  __device__ __forceinline__ void offer(float x, int v, bool valid) {
-    bool want = valid && x >= least;  // (no NaN)
-    if (!__ballot(want)) return;
+  __device__ __forceinline__ void put(float x, int v, bool valid) {
     const uint64_t key = key_of(x, v);
-    want = want && key > bound;
+    const bool want = valid && x == x && key > bound;
     const uint64_t mask = __ballot(want);
     if (want) buf[n + lanes_below(mask)] = key;
     n += __popcll(mask);
   }
+  __device__ __forceinline__ void note(float m, int v) {
+    const bool want = m >= least;
+    const uint64_t mask = __ballot(want);
+    if (want) noted[vectors + lanes_below(mask)] = v;
+    vectors += __popcll(mask);
+  }
+  // The noted vectors' logits; vector v of x begins at logit head + N v.
+  __device__ __forceinline__ void look(const u32x4_t *x, int head, int end) {
+    constexpr int N = Vec16<T>::N;
+    const int lane = threadIdx.x & 63;
+    wave_order();
+#pragma unroll 1
+    for (int i = 0; i < vectors; i += 64) {
+      int v = i + lane < vectors ? noted[i + lane] : end;
+      const bool valid = v < end;  // (behind the slice there are none)
+      v = valid ? v : 0;
+      u32x4_t w{0, 0, 0, 0};
+      if (valid) w = x[v];
+#pragma unroll 1
+      for (int e = 0; e < N; ++e) {
+        if (n > kKeep - 64) {
+          n = keep_largest<LOW>(buf, n, k);
+          if (n == k) raise(wave_min64(lane < n ? buf[lane] : ~0ull));
+        }
+        float f;
+        if constexpr (sizeof(T) == 2) {
+          f = __uint_as_float(w[0] << 16);
+          w = u32x4_t{w[0] >> 16 | w[1] << 16, w[1] >> 16 | w[2] << 16, w[2] >> 16 | w[3] << 16, w[3] >> 16};
+        } else {
+          f = __uint_as_float(w[0]);
+          w = u32x4_t{w[1], w[2], w[3], 0};
+        }
+        put(f, head + N * v + e, valid);
+      }
+    }
+    vectors = 0;
+  }
 };
 
-// Results of a row by one wave: its sums, and its m best keys in buf.
+// Results of a row by one wave: its sums, its token (-1: none) with the
+// token's logit, and its m best keys in buf.
 template <typename T, bool TOP>
-__device__ void put_row(const LogprobArgs &a, int64_t r, Sums s, const uint64_t *buf, int m) {
+__device__ __forceinline__ void put_row(const LogprobArgs &a, int64_t r, Sums s, int tok, float x_tok, const uint64_t *buf,
+                                        int m) {
   const int lane = threadIdx.x & 63;
   const T *x = (const T *)a.logits + r * a.stride;
   const float log_s = __builtin_amdgcn_logf(s.S) * kLn2;
@@ -210,11 +247,8 @@ __device__ void put_row(const LogprobArgs &a, int64_t r, Sums s, const uint64_t 
       a.entropy[r] = h < 0.f ? 0.f : h;
     }
     if (a.logprob) {
-      const int tok = a.tokens[r];
-      float lp = 0.f;
-      if (tok >= 0 && tok < a.vocab) lp = logprob(Elem<T>::load(x + tok));
-      else if (tok != -1 && a.err) set_err(a.err, SM_ERR_EINVAL);
-      a.logprob[r] = lp;
+      a.logprob[r] = tok >= 0 && tok < a.vocab ? logprob(x_tok) : 0.f;
+      if ((tok < -1 || tok >= a.vocab) && a.err) set_err(a.err, SM_ERR_EINVAL);
     }
   }
   if constexpr (TOP) {
@@ -248,13 +282,15 @@ __device__ __forceinline__ V get_shared(V *p) {
   return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-template <typename T, bool TOP>
-__global__ __launch_bounds__(kLpThreads) void logprobs_kernel(LogprobArgs a) {
-  constexpr int N = Vec16<T>::N, LOW = Candidates<T>::LOW;
-  __shared__ uint64_t keys[TOP ? kLpWaves : 1][TOP ? kKeep : 1];
-  __shared__ float w_max[kLpWaves], w_r[kLpWaves], w_S[kLpWaves], w_E[kLpWaves];
-  __shared__ uint32_t w_bound[kLpWaves];
-  __shared__ int w_n[kLpWaves], last;
+// W waves to a workgroup.
+template <typename T, bool TOP, int W>
+__global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs a) {
+  constexpr int N = Vec16<T>::N, LOW = Candidates<T>::LOW, THREADS = 64 * W, CHUNK = THREADS * kLpUnroll;
+  __shared__ uint64_t keys[TOP ? W : 1][TOP ? kKeep : 1];
+  __shared__ int noted[TOP ? W : 1][TOP ? kNoted : 1];
+  __shared__ float w_max[W], w_r[W], w_S[W], w_E[W];
+  __shared__ uint32_t w_bound[W];
+  __shared__ int w_n[W], last;
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
   const int64_t r = blockIdx.x / a.slices;
   const int slice = blockIdx.x - (int)r * a.slices;
@@ -264,13 +300,19 @@ __global__ __launch_bounds__(kLpThreads) void logprobs_kernel(LogprobArgs a) {
   const int nvec = (a.vocab - head) / N;
   const u32x4_t *xv = (const u32x4_t *)(x + head);
   const int begin = min(slice * a.per_slice, nvec), end = min(begin + a.per_slice, nvec);
-  u32x4_t raw[kLpUnroll];
+  // the chunk at v0: -infinity behind the slice's end
+  u32x4_t cur[kLpUnroll];
   auto load = [&](int v0) {
+    if (v0 + CHUNK <= end) {
 #pragma unroll
-    for (int u = 0; u < kLpUnroll; ++u) {
-      const int v = v0 + u * kLpThreads + t;
-      raw[u] = u32x4_t{Vec16<T>::kMinusInf, Vec16<T>::kMinusInf, Vec16<T>::kMinusInf, Vec16<T>::kMinusInf};
-      if (v < end) raw[u] = __builtin_nontemporal_load(xv + v);
+      for (int u = 0; u < kLpUnroll; ++u) cur[u] = __builtin_nontemporal_load(xv + v0 + u * THREADS + t);
+    } else {
+#pragma unroll
+      for (int u = 0; u < kLpUnroll; ++u) {
+        const int v = v0 + u * THREADS + t;
+        cur[u] = u32x4_t{Vec16<T>::kMinusInf, Vec16<T>::kMinusInf, Vec16<T>::kMinusInf, Vec16<T>::kMinusInf};
+        if (v < end) cur[u] = __builtin_nontemporal_load(xv + v);
+      }
     }
   };
   auto largest = [&](const float *f) {
@@ -280,39 +322,48 @@ __global__ __launch_bounds__(kLpThreads) void logprobs_kernel(LogprobArgs a) {
     return m;
   };
   Sums s{kLowest, 0.f, 0.f};
-  Candidates<T> top{keys[TOP ? w : 0], 0, a.k, 0, -INFINITY};
+  Candidates<T> top{keys[TOP ? w : 0], noted[TOP ? w : 0], 0, 0, a.k, head + nvec * N, 0, -INFINITY};
+  float best = -INFINITY;  // this lane's largest
+  // A bound below the slice's k-th largest: k / W of each wave's lanes hold
+  // its least one's value or more (few alternatives: k of one wave's lanes).
+  const bool one_wave = a.k < W;
+  auto wave_bound = [&]() {
+    const uint32_t o = order_of(best);
+    return kth<16>([&](uint32_t y) { return __popcll(__ballot(o >= y)); }, one_wave ? a.k : (a.k + W - 1) / W);
+  };
+  auto use_bounds = [&]() {
+    uint32_t b = one_wave ? 0 : ~0u;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      const uint32_t o = __hip_atomic_load(w_bound + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+      b = one_wave ? max(b, o) : min(b, o);
+    }
+    b = max(b, 0x007fffffu);  // (-infinity's)
+    top.raise((uint64_t)b << 32);
+  };
+  // the token's logit, long before it is used
+  const int tok = a.logprob ? a.tokens[r] : -1;
+  float x_tok = 0.f;
+  if (begin < end) load(begin);
+  if (t == 0 && tok >= 0 && tok < a.vocab) x_tok = Elem<T>::load(x + tok);
   if (begin < end) {
-    load(begin);
-    float m = -INFINITY;
 #pragma unroll
     for (int u = 0; u < kLpUnroll; ++u) {
       float f[N];
-      Vec16<T>::open(raw[u], f);
-      m = fmaxf(m, largest(f));
+      Vec16<T>::open(cur[u], f);
+      best = fmaxf(best, largest(f));
     }
-    const float mw = wave_max(m);
+    const float mw = wave_max(best);
     uint32_t b = 0;
-    if constexpr (TOP) {
-      // k / 4 of each wave's lanes hold a logit of this or more, so k of the row's do
-      const uint32_t o = order_of(m);
-      b = kth<16>([&](uint32_t y) { return __popcll(__ballot(o >= y)); }, (a.k + kLpWaves - 1) / kLpWaves);
-    }
+    if constexpr (TOP) b = wave_bound();
     if (lane == 0) {
       w_max[w] = mw;
       w_bound[w] = b;
     }
     __syncthreads();
-    b = w_bound[0];
 #pragma unroll
-    for (int i = 0; i < kLpWaves; ++i) {
-      s.r = fmaxf(s.r, w_max[i]);
-      b = min(b, w_bound[i]);
-    }
-    if constexpr (TOP) {
-      b = max(b, 0x007fffffu);  // (-infinity's)
-      top.bound = (uint64_t)b << 32;
-      top.least = value_of(b);
-    }
+    for (int i = 0; i < W; ++i) s.r = fmaxf(s.r, w_max[i]);
+    if constexpr (TOP) use_bounds();
   }
   auto add = [&](const float *f, bool clamp) {
 #pragma unroll
@@ -332,49 +383,72 @@ __global__ __launch_bounds__(kLpThreads) void logprobs_kernel(LogprobArgs a) {
     const float m = wave_max(f[0]);
     if ((m - s.r) * a.c > kLift) move_to(s, m, a.c);
     add(f, true);
-    if constexpr (TOP) {
-      top.offer(f[0], v, lane < head + rest);
-    }
+    if constexpr (TOP) top.put(f[0], v, lane < head + rest);
   }
-  for (int v0 = begin; v0 < end; v0 += kLpChunk) {
-    u32x4_t cur[kLpUnroll];
+  bool clamp = false;  // whether the slice has shown -infinity
+  for (int v0 = begin, seen = 1;; v0 += CHUNK, ++seen) {
+    const bool more = v0 < end;
+    if (more) {
+      if (v0 != begin) load(v0);  // (no chunk ahead: the other waves' work covers the wait)
+      if (v0 + CHUNK > end && s.r > -1e38f) {
+        // nothing behind the end, by a value of probability 0 (-infinity would have the chunk added again)
 #pragma unroll
-    for (int u = 0; u < kLpUnroll; ++u) cur[u] = raw[u];
-    if (v0 + kLpChunk < end) load(v0 + kLpChunk);
-    const Sums before = s;
-    float m[kLpUnroll], all = -INFINITY;
-#pragma unroll
-    for (int u = 0; u < kLpUnroll; ++u) {
-      float f[N];
-      Vec16<T>::open(cur[u], f);
-      m[u] = largest(f);
-      all = fmaxf(all, m[u]);
-      add(f, false);
-    }
-    if (__ballot((all - s.r) * a.c > kLift || s.E != s.E)) {
-      s = before;
-      move_to(s, fmaxf(s.r, wave_max(all)), a.c);
-#pragma unroll 1
-      for (int u = 0; u < kLpUnroll; ++u) {
-        float f[N];
-        Vec16<T>::open(u == 0 ? cur[0] : u == 1 ? cur[1] : u == 2 ? cur[2] : cur[3], f);
-        add(f, true);
+        for (int u = 0; u < kLpUnroll; ++u)
+          if (v0 + u * THREADS + t >= end)
+            cur[u] = u32x4_t{Vec16<T>::kLowest, Vec16<T>::kLowest, Vec16<T>::kLowest, Vec16<T>::kLowest};
       }
-    }
-    if constexpr (TOP) {
-      if (__ballot(all >= top.least)) {
-#pragma unroll 1
-        for (int u = 0; u < kLpUnroll; ++u) {  // (rolled: the code below once)
-          if (!__ballot((u == 0 ? m[0] : u == 1 ? m[1] : u == 2 ? m[2] : m[3]) >= top.least)) continue;
-          float f[N];
-          Vec16<T>::open(u == 0 ? cur[0] : u == 1 ? cur[1] : u == 2 ? cur[2] : cur[3], f);
-          top.make_room(64 * N);
-          const int v = v0 + u * kLpThreads + t;
+      const Sums before = s;
+      float m[kLpUnroll] = {}, all = -INFINITY;
+      if (!clamp) {
 #pragma unroll
-          for (int e = 0; e < N; ++e) top.offer(f[e], head + v * N + e, v < end);
+        for (int u = 0; u < kLpUnroll; ++u) {
+          float f[N];
+          Vec16<T>::open(cur[u], f);
+          m[u] = largest(f);
+          all = fmaxf(all, m[u]);
+          add(f, false);
+        }
+      }
+      const bool infinite = __ballot(s.E != s.E) != 0;
+      if (clamp || infinite || __ballot((all - s.r) * a.c > kLift)) {
+        s = before;
+#pragma unroll 1
+        for (int pass = clamp ? 0 : 1; pass < 2; ++pass) {  // the maxima, if they are not there, and the sums
+#pragma unroll 1
+          for (int u = 0; u < kLpUnroll; ++u) {
+            float f[N];
+            Vec16<T>::open(u == 0 ? cur[0] : u == 1 ? cur[1] : u == 2 ? cur[2] : cur[3], f);
+            if (pass == 0) {
+              const float mu = largest(f);
+#pragma unroll
+              for (int i = 0; i < kLpUnroll; ++i) m[i] = u == i ? mu : m[i];
+              all = fmaxf(all, mu);
+            } else {
+              if (u == 0 && __ballot((all - s.r) * a.c > kLift)) move_to(s, fmaxf(s.r, wave_max(all)), a.c);
+              add(f, true);
+            }
+          }
+        }
+        clamp |= infinite;
+      }
+      if constexpr (TOP) {
+        if (v0 + CHUNK <= end) {
+          best = fmaxf(best, all);
+          if (seen > 1 && (seen & (seen - 1)) == 0) {
+            const uint32_t b = wave_bound();
+            if (lane == 0) __hip_atomic_store(w_bound + w, b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+            use_bounds();  // (another wave's may be an earlier one: a lower bound all the same)
+          }
+        }
+        if (__ballot(all >= top.least)) {
+#pragma unroll
+          for (int u = 0; u < kLpUnroll; ++u) top.note(m[u], v0 + u * THREADS + t);
         }
       }
     }
+    if constexpr (TOP)
+      if (top.vectors > 64 || !more) top.look(xv, head, end);
+    if (!more) break;
   }
   // Each wave's results, then the first one's of all waves; for a row of
   // several slices that twice, the second time of the slices' results.
@@ -393,10 +467,10 @@ __global__ __launch_bounds__(kLpThreads) void logprobs_kernel(LogprobArgs a) {
       }
       __syncthreads();
       if (w == 0) {
-        s = Sums{lane < kLpWaves ? w_r[lane] : kLowest, lane < kLpWaves ? w_S[lane] : 0.f,
-                 lane < kLpWaves ? w_E[lane] : 0.f};
+        s = Sums{lane < W ? w_r[lane] : kLowest, lane < W ? w_S[lane] : 0.f,
+                 lane < W ? w_E[lane] : 0.f};
         if constexpr (TOP)
-          for (int i = 1; i < kLpWaves; ++i) {
+          for (int i = 1; i < W; ++i) {
             const int n = w_n[i];
             if (lane < n) top.buf[top.n + lane] = keys[i][lane];
             top.n += n;
@@ -405,7 +479,7 @@ __global__ __launch_bounds__(kLpThreads) void logprobs_kernel(LogprobArgs a) {
       continue;
     }
     if (stage == 3 || a.slices == 1) {
-      if (w == 0) put_row<T, TOP>(a, r, s, top.buf, top.n);
+      if (w == 0) put_row<T, TOP>(a, r, s, tok, x_tok, top.buf, top.n);
       return;
     }
     if (w == 0) {
@@ -429,7 +503,7 @@ __global__ __launch_bounds__(kLpThreads) void logprobs_kernel(LogprobArgs a) {
     }
     if constexpr (TOP) {
       uint64_t *pk = a.part_keys + r * a.slices * a.k;
-      for (int i = t - lane; i < a.slices * a.k; i += kLpThreads) {  // (kMostKeys: they fit)
+      for (int i = t - lane; i < a.slices * a.k; i += THREADS) {  // (kMostKeys: they fit)
         const uint64_t key = i + lane < a.slices * a.k ? get_shared(pk + i + lane) : 0;
         const uint64_t mask = __ballot(key != 0);
         if (key != 0) top.buf[top.n + lanes_below(mask)] = key;
@@ -446,6 +520,8 @@ struct LogprobPlan {
 // Slices of a row: while there are fewer workgroups than kLpFill, a row is
 // cut into chunks.
 constexpr int kLpFill = 1024;
+// Vectors of a row that one wave takes.
+constexpr int kLpShort = 1024;
 
 static LogprobPlan plan_logprobs(int rows, int vocab, int k) {
   const int nvec = (vocab + 3) / 4;  // (of fp32; bf16 rows have half as many)
@@ -485,8 +561,13 @@ SM_API sm_status sm_token_logprobs(const void *logits, int64_t stride, int rows,
   const LogprobArgs a{logits, stride, rows, vocab, k, scale, c, tokens, logprob, entropy, top_ids, top_logprobs, err,
                       p.slices, p.per_slice, (int *)ws, sums, (uint64_t *)(sums + (size_t)rows * p.slices)};
   const dim3 grid((unsigned)((int64_t)rows * p.slices));
-  const auto kernel = dt == SM_BF16 ? (k ? logprobs_kernel<uint16_t, true> : logprobs_kernel<uint16_t, false>)
-                                    : (k ? logprobs_kernel<float, true> : logprobs_kernel<float, false>);
-  hipLaunchKernelGGL(kernel, grid, dim3(kLpThreads), 0, stream, a);
+  const bool bf = dt == SM_BF16;
+  const bool short_row = p.slices == 1 && nvec <= kLpShort;
+  const auto kernel =
+      short_row ? (bf ? (k ? logprobs_kernel<uint16_t, true, 1> : logprobs_kernel<uint16_t, false, 1>)
+                      : (k ? logprobs_kernel<float, true, 1> : logprobs_kernel<float, false, 1>))
+                : (bf ? (k ? logprobs_kernel<uint16_t, true, kLpWaves> : logprobs_kernel<uint16_t, false, kLpWaves>)
+                      : (k ? logprobs_kernel<float, true, kLpWaves> : logprobs_kernel<float, false, kLpWaves>));
+  hipLaunchKernelGGL(kernel, grid, dim3(short_row ? 64 : 64 * kLpWaves), 0, stream, a);
   return hipGetLastError() == hipSuccess ? SM_OK : SM_EHIP;
 }

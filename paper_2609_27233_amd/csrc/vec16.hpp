@@ -8,7 +8,7 @@ namespace sm {
 template <typename T> struct Vec16;
 template <> struct Vec16<float> {
   static constexpr int N = 4;
-  static constexpr uint32_t kMinusInf = 0xff800000u;  // in every 32-bit word
+  static constexpr uint32_t kMinusInf = 0xff800000u, kLowest = 0xff7fffffu;  // as 32-bit words
   static __device__ __forceinline__ void open(u32x4_t v, float *f) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(v[i]);
@@ -19,7 +19,7 @@ template <> struct Vec16<float> {
 };
 template <> struct Vec16<uint16_t> {
   static constexpr int N = 8;
-  static constexpr uint32_t kMinusInf = 0xff80ff80u;
+  static constexpr uint32_t kMinusInf = 0xff80ff80u, kLowest = 0xff7fff7fu;
   static __device__ __forceinline__ void open(u32x4_t v, float *f) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
