@@ -31,7 +31,7 @@ constexpr int kLpWaves = 4;                                   // waves of a work
 constexpr int kLpUnroll = 4;                                  // 16-byte vectors that a thread holds at a time
 constexpr int kLpChunk = 64 * kLpWaves * kLpUnroll;           // vectors that they hold
 constexpr int kKeep = 256;                                    // keys that a wave keeps: SM_MAX_TOP and one of each lane at least
-constexpr int kNoted = 64 + 64 * kLpUnroll;                   // vectors that it has noted: a chunk's, and those before
+constexpr int kNoted = 64 + 2 * 64 * kLpUnroll;               // vectors that it has noted: two chunks', and those before
 constexpr int kMostSlices = 64;                               // (one wave reads their sums)
 constexpr int kMostKeys = kLpWaves * kKeep;                   // of all slices of a row
 constexpr int kCounters = 65536 / 4;
@@ -300,20 +300,20 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs a) {
   const int nvec = (a.vocab - head) / N;
   const u32x4_t *xv = (const u32x4_t *)(x + head);
   const int begin = min(slice * a.per_slice, nvec), end = min(begin + a.per_slice, nvec);
-  // the chunk at v0: -infinity behind the slice's end
-  u32x4_t cur[kLpUnroll];
-  auto load = [&](int v0) {
-    if (v0 + CHUNK <= end) {
+  // The chunk at v0.  Two are held, the next one on its way while one is
+  // worked on; the loads are unconditional (behind the slice's end its last
+  // vector again), so that waiting for one chunk leaves the other in flight.
+  u32x4_t even[kLpUnroll], odd[kLpUnroll];
+  auto load = [&](u32x4_t (&cur)[kLpUnroll], int v0) {
 #pragma unroll
-      for (int u = 0; u < kLpUnroll; ++u) cur[u] = __builtin_nontemporal_load(xv + v0 + u * THREADS + t);
-    } else {
+    for (int u = 0; u < kLpUnroll; ++u)
+      cur[u] = __builtin_nontemporal_load(xv + min(v0 + u * THREADS + t, end - 1));
+  };
+  auto fill = [&](u32x4_t (&cur)[kLpUnroll], int v0, uint32_t with) {  // behind the end
+    if (v0 + CHUNK <= end) return;
 #pragma unroll
-      for (int u = 0; u < kLpUnroll; ++u) {
-        const int v = v0 + u * THREADS + t;
-        cur[u] = u32x4_t{Vec16<T>::kMinusInf, Vec16<T>::kMinusInf, Vec16<T>::kMinusInf, Vec16<T>::kMinusInf};
-        if (v < end) cur[u] = __builtin_nontemporal_load(xv + v);
-      }
-    }
+    for (int u = 0; u < kLpUnroll; ++u)
+      if (v0 + u * THREADS + t >= end) cur[u] = u32x4_t{with, with, with, with};
   };
   auto largest = [&](const float *f) {
     float m = f[0];
@@ -344,13 +344,14 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs a) {
   // the token's logit, long before it is used
   const int tok = a.logprob ? a.tokens[r] : -1;
   float x_tok = 0.f;
-  if (begin < end) load(begin);
+  if (begin < end) load(even, begin);
   if (t == 0 && tok >= 0 && tok < a.vocab) x_tok = Elem<T>::load(x + tok);
   if (begin < end) {
+    fill(even, begin, Vec16<T>::kMinusInf);
 #pragma unroll
     for (int u = 0; u < kLpUnroll; ++u) {
       float f[N];
-      Vec16<T>::open(cur[u], f);
+      Vec16<T>::open(even[u], f);
       best = fmaxf(best, largest(f));
     }
     const float mw = wave_max(best);
@@ -386,69 +387,65 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs a) {
     if constexpr (TOP) top.put(f[0], v, lane < head + rest);
   }
   bool clamp = false;  // whether the slice has shown -infinity
-  for (int v0 = begin, seen = 1;; v0 += CHUNK, ++seen) {
-    const bool more = v0 < end;
-    if (more) {
-      if (v0 != begin) load(v0);  // (no chunk ahead: the other waves' work covers the wait)
-      if (v0 + CHUNK > end && s.r > -1e38f) {
-        // nothing behind the end, by a value of probability 0 (-infinity would have the chunk added again)
+  auto chunk = [&](u32x4_t (&cur)[kLpUnroll], int v0, int seen) {
+    // nothing behind the end: by a value of probability 0 (-infinity would have the chunk added again)
+    fill(cur, v0, s.r > -1e38f ? Vec16<T>::kLowest : Vec16<T>::kMinusInf);
+    const Sums before = s;
+    float m[kLpUnroll] = {}, all = -INFINITY;
+    if (!clamp) {
 #pragma unroll
-        for (int u = 0; u < kLpUnroll; ++u)
-          if (v0 + u * THREADS + t >= end)
-            cur[u] = u32x4_t{Vec16<T>::kLowest, Vec16<T>::kLowest, Vec16<T>::kLowest, Vec16<T>::kLowest};
-      }
-      const Sums before = s;
-      float m[kLpUnroll] = {}, all = -INFINITY;
-      if (!clamp) {
-#pragma unroll
-        for (int u = 0; u < kLpUnroll; ++u) {
-          float f[N];
-          Vec16<T>::open(cur[u], f);
-          m[u] = largest(f);
-          all = fmaxf(all, m[u]);
-          add(f, false);
-        }
-      }
-      const bool infinite = __ballot(s.E != s.E) != 0;
-      if (clamp || infinite || __ballot((all - s.r) * a.c > kLift)) {
-        s = before;
-#pragma unroll 1
-        for (int pass = clamp ? 0 : 1; pass < 2; ++pass) {  // the maxima, if they are not there, and the sums
-#pragma unroll 1
-          for (int u = 0; u < kLpUnroll; ++u) {
-            float f[N];
-            Vec16<T>::open(u == 0 ? cur[0] : u == 1 ? cur[1] : u == 2 ? cur[2] : cur[3], f);
-            if (pass == 0) {
-              const float mu = largest(f);
-#pragma unroll
-              for (int i = 0; i < kLpUnroll; ++i) m[i] = u == i ? mu : m[i];
-              all = fmaxf(all, mu);
-            } else {
-              if (u == 0 && __ballot((all - s.r) * a.c > kLift)) move_to(s, fmaxf(s.r, wave_max(all)), a.c);
-              add(f, true);
-            }
-          }
-        }
-        clamp |= infinite;
-      }
-      if constexpr (TOP) {
-        if (v0 + CHUNK <= end) {
-          best = fmaxf(best, all);
-          if (seen > 1 && (seen & (seen - 1)) == 0) {
-            const uint32_t b = wave_bound();
-            if (lane == 0) __hip_atomic_store(w_bound + w, b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-            use_bounds();  // (another wave's may be an earlier one: a lower bound all the same)
-          }
-        }
-        if (__ballot(all >= top.least)) {
-#pragma unroll
-          for (int u = 0; u < kLpUnroll; ++u) top.note(m[u], v0 + u * THREADS + t);
-        }
+      for (int u = 0; u < kLpUnroll; ++u) {
+        float f[N];
+        Vec16<T>::open(cur[u], f);
+        m[u] = largest(f);
+        all = fmaxf(all, m[u]);
+        add(f, false);
       }
     }
+    const bool infinite = __ballot(s.E != s.E) != 0;
+    if (clamp || infinite || __ballot((all - s.r) * a.c > kLift)) {
+      s = before;
+#pragma unroll 1
+      for (int pass = clamp ? 0 : 1; pass < 2; ++pass) {  // the maxima, if they are not there, and the sums
+#pragma unroll 1
+        for (int u = 0; u < kLpUnroll; ++u) {
+          float f[N];
+          Vec16<T>::open(u == 0 ? cur[0] : u == 1 ? cur[1] : u == 2 ? cur[2] : cur[3], f);
+          if (pass == 0) {
+            const float mu = largest(f);
+#pragma unroll
+            for (int i = 0; i < kLpUnroll; ++i) m[i] = u == i ? mu : m[i];
+            all = fmaxf(all, mu);
+          } else {
+            if (u == 0 && __ballot((all - s.r) * a.c > kLift)) move_to(s, fmaxf(s.r, wave_max(all)), a.c);
+            add(f, true);
+          }
+        }
+      }
+      clamp |= infinite;
+    }
+    if constexpr (TOP) {
+      if (v0 + CHUNK <= end) {
+        best = fmaxf(best, all);
+        if (seen > 1 && (seen & (seen - 1)) == 0) {
+          const uint32_t b = wave_bound();
+          if (lane == 0) __hip_atomic_store(w_bound + w, b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+          use_bounds();  // (another wave's may be an earlier one: a lower bound all the same)
+        }
+      }
+      if (__ballot(all >= top.least)) {
+#pragma unroll
+        for (int u = 0; u < kLpUnroll; ++u) top.note(m[u], v0 + u * THREADS + t);
+      }
+    }
+  };
+  for (int v0 = begin, seen = 1; v0 < end; v0 += 2 * CHUNK, seen += 2) {
+    load(odd, v0 + CHUNK);
+    chunk(even, v0, seen);
+    load(even, v0 + 2 * CHUNK);
+    if (v0 + CHUNK < end) chunk(odd, v0 + CHUNK, seen + 1);
     if constexpr (TOP)
-      if (top.vectors > 64 || !more) top.look(xv, head, end);
-    if (!more) break;
+      if (top.vectors > 64 || v0 + 2 * CHUNK >= end) top.look(xv, head, end);
   }
   // Each wave's results, then the first one's of all waves; for a row of
   // several slices that twice, the second time of the slices' results.
