@@ -34,7 +34,7 @@ constexpr int kKeep = 256;                                    // keys that a wav
 constexpr int kNoted = 64 + 2 * 64 * kLpUnroll;               // vectors that it has noted: two chunks', and those before
 constexpr int kMostSlices = 64;                               // (one wave reads their sums)
 constexpr int kMostKeys = kLpWaves * kKeep;                   // of all slices of a row
-constexpr int kCounters = 65536 / 4;
+constexpr int kCounterStep = 32;                              // counters stand 128 bytes apart
 constexpr float kLn2 = 0.69314718055994531f;
 constexpr float kLowest = -3.4028234663852886e38f;
 constexpr float kLift = 4.f;
@@ -88,70 +88,101 @@ __device__ __forceinline__ Sums wave_sums(Sums s, float c) {
   return s;
 }
 
-// Largest x in steps of 2^LOW for which at least k of the counted values are x or more.
-template <int LOW, class Count>
-__device__ __forceinline__ uint32_t kth(Count count, int k) {
-  uint32_t x = 0;
-  for (int b = 31; b >= LOW; --b) {
-    const uint32_t y = x | 1u << b;
-    if (count(y) >= k) x = y;
-  }
-  return x;
-}
-
 __device__ __forceinline__ void wave_order() {  // LDS accesses of the wave's lanes, in program order
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
   __builtin_amdgcn_wave_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
 }
 
-// The k largest of a wave's n keys (n <= kKeep) to the front of buf, in any
-// order; returns how many there are.  Values below 2^LOW are all alike.
-template <int LOW>
-__device__ __forceinline__ int keep_largest(uint64_t *buf, int n, int k) {
-  if (n <= k) return n;
-  constexpr int NR = kKeep / 64;
-  const int lane = threadIdx.x & 63;
+// rank[i]: how many of a wave's n keys (n <= 64 NK) are above key[i], this
+// lane's i-th.  kRankStep keys' reads are in flight at a time; 0 takes the
+// place of those behind the last.
+constexpr int kRankStep = 16;
+template <int NK>
+__device__ __forceinline__ void rank_keys(uint64_t *buf, int n, uint64_t (&key)[NK], int (&rank)[NK]) {
+  const int lane = threadIdx.x & 63, padded = (n + kRankStep - 1) / kRankStep * kRankStep;
+#pragma unroll
+  for (int i = 0; i < NK; ++i) {
+    const int at = lane + 64 * i;
+    rank[i] = 0;
+    if (at >= n && at < padded) buf[at] = 0;
+  }
   wave_order();
-  if (n <= 64) {  // by their ranks: n reads, where the search takes up to 64 counts
-    const uint64_t key = lane < n ? buf[lane] : 0;
-    int rank = 0;
-    for (int j = 0; j < n; ++j) rank += buf[j] > key;
-    wave_order();
-    if (lane < n && rank < k) buf[rank] = key;
-    wave_order();
+#pragma unroll
+  for (int i = 0; i < NK; ++i) key[i] = lane + 64 * i < n ? buf[lane + 64 * i] : 0;
+  for (int j = 0; j < n; j += kRankStep) {
+    uint64_t other[kRankStep];
+#pragma unroll
+    for (int i = 0; i < kRankStep; ++i) other[i] = buf[j + i];
+#pragma unroll
+    for (int i = 0; i < kRankStep; ++i)
+#pragma unroll
+      for (int l = 0; l < NK; ++l) rank[l] += other[i] > key[l];
+  }
+  wave_order();
+}
+template <int NK>
+__device__ __forceinline__ void keep_by_rank(uint64_t *buf, int n, int k) {
+  uint64_t key[NK];
+  int rank[NK];
+  rank_keys(buf, n, key, rank);
+#pragma unroll
+  for (int i = 0; i < NK; ++i)
+    if ((int)(threadIdx.x & 63) + 64 * i < n && rank[i] < k) buf[rank[i]] = key[i];
+  wave_order();
+}
+
+// The k largest of a wave's n keys (n <= kKeep) to the front of buf, in any
+// order; returns how many there are.  `bits`: of an index.  Values below
+// 2^LOW are all alike.
+template <int LOW>
+__device__ __forceinline__ int keep_largest(uint64_t *buf, int n, int k, int bits) {
+  if (n <= k) return n;
+  if (n <= 64) {
+    keep_by_rank<1>(buf, n, k);
     return k;
   }
+  if (n <= 128) {
+    keep_by_rank<2>(buf, n, k);
+    return k;
+  }
+  constexpr int NR = kKeep / 64;
+  const int lane = threadIdx.x & 63;
   uint32_t hi[NR], lo[NR];
+  wave_order();
 #pragma unroll
   for (int i = 0; i < NR; ++i) {
     const uint64_t key = lane + 64 * i < n ? buf[lane + 64 * i] : 0;
-    hi[i] = (uint32_t)(key >> 32);
+    hi[i] = (uint32_t)(key >> 32) >> LOW;
     lo[i] = (uint32_t)key;
   }
   wave_order();
   const auto count = [&](auto f) {
     int cnt = 0;
 #pragma unroll
-    for (int i = 0; i < NR; ++i)
-      if (64 * i < n) cnt += __popcll(__ballot(f(i)));
+    for (int i = 0; i < NR; ++i) cnt += __popcll(__ballot(f(i)));
     return cnt;
   };
-  const uint32_t v = kth<LOW>([&](uint32_t x) { return count([&](int i) { return hi[i] >= x; }); }, k);
-  const int above = count([&](int i) { return hi[i] >> LOW > v >> LOW; });
-  const int alike = count([&](int i) { return hi[i] >> LOW == v >> LOW; });
-  uint32_t from = 0;
-  if (above + alike > k)  // the lower indices among the equal ones
-    from = kth<0>([&](uint32_t x) { return count([&](int i) { return hi[i] >> LOW == v >> LOW && lo[i] >= x; }); }, k - above);
+  uint32_t v = 0;  // the k-th value
+  for (int b = 31 - LOW; b >= 0; --b) {
+    const uint32_t y = v | 1u << b;
+    if (count([&](int i) { return hi[i] >= y; }) >= k) v = y;
+  }
+  const int above = count([&](int i) { return hi[i] > v; });
+  uint32_t from = ~0u << (bits - 1) << 1;  // the least index (counted down) among the equal ones
+  for (int b = bits - 1; b >= 0; --b) {
+    const uint32_t y = from | 1u << b;
+    if (above + count([&](int i) { return hi[i] == v && lo[i] >= y; }) >= k) from = y;
+  }
   int at = 0;
 #pragma unroll
-  for (int i = 0; i < NR; ++i)
-    if (64 * i < n) {
-      const bool keep = hi[i] >> LOW > v >> LOW || (hi[i] >> LOW == v >> LOW && lo[i] >= from);
-      const uint64_t mask = __ballot(keep);
-      if (keep) buf[at + lanes_below(mask)] = (uint64_t)hi[i] << 32 | lo[i];
-      at += __popcll(mask);
-    }
+  for (int i = 0; i < NR; ++i) {
+    const bool keep = hi[i] > v || (hi[i] == v && lo[i] >= from);
+    const uint64_t mask = __ballot(keep);
+    // (the values' low bits are those of their sign: all 1 below 0)
+    if (keep) buf[at + lanes_below(mask)] = (uint64_t)(hi[i] << LOW | (LOW && !(hi[i] >> (31 - LOW)) ? 0xffffu : 0u)) << 32 | lo[i];
+    at += __popcll(mask);
+  }
   wave_order();
   return at;
 }
@@ -171,7 +202,7 @@ struct Candidates {
   static constexpr int LOW = sizeof(T) == 2 ? 16 : 0;
   uint64_t *buf;
   int *noted;
-  int n, vectors, k;
+  int n, vectors, k, bits;  // bits: of an index
   int ordered;     // a bound of an index below this is the lowest index of its value to come
   uint64_t bound;  // keys above it are wanted
   float least;     // vectors whose largest is this or more may hold one
@@ -210,7 +241,7 @@ struct Candidates {
 #pragma unroll 1
       for (int e = 0; e < N; ++e) {
         if (n > kKeep - 64) {
-          n = keep_largest<LOW>(buf, n, k);
+          n = keep_largest<LOW>(buf, n, k, bits);
           if (n == k) raise(wave_min64(lane < n ? buf[lane] : ~0ull));
         }
         float f;
@@ -231,7 +262,7 @@ struct Candidates {
 // Results of a row by one wave: its sums, its token (-1: none) with the
 // token's logit, and its m best keys in buf.
 template <typename T, bool TOP>
-__device__ __forceinline__ void put_row(const LogprobArgs &a, int64_t r, Sums s, int tok, float x_tok, const uint64_t *buf,
+__device__ __forceinline__ void put_row(const LogprobArgs &a, int64_t r, Sums s, int tok, float x_tok, uint64_t *buf,
                                         int m) {
   const int lane = threadIdx.x & 63;
   const T *x = (const T *)a.logits + r * a.stride;
@@ -252,13 +283,12 @@ __device__ __forceinline__ void put_row(const LogprobArgs &a, int64_t r, Sums s,
     }
   }
   if constexpr (TOP) {
-    wave_order();
-    const uint64_t key = lane < m ? buf[lane] : 0;
-    int rank = 0;
-    for (int j = 0; j < m; ++j) rank += buf[j] > key;
+    uint64_t key[1];
+    int rank[1];
+    rank_keys(buf, m, key, rank);
     if (lane < m) {
-      a.top_ids[r * a.k + rank] = (int)~(uint32_t)key;
-      if (a.top_logprobs) a.top_logprobs[r * a.k + rank] = logprob(value_of((uint32_t)(key >> 32)));
+      a.top_ids[r * a.k + rank[0]] = (int)~(uint32_t)key[0];
+      if (a.top_logprobs) a.top_logprobs[r * a.k + rank[0]] = logprob(value_of((uint32_t)(key[0] >> 32)));
     }
     for (int v0 = 0; m < a.k && v0 < a.vocab; v0 += 64) {  // fewer numbers than alternatives: NaN follow
       const float f = v0 + lane < a.vocab ? Elem<T>::load(x + v0 + lane) : 0.f;
@@ -322,14 +352,18 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs a) {
     return m;
   };
   Sums s{kLowest, 0.f, 0.f};
-  Candidates<T> top{keys[TOP ? w : 0], noted[TOP ? w : 0], 0, 0, a.k, head + nvec * N, 0, -INFINITY};
+  Candidates<T> top{keys[TOP ? w : 0], noted[TOP ? w : 0], 0, 0, a.k, 32 - __clz(a.vocab), head + nvec * N, 0, -INFINITY};
   float best = -INFINITY;  // this lane's largest
   // A bound below the slice's k-th largest: k / W of each wave's lanes hold
   // its least one's value or more (few alternatives: k of one wave's lanes).
   const bool one_wave = a.k < W;
   auto wave_bound = [&]() {
     const uint32_t o = order_of(best);
-    return kth<16>([&](uint32_t y) { return __popcll(__ballot(o >= y)); }, one_wave ? a.k : (a.k + W - 1) / W);
+    const int want = one_wave ? a.k : (a.k + W - 1) / W;
+    uint32_t b = 0;
+    for (int bit = 31; bit >= 16; --bit)  // (the low bits are not worth their time)
+      if (__popcll(__ballot(o >= (b | 1u << bit))) >= want) b |= 1u << bit;
+    return b;
   };
   auto use_bounds = [&]() {
     uint32_t b = one_wave ? 0 : ~0u;
@@ -391,38 +425,32 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs a) {
     // nothing behind the end: by a value of probability 0 (-infinity would have the chunk added again)
     fill(cur, v0, s.r > -1e38f ? Vec16<T>::kLowest : Vec16<T>::kMinusInf);
     const Sums before = s;
-    float m[kLpUnroll] = {}, all = -INFINITY;
-    if (!clamp) {
+    float m[kLpUnroll], all = -INFINITY;
+    auto pass = [&](bool clamped) {
 #pragma unroll
       for (int u = 0; u < kLpUnroll; ++u) {
+        u32x4_t x = cur[u];
+        if (clamped) asm("" : "+v"(x));  // (apart from the other pass, whose values would else be formed before the branch)
         float f[N];
-        Vec16<T>::open(cur[u], f);
+        Vec16<T>::open(x, f);
         m[u] = largest(f);
         all = fmaxf(all, m[u]);
-        add(f, false);
+        add(f, clamped);
       }
-    }
-    const bool infinite = __ballot(s.E != s.E) != 0;
-    if (clamp || infinite || __ballot((all - s.r) * a.c > kLift)) {
-      s = before;
-#pragma unroll 1
-      for (int pass = clamp ? 0 : 1; pass < 2; ++pass) {  // the maxima, if they are not there, and the sums
-#pragma unroll 1
-        for (int u = 0; u < kLpUnroll; ++u) {
-          float f[N];
-          Vec16<T>::open(u == 0 ? cur[0] : u == 1 ? cur[1] : u == 2 ? cur[2] : cur[3], f);
-          if (pass == 0) {
-            const float mu = largest(f);
-#pragma unroll
-            for (int i = 0; i < kLpUnroll; ++i) m[i] = u == i ? mu : m[i];
-            all = fmaxf(all, mu);
-          } else {
-            if (u == 0 && __ballot((all - s.r) * a.c > kLift)) move_to(s, fmaxf(s.r, wave_max(all)), a.c);
-            add(f, true);
-          }
-        }
-      }
+    };
+    if (clamp) pass(true);
+    else pass(false);
+    const bool infinite = !clamp && __ballot(s.E != s.E) != 0;
+    if (infinite || __ballot((all - s.r) * a.c > kLift)) {
       clamp |= infinite;
+      s = before;
+      move_to(s, fmaxf(s.r, wave_max(all)), a.c);
+#pragma unroll 1
+      for (int u = 0; u < kLpUnroll; ++u) {
+        float f[N];
+        Vec16<T>::open(u == 0 ? cur[0] : u == 1 ? cur[1] : u == 2 ? cur[2] : cur[3], f);
+        add(f, true);
+      }
     }
     if constexpr (TOP) {
       if (v0 + CHUNK <= end) {
@@ -453,7 +481,7 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs a) {
   for (int stage = 0;; ++stage) {
     if (w == 0 || !(stage & 1)) {
       s = wave_sums(s, a.c);
-      if constexpr (TOP) top.n = keep_largest<LOW>(top.buf, top.n, a.k);
+      if constexpr (TOP) top.n = keep_largest<LOW>(top.buf, top.n, a.k, top.bits);
     }
     if (!(stage & 1)) {
       if (lane == 0) {
@@ -487,11 +515,11 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs a) {
       }
       __builtin_amdgcn_s_waitcnt(0);  // in before the arrival counts
       if (lane == 0)
-        last = __hip_atomic_fetch_add(a.counters + r, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.slices - 1;
+        last = __hip_atomic_fetch_add(a.counters + r * kCounterStep, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.slices - 1;
     }
     __syncthreads();
     if (!last) return;
-    if (t == 0) put_shared(a.counters + r, 0);
+    if (t == 0) put_shared(a.counters + r * kCounterStep, 0);
     s = Sums{kLowest, 0.f, 0.f};
     top.n = 0;
     if (t < a.slices) {
@@ -514,16 +542,21 @@ struct LogprobPlan {
   int slices, per_slice;
 };
 
-// Slices of a row: while there are fewer workgroups than kLpFill, a row is
-// cut into chunks.
-constexpr int kLpFill = 1024;
-// Vectors of a row that one wave takes.
-constexpr int kLpShort = 1024;
+// Slices of a row: about kLpFill workgroups in all.  130 rows of 128,256 bf16
+// logits, 20 alternatives, us: 1 slice 29.5, 2 24.5, 4 23.0, 8 22.8; 16 rows, 8
+// and 16 slices: 16.6 and 22.7; 500 rows, 1, 2 and 3 slices: 37.0, 38.0, 41.6.
+constexpr int kLpFill = 512;
+// Rows of up to kLpShort vectors are one wave's, and where there are kLpMany
+// rows all are: its fixed part is smaller, and nothing waits at a barrier.
+constexpr int kLpShort = 1024, kLpMany = 1536;
+
+// (no row is cut beyond kLpFill rows, so its counter is within the first 64 KiB)
+static_assert(kLpFill * kCounterStep * sizeof(int) <= 65536, "counters");
 
 static LogprobPlan plan_logprobs(int rows, int vocab, int k) {
   const int nvec = (vocab + 3) / 4;  // (of fp32; bf16 rows have half as many)
-  int slices = rows > 0 && rows < kLpFill && rows <= kCounters ? (kLpFill + rows - 1) / rows : 1;
   const int chunks = (nvec + kLpChunk - 1) / kLpChunk;
+  int slices = rows > 0 && rows < kLpFill ? (kLpFill + rows / 2) / rows : 1;
   slices = slices < chunks ? slices : chunks;
   slices = slices < kMostSlices ? slices : kMostSlices;
   if (k > 0 && slices > kMostKeys / k) slices = kMostKeys / k;
@@ -559,7 +592,7 @@ SM_API sm_status sm_token_logprobs(const void *logits, int64_t stride, int rows,
                       p.slices, p.per_slice, (int *)ws, sums, (uint64_t *)(sums + (size_t)rows * p.slices)};
   const dim3 grid((unsigned)((int64_t)rows * p.slices));
   const bool bf = dt == SM_BF16;
-  const bool short_row = p.slices == 1 && nvec <= kLpShort;
+  const bool short_row = p.slices == 1 && (nvec <= kLpShort || rows >= kLpMany);
   const auto kernel =
       short_row ? (bf ? (k ? logprobs_kernel<uint16_t, true, 1> : logprobs_kernel<uint16_t, false, 1>)
                       : (k ? logprobs_kernel<float, true, 1> : logprobs_kernel<float, false, 1>))
