@@ -5,23 +5,27 @@
 // of a row are the same for all its heads.  Both calls read and write each
 // row once and are bound by that traffic.  A workgroup takes a tile of rows
 // and a range of heads: it forms the tile's cosines and sines in LDS (angle
-// and reduction in double precision, then fp32), and turns 16 bytes of each
-// half of a pair per thread.
+// and reduction in double precision, then fp32); a thread keeps those of one
+// row's 16-byte unit in registers and turns that unit of one head after
+// another, several heads' loads in flight.
 //
 // K rows go to token-major pages 16 bytes at a time.  V pages are dim-major,
-// so V is transposed in registers: 8 rows (fp32: 4) that fill an aligned
-// group of a page's slots become 16-byte stores.  Tiles are cut where such
-// groups begin, so a prompt's rows are stored whole wherever its sequence
-// starts in the batch; single rows (a decode step) are stored an element at
-// a time, which the layout of the pages asks for.
+// so V is transposed in registers: VEC rows (bf16 8, fp32 4) that fill an
+// aligned group of a page's slots become 16-byte stores.  Tiles are cut where
+// a 16-slot segment of a page begins, so a prompt's rows are stored whole
+// wherever its sequence starts in the batch, and two neighbouring lanes fill
+// 32 bytes of a page's row; single rows (a decode step) are stored an element
+// at a time, which the layout of the pages asks for.
 #include <cmath>
 
 #include "cache_meta.hpp"
+#include "vec16.hpp"
 
 namespace sm {
 
 constexpr int kRotThreads = 256;
 constexpr int kTileRows = 16;
+constexpr int kMostRows = 2 * kTileRows - 1;  // of a tile cut by slots
 constexpr int kMaxPairs = 128;
 
 // One stream of rows of heads: [rows][heads][D] with a row stride.
@@ -37,7 +41,7 @@ struct RopeArgs {
   const int32_t *pos;
   int rows, R, sign;        // sign -1: transposed
   float scale;
-  FastDiv per_head;         // units of a head: R / (2 VEC) turned pairs and (D - R) / VEC copies (scalar: R / 2 and D - R)
+  int per_head;             // units of a head
 };
 
 // Cosine and sine of the tile's rows, [row][pair]: the angle in turns is
@@ -54,94 +58,128 @@ __device__ __forceinline__ void fill_angles(const RopeArgs &a, int r0, int nr, f
   }
 }
 
-template <typename T> struct Vec;  // 16 bytes of T as floats
-template <> struct Vec<float> {
-  static constexpr int N = 4;
-  static __device__ __forceinline__ void open(u32x4_t v, float (&f)[4]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(v[i]);
-  }
-  static __device__ __forceinline__ u32x4_t close(const float (&f)[4]) {
-    return u32x4_t{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
-  }
-};
-template <> struct Vec<uint16_t> {
-  static constexpr int N = 8;
-  static __device__ __forceinline__ void open(u32x4_t v, float (&f)[8]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      f[2 * i] = __uint_as_float(v[i] << 16);
-      f[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
-    }
-  }
-  static __device__ __forceinline__ u32x4_t close(const float (&f)[8]) {
-    return u32x4_t{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])};
-  }
-};
-
 __device__ __forceinline__ float2 turned(float a, float b, float2 cs) {
   return make_float2(a * cs.x - b * cs.y, a * cs.y + b * cs.x);
 }
 
-// Unit `j` of a head at `in` to `out`, cs: the row's cosines and sines.
-// WIDE: a unit moves 16 bytes (half layout: of each half); else one pair or
-// one feature.
-template <typename T, bool HALF, bool WIDE>
-__device__ __forceinline__ void turn_unit(const T *in, T *out, int j, int R, const float2 *cs) {
-  if constexpr (WIDE) {
-    constexpr int N = Vec<T>::N;
-    const int turning = HALF ? R / (2 * N) : R / N;
-    if (j >= turning) {  // behind the turned part
-      const int at = R + (j - turning) * N;
-      *(u32x4_t *)(out + at) = *(const u32x4_t *)(in + at);
-    } else if constexpr (HALF) {
-      float a[N], b[N];
-      Vec<T>::open(*(const u32x4_t *)(in + j * N), a);
-      Vec<T>::open(*(const u32x4_t *)(in + R / 2 + j * N), b);
+// A thread's unit: 16 bytes of a row's head (half layout: of each half), or 16
+// bytes behind the turned part, which are copied.
+template <typename T, bool HALF>
+struct Unit {
+  static constexpr int N = Vec16<T>::N, NP = HALF ? N : N / 2;  // pairs
+  int at, far;  // features; far 0: no second half
+  bool turning;
+  float2 cs[NP];
+
+  __device__ __forceinline__ void set(int j, int R, const float2 *row_cs) {
+    const int units = HALF ? R / (2 * N) : R / N;
+    turning = j < units;
+    at = turning ? j * N : R + (j - units) * N;
+    far = HALF && turning ? R / 2 : 0;
+    if (turning)
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        const float2 t = turned(a[e], b[e], cs[j * N + e]);
-        a[e] = t.x;
-        b[e] = t.y;
-      }
-      *(u32x4_t *)(out + j * N) = Vec<T>::close(a);
-      *(u32x4_t *)(out + R / 2 + j * N) = Vec<T>::close(b);
-    } else {
-      float a[N];
-      Vec<T>::open(*(const u32x4_t *)(in + j * N), a);
-#pragma unroll
-      for (int e = 0; e < N; e += 2) {
-        const float2 t = turned(a[e], a[e + 1], cs[(j * N + e) / 2]);
-        a[e] = t.x;
-        a[e + 1] = t.y;
-      }
-      *(u32x4_t *)(out + j * N) = Vec<T>::close(a);
-    }
-  } else {
-    if (j >= R / 2) {
-      out[R / 2 + j] = in[R / 2 + j];
-      return;
-    }
-    const int i0 = HALF ? j : 2 * j, i1 = HALF ? j + R / 2 : 2 * j + 1;
-    const float2 t = turned(Elem<T>::load(in + i0), Elem<T>::load(in + i1), cs[j]);
-    out[i0] = Elem<T>::to_store(t.x);
-    out[i1] = Elem<T>::to_store(t.y);
+      for (int e = 0; e < NP; ++e) cs[e] = row_cs[j * NP + e];
   }
+  // Heads h, h + step, ... below h1: in(h), out(h) give a head's first
+  // feature.  The loads are unconditional (the last head's again).
+  template <class In, class Out>
+  __device__ __forceinline__ void run(int h, int h1, int step, In in, Out out) const {
+    constexpr int U = 4;
+    for (; h < h1; h += U * step) {
+      u32x4_t a[U], b[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const T *p = in(min(h + u * step, h1 - 1)) + at;
+        a[u] = *(const u32x4_t *)p;
+        if constexpr (HALF) b[u] = *(const u32x4_t *)(p + far);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (h + u * step >= h1) break;
+        T *p = out(h + u * step) + at;
+        if (!turning) {
+          *(u32x4_t *)p = a[u];
+          continue;
+        }
+        float f[N], g[N];
+        Vec16<T>::open(a[u], f);
+        if constexpr (HALF) {
+          Vec16<T>::open(b[u], g);
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            const float2 t = turned(f[e], g[e], cs[e]);
+            f[e] = t.x;
+            g[e] = t.y;
+          }
+          *(u32x4_t *)(p + far) = Vec16<T>::close(g);
+        } else {
+#pragma unroll
+          for (int e = 0; e < N; e += 2) {
+            const float2 t = turned(f[e], f[e + 1], cs[e / 2]);
+            f[e] = t.x;
+            f[e + 1] = t.y;
+          }
+        }
+        *(u32x4_t *)p = Vec16<T>::close(f);
+      }
+    }
+  }
+};
+
+// The units of `nr` rows over the workgroup: f(row, unit of the head, first
+// head, step over the heads).  Where the rows' units are fewer than the
+// threads, several threads share a unit's heads.
+template <class F>
+__device__ __forceinline__ void each_unit(int nr, int per_head, F f) {
+  const int units = nr * per_head, share = max(1, kRotThreads / units);
+  const int part = share > 1 ? (int)threadIdx.x / units : 0;
+  if (part >= share) return;
+  for (int u = threadIdx.x - part * units; u < units; u += kRotThreads) f(u / per_head, u % per_head, part, share);
 }
 
-template <typename T, bool HALF, bool WIDE>
+template <typename T, bool HALF>
 __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RopeArgs a, Rows x, int D, int heads_per) {
   extern __shared__ float2 cs[];  // [rows of a tile][R / 2]
-  const int r0 = blockIdx.x * kTileRows, nr = min(kTileRows, a.rows - r0);
-  const int h0 = blockIdx.y * heads_per, nh = min(heads_per, x.heads - h0);
-  fill_angles(a, r0, nr, cs);
+  const int64_t r0 = (int64_t)blockIdx.x * kTileRows;
+  const int nr = (int)min((int64_t)kTileRows, a.rows - r0);
+  const int h0 = blockIdx.y * heads_per, h1 = min(h0 + heads_per, x.heads);
+  fill_angles(a, (int)r0, nr, cs);
   __syncthreads();
-  const int per = a.per_head.d;
-  const T *in = (const T *)x.in + (int64_t)r0 * x.in_stride + (int64_t)h0 * D;
-  T *out = (T *)x.out + (int64_t)r0 * x.out_stride + (int64_t)h0 * D;
+  each_unit(nr, a.per_head, [&](int r, int j, int part, int share) {
+    Unit<T, HALF> unit;
+    unit.set(j, a.R, cs + r * (a.R / 2));
+    const T *in = (const T *)x.in + (r0 + r) * x.in_stride;
+    T *out = (T *)x.out + (r0 + r) * x.out_stride;
+    unit.run(h0 + part, h1, share, [&](int h) { return in + h * D; }, [&](int h) { return out + h * D; });
+  });
+}
+
+// Rows, heads or strides that 16 bytes do not divide: a pair or a copied
+// feature at a time.  Unit j of a head at `in` to `out`.
+template <typename T, bool HALF>
+__device__ __forceinline__ void turn_one(const T *in, T *out, int j, int R, const float2 *cs) {
+  if (j >= R / 2) {
+    out[R / 2 + j] = in[R / 2 + j];
+    return;
+  }
+  const int i0 = HALF ? j : 2 * j, i1 = HALF ? j + R / 2 : 2 * j + 1;
+  const float2 t = turned(Elem<T>::load(in + i0), Elem<T>::load(in + i1), cs[j]);
+  out[i0] = Elem<T>::to_store(t.x);
+  out[i1] = Elem<T>::to_store(t.y);
+}
+
+template <typename T, bool HALF>
+__global__ __launch_bounds__(kRotThreads) void rotary_any_kernel(RopeArgs a, Rows x, int D, int heads_per) {
+  extern __shared__ float2 cs[];
+  const int64_t r0 = (int64_t)blockIdx.x * kTileRows;
+  const int nr = (int)min((int64_t)kTileRows, a.rows - r0);
+  const int h0 = blockIdx.y * heads_per, nh = min(heads_per, x.heads - h0), per = a.per_head;
+  fill_angles(a, (int)r0, nr, cs);
+  __syncthreads();
   for (int u = threadIdx.x; u < nr * nh * per; u += kRotThreads) {
-    const int hr = fdiv(u, a.per_head), j = u - hr * per, r = hr / nh, h = hr - r * nh;
-    turn_unit<T, HALF, WIDE>(in + r * x.in_stride + h * D, out + r * x.out_stride + h * D, j, a.R, cs + r * (a.R / 2));
+    const int hr = u / per, j = u - hr * per, r = hr / nh, h = h0 + hr - r * nh;
+    turn_one<T, HALF>((const T *)x.in + (r0 + r) * x.in_stride + h * D, (T *)x.out + (r0 + r) * x.out_stride + h * D, j,
+                      a.R, cs + r * (a.R / 2));
   }
 }
 
@@ -156,80 +194,145 @@ struct WriteArgs {
   int bs_log2, dh_log2, num_slots;
 };
 
-// Whether row r begins a group: rows that fill consecutive slots of one
-// aligned group of VEC slots.
-template <int VEC>
-__device__ __forceinline__ bool begins_group(const int32_t *slots, int r) {
-  const int s = slots[r];
-  return r == 0 || s < 0 || s % VEC == 0 || slots[r - 1] != s - 1;
+// out[i] = element i of in[0 .. VEC-1]
+__device__ __forceinline__ void transpose16(const u32x4_t (&in)[8], u32x4_t (&out)[8]) {  // bf16
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const uint32_t x = in[2 * w][i >> 1], y = in[2 * w + 1][i >> 1];
+      out[i][w] = (i & 1) ? ((x >> 16) | (y & 0xffff0000u)) : ((x & 0xffffu) | (y << 16));
+    }
+}
+__device__ __forceinline__ void transpose16(const u32x4_t (&in)[4], u32x4_t (&out)[4]) {  // fp32
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) out[i][j] = in[j][i];
 }
 
-// Rows of a tile: from the first row at or past `r` (at most VEC - 1 further,
-// the last row of a run aside) that begins a group.
-template <int VEC>
-__device__ __forceinline__ int tile_begin(const int32_t *slots, int r, int rows) {
-  while (r < rows && !begins_group<VEC>(slots, r)) ++r;
-  return min(r, rows);
+// Head 0 of the page that holds slot s, and the slot in it.
+template <typename T>
+__device__ __forceinline__ T *page_of(T *pool, int s, const WriteArgs &w, int *in_page) {
+  *in_page = s & ((1 << w.bs_log2) - 1);
+  return pool + (((int64_t)(s >> w.bs_log2) * w.k.heads) << (w.bs_log2 + w.dh_log2));
 }
 
-template <typename T, bool HALF, bool WIDE>
+template <typename T, bool HALF>
 __global__ __launch_bounds__(kRotThreads) void kv_write_kernel(RopeArgs a, WriteArgs w, int heads_per) {
   constexpr int VEC = 16 / sizeof(T);
-  constexpr int kMost = kTileRows + VEC;
   extern __shared__ float2 cs[];
-  __shared__ int slot[kMost], bounds[2];
-  const int t = threadIdx.x, D = 1 << w.dh_log2, bs = 1 << w.bs_log2;
-  if (t < 2) bounds[t] = tile_begin<VEC>(w.slots, (int)min((int64_t)a.rows, ((int64_t)blockIdx.x + t) * kTileRows), a.rows);
-  __syncthreads();
-  const int r0 = bounds[0], nr = bounds[1] - r0;
+  __shared__ int slot[kMostRows + 1], group[kMostRows + 1];
+  const int t = threadIdx.x, lane = t & 63, D = 1 << w.dh_log2, bs = 1 << w.bs_log2;
+  // The tile: from the first row at or past base that begins a 16-slot
+  // segment, a run of its own or padding, to the next tile's first.  Each
+  // wave looks at the slots of rows base - 1 .. base + 62.
+  const int64_t base = (int64_t)blockIdx.x * kTileRows;
+  const int64_t mine = base + lane - 1;
+  int s = mine >= 0 && mine < a.rows ? w.slots[mine] : -1;
+  const bool bad = s < -1 || s >= w.num_slots;
+  if (bad) s = -1;
+  const int before = __shfl_up(s, 1, kWave);
+  const bool end = mine >= a.rows;
+  const uint64_t first = __ballot(s < 0 || before != s - 1 || s % kTileRows == 0 || mine == 0 || end) >> 1;
+  const uint64_t fill = __ballot(s < 0 || before != s - 1 || s % VEC == 0 || mine == 0 || end) >> 1;  // group starts
+  const int b0 = __builtin_ctzll(first), b1 = kTileRows + __builtin_ctzll(first >> kTileRows);
+  const int r0 = (int)(base + b0), nr = (int)min((int64_t)a.rows, base + b1) - r0;
+  if (nr <= 0) return;
   const int h0 = blockIdx.y * heads_per, h1 = min(h0 + heads_per, w.q.heads + 2 * w.k.heads);
-  if (t < nr) {
-    const int s = w.slots[r0 + t];
-    if (s < -1 || s >= w.num_slots) {
-      if (h0 == 0) set_err(w.err, SM_ERR_EINVAL);
-      slot[t] = -1;
-    } else {
-      slot[t] = s;
-    }
+  const int me = lane - 1 - b0;  // this lane's row of the tile
+  // groups of rows that fill consecutive slots of VEC aligned ones
+  const uint64_t mask = fill >> b0 & ((1ull << nr) - 1);
+  const int groups = __popcll(mask);
+  if (t < 64 && me >= 0 && me < nr) {
+    slot[me] = s;
+    if (bad && h0 == 0) set_err(w.err, SM_ERR_EINVAL);
+    if (mask >> me & 1) group[__popcll(mask & ((1ull << me) - 1))] = me;
   }
-  const bool turns = h0 < w.q.heads + w.k.heads;
-  if (turns) fill_angles(a, r0, nr, cs);
+  if (t == 0) group[groups] = nr;
+  if (h0 < w.q.heads + w.k.heads) fill_angles(a, r0, nr, cs);
   __syncthreads();
-  const int per = a.per_head.d;
-  // q: this range's heads below q.heads
-  {
-    const int nh = min(h1, w.q.heads) - h0;
-    const T *in = (const T *)w.q.in + (int64_t)r0 * w.q.in_stride + (int64_t)h0 * D;
-    T *out = (T *)w.q.out + (int64_t)r0 * w.q.out_stride + (int64_t)h0 * D;
-    for (int u = t; nh > 0 && u < nr * nh * per; u += kRotThreads) {
-      const int hr = fdiv(u, a.per_head), j = u - hr * per, r = hr / nh, h = hr - r * nh;
-      turn_unit<T, HALF, WIDE>(in + r * w.q.in_stride + h * D, out + r * w.q.out_stride + h * D, j, a.R,
-                               cs + r * (a.R / 2));
+  // V: unit = (head, VEC dims, group), the groups of a segment side by side
+  const int g0 = max(h0 - w.q.heads - w.k.heads, 0), g1 = h1 - w.q.heads - w.k.heads;
+  if (g1 > g0) {
+    const int dgs = D / VEC, units = (g1 - g0) * dgs * groups;
+    const float inv = 1.f / groups;
+    for (int u = t; u < units; u += kRotThreads) {
+      const int hd = (int)((u + 0.5f) * inv), g = u - hd * groups;  // (exact below 2^21)
+      const int h = g0 + hd / dgs, d0 = hd % dgs * VEC;
+      const int f = group[g], n = group[g + 1] - f, sl = slot[f];
+      const T *in = (const T *)w.v.in + (int64_t)(r0 + f) * w.v.in_stride + h * D + d0;
+      u32x4_t v[VEC], vt[VEC];
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) v[i] = *(const u32x4_t *)(in + min(i, n - 1) * w.v.in_stride);
+      if (sl < 0) continue;
+      int at;
+      T *out = page_of((T *)w.v_pool, sl, w, &at) + (((int64_t)h * D + d0) << w.bs_log2) + at;
+      transpose16(v, vt);
+      if (n == VEC) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) *(u32x4_t *)(out + (int64_t)i * bs) = vt[i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          const T *e = (const T *)&vt[i];
+#pragma unroll
+          for (int j = 0; j < VEC; ++j)
+            if (j < n) out[(int64_t)i * bs + j] = e[j];
+        }
+      }
     }
   }
-  // k
-  {
-    const int g0 = max(h0 - w.q.heads, 0), nh = min(h1 - w.q.heads, w.k.heads) - g0;
-    const T *in = (const T *)w.k.in + (int64_t)r0 * w.k.in_stride;
-    for (int u = t; nh > 0 && u < nr * nh * per; u += kRotThreads) {
-      const int hr = fdiv(u, a.per_head), j = u - hr * per, r = hr / nh, h = g0 + hr - r * nh;
-      const int s = slot[r];
-      if (s < 0) continue;
-      T *out = (T *)w.k_pool + ((((int64_t)(s >> w.bs_log2) * w.k.heads + h) << w.bs_log2) + (s & (bs - 1))) * D;
-      turn_unit<T, HALF, WIDE>(in + r * w.k.in_stride + h * D, out, j, a.R, cs + r * (a.R / 2));
+  const int hq1 = min(h1, w.q.heads), k0 = max(h0 - w.q.heads, 0), k1 = min(h1 - w.q.heads, w.k.heads);
+  if (h0 >= w.q.heads + w.k.heads) return;
+  each_unit(nr, a.per_head, [&](int r, int j, int part, int share) {
+    Unit<T, HALF> unit;
+    unit.set(j, a.R, cs + r * (a.R / 2));
+    const T *q = (const T *)w.q.in + (r0 + r) * w.q.in_stride, *k = (const T *)w.k.in + (r0 + r) * w.k.in_stride;
+    T *q_out = (T *)w.q.out + (r0 + r) * w.q.out_stride;
+    unit.run(h0 + part, hq1, share, [&](int h) { return q + h * D; }, [&](int h) { return q_out + h * D; });
+    const int sl = slot[r];
+    if (sl < 0) return;
+    int at;
+    T *page = page_of((T *)w.k_pool, sl, w, &at) + at * D;
+    unit.run(k0 + part, k1, share, [&](int h) { return k + h * D; },
+             [&](int h) { return page + ((int64_t)h << (w.bs_log2 + w.dh_log2)); });
+  });
+}
+
+template <typename T, bool HALF>
+__global__ __launch_bounds__(kRotThreads) void kv_write_any_kernel(RopeArgs a, WriteArgs w, int heads_per) {
+  extern __shared__ float2 cs[];
+  const int64_t r0 = (int64_t)blockIdx.x * kTileRows;
+  const int nr = (int)min((int64_t)kTileRows, a.rows - r0), t = threadIdx.x, D = 1 << w.dh_log2, per = a.per_head;
+  const int h0 = blockIdx.y * heads_per, nh = min(heads_per, w.q.heads + 2 * w.k.heads - h0);
+  fill_angles(a, (int)r0, nr, cs);
+  __syncthreads();
+  for (int rh = t >> 6; rh < nr * nh; rh += kRotThreads / 64) {  // a wave per head of a row
+    const int r = rh / nh, h = h0 + rh - r * nh, hk = h - w.q.heads, hv = hk - w.k.heads;
+    const int64_t row = r0 + r;
+    const float2 *rcs = cs + r * (a.R / 2);
+    if (hk < 0) {
+      for (int j = t & 63; j < per; j += 64)
+        turn_one<T, HALF>((const T *)w.q.in + row * w.q.in_stride + h * D, (T *)w.q.out + row * w.q.out_stride + h * D, j,
+                          a.R, rcs);
+      continue;
     }
-  }
-  // v
-  {
-    const int g0 = max(h0 - w.q.heads - w.k.heads, 0), nh = h1 - w.q.heads - w.k.heads - g0;
-    const T *in = (const T *)w.v.in + (int64_t)r0 * w.v.in_stride;
-    for (int u = t; nh > 0 && u < nr * nh * D; u += kRotThreads) {
-      const int d = u & (D - 1), hr = u >> w.dh_log2, r = hr / nh, h = g0 + hr - r * nh;
-      const int s = slot[r];
-      if (s < 0) continue;
-      T *out = (T *)w.v_pool + (((((int64_t)(s >> w.bs_log2) * w.k.heads + h) << w.dh_log2) + d) << w.bs_log2) +
-               (s & (bs - 1));
-      *out = in[r * w.v.in_stride + h * D + d];
+    const int s = w.slots[row];
+    if (s < -1 || s >= w.num_slots) {
+      if (hk == 0 && (t & 63) == 0) set_err(w.err, SM_ERR_EINVAL);
+      continue;
+    }
+    if (s < 0) continue;
+    int at;
+    if (hv < 0) {
+      T *out = page_of((T *)w.k_pool, s, w, &at) + (((int64_t)hk << w.bs_log2) + at) * D;
+      for (int j = t & 63; j < per; j += 64)
+        turn_one<T, HALF>((const T *)w.k.in + row * w.k.in_stride + hk * D, out, j, a.R, rcs);
+    } else {
+      T *out = page_of((T *)w.v_pool, s, w, &at) + at;
+      for (int d = t & 63; d < D; d += 64)
+        out[((int64_t)hv * D + d) << w.bs_log2] = ((const T *)w.v.in)[row * w.v.in_stride + hv * D + d];
     }
   }
 }
@@ -289,9 +392,8 @@ static RopeArgs rope_args(const sm_rope_params *p, const int32_t *pos, int rows,
   a.sign = transpose ? -1 : 1;
   a.scale = p->attn_scale;
   const int vec = 16 / (int)es;
-  a.per_head = make_fastdiv((uint32_t)(!wide ? p->rot_dim / 2 + D - p->rot_dim
-                                              : (p->layout == SM_ROPE_HALF ? p->rot_dim / (2 * vec) : p->rot_dim / vec) +
-                                                    (D - p->rot_dim) / vec));
+  a.per_head = !wide ? D - p->rot_dim / 2
+                     : (p->layout == SM_ROPE_HALF ? p->rot_dim / (2 * vec) : p->rot_dim / vec) + (D - p->rot_dim) / vec;
   return a;
 }
 
@@ -313,8 +415,8 @@ static void launch_rotary(const RopeArgs &a, const Rows &x, int D, bool half, bo
   const int per = heads_per_wg(x.heads, tiles);
   const dim3 grid((unsigned)tiles, (x.heads + per - 1) / per);
   const size_t lds = kTileRows * (a.R / 2) * sizeof(float2);
-  const auto kernel = half ? (wide ? rotary_kernel<T, true, true> : rotary_kernel<T, true, false>)
-                           : (wide ? rotary_kernel<T, false, true> : rotary_kernel<T, false, false>);
+  const auto kernel = wide ? (half ? rotary_kernel<T, true> : rotary_kernel<T, false>)
+                           : (half ? rotary_any_kernel<T, true> : rotary_any_kernel<T, false>);
   hipLaunchKernelGGL(kernel, grid, dim3(kRotThreads), lds, stream, a, x, D, per);
 }
 
@@ -342,9 +444,9 @@ static void launch_write(const RopeArgs &a, const WriteArgs &w, bool half, bool 
   const int64_t tiles = ((int64_t)a.rows + kTileRows - 1) / kTileRows;
   const int heads = w.q.heads + 2 * w.k.heads, per = heads_per_wg(heads, tiles);
   const dim3 grid((unsigned)tiles, (heads + per - 1) / per);
-  const size_t lds = (kTileRows + 16 / sizeof(T)) * (a.R / 2) * sizeof(float2);
-  const auto kernel = half ? (wide ? kv_write_kernel<T, true, true> : kv_write_kernel<T, true, false>)
-                           : (wide ? kv_write_kernel<T, false, true> : kv_write_kernel<T, false, false>);
+  const size_t lds = kMostRows * (a.R / 2) * sizeof(float2);
+  const auto kernel = wide ? (half ? kv_write_kernel<T, true> : kv_write_kernel<T, false>)
+                           : (half ? kv_write_any_kernel<T, true> : kv_write_any_kernel<T, false>);
   hipLaunchKernelGGL(kernel, grid, dim3(kRotThreads), lds, stream, a, w, per);
 }
 
