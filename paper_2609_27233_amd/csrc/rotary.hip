@@ -41,7 +41,7 @@ struct RopeArgs {
   const int32_t *pos;
   int rows, R, sign;        // sign -1: transposed
   float scale;
-  int per_head;             // units of a head
+  FastDiv per_head;         // by the units of a head
 };
 
 // Cosine and sine of the tile's rows, [row][pair]: the angle in turns is
@@ -127,14 +127,25 @@ struct Unit {
 };
 
 // The units of `nr` rows over the workgroup: f(row, unit of the head, first
-// head, step over the heads).  Where the rows' units are fewer than the
-// threads, several threads share a unit's heads.
-template <class F>
-__device__ __forceinline__ void each_unit(int nr, int per_head, F f) {
-  const int units = nr * per_head, share = max(1, kRotThreads / units);
-  const int part = share > 1 ? (int)threadIdx.x / units : 0;
-  if (part >= share) return;
-  for (int u = threadIdx.x - part * units; u < units; u += kRotThreads) f(u / per_head, u % per_head, part, share);
+// head, step over the heads).  Lanes that are neighbours hold the units of a
+// head, then BY_ROW those of the row's other heads (rows are read and written
+// in long pieces), else those of the next rows (as pages hold them); with
+// fewer units than threads, more threads share the heads.
+template <bool BY_ROW, class F>
+__device__ __forceinline__ void each_unit(int nr, const FastDiv &per_head, int heads, F f) {
+  const int units = nr * (int)per_head.d;
+  int share_log2 = 0;
+  while (((BY_ROW && (int)per_head.d << share_log2 < 64) || units << share_log2 < kRotThreads) && 1 << share_log2 < heads)
+    ++share_log2;
+  for (int u = threadIdx.x; u < units << share_log2; u += kRotThreads) {
+    if constexpr (BY_ROW) {
+      const int rp = fdiv(u, per_head), part = rp & ((1 << share_log2) - 1);
+      f(rp >> share_log2, u - rp * (int)per_head.d, part, 1 << share_log2);
+    } else {
+      const int part = share_log2 == 0 ? 0 : u / units, at = u - part * units, r = fdiv(at, per_head);
+      f(r, at - r * (int)per_head.d, part, 1 << share_log2);
+    }
+  }
 }
 
 template <typename T, bool HALF>
@@ -145,7 +156,7 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RopeArgs a, Rows x,
   const int h0 = blockIdx.y * heads_per, h1 = min(h0 + heads_per, x.heads);
   fill_angles(a, (int)r0, nr, cs);
   __syncthreads();
-  each_unit(nr, a.per_head, [&](int r, int j, int part, int share) {
+  each_unit<true>(nr, a.per_head, h1 - h0, [&](int r, int j, int part, int share) {
     Unit<T, HALF> unit;
     unit.set(j, a.R, cs + r * (a.R / 2));
     const T *in = (const T *)x.in + (r0 + r) * x.in_stride;
@@ -173,7 +184,7 @@ __global__ __launch_bounds__(kRotThreads) void rotary_any_kernel(RopeArgs a, Row
   extern __shared__ float2 cs[];
   const int64_t r0 = (int64_t)blockIdx.x * kTileRows;
   const int nr = (int)min((int64_t)kTileRows, a.rows - r0);
-  const int h0 = blockIdx.y * heads_per, nh = min(heads_per, x.heads - h0), per = a.per_head;
+  const int h0 = blockIdx.y * heads_per, nh = min(heads_per, x.heads - h0), per = a.per_head.d;
   fill_angles(a, (int)r0, nr, cs);
   __syncthreads();
   for (int u = threadIdx.x; u < nr * nh * per; u += kRotThreads) {
@@ -285,26 +296,33 @@ __global__ __launch_bounds__(kRotThreads) void kv_write_kernel(RopeArgs a, Write
   }
   const int hq1 = min(h1, w.q.heads), k0 = max(h0 - w.q.heads, 0), k1 = min(h1 - w.q.heads, w.k.heads);
   if (h0 >= w.q.heads + w.k.heads) return;
-  each_unit(nr, a.per_head, [&](int r, int j, int part, int share) {
-    Unit<T, HALF> unit;
-    unit.set(j, a.R, cs + r * (a.R / 2));
-    const T *q = (const T *)w.q.in + (r0 + r) * w.q.in_stride, *k = (const T *)w.k.in + (r0 + r) * w.k.in_stride;
-    T *q_out = (T *)w.q.out + (r0 + r) * w.q.out_stride;
-    unit.run(h0 + part, hq1, share, [&](int h) { return q + h * D; }, [&](int h) { return q_out + h * D; });
-    const int sl = slot[r];
-    if (sl < 0) return;
-    int at;
-    T *page = page_of((T *)w.k_pool, sl, w, &at) + at * D;
-    unit.run(k0 + part, k1, share, [&](int h) { return k + h * D; },
-             [&](int h) { return page + ((int64_t)h << (w.bs_log2 + w.dh_log2)); });
-  });
+  if (hq1 > h0)
+    each_unit<false>(nr, a.per_head, hq1 - h0, [&](int r, int j, int part, int share) {
+      Unit<T, HALF> unit;
+      unit.set(j, a.R, cs + r * (a.R / 2));
+      const T *q = (const T *)w.q.in + (r0 + r) * w.q.in_stride;
+      T *out = (T *)w.q.out + (r0 + r) * w.q.out_stride;
+      unit.run(h0 + part, hq1, share, [&](int h) { return q + h * D; }, [&](int h) { return out + h * D; });
+    });
+  if (k1 > k0)
+    each_unit<false>(nr, a.per_head, k1 - k0, [&](int r, int j, int part, int share) {
+      const int sl = slot[r];
+      if (sl < 0) return;
+      Unit<T, HALF> unit;
+      unit.set(j, a.R, cs + r * (a.R / 2));
+      const T *k = (const T *)w.k.in + (r0 + r) * w.k.in_stride;
+      int at;
+      T *page = page_of((T *)w.k_pool, sl, w, &at) + at * D;
+      unit.run(k0 + part, k1, share, [&](int h) { return k + h * D; },
+               [&](int h) { return page + ((int64_t)h << (w.bs_log2 + w.dh_log2)); });
+    });
 }
 
 template <typename T, bool HALF>
 __global__ __launch_bounds__(kRotThreads) void kv_write_any_kernel(RopeArgs a, WriteArgs w, int heads_per) {
   extern __shared__ float2 cs[];
   const int64_t r0 = (int64_t)blockIdx.x * kTileRows;
-  const int nr = (int)min((int64_t)kTileRows, a.rows - r0), t = threadIdx.x, D = 1 << w.dh_log2, per = a.per_head;
+  const int nr = (int)min((int64_t)kTileRows, a.rows - r0), t = threadIdx.x, D = 1 << w.dh_log2, per = a.per_head.d;
   const int h0 = blockIdx.y * heads_per, nh = min(heads_per, w.q.heads + 2 * w.k.heads - h0);
   fill_angles(a, (int)r0, nr, cs);
   __syncthreads();
@@ -392,8 +410,9 @@ static RopeArgs rope_args(const sm_rope_params *p, const int32_t *pos, int rows,
   a.sign = transpose ? -1 : 1;
   a.scale = p->attn_scale;
   const int vec = 16 / (int)es;
-  a.per_head = !wide ? D - p->rot_dim / 2
-                     : (p->layout == SM_ROPE_HALF ? p->rot_dim / (2 * vec) : p->rot_dim / vec) + (D - p->rot_dim) / vec;
+  a.per_head = make_fastdiv(
+      !wide ? D - p->rot_dim / 2
+            : (p->layout == SM_ROPE_HALF ? p->rot_dim / (2 * vec) : p->rot_dim / vec) + (D - p->rot_dim) / vec);
   return a;
 }
 
