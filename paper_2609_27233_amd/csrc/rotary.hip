@@ -62,20 +62,52 @@ __device__ __forceinline__ float2 turned(float a, float b, float2 cs) {
   return make_float2(a * cs.x - b * cs.y, a * cs.y + b * cs.x);
 }
 
-// A thread's unit: 16 bytes of a row's head (half layout: of each half), or 16
-// bytes behind the turned part, which are copied.
-template <typename T, bool HALF>
+// V features as they lie in memory: 16, 8, 4 or 2 bytes.
+template <int BYTES> struct Raw;
+template <> struct Raw<16> { typedef u32x4_t type; };
+template <> struct Raw<8> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
+template <> struct Raw<4> { typedef uint32_t type; };
+template <> struct Raw<2> { typedef uint16_t type; };
+template <typename T, int V>
+struct Piece {
+  typedef typename Raw<V * sizeof(T)>::type raw;
+  static __device__ __forceinline__ void open(raw r, float (&f)[V]) {
+    T t[V];
+    __builtin_memcpy(t, &r, sizeof r);
+#pragma unroll
+    for (int e = 0; e < V; ++e) f[e] = Elem<T>::load(t + e);
+  }
+  static __device__ __forceinline__ raw close(const float (&f)[V]) {
+    T t[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) t[e] = Elem<T>::to_store(f[e]);
+    raw r;
+    __builtin_memcpy(&r, t, sizeof r);
+    return r;
+  }
+};
+template <> struct Piece<uint16_t, 8> {
+  typedef u32x4_t raw;
+  static __device__ __forceinline__ void open(raw r, float (&f)[8]) { Vec16<uint16_t>::open(r, f); }
+  static __device__ __forceinline__ raw close(const float (&f)[8]) { return Vec16<uint16_t>::close(f); }
+};
+
+// A thread's unit: V features of a row's head that are turned with V more
+// (half layout: the second half's; single features: a pair's other one), or
+// among themselves, or behind the turned part, where they are copied.
+template <typename T, bool HALF, int V>
 struct Unit {
-  static constexpr int N = Vec16<T>::N, NP = HALF ? N : N / 2;  // pairs
-  int at, far;  // features; far 0: no second half
+  static constexpr bool TWO = HALF || V == 1;
+  static constexpr int NP = TWO ? V : V / 2;  // pairs
+  int at, far;  // features; far 0: no second piece
   bool turning;
   float2 cs[NP];
 
   __device__ __forceinline__ void set(int j, int R, const float2 *row_cs) {
-    const int units = HALF ? R / (2 * N) : R / N;
+    const int units = TWO ? R / (2 * V) : R / V;
     turning = j < units;
-    at = turning ? j * N : R + (j - units) * N;
-    far = HALF && turning ? R / 2 : 0;
+    at = !turning ? R + (j - units) * V : HALF || !TWO ? j * V : 2 * j;
+    far = !turning || !TWO ? 0 : HALF ? R / 2 : 1;
     if (turning)
 #pragma unroll
       for (int e = 0; e < NP; ++e) cs[e] = row_cs[j * NP + e];
@@ -84,43 +116,45 @@ struct Unit {
   // feature.  The loads are unconditional (the last head's again).
   template <class In, class Out>
   __device__ __forceinline__ void run(int h, int h1, int step, In in, Out out) const {
+    typedef Piece<T, V> P;
+    typedef typename P::raw raw;
     constexpr int U = 4;
     for (; h < h1; h += U * step) {
-      u32x4_t a[U], b[U];
+      raw a[U], b[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const T *p = in(min(h + u * step, h1 - 1)) + at;
-        a[u] = *(const u32x4_t *)p;
-        if constexpr (HALF) b[u] = *(const u32x4_t *)(p + far);
+        a[u] = *(const raw *)p;
+        if constexpr (TWO) b[u] = *(const raw *)(p + far);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         if (h + u * step >= h1) break;
         T *p = out(h + u * step) + at;
         if (!turning) {
-          *(u32x4_t *)p = a[u];
+          *(raw *)p = a[u];
           continue;
         }
-        float f[N], g[N];
-        Vec16<T>::open(a[u], f);
-        if constexpr (HALF) {
-          Vec16<T>::open(b[u], g);
+        float f[V], g[V];
+        P::open(a[u], f);
+        if constexpr (TWO) {
+          P::open(b[u], g);
 #pragma unroll
-          for (int e = 0; e < N; ++e) {
+          for (int e = 0; e < V; ++e) {
             const float2 t = turned(f[e], g[e], cs[e]);
             f[e] = t.x;
             g[e] = t.y;
           }
-          *(u32x4_t *)(p + far) = Vec16<T>::close(g);
+          *(raw *)(p + far) = P::close(g);
         } else {
 #pragma unroll
-          for (int e = 0; e < N; e += 2) {
+          for (int e = 0; e < V; e += 2) {
             const float2 t = turned(f[e], f[e + 1], cs[e / 2]);
             f[e] = t.x;
             f[e + 1] = t.y;
           }
         }
-        *(u32x4_t *)p = Vec16<T>::close(f);
+        *(raw *)p = P::close(f);
       }
     }
   }
@@ -148,7 +182,7 @@ __device__ __forceinline__ void each_unit(int nr, const FastDiv &per_head, int h
   }
 }
 
-template <typename T, bool HALF>
+template <typename T, bool HALF, int V>
 __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RopeArgs a, Rows x, int D, int heads_per) {
   extern __shared__ float2 cs[];  // [rows of a tile][R / 2]
   const int64_t r0 = (int64_t)blockIdx.x * kTileRows;
@@ -157,41 +191,12 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RopeArgs a, Rows x,
   fill_angles(a, (int)r0, nr, cs);
   __syncthreads();
   each_unit<true>(nr, a.per_head, h1 - h0, [&](int r, int j, int part, int share) {
-    Unit<T, HALF> unit;
+    Unit<T, HALF, V> unit;
     unit.set(j, a.R, cs + r * (a.R / 2));
     const T *in = (const T *)x.in + (r0 + r) * x.in_stride;
     T *out = (T *)x.out + (r0 + r) * x.out_stride;
     unit.run(h0 + part, h1, share, [&](int h) { return in + h * D; }, [&](int h) { return out + h * D; });
   });
-}
-
-// Rows, heads or strides that 16 bytes do not divide: a pair or a copied
-// feature at a time.  Unit j of a head at `in` to `out`.
-template <typename T, bool HALF>
-__device__ __forceinline__ void turn_one(const T *in, T *out, int j, int R, const float2 *cs) {
-  if (j >= R / 2) {
-    out[R / 2 + j] = in[R / 2 + j];
-    return;
-  }
-  const int i0 = HALF ? j : 2 * j, i1 = HALF ? j + R / 2 : 2 * j + 1;
-  const float2 t = turned(Elem<T>::load(in + i0), Elem<T>::load(in + i1), cs[j]);
-  out[i0] = Elem<T>::to_store(t.x);
-  out[i1] = Elem<T>::to_store(t.y);
-}
-
-template <typename T, bool HALF>
-__global__ __launch_bounds__(kRotThreads) void rotary_any_kernel(RopeArgs a, Rows x, int D, int heads_per) {
-  extern __shared__ float2 cs[];
-  const int64_t r0 = (int64_t)blockIdx.x * kTileRows;
-  const int nr = (int)min((int64_t)kTileRows, a.rows - r0);
-  const int h0 = blockIdx.y * heads_per, nh = min(heads_per, x.heads - h0), per = a.per_head.d;
-  fill_angles(a, (int)r0, nr, cs);
-  __syncthreads();
-  for (int u = threadIdx.x; u < nr * nh * per; u += kRotThreads) {
-    const int hr = u / per, j = u - hr * per, r = hr / nh, h = h0 + hr - r * nh;
-    turn_one<T, HALF>((const T *)x.in + (r0 + r) * x.in_stride + h * D, (T *)x.out + (r0 + r) * x.out_stride + h * D, j,
-                      a.R, cs + r * (a.R / 2));
-  }
 }
 
 // ---------------------------------------------------------------------------
@@ -298,7 +303,7 @@ __global__ __launch_bounds__(kRotThreads) void kv_write_kernel(RopeArgs a, Write
   if (h0 >= w.q.heads + w.k.heads) return;
   if (hq1 > h0)
     each_unit<false>(nr, a.per_head, hq1 - h0, [&](int r, int j, int part, int share) {
-      Unit<T, HALF> unit;
+      Unit<T, HALF, VEC> unit;
       unit.set(j, a.R, cs + r * (a.R / 2));
       const T *q = (const T *)w.q.in + (r0 + r) * w.q.in_stride;
       T *out = (T *)w.q.out + (r0 + r) * w.q.out_stride;
@@ -308,7 +313,7 @@ __global__ __launch_bounds__(kRotThreads) void kv_write_kernel(RopeArgs a, Write
     each_unit<false>(nr, a.per_head, k1 - k0, [&](int r, int j, int part, int share) {
       const int sl = slot[r];
       if (sl < 0) return;
-      Unit<T, HALF> unit;
+      Unit<T, HALF, VEC> unit;
       unit.set(j, a.R, cs + r * (a.R / 2));
       const T *k = (const T *)w.k.in + (r0 + r) * w.k.in_stride;
       int at;
@@ -318,41 +323,49 @@ __global__ __launch_bounds__(kRotThreads) void kv_write_kernel(RopeArgs a, Write
     });
 }
 
+// Rows or strides that 16 bytes do not divide: a feature at a time.
 template <typename T, bool HALF>
 __global__ __launch_bounds__(kRotThreads) void kv_write_any_kernel(RopeArgs a, WriteArgs w, int heads_per) {
   extern __shared__ float2 cs[];
+  __shared__ int slot[kTileRows];
   const int64_t r0 = (int64_t)blockIdx.x * kTileRows;
-  const int nr = (int)min((int64_t)kTileRows, a.rows - r0), t = threadIdx.x, D = 1 << w.dh_log2, per = a.per_head.d;
-  const int h0 = blockIdx.y * heads_per, nh = min(heads_per, w.q.heads + 2 * w.k.heads - h0);
-  fill_angles(a, (int)r0, nr, cs);
-  __syncthreads();
-  for (int rh = t >> 6; rh < nr * nh; rh += kRotThreads / 64) {  // a wave per head of a row
-    const int r = rh / nh, h = h0 + rh - r * nh, hk = h - w.q.heads, hv = hk - w.k.heads;
-    const int64_t row = r0 + r;
-    const float2 *rcs = cs + r * (a.R / 2);
-    if (hk < 0) {
-      for (int j = t & 63; j < per; j += 64)
-        turn_one<T, HALF>((const T *)w.q.in + row * w.q.in_stride + h * D, (T *)w.q.out + row * w.q.out_stride + h * D, j,
-                          a.R, rcs);
-      continue;
-    }
-    const int s = w.slots[row];
-    if (s < -1 || s >= w.num_slots) {
-      if (hk == 0 && (t & 63) == 0) set_err(w.err, SM_ERR_EINVAL);
-      continue;
-    }
-    if (s < 0) continue;
-    int at;
-    if (hv < 0) {
-      T *out = page_of((T *)w.k_pool, s, w, &at) + (((int64_t)hk << w.bs_log2) + at) * D;
-      for (int j = t & 63; j < per; j += 64)
-        turn_one<T, HALF>((const T *)w.k.in + row * w.k.in_stride + hk * D, out, j, a.R, rcs);
-    } else {
-      T *out = page_of((T *)w.v_pool, s, w, &at) + at;
-      for (int d = t & 63; d < D; d += 64)
-        out[((int64_t)hv * D + d) << w.bs_log2] = ((const T *)w.v.in)[row * w.v.in_stride + hv * D + d];
-    }
+  const int nr = (int)min((int64_t)kTileRows, a.rows - r0), t = threadIdx.x, D = 1 << w.dh_log2;
+  const int h0 = blockIdx.y * heads_per, h1 = min(h0 + heads_per, w.q.heads + 2 * w.k.heads);
+  if (t < nr) {
+    const int s = w.slots[r0 + t];
+    const bool bad = s < -1 || s >= w.num_slots;
+    if (bad && h0 == 0) set_err(w.err, SM_ERR_EINVAL);
+    slot[t] = bad ? -1 : s;
   }
+  if (h0 < w.q.heads + w.k.heads) fill_angles(a, (int)r0, nr, cs);
+  __syncthreads();
+  const int hq1 = min(h1, w.q.heads), k0 = max(h0 - w.q.heads, 0), k1 = min(h1 - w.q.heads, w.k.heads);
+  const int g0 = max(h0 - w.q.heads - w.k.heads, 0), g1 = h1 - w.q.heads - w.k.heads;
+  int at;
+  for (int r = 0; r < nr && g1 > g0; ++r) {
+    if (slot[r] < 0) continue;
+    const T *in = (const T *)w.v.in + (r0 + r) * w.v.in_stride;
+    T *out = page_of((T *)w.v_pool, slot[r], w, &at) + at;
+    for (int hd = g0 * D + t; hd < g1 * D; hd += kRotThreads) out[(int64_t)hd << w.bs_log2] = in[hd];
+  }
+  if (hq1 > h0)
+    each_unit<true>(nr, a.per_head, hq1 - h0, [&](int r, int j, int part, int share) {
+      Unit<T, HALF, 1> unit;
+      unit.set(j, a.R, cs + r * (a.R / 2));
+      const T *q = (const T *)w.q.in + (r0 + r) * w.q.in_stride;
+      T *out = (T *)w.q.out + (r0 + r) * w.q.out_stride;
+      unit.run(h0 + part, hq1, share, [&](int h) { return q + h * D; }, [&](int h) { return out + h * D; });
+    });
+  if (k1 > k0)
+    each_unit<true>(nr, a.per_head, k1 - k0, [&](int r, int j, int part, int share) {
+      if (slot[r] < 0) return;
+      Unit<T, HALF, 1> unit;
+      unit.set(j, a.R, cs + r * (a.R / 2));
+      const T *k = (const T *)w.k.in + (r0 + r) * w.k.in_stride;
+      T *page = page_of((T *)w.k_pool, slot[r], w, &at) + at * D;
+      unit.run(k0 + part, k1, share, [&](int h) { return k + h * D; },
+               [&](int h) { return page + ((int64_t)h << (w.bs_log2 + w.dh_log2)); });
+    });
 }
 
 }  // namespace sm
@@ -396,12 +409,18 @@ static void set_turns(const sm_rope_params *p, RopeArgs *a) {
   }
 }
 
-static bool wide_rows(const void *p, int64_t stride, size_t es) {
-  return (uintptr_t)p % 16 == 0 && stride * es % 16 == 0;
+static bool aligned(const void *p, int64_t stride, int64_t bytes, int64_t es) {
+  return (uintptr_t)p % bytes == 0 && stride * es % bytes == 0;
 }
 
-static RopeArgs rope_args(const sm_rope_params *p, const int32_t *pos, int rows, int D, size_t es, bool wide,
-                          int transpose) {
+// Whether pieces of v features divide a head's turned part (half layout: each
+// half of it) and the rest.
+static bool divides(const sm_rope_params *p, int D, int v) {
+  return (p->layout == SM_ROPE_HALF ? p->rot_dim / 2 : p->rot_dim) % v == 0 && (D - p->rot_dim) % v == 0;
+}
+
+// v: features of a piece
+static RopeArgs rope_args(const sm_rope_params *p, const int32_t *pos, int rows, int D, int v, int transpose) {
   RopeArgs a;
   set_turns(p, &a);
   a.pos = pos;
@@ -409,16 +428,8 @@ static RopeArgs rope_args(const sm_rope_params *p, const int32_t *pos, int rows,
   a.R = p->rot_dim;
   a.sign = transpose ? -1 : 1;
   a.scale = p->attn_scale;
-  const int vec = 16 / (int)es;
-  a.per_head = make_fastdiv(
-      !wide ? D - p->rot_dim / 2
-            : (p->layout == SM_ROPE_HALF ? p->rot_dim / (2 * vec) : p->rot_dim / vec) + (D - p->rot_dim) / vec);
+  a.per_head = make_fastdiv(p->rot_dim / (p->layout == SM_ROPE_HALF || v == 1 ? 2 * v : v) + (D - p->rot_dim) / v);
   return a;
-}
-
-static bool wide_head(const sm_rope_params *p, int D, size_t es) {
-  const int vec = 16 / (int)es;
-  return D % vec == 0 && p->rot_dim % (2 * vec) == 0;
 }
 
 // Heads per workgroup: enough workgroups for the device where there are few rows.
@@ -428,15 +439,14 @@ static int heads_per_wg(int heads, int64_t tiles) {
   return per;
 }
 
-template <typename T>
-static void launch_rotary(const RopeArgs &a, const Rows &x, int D, bool half, bool wide, hipStream_t stream) {
+template <typename T, int V>
+static void launch_rotary(const RopeArgs &a, const Rows &x, int D, bool half, hipStream_t stream) {
   const int64_t tiles = ((int64_t)a.rows + kTileRows - 1) / kTileRows;
   const int per = heads_per_wg(x.heads, tiles);
   const dim3 grid((unsigned)tiles, (x.heads + per - 1) / per);
   const size_t lds = kTileRows * (a.R / 2) * sizeof(float2);
-  const auto kernel = wide ? (half ? rotary_kernel<T, true> : rotary_kernel<T, false>)
-                           : (half ? rotary_any_kernel<T, true> : rotary_any_kernel<T, false>);
-  hipLaunchKernelGGL(kernel, grid, dim3(kRotThreads), lds, stream, a, x, D, per);
+  hipLaunchKernelGGL((half ? rotary_kernel<T, true, V> : rotary_kernel<T, false, V>), grid, dim3(kRotThreads), lds, stream,
+                     a, x, D, per);
 }
 
 SM_API sm_status sm_rotary(const void *x, int64_t x_stride, const int32_t *pos, int rows, int heads, int head_dim,
@@ -449,12 +459,23 @@ SM_API sm_status sm_rotary(const void *x, int64_t x_stride, const int32_t *pos, 
   if (x_stride < width || out_stride < width || (transpose != 0 && transpose != 1)) return SM_EINVAL;
   if (rows == 0) return SM_OK;
   if (!x || !pos || !out) return SM_EINVAL;
-  const size_t es = dt == SM_BF16 ? 2 : 4;
-  const bool wide = wide_head(p, head_dim, es) && wide_rows(x, x_stride, es) && wide_rows(out, out_stride, es);
-  const RopeArgs a = rope_args(p, pos, rows, head_dim, es, wide, transpose);
+  const int es = dt == SM_BF16 ? 2 : 4;
+  int v = 16 / es;  // features of a piece: the most that divide the head and are aligned in every row
+  while (v > 1 && !(divides(p, head_dim, v) && aligned(x, x_stride, v * es, es) && aligned(out, out_stride, v * es, es)))
+    v /= 2;
+  const RopeArgs a = rope_args(p, pos, rows, head_dim, v, transpose);
   const Rows r{x, out, x_stride, out_stride, heads};
-  if (dt == SM_BF16) launch_rotary<uint16_t>(a, r, head_dim, p->layout == SM_ROPE_HALF, wide, stream);
-  else launch_rotary<float>(a, r, head_dim, p->layout == SM_ROPE_HALF, wide, stream);
+  const bool half = p->layout == SM_ROPE_HALF;
+  if (dt == SM_BF16) {
+    if (v == 8) launch_rotary<uint16_t, 8>(a, r, head_dim, half, stream);
+    else if (v == 4) launch_rotary<uint16_t, 4>(a, r, head_dim, half, stream);
+    else if (v == 2) launch_rotary<uint16_t, 2>(a, r, head_dim, half, stream);
+    else launch_rotary<uint16_t, 1>(a, r, head_dim, half, stream);
+  } else {
+    if (v == 4) launch_rotary<float, 4>(a, r, head_dim, half, stream);
+    else if (v == 2) launch_rotary<float, 2>(a, r, head_dim, half, stream);
+    else launch_rotary<float, 1>(a, r, head_dim, half, stream);
+  }
   return hipGetLastError() == hipSuccess ? SM_OK : SM_EHIP;
 }
 
@@ -482,11 +503,11 @@ SM_API sm_status sm_kv_write_rotary(const sm_paged_cache *c, const int32_t *pos,
   if (num_q_heads > 0 && (q_stride < q_width || q_out_stride < q_width)) return SM_EINVAL;
   if (rows == 0) return SM_OK;
   if (!pos || !slots || !k || !v || (num_q_heads > 0 && (!q || !q_out))) return SM_EINVAL;
-  const size_t es = c->dtype == SM_BF16 ? 2 : 4;
-  const bool wide = wide_head(p, D, es) && wide_rows(k, k_stride, es) && wide_rows(v, v_stride, es) &&
-                    wide_rows(c->k_pool, 0, es) && wide_rows(c->v_pool, 0, es) &&
-                    (num_q_heads == 0 || (wide_rows(q, q_stride, es) && wide_rows(q_out, q_out_stride, es)));
-  const RopeArgs a = rope_args(p, pos, rows, D, es, wide, 0);
+  const int es = c->dtype == SM_BF16 ? 2 : 4;
+  const bool wide = divides(p, D, 16 / es) && aligned(k, k_stride, 16, es) && aligned(v, v_stride, 16, es) &&
+                    aligned(c->k_pool, 0, 16, es) && aligned(c->v_pool, 0, 16, es) &&
+                    (num_q_heads == 0 || (aligned(q, q_stride, 16, es) && aligned(q_out, q_out_stride, 16, es)));
+  const RopeArgs a = rope_args(p, pos, rows, D, wide ? 16 / es : 1, 0);
   WriteArgs w{Rows{q, q_out, q_stride, q_out_stride, num_q_heads}, Rows{k, nullptr, k_stride, 0, c->num_kv_heads},
               Rows{v, nullptr, v_stride, 0, c->num_kv_heads}, slots, c->k_pool, c->v_pool, c->err, ca.bs_log2,
               ca.dh_log2, c->num_blocks * c->block_size};
