@@ -5,9 +5,14 @@
 // (fp32) between the norms, so both norms, the gate and the sum cost no
 // traffic beyond h, y, h_out and n_out, which bound the call.  LayerNorm
 // takes its mean first and sums squares of the differences from registers.
+//
+// A row is held by 8 threads to 1024, two 16-byte chunks each, so that its
+// loads are all in flight at once and short rows fill a wave.  Rows that 16
+// bytes do not divide are read by the same chunks at the alignment they have,
+// the last one by features.
 #include <cmath>
 
-#include "common.hpp"
+#include "vec16.hpp"
 
 namespace sm {
 
@@ -23,124 +28,150 @@ struct NormArgs {
   float scale, eps_post, eps_pre;
 };
 
-// Sum over the WPR waves that hold a row; `red`: WPR floats of the row's own.
-template <int WPR>
+// Sum over the TPR threads that hold a row; `red`: a float for each of their waves.
+template <int TPR>
 __device__ __forceinline__ float row_sum(float v, float *red) {
-  v = wave_sum(v);
-  if constexpr (WPR > 1) {
-    const int w = (threadIdx.x >> 6) % WPR;
+  if constexpr (TPR < 64) {
+    v += dpp_f32<kDppXor1>(v);
+    v += dpp_f32<kDppXor2>(v);
+    v += dpp_f32<kDppHalfMirror>(v);
+    if constexpr (TPR == 32) {
+      v += dpp_f32<kDppMirror>(v);
+      float a, b;
+      swap16(v, a, b);
+      v = a + b;
+    }
+  } else {
+    v = wave_sum(v);
+  }
+  if constexpr (TPR > 64) {
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[w] = v;
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
     __syncthreads();
     v = 0.f;
 #pragma unroll
-    for (int i = 0; i < WPR; ++i) v += red[i];
+    for (int i = 0; i < TPR / 64; ++i) v += red[i];
   }
   return v;
 }
 
-template <typename T, int VEC>
-struct Chunk {  // VEC features at once
+// 16 bytes of features.  WHOLE: every chunk of a row is 16-byte aligned and
+// within it; else at any address, and cut at feature d.
+template <typename T, bool WHOLE>
+struct Chunk {
+  static constexpr int VEC = Vec16<T>::N;
   float f[VEC];
-  __device__ __forceinline__ void load(const void *p, int64_t at) {
-    if constexpr (VEC == 1) {
-      f[0] = Elem<T>::load((const T *)p + at);
-    } else if constexpr (sizeof(T) == 4) {
-      const u32x4_t v = *(const u32x4_t *)((const T *)p + at);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(v[i]);
-    } else {
-      const u32x4_t v = *(const u32x4_t *)((const T *)p + at);
+  __device__ __forceinline__ void load(const void *row, int64_t offset, int at, int d) {
+    const T *p = (const T *)row + offset + at;
+    u32x4_t v;
+    if (WHOLE) {
+      Vec16<T>::open(*(const u32x4_t *)p, f);
+    } else if (at + VEC <= d) {
+      __builtin_memcpy(&v, p, 16);
+      Vec16<T>::open(v, f);
+    } else {  // whole words, and for bf16 a half
+      const int n = (d - at) * (int)sizeof(T);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        f[2 * i] = __uint_as_float(v[i] << 16);
-        f[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+        uint32_t x = 0;
+        if (4 * i + 4 <= n) __builtin_memcpy(&x, (const char *)p + 4 * i, 4);
+        else if (4 * i < n) x = *(const uint16_t *)((const char *)p + 4 * i);
+        v[i] = x;
       }
+      Vec16<T>::open(v, f);
     }
   }
-  __device__ __forceinline__ void store(void *p, int64_t at) const {
-    if constexpr (VEC == 1) {
-      ((T *)p)[at] = Elem<T>::to_store(f[0]);
-    } else if constexpr (sizeof(T) == 4) {
-      *(u32x4_t *)((T *)p + at) = u32x4_t{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]),
-                                          __float_as_uint(f[3])};
+  __device__ __forceinline__ void store(void *row, int64_t offset, int at, int d) const {
+    T *p = (T *)row + offset + at;
+    const u32x4_t v = Vec16<T>::close(f);
+    if (WHOLE) {
+      *(u32x4_t *)p = v;
+    } else if (at + VEC <= d) {
+      __builtin_memcpy(p, &v, 16);
     } else {
-      *(u32x4_t *)((T *)p + at) = u32x4_t{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]),
-                                          pack_bf16x2(f[6], f[7])};
+      const int n = (d - at) * (int)sizeof(T);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t x = v[i];
+        if (4 * i + 4 <= n) __builtin_memcpy((char *)p + 4 * i, &x, 4);
+        else if (4 * i < n) *(uint16_t *)((char *)p + 4 * i) = (uint16_t)x;
+      }
     }
   }
 };
 
-// x <- norm(x), the row spread over WPR waves, NV chunks a thread.
-template <typename T, int VEC, int NV, int WPR>
-__device__ __forceinline__ void norm_row(Chunk<T, VEC> (&x)[NV], int kind, float eps, const void *gain, const void *bias,
-                                         int d, int lane0, float *red) {
-  constexpr int STEP = 64 * WPR * VEC;
-  float mean = 0.f;
+// x <- norm(x), the row spread over TPR threads, NV chunks a thread.
+template <typename T, bool WHOLE, int NV, int TPR>
+__device__ __forceinline__ void norm_row(Chunk<T, WHOLE> (&x)[NV], int kind, float eps, const void *gain, const void *bias,
+                                         int d, int at0, float *red) {
+  constexpr int VEC = Vec16<T>::N, STEP = TPR * VEC;
   if (kind == SM_NORM_LAYER) {
     float s = 0.f;
 #pragma unroll
     for (int v = 0; v < NV; ++v)
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) s += x[v].f[e];  // (chunks past d hold zeros)
-    mean = row_sum<WPR>(s, red) / d;
+      for (int e = 0; e < VEC; ++e) s += x[v].f[e];  // (features past d are zeros)
+    const float mean = row_sum<TPR>(s, red) / d;
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e)
+        if (at0 + v * STEP + (WHOLE ? 0 : e) < d) x[v].f[e] -= mean;
   }
   float q = 0.f;
 #pragma unroll
   for (int v = 0; v < NV; ++v)
-    if (lane0 + v * STEP < d)
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        x[v].f[e] -= mean;
-        q += x[v].f[e] * x[v].f[e];
-      }
-  const float inv = 1.f / sqrtf(row_sum<WPR>(q, red) / d + eps);
-#pragma unroll
-  for (int v = 0; v < NV; ++v)
-    if (lane0 + v * STEP < d) {
-      Chunk<T, VEC> g, b;
-      if (gain) g.load(gain, lane0 + v * STEP);
-      if (bias) b.load(bias, lane0 + v * STEP);
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        float n = x[v].f[e] * inv;
-        if (gain) n *= g.f[e];
-        if (bias) n += b.f[e];
-        x[v].f[e] = n;
-      }
-    }
-}
-
-constexpr int wg_threads(int wpr) { return wpr < 4 ? 256 : 64 * wpr; }
-
-// WPR waves hold a row, NV chunks of VEC features a thread.
-template <typename T, int VEC, int NV, int WPR>
-__global__ __launch_bounds__(wg_threads(WPR)) void block_norm_kernel(NormArgs a) {
-  constexpr int RPW = wg_threads(WPR) / (64 * WPR);  // rows per workgroup
-  constexpr int STEP = 64 * WPR * VEC;
-  __shared__ float red[WPR];  // (several waves to a row: one row per workgroup)
-  const int64_t r = (int64_t)blockIdx.x * RPW + threadIdx.x / (64 * WPR);
-  if (r >= a.rows) return;  // (whole waves, and never a part of a row)
-  const int lane0 = threadIdx.x % (64 * WPR) * VEC;
-  Chunk<T, VEC> h[NV], y[NV];
+    for (int e = 0; e < VEC; ++e) q += x[v].f[e] * x[v].f[e];
+  const float inv = 1.f / sqrtf(row_sum<TPR>(q, red) / d + eps);
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
-    const int at = lane0 + v * STEP;
+    const int at = at0 + v * STEP;
+    if (at >= d) continue;
+    Chunk<T, WHOLE> g, b;
+    if (gain) g.load(gain, 0, at, d);
+    if (bias) b.load(bias, 0, at, d);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      float n = x[v].f[e] * inv;
+      if (gain) n *= g.f[e];
+      if (bias) n += b.f[e];
+      x[v].f[e] = n;
+    }
+  }
+}
+
+constexpr int wg_threads(int tpr) { return tpr <= 64 ? 256 : tpr; }
+
+// TPR threads hold a row, NV chunks each.
+template <typename T, bool WHOLE, int NV, int TPR>
+__global__ __launch_bounds__(wg_threads(TPR)) void block_norm_kernel(NormArgs a) {
+  constexpr int RPW = wg_threads(TPR) / TPR;  // rows per workgroup
+  constexpr int VEC = Vec16<T>::N, STEP = TPR * VEC;
+  __shared__ float red[TPR > 64 ? TPR / 64 : 1];  // (several waves to a row: one row per workgroup)
+  const int64_t row = (int64_t)blockIdx.x * RPW + threadIdx.x / TPR;
+  const bool there = row < a.rows;
+  const int64_t r = there ? row : a.rows - 1;  // (all lanes take part in the sums)
+  const int at0 = threadIdx.x % TPR * VEC;
+  Chunk<T, WHOLE> h[NV], y[NV];
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const int at = at0 + v * STEP;
 #pragma unroll
     for (int e = 0; e < VEC; ++e) h[v].f[e] = y[v].f[e] = 0.f;
     if (at < a.d) {
-      h[v].load(a.h, r * a.sh + at);
-      if (a.y) y[v].load(a.y, r * a.sy + at);
+      h[v].load(a.h, r * a.sh, at, a.d);
+      if (a.y) y[v].load(a.y, r * a.sy, at, a.d);
     }
   }
   if (a.y) {
-    if (a.post != kNone) norm_row<T, VEC, NV, WPR>(y, a.post, a.eps_post, a.g_post, a.b_post, a.d, lane0, red);
+    if (a.post != kNone) norm_row<T, WHOLE, NV, TPR>(y, a.post, a.eps_post, a.g_post, a.b_post, a.d, at0, red);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int at = lane0 + v * STEP;
+      const int at = at0 + v * STEP;
       if (at >= a.d) continue;
-      Chunk<T, VEC> g;
-      if (a.gate) g.load(a.gate, r * a.sg + at);
+      Chunk<T, WHOLE> g;
+      if (a.gate) g.load(a.gate, r * a.sg, at, a.d);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
         const float t = a.gate ? y[v].f[e] * g.f[e] : y[v].f[e];
@@ -148,36 +179,35 @@ __global__ __launch_bounds__(wg_threads(WPR)) void block_norm_kernel(NormArgs a)
       }
     }
   }
-  if (a.h_out)
+  if (a.h_out && there)
 #pragma unroll
     for (int v = 0; v < NV; ++v)
-      if (lane0 + v * STEP < a.d) h[v].store(a.h_out, r * a.sho + lane0 + v * STEP);
+      if (at0 + v * STEP < a.d) h[v].store(a.h_out, r * a.sho, at0 + v * STEP, a.d);
   if (!a.n_out) return;
-  norm_row<T, VEC, NV, WPR>(h, a.pre, a.eps_pre, a.g_pre, a.b_pre, a.d, lane0, red);
+  norm_row<T, WHOLE, NV, TPR>(h, a.pre, a.eps_pre, a.g_pre, a.b_pre, a.d, at0, red);
+  if (there)
 #pragma unroll
-  for (int v = 0; v < NV; ++v)
-    if (lane0 + v * STEP < a.d) h[v].store(a.n_out, r * a.sno + lane0 + v * STEP);
+    for (int v = 0; v < NV; ++v)
+      if (at0 + v * STEP < a.d) h[v].store(a.n_out, r * a.sno, at0 + v * STEP, a.d);
 }
 
-template <typename T, int VEC, int NV, int WPR>
+template <typename T, bool WHOLE, int NV, int TPR>
 static void launch(const NormArgs &a, hipStream_t stream) {
-  constexpr int RPW = wg_threads(WPR) / (64 * WPR);
-  hipLaunchKernelGGL((block_norm_kernel<T, VEC, NV, WPR>), dim3((unsigned)(((int64_t)a.rows + RPW - 1) / RPW)),
-                     dim3(wg_threads(WPR)), 0, stream, a);
+  constexpr int RPW = wg_threads(TPR) / TPR;
+  hipLaunchKernelGGL((block_norm_kernel<T, WHOLE, NV, TPR>), dim3((unsigned)(((int64_t)a.rows + RPW - 1) / RPW)),
+                     dim3(wg_threads(TPR)), 0, stream, a);
 }
 
-template <typename T>
-static void launch_block_norm(const NormArgs &a, bool wide, hipStream_t stream) {
-  constexpr int VEC = 16 / sizeof(T);
-  if (wide) {
-    if (a.d <= 64 * VEC * 2) return launch<T, VEC, 2, 1>(a, stream);
-    if (a.d <= 256 * VEC * 2) return launch<T, VEC, 2, 4>(a, stream);
-    if (a.d <= 512 * VEC * 2) return launch<T, VEC, 2, 8>(a, stream);
-    return launch<T, VEC, 16 / VEC, 16>(a, stream);  // 1024 threads: 2 (bf16) or 4 chunks each
-  }
-  if (a.d <= 64 * 16) return launch<T, 1, 16, 1>(a, stream);
-  if (a.d <= 256 * 16) return launch<T, 1, 16, 4>(a, stream);
-  launch<T, 1, 16, 16>(a, stream);
+template <typename T, bool WHOLE>
+static void launch_block_norm(const NormArgs &a, hipStream_t stream) {
+  constexpr int VEC = Vec16<T>::N;
+  if (a.d <= 8 * VEC * 2) return launch<T, WHOLE, 2, 8>(a, stream);
+  if (a.d <= 32 * VEC * 2) return launch<T, WHOLE, 2, 32>(a, stream);
+  if (a.d <= 64 * VEC * 2) return launch<T, WHOLE, 2, 64>(a, stream);
+  if (a.d <= 128 * VEC * 2) return launch<T, WHOLE, 2, 128>(a, stream);
+  if (a.d <= 256 * VEC * 2) return launch<T, WHOLE, 2, 256>(a, stream);
+  if (a.d <= 512 * VEC * 2) return launch<T, WHOLE, 2, 512>(a, stream);
+  launch<T, WHOLE, 16 / VEC, 1024>(a, stream);  // d <= 16384: 2 (bf16) or 4 chunks
 }
 
 static bool norm_ok(const sm_norm *n) {
@@ -209,7 +239,7 @@ SM_API sm_status sm_block_norm(const void *h, int64_t h_stride, const void *y, i
              pre ? pre->bias : nullptr, h_out, n_out, h_stride, y_stride, gate_stride, h_out_stride, n_out_stride,
              rows, d, post ? post->kind : kNone, pre ? pre->kind : kNone, scale, post ? post->eps : 0.f,
              pre ? pre->eps : 0.f};
-  if (dt == SM_BF16) launch_block_norm<uint16_t>(a, wide, stream);
-  else launch_block_norm<float>(a, wide, stream);
+  if (dt == SM_BF16) wide ? launch_block_norm<uint16_t, true>(a, stream) : launch_block_norm<uint16_t, false>(a, stream);
+  else wide ? launch_block_norm<float, true>(a, stream) : launch_block_norm<float, false>(a, stream);
   return hipGetLastError() == hipSuccess ? SM_OK : SM_EHIP;
 }
