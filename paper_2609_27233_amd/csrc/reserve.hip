@@ -19,28 +19,12 @@ struct ReserveArgs {
   int32_t *row_offsets, *pos, *slots;
 };
 
-// Inclusive prefix sum over kMetaThreads threads in 64 bits; `red` needs 16.
-__device__ __forceinline__ int64_t scan64(int64_t v, int64_t *red, int64_t *total) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const int64_t u = __shfl_up(v, off, kWave);
-    if (lane >= off) v += u;
-  }
-  __syncthreads();
-  if (lane == 63) red[w] = v;
-  __syncthreads();
-  int64_t before = 0, tot = 0;
-  for (int i = 0; i < kMetaThreads / 64; ++i) {
-    if (i < w) before += red[i];
-    tot += red[i];
-  }
-  *total = tot;
-  return v + before;
-}
+// Sums that stay at 2^32 - 1 once they pass it: bad counts cannot wrap round
+// to a small total.
+__device__ __forceinline__ uint32_t sum_of(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
 
 // first i in [0, n) with ends[i] > x (x < ends[n - 1])
-__device__ __forceinline__ int first_past(const int *ends, int n, int x) {
+__device__ __forceinline__ int first_past(const uint32_t *ends, int n, uint32_t x) {
   int lo = 0, hi = n - 1;
   while (lo < hi) {
     const int mid = (lo + hi) >> 1;
@@ -50,165 +34,251 @@ __device__ __forceinline__ int first_past(const int *ends, int n, int x) {
   return lo;
 }
 
+constexpr int kHeld = 2048;  // blocks whose numbers stay in LDS
+constexpr int kOwn = 4;      // and in a thread's registers
+
+enum { kRows, kFreed, kTaken, kSums };
+
+template <int NT>
 struct ReserveShared {
-  int64_t red[16];
-  int ids[kMetaThreads];
-  int keep[kMetaThreads];       // entries kept
-  int row_end[kMetaThreads];    // inclusive prefix sums of the rows,
-  int freed_end[kMetaThreads];  // of the blocks given back
-  int taken_end[kMetaThreads];  // and of the blocks taken
-  int fl_inval, fl_range, fl_stack, s_err, s_top;
+  int table[2 * NT];           // sequence ids seen (hashed)
+  int ids[NT], keep[NT];       // sequence, entries kept
+  int tail[NT];                // the partly filled page that a request's first row goes to
+  uint32_t end[kSums][NT];     // inclusive prefix sums of rows, blocks given back, blocks taken
+  uint32_t waves[kSums][NT / 64];
+  int freed[kHeld], taken[kHeld];
+  int flags;                   // 1: bad argument, 2: out of range, 4: corrupt table or stack
 };
 
-// The position and slot of row r: of request i, which ends[] names.
-__device__ __forceinline__ void put_row(const CacheArgs &c, const ReserveArgs &a, int r, int s, int p) {
-  const int blk = c.block_table[(int64_t)s * c.max_blocks + (p >> c.bs_log2)];
-  a.pos[r] = p;
-  a.slots[r] = (blk << c.bs_log2) + (p & ((1 << c.bs_log2) - 1));
+// Whether another thread's request has put the same id into the table (2 NT
+// places for NT ids: the search ends).
+template <int NT>
+__device__ __forceinline__ bool seen_before(int *table, int s) {
+  for (uint32_t at = (uint32_t)s * 2654435761u >> (32 - __builtin_ctz(2 * NT));; at = (at + 1) & (2 * NT - 1)) {
+    const int was = atomicCAS(&table[at], -1, s);
+    if (was == -1) return false;
+    if (was == s) return true;
+  }
 }
 
-// The checks and the block moves; returns 0 when all of it was applied, else
-// the error bit (uniform).
-__device__ int reserve_meta(const CacheArgs &c, const ReserveArgs &a, ReserveShared &sh) {
-  const int t = threadIdx.x;
-  const bool active = t < a.n;
+// By one workgroup, request t on thread t (n <= NT).  Dependent reads: the
+// request and the cache's state, its length, the blocks concerned; a request
+// whose page has room for its rows moves no block.  HERE: positions and slots
+// in this launch too.
+template <int NT, bool HERE>
+__global__ __launch_bounds__(NT) void reserve_kernel(CacheArgs c, ReserveArgs a) {
+  __shared__ ReserveShared<NT> sh;
+  const int t = threadIdx.x, n = a.n, bs = 1 << c.bs_log2;
+  const bool active = t < n;
   const int s = active ? a.seq_ids[t] : -1, k = active && a.crop ? a.crop[t] : 0, m = active ? a.rows[t] : 0;
-  sh.ids[t] = s;
-  if (t == 0) {
-    sh.fl_inval = sh.fl_range = sh.fl_stack = 0;
-    sh.s_err = *c.err;
-    sh.s_top = *c.free_top;
-  }
+  const int err = *c.err, top = *c.free_top;
+  const bool known = s >= 0 && s < c.max_seqs;
+  const int L = known ? c.lengths[s] : 0;
+  sh.table[t] = sh.table[NT + t] = -1;
+  if (t == 0) sh.flags = 0;
   __syncthreads();
-  if (sh.s_err != 0) return sh.s_err;  // sticky: the cache is frozen
-  if (active && (k < 0 || m < 0 || !id_ok(sh.ids, t, s, c.max_seqs))) sh.fl_inval = 1;
-  int64_t total_rows;
-  const int64_t row_end = scan64(m < 0 ? 0 : m, sh.red, &total_rows);  // (its barriers: the flag is there)
-  const int top = sh.s_top;
-  if (sh.fl_inval || total_rows > a.max_rows || top < 0 || top > c.num_blocks) return SM_ERR_EINVAL;
-  const int cap = c.max_blocks << c.bs_log2;
-  int keep = 0, had = 0, kept = 0, want = 0;
+  int flags = 0, keep = 0;
+  uint32_t sum[kSums] = {};
   if (active) {
-    const int L = c.lengths[s];
-    if (L < 0 || L > cap || k > L || (int64_t)L - k + m > cap) {
-      sh.fl_range = 1;
-    } else {
+    if (!known || k < 0 || m < 0 || seen_before<NT>(sh.table, s)) flags = 1;
+    if (L < 0 || L > c.max_blocks << c.bs_log2 || k > L || (int64_t)L - k + m > c.max_blocks << c.bs_log2) {
+      flags |= 2;
+    } else if (!flags) {
       keep = L - k;
-      had = blocks_for(L, c.bs_log2);
-      kept = blocks_for(keep, c.bs_log2);
-      want = blocks_for(keep + m, c.bs_log2);
+      const int kept = blocks_for(keep, c.bs_log2);
+      sum[kFreed] = blocks_for(L, c.bs_log2) - kept;
+      sum[kTaken] = blocks_for(keep + m, c.bs_log2) - kept;
+    }
+    sum[kRows] = max(m, 0);
+  }
+  // inclusive prefix sums
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1)
+#pragma unroll
+    for (int q = 0; q < kSums; ++q) {
+      const uint32_t u = __shfl_up(sum[q], off, kWave);
+      if ((t & 63) >= off) sum[q] = sum_of(sum[q], u);
+    }
+  if ((t & 63) == 63)
+#pragma unroll
+    for (int q = 0; q < kSums; ++q) sh.waves[q][t >> 6] = sum[q];
+  if (flags) atomicOr(&sh.flags, flags);
+  __syncthreads();
+  uint32_t all[kSums];
+#pragma unroll
+  for (int q = 0; q < kSums; ++q) {
+    uint32_t before = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) {
+      if (w < t >> 6) before = sum_of(before, sh.waves[q][w]);
+      total = sum_of(total, sh.waves[q][w]);
+    }
+    sh.end[q][t] = sum_of(before, sum[q]);
+    all[q] = total;
+  }
+  flags = sh.flags;
+  // (all values here are the same in every thread)
+  int bit = 0;
+  if (err != 0) bit = err;  // sticky: the cache is frozen
+  else if (flags & 1 || all[kRows] > (uint32_t)a.max_rows || top < 0 || top > c.num_blocks) bit = SM_ERR_EINVAL;
+  else if (flags & 2 || (uint64_t)top + all[kFreed] > (uint32_t)c.num_blocks) bit = SM_ERR_ERANGE;
+  else if (all[kTaken] > (uint64_t)top + all[kFreed]) bit = SM_ERR_ENOMEM;
+  if (!bit) {
+    const int F = (int)all[kFreed], N = (int)all[kTaken];  // (at most num_blocks)
+    sh.ids[t] = s;
+    sh.keep[t] = keep;
+    __syncthreads();
+    // Every block that moves, and the partly filled page of a request's first
+    // row, must be a real one.  The e-th block given back, the first request's
+    // first and its highest logical block first, goes to place F - 1 - .. of
+    // the stack above top: the last request is served first.
+    auto given = [&](int e, int *place) {
+      const int i = first_past(sh.end[kFreed], n, e);
+      const int end = sh.end[kFreed][i], first = i ? sh.end[kFreed][i - 1] : 0;
+      *place = F - end + e - first;
+      return c.block_table + (int64_t)sh.ids[i] * c.max_blocks + blocks_for(sh.keep[i], c.bs_log2) + end - 1 - e;
+    };
+    bool bad = false;
+    int own[kOwn], place[kOwn];
+    int32_t *cell[kOwn];
+#pragma unroll
+    for (int u = 0; u < kOwn; ++u) {
+      const int e = t + u * NT;
+      if (e >= F) break;
+      cell[u] = given(e, &place[u]);
+      own[u] = *cell[u];
+      bad |= own[u] < 0 || own[u] >= c.num_blocks;
+    }
+    for (int e = t + kOwn * NT; e < F; e += NT) {
+      int p;
+      const int blk = *given(e, &p);
+      bad |= blk < 0 || blk >= c.num_blocks;
+    }
+    int popped[kOwn];  // those that lay on the stack before: pops F, F + 1, ...
+#pragma unroll
+    for (int u = 0; u < kOwn; ++u) {
+      const int j = F + t + u * NT;
+      popped[u] = j < N ? c.free_stack[top + F - 1 - j] : 0;
+      bad |= popped[u] < 0 || popped[u] >= c.num_blocks;
+    }
+    for (int j = F + t + kOwn * NT; j < N; j += NT) {
+      const int blk = c.free_stack[top + F - 1 - j];
+      bad |= blk < 0 || blk >= c.num_blocks;
+    }
+    int tail = 0;
+    if (active && m > 0 && (keep & (bs - 1)) != 0) {
+      tail = c.block_table[(int64_t)s * c.max_blocks + (keep >> c.bs_log2)];
+      bad |= tail < 0 || tail >= c.num_blocks;
+    }
+    sh.tail[t] = tail;
+    if (bad) atomicOr(&sh.flags, 4);
+    __syncthreads();
+    if (sh.flags) {
+      bit = SM_ERR_EINVAL;
+    } else {
+      // pushes
+#pragma unroll
+      for (int u = 0; u < kOwn; ++u) {
+        if (t + u * NT >= F) break;
+        c.free_stack[top + place[u]] = own[u];
+        if (place[u] < kHeld) sh.freed[place[u]] = own[u];
+        *cell[u] = -1;
+      }
+      for (int e = t + kOwn * NT; e < F; e += NT) {
+        int p;
+        int32_t *from = given(e, &p);
+        const int blk = *from;
+        c.free_stack[top + p] = blk;
+        if (p < kHeld) sh.freed[p] = blk;
+        *from = -1;
+      }
+      if (F) __syncthreads();  // (a cell given back may be taken again)
+      // pops
+      auto take = [&](int j, int blk) {
+        const int i = first_past(sh.end[kTaken], n, j);
+        c.block_table[(int64_t)sh.ids[i] * c.max_blocks + blocks_for(sh.keep[i], c.bs_log2) + j -
+                      (i ? sh.end[kTaken][i - 1] : 0)] = blk;
+        if (j < kHeld) sh.taken[j] = blk;
+      };
+      for (int j = t; j < min(F, N); j += NT) {
+        const int p = F - 1 - j;
+        take(j, p < kHeld ? sh.freed[p] : c.free_stack[top + p]);
+      }
+#pragma unroll
+      for (int u = 0; u < kOwn; ++u)
+        if (F + t + u * NT < N) take(F + t + u * NT, popped[u]);
+      for (int j = F + t + kOwn * NT; j < N; j += NT) take(j, c.free_stack[top + F - 1 - j]);
+      if (active) c.lengths[s] = keep + m;
+      if (t == 0) *c.free_top = top + F - N;
     }
   }
-  int64_t all_freed, all_taken;
-  const int64_t freed_end = scan64(had - kept, sh.red, &all_freed);
-  const int64_t taken_end = scan64(want - kept, sh.red, &all_taken);
-  if (sh.fl_range || top + all_freed > c.num_blocks) return SM_ERR_ERANGE;
-  if (all_taken > top + all_freed) return SM_ERR_ENOMEM;
-  // (all sums are at most num_blocks from here)
-  const int F = (int)all_freed, N = (int)all_taken;
-  sh.keep[t] = keep;
-  sh.row_end[t] = (int)row_end;
-  sh.freed_end[t] = (int)freed_end;
-  sh.taken_end[t] = (int)taken_end;
-  __syncthreads();
-  // every block that moves, and the partly filled page of a request's first
-  // row, must name a real block
-  // e-th block of the list that the pushes go through, the first request's first
-  auto freed_cell = [&](int e, int *place) {
-    const int i = first_past(sh.freed_end, a.n, e);
-    const int at = e - (i ? sh.freed_end[i - 1] : 0), cnt = sh.freed_end[i] - (i ? sh.freed_end[i - 1] : 0);
-    *place = top + F - sh.freed_end[i] + at;
-    return c.block_table + (int64_t)sh.ids[i] * c.max_blocks + blocks_for(sh.keep[i], c.bs_log2) + cnt - 1 - at;
-  };
-  bool bad = false;
-  for (int e = t; e < F; e += kMetaThreads) {
-    int place;
-    const int blk = *freed_cell(e, &place);
-    bad |= blk < 0 || blk >= c.num_blocks;
+  if (t == 0) {
+    a.row_offsets[0] = 0;
+    if (bit && err == 0) set_err(c.err, bit);
   }
-  for (int j = F + t; j < N; j += kMetaThreads) {
-    const int blk = c.free_stack[top + F - 1 - j];
-    bad |= blk < 0 || blk >= c.num_blocks;
-  }
-  if (active && m > 0 && (keep & ((1 << c.bs_log2) - 1)) != 0) {
-    const int blk = c.block_table[(int64_t)s * c.max_blocks + (keep >> c.bs_log2)];
-    bad |= blk < 0 || blk >= c.num_blocks;
-  }
-  if (bad) sh.fl_stack = 1;
-  __syncthreads();
-  if (sh.fl_stack) return SM_ERR_EINVAL;
-  for (int e = t; e < F; e += kMetaThreads) {
-    int place;
-    int32_t *cell = freed_cell(e, &place);
-    c.free_stack[place] = *cell;
-    *cell = -1;
-  }
-  if (F) __syncthreads();  // (uniform)
-  for (int j = t; j < N; j += kMetaThreads) {
-    const int i = first_past(sh.taken_end, a.n, j);
-    c.block_table[(int64_t)sh.ids[i] * c.max_blocks + blocks_for(sh.keep[i], c.bs_log2) + j -
-                  (i ? sh.taken_end[i - 1] : 0)] = c.free_stack[top + F - 1 - j];
-  }
-  if (active) c.lengths[s] = keep + m;
-  if (t == 0) *c.free_top = top + F - N;
-  return 0;
-}
-
-// HERE: positions and slots in this launch too.
-template <bool HERE>
-__global__ __launch_bounds__(kMetaThreads) void reserve_kernel(CacheArgs c, ReserveArgs a) {
-  __shared__ ReserveShared sh;
-  const int t = threadIdx.x;
-  const int bit = reserve_meta(c, a, sh);
-  if (bit) {
-    if (t == 0 && sh.s_err == 0) set_err(c.err, bit);
-    for (int i = t; i <= a.n; i += kMetaThreads) a.row_offsets[i] = 0;
-  } else {
-    if (t == 0) a.row_offsets[0] = 0;
-    if (t < a.n) a.row_offsets[t + 1] = sh.row_end[t];
-  }
+  if (active) a.row_offsets[t + 1] = bit ? 0 : (int)sh.end[kRows][t];
   if constexpr (HERE) {
-    __syncthreads();  // the table's new cells
-    const int total = bit || a.n == 0 ? 0 : sh.row_end[a.n - 1];
-    for (int r = t; r < a.max_rows; r += kMetaThreads) {
+    __syncthreads();
+    const int total = bit ? 0 : (int)all[kRows];
+    for (int r = t; r < a.max_rows; r += NT) {
+      int p = 0, slot = -1;
       if (r < total) {
-        const int i = first_past(sh.row_end, a.n, r);
-        put_row(c, a, r, sh.ids[i], sh.keep[i] + r - (i ? sh.row_end[i - 1] : 0));
-      } else {
-        a.pos[r] = 0;
-        a.slots[r] = -1;
+        const int i = first_past(sh.end[kRows], n, r), kept = blocks_for(sh.keep[i], c.bs_log2);
+        p = sh.keep[i] + r - (i ? (int)sh.end[kRows][i - 1] : 0);
+        const int page = p >> c.bs_log2, j = page - kept + (i ? (int)sh.end[kTaken][i - 1] : 0);
+        const int blk = page < kept  ? sh.tail[i]
+                        : j < kHeld  ? sh.taken[j]
+                                     : c.block_table[(int64_t)sh.ids[i] * c.max_blocks + page];
+        slot = (blk << c.bs_log2) + (p & (bs - 1));
       }
+      a.pos[r] = p;
+      a.slots[r] = slot;
     }
   }
 }
 
 // Positions and slots of many rows, after reserve_kernel (whose offsets are
 // all 0 where it failed).
-constexpr int kRowThreads = 256, kRowsPerThread = 4;
+constexpr int kRowThreads = 256;
 
 __global__ __launch_bounds__(kRowThreads) void reserve_rows_kernel(CacheArgs c, ReserveArgs a) {
-  __shared__ int ends[SM_MAX_REQUESTS];
+  __shared__ uint32_t ends[SM_MAX_REQUESTS];
+  __shared__ int ids[SM_MAX_REQUESTS], last[SM_MAX_REQUESTS];  // last: the length with the rows
   const int t = threadIdx.x;
-  for (int i = t; i < a.n; i += kRowThreads) ends[i] = a.row_offsets[i + 1];
-  __syncthreads();
-  const int total = a.n ? ends[a.n - 1] : 0;
-#pragma unroll
-  for (int u = 0; u < kRowsPerThread; ++u) {
-    const int64_t r = ((int64_t)blockIdx.x * kRowsPerThread + u) * kRowThreads + t;
-    if (r >= a.max_rows) continue;
-    if (r < total) {
-      const int i = first_past(ends, a.n, (int)r);
-      const int s = a.seq_ids[i];
-      put_row(c, a, (int)r, s, c.lengths[s] - (ends[i] - (int)r));
-    } else {
-      a.pos[r] = 0;
-      a.slots[r] = -1;
-    }
+  const int64_t r = (int64_t)blockIdx.x * kRowThreads + t;
+  for (int i = t; i < a.n; i += kRowThreads) {
+    const int s = a.seq_ids[i], end = a.row_offsets[i + 1];
+    ends[i] = end;
+    ids[i] = s;
+    last[i] = s >= 0 && s < c.max_seqs ? c.lengths[s] : 0;
   }
+  __syncthreads();
+  if (r >= a.max_rows) return;
+  int p = 0, slot = -1;
+  if (a.n && r < ends[a.n - 1]) {
+    const int i = first_past(ends, a.n, (uint32_t)r);
+    p = last[i] - ((int)ends[i] - (int)r);
+    slot = (c.block_table[(int64_t)ids[i] * c.max_blocks + (p >> c.bs_log2)] << c.bs_log2) + (p & ((1 << c.bs_log2) - 1));
+  }
+  a.pos[r] = p;
+  a.slots[r] = slot;
 }
 
 // Rows that the one workgroup places itself.
 constexpr int kHereRows = 4096;
+
+template <int NT>
+static sm_status launch_reserve(const CacheArgs &c, const ReserveArgs &a, hipStream_t stream) {
+  if (a.max_rows <= kHereRows) {
+    hipLaunchKernelGGL((reserve_kernel<NT, true>), dim3(1), dim3(NT), 0, stream, c, a);
+  } else {
+    hipLaunchKernelGGL((reserve_kernel<NT, false>), dim3(1), dim3(NT), 0, stream, c, a);
+    if (hipGetLastError() != hipSuccess) return SM_EHIP;
+    hipLaunchKernelGGL(reserve_rows_kernel, dim3((unsigned)(((int64_t)a.max_rows + kRowThreads - 1) / kRowThreads)),
+                       dim3(kRowThreads), 0, stream, c, a);
+  }
+  return hipGetLastError() == hipSuccess ? SM_OK : SM_EHIP;
+}
 
 }  // namespace sm
 
@@ -222,14 +292,8 @@ SM_API sm_status sm_kv_reserve(const sm_paged_cache *c, const int32_t *seq_ids, 
   if ((int64_t)c->num_blocks * c->block_size > INT32_MAX) return SM_EINVAL;
   if (!row_offsets || (n > 0 && (!seq_ids || !rows)) || (max_rows > 0 && (!pos || !slots))) return SM_EINVAL;
   const ReserveArgs r{seq_ids, crop, rows, n, max_rows, row_offsets, pos, slots};
-  if (max_rows <= kHereRows) {
-    hipLaunchKernelGGL(reserve_kernel<true>, dim3(1), dim3(kMetaThreads), 0, stream, a, r);
-  } else {
-    hipLaunchKernelGGL(reserve_kernel<false>, dim3(1), dim3(kMetaThreads), 0, stream, a, r);
-    if (hipGetLastError() != hipSuccess) return SM_EHIP;
-    const int per = kRowThreads * kRowsPerThread;
-    hipLaunchKernelGGL(reserve_rows_kernel, dim3((unsigned)(((int64_t)max_rows + per - 1) / per)), dim3(kRowThreads), 0,
-                       stream, a, r);
-  }
-  return hipGetLastError() == hipSuccess ? SM_OK : SM_EHIP;
+  // one wave for a small step: no barrier waits (16 requests of a row each)
+  if (n <= 64 && max_rows <= 256) return launch_reserve<64>(a, r, stream);
+  if (n <= 256 && max_rows <= 1024) return launch_reserve<256>(a, r, stream);
+  return launch_reserve<kMetaThreads>(a, r, stream);
 }
