@@ -8,8 +8,8 @@
 // structure for a cache or a rule table, the bytes that merge_params or
 // kv_proj_params gave (or a structure's own bytes) for parameters, an int (or
 // None) for a stream handle, plain numbers for the rest; it returns the
-// status.  A tensor in a tuple of its own is taken by its address alone: rows
-// with a stride, which the caller has looked at.  Values are taken and
+// status.  The checked entries take rows with a stride as a tensor in a tuple
+// of its own, which row_stride has looked at.  Values are taken and
 // refused as ctypes does for the same prototypes: integers wrap to the C
 // type's width, a ctypes number of the argument's own type counts as its
 // value, and what does not fit raises ctypes.ArgumentError.
@@ -31,12 +31,17 @@ namespace {
   X(sm_merge_spans) X(sm_merge_token_table) X(sm_merge_spans_tabled) X(sm_pack_spans) X(sm_kv_rollback)       \
   X(sm_kv_append) X(sm_decode_attention) X(sm_decode_step) X(sm_decode_merge_step)                            \
   X(sm_decode_step_noalloc) X(sm_prefill_attention) X(sm_rules_build) X(sm_rules_lookup) X(sm_match_prompt)   \
-  X(sm_match_decode) X(sm_gather_surrogates) X(sm_span_dedupe) X(sm_kv_project) X(sm_kv_append_projected)     \
+  X(sm_match_decode) X(sm_gather_surrogates) X(sm_span_dedupe) X(sm_kv_project) X(sm_kv_append_projected)
+// Entries that look at each tensor's type (of a typed pointer) and device too;
+// one argument more, the current device's index, comes last.
+#define SM_CHECKED(X) \
   X(sm_kv_reserve) X(sm_rotary) X(sm_kv_write_rotary) X(sm_block_norm) X(sm_token_logprobs)
 #define SM_SLOT(name) decltype(&::name) p_##name;
 SM_ENTRIES(SM_SLOT)
+SM_CHECKED(SM_SLOT)
 
 PyObject *g_is_cuda, *g_is_contiguous, *g_data_ptr, *g_value;  // interned names
+PyObject *g_dtype, *g_get_device, *g_numel, *g_shape, *g_stride;
 
 // What setup() is given: the exceptions for unusable tensors and for other
 // unusable arguments, the structures, and the C types of plain arguments.
@@ -54,10 +59,47 @@ bool is_true(PyObject *r, const char *otherwise) {
 bool tensor_address(PyObject *t, void **p) {
   *p = nullptr;
   if (t == Py_None) return true;
+  if (!is_true(PyObject_GetAttr(t, g_is_cuda), "expected a GPU tensor")) return false;
+  if (!is_true(PyObject_CallMethodNoArgs(t, g_is_contiguous), "expected a contiguous tensor")) return false;
+  PyObject *r = PyObject_CallMethodNoArgs(t, g_data_ptr);
+  if (!r) return false;
+  *p = PyLong_AsVoidPtr(r);
+  Py_DECREF(r);
+  return !PyErr_Occurred();
+}
+
+bool is_dtype(PyObject *t, PyObject *dtype) {  // (there is one object for each type)
+  PyObject *d = PyObject_GetAttr(t, g_dtype);
+  Py_XDECREF(d);
+  return d == dtype;
+}
+
+bool as_long(PyObject *r, long *v) {
+  if (!r) return false;
+  *v = PyLong_AsLong(r);
+  Py_DECREF(r);
+  return !(*v == -1 && PyErr_Occurred());
+}
+
+// tensor_address for the checked entries: a tensor of type `dtype` (unless
+// that is null) on the current device; one in a tuple of its own need not be
+// contiguous.
+bool checked_address(PyObject *t, PyObject *dtype, long device, void **p) {
+  *p = nullptr;
+  if (t == Py_None) return true;
   const bool strided = PyTuple_CheckExact(t) && PyTuple_GET_SIZE(t) == 1;
   if (strided) t = PyTuple_GET_ITEM(t, 0);
-  if (!is_true(PyObject_GetAttr(t, g_is_cuda), "expected a GPU tensor")) return false;
+  long at;
+  if (!as_long(PyObject_CallMethodNoArgs(t, g_get_device), &at)) return false;  // (-1: host memory)
+  if (at != device) {
+    PyErr_Format(g_type[kError], "expected tensors on the current device %ld, got one on %ld", device, at);
+    return false;
+  }
   if (!strided && !is_true(PyObject_CallMethodNoArgs(t, g_is_contiguous), "expected a contiguous tensor")) return false;
+  if (dtype && !is_dtype(t, dtype)) {
+    if (!PyErr_Occurred()) PyErr_Format(g_type[kError], "expected a tensor of %S", dtype);
+    return false;
+  }
   PyObject *r = PyObject_CallMethodNoArgs(t, g_data_ptr);
   if (!r) return false;
   *p = PyLong_AsVoidPtr(r);
@@ -135,6 +177,26 @@ bool get(PyObject *o, A *v) {
   }
 }
 
+PyObject *g_int32, *g_float32;  // torch's types
+
+template <class A>
+bool get_checked(PyObject *o, A *v, long device) {
+  if constexpr (std::is_pointer_v<A> && !std::is_same_v<A, hipStream_t>) {
+    typedef std::remove_cv_t<std::remove_pointer_t<A>> T;
+    if constexpr (is_host_struct<T>) {
+      return get_struct(o, v);
+    } else {
+      void *p;
+      PyObject *dtype = std::is_same_v<T, int32_t> ? g_int32 : std::is_same_v<T, float> ? g_float32 : nullptr;
+      if (!checked_address(o, dtype, device, &p)) return false;
+      *v = (A)p;
+      return true;
+    }
+  } else {
+    return get(o, v);
+  }
+}
+
 // A TypeError of argument `at` (from 1) as ctypes reports it.
 void argument_error(int at) {
   if (!PyErr_ExceptionMatches(PyExc_TypeError)) return;
@@ -165,18 +227,40 @@ PyObject *call(sm_status (*fn)(A...), PyObject *const *args, Py_ssize_t n, std::
   return PyLong_FromLong(st);
 }
 
-template <class... A>
-PyObject *dispatch(sm_status (*fn)(A...), PyObject *const *args, Py_ssize_t n) {
-  return call(fn, args, n, std::index_sequence_for<A...>{});
+template <class... A, size_t... I>
+PyObject *call_checked(sm_status (*fn)(A...), PyObject *const *args, Py_ssize_t n, std::index_sequence<I...>) {
+  if (n != (Py_ssize_t)sizeof...(A) + 1) {
+    PyErr_SetString(PyExc_TypeError, "wrong number of arguments");
+    return nullptr;
+  }
+  const long device = PyLong_AsLong(args[n - 1]);
+  if (device == -1 && PyErr_Occurred()) return nullptr;
+  std::tuple<A...> v;
+  int at = 0;
+  if (!((++at, get_checked(args[I], &std::get<I>(v), device)) && ...)) {
+    argument_error(at);
+    return nullptr;
+  }
+  sm_status st;
+  Py_BEGIN_ALLOW_THREADS;
+  st = fn(std::get<I>(v)...);
+  Py_END_ALLOW_THREADS;
+  return PyLong_FromLong(st);
 }
 
-template <auto *Fn>
+template <bool CHECKED, class... A>
+PyObject *dispatch(sm_status (*fn)(A...), PyObject *const *args, Py_ssize_t n) {
+  if constexpr (CHECKED) return call_checked(fn, args, n, std::index_sequence_for<A...>{});
+  else return call(fn, args, n, std::index_sequence_for<A...>{});
+}
+
+template <auto *Fn, bool CHECKED = false>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {
   if (!*Fn) {
     PyErr_SetString(g_type[kError], "the library is not open");
     return nullptr;
   }
-  return dispatch(*Fn, args, n);
+  return dispatch<CHECKED>(*Fn, args, n);
 }
 
 // open(path): the entries of the library at `path` (kept loaded)
@@ -196,8 +280,10 @@ PyObject *open_library(PyObject *, PyObject *path) {
     return nullptr;                                                     \
   }
   SM_ENTRIES(SM_FIND)
+  SM_CHECKED(SM_FIND)
 #define SM_STORE(name) p_##name = (decltype(&::name))f_##name;
   SM_ENTRIES(SM_STORE)
+  SM_CHECKED(SM_STORE)
   Py_RETURN_NONE;
 }
 
@@ -248,9 +334,78 @@ PyObject *setup(PyObject *, PyObject *types) {
   Py_RETURN_NONE;
 }
 
+// dtypes(int32, float32): torch's types, for the checked entries
+PyObject *dtypes(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  if (n != 2) {
+    PyErr_SetString(PyExc_TypeError, "dtypes takes 2 arguments");
+    return nullptr;
+  }
+  Py_INCREF(args[0]);
+  Py_XSETREF(g_int32, args[0]);
+  Py_INCREF(args[1]);
+  Py_XSETREF(g_float32, args[1]);
+  Py_RETURN_NONE;
+}
+
+// need(tensor, count, name): it has at least so many values
+PyObject *need(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  if (n != 3) {
+    PyErr_SetString(PyExc_TypeError, "need takes 3 arguments");
+    return nullptr;
+  }
+  long has, count = PyLong_AsLong(args[1]);
+  if ((count == -1 && PyErr_Occurred()) || !as_long(PyObject_CallMethodNoArgs(args[0], g_numel), &has)) return nullptr;
+  if (has < count) {
+    PyErr_Format(g_type[kError], "%S: expected %ld values, got %ld", args[2], count, has);
+    return nullptr;
+  }
+  Py_RETURN_NONE;
+}
+
+// row_stride(tensor, dtype, name, rows, inner, ...): the row stride of a [rows, *inner] tensor of that type whose
+// rows are contiguous (one row: its length)
+PyObject *row_stride(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  if (n < 5 || n > 7) {
+    PyErr_SetString(PyExc_TypeError, "row_stride takes 5 to 7 arguments");
+    return nullptr;
+  }
+  PyObject *t = args[0];
+  const Py_ssize_t dims = n - 3;
+  const bool typed = is_dtype(t, args[1]);
+  if (PyErr_Occurred()) return nullptr;
+  PyObject *shape = PyObject_GetAttr(t, g_shape), *stride = shape ? PyObject_CallMethodNoArgs(t, g_stride) : nullptr;
+  PyObject *answer = nullptr;
+  if (stride && PyTuple_Check(shape) && PyTuple_Check(stride)) {
+    bool right = typed && PyTuple_GET_SIZE(shape) == dims && PyTuple_GET_SIZE(stride) == dims;
+    long long width = 1, row = 0;
+    for (Py_ssize_t i = dims - 1; right && i >= 0; --i) {
+      const long long size = PyLong_AsLongLong(PyTuple_GET_ITEM(shape, i)), want = PyLong_AsLongLong(args[3 + i]);
+      const long long s = PyLong_AsLongLong(PyTuple_GET_ITEM(stride, i));
+      right = size == want && (i == 0 || size == 1 || s == width);
+      if (i == 0) row = size > 1 ? s : width;
+      width *= size;
+    }
+    if (!PyErr_Occurred()) {
+      if (right) answer = PyLong_FromLongLong(row);
+      else PyErr_Format(g_type[kError], "%S: expected %S rows that are contiguous, of the other tensors' sizes; got shape %S, strides %S",
+                        args[2], args[1], shape, stride);
+    }
+  } else if (!PyErr_Occurred()) {
+    PyErr_SetString(PyExc_TypeError, "expected a tensor");
+  }
+  Py_XDECREF(shape);
+  Py_XDECREF(stride);
+  return answer;
+}
+
+#define SM_CHECKED_ENTRY(name) {#name, (PyCFunction)(void (*)(void))entry<&p_##name, true>, METH_FASTCALL, nullptr},
 #define SM_ENTRY(name) {#name, (PyCFunction)(void (*)(void))entry<&p_##name>, METH_FASTCALL, nullptr},
 PyMethodDef methods[] = {
     SM_ENTRIES(SM_ENTRY)
+    SM_CHECKED(SM_CHECKED_ENTRY)
+    {"dtypes", (PyCFunction)(void (*)(void))dtypes, METH_FASTCALL, nullptr},
+    {"need", (PyCFunction)(void (*)(void))need, METH_FASTCALL, nullptr},
+    {"row_stride", (PyCFunction)(void (*)(void))row_stride, METH_FASTCALL, nullptr},
     {"merge_params", (PyCFunction)(void (*)(void))merge_params, METH_FASTCALL, nullptr},
     {"kv_proj_params", (PyCFunction)(void (*)(void))kv_proj_params, METH_FASTCALL, nullptr},
     {"setup", setup, METH_O, nullptr},
@@ -267,6 +422,12 @@ PyMODINIT_FUNC PyInit__binding(void) {
   g_data_ptr = PyUnicode_InternFromString("data_ptr");
   g_value = PyUnicode_InternFromString("value");
   if (!g_is_cuda || !g_is_contiguous || !g_data_ptr || !g_value) return nullptr;
+  g_dtype = PyUnicode_InternFromString("dtype");
+  g_get_device = PyUnicode_InternFromString("get_device");
+  g_numel = PyUnicode_InternFromString("numel");
+  g_shape = PyUnicode_InternFromString("shape");
+  g_stride = PyUnicode_InternFromString("stride");
+  if (!g_dtype || !g_get_device || !g_numel || !g_shape || !g_stride) return nullptr;
   for (PyObject *&t : g_type) {  // (until setup: no structure or ctypes number is of these types)
     Py_INCREF(PyExc_RuntimeError);
     t = PyExc_RuntimeError;

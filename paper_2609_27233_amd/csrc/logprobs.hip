@@ -400,12 +400,14 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs a) {
     for (int i = 0; i < W; ++i) s.r = fmaxf(s.r, w_max[i]);
     if constexpr (TOP) use_bounds();
   }
-  auto add = [&](const float *f, bool clamp) {
+  // adds a vector's logits to a chunk's sums, which join the row's together:
+  // a sum of few terms at a time loses less
+  auto add = [&](const float *f, Sums &to, bool clamp) {
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-      const float d = f[e] - s.r, p = __builtin_amdgcn_exp2f(d * a.c);
-      s.S += p;
-      s.E = fmaf(p, clamp ? fmaxf(d, kLowest) : d, s.E);
+      const float d = f[e] - to.r, p = __builtin_amdgcn_exp2f(d * a.c);
+      to.S += p;
+      to.E = fmaf(p, clamp ? fmaxf(d, kLowest) : d, to.E);
     }
   };
   if (slice == 0 && w == 0) {
@@ -417,14 +419,14 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs a) {
     if (lane < head + rest) f[0] = Elem<T>::load(x + v);
     const float m = wave_max(f[0]);
     if ((m - s.r) * a.c > kLift) move_to(s, m, a.c);
-    add(f, true);
+    add(f, s, true);
     if constexpr (TOP) top.put(f[0], v, lane < head + rest);
   }
   bool clamp = false;  // whether the slice has shown -infinity
   auto chunk = [&](u32x4_t (&cur)[kLpUnroll], int v0, int seen) {
     // nothing behind the end: by a value of probability 0 (-infinity would have the chunk added again)
     fill(cur, v0, s.r > -1e38f ? Vec16<T>::kLowest : Vec16<T>::kMinusInf);
-    const Sums before = s;
+    Sums part{s.r, 0.f, 0.f};
     float m[kLpUnroll], all = -INFINITY;
     auto pass = [&](bool clamped) {
 #pragma unroll
@@ -435,23 +437,25 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs a) {
         Vec16<T>::open(x, f);
         m[u] = largest(f);
         all = fmaxf(all, m[u]);
-        add(f, clamped);
+        add(f, part, clamped);
       }
     };
     if (clamp) pass(true);
     else pass(false);
-    const bool infinite = !clamp && __ballot(s.E != s.E) != 0;
+    const bool infinite = !clamp && __ballot(part.E != part.E) != 0;
     if (infinite || __ballot((all - s.r) * a.c > kLift)) {
       clamp |= infinite;
-      s = before;
       move_to(s, fmaxf(s.r, wave_max(all)), a.c);
+      part = Sums{s.r, 0.f, 0.f};
 #pragma unroll 1
       for (int u = 0; u < kLpUnroll; ++u) {
         float f[N];
         Vec16<T>::open(u == 0 ? cur[0] : u == 1 ? cur[1] : u == 2 ? cur[2] : cur[3], f);
-        add(f, true);
+        add(f, part, true);
       }
     }
+    s.S += part.S;
+    s.E += part.E;
     if constexpr (TOP) {
       if (v0 + CHUNK <= end) {
         best = fmaxf(best, all);

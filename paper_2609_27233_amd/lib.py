@@ -174,6 +174,7 @@ def load(path: str = LIB_PATH):
         raise SpanMergeError(f"the extension module is missing ({e}); build it with "
                              "`python -m paper_2609_27233_amd.build`") from e
     fast.setup((SpanMergeError, C.ArgumentError, PagedCacheDesc, RuleTableDesc, _I, _L, _F, _Z, _P))
+    fast.dtypes(torch.int32, torch.float32)
     fast.open(path)
     _fast = fast
     _lib = L
@@ -198,6 +199,7 @@ def _ptr(t: Optional[torch.Tensor]):
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream(stream=None):
@@ -521,51 +523,42 @@ def kv_append_projected(cache: PagedCache, seq_ids, x, W_k, W_v, ws=None, rope_t
 # rows of a backbone's layers: reserved, normed, turned, written, scored
 #
 # These calls look at their tensors before anything is enqueued: a wrong
-# type, device or size raises SpanMergeError.
+# type, size or device raises SpanMergeError.
 
-def _here(stream, *tensors):
-    """The stream's handle; every tensor has to be on the current device, and the stream one of its."""
-    now = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.get_device() != now:
-            raise SpanMergeError(f"expected tensors on the current device cuda:{now}, got one on {t.device}")
-    if stream is not None and stream.device_index != now:
-        raise SpanMergeError(f"expected a stream of the current device cuda:{now}")
-    return _stream(stream)
-
-
-def _need(t, dtype, count: int, name: str):
-    if t.dtype is not dtype or t.numel() < count:
-        raise SpanMergeError(f"{name}: expected {count} values of {dtype}, got {t.numel()} of {t.dtype}")
+def _here(stream):
+    """(handle of the stream, index of the current device, which its tensors have to be on as well)"""
+    dev = _device()
+    if stream is None:
+        return (_raw_stream(dev) if _raw_stream is not None else _stream()), dev
+    if stream.device_index != dev:
+        raise SpanMergeError(f"expected a stream of the current device cuda:{dev}")
+    return stream.cuda_stream, dev
 
 
-def _row_stride(t, dtype, rows: int, inner, name: str) -> int:
-    """The row stride of a [rows, *inner] tensor whose rows are contiguous."""
-    shape, st = t.shape, t.stride()
-    if t.dtype is not dtype or len(shape) != 1 + len(inner) or shape[0] != rows or shape[1:] != inner:
-        raise SpanMergeError(f"{name}: expected {dtype} of shape {(rows, *inner)}, got {t.dtype} of {tuple(shape)}")
-    width = 1
-    for size, s in zip(reversed(inner), reversed(st[1:])):
-        if size != 1 and s != width:
-            raise SpanMergeError(f"{name}: expected contiguous rows, got strides {st}")
-        width *= size
-    return st[0] if rows > 1 else width
+def _cache_here(cache: PagedCache, dev: int):
+    if cache.k_pool.get_device() != dev:
+        raise SpanMergeError(f"expected a cache on the current device cuda:{dev}")
+
+
+def _rows(t):
+    """Rows with a stride, which row_stride has looked at, for a call."""
+    return None if t is None else (t,)
 
 
 def kv_reserve(cache: PagedCache, seq_ids, rows, row_offsets, pos, slots, crop=None, stream=None):
     """Drop crop[i] entries of each listed sequence, then take room for rows[i]
     more: block tables and lengths, and for each row its position and slot.
     pos and slots (their size is the room for rows) get 0 and -1 past the last."""
-    n, most, i32 = seq_ids.numel(), pos.numel(), torch.int32
-    _need(seq_ids, i32, n, "seq_ids")
-    _need(rows, i32, n, "rows")
-    _need(row_offsets, i32, n + 1, "row_offsets")
-    _need(pos, i32, most, "pos")
-    _need(slots, i32, most, "slots")
+    b = _calls()
+    n, most, need = seq_ids.numel(), pos.numel(), b.need
+    need(rows, n, "rows")
+    need(row_offsets, n + 1, "row_offsets")
+    need(slots, most, "slots")
     if crop is not None:
-        _need(crop, i32, n, "crop")
-    st = _calls().sm_kv_reserve(cache.desc, seq_ids, crop, rows, n, most, row_offsets, pos, slots,
-                                _here(stream, cache.err, seq_ids, crop, rows, row_offsets, pos, slots))
+        need(crop, n, "crop")
+    handle, dev = _here(stream)
+    _cache_here(cache, dev)
+    st = b.sm_kv_reserve(cache.desc, seq_ids, crop, rows, n, most, row_offsets, pos, slots, handle, dev)
     _check(st, "sm_kv_reserve")
 
 
@@ -583,13 +576,13 @@ def rope_params(rot_dim: int, theta: float = 500000.0, layout: str = "half", sca
 def rotary(x, pos, rope: bytes, out, transpose: bool = False, stream=None):
     """out[r, h] = x[r, h] turned by pos[r]; x, out [rows, heads, D], each row
     contiguous; out may be x.  transpose: the gradient of that with respect to x."""
+    b = _calls()
     rows, heads, D = x.shape
     dt = x.dtype
-    _need(pos, torch.int32, rows, "pos")
-    sx = _row_stride(x, dt, rows, (heads, D), "x")
-    so = _row_stride(out, dt, rows, (heads, D), "out")
-    st = _calls().sm_rotary((x,), sx, pos, rows, heads, D, rope, int(transpose), dtype_code(dt), (out,), so,
-                            _here(stream, x, pos, out))
+    sx, so = b.row_stride(x, dt, "x", rows, heads, D), b.row_stride(out, dt, "out", rows, heads, D)
+    b.need(pos, rows, "pos")
+    handle, dev = _here(stream)
+    st = b.sm_rotary((x,), sx, pos, rows, heads, D, rope, int(transpose), dtype_code(dt), (out,), so, handle, dev)
     _check(st, "sm_rotary")
 
 
@@ -597,19 +590,22 @@ def kv_write_rotary(cache: PagedCache, pos, slots, q, k, v, rope: bytes, q_out, 
     """q_out = q turned by pos; K (turned) and V rows into the slots of the
     cache's pages (-1: not written).  q, q_out [rows, Hq, D] or both None; k, v
     [rows, Hkv, D]; each row contiguous, so the three may be views of one buffer."""
-    rows, dt, kv = k.shape[0], cache.dtype, (cache.H, cache.D)
-    _need(pos, torch.int32, rows, "pos")
-    _need(slots, torch.int32, rows, "slots")
-    sk, sv = _row_stride(k, dt, rows, kv, "k"), _row_stride(v, dt, rows, kv, "v")
+    b = _calls()
+    row_stride, dt, H, D = b.row_stride, cache.dtype, cache.H, cache.D
+    rows = k.shape[0]
+    sk, sv = row_stride(k, dt, "k", rows, H, D), row_stride(v, dt, "v", rows, H, D)
+    b.need(pos, rows, "pos")
+    b.need(slots, rows, "slots")
     hq = sq = so = 0
     if (q is None) != (q_out is None):
         raise SpanMergeError("q and q_out go together")
     if q is not None:
         hq = q.shape[1]
-        sq, so = _row_stride(q, dt, rows, (hq, cache.D), "q"), _row_stride(q_out, dt, rows, (hq, cache.D), "q_out")
-    st = _calls().sm_kv_write_rotary(cache.desc, pos, slots, rows, q if q is None else (q,), sq, hq, (k,), sk, (v,), sv,
-                                     rope, q_out if q is None else (q_out,), so,
-                                     _here(stream, cache.err, pos, slots, q, k, v, q_out))
+        sq, so = row_stride(q, dt, "q", rows, hq, D), row_stride(q_out, dt, "q_out", rows, hq, D)
+    handle, dev = _here(stream)
+    _cache_here(cache, dev)
+    st = b.sm_kv_write_rotary(cache.desc, pos, slots, rows, _rows(q), sq, hq, (k,), sk, (v,), sv, rope, _rows(q_out), so,
+                              handle, dev)
     _check(st, "sm_kv_write_rotary")
 
 
@@ -623,10 +619,11 @@ class Norm:
         self.gain, self.bias = gain, bias
         self.packed = bytes(NormParams(NORM_KINDS[kind], eps, _ptr(gain), _ptr(bias)))
 
-    def look(self, dtype, d: int, name: str):
+    def look(self, dtype, d: int, dev: int, name: str):
         for t in (self.gain, self.bias):
-            if t is not None and (t.dtype is not dtype or t.numel() != d):
-                raise SpanMergeError(f"{name}: expected {d} values of {dtype}, got {t.numel()} of {t.dtype}")
+            if t is not None and (t.dtype is not dtype or t.numel() != d or t.get_device() != dev):
+                raise SpanMergeError(f"{name}: expected {d} values of {dtype} on cuda:{dev}, got {t.numel()} of {t.dtype} "
+                                     f"on {t.device}")
 
 
 def norm_params(kind: str = "rms", gain=None, bias=None, eps: float = 1e-5) -> Norm:
@@ -638,26 +635,26 @@ def block_norm(h, y, h_out, n_out, post: Optional[Norm] = None, gate=None, scale
     """h_out = h + scale * gate * post(y), n_out = pre(h_out) of the unrounded
     sum; [rows, d] with contiguous rows.  y None: h alone; gate [d] or
     [rows, d]; h_out or n_out may be None, or an input itself."""
-    (rows, d), dt = h.shape, h.dtype
-    sh = _row_stride(h, dt, rows, (d,), "h")
-    sy = 0 if y is None else _row_stride(y, dt, rows, (d,), "y")
-    sho = 0 if h_out is None else _row_stride(h_out, dt, rows, (d,), "h_out")
-    sno = 0 if n_out is None else _row_stride(n_out, dt, rows, (d,), "n_out")
+    b = _calls()
+    row_stride, (rows, d), dt = b.row_stride, h.shape, h.dtype
+    sh = row_stride(h, dt, "h", rows, d)
+    sy = 0 if y is None else row_stride(y, dt, "y", rows, d)
+    sho = 0 if h_out is None else row_stride(h_out, dt, "h_out", rows, d)
+    sno = 0 if n_out is None else row_stride(n_out, dt, "n_out", rows, d)
     sg = 0
     if gate is not None:
         if gate.dim() == 1:
-            _row_stride(gate.unsqueeze(0), dt, 1, (d,), "gate")
+            row_stride(gate.unsqueeze(0), dt, "gate", 1, d)
         else:
-            sg = _row_stride(gate, dt, rows, (d,), "gate")
-    at = [h, y, gate, h_out, n_out]
-    for norm, name in ((post, "post"), (pre, "pre")):
-        if norm is not None:
-            norm.look(dt, d, name)
-            at += (norm.gain, norm.bias)
-    one = lambda t: None if t is None else (t,)   # noqa: E731
-    st = _calls().sm_block_norm((h,), sh, one(y), sy, rows, d, None if post is None else post.packed, one(gate), sg, scale,
-                                None if pre is None else pre.packed, dtype_code(dt), one(h_out), sho, one(n_out), sno,
-                                _here(stream, *at))
+            sg = row_stride(gate, dt, "gate", rows, d)
+    handle, dev = _here(stream)
+    if post is not None:
+        post.look(dt, d, dev, "post")
+    if pre is not None:
+        pre.look(dt, d, dev, "pre")
+    st = b.sm_block_norm((h,), sh, _rows(y), sy, rows, d, None if post is None else post.packed, _rows(gate), sg, scale,
+                         None if pre is None else pre.packed, dtype_code(dt), _rows(h_out), sho, _rows(n_out), sno,
+                         handle, dev)
     _check(st, "sm_block_norm")
 
 
@@ -669,26 +666,26 @@ def token_logprobs(logits, tokens, logprob, entropy, top_ids, top_logprobs, ws, 
     """Log probability of tokens[r], entropy and the k = top_ids.shape[1]
     largest logits of each row of logits [rows, vocab] (contiguous rows);
     scale = 1 / temperature.  Each output may be None."""
-    rows, vocab = logits.shape
-    dt, f32, i32 = logits.dtype, torch.float32, torch.int32
-    sl = _row_stride(logits, dt, rows, (vocab,), "logits")
+    b = _calls()
+    (rows, vocab), dt, need = logits.shape, logits.dtype, b.need
+    sl = b.row_stride(logits, dt, "logits", rows, vocab)
     k = 0
     if tokens is not None:
-        _need(tokens, i32, rows, "tokens")
+        need(tokens, rows, "tokens")
     if logprob is not None:
-        _need(logprob, f32, rows, "logprob")
+        need(logprob, rows, "logprob")
     if entropy is not None:
-        _need(entropy, f32, rows, "entropy")
+        need(entropy, rows, "entropy")
     if top_ids is not None:
         k = top_ids.shape[-1] if top_ids.dim() > 1 else 1
-        _need(top_ids, i32, rows * k, "top_ids")
+        need(top_ids, rows * k, "top_ids")
         if top_logprobs is not None:
-            _need(top_logprobs, f32, rows * k, "top_logprobs")
+            need(top_logprobs, rows * k, "top_logprobs")
     elif top_logprobs is not None and top_logprobs.numel():
         raise SpanMergeError("top_logprobs without top_ids")
     if err is not None:
-        _need(err, i32, 1, "err")
-    st = _calls().sm_token_logprobs((logits,), sl, rows, vocab, dtype_code(dt), scale, tokens, logprob, entropy, k,
-                                    top_ids, top_logprobs, ws, ws.nbytes, err,
-                                    _here(stream, logits, tokens, logprob, entropy, top_ids, top_logprobs, ws, err))
+        need(err, 1, "err")
+    handle, dev = _here(stream)
+    st = b.sm_token_logprobs((logits,), sl, rows, vocab, dtype_code(dt), scale, tokens, logprob, entropy, k, top_ids,
+                             top_logprobs, ws, ws.nbytes, err, handle, dev)
     _check(st, "sm_token_logprobs")

@@ -128,25 +128,26 @@ def _gpu(shape, dtype=torch.float32):
     return torch.zeros(shape, dtype=dtype).as_subclass(_Gpu)
 
 
-def test_row_strides_are_looked_at():
-    f = torch.float32
+def test_row_strides_are_looked_at(L):
+    f, stride = torch.float32, sm._calls().row_stride
     x = torch.zeros((6, 4, 8))
-    assert sm._row_stride(x, f, 6, (4, 8), "x") == 32
+    assert stride(x, f, "x", 6, 4, 8) == 32
     buf = torch.zeros((6, 80))
-    assert sm._row_stride(buf[:, 8:40].view(6, 4, 8), f, 6, (4, 8), "x") == 80
-    assert sm._row_stride(buf[:1, :32].view(1, 4, 8), f, 1, (4, 8), "x") == 32          # one row: any stride
-    assert sm._row_stride(torch.zeros(6, 8, 1).transpose(1, 2), f, 6, (1, 8), "x") == 8
+    assert stride(buf[:, 8:40].view(6, 4, 8), f, "x", 6, 4, 8) == 80
+    assert stride(buf[:1, :32].view(1, 4, 8), f, "x", 1, 4, 8) == 32                    # one row: any stride
+    assert stride(torch.zeros(6, 8, 1).transpose(1, 2), f, "x", 6, 1, 8) == 8
+    assert stride(torch.zeros((0, 4, 8)), f, "x", 0, 4, 8) == 32
     for bad in (x.transpose(1, 2), x.transpose(0, 1), torch.zeros((6, 4, 16))[..., ::2], torch.zeros((6, 8, 8))[:, ::2],
                 x.double(), x[:5], torch.zeros((6, 32))):
-        with pytest.raises(sm.SpanMergeError):
-            sm._row_stride(bad, f, 6, (4, 8), "x")
+        with pytest.raises(sm.SpanMergeError, match="x: expected"):
+            stride(bad, f, "x", 6, 4, 8)
 
 
-def test_wrong_types_and_sizes_are_refused(monkeypatch):
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+def test_wrong_types_and_sizes_are_refused(monkeypatch, L):
+    monkeypatch.setattr(sm, "_here", lambda stream: (0, 0))
     i64, i32 = torch.int64, torch.int32
     err = sm.SpanMergeError
-    with pytest.raises(err, match="pos"):
+    with pytest.raises(err, match="torch.int32"):
         sm.rotary(_gpu((3, 2, 8)), _gpu(3, i64), sm.rope_params(8), _gpu((3, 2, 8)))
     with pytest.raises(err, match="pos"):
         sm.rotary(_gpu((3, 2, 8)), _gpu(2, i32), sm.rope_params(8), _gpu((3, 2, 8)))
@@ -156,22 +157,33 @@ def test_wrong_types_and_sizes_are_refused(monkeypatch):
         sm.block_norm(_gpu((3, 8)), None, None, _gpu((3, 8)), pre=sm.norm_params("rms", _gpu(7)))
     with pytest.raises(err, match="gate"):
         sm.block_norm(_gpu((3, 8)), _gpu((3, 8)), _gpu((3, 8)), None, gate=_gpu((2, 8)))
-    with pytest.raises(err, match="tokens"):
+    with pytest.raises(err, match="torch.int32"):
         sm.token_logprobs(_gpu((3, 8)), _gpu(3, i64), _gpu(3), None, None, None, _gpu(65536, torch.uint8))
+    with pytest.raises(err, match="torch.float32"):
+        sm.token_logprobs(_gpu((3, 8)), _gpu(3, i32), _gpu(3, torch.float64), None, None, None, _gpu(65536, torch.uint8))
     with pytest.raises(err, match="top_ids"):
         sm.token_logprobs(_gpu((3, 8)), None, None, None, _gpu((2, 4), i32), None, _gpu(65536, torch.uint8))
     with pytest.raises(err, match="dtype"):
         sm.token_logprobs(_gpu((3, 8), torch.float16), None, None, None, None, None, _gpu(65536, torch.uint8))
+    with pytest.raises(err, match="contiguous"):
+        sm.rotary(_gpu((3, 2, 8)), _gpu(6, i32)[::2], sm.rope_params(8), _gpu((3, 2, 8)))
 
 
-def test_other_devices_are_refused(monkeypatch):
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
-    with pytest.raises(sm.SpanMergeError, match="current device"):
-        sm.rotary(_gpu((3, 2, 8)), _gpu(3, torch.int32), sm.rope_params(8), _gpu((3, 2, 8)))
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+def test_other_devices_are_refused(monkeypatch, L):
+    x, pos, rope = _gpu((3, 2, 8)), _gpu(3, torch.int32), sm.rope_params(8)
+    monkeypatch.setattr(sm, "_raw_stream", lambda dev: 0)
+    monkeypatch.setattr(sm, "_device", lambda: 1)
+    with pytest.raises(sm.SpanMergeError, match="current device 1"):
+        sm.rotary(x, pos, rope, _gpu((3, 2, 8)))
+    monkeypatch.setattr(sm, "_device", lambda: 0)
+    with pytest.raises(sm.SpanMergeError, match="current device 0, got one on -1"):      # a CPU tensor
+        sm.rotary(x, torch.zeros(3, dtype=torch.int32), rope, _gpu((3, 2, 8)))
     stream = type("S", (), dict(device_index=1, cuda_stream=0))()
     with pytest.raises(sm.SpanMergeError, match="stream"):
-        sm.rotary(_gpu((3, 2, 8)), _gpu(3, torch.int32), sm.rope_params(8), _gpu((3, 2, 8)), stream=stream)
+        sm.rotary(x, pos, rope, _gpu((3, 2, 8)), stream=stream)
+    with pytest.raises(sm.SpanMergeError, match="post"):
+        monkeypatch.setattr(sm, "_device", lambda: 2)
+        sm.block_norm(_gpu((3, 8)), _gpu((3, 8)), _gpu((3, 8)), None, post=sm.norm_params("rms", _gpu(8)))
 
 
 def test_caches_that_share_tables():
