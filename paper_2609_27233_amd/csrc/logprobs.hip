@@ -290,12 +290,12 @@ __device__ __forceinline__ void put_row(const LogprobArgs &a, int64_t r, Sums s,
       a.top_ids[r * a.k + rank[0]] = (int)~(uint32_t)key[0];
       if (a.top_logprobs) a.top_logprobs[r * a.k + rank[0]] = logprob(value_of((uint32_t)(key[0] >> 32)));
     }
-    for (int v0 = 0; m < a.k && v0 < a.vocab; v0 += 64) {  // fewer numbers than alternatives: NaN follow
+    for (int64_t v0 = 0; m < a.k && v0 < a.vocab; v0 += 64) {  // fewer numbers than alternatives: NaN follow
       const float f = v0 + lane < a.vocab ? Elem<T>::load(x + v0 + lane) : 0.f;
       const uint64_t mask = __ballot(f != f);
       const int at = m + lanes_below(mask);
       if (f != f && at < a.k) {
-        a.top_ids[r * a.k + at] = v0 + lane;
+        a.top_ids[r * a.k + at] = (int)v0 + lane;
         if (a.top_logprobs) a.top_logprobs[r * a.k + at] = f;
       }
       m += __popcll(mask);
@@ -558,7 +558,7 @@ constexpr int kLpShort = 1024, kLpMany = 1536;
 static_assert(kLpFill * kCounterStep * sizeof(int) <= 65536, "counters");
 
 static LogprobPlan plan_logprobs(int rows, int vocab, int k) {
-  const int nvec = (vocab + 3) / 4;  // (of fp32; bf16 rows have half as many)
+  const int nvec = vocab / 4 + 1;  // (of fp32; bf16 rows have half as many)
   const int chunks = (nvec + kLpChunk - 1) / kLpChunk;
   int slices = rows > 0 && rows < kLpFill ? (kLpFill + rows / 2) / rows : 1;
   slices = slices < chunks ? slices : chunks;
@@ -588,7 +588,7 @@ SM_API sm_status sm_token_logprobs(const void *logits, int64_t stride, int rows,
   if (!ws || ws_bytes < sm_token_logprobs_workspace_bytes(rows, vocab, k)) return SM_EINVAL;
   const int n = dt == SM_BF16 ? 8 : 4;
   LogprobPlan p = plan_logprobs(rows, vocab, k);
-  const int nvec = (vocab + n - 1) / n, chunks = (nvec + kLpChunk - 1) / kLpChunk;
+  const int nvec = vocab / n + 1, chunks = (nvec + kLpChunk - 1) / kLpChunk;
   p.per_slice = (chunks + p.slices - 1) / p.slices * kLpChunk;
   p.slices = (nvec + p.per_slice - 1) / p.per_slice;
   float4 *sums = (float4 *)((char *)ws + 65536);

@@ -383,7 +383,10 @@ static bool rope_ok(const sm_rope_params *p, int head_dim) {
          (p->scaling != SM_ROPE_RAMP || p->theta > 1.f);
 }
 
-// Frequencies in turns per position, on the host in double precision.
+// Frequencies in turns per position, on the host in double precision:
+// theta^(-j / P) as a power for every eighth pair times one for the pairs
+// between (64 exponentials took 0.8 us of a small call's 7, 16 take 0.2; the
+// product's rounding is a fraction of the exponentials' own).
 static void set_turns(const sm_rope_params *p, RopeArgs *a) {
   constexpr double two_pi = 6.283185307179586476925286766559;
   const int P = p->rot_dim / 2;
@@ -394,8 +397,11 @@ static void set_turns(const sm_rope_params *p, RopeArgs *a) {
     j0 = std::fmax(std::floor(pair_of(p->high)), 0.0);
     span = std::fmax(std::fmin(std::ceil(pair_of(p->low)), p->rot_dim - 1.0) - j0, 0.001);
   }
+  double step[8], base = 1;
+  for (int i = 0; i < 8 && i < P; ++i) step[i] = std::exp(-ln_theta * i / P);
   for (int j = 0; j < P; ++j) {
-    double w = std::exp(-ln_theta * j / P) / two_pi;  // turns per position
+    if (j % 8 == 0) base = std::exp(-ln_theta * j / P);
+    double w = base * step[j % 8] / two_pi;  // turns per position
     if (p->scaling == SM_ROPE_LINEAR) {
       w /= s;
     } else if (p->scaling == SM_ROPE_BANDS) {

@@ -289,8 +289,11 @@ class PagedCache:
     """Device buffers of one paged KV cache (allocated with torch) and the
     descriptor the C calls take.  Pools: K [NB, Hkv, bs, D], V [NB, Hkv, D, bs].
     ``tables``: another cache of the same sizes, a layer's neighbour, whose
-    block table, lengths, free stack and error word this one shares (kv_reserve
-    keeps them for all layers; only the pools are this one's own)."""
+    block table, lengths, free stack and error word this one shares; only the
+    pools are its own.  kv_reserve (or kv_rollback) moves the shared lengths
+    once for all layers and kv_write_rotary fills each layer's pages; the calls
+    that append to one cache (kv_append, decode_step and their like) would
+    move them once a layer."""
 
     def __init__(self, *, dtype: torch.dtype, num_kv_heads: int, head_dim: int,
                  block_size: int, num_blocks: int, max_seqs: int,

@@ -1,0 +1,151 @@
+"""The calls around a backbone's projections beyond the sizes of their own
+tests: offsets past 32 bits, other streams, a captured step."""
+import numpy as np
+import pytest
+import torch
+
+from gpu_util import dev, i32, say
+from paper_2609_27233_amd import lib as sm
+
+pytestmark = pytest.mark.gpu
+
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def _rand(shape, dt, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.empty(shape, device=dev()).normal_(0, 1, generator=g).to(dt)
+
+
+def test_pages_past_32_bits():
+    """A cache of 140,000 pages of 16 x 8 x 128: 2.3 x 10^9 elements in each pool."""
+    H, D, bs, nb = 8, 128, 16, 140_000
+    c = sm.PagedCache(dtype=BF, num_kv_heads=H, head_dim=D, block_size=bs, num_blocks=nb, max_seqs=2, max_blocks_per_seq=8)
+    n = 40
+    ro, pos, slots = (torch.empty(m, dtype=torch.int32, device=dev()) for m in (2, n, n))
+    say("large pools", c.k_pool.numel())
+    # the stack hands out the last pages first when it is turned round
+    c.free_stack.copy_(torch.arange(nb, dtype=torch.int32))
+    sm.kv_reserve(c, i32([1]), i32([n]), ro, pos, slots)
+    assert slots.tolist() == [(nb - 1 - j // bs) * bs + j % bs for j in range(n)]
+    k, v = _rand((n, H, D), BF, 1), _rand((n, H, D), BF, 2)
+    sm.kv_write_rotary(c, torch.zeros_like(pos), slots, None, k, v, sm.rope_params(D), None)
+    torch.cuda.synchronize()
+    assert c.error_bits() == 0
+    for j in (0, 15, 16, 39):
+        blk, s = nb - 1 - j // bs, j % bs
+        assert torch.equal(c.k_pool[blk, :, s], k[j]) and torch.equal(c.v_pool[blk, :, :, s], v[j])
+    assert int((c.k_pool[: nb - 3] != 0).any(-1).any(-1).any(-1).sum()) == 0
+
+
+def test_rows_past_32_bits():
+    rows, d = 600_000, 4096
+    h = _rand((1, d), BF, 3).expand(rows, d).contiguous()                # 2.5 x 10^9 elements
+    out = torch.empty_like(h)
+    n = sm.norm_params("rms", None)
+    say("large rows", h.numel())
+    sm.block_norm(h, None, None, out, pre=n)
+    assert torch.equal(out[0], out[rows - 1]) and torch.equal(out[0], out[rows // 2]) and float(out[0].abs().sum()) > 0
+    x = out.view(rows, 32, 128)
+    pos = torch.full((rows,), 77, dtype=torch.int32, device=dev())
+    sm.rotary(x, pos, sm.rope_params(128), x)
+    assert torch.equal(x[0], x[rows - 1]) and torch.equal(x[0], x[rows // 2])
+    del x, out
+    V = 128_256
+    x = h.view(-1)[: 19_000 * V].view(19_000, V)
+    lp, ent = torch.empty(19_000, device=dev()), torch.empty(19_000, device=dev())
+    ids = torch.empty((19_000, 2), dtype=torch.int32, device=dev())
+    ws = torch.zeros(sm.token_logprobs_workspace_bytes(19_000, V, 2), dtype=torch.uint8, device=dev())
+    tok = torch.full((19_000,), V - 1, dtype=torch.int32, device=dev())
+    sm.token_logprobs(x, tok, lp, ent, ids, None, ws)
+    for r in (0, 16_743, 18_999):                                        # the middle one begins behind 2^31 elements
+        z = x[r].double()
+        assert abs(float(lp[r]) - float(torch.log_softmax(z, 0)[V - 1])) <= 1e-4
+        assert int(ids[r, 0]) == int(torch.argmax(x[r].float()))
+
+
+def test_other_streams():
+    """Each call on a stream of its own, beside work on the current one."""
+    side = torch.cuda.Stream()
+    x, big = _rand((3000, 8, 64), BF, 1), _rand((4096, 4096), F32, 2)
+    pos, rope = torch.arange(3000, dtype=torch.int32, device=dev()), sm.rope_params(64)
+    want, got = torch.empty_like(x), torch.zeros_like(x)
+    logits, ids, got_ids = _rand((9, 40_000), BF, 5), *(torch.zeros((9, 4), dtype=torch.int32, device=dev()) for _ in range(2))
+    ws = [torch.zeros(sm.token_logprobs_workspace_bytes(9, 40_000, 4), dtype=torch.uint8, device=dev()) for _ in range(2)]
+    n = sm.norm_params("rms", None)
+    h, a, b = _rand((500, 512), BF, 3), *(torch.zeros((500, 512), dtype=BF, device=dev()) for _ in range(2))
+    sm.rotary(x, pos, rope, want)
+    sm.block_norm(h, h, None, a, pre=n)
+    sm.token_logprobs(logits, None, None, None, ids, None, ws[0])
+    torch.cuda.synchronize()
+    for _ in range(5):
+        big @ big
+    side.wait_stream(torch.cuda.current_stream())
+    sm.rotary(x, pos, rope, got, stream=side)
+    sm.block_norm(h, h, None, b, pre=n, stream=side)
+    sm.token_logprobs(logits, None, None, None, got_ids, None, ws[1], stream=side)
+    side.synchronize()
+    assert torch.equal(want, got) and torch.equal(a, b) and torch.equal(ids, got_ids)
+
+
+def test_captured_decode_step():
+    """A step's calls in one graph (padded to a fixed number of rows), its inputs and counts changed between replays,
+    against the same calls one by one on a twin cache."""
+    H, Hq, D, bs, n, room, V = 2, 8, 64, 16, 5, 9, 5000
+    rng = np.random.RandomState(3)
+    order = rng.permutation(60)
+    kw = dict(dtype=BF, num_kv_heads=H, head_dim=D, block_size=bs, num_blocks=60, max_seqs=n, max_blocks_per_seq=12,
+              free_order=order)
+    rope, norm = sm.rope_params(D, scaling="linear", factor=2.0), sm.norm_params("rms", _rand((512,), BF, 9))
+    head = _rand((512, V), F32, 10) * 0.05
+    ids = i32(rng.permutation(n))
+
+    class Side:
+        def __init__(self):
+            self.c = sm.PagedCache(**kw)
+            e = lambda *s, dt=BF: torch.zeros(s, dtype=dt, device=dev())             # noqa: E731
+            self.ro, self.pos, self.slots = e(n + 1, dt=torch.int32), e(room, dt=torch.int32), e(room, dt=torch.int32)
+            self.qkv, self.q_out, self.att = e(room, (Hq + 2 * H) * D), e(room, Hq, D), e(room, Hq, D)
+            self.h, self.nrm, self.crop, self.rows = e(room, 512), e(room, 512), e(n, dt=torch.int32), e(n, dt=torch.int32)
+            self.ws = torch.zeros(sm.decode_workspace_bytes(n, Hq, D, 192), dtype=torch.uint8, device=dev())
+            self.lws = torch.zeros(sm.token_logprobs_workspace_bytes(n, V, 3), dtype=torch.uint8, device=dev())
+            self.top, self.ent = e(n, 3, dt=torch.int32), e(n, dt=F32)
+
+        def step(self):
+            sm.kv_reserve(self.c, ids, self.rows, self.ro, self.pos, self.slots, crop=self.crop)
+            q, k, v = (t.unflatten(1, (-1, D)) for t in self.qkv.split([Hq * D, H * D, H * D], 1))
+            sm.kv_write_rotary(self.c, self.pos, self.slots, q, k, v, rope, self.q_out)
+            sm.decode_attention(self.c, ids, self.q_out[:n], self.att[:n], self.ws, 192)
+            sm.block_norm(self.h, self.att.flatten(1), self.h, self.nrm, scale=0.5, pre=norm)
+            sm.token_logprobs(self.nrm[:n].float() @ head, None, None, self.ent, self.top, None, self.lws)
+
+        def state(self):
+            return [self.ro, self.pos, self.slots, self.q_out, self.att[:n], self.h[:n], self.nrm[:n], self.top, self.ent,
+                    self.c.k_pool, self.c.v_pool, self.c.block_table, self.c.lengths, self.c.free_top]
+
+    a, b = Side(), Side()
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        b.step()                                                          # (no rows: the caches stay empty)
+    a.step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=stream):
+        b.step()
+    for rep in range(8):
+        crop = np.minimum(rng.randint(0, 3, n), a.c.lengths.cpu().numpy()[ids.cpu().numpy()])
+        rows = np.ones(n, int) if rep % 2 else rng.randint(1, 3, n).clip(max=1 + (rep == 0))
+        rows = rows if rows.sum() <= room else np.ones(n, int)
+        for s in (a, b):
+            s.crop.copy_(i32(crop))
+            s.rows.copy_(i32(rows))
+            s.qkv.copy_(_rand(s.qkv.shape, BF, 100 + rep))
+            s.h.copy_(_rand(s.h.shape, BF, 200 + rep))
+        say("replay", rep)
+        a.step()
+        g.replay()
+        torch.cuda.synchronize()
+        assert a.c.error_bits() == 0 and b.c.error_bits() == 0
+        for x, y in zip(a.state(), b.state()):
+            assert torch.equal(x, y)
