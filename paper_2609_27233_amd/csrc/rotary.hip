@@ -92,6 +92,20 @@ template <> struct Piece<uint16_t, 8> {
   static __device__ __forceinline__ raw close(const float (&f)[8]) { return Vec16<uint16_t>::close(f); }
 };
 
+// Input that would fill the 256 MB of last-level cache with what is made of it
+// is read past it (STREAM), as nothing reads it again: beside what writes the
+// rows and what reads the result, 6000 rows of 12 KB take 25 us so and 31 with
+// plain loads, 20,000 rows 102 and 108; 4000 rows, which the cache holds
+// anyway, 20.4 and 18.4.  What the cache could not hold by itself is read
+// plainly: 268 MB of fp32 rows 117 us past it, 111 so.
+constexpr int64_t kStreamFrom = 64 << 20, kStreamTo = 256 << 20;
+
+template <bool STREAM, typename R>
+__device__ __forceinline__ R load_as(const void *p) {
+  if constexpr (STREAM) return __builtin_nontemporal_load((const R *)p);
+  else return *(const R *)p;
+}
+
 // A thread's unit: V features of a row's head that are turned with V more
 // (half layout: the second half's; single features: a pair's other one), or
 // among themselves, or behind the turned part, where they are copied.
@@ -114,7 +128,7 @@ struct Unit {
   }
   // Heads h, h + step, ... below h1: in(h), out(h) give a head's first
   // feature.  The loads are unconditional (the last head's again).
-  template <class In, class Out>
+  template <bool STREAM, class In, class Out>
   __device__ __forceinline__ void run(int h, int h1, int step, In in, Out out) const {
     typedef Piece<T, V> P;
     typedef typename P::raw raw;
@@ -124,8 +138,8 @@ struct Unit {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const T *p = in(min(h + u * step, h1 - 1)) + at;
-        a[u] = *(const raw *)p;
-        if constexpr (TWO) b[u] = *(const raw *)(p + far);
+        a[u] = load_as<STREAM, raw>(p);
+        if constexpr (TWO) b[u] = load_as<STREAM, raw>(p + far);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -182,7 +196,7 @@ __device__ __forceinline__ void each_unit(int nr, const FastDiv &per_head, int h
   }
 }
 
-template <typename T, bool HALF, int V>
+template <typename T, bool HALF, int V, bool STREAM>
 __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RopeArgs a, Rows x, int D, int heads_per) {
   extern __shared__ float2 cs[];  // [rows of a tile][R / 2]
   const int64_t r0 = (int64_t)blockIdx.x * kTileRows;
@@ -195,7 +209,7 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RopeArgs a, Rows x,
     unit.set(j, a.R, cs + r * (a.R / 2));
     const T *in = (const T *)x.in + (r0 + r) * x.in_stride;
     T *out = (T *)x.out + (r0 + r) * x.out_stride;
-    unit.run(h0 + part, h1, share, [&](int h) { return in + h * D; }, [&](int h) { return out + h * D; });
+    unit.template run<STREAM>(h0 + part, h1, share, [&](int h) { return in + h * D; }, [&](int h) { return out + h * D; });
   });
 }
 
@@ -234,7 +248,7 @@ __device__ __forceinline__ T *page_of(T *pool, int s, const WriteArgs &w, int *i
   return pool + (((int64_t)(s >> w.bs_log2) * w.k.heads) << (w.bs_log2 + w.dh_log2));
 }
 
-template <typename T, bool HALF>
+template <typename T, bool HALF, bool STREAM>
 __global__ __launch_bounds__(kRotThreads) void kv_write_kernel(RopeArgs a, WriteArgs w, int heads_per) {
   constexpr int VEC = 16 / sizeof(T);
   extern __shared__ float2 cs[];
@@ -280,7 +294,7 @@ __global__ __launch_bounds__(kRotThreads) void kv_write_kernel(RopeArgs a, Write
       const T *in = (const T *)w.v.in + (int64_t)(r0 + f) * w.v.in_stride + h * D + d0;
       u32x4_t v[VEC], vt[VEC];
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) v[i] = *(const u32x4_t *)(in + min(i, n - 1) * w.v.in_stride);
+      for (int i = 0; i < VEC; ++i) v[i] = load_as<STREAM, u32x4_t>(in + min(i, n - 1) * w.v.in_stride);
       if (sl < 0) continue;
       int at;
       T *out = page_of((T *)w.v_pool, sl, w, &at) + (((int64_t)h * D + d0) << w.bs_log2) + at;
@@ -307,7 +321,7 @@ __global__ __launch_bounds__(kRotThreads) void kv_write_kernel(RopeArgs a, Write
       unit.set(j, a.R, cs + r * (a.R / 2));
       const T *q = (const T *)w.q.in + (r0 + r) * w.q.in_stride;
       T *out = (T *)w.q.out + (r0 + r) * w.q.out_stride;
-      unit.run(h0 + part, hq1, share, [&](int h) { return q + h * D; }, [&](int h) { return out + h * D; });
+      unit.template run<STREAM>(h0 + part, hq1, share, [&](int h) { return q + h * D; }, [&](int h) { return out + h * D; });
     });
   if (k1 > k0)
     each_unit<false>(nr, a.per_head, k1 - k0, [&](int r, int j, int part, int share) {
@@ -318,7 +332,7 @@ __global__ __launch_bounds__(kRotThreads) void kv_write_kernel(RopeArgs a, Write
       const T *k = (const T *)w.k.in + (r0 + r) * w.k.in_stride;
       int at;
       T *page = page_of((T *)w.k_pool, sl, w, &at) + at * D;
-      unit.run(k0 + part, k1, share, [&](int h) { return k + h * D; },
+      unit.template run<STREAM>(k0 + part, k1, share, [&](int h) { return k + h * D; },
                [&](int h) { return page + ((int64_t)h << (w.bs_log2 + w.dh_log2)); });
     });
 }
@@ -354,7 +368,7 @@ __global__ __launch_bounds__(kRotThreads) void kv_write_any_kernel(RopeArgs a, W
       unit.set(j, a.R, cs + r * (a.R / 2));
       const T *q = (const T *)w.q.in + (r0 + r) * w.q.in_stride;
       T *out = (T *)w.q.out + (r0 + r) * w.q.out_stride;
-      unit.run(h0 + part, hq1, share, [&](int h) { return q + h * D; }, [&](int h) { return out + h * D; });
+      unit.template run<false>(h0 + part, hq1, share, [&](int h) { return q + h * D; }, [&](int h) { return out + h * D; });
     });
   if (k1 > k0)
     each_unit<true>(nr, a.per_head, k1 - k0, [&](int r, int j, int part, int share) {
@@ -363,7 +377,7 @@ __global__ __launch_bounds__(kRotThreads) void kv_write_any_kernel(RopeArgs a, W
       unit.set(j, a.R, cs + r * (a.R / 2));
       const T *k = (const T *)w.k.in + (r0 + r) * w.k.in_stride;
       T *page = page_of((T *)w.k_pool, slot[r], w, &at) + at * D;
-      unit.run(k0 + part, k1, share, [&](int h) { return k + h * D; },
+      unit.template run<false>(k0 + part, k1, share, [&](int h) { return k + h * D; },
                [&](int h) { return page + ((int64_t)h << (w.bs_log2 + w.dh_log2)); });
     });
 }
@@ -445,14 +459,24 @@ static int heads_per_wg(int heads, int64_t tiles) {
   return per;
 }
 
+// Whether rows are read past the last-level cache.  Pieces that leave part of a
+// 128-byte line for another load would have it fetched twice (halves of 64
+// bytes: 108 us, not 87, for 65,536 rows of 24 heads of 64).
+static bool streams(const RopeArgs &a, int D, int es, bool half, int heads) {
+  const int64_t bytes = (int64_t)a.rows * heads * D * es;
+  return bytes >= kStreamFrom && bytes < kStreamTo && D * es % 128 == 0 && (!half || a.R / 2 * es % 128 == 0);
+}
+
 template <typename T, int V>
 static void launch_rotary(const RopeArgs &a, const Rows &x, int D, bool half, hipStream_t stream) {
   const int64_t tiles = ((int64_t)a.rows + kTileRows - 1) / kTileRows;
   const int per = heads_per_wg(x.heads, tiles);
   const dim3 grid((unsigned)tiles, (x.heads + per - 1) / per);
   const size_t lds = kTileRows * (a.R / 2) * sizeof(float2);
-  hipLaunchKernelGGL((half ? rotary_kernel<T, true, V> : rotary_kernel<T, false, V>), grid, dim3(kRotThreads), lds, stream,
-                     a, x, D, per);
+  auto kernel = half ? rotary_kernel<T, true, V, false> : rotary_kernel<T, false, V, false>;
+  if constexpr (V * sizeof(T) == 16)
+    if (streams(a, D, sizeof(T), half, x.heads)) kernel = half ? rotary_kernel<T, true, V, true> : rotary_kernel<T, false, V, true>;
+  hipLaunchKernelGGL(kernel, grid, dim3(kRotThreads), lds, stream, a, x, D, per);
 }
 
 SM_API sm_status sm_rotary(const void *x, int64_t x_stride, const int32_t *pos, int rows, int heads, int head_dim,
@@ -491,8 +515,10 @@ static void launch_write(const RopeArgs &a, const WriteArgs &w, bool half, bool 
   const int heads = w.q.heads + 2 * w.k.heads, per = heads_per_wg(heads, tiles);
   const dim3 grid((unsigned)tiles, (heads + per - 1) / per);
   const size_t lds = kMostRows * (a.R / 2) * sizeof(float2);
-  const auto kernel = wide ? (half ? kv_write_kernel<T, true> : kv_write_kernel<T, false>)
-                           : (half ? kv_write_any_kernel<T, true> : kv_write_any_kernel<T, false>);
+  const bool past = streams(a, 1 << w.dh_log2, sizeof(T), half, heads);
+  const auto kernel = !wide  ? (half ? kv_write_any_kernel<T, true> : kv_write_any_kernel<T, false>)
+                      : past ? (half ? kv_write_kernel<T, true, true> : kv_write_kernel<T, false, true>)
+                             : (half ? kv_write_kernel<T, true, false> : kv_write_kernel<T, false, false>);
   hipLaunchKernelGGL(kernel, grid, dim3(kRotThreads), lds, stream, a, w, per);
 }
 
