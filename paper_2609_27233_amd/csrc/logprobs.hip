@@ -546,13 +546,22 @@ struct LogprobPlan {
   int slices, per_slice;
 };
 
-// Slices of a row: about kLpFill workgroups in all.  130 rows of 128,256 bf16
-// logits, 20 alternatives, us: 1 slice 29.5, 2 24.5, 4 23.0, 8 22.8; 16 rows, 8
-// and 16 slices: 16.6 and 22.7; 500 rows, 1, 2 and 3 slices: 37.0, 38.0, 41.6.
+// Slices of a row: about kLpFill workgroups in all.  128,256 bf16 logits and
+// 20 alternatives, us, with about 256, 512 and 1024 workgroups: 64 rows 16.4,
+// 15.4, 17.8; 130 rows 21.3, 19.8, 20.3; 200 rows 26.1, 23.1, 23.8; 500 rows
+// (one slice, one, two) 33.2, 32.5, 33.5.
 constexpr int kLpFill = 512;
-// Rows of up to kLpShort vectors are one wave's, and where there are kLpMany
-// rows all are: its fixed part is smaller, and nothing waits at a barrier.
-constexpr int kLpShort = 1024, kLpMany = 1536;
+// Rows of up to kLpShort vectors are one wave's, longer ones where there are
+// many rows: a wave alone has less to do once a row, and waits at no barrier.
+// Four waves and one, us: 8192 x 16,000 bf16 logits 76 and 54, 8192 x 50,257
+// 166 and 146, 4096 x 128,256 214 and 214; 1536 x 128,256 77 and 83.
+constexpr int kLpShort = 1024;
+constexpr int kLpMany = 1536, kLpManyVectors = 8192;  // this many rows of up to so many vectors,
+constexpr int kLpAll = 4096;                          // or this many of any length
+
+static bool one_wave_rows(int rows, int nvec) {
+  return nvec <= kLpShort || (rows >= kLpMany && nvec <= kLpManyVectors) || rows >= kLpAll;
+}
 
 // (no row is cut beyond kLpFill rows, so its counter is within the first 64 KiB)
 static_assert(kLpFill * kCounterStep * sizeof(int) <= 65536, "counters");
@@ -596,7 +605,7 @@ SM_API sm_status sm_token_logprobs(const void *logits, int64_t stride, int rows,
                       p.slices, p.per_slice, (int *)ws, sums, (uint64_t *)(sums + (size_t)rows * p.slices)};
   const dim3 grid((unsigned)((int64_t)rows * p.slices));
   const bool bf = dt == SM_BF16;
-  const bool short_row = p.slices == 1 && (nvec <= kLpShort || rows >= kLpMany);
+  const bool short_row = p.slices == 1 && one_wave_rows(rows, nvec);
   const auto kernel =
       short_row ? (bf ? (k ? logprobs_kernel<uint16_t, true, 1> : logprobs_kernel<uint16_t, false, 1>)
                       : (k ? logprobs_kernel<float, true, 1> : logprobs_kernel<float, false, 1>))
