@@ -773,8 +773,9 @@ typedef struct {
  *               of the forward call with respect to x, and its inverse
  *               where attn_scale is 1; 0: the forward map
  *  out, out_stride  as x; x itself (same address and stride) or no overlap
- * Any element-aligned address; 16-byte aligned rows with rot_dim a multiple
- * of 16 (fp32: 8) take the wide path.  No device errors.
+ * Any element-aligned address: rows are moved in the largest pieces of 16, 8,
+ * 4 or 2 bytes that divide the halves of the turned part (interleaved: that
+ * part) and the rest, and to which every row is aligned.  No device errors.
  */
 sm_status sm_rotary(const void *x, int64_t x_stride, const int32_t *pos,
                     int rows, int heads, int head_dim, const sm_rope_params *p,
@@ -841,10 +842,12 @@ typedef struct {
  *               null for 1
  *  scale        (host) finite
  *  h_out, n_out row strides as h; either may be null, not both.  Each may
- *               be an input itself (same address and stride) or overlaps
- *               nothing
+ *               be h, y or a gate of a row each (same address and stride),
+ *               but overlaps no other input and not the other output
  * Any element-aligned address; 16-byte aligned rows with d a multiple of 8
- * (fp32: 4) take the wide path.  No device errors.
+ * (fp32: 4) are read as they are, others in unaligned pieces.  Squares are
+ * summed in fp32: a row whose squares come to more than 3.4e38 is normed to
+ * 0; with eps 0 a row of zeros has NaN.  No device errors.
  */
 sm_status sm_block_norm(const void *h, int64_t h_stride, const void *y,
                         int64_t y_stride, int rows, int d, const sm_norm *post,
@@ -871,7 +874,7 @@ size_t sm_token_logprobs_workspace_bytes(int rows, int vocab, int k);
  *
  *  logits, stride  [rows][vocab] (dtype dt), row stride in elements (>= vocab)
  *  rows, vocab  (host) vocab >= 1
- *  scale        (host) 1 / temperature: > 0, at most 2e38
+ *  scale        (host) 1 / temperature: 1e-20 to 2e38
  *  tokens       [rows] -1 or an id in [0, vocab); null with logprob
  *  logprob, entropy  [rows] fp32 out; each may be null
  *  k            (host) 0 <= k <= min(SM_MAX_TOP, vocab)

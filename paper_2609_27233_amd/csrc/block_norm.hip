@@ -227,7 +227,13 @@ SM_API sm_status sm_block_norm(const void *h, int64_t h_stride, const void *y, i
   if (rows == 0) return SM_OK;
   if (!h || (!h_out && !n_out) || (n_out && !pre)) return SM_EINVAL;
   if (h_stride < d || (y && y_stride < d) || (gate && gate_stride != 0 && gate_stride < d)) return SM_EINVAL;
-  if ((h_out && h_out_stride < d) || (n_out && n_out_stride < d)) return SM_EINVAL;
+  if ((h_out && h_out_stride < d) || (n_out && n_out_stride < d) || (h_out && h_out == n_out)) return SM_EINVAL;
+  // an output in an input's place lies where that is read
+  const auto placed = [&](const void *out, int64_t out_stride) {
+    return rows == 1 || !out || ((out != h || out_stride == h_stride) && (out != y || out_stride == y_stride) &&
+                                 (out != gate || out_stride == gate_stride));
+  };
+  if (!placed(h_out, h_out_stride) || !placed(n_out, n_out_stride)) return SM_EINVAL;
   const int64_t es = dt == SM_BF16 ? 2 : 4;
   const auto aligned = [&](const void *p, int64_t stride) { return (uintptr_t)p % 16 == 0 && stride * es % 16 == 0; };
   const bool wide = d * es % 16 == 0 && aligned(h, h_stride) && (!y || aligned(y, y_stride)) &&

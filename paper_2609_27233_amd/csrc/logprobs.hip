@@ -591,7 +591,8 @@ SM_API sm_status sm_token_logprobs(const void *logits, int64_t stride, int rows,
                                    float *top_logprobs, void *ws, size_t ws_bytes, int32_t *err, hipStream_t stream) {
   if ((dt != SM_F32 && dt != SM_BF16) || rows < 0 || vocab < 1 || k < 0 || k > SM_MAX_TOP || k > vocab) return SM_EINVAL;
   const float c = (float)(scale * 1.4426950408889634);
-  if (!(scale > 0.f) || !std::isfinite(c) || stride < vocab) return SM_EINVAL;
+  // (p |d| is at most 16 / scale: 2^31 of them stay finite)
+  if (!(scale >= 1e-20f) || !std::isfinite(c) || stride < vocab) return SM_EINVAL;
   if (rows == 0) return SM_OK;
   if (!logits || (logprob && !tokens) || (k > 0 && !top_ids) || (uintptr_t)ws % 16 != 0) return SM_EINVAL;
   if (!ws || ws_bytes < sm_token_logprobs_workspace_bytes(rows, vocab, k)) return SM_EINVAL;

@@ -429,6 +429,11 @@ static void set_turns(const sm_rope_params *p, RopeArgs *a) {
   }
 }
 
+// Rows made in place lie where they are read.
+static bool placed(const void *in, int64_t in_stride, const void *out, int64_t out_stride, int rows) {
+  return in != out || in_stride == out_stride || rows == 1;
+}
+
 static bool aligned(const void *p, int64_t stride, int64_t bytes, int64_t es) {
   return (uintptr_t)p % bytes == 0 && stride * es % bytes == 0;
 }
@@ -488,7 +493,7 @@ SM_API sm_status sm_rotary(const void *x, int64_t x_stride, const int32_t *pos, 
   const int64_t width = (int64_t)heads * head_dim;
   if (x_stride < width || out_stride < width || (transpose != 0 && transpose != 1)) return SM_EINVAL;
   if (rows == 0) return SM_OK;
-  if (!x || !pos || !out) return SM_EINVAL;
+  if (!x || !pos || !out || !placed(x, x_stride, out, out_stride, rows)) return SM_EINVAL;
   const int es = dt == SM_BF16 ? 2 : 4;
   int v = 16 / es;  // features of a piece: the most that divide the head and are aligned in every row
   while (v > 1 && !(divides(p, head_dim, v) && aligned(x, x_stride, v * es, es) && aligned(out, out_stride, v * es, es)))
@@ -534,7 +539,8 @@ SM_API sm_status sm_kv_write_rotary(const sm_paged_cache *c, const int32_t *pos,
   if (k_stride < kv_width || v_stride < kv_width) return SM_EINVAL;
   if (num_q_heads > 0 && (q_stride < q_width || q_out_stride < q_width)) return SM_EINVAL;
   if (rows == 0) return SM_OK;
-  if (!pos || !slots || !k || !v || (num_q_heads > 0 && (!q || !q_out))) return SM_EINVAL;
+  if (!pos || !slots || !k || !v) return SM_EINVAL;
+  if (num_q_heads > 0 && (!q || !q_out || !placed(q, q_stride, q_out, q_out_stride, rows))) return SM_EINVAL;
   const int es = c->dtype == SM_BF16 ? 2 : 4;
   const bool wide = divides(p, D, 16 / es) && aligned(k, k_stride, 16, es) && aligned(v, v_stride, 16, es) &&
                     aligned(c->k_pool, 0, 16, es) && aligned(c->v_pool, 0, 16, es) &&

@@ -543,6 +543,13 @@ def _cache_here(cache: PagedCache, dev: int):
         raise SpanMergeError(f"expected a cache on the current device cuda:{dev}")
 
 
+def _shape(t, dims: int, name: str):
+    s = t.shape
+    if len(s) != dims:
+        raise SpanMergeError(f"{name}: expected {dims} dimensions, got {len(s)}")
+    return s
+
+
 def _rows(t):
     """Rows with a stride, which row_stride has looked at, for a call."""
     return None if t is None else (t,)
@@ -580,8 +587,7 @@ def rotary(x, pos, rope: bytes, out, transpose: bool = False, stream=None):
     """out[r, h] = x[r, h] turned by pos[r]; x, out [rows, heads, D], each row
     contiguous; out may be x.  transpose: the gradient of that with respect to x."""
     b = _calls()
-    rows, heads, D = x.shape
-    dt = x.dtype
+    (rows, heads, D), dt = _shape(x, 3, "x"), x.dtype
     sx, so = b.row_stride(x, dt, "x", rows, heads, D), b.row_stride(out, dt, "out", rows, heads, D)
     b.need(pos, rows, "pos")
     handle, dev = _here(stream)
@@ -595,7 +601,7 @@ def kv_write_rotary(cache: PagedCache, pos, slots, q, k, v, rope: bytes, q_out, 
     [rows, Hkv, D]; each row contiguous, so the three may be views of one buffer."""
     b = _calls()
     row_stride, dt, H, D = b.row_stride, cache.dtype, cache.H, cache.D
-    rows = k.shape[0]
+    rows = _shape(k, 3, "k")[0]
     sk, sv = row_stride(k, dt, "k", rows, H, D), row_stride(v, dt, "v", rows, H, D)
     b.need(pos, rows, "pos")
     b.need(slots, rows, "slots")
@@ -603,7 +609,7 @@ def kv_write_rotary(cache: PagedCache, pos, slots, q, k, v, rope: bytes, q_out, 
     if (q is None) != (q_out is None):
         raise SpanMergeError("q and q_out go together")
     if q is not None:
-        hq = q.shape[1]
+        hq = _shape(q, 3, "q")[1]
         sq, so = row_stride(q, dt, "q", rows, hq, D), row_stride(q_out, dt, "q_out", rows, hq, D)
     handle, dev = _here(stream)
     _cache_here(cache, dev)
@@ -619,14 +625,26 @@ class Norm:
     def __init__(self, kind: str = "rms", gain=None, bias=None, eps: float = 1e-5):
         if kind not in NORM_KINDS:
             raise SpanMergeError(f"unknown norm: {kind!r}")
-        self.gain, self.bias = gain, bias
-        self.packed = bytes(NormParams(NORM_KINDS[kind], eps, _ptr(gain), _ptr(bias)))
+        self.kind, self.eps, self.gain, self.bias = NORM_KINDS[kind], eps, gain, bias
+        self._pack()
 
-    def look(self, dtype, d: int, dev: int, name: str):
-        for t in (self.gain, self.bias):
-            if t is not None and (t.dtype is not dtype or t.numel() != d or t.get_device() != dev):
+    def _pack(self):
+        self.packed = bytes(NormParams(self.kind, self.eps, _ptr(self.gain), _ptr(self.bias)))
+        self.at = [None if t is None else t.data_ptr() for t in (self.gain, self.bias)]
+
+    def look(self, dtype, d: int, dev: int, name: str) -> bytes:
+        """The structure for a call over rows of d values; the tensors may have new memory (a module that was moved)."""
+        moved = False
+        for t, at in zip((self.gain, self.bias), self.at):
+            if t is None:
+                continue
+            if t.dtype is not dtype or t.numel() != d or t.get_device() != dev:
                 raise SpanMergeError(f"{name}: expected {d} values of {dtype} on cuda:{dev}, got {t.numel()} of {t.dtype} "
                                      f"on {t.device}")
+            moved |= t.data_ptr() != at
+        if moved:
+            self._pack()
+        return self.packed
 
 
 def norm_params(kind: str = "rms", gain=None, bias=None, eps: float = 1e-5) -> Norm:
@@ -639,7 +657,7 @@ def block_norm(h, y, h_out, n_out, post: Optional[Norm] = None, gate=None, scale
     sum; [rows, d] with contiguous rows.  y None: h alone; gate [d] or
     [rows, d]; h_out or n_out may be None, or an input itself."""
     b = _calls()
-    row_stride, (rows, d), dt = b.row_stride, h.shape, h.dtype
+    row_stride, (rows, d), dt = b.row_stride, _shape(h, 2, "h"), h.dtype
     sh = row_stride(h, dt, "h", rows, d)
     sy = 0 if y is None else row_stride(y, dt, "y", rows, d)
     sho = 0 if h_out is None else row_stride(h_out, dt, "h_out", rows, d)
@@ -651,13 +669,10 @@ def block_norm(h, y, h_out, n_out, post: Optional[Norm] = None, gate=None, scale
         else:
             sg = row_stride(gate, dt, "gate", rows, d)
     handle, dev = _here(stream)
-    if post is not None:
-        post.look(dt, d, dev, "post")
-    if pre is not None:
-        pre.look(dt, d, dev, "pre")
-    st = b.sm_block_norm((h,), sh, _rows(y), sy, rows, d, None if post is None else post.packed, _rows(gate), sg, scale,
-                         None if pre is None else pre.packed, dtype_code(dt), _rows(h_out), sho, _rows(n_out), sno,
-                         handle, dev)
+    po = None if post is None else post.look(dt, d, dev, "post")
+    pr = None if pre is None else pre.look(dt, d, dev, "pre")
+    st = b.sm_block_norm((h,), sh, _rows(y), sy, rows, d, po, _rows(gate), sg, scale, pr, dtype_code(dt), _rows(h_out), sho,
+                         _rows(n_out), sno, handle, dev)
     _check(st, "sm_block_norm")
 
 
@@ -670,7 +685,7 @@ def token_logprobs(logits, tokens, logprob, entropy, top_ids, top_logprobs, ws, 
     largest logits of each row of logits [rows, vocab] (contiguous rows);
     scale = 1 / temperature.  Each output may be None."""
     b = _calls()
-    (rows, vocab), dt, need = logits.shape, logits.dtype, b.need
+    (rows, vocab), dt, need = _shape(logits, 2, "logits"), logits.dtype, b.need
     sl = b.row_stride(logits, dt, "logits", rows, vocab)
     k = 0
     if tokens is not None:

@@ -58,7 +58,7 @@ def test_rotary_argument_checks(L):
     assert call() == sm.SM_OK and call(x=None, pos=None, out=None) == sm.SM_OK        # no row: nothing to do
     for kw in (dict(rows=-1), dict(heads=0), dict(heads=1025), dict(D=1), dict(D=258), dict(D=64), dict(sx=4095),
                dict(so=4095), dict(dt=2), dict(back=2), dict(rows=1, x=None), dict(rows=1, pos=None),
-               dict(rows=1, out=None)):
+               dict(rows=1, out=None), dict(rows=2, so=4104)):                        # (in place with another stride)
         assert call(**kw) == sm.SM_EINVAL, kw
     assert L.sm_rotary(1, 4096, 1, 0, 32, 128, None, 0, sm.SM_BF16, 1, 4096, None) == sm.SM_EINVAL
 
@@ -71,7 +71,7 @@ def test_write_argument_checks(L):
     assert call(q=None, sq=0, hq=0, qo=None, so=0) == sm.SM_OK                        # K and V alone
     for kw in (dict(rows=-1), dict(hq=-1), dict(hq=1025), dict(sq=4095), dict(so=4095), dict(sk=1023), dict(sv=1023),
                dict(rows=1, pos=None), dict(rows=1, slots=None), dict(rows=1, q=None), dict(rows=1, k=None),
-               dict(rows=1, v=None), dict(rows=1, qo=None), dict(desc=_desc(num_blocks=1 << 27)),
+               dict(rows=1, v=None), dict(rows=1, qo=None), dict(rows=2, so=4104), dict(desc=_desc(num_blocks=1 << 27)),
                dict(desc=_desc(k_pool=None)), dict(desc=_desc(head_dim=64))):         # (rot_dim 128 of 64)
         assert call(**kw) == sm.SM_EINVAL, kw
 
@@ -88,7 +88,9 @@ def test_block_norm_argument_checks(L):
                dict(post=sm.NormParams(2, 1e-5, 1, None)), dict(pre=sm.NormParams(0, -1.0, 1, None)),
                dict(pre=sm.NormParams(0, NAN, 1, None)), dict(post=sm.NormParams(1, INF, 1, None)),
                dict(rows=1, h=None), dict(rows=1, ho=None, no=None), dict(rows=1, pre=None), dict(rows=1, sh=63),
-               dict(rows=1, sy=63), dict(rows=1, sg=63), dict(rows=1, sho=63), dict(rows=1, sno=0)):
+               dict(rows=1, sy=63), dict(rows=1, sg=63), dict(rows=1, sho=63), dict(rows=1, sno=0),
+               dict(rows=2, ho=64, no=64),                                            # one place for both outputs
+               dict(rows=2, h=64, ho=64, sho=72), dict(rows=2, y=64, no=64, sno=72), dict(rows=2, gate=64, no=64)):
         assert call(**kw) == sm.SM_EINVAL, kw
 
 
@@ -103,7 +105,7 @@ def test_logprobs_argument_checks(L):
         return L.sm_token_logprobs(x, s, rows, V, dt, scale, tok, lp, h, k, ids, tlp, ws, nbytes, err, None)
     assert call(rows=0) == sm.SM_OK
     for kw in (dict(x=None), dict(s=999), dict(rows=-1), dict(V=0), dict(dt=5), dict(scale=0.0), dict(scale=-1.0),
-               dict(scale=NAN), dict(scale=INF), dict(scale=3e38), dict(tok=None), dict(k=-1), dict(k=65), dict(V=7, k=8),
+               dict(scale=NAN), dict(scale=INF), dict(scale=3e38), dict(scale=9e-21), dict(tok=None), dict(k=-1), dict(k=65), dict(V=7, k=8),
                dict(ids=None), dict(ws=None), dict(ws=8), dict(nbytes=need - 1)):
         assert call(**kw) == sm.SM_EINVAL, kw
 
@@ -165,8 +167,27 @@ def test_wrong_types_and_sizes_are_refused(monkeypatch, L):
         sm.token_logprobs(_gpu((3, 8)), None, None, None, _gpu((2, 4), i32), None, _gpu(65536, torch.uint8))
     with pytest.raises(err, match="dtype"):
         sm.token_logprobs(_gpu((3, 8), torch.float16), None, None, None, None, None, _gpu(65536, torch.uint8))
+    for bad in (_gpu((6, 8)), _gpu((3, 2, 2, 4)), _gpu(8)):
+        with pytest.raises(err, match="x: expected 3 dimensions"):
+            sm.rotary(bad, _gpu(3, i32), sm.rope_params(8), _gpu((3, 2, 8)))
+    with pytest.raises(err, match="h: expected 2 dimensions"):
+        sm.block_norm(_gpu(8), None, None, _gpu(8), pre=sm.norm_params("rms"))
+    with pytest.raises(err, match="logits: expected 2 dimensions"):
+        sm.token_logprobs(_gpu(8), None, None, _gpu(1), None, None, _gpu(65536, torch.uint8))
     with pytest.raises(err, match="contiguous"):
         sm.rotary(_gpu((3, 2, 8)), _gpu(6, i32)[::2], sm.rope_params(8), _gpu((3, 2, 8)))
+
+
+def test_a_norm_follows_its_tensors(L):
+    gain = _gpu(8)
+    n = sm.norm_params("rms", gain)
+    where = lambda packed: sm.NormParams.from_buffer_copy(packed).gain                   # noqa: E731
+    assert where(n.look(torch.float32, 8, 0, "pre")) == gain.data_ptr()
+    gain.data = _gpu(8)
+    assert where(n.look(torch.float32, 8, 0, "pre")) == gain.data_ptr()
+    gain.data = _gpu(16)[::2]
+    with pytest.raises(sm.SpanMergeError, match="contiguous"):
+        n.look(torch.float32, 8, 0, "pre")
 
 
 def test_other_devices_are_refused(monkeypatch, L):

@@ -84,6 +84,20 @@ def test_logprobs_match(dt, size):
         assert_matches(x, tokens, k, scale, call(x, tokens, k, scale))
 
 
+@pytest.mark.parametrize("dt,rows,V", [(BF, 1536, 33333), (F32, 1600, 20001), (BF, 4096, 70003), (F32, 4097, 33001),
+                                       (BF, 511, 128256)], ids=str)
+def test_many_long_rows(dt, rows, V):
+    x = _rand((rows, V), dt, rows)
+    x[5, 7:] = -math.inf
+    tokens = torch.arange(rows, dtype=torch.int32, device=dev()) % V
+    say("logprobs", dt, rows, V)
+    got = call(x, tokens, 20)
+    values, _ = torch.topk(x[6:].float(), 20, dim=1)
+    assert torch.equal(x[6:].float().gather(1, got[2][6:].long()), values)
+    some = torch.tensor([0, 1, 5, 6, rows // 2, rows - 2, rows - 1], device=dev())
+    assert_matches(x[some], tokens[some], 20, 1.0, [t[some] for t in got])
+
+
 def _orders(V):
     g = torch.Generator(device="cuda").manual_seed(V)
     up = torch.arange(V, device=dev(), dtype=F32) / V * 8
