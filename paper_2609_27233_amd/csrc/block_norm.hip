@@ -3,13 +3,20 @@
 //
 // Each row is read and written once: the row's features stay in registers
 // (fp32) between the norms, so both norms, the gate and the sum cost no
-// traffic beyond h, y, h_out and n_out, which bound the call.  LayerNorm
-// takes its mean first and sums squares of the differences from registers.
+// traffic beyond h, y, h_out and n_out, which bound the call: 39,328 bf16 rows
+// of 4096 take 220 us (5.9 TB/s; a plain copy of 1 GiB reaches 5.1), with a
+// norm behind y and a gate 230.  Few rows are bound by the loads' latency and
+// the sums' barriers: 16 rows of 4096 2.7 and 3.5 us.  LayerNorm takes its
+// mean first and sums squares of the differences from registers.
 //
 // A row is held by 8 threads to 1024, two 16-byte chunks each, so that its
-// loads are all in flight at once and short rows fill a wave.  Rows that 16
-// bytes do not divide are read by the same chunks at the alignment they have,
-// the last one by features.
+// loads are all in flight at once and short rows fill a wave.  One chunk each
+// (twice the threads) is faster without a norm behind y (39,328 rows of 4096
+// 218 us) and for few rows, but has more waves wait for each sum where there
+// are two (265 us); four are slower for all but rows of 16,384 (16 rows of
+// 4096 4.1 us).  Rows that 16 bytes do not divide are read by the same chunks
+// at the alignment they have, the last one by features (16,384 rows of 4095 bf16
+// features 120 us, of 4096 93).
 #include <cmath>
 
 #include "vec16.hpp"
@@ -61,14 +68,13 @@ template <typename T, bool WHOLE>
 struct Chunk {
   static constexpr int VEC = Vec16<T>::N;
   float f[VEC];
-  __device__ __forceinline__ void load(const void *row, int64_t offset, int at, int d) {
+  static __device__ __forceinline__ u32x4_t load(const void *row, int64_t offset, int at, int d) {
     const T *p = (const T *)row + offset + at;
     u32x4_t v;
     if (WHOLE) {
-      Vec16<T>::open(*(const u32x4_t *)p, f);
+      v = *(const u32x4_t *)p;
     } else if (at + VEC <= d) {
       __builtin_memcpy(&v, p, 16);
-      Vec16<T>::open(v, f);
     } else {  // whole words, and for bf16 a half
       const int n = (d - at) * (int)sizeof(T);
 #pragma unroll
@@ -78,8 +84,8 @@ struct Chunk {
         else if (4 * i < n) x = *(const uint16_t *)((const char *)p + 4 * i);
         v[i] = x;
       }
-      Vec16<T>::open(v, f);
     }
+    return v;
   }
   __device__ __forceinline__ void store(void *row, int64_t offset, int at, int d) const {
     T *p = (T *)row + offset + at;
@@ -100,11 +106,30 @@ struct Chunk {
   }
 };
 
+// Whether a row's gate, gain and bias are on their way before they are used.
+// Aligned rows gain by it (16,384 fp32 rows of 2048 with both norms and a gate
+// 94 us, 102 without; 16 bf16 rows of 4096 3.5 and 4.0); workgroups of 1024
+// threads, of which a compute unit then holds one and not two, lose (8192
+// bf16 rows of 16,384 245 and 209), and so do unaligned rows (16,384 rows of
+// 2049 78 and 66).
+template <bool WHOLE, int TPR>
+constexpr bool kEarly = WHOLE && TPR < 1024;
+
 // x <- norm(x), the row spread over TPR threads, NV chunks a thread.
 template <typename T, bool WHOLE, int NV, int TPR>
 __device__ __forceinline__ void norm_row(Chunk<T, WHOLE> (&x)[NV], int kind, float eps, const void *gain, const void *bias,
                                          int d, int at0, float *red) {
   constexpr int VEC = Vec16<T>::N, STEP = TPR * VEC;
+  u32x4_t gains[NV], biases[NV];
+  const auto load = [&](int v) {
+    const int at = at0 + v * STEP;
+    if (at >= d) return;
+    if (gain) gains[v] = Chunk<T, WHOLE>::load(gain, 0, at, d);
+    if (bias) biases[v] = Chunk<T, WHOLE>::load(bias, 0, at, d);
+  };
+  if (kEarly<WHOLE, TPR>)
+#pragma unroll
+    for (int v = 0; v < NV; ++v) load(v);
   if (kind == SM_NORM_LAYER) {
     float s = 0.f;
 #pragma unroll
@@ -128,14 +153,15 @@ __device__ __forceinline__ void norm_row(Chunk<T, WHOLE> (&x)[NV], int kind, flo
   for (int v = 0; v < NV; ++v) {
     const int at = at0 + v * STEP;
     if (at >= d) continue;
-    Chunk<T, WHOLE> g, b;
-    if (gain) g.load(gain, 0, at, d);
-    if (bias) b.load(bias, 0, at, d);
+    if (!kEarly<WHOLE, TPR>) load(v);
+    float g[VEC], b[VEC];
+    if (gain) Vec16<T>::open(gains[v], g);
+    if (bias) Vec16<T>::open(biases[v], b);
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
       float n = x[v].f[e] * inv;
-      if (gain) n *= g.f[e];
-      if (bias) n += b.f[e];
+      if (gain) n *= g[e];
+      if (bias) n += b[e];
       x[v].f[e] = n;
     }
   }
@@ -153,16 +179,34 @@ __global__ __launch_bounds__(wg_threads(TPR)) void block_norm_kernel(NormArgs a)
   const bool there = row < a.rows;
   const int64_t r = there ? row : a.rows - 1;  // (all lanes take part in the sums)
   const int at0 = threadIdx.x % TPR * VEC;
+  u32x4_t hv[NV], yv[NV], gates[NV];
+  const auto load = [&](u32x4_t (&to)[NV], int v, const void *p, int64_t stride) {
+    to[v] = u32x4_t{0, 0, 0, 0};
+    if (p && at0 + v * STEP < a.d) to[v] = Chunk<T, WHOLE>::load(p, r * stride, at0 + v * STEP, a.d);
+  };
+  if constexpr (kEarly<WHOLE, TPR>) {  // (in the order of their use)
+#pragma unroll
+    for (int v = 0; v < NV; ++v) load(yv, v, a.y, a.sy);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) load(hv, v, a.h, a.sh);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) load(gates, v, a.gate, a.sg);
+  } else {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int at = at0 + v * STEP;
+      hv[v] = yv[v] = u32x4_t{0, 0, 0, 0};
+      if (at < a.d) {
+        hv[v] = Chunk<T, WHOLE>::load(a.h, r * a.sh, at, a.d);
+        if (a.y) yv[v] = Chunk<T, WHOLE>::load(a.y, r * a.sy, at, a.d);
+      }
+    }
+  }
   Chunk<T, WHOLE> h[NV], y[NV];
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
-    const int at = at0 + v * STEP;
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) h[v].f[e] = y[v].f[e] = 0.f;
-    if (at < a.d) {
-      h[v].load(a.h, r * a.sh, at, a.d);
-      if (a.y) y[v].load(a.y, r * a.sy, at, a.d);
-    }
+    Vec16<T>::open(hv[v], h[v].f);
+    Vec16<T>::open(yv[v], y[v].f);
   }
   if (a.y) {
     if (a.post != kNone) norm_row<T, WHOLE, NV, TPR>(y, a.post, a.eps_post, a.g_post, a.b_post, a.d, at0, red);
@@ -170,11 +214,12 @@ __global__ __launch_bounds__(wg_threads(TPR)) void block_norm_kernel(NormArgs a)
     for (int v = 0; v < NV; ++v) {
       const int at = at0 + v * STEP;
       if (at >= a.d) continue;
-      Chunk<T, WHOLE> g;
-      if (a.gate) g.load(a.gate, r * a.sg, at, a.d);
+      if (!kEarly<WHOLE, TPR>) load(gates, v, a.gate, a.sg);
+      float g[VEC];
+      if (a.gate) Vec16<T>::open(gates[v], g);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        const float t = a.gate ? y[v].f[e] * g.f[e] : y[v].f[e];
+        const float t = a.gate ? y[v].f[e] * g[e] : y[v].f[e];
         h[v].f[e] += a.scale * t;
       }
     }
