@@ -14,9 +14,10 @@
 // to ascend with it, then the index counted down, so that no two are equal.
 // Lanes' maxima give a bound below the k-th largest (a count over them, bit by
 // bit), after the first chunk and whenever the chunks seen have doubled.  A
-// wave notes which 16-byte vectors reach the bound, and looks at their logits
-// 64 vectors at a time: keys above the bound go to LDS, where they are reduced
-// to the k largest, with a bound of the wave's own, when there is no room.
+// wave notes the 16-byte vectors that reach the bound, in LDS, and looks at
+// their logits 64 vectors at a time: keys above the bound go to LDS, where they
+// are reduced to the k largest, with a bound of the wave's own, when there is
+// no room.
 //
 // A row is one workgroup's (of one wave where it is short), or for few rows
 // its slices are several ones', joined by the last to arrive at the row's
@@ -31,10 +32,15 @@ constexpr int kLpWaves = 4;                                   // waves of a work
 constexpr int kLpUnroll = 4;                                  // 16-byte vectors that a thread holds at a time
 constexpr int kLpChunk = 64 * kLpWaves * kLpUnroll;           // vectors that they hold
 constexpr int kKeep = 256;                                    // keys that a wave keeps: SM_MAX_TOP and one of each lane at least
-constexpr int kNoted = 64 + 2 * 64 * kLpUnroll;               // vectors that it has noted: two chunks', and those before
+constexpr int kNoted = 64 + 64 * kLpUnroll;                   // vectors that it has noted: a chunk's, and those before
 constexpr int kMostSlices = 64;                               // (one wave reads their sums)
 constexpr int kMostKeys = kLpWaves * kKeep;                   // of all slices of a row
 constexpr int kCounterStep = 32;                              // counters stand 128 bytes apart
+// Up to this many lanes' largest of a wave bound its first chunk, beyond it its
+// vectors' largest: the lanes' few largest are in different vectors, but all of
+// them are a weak bound.  64 rows of 2000 bf16 logits, us: 64 alternatives
+// 12.5 by lanes and 8.4 by vectors, 20 alternatives 6.1 and 6.9.
+constexpr int kLanesWanted = 32;
 constexpr float kLn2 = 0.69314718055994531f;
 constexpr float kLowest = -3.4028234663852886e38f;
 constexpr float kLift = 4.f;
@@ -163,16 +169,29 @@ __device__ __forceinline__ int keep_largest(uint64_t *buf, int n, int k, int bit
     for (int i = 0; i < NR; ++i) cnt += __popcll(__ballot(f(i)));
     return cnt;
   };
-  uint32_t v = 0;  // the k-th value
-  for (int b = 31 - LOW; b >= 0; --b) {
+  // The k-th value, bit by bit; or one that k keys reach, which is as good.
+  // Then, if more do, the least index (counted down) among the equal ones.
+  uint32_t v = 0, from = 0;
+  int c = n;
+  for (int b = 31 - LOW; b >= 0 && c != k; --b) {
     const uint32_t y = v | 1u << b;
-    if (count([&](int i) { return hi[i] >= y; }) >= k) v = y;
+    const int cy = count([&](int i) { return hi[i] >= y; });
+    if (cy >= k) {
+      v = y;
+      c = cy;
+    }
   }
-  const int above = count([&](int i) { return hi[i] > v; });
-  uint32_t from = ~0u << (bits - 1) << 1;  // the least index (counted down) among the equal ones
-  for (int b = bits - 1; b >= 0; --b) {
-    const uint32_t y = from | 1u << b;
-    if (above + count([&](int i) { return hi[i] == v && lo[i] >= y; }) >= k) from = y;
+  if (c != k) {
+    const int above = count([&](int i) { return hi[i] > v; });
+    from = ~0u << (bits - 1) << 1;
+    for (int b = bits - 1; b >= 0 && c != k; --b) {
+      const uint32_t y = from | 1u << b;
+      const int cy = above + count([&](int i) { return hi[i] == v && lo[i] >= y; });
+      if (cy >= k) {
+        from = y;
+        c = cy;
+      }
+    }
   }
   int at = 0;
 #pragma unroll
@@ -201,7 +220,8 @@ template <typename T>
 struct Candidates {
   static constexpr int LOW = sizeof(T) == 2 ? 16 : 0;
   uint64_t *buf;
-  int *noted;
+  u32x4_t *noted;  // vectors and their numbers
+  int *numbers;
   int n, vectors, k, bits;  // bits: of an index
   int ordered;     // a bound of an index below this is the lowest index of its value to come
   uint64_t bound;  // keys above it are wanted
@@ -220,39 +240,50 @@ struct Candidates {
     if (want) buf[n + lanes_below(mask)] = key;
     n += __popcll(mask);
   }
-  __device__ __forceinline__ void note(float m, int v) {
+  __device__ __forceinline__ void note(float m, int v, u32x4_t x) {
     const bool want = m >= least;
     const uint64_t mask = __ballot(want);
-    if (want) noted[vectors + lanes_below(mask)] = v;
+    if (want) {
+      const int at = vectors + lanes_below(mask);
+      noted[at] = x;
+      numbers[at] = v;
+    }
     vectors += __popcll(mask);
   }
-  // The noted vectors' logits; vector v of x begins at logit head + N v.
-  __device__ __forceinline__ void look(const u32x4_t *x, int head, int end) {
+  // The noted vectors' logits that reach the bound, one of each vector at a
+  // time; vector v begins at logit head + N v.
+  __device__ __forceinline__ void look(int head, int end) {
     constexpr int N = Vec16<T>::N;
     const int lane = threadIdx.x & 63;
     wave_order();
 #pragma unroll 1
     for (int i = 0; i < vectors; i += 64) {
-      int v = i + lane < vectors ? noted[i + lane] : end;
-      const bool valid = v < end;  // (behind the slice there are none)
-      v = valid ? v : 0;
+      const int v = i + lane < vectors ? numbers[i + lane] : end;
       u32x4_t w{0, 0, 0, 0};
-      if (valid) w = x[v];
+      uint32_t left = 0;
+      if (v < end) {  // (behind the slice there are none)
+        w = noted[i + lane];
+        float f[N];
+        Vec16<T>::open(w, f);
+#pragma unroll
+        for (int e = 0; e < N; ++e) left |= f[e] >= least ? 1u << e : 0u;
+      }
 #pragma unroll 1
-      for (int e = 0; e < N; ++e) {
+      while (__ballot(left != 0)) {
         if (n > kKeep - 64) {
           n = keep_largest<LOW>(buf, n, k, bits);
           if (n == k) raise(wave_min64(lane < n ? buf[lane] : ~0ull));
         }
-        float f;
-        if constexpr (sizeof(T) == 2) {
-          f = __uint_as_float(w[0] << 16);
-          w = u32x4_t{w[0] >> 16 | w[1] << 16, w[1] >> 16 | w[2] << 16, w[2] >> 16 | w[3] << 16, w[3] >> 16};
+        const int e = __builtin_ctz(left | 0x80000000u) % N;
+        uint32_t x;
+        if constexpr (N == 8) {
+          x = e < 4 ? (e < 2 ? w[0] : w[1]) : (e < 6 ? w[2] : w[3]);
+          x = e & 1 ? x & 0xffff0000u : x << 16;
         } else {
-          f = __uint_as_float(w[0]);
-          w = u32x4_t{w[1], w[2], w[3], 0};
+          x = e < 2 ? (e < 1 ? w[0] : w[1]) : (e < 3 ? w[2] : w[3]);
         }
-        put(f, head + N * v + e, valid);
+        put(__uint_as_float(x), head + N * v + e, left != 0);
+        left &= left - 1;
       }
     }
     vectors = 0;
@@ -317,7 +348,8 @@ template <typename T, bool TOP, int W>
 __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs a) {
   constexpr int N = Vec16<T>::N, LOW = Candidates<T>::LOW, THREADS = 64 * W, CHUNK = THREADS * kLpUnroll;
   __shared__ uint64_t keys[TOP ? W : 1][TOP ? kKeep : 1];
-  __shared__ int noted[TOP ? W : 1][TOP ? kNoted : 1];
+  __shared__ u32x4_t noted[TOP ? W : 1][TOP ? kNoted : 1];
+  __shared__ int numbers[TOP ? W : 1][TOP ? kNoted : 1];
   __shared__ float w_max[W], w_r[W], w_S[W], w_E[W];
   __shared__ uint32_t w_bound[W];
   __shared__ int w_n[W], last;
@@ -352,18 +384,22 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs a) {
     return m;
   };
   Sums s{kLowest, 0.f, 0.f};
-  Candidates<T> top{keys[TOP ? w : 0], noted[TOP ? w : 0], 0, 0, a.k, 32 - __clz(a.vocab), head + nvec * N, 0, -INFINITY};
+  Candidates<T> top{keys[TOP ? w : 0], noted[TOP ? w : 0], numbers[TOP ? w : 0], 0, 0, a.k, 32 - __clz(a.vocab), head + nvec * N, 0, -INFINITY};
   float best = -INFINITY;  // this lane's largest
-  // A bound below the slice's k-th largest: k / W of each wave's lanes hold
-  // its least one's value or more (few alternatives: k of one wave's lanes).
+  // A bound below the slice's k-th largest: k / W of the largest of each wave's
+  // lanes (few alternatives: k of one wave's) are the bound of its least one or
+  // more; or of its vectors (reached(o): how many are o or more).
   const bool one_wave = a.k < W;
-  auto wave_bound = [&]() {
-    const uint32_t o = order_of(best);
-    const int want = one_wave ? a.k : (a.k + W - 1) / W;
+  const int want = one_wave ? a.k : (a.k + W - 1) / W;
+  auto bound_of = [&](auto reached) {
     uint32_t b = 0;
     for (int bit = 31; bit >= 16; --bit)  // (the low bits are not worth their time)
-      if (__popcll(__ballot(o >= (b | 1u << bit))) >= want) b |= 1u << bit;
+      if (reached(b | 1u << bit) >= want) b |= 1u << bit;
     return b;
+  };
+  auto lanes_bound = [&]() {
+    const uint32_t o = order_of(best);
+    return bound_of([&](uint32_t b) { return __popcll(__ballot(o >= b)); });
   };
   auto use_bounds = [&]() {
     uint32_t b = one_wave ? 0 : ~0u;
@@ -382,15 +418,24 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs a) {
   if (t == 0 && tok >= 0 && tok < a.vocab) x_tok = Elem<T>::load(x + tok);
   if (begin < end) {
     fill(even, begin, Vec16<T>::kMinusInf);
+    float m[kLpUnroll];
 #pragma unroll
     for (int u = 0; u < kLpUnroll; ++u) {
       float f[N];
       Vec16<T>::open(even[u], f);
-      best = fmaxf(best, largest(f));
+      m[u] = largest(f);
+      best = fmaxf(best, m[u]);
     }
     const float mw = wave_max(best);
     uint32_t b = 0;
-    if constexpr (TOP) b = wave_bound();
+    if constexpr (TOP) {
+      b = want <= kLanesWanted ? lanes_bound() : bound_of([&](uint32_t b) {
+        int n = 0;
+#pragma unroll
+        for (int u = 0; u < kLpUnroll; ++u) n += __popcll(__ballot(order_of(m[u]) >= b));
+        return n;
+      });
+    }
     if (lane == 0) {
       w_max[w] = mw;
       w_bound[w] = b;
@@ -460,24 +505,26 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs a) {
       if (v0 + CHUNK <= end) {
         best = fmaxf(best, all);
         if (seen > 1 && (seen & (seen - 1)) == 0) {
-          const uint32_t b = wave_bound();
+          const uint32_t b = lanes_bound();
           if (lane == 0) __hip_atomic_store(w_bound + w, b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
           use_bounds();  // (another wave's may be an earlier one: a lower bound all the same)
         }
       }
       if (__ballot(all >= top.least)) {
 #pragma unroll
-        for (int u = 0; u < kLpUnroll; ++u) top.note(m[u], v0 + u * THREADS + t);
+        for (int u = 0; u < kLpUnroll; ++u) top.note(m[u], v0 + u * THREADS + t, cur[u]);
       }
     }
   };
   for (int v0 = begin, seen = 1; v0 < end; v0 += 2 * CHUNK, seen += 2) {
     load(odd, v0 + CHUNK);
     chunk(even, v0, seen);
+    if constexpr (TOP)
+      if (top.vectors > 64) top.look(head, end);
     load(even, v0 + 2 * CHUNK);
     if (v0 + CHUNK < end) chunk(odd, v0 + CHUNK, seen + 1);
     if constexpr (TOP)
-      if (top.vectors > 64 || v0 + 2 * CHUNK >= end) top.look(xv, head, end);
+      if (top.vectors > 64 || v0 + 2 * CHUNK >= end) top.look(head, end);
   }
   // Each wave's results, then the first one's of all waves; for a row of
   // several slices that twice, the second time of the slices' results.
