@@ -362,6 +362,30 @@ PyObject *need(PyObject *, PyObject *const *args, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
+// parameter(tensor, dtype, count, device, name): the address of a contiguous tensor of that type, device and number of
+// values; 0 for None
+PyObject *parameter(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  if (n != 5) {
+    PyErr_SetString(PyExc_TypeError, "parameter takes 5 arguments");
+    return nullptr;
+  }
+  PyObject *t = args[0];
+  if (t == Py_None) return PyLong_FromLong(0);
+  long has, at, count = PyLong_AsLong(args[2]), device = PyLong_AsLong(args[3]);
+  if (PyErr_Occurred() || !as_long(PyObject_CallMethodNoArgs(t, g_numel), &has) ||
+      !as_long(PyObject_CallMethodNoArgs(t, g_get_device), &at))
+    return nullptr;
+  const bool typed = is_dtype(t, args[1]);
+  if (PyErr_Occurred()) return nullptr;
+  if (!typed || has != count || at != device) {
+    PyErr_Format(g_type[kError], "%S: expected %ld values of %S on device %ld, got %ld on %ld%s", args[4], count, args[1], device,
+                 has, at, typed ? "" : " of another type");
+    return nullptr;
+  }
+  if (!is_true(PyObject_CallMethodNoArgs(t, g_is_contiguous), "expected a contiguous tensor")) return nullptr;
+  return PyObject_CallMethodNoArgs(t, g_data_ptr);
+}
+
 // row_stride(tensor, dtype, name, rows, inner, ...): the row stride of a [rows, *inner] tensor of that type whose
 // rows are contiguous (one row: its length)
 PyObject *row_stride(PyObject *, PyObject *const *args, Py_ssize_t n) {
@@ -405,6 +429,7 @@ PyMethodDef methods[] = {
     SM_CHECKED(SM_CHECKED_ENTRY)
     {"dtypes", (PyCFunction)(void (*)(void))dtypes, METH_FASTCALL, nullptr},
     {"need", (PyCFunction)(void (*)(void))need, METH_FASTCALL, nullptr},
+    {"parameter", (PyCFunction)(void (*)(void))parameter, METH_FASTCALL, nullptr},
     {"row_stride", (PyCFunction)(void (*)(void))row_stride, METH_FASTCALL, nullptr},
     {"merge_params", (PyCFunction)(void (*)(void))merge_params, METH_FASTCALL, nullptr},
     {"kv_proj_params", (PyCFunction)(void (*)(void))kv_proj_params, METH_FASTCALL, nullptr},

@@ -626,24 +626,14 @@ class Norm:
         if kind not in NORM_KINDS:
             raise SpanMergeError(f"unknown norm: {kind!r}")
         self.kind, self.eps, self.gain, self.bias = NORM_KINDS[kind], eps, gain, bias
-        self._pack()
+        self.at = None
 
-    def _pack(self):
-        self.packed = bytes(NormParams(self.kind, self.eps, _ptr(self.gain), _ptr(self.bias)))
-        self.at = [None if t is None else t.data_ptr() for t in (self.gain, self.bias)]
-
-    def look(self, dtype, d: int, dev: int, name: str) -> bytes:
-        """The structure for a call over rows of d values; the tensors may have new memory (a module that was moved)."""
-        moved = False
-        for t, at in zip((self.gain, self.bias), self.at):
-            if t is None:
-                continue
-            if t.dtype is not dtype or t.numel() != d or t.get_device() != dev:
-                raise SpanMergeError(f"{name}: expected {d} values of {dtype} on cuda:{dev}, got {t.numel()} of {t.dtype} "
-                                     f"on {t.device}")
-            moved |= t.data_ptr() != at
-        if moved:
-            self._pack()
+    def look(self, b, dtype, d: int, dev: int, name: str) -> bytes:
+        """The structure for a call over rows of d values (the tensors may have
+        new memory since the last one: a module that was moved)."""
+        at = (b.parameter(self.gain, dtype, d, dev, name), b.parameter(self.bias, dtype, d, dev, name))
+        if at != self.at:
+            self.packed, self.at = bytes(NormParams(self.kind, self.eps, *at)), at
         return self.packed
 
 
@@ -669,8 +659,8 @@ def block_norm(h, y, h_out, n_out, post: Optional[Norm] = None, gate=None, scale
         else:
             sg = row_stride(gate, dt, "gate", rows, d)
     handle, dev = _here(stream)
-    po = None if post is None else post.look(dt, d, dev, "post")
-    pr = None if pre is None else pre.look(dt, d, dev, "pre")
+    po = None if post is None else post.look(b, dt, d, dev, "post")
+    pr = None if pre is None else pre.look(b, dt, d, dev, "pre")
     st = b.sm_block_norm((h,), sh, _rows(y), sy, rows, d, po, _rows(gate), sg, scale, pr, dtype_code(dt), _rows(h_out), sho,
                          _rows(n_out), sno, handle, dev)
     _check(st, "sm_block_norm")

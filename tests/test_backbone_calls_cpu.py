@@ -181,13 +181,19 @@ def test_wrong_types_and_sizes_are_refused(monkeypatch, L):
 def test_a_norm_follows_its_tensors(L):
     gain = _gpu(8)
     n = sm.norm_params("rms", gain)
-    where = lambda packed: sm.NormParams.from_buffer_copy(packed).gain                   # noqa: E731
-    assert where(n.look(torch.float32, 8, 0, "pre")) == gain.data_ptr()
-    gain.data = _gpu(8)
-    assert where(n.look(torch.float32, 8, 0, "pre")) == gain.data_ptr()
+
+    def look():
+        return sm.NormParams.from_buffer_copy(n.look(sm._calls(), torch.float32, 8, 0, "pre"))
+    first = look()
+    assert first.gain == gain.data_ptr() and first.bias is None and first.kind == 0
+    old, gain.data = gain.data, _gpu(8)
+    assert look().gain == gain.data_ptr() != old.data_ptr()
     gain.data = _gpu(16)[::2]
     with pytest.raises(sm.SpanMergeError, match="contiguous"):
-        n.look(torch.float32, 8, 0, "pre")
+        look()
+    for other in (_gpu(9), _gpu(8, torch.bfloat16)):
+        with pytest.raises(sm.SpanMergeError, match="pre: expected 8 values"):
+            sm.norm_params("rms", other).look(sm._calls(), torch.float32, 8, 0, "pre")
 
 
 def test_other_devices_are_refused(monkeypatch, L):
