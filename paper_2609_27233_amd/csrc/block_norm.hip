@@ -5,8 +5,8 @@
 // (fp32) between the norms, so both norms, the gate and the sum cost no
 // traffic beyond h, y, h_out and n_out, which bound the call: 39,328 bf16 rows
 // of 4096 take 220 us (5.9 TB/s; a plain copy of 1 GiB reaches 5.1), with a
-// norm behind y and a gate 230.  Few rows are bound by the loads' latency and
-// the sums' barriers: 16 rows of 4096 2.7 and 3.5 us.  LayerNorm takes its
+// norm behind y and a gate 228.  Few rows are bound by the loads' latency and
+// the sums' barriers: 16 rows of 4096 2.6 and 3.4 us.  LayerNorm takes its
 // mean first and sums squares of the differences from registers.
 //
 // A row is held by 8 threads to 1024, two 16-byte chunks each, so that its
@@ -32,7 +32,7 @@ struct NormArgs {
   void *h_out, *n_out;
   int64_t sh, sy, sg, sho, sno;
   int rows, d, post, pre;
-  float scale, eps_post, eps_pre;
+  float scale, eps_post, eps_pre, inv_d;
 };
 
 // Sum over the TPR threads that hold a row; `red`: a float for each of their waves.
@@ -118,7 +118,7 @@ constexpr bool kEarly = WHOLE && TPR < 1024;
 // x <- norm(x), the row spread over TPR threads, NV chunks a thread.
 template <typename T, bool WHOLE, int NV, int TPR>
 __device__ __forceinline__ void norm_row(Chunk<T, WHOLE> (&x)[NV], int kind, float eps, const void *gain, const void *bias,
-                                         int d, int at0, float *red) {
+                                         int d, float inv_d, int at0, float *red) {
   constexpr int VEC = Vec16<T>::N, STEP = TPR * VEC;
   u32x4_t gains[NV], biases[NV];
   const auto load = [&](int v) {
@@ -136,7 +136,7 @@ __device__ __forceinline__ void norm_row(Chunk<T, WHOLE> (&x)[NV], int kind, flo
     for (int v = 0; v < NV; ++v)
 #pragma unroll
       for (int e = 0; e < VEC; ++e) s += x[v].f[e];  // (features past d are zeros)
-    const float mean = row_sum<TPR>(s, red) / d;
+    const float mean = row_sum<TPR>(s, red) * inv_d;
 #pragma unroll
     for (int v = 0; v < NV; ++v)
 #pragma unroll
@@ -148,7 +148,9 @@ __device__ __forceinline__ void norm_row(Chunk<T, WHOLE> (&x)[NV], int kind, flo
   for (int v = 0; v < NV; ++v)
 #pragma unroll
     for (int e = 0; e < VEC; ++e) q += x[v].f[e] * x[v].f[e];
-  const float inv = 1.f / sqrtf(row_sum<TPR>(q, red) / d + eps);
+  // (the hardware's root, off by one unit, is for normal numbers: an epsilon of
+  // 0 may leave less)
+  const float m = row_sum<TPR>(q, red) * inv_d + eps, inv = m < 1.2e-38f ? 1.f / sqrtf(m) : __builtin_amdgcn_rsqf(m);
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     const int at = at0 + v * STEP;
@@ -209,7 +211,7 @@ __global__ __launch_bounds__(wg_threads(TPR)) void block_norm_kernel(NormArgs a)
     Vec16<T>::open(yv[v], y[v].f);
   }
   if (a.y) {
-    if (a.post != kNone) norm_row<T, WHOLE, NV, TPR>(y, a.post, a.eps_post, a.g_post, a.b_post, a.d, at0, red);
+    if (a.post != kNone) norm_row<T, WHOLE, NV, TPR>(y, a.post, a.eps_post, a.g_post, a.b_post, a.d, a.inv_d, at0, red);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int at = at0 + v * STEP;
@@ -229,7 +231,7 @@ __global__ __launch_bounds__(wg_threads(TPR)) void block_norm_kernel(NormArgs a)
     for (int v = 0; v < NV; ++v)
       if (at0 + v * STEP < a.d) h[v].store(a.h_out, r * a.sho, at0 + v * STEP, a.d);
   if (!a.n_out) return;
-  norm_row<T, WHOLE, NV, TPR>(h, a.pre, a.eps_pre, a.g_pre, a.b_pre, a.d, at0, red);
+  norm_row<T, WHOLE, NV, TPR>(h, a.pre, a.eps_pre, a.g_pre, a.b_pre, a.d, a.inv_d, at0, red);
   if (there)
 #pragma unroll
     for (int v = 0; v < NV; ++v)
@@ -289,7 +291,7 @@ SM_API sm_status sm_block_norm(const void *h, int64_t h_stride, const void *y, i
   NormArgs a{h, y, gate, post ? post->gain : nullptr, post ? post->bias : nullptr, pre ? pre->gain : nullptr,
              pre ? pre->bias : nullptr, h_out, n_out, h_stride, y_stride, gate_stride, h_out_stride, n_out_stride,
              rows, d, post ? post->kind : kNone, pre ? pre->kind : kNone, scale, post ? post->eps : 0.f,
-             pre ? pre->eps : 0.f};
+             pre ? pre->eps : 0.f, (float)(1.0 / d)};
   if (dt == SM_BF16) wide ? launch_block_norm<uint16_t, true>(a, stream) : launch_block_norm<uint16_t, false>(a, stream);
   else wide ? launch_block_norm<float, true>(a, stream) : launch_block_norm<float, false>(a, stream);
   return hipGetLastError() == hipSuccess ? SM_OK : SM_EHIP;

@@ -22,6 +22,13 @@
 // A row is one workgroup's (of one wave where it is short), or for few rows
 // its slices are several ones', joined by the last to arrive at the row's
 // counter.
+//
+// Many rows are bound by the read: 4096 rows of 128,256 bf16 logits (1.05 GB)
+// take 169 us without alternatives, 6.2 TB/s, 176 with one, and 174 to 205 with
+// 20, where the vector instructions of a compute unit are busy nine tenths of
+// the time; fp32 rows of the same size 167 us with 20.  Few rows are bound by
+// latency: 16 rows 5.3 us without alternatives and 9.4 with 8 (bound, look,
+// sort, then the same of the slices' keys).
 #include <cmath>
 
 #include "vec16.hpp"

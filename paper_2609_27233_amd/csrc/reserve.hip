@@ -8,7 +8,10 @@
 // block first, and the taken ones popped in request order, lowest first, so
 // the state is the one of a rollback followed by an append.  The rows'
 // positions and slots follow in the same launch, or for many rows in a
-// second one over all compute units.
+// second one over all compute units.  What bounds it is the chain of dependent
+// reads (request, length, blocks, stores) and barriers, not its bytes: 16
+// requests of a row each 3.4 us, 256 of four rows 5.2, and 16 prompts of 2458
+// rows (354 KB) 7.1 and 3.0 for the two launches.
 #include "cache_meta.hpp"
 
 namespace sm {

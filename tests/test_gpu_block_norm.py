@@ -166,6 +166,17 @@ def test_zero_rows_and_special_values():
     sm.block_norm(e, e, e, e, pre=n)
 
 
+def test_mean_squares_below_the_normal_numbers():
+    d = 4096
+    sign = torch.randint(0, 2, (3, d), generator=torch.Generator().manual_seed(1)) * 2.0 - 1
+    x = (4e-20 * sign).to(dev())                                         # squares of 1.6e-39
+    n = torch.empty_like(x)
+    sm.block_norm(x, None, None, n, pre=sm.norm_params("rms", eps=0.0))
+    # a square's rounding to steps of 2^-149, the sum's, the mean's; halved by the root, then that and the product
+    tol = (2.0 ** -150 / 1.6e-39 + SUM + 2 ** -150 / 1.6e-39) / 2 + 4 * U
+    assert float((n.double().cpu() - sign).abs().max()) <= tol
+
+
 def test_many_rows():
     """More rows than a 16-bit grid, each its own."""
     rows, d = 300001, 16
