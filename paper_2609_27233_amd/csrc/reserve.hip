@@ -10,7 +10,7 @@
 // positions and slots follow in the same launch, or for many rows in a
 // second one over all compute units.  What bounds it is the chain of dependent
 // reads (request, length, blocks, stores) and barriers, not its bytes: 16
-// requests of a row each 3.4 us, 256 of four rows 5.2, and 16 prompts of 2458
+// requests of a row each 3.4 us, 256 of four rows 4.9, and 16 prompts of 2458
 // rows (354 KB) 7.1 and 3.0 for the two launches.
 #include "cache_meta.hpp"
 
@@ -296,10 +296,12 @@ SM_API sm_status sm_kv_reserve(const sm_paged_cache *c, const int32_t *seq_ids, 
   if ((int64_t)c->num_blocks * c->block_size > INT32_MAX) return SM_EINVAL;
   if (!row_offsets || (n > 0 && (!seq_ids || !rows)) || (max_rows > 0 && (!pos || !slots))) return SM_EINVAL;
   const ReserveArgs r{seq_ids, crop, rows, n, max_rows, row_offsets, pos, slots};
-  // One wave, four or sixteen, by the rows that a thread places: 64 rows 3.5,
-  // 3.7 and 4.9 us, 256 (of 64 requests) 5.1, 3.7 and 4.9, 512 (of 128)
-  // 4.5 and 5.0 with four and sixteen, 1024 (of 256) 6.1 and 5.2.
+  // 1, 4, 8 or 16 waves by the rows that a thread places, us: 64 rows 3.5, 3.7,
+  // 3.9, 4.9; 256 rows of 64 requests 5.1, 3.7, 3.9, 4.9; 512 of 128 with 4 and
+  // more waves 4.4, 4.0, 5.0, 1024 of 256 6.1, 4.9, 5.2; 4000 of 16 with 8 and
+  // more 8.1, 7.5.
   if (n <= 64 && max_rows <= 64) return launch_reserve<64>(a, r, stream);
-  if (n <= 256 && max_rows <= 512) return launch_reserve<256>(a, r, stream);
+  if (n <= 256 && max_rows <= 256) return launch_reserve<256>(a, r, stream);
+  if (n <= 512 && max_rows <= 1024) return launch_reserve<512>(a, r, stream);
   return launch_reserve<kMetaThreads>(a, r, stream);
 }

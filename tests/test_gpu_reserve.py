@@ -83,7 +83,8 @@ def test_reserve_matches_rollback_then_append(orc, case, order):
     _check(orc, oc, c, at.astype(np.int32), crop, rows, _reserve(c, at, crop, rows, sum(rows) + room))
 
 
-@pytest.mark.parametrize("n,top_len,top_rows", [(1, 5000, 3000), (33, 200, 40), (256, 90, 8), (1024, 40, 3), (1000, 33, 60)])
+@pytest.mark.parametrize("n,top_len,top_rows", [(1, 5000, 3000), (33, 200, 40), (256, 90, 8), (1024, 40, 3), (1000, 33, 60),
+                                                (500, 60, 2), (200, 50, 1), (40, 70, 1)])
 def test_reserve_random_batches(orc, n, top_len, top_rows):
     rng = np.random.RandomState(n)
     lens = rng.randint(0, top_len + 1, n)
