@@ -17,6 +17,7 @@
 // 4096 4.1 us).  Rows that 16 bytes do not divide are read by the same chunks
 // at the alignment they have, the last one by features (16,384 rows of 4095 bf16
 // features 120 us, of 4096 93).
+#include <algorithm>
 #include <cmath>
 
 #include "vec16.hpp"
@@ -257,6 +258,9 @@ static void launch_block_norm(const NormArgs &a, hipStream_t stream) {
   launch<T, WHOLE, 16 / VEC, 1024>(a, stream);  // d <= 16384: 2 (bf16) or 4 chunks
 }
 
+// Rows of a launch: its threads are counted in 32 bits, 1024 a row at most.
+constexpr int64_t kLaunchRows = 1 << 21;
+
 static bool norm_ok(const sm_norm *n) {
   return !n || ((n->kind == SM_NORM_RMS || n->kind == SM_NORM_LAYER) && n->eps >= 0.f && std::isfinite(n->eps));
 }
@@ -281,7 +285,7 @@ SM_API sm_status sm_block_norm(const void *h, int64_t h_stride, const void *y, i
                                  (out != gate || out_stride == gate_stride));
   };
   if (!placed(h_out, h_out_stride) || !placed(n_out, n_out_stride)) return SM_EINVAL;
-  const int64_t es = dt == SM_BF16 ? 2 : 4;
+  const int es = dt == SM_BF16 ? 2 : 4;
   const auto aligned = [&](const void *p, int64_t stride) { return (uintptr_t)p % 16 == 0 && stride * es % 16 == 0; };
   const bool wide = d * es % 16 == 0 && aligned(h, h_stride) && (!y || aligned(y, y_stride)) &&
                     (!gate || aligned(gate, gate_stride)) && (!h_out || aligned(h_out, h_out_stride)) &&
@@ -292,7 +296,16 @@ SM_API sm_status sm_block_norm(const void *h, int64_t h_stride, const void *y, i
              pre ? pre->bias : nullptr, h_out, n_out, h_stride, y_stride, gate_stride, h_out_stride, n_out_stride,
              rows, d, post ? post->kind : kNone, pre ? pre->kind : kNone, scale, post ? post->eps : 0.f,
              pre ? pre->eps : 0.f, (float)(1.0 / d)};
-  if (dt == SM_BF16) wide ? launch_block_norm<uint16_t, true>(a, stream) : launch_block_norm<uint16_t, false>(a, stream);
-  else wide ? launch_block_norm<float, true>(a, stream) : launch_block_norm<float, false>(a, stream);
-  return hipGetLastError() == hipSuccess ? SM_OK : SM_EHIP;
+  for (int64_t r = 0; r < rows; r += kLaunchRows) {
+    a.h = row_at(h, r, h_stride, es);
+    a.y = row_at(y, r, y_stride, es);
+    a.gate = row_at(gate, r, gate_stride, es);
+    a.h_out = row_at(h_out, r, h_out_stride, es);
+    a.n_out = row_at(n_out, r, n_out_stride, es);
+    a.rows = (int)std::min(rows - r, kLaunchRows);
+    if (dt == SM_BF16) wide ? launch_block_norm<uint16_t, true>(a, stream) : launch_block_norm<uint16_t, false>(a, stream);
+    else wide ? launch_block_norm<float, true>(a, stream) : launch_block_norm<float, false>(a, stream);
+    if (hipGetLastError() != hipSuccess) return SM_EHIP;
+  }
+  return SM_OK;
 }

@@ -29,6 +29,7 @@
 // the time; fp32 rows of the same size 167 us with 20.  Few rows are bound by
 // latency: 16 rows 5.3 us without alternatives and 9.4 with 8 (bound, look,
 // sort, then the same of the slices' keys).
+#include <algorithm>
 #include <cmath>
 
 #include "vec16.hpp"
@@ -620,6 +621,9 @@ static bool one_wave_rows(int rows, int nvec) {
 // (no row is cut beyond kLpFill rows, so its counter is within the first 64 KiB)
 static_assert(kLpFill * kCounterStep * sizeof(int) <= 65536, "counters");
 
+// Rows of a launch: its threads are counted in 32 bits, 64 a row where there are many.
+constexpr int64_t kLpLaunchRows = 1 << 24;
+
 static LogprobPlan plan_logprobs(int rows, int vocab, int k) {
   const int nvec = vocab / 4 + 1;  // (of fp32; bf16 rows have half as many)
   const int chunks = (nvec + kLpChunk - 1) / kLpChunk;
@@ -656,9 +660,8 @@ SM_API sm_status sm_token_logprobs(const void *logits, int64_t stride, int rows,
   p.per_slice = (chunks + p.slices - 1) / p.slices * kLpChunk;
   p.slices = (nvec + p.per_slice - 1) / p.per_slice;
   float4 *sums = (float4 *)((char *)ws + 65536);
-  const LogprobArgs a{logits, stride, rows, vocab, k, scale, c, tokens, logprob, entropy, top_ids, top_logprobs, err,
+  LogprobArgs a{logits, stride, rows, vocab, k, scale, c, tokens, logprob, entropy, top_ids, top_logprobs, err,
                       p.slices, p.per_slice, (int *)ws, sums, (uint64_t *)(sums + (size_t)rows * p.slices)};
-  const dim3 grid((unsigned)((int64_t)rows * p.slices));
   const bool bf = dt == SM_BF16;
   const bool short_row = p.slices == 1 && one_wave_rows(rows, nvec);
   const auto kernel =
@@ -666,6 +669,16 @@ SM_API sm_status sm_token_logprobs(const void *logits, int64_t stride, int rows,
                       : (k ? logprobs_kernel<float, true, 1> : logprobs_kernel<float, false, 1>))
                 : (bf ? (k ? logprobs_kernel<uint16_t, true, kLpWaves> : logprobs_kernel<uint16_t, false, kLpWaves>)
                       : (k ? logprobs_kernel<float, true, kLpWaves> : logprobs_kernel<float, false, kLpWaves>));
-  hipLaunchKernelGGL(kernel, grid, dim3(short_row ? 64 : 64 * kLpWaves), 0, stream, a);
-  return hipGetLastError() == hipSuccess ? SM_OK : SM_EHIP;
+  for (int64_t r = 0; r < rows; r += kLpLaunchRows) {
+    a.rows = (int)std::min(rows - r, kLpLaunchRows);
+    a.logits = row_at(logits, r, stride, 16 / n);
+    a.tokens = (const int32_t *)row_at(tokens, r, 1, 4);
+    a.logprob = (float *)row_at(logprob, r, 1, 4);
+    a.entropy = (float *)row_at(entropy, r, 1, 4);
+    a.top_ids = (int32_t *)row_at(top_ids, r, k, 4);
+    a.top_logprobs = (float *)row_at(top_logprobs, r, k, 4);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(a.rows * p.slices)), dim3(short_row ? 64 : 64 * kLpWaves), 0, stream, a);
+    if (hipGetLastError() != hipSuccess) return SM_EHIP;
+  }
+  return SM_OK;
 }

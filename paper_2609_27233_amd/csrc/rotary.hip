@@ -21,6 +21,7 @@
 // 32 bytes of a page's row; single rows (a decode step) are stored an element
 // at a time, which the layout of the pages asks for (39,328 rows of slots in
 // no order: 539 us).
+#include <algorithm>
 #include <cmath>
 
 #include "cache_meta.hpp"
@@ -391,6 +392,9 @@ __global__ __launch_bounds__(kRotThreads) void kv_write_any_kernel(RopeArgs a, W
 
 using namespace sm;
 
+// Rows of a launch: its threads are counted in 32 bits, 256 for 16 rows.
+constexpr int64_t kLaunchRows = 1 << 24;
+
 static bool rope_ok(const sm_rope_params *p, int head_dim) {
   if (!p || p->rot_dim < 2 || (p->rot_dim & 1) || p->rot_dim > head_dim) return false;
   if (p->layout != SM_ROPE_HALF && p->layout != SM_ROPE_INTERLEAVED) return false;
@@ -450,11 +454,9 @@ static bool divides(const sm_rope_params *p, int D, int v) {
 }
 
 // v: features of a piece
-static RopeArgs rope_args(const sm_rope_params *p, const int32_t *pos, int rows, int D, int v, int transpose) {
+static RopeArgs rope_args(const sm_rope_params *p, int D, int v, int transpose) {
   RopeArgs a;
   set_turns(p, &a);
-  a.pos = pos;
-  a.rows = rows;
   a.R = p->rot_dim;
   a.sign = transpose ? -1 : 1;
   a.scale = p->attn_scale;
@@ -503,20 +505,25 @@ SM_API sm_status sm_rotary(const void *x, int64_t x_stride, const int32_t *pos, 
   int v = 16 / es;  // features of a piece: the most that divide the head and are aligned in every row
   while (v > 1 && !(divides(p, head_dim, v) && aligned(x, x_stride, v * es, es) && aligned(out, out_stride, v * es, es)))
     v /= 2;
-  const RopeArgs a = rope_args(p, pos, rows, head_dim, v, transpose);
-  const Rows r{x, out, x_stride, out_stride, heads};
+  RopeArgs a = rope_args(p, head_dim, v, transpose);
   const bool half = p->layout == SM_ROPE_HALF;
-  if (dt == SM_BF16) {
-    if (v == 8) launch_rotary<uint16_t, 8>(a, r, head_dim, half, stream);
-    else if (v == 4) launch_rotary<uint16_t, 4>(a, r, head_dim, half, stream);
-    else if (v == 2) launch_rotary<uint16_t, 2>(a, r, head_dim, half, stream);
-    else launch_rotary<uint16_t, 1>(a, r, head_dim, half, stream);
-  } else {
-    if (v == 4) launch_rotary<float, 4>(a, r, head_dim, half, stream);
-    else if (v == 2) launch_rotary<float, 2>(a, r, head_dim, half, stream);
-    else launch_rotary<float, 1>(a, r, head_dim, half, stream);
+  for (int64_t first = 0; first < rows; first += kLaunchRows) {
+    a.pos = pos + first;
+    a.rows = (int)std::min(rows - first, kLaunchRows);
+    const Rows r{row_at(x, first, x_stride, es), row_at(out, first, out_stride, es), x_stride, out_stride, heads};
+    if (dt == SM_BF16) {
+      if (v == 8) launch_rotary<uint16_t, 8>(a, r, head_dim, half, stream);
+      else if (v == 4) launch_rotary<uint16_t, 4>(a, r, head_dim, half, stream);
+      else if (v == 2) launch_rotary<uint16_t, 2>(a, r, head_dim, half, stream);
+      else launch_rotary<uint16_t, 1>(a, r, head_dim, half, stream);
+    } else {
+      if (v == 4) launch_rotary<float, 4>(a, r, head_dim, half, stream);
+      else if (v == 2) launch_rotary<float, 2>(a, r, head_dim, half, stream);
+      else launch_rotary<float, 1>(a, r, head_dim, half, stream);
+    }
+    if (hipGetLastError() != hipSuccess) return SM_EHIP;
   }
-  return hipGetLastError() == hipSuccess ? SM_OK : SM_EHIP;
+  return SM_OK;
 }
 
 template <typename T>
@@ -550,11 +557,18 @@ SM_API sm_status sm_kv_write_rotary(const sm_paged_cache *c, const int32_t *pos,
   const bool wide = divides(p, D, 16 / es) && aligned(k, k_stride, 16, es) && aligned(v, v_stride, 16, es) &&
                     aligned(c->k_pool, 0, 16, es) && aligned(c->v_pool, 0, 16, es) &&
                     (num_q_heads == 0 || (aligned(q, q_stride, 16, es) && aligned(q_out, q_out_stride, 16, es)));
-  const RopeArgs a = rope_args(p, pos, rows, D, wide ? 16 / es : 1, 0);
-  WriteArgs w{Rows{q, q_out, q_stride, q_out_stride, num_q_heads}, Rows{k, nullptr, k_stride, 0, c->num_kv_heads},
-              Rows{v, nullptr, v_stride, 0, c->num_kv_heads}, slots, c->k_pool, c->v_pool, c->err, ca.bs_log2,
-              ca.dh_log2, c->num_blocks * c->block_size};
-  if (c->dtype == SM_BF16) launch_write<uint16_t>(a, w, p->layout == SM_ROPE_HALF, wide, stream);
-  else launch_write<float>(a, w, p->layout == SM_ROPE_HALF, wide, stream);
-  return hipGetLastError() == hipSuccess ? SM_OK : SM_EHIP;
+  RopeArgs a = rope_args(p, D, wide ? 16 / es : 1, 0);
+  const int hkv = c->num_kv_heads;
+  for (int64_t r = 0; r < rows; r += kLaunchRows) {
+    a.pos = pos + r;
+    a.rows = (int)std::min(rows - r, kLaunchRows);
+    const WriteArgs w{Rows{row_at(q, r, q_stride, es), row_at(q_out, r, q_out_stride, es), q_stride, q_out_stride, num_q_heads},
+                      Rows{row_at(k, r, k_stride, es), nullptr, k_stride, 0, hkv},
+                      Rows{row_at(v, r, v_stride, es), nullptr, v_stride, 0, hkv},
+                      slots + r, c->k_pool, c->v_pool, c->err, ca.bs_log2, ca.dh_log2, c->num_blocks * c->block_size};
+    if (c->dtype == SM_BF16) launch_write<uint16_t>(a, w, p->layout == SM_ROPE_HALF, wide, stream);
+    else launch_write<float>(a, w, p->layout == SM_ROPE_HALF, wide, stream);
+    if (hipGetLastError() != hipSuccess) return SM_EHIP;
+  }
+  return SM_OK;
 }

@@ -5,6 +5,14 @@
 
 namespace sm {
 
+// The address of row `row` (no rows: none).
+static inline const void *row_at(const void *p, int64_t row, int64_t stride, int es) {
+  return p ? (const char *)p + row * stride * es : nullptr;
+}
+static inline void *row_at(void *p, int64_t row, int64_t stride, int es) {
+  return p ? (char *)p + row * stride * es : nullptr;
+}
+
 template <typename T> struct Vec16;
 template <> struct Vec16<float> {
   static constexpr int N = 4;

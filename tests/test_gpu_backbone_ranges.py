@@ -1,5 +1,7 @@
 """The calls around a backbone's projections beyond the sizes of their own
 tests: offsets past 32 bits, other streams, a captured step."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -62,6 +64,52 @@ def test_rows_past_32_bits():
         z = x[r].double()
         assert abs(float(lp[r]) - float(torch.log_softmax(z, 0)[V - 1])) <= 1e-4
         assert int(ids[r, 0]) == int(torch.argmax(x[r].float()))
+
+
+def test_rows_of_several_launches():
+    """More rows than one launch has threads for (counted in 32 bits), or takes."""
+    rows = (1 << 26) + 5                                     # 64 threads a row
+    x = torch.zeros((rows, 1), dtype=torch.bfloat16, device=dev())
+    lp = torch.full((rows,), -1.0, device=dev())
+    ws = torch.zeros(sm.token_logprobs_workspace_bytes(rows, 1, 1), dtype=torch.uint8, device=dev())
+    say("logprobs", rows)
+    ids = torch.full((rows, 1), -1, dtype=torch.int32, device=dev())
+    sm.token_logprobs(x, ids + 1, lp, None, ids, None, ws)
+    assert not lp.any() and not ids.any()
+    del x, lp, ids
+    for rows, d in (((1 << 29) + 70, 1), ((1 << 21) + 33, 64)):  # 256 threads for 32 rows
+        say("block_norm", rows, d)
+        x = torch.ones((rows, d), dtype=torch.bfloat16, device=dev())
+        x[rows - 2] = -3.0
+        n = torch.zeros_like(x)
+        sm.block_norm(x, None, None, n, pre=sm.norm_params("rms", eps=0.0))
+        assert (n[:-2] == 1).all() and (n[-2] == -1).all() and (n[-1] == 1).all()
+        del x, n
+    rows = (1 << 28) + 70                                    # 256 threads for 16 rows
+    say("rotary", rows)
+    x = torch.ones((rows, 1, 2), dtype=torch.bfloat16, device=dev())
+    pos = torch.zeros(rows, dtype=torch.int32, device=dev())
+    p = sm.rope_params(2)
+    pos[-1] = 1
+    out = torch.zeros_like(x)
+    sm.rotary(x, pos, p, out)
+    turn = torch.tensor([math.cos(1) - math.sin(1), math.cos(1) + math.sin(1)]).bfloat16().to(dev())
+    assert (out[:-1] == 1).all() and torch.equal(out[-1, 0], turn)
+    del x, out, pos
+    rows = (1 << 24) + 21                                    # the last 22 rows have slots
+    say("write", rows)
+    c = sm.PagedCache(dtype=torch.bfloat16, num_kv_heads=1, head_dim=64, block_size=16, num_blocks=4, max_seqs=1,
+                      max_blocks_per_seq=4)
+    slots = torch.full((rows,), -1, dtype=torch.int32, device=dev())
+    slots[-22:] = torch.arange(7, 29, dtype=torch.int32, device=dev())
+    k = torch.zeros((rows, 1, 64), dtype=torch.bfloat16, device=dev())
+    k[-22:] = torch.arange(1.0, 23.0, device=dev())[:, None, None].bfloat16()
+    sm.kv_write_rotary(c, torch.zeros_like(slots), slots, None, k, k, sm.rope_params(64), None)
+    got_k = c.k_pool[:2, 0].reshape(32, 64)
+    got_v = c.v_pool[:2, 0].transpose(1, 2).reshape(32, 64)
+    want = torch.zeros((32, 64), device=dev())
+    want[7:29] = torch.arange(1.0, 23.0, device=dev())[:, None]
+    assert torch.equal(got_k.float(), want) and torch.equal(got_v.float(), want) and c.error_bits() == 0
 
 
 def test_other_streams():
