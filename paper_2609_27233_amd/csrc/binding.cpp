@@ -81,6 +81,63 @@ bool as_long(PyObject *r, long *v) {
   return !(*v == -1 && PyErr_Occurred());
 }
 
+// What a tensor is, without a call per property: the DLPack standard's C
+// exchange interface, version 1, which torch.Tensor offers in a capsule.  Its
+// structures, as the standard lays them out (of the interface up to the one
+// function used here).
+struct DlVersion { uint32_t major, minor; };
+struct DlTensor {
+  void *data;
+  int32_t device_type, device_id;  // device type 1: host memory
+  int32_t ndim;
+  uint8_t code, bits;  // of a value: code 0 integer, 2 float, 4 bfloat16
+  uint16_t lanes;
+  int64_t *shape, *strides;
+  uint64_t byte_offset;
+};
+struct DlExchange {
+  DlVersion version;
+  void *previous, *allocator, *managed_from_object, *managed_to_object;
+  int (*tensor_from_object)(void *object, DlTensor *out);  // what it points to is the tensor's
+};
+
+const DlExchange *g_exchange;
+PyObject *g_plain[2];                       // the classes that it is asked for: others may have properties of their own
+PyObject *g_int32, *g_float32, *g_bf16;     // torch's types
+
+struct View : DlTensor {
+  long device() const { return device_type == 1 ? -1 : device_id; }
+  bool is(PyObject *dtype) const {
+    return lanes == 1 && (dtype == g_int32 ? code == 0 && bits == 32 : dtype == g_float32 ? code == 2 && bits == 32
+                                                                                           : code == 4 && bits == 16);
+  }
+  int64_t numel() const {
+    int64_t n = 1;
+    for (int i = 0; i < ndim; ++i) n *= shape[i];
+    return n;
+  }
+  bool contiguous() const {
+    int64_t width = 1;
+    for (int i = ndim - 1; i >= 0; --i) {
+      if (shape[i] != 1 && strides[i] != width) return numel() == 0;
+      width *= shape[i];
+    }
+    return true;
+  }
+  char *address() const { return data ? (char *)data + byte_offset : nullptr; }
+};
+
+// Whether v is a view of t, which is to be of type `dtype` (any, if that is
+// null): not for other classes and types, whose methods are called.
+bool view_of(PyObject *t, PyObject *dtype, View *v) {
+  PyObject *cls = (PyObject *)Py_TYPE(t);
+  if (!g_exchange || (cls != g_plain[0] && cls != g_plain[1])) return false;
+  if (dtype && dtype != g_int32 && dtype != g_float32 && dtype != g_bf16) return false;
+  if (g_exchange->tensor_from_object(t, v) == 0 && (v->strides || v->ndim == 0)) return true;
+  PyErr_Clear();
+  return false;
+}
+
 // tensor_address for the checked entries: a tensor of type `dtype` (unless
 // that is null) on the current device; one in a tuple of its own need not be
 // contiguous.
@@ -89,7 +146,12 @@ bool checked_address(PyObject *t, PyObject *dtype, long device, void **p) {
   if (t == Py_None) return true;
   const bool strided = PyTuple_CheckExact(t) && PyTuple_GET_SIZE(t) == 1;
   if (strided) t = PyTuple_GET_ITEM(t, 0);
-  long at;
+  View view;
+  if (view_of(t, dtype, &view) && view.device() == device && (strided || view.contiguous()) && (!dtype || view.is(dtype))) {
+    *p = view.address();
+    return true;
+  }
+  long at;  // (what is wrong, or another class)
   if (!as_long(PyObject_CallMethodNoArgs(t, g_get_device), &at)) return false;  // (-1: host memory)
   if (at != device) {
     PyErr_Format(g_type[kError], "expected tensors on the current device %ld, got one on %ld", device, at);
@@ -176,8 +238,6 @@ bool get(PyObject *o, A *v) {
     return !PyErr_Occurred();
   }
 }
-
-PyObject *g_int32, *g_float32;  // torch's types
 
 template <class A>
 bool get_checked(PyObject *o, A *v, long device) {
@@ -334,16 +394,24 @@ PyObject *setup(PyObject *, PyObject *types) {
   Py_RETURN_NONE;
 }
 
-// dtypes(int32, float32): torch's types, for the checked entries
-PyObject *dtypes(PyObject *, PyObject *const *args, Py_ssize_t n) {
-  if (n != 2) {
-    PyErr_SetString(PyExc_TypeError, "dtypes takes 2 arguments");
+// torch_types(int32, float32, bfloat16, Tensor, Parameter, exchange): torch's types and classes for the checked
+// entries, and its exchange interface (None: its methods are called)
+PyObject *torch_types(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  if (n != 6) {
+    PyErr_SetString(PyExc_TypeError, "torch_types takes 6 arguments");
     return nullptr;
   }
-  Py_INCREF(args[0]);
-  Py_XSETREF(g_int32, args[0]);
-  Py_INCREF(args[1]);
-  Py_XSETREF(g_float32, args[1]);
+  PyObject **to[] = {&g_int32, &g_float32, &g_bf16, &g_plain[0], &g_plain[1]};
+  for (int i = 0; i < 5; ++i) {
+    Py_INCREF(args[i]);
+    Py_XSETREF(*to[i], args[i]);
+  }
+  g_exchange = nullptr;
+  if (args[5] != Py_None) {
+    const auto *e = (const DlExchange *)PyCapsule_GetPointer(args[5], "dlpack_exchange_api");
+    if (!e) return nullptr;
+    if (e->version.major == 1 && e->tensor_from_object) g_exchange = e;
+  }
   Py_RETURN_NONE;
 }
 
@@ -354,7 +422,10 @@ PyObject *need(PyObject *, PyObject *const *args, Py_ssize_t n) {
     return nullptr;
   }
   long has, count = PyLong_AsLong(args[1]);
-  if ((count == -1 && PyErr_Occurred()) || !as_long(PyObject_CallMethodNoArgs(args[0], g_numel), &has)) return nullptr;
+  if (count == -1 && PyErr_Occurred()) return nullptr;
+  View view;
+  if (view_of(args[0], nullptr, &view)) has = (long)view.numel();
+  else if (!as_long(PyObject_CallMethodNoArgs(args[0], g_numel), &has)) return nullptr;
   if (has < count) {
     PyErr_Format(g_type[kError], "%S: expected %ld values, got %ld", args[2], count, has);
     return nullptr;
@@ -372,7 +443,11 @@ PyObject *parameter(PyObject *, PyObject *const *args, Py_ssize_t n) {
   PyObject *t = args[0];
   if (t == Py_None) return PyLong_FromLong(0);
   long has, at, count = PyLong_AsLong(args[2]), device = PyLong_AsLong(args[3]);
-  if (PyErr_Occurred() || !as_long(PyObject_CallMethodNoArgs(t, g_numel), &has) ||
+  if (PyErr_Occurred()) return nullptr;
+  View view;
+  if (view_of(t, args[1], &view) && view.is(args[1]) && view.numel() == count && view.device() == device && view.contiguous())
+    return PyLong_FromVoidPtr(view.address());
+  if (!as_long(PyObject_CallMethodNoArgs(t, g_numel), &has) ||
       !as_long(PyObject_CallMethodNoArgs(t, g_get_device), &at))
     return nullptr;
   const bool typed = is_dtype(t, args[1]);
@@ -395,6 +470,19 @@ PyObject *row_stride(PyObject *, PyObject *const *args, Py_ssize_t n) {
   }
   PyObject *t = args[0];
   const Py_ssize_t dims = n - 3;
+  View view;
+  if (view_of(t, args[1], &view) && view.is(args[1]) && view.ndim == dims) {
+    bool right = true;
+    long long width = 1, row = 0;
+    for (Py_ssize_t i = dims - 1; right && i >= 0; --i) {
+      const long long size = view.shape[i], s = view.strides[i];
+      right = size == PyLong_AsLongLong(args[3 + i]) && (i == 0 || size == 1 || s == width);
+      if (i == 0) row = size > 1 ? s : width;
+      width *= size;
+    }
+    if (PyErr_Occurred()) return nullptr;
+    if (right) return PyLong_FromLongLong(row);
+  }
   const bool typed = is_dtype(t, args[1]);
   if (PyErr_Occurred()) return nullptr;
   PyObject *shape = PyObject_GetAttr(t, g_shape), *stride = shape ? PyObject_CallMethodNoArgs(t, g_stride) : nullptr;
@@ -427,7 +515,7 @@ PyObject *row_stride(PyObject *, PyObject *const *args, Py_ssize_t n) {
 PyMethodDef methods[] = {
     SM_ENTRIES(SM_ENTRY)
     SM_CHECKED(SM_CHECKED_ENTRY)
-    {"dtypes", (PyCFunction)(void (*)(void))dtypes, METH_FASTCALL, nullptr},
+    {"torch_types", (PyCFunction)(void (*)(void))torch_types, METH_FASTCALL, nullptr},
     {"need", (PyCFunction)(void (*)(void))need, METH_FASTCALL, nullptr},
     {"parameter", (PyCFunction)(void (*)(void))parameter, METH_FASTCALL, nullptr},
     {"row_stride", (PyCFunction)(void (*)(void))row_stride, METH_FASTCALL, nullptr},

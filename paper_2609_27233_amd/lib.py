@@ -174,7 +174,8 @@ def load(path: str = LIB_PATH):
         raise SpanMergeError(f"the extension module is missing ({e}); build it with "
                              "`python -m paper_2609_27233_amd.build`") from e
     fast.setup((SpanMergeError, C.ArgumentError, PagedCacheDesc, RuleTableDesc, _I, _L, _F, _Z, _P))
-    fast.dtypes(torch.int32, torch.float32)
+    fast.torch_types(torch.int32, torch.float32, torch.bfloat16, torch.Tensor, torch.nn.Parameter,
+                     getattr(torch.Tensor, "__dlpack_c_exchange_api__", None))
     fast.open(path)
     _fast = fast
     _lib = L

@@ -178,6 +178,43 @@ def test_wrong_types_and_sizes_are_refused(monkeypatch, L):
         sm.rotary(_gpu((3, 2, 8)), _gpu(6, i32)[::2], sm.rope_params(8), _gpu((3, 2, 8)))
 
 
+@pytest.mark.parametrize("exchange", [True, False], ids=["exchange", "methods"])
+def test_what_tensors_are(L, exchange):
+    """The same answers by torch's exchange interface, by its methods, and of a class of one's own."""
+    b, i32, f32, bf = sm._calls(), torch.int32, torch.float32, torch.bfloat16
+    capsule = getattr(torch.Tensor, "__dlpack_c_exchange_api__", None)
+    assert capsule is not None                                                          # (this torch has it)
+    types = (i32, f32, bf, torch.Tensor, torch.nn.Parameter)
+    b.torch_types(*types, capsule if exchange else None)
+    try:
+        buf = torch.arange(480, dtype=f32).reshape(6, 80)
+        for cls in (torch.Tensor, _Gpu):
+            dev = 0 if cls is _Gpu else -1
+
+            def t(x):
+                return x if cls is torch.Tensor else x.as_subclass(_Gpu)
+            assert b.row_stride(t(buf[:, 8:40].view(6, 4, 8)), f32, "x", 6, 4, 8) == 80
+            assert b.row_stride(t(buf[:1, :32].view(1, 4, 8).requires_grad_()), f32, "x", 1, 4, 8) == 32
+            assert b.row_stride(t(torch.zeros((0, 4, 8), dtype=bf)), bf, "x", 0, 4, 8) == 32
+            assert b.row_stride(t(torch.zeros((3, 5), dtype=torch.float16)), torch.float16, "x", 3, 5) == 5
+            for bad in (buf.t(), buf.double(), buf.int(), buf[:5], buf[:, ::2], buf.view(6, 8, 10)):
+                with pytest.raises(sm.SpanMergeError, match="x: expected"):
+                    b.row_stride(t(bad), f32, "x", 6, 80)
+            b.need(t(buf), 480, "x")
+            b.need(t(torch.zeros(())), 1, "x")
+            with pytest.raises(sm.SpanMergeError, match="x: expected 481 values, got 480"):
+                b.need(t(buf), 481, "x")
+            gain = t(buf[1])
+            assert b.parameter(gain, f32, 80, dev, "g") == gain.data_ptr() and b.parameter(None, f32, 80, dev, "g") == 0
+            for bad in ((gain, bf, 80, dev), (gain, f32, 79, dev), (gain, f32, 80, 1), (t(buf[:, 0]), f32, 6, dev)):
+                with pytest.raises(sm.SpanMergeError):
+                    b.parameter(*bad, "g")
+        param = torch.nn.Parameter(torch.zeros(7))
+        assert b.parameter(param, f32, 7, -1, "g") == param.data_ptr()
+    finally:
+        b.torch_types(*types, capsule)
+
+
 def test_a_norm_follows_its_tensors(L):
     gain = _gpu(8)
     n = sm.norm_params("rms", gain)
