@@ -88,7 +88,7 @@ bool as_long(PyObject *r, long *v) {
 struct DlVersion { uint32_t major, minor; };
 struct DlTensor {
   void *data;
-  int32_t device_type, device_id;  // device type 1: host memory
+  int32_t device_type, device_id;  // device types 2 and 10: GPU memory (host memory has others, pinned or not)
   int32_t ndim;
   uint8_t code, bits;  // of a value: code 0 integer, 2 float, 4 bfloat16
   uint16_t lanes;
@@ -106,7 +106,7 @@ PyObject *g_plain[2];                       // the classes that it is asked for:
 PyObject *g_int32, *g_float32, *g_bf16;     // torch's types
 
 struct View : DlTensor {
-  long device() const { return device_type == 1 ? -1 : device_id; }
+  long device() const { return device_type == 2 || device_type == 10 ? device_id : -1; }
   bool is(PyObject *dtype) const {
     return lanes == 1 && (dtype == g_int32 ? code == 0 && bits == 32 : dtype == g_float32 ? code == 2 && bits == 32
                                                                                            : code == 4 && bits == 16);

@@ -112,6 +112,20 @@ def test_rows_of_several_launches():
     assert torch.equal(got_k.float(), want) and torch.equal(got_v.float(), want) and c.error_bits() == 0
 
 
+def test_host_tensors_are_refused():
+    x, pos, rope = _rand((3, 2, 8), BF, 1), i32([0, 1, 2]), sm.rope_params(8)
+    out = torch.empty_like(x)
+    for pinned in (False, True):
+        host = torch.zeros((3, 2, 8), dtype=BF, pin_memory=pinned)
+        host_pos = torch.zeros(3, dtype=torch.int32, pin_memory=pinned)
+        for bad in ((host, pos, out), (x, host_pos, out), (x, pos, host)):
+            with pytest.raises(sm.SpanMergeError, match="current device"):
+                sm.rotary(bad[0], bad[1], rope, bad[2])
+        gain = torch.ones(8, dtype=BF, pin_memory=pinned)
+        with pytest.raises(sm.SpanMergeError, match="pre: expected"):
+            sm.block_norm(x[:, 0], None, None, out[:, 0], pre=sm.norm_params("rms", gain))
+
+
 def test_other_streams():
     """Each call on a stream of its own, beside work on the current one."""
     side = torch.cuda.Stream()
