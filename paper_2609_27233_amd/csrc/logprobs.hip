@@ -69,7 +69,8 @@ struct LogprobArgs {
   uint64_t *part_keys;  // [row][slice][k], 0 behind the last
 };
 
-// Ascends with x; -0 counts as 0, NaN is below everything.
+// Ascends with x; -0 counts as 0.  NaN has no place: one without the sign bit
+// would come above +infinity, so none is asked for.
 __device__ __forceinline__ uint32_t order_of(float x) {
   const uint32_t b = __float_as_uint(x + 0.f);
   return b & 0x80000000u ? ~b : b | 0x80000000u;
@@ -440,7 +441,8 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs a) {
       b = want <= kLanesWanted ? lanes_bound() : bound_of([&](uint32_t b) {
         int n = 0;
 #pragma unroll
-        for (int u = 0; u < kLpUnroll; ++u) n += __popcll(__ballot(order_of(m[u]) >= b));
+        for (int u = 0; u < kLpUnroll; ++u)  // (a vector of nothing but NaN has no largest: as -infinity)
+          n += __popcll(__ballot(order_of(fmaxf(m[u], -INFINITY)) >= b));
         return n;
       });
     }

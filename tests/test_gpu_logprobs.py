@@ -246,3 +246,33 @@ def test_captured_and_replayed():
         eager = call(x, tokens, 5, 0.5)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, eager))
+
+
+NANS = {BF: (0x7fc0, -0x40), F32: (0x7fc00000, -0x400000)}  # quiet, of both signs
+
+
+@pytest.mark.parametrize("dt", [BF, F32], ids=str)
+@pytest.mark.parametrize("rows,V", [(4, 4000), (3, 648), (4097, 9008)])
+@pytest.mark.parametrize("k", [8, 33, 64])
+def test_whole_vectors_of_nan(dt, rows, V, k):
+    """16-byte vectors of nothing but NaN, one to all of a row's first ones: every number comes before them."""
+    n = 16 // dt.itemsize
+    for several, bits in enumerate(NANS[dt]):
+        x = _rand((rows, V), dt, V + k, 0.01)
+        raw = x.view(torch.int16 if dt == BF else torch.int32)
+        peak = torch.arange(63, device=dev())
+        x[0, peak * n + 3 + n * (peak >= 5)] += 20.0                    # 63 vectors with a peak each, the sixth one of NaN
+        raw[0, 5 * n:6 * n] = bits
+        raw[1, :7 * n] = bits
+        raw[2, :(k + 2) * n] = bits                                     # more such vectors than alternatives
+        raw[2, V - 1] = bits
+        raw[rows - 1, 1::n] = bits                                      # one NaN in every vector
+        tokens = torch.zeros(rows, dtype=torch.int32, device=dev())
+        say("nan vectors", dt, rows, V, "k", k, hex(bits & 0xffffffff))
+        lp, h, ids, tlp = call(x, tokens, k)
+        some = torch.tensor([0, 1, 2, rows - 1], device=dev())
+        _, _, order = reference(x[some], 1.0)
+        assert torch.equal(ids[some].long(), order[:, :k]), (several, [int((a != b).sum()) for a, b in zip(ids[some], order[:, :k])])
+        assert lp[some].isnan().all() and h[some].isnan().all() and tlp[some].isnan().all()
+        if rows > 4:
+            assert torch.equal(ids[3].long(), reference(x[3:4], 1.0)[2][0, :k]) and not lp[3:-1].isnan().any()
