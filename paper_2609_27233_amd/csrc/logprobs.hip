@@ -497,7 +497,25 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs a) {
     };
     if (clamp) pass(true);
     else pass(false);
-    const bool infinite = !clamp && __ballot(part.E != part.E) != 0;
+    const bool odd = (TOP || !clamp) && __ballot(part.E != part.E) != 0, infinite = !clamp && odd;
+    if constexpr (TOP) {
+      // A maximum with a signaling NaN forgets what it was before: where there
+      // may be one, the vectors' largest are taken again without any NaN.
+      if (odd) {
+        all = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < kLpUnroll; ++u) {
+          u32x4_t x = cur[u];
+          asm("" : "+v"(x));  // (as above)
+          float f[N];
+          Vec16<T>::open(x, f);
+          m[u] = -INFINITY;
+#pragma unroll
+          for (int e = 0; e < N; ++e) m[u] = f[e] > m[u] ? f[e] : m[u];
+          all = fmaxf(all, m[u]);
+        }
+      }
+    }
     if (infinite || __ballot((all - s.r) * a.c > kLift)) {
       clamp |= infinite;
       move_to(s, fmaxf(s.r, wave_max(all)), a.c);

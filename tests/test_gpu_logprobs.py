@@ -276,3 +276,27 @@ def test_whole_vectors_of_nan(dt, rows, V, k):
         assert lp[some].isnan().all() and h[some].isnan().all() and tlp[some].isnan().all()
         if rows > 4:
             assert torch.equal(ids[3].long(), reference(x[3:4], 1.0)[2][0, :k]) and not lp[3:-1].isnan().any()
+
+
+SIGNALING = {BF: (0x7f81, -0x7f), F32: (0x7f800001, -0x7fffff)}
+
+
+@pytest.mark.parametrize("dt", [BF, F32], ids=str)
+@pytest.mark.parametrize("rows,V", [(9, 648), (9, 40000), (600, 20000), (4097, 9008)])
+@pytest.mark.parametrize("k", [1, 8, 64])
+def test_signaling_nan(dt, rows, V, k):
+    """A signaling NaN hides no number of its 16 bytes, wherever it stands in them."""
+    n = 16 // dt.itemsize
+    for bits in SIGNALING[dt]:
+        x = _rand((rows, V), dt, V + k)
+        raw = x.view(torch.int16 if dt == BF else torch.int32)
+        for at in range(n):
+            raw[at, at::n] = bits                                       # one in every vector
+        raw[8, -3 * n + 1] = bits
+        tokens = torch.zeros(rows, dtype=torch.int32, device=dev())
+        say("signaling", dt, rows, V, "k", k, hex(bits & 0xffffffff))
+        lp, h, ids, tlp = call(x, tokens, k)
+        some = torch.tensor([*range(n), 8], device=dev())
+        _, _, order = reference(x[some], 1.0)
+        assert torch.equal(ids[some].long(), order[:, :k])
+        assert lp[some].isnan().all() and h[some].isnan().all() and tlp[some].isnan().all()
