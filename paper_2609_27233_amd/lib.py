@@ -627,15 +627,18 @@ class Norm:
         if kind not in NORM_KINDS:
             raise SpanMergeError(f"unknown norm: {kind!r}")
         self.kind, self.eps, self.gain, self.bias = NORM_KINDS[kind], eps, gain, bias
-        self.at = None
+        self.last = (None, None)
 
     def look(self, b, dtype, d: int, dev: int, name: str) -> bytes:
-        """The structure for a call over rows of d values (the tensors may have
-        new memory since the last one: a module that was moved)."""
-        at = (b.parameter(self.gain, dtype, d, dev, name), b.parameter(self.bias, dtype, d, dev, name))
-        if at != self.at:
-            self.packed, self.at = bytes(NormParams(self.kind, self.eps, *at)), at
-        return self.packed
+        """The structure for a call over rows of d values (its fields may have
+        other values since the last one, its tensors new memory: a module that
+        was moved)."""
+        fields = (self.kind, self.eps, b.parameter(self.gain, dtype, d, dev, name), b.parameter(self.bias, dtype, d, dev, name))
+        last, packed = self.last
+        if fields != last:
+            packed = bytes(NormParams(*fields))
+            self.last = (fields, packed)
+        return packed
 
 
 def norm_params(kind: str = "rms", gain=None, bias=None, eps: float = 1e-5) -> Norm:

@@ -266,3 +266,14 @@ def test_caches_that_share_tables():
             sm.PagedCache(**kw, tables=a, free_order=range(8))
     finally:
         sm._ptr = sm_ptr
+
+
+def test_a_norm_follows_its_kind_and_epsilon(L):
+    def look(n):
+        return sm.NormParams.from_buffer_copy(n.look(sm._calls(), torch.float32, 8, 0, "pre"))
+    for n in (sm.norm_params("rms"), sm.norm_params("rms", _gpu(8), _gpu(8))):
+        first = look(n)
+        n.eps = 0.25
+        assert look(n).eps == 0.25 and look(n).kind == first.kind == 0 and look(n).gain == first.gain
+        n.kind = sm.NORM_KINDS["layer"]
+        assert look(n).kind == 1 and look(n).eps == 0.25 and look(n).bias == first.bias
