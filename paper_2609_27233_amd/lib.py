@@ -551,6 +551,14 @@ def _shape(t, dims: int, name: str):
     return s
 
 
+def _columns(t, rows: int, name: str) -> int:
+    """k of a [rows, k] tensor ([rows]: 1), which may have more rows."""
+    s = t.shape
+    if len(s) not in (1, 2) or s[0] < rows:
+        raise SpanMergeError(f"{name}: expected {rows} rows of alternatives, got {tuple(s)}")
+    return s[1] if len(s) == 2 else 1
+
+
 def _rows(t):
     """Rows with a stride, which row_stride has looked at, for a call."""
     return None if t is None else (t,)
@@ -677,7 +685,8 @@ def token_logprobs_workspace_bytes(rows: int, vocab: int, k: int) -> int:
 def token_logprobs(logits, tokens, logprob, entropy, top_ids, top_logprobs, ws, scale: float = 1.0, err=None, stream=None):
     """Log probability of tokens[r], entropy and the k = top_ids.shape[1]
     largest logits of each row of logits [rows, vocab] (contiguous rows);
-    scale = 1 / temperature.  Each output may be None."""
+    scale = 1 / temperature.  top_ids and top_logprobs are [rows, k] (or [rows]:
+    one alternative).  Each output may be None."""
     b = _calls()
     (rows, vocab), dt, need = _shape(logits, 2, "logits"), logits.dtype, b.need
     sl = b.row_stride(logits, dt, "logits", rows, vocab)
@@ -689,10 +698,9 @@ def token_logprobs(logits, tokens, logprob, entropy, top_ids, top_logprobs, ws, 
     if entropy is not None:
         need(entropy, rows, "entropy")
     if top_ids is not None:
-        k = top_ids.shape[-1] if top_ids.dim() > 1 else 1
-        need(top_ids, rows * k, "top_ids")
-        if top_logprobs is not None:
-            need(top_logprobs, rows * k, "top_logprobs")
+        k = _columns(top_ids, rows, "top_ids")
+        if top_logprobs is not None and _columns(top_logprobs, rows, "top_logprobs") != k:
+            raise SpanMergeError(f"top_logprobs: expected {k} columns, as top_ids has, got {tuple(top_logprobs.shape)}")
     elif top_logprobs is not None and top_logprobs.numel():
         raise SpanMergeError("top_logprobs without top_ids")
     if err is not None:

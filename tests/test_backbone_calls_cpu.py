@@ -277,3 +277,19 @@ def test_a_norm_follows_its_kind_and_epsilon(L):
         assert look(n).eps == 0.25 and look(n).kind == first.kind == 0 and look(n).gain == first.gain
         n.kind = sm.NORM_KINDS["layer"]
         assert look(n).kind == 1 and look(n).eps == 0.25 and look(n).bias == first.bias
+
+
+def test_alternatives_of_other_shapes_are_refused(monkeypatch, L):
+    monkeypatch.setattr(sm, "_here", lambda stream: (0, 0))
+    i32, x, ws = torch.int32, _gpu((4, 100), torch.bfloat16), _gpu(65536, torch.uint8)
+    for ids, tlp, name in (((4, 8), (4, 20), "top_logprobs"), ((4, 8), (2, 16), "top_logprobs"), ((4, 8), (32,), "top_logprobs"),
+                           ((4,), (4, 2), "top_logprobs"), ((4, 8), (3, 8), "top_logprobs"), ((4, 8), (4, 1, 8), "top_logprobs"),
+                           ((4, 2, 4), (4, 2, 4), "top_ids"), ((2, 2, 8), (4, 8), "top_ids"), ((3, 8), (4, 8), "top_ids"),
+                           ((), (4,), "top_ids"), ((3,), (4,), "top_ids")):
+        with pytest.raises(sm.SpanMergeError, match=name):
+            sm.token_logprobs(x, None, None, None, _gpu(ids, i32), _gpu(tlp), ws)
+    # as they may be: [rows, k], or [rows] for one alternative, with more rows behind (the argument checks then refuse
+    # the call, whose workspace is too small, before anything is enqueued)
+    for ids, tlp in (((4, 8), (4, 8)), ((6, 8), (5, 8)), ((4,), (4,)), ((4,), (4, 1)), ((4, 1), (4,)), ((4, 0), (4, 0))):
+        with pytest.raises(sm.SpanMergeError, match="sm_token_logprobs"):
+            sm.token_logprobs(x, None, None, None, _gpu(ids, i32), _gpu(tlp), ws[:65535])
