@@ -11,8 +11,9 @@
 // status.  The checked entries take rows with a stride as a tensor in a tuple
 // of its own, which row_stride has looked at.  Values are taken and
 // refused as ctypes does for the same prototypes: integers wrap to the C
-// type's width, a ctypes number of the argument's own type counts as its
-// value, and what does not fit raises ctypes.ArgumentError.
+// type's width (the checked entries refuse what an int does not hold: 2^32
+// rows would count as none), a ctypes number of the argument's own type counts
+// as its value, and what does not fit raises ctypes.ArgumentError.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <dlfcn.h>
@@ -252,6 +253,17 @@ bool get_checked(PyObject *o, A *v, long device) {
       *v = (A)p;
       return true;
     }
+  } else if constexpr (std::is_same_v<A, int>) {
+    PyObject *x = plain_value(o, kInt);
+    if (!x) return false;
+    const long value = PyLong_Check(x) ? PyLong_AsLong(x) : 0;
+    const bool over = (value == -1 && PyErr_Occurred()) || value != (int)value;
+    if (over) {
+      PyErr_Clear();
+      PyErr_Format(g_type[kError], "an argument is out of range: no int holds %S", x);
+    }
+    Py_DECREF(x);
+    return !over && get(o, v);
   } else {
     return get(o, v);
   }

@@ -293,3 +293,24 @@ def test_alternatives_of_other_shapes_are_refused(monkeypatch, L):
     for ids, tlp in (((4, 8), (4, 8)), ((6, 8), (5, 8)), ((4,), (4,)), ((4,), (4, 1)), ((4, 1), (4,)), ((4, 0), (4, 0))):
         with pytest.raises(sm.SpanMergeError, match="sm_token_logprobs"):
             sm.token_logprobs(x, None, None, None, _gpu(ids, i32), _gpu(tlp), ws[:65535])
+
+
+def test_sizes_that_no_int_holds_are_refused(L):
+    """2^32 rows more than none would count as none."""
+    b, rope = sm._calls(), sm.rope_params(8)
+    x, pos, many = torch.zeros((1, 2, 8)), torch.zeros(2, dtype=torch.int32), 1 << 32
+    rows = (x,)
+    args = {"sm_rotary": [rows, 16, pos, 0, 2, 8, rope, 0, 0, rows, 16, 0, -1],
+            "sm_block_norm": [rows, 16, None, 0, 0, 16, None, None, 0, 1.0, bytes(sm.NormParams(0, 1e-5)), 0, rows, 16,
+                              None, 0, 0, -1],
+            "sm_token_logprobs": [rows, 16, 0, 16, 0, 1.0, None, None, None, 0, None, None, pos, 8, None, 0, -1]}
+    sizes = {"sm_rotary": (3, 4, 5), "sm_block_norm": (4, 5), "sm_token_logprobs": (2, 3, 9)}
+    for name, good in args.items():
+        entry = getattr(b, name)
+        assert entry(*good) == sm.SM_OK, name                                   # no row: nothing to do
+        for at in sizes[name]:
+            for off in (many, -many, 1 << 31, many << 32):
+                bad = list(good)
+                bad[at] += off
+                with pytest.raises(sm.SpanMergeError, match="argument"):
+                    entry(*bad)
