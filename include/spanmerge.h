@@ -845,10 +845,12 @@ typedef struct {
  *               be h, y or a gate of a row each (same address and stride),
  *               but overlaps no other input and not the other output
  * Any element-aligned address; 16-byte aligned rows with d a multiple of 8
- * (fp32: 4) are read as they are, others in unaligned pieces.  Squares are
- * summed in fp32: a row whose squares come to more than 3.4e38 is normed to
- * 0; with eps 0 one whose mean square is below 1e-38 has few right bits, and a
- * row of zeros NaN.  No device errors.
+ * (fp32: 4) are read as they are, others in unaligned pieces.  Sums are
+ * fp32: a row whose squares (LAYER: of the differences from the mean) come to
+ * more than 3.4e38 is normed to 0, plus the bias, and with LAYER to NaN where
+ * the sum of the features or a difference does too; with eps 0 a row whose
+ * mean square is below 1e-38 has few right bits, and a row of zeros is NaN.
+ * No device errors.
  */
 sm_status sm_block_norm(const void *h, int64_t h_stride, const void *y,
                         int64_t y_stride, int rows, int d, const sm_norm *post,

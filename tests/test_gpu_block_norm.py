@@ -185,3 +185,24 @@ def test_many_rows():
     n, _ = _make("rms", d, F32, 1, gain=False)
     sm.block_norm(h, None, None, out, pre=n)
     assert float((out - 1).abs().max()) <= 1e-5                         # every row is its own mean square
+
+
+@pytest.mark.parametrize("dt", [BF, F32], ids=str)
+@pytest.mark.parametrize("d", [512, 16384])
+def test_sums_past_the_largest_number(dt, d):
+    """Rows whose squares come to more than 3.4e38 are normed to 0, plus a bias; a LayerNorm is NaN where the features'
+    plain sum (or a difference from their mean) does too."""
+    sign = torch.randint(0, 2, (d,), generator=torch.Generator().manual_seed(1)) * 2.0 - 1
+    sign[1::2] = -sign[::2]                                              # (their sum is 0)
+    h = torch.stack([sign * 1e35, torch.full((d,), 3e38), torch.full((d,), 1e30)]).to(dt).to(dev())
+    bias = _rand((d,), dt, 3)
+    for b in (None, bias):
+        want = torch.zeros_like(h[0]) if b is None else bias
+        rms, layer = torch.full_like(h, 7.0), torch.full_like(h, 7.0)
+        sm.block_norm(h, None, None, rms, pre=sm.norm_params("rms", None, b))
+        sm.block_norm(h, None, None, layer, pre=sm.norm_params("layer", None, b))
+        torch.cuda.synchronize()
+        assert all(torch.equal(r, want) for r in rms)
+        assert torch.equal(layer[0], want)
+        assert layer[1].isnan().all()                                    # (512 x 3e38 is past the largest number)
+        assert torch.equal(layer[2], want)                               # equal features: no difference, as the formula has it
