@@ -669,7 +669,8 @@ SM_API sm_status sm_token_logprobs(const void *logits, int64_t stride, int rows,
                                    float *top_logprobs, void *ws, size_t ws_bytes, int32_t *err, hipStream_t stream) {
   if ((dt != SM_F32 && dt != SM_BF16) || rows < 0 || vocab < 1 || k < 0 || k > SM_MAX_TOP || k > vocab) return SM_EINVAL;
   const float c = (float)(scale * 1.4426950408889634);
-  // (p |d| is at most 16 / scale: 2^31 of them stay finite)
+  // (a chunk's terms p |d| are at most 2^kLift kLift ln 2 / scale = 44 / scale, for d below the reference at most
+  // 1 / (e scale): from a scale of 1e-20 on 2^31 of them come to at most 1e31)
   if (!(scale >= 1e-20f) || !std::isfinite(c) || stride < vocab) return SM_EINVAL;
   if (rows == 0) return SM_OK;
   if (!logits || (logprob && !tokens) || (k > 0 && !top_ids) || (uintptr_t)ws % 16 != 0) return SM_EINVAL;
