@@ -739,7 +739,9 @@ sm_status sm_kv_reserve(const sm_paged_cache *c, const int32_t *seq_ids,
  *           times, J(t) = rot_dim ln(context / (2 pi t)) / (2 ln theta):
  *           j0 = max(floor J(high), 0), j1 = min(ceil J(low), rot_dim - 1)
  * Features from rot_dim on are copied.  Angles are formed and reduced in
- * double precision; positions may be any int32.
+ * double precision of the numbers below, which are floats: a factor that no
+ * float holds is off by 2^-25 of itself and so are the angles, 0.03 rad of the
+ * fastest pair's at position 10^6.  Positions may be any int32.
  */
 typedef enum { SM_ROPE_HALF = 0, SM_ROPE_INTERLEAVED = 1 } sm_rope_layout;
 typedef enum {

@@ -149,8 +149,9 @@ __device__ __forceinline__ void norm_row(Chunk<T, WHOLE> (&x)[NV], int kind, flo
   for (int v = 0; v < NV; ++v)
 #pragma unroll
     for (int e = 0; e < VEC; ++e) q += x[v].f[e] * x[v].f[e];
-  // (the hardware's root, off by one unit, is for normal numbers: an epsilon of
-  // 0 may leave less)
+  // (the hardware's root is off by a unit, the product with 1 / d rounded to fp32
+  // by one more: the sum passes up to 40 roundings.  The root is for normal
+  // numbers: an epsilon of 0 may leave less)
   const float m = row_sum<TPR>(q, red) * inv_d + eps, inv = m < 1.2e-38f ? 1.f / sqrtf(m) : __builtin_amdgcn_rsqf(m);
 #pragma unroll
   for (int v = 0; v < NV; ++v) {

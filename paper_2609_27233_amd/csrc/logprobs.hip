@@ -57,7 +57,7 @@ struct LogprobArgs {
   const void *logits;
   int64_t stride;
   int rows, vocab, k;
-  float scale, c;  // c: scale x log2 e
+  float scale, c;  // c: scale x log2 e, in fp32: an exponent is off by a unit of itself, as its product with d is
   const int32_t *tokens;
   float *logprob, *entropy;
   int32_t *top_ids;

@@ -51,7 +51,9 @@ struct RopeArgs {
 };
 
 // Cosine and sine of the tile's rows, [row][pair]: the angle in turns is
-// reduced to [-1/2, 1/2] in double precision.
+// reduced to [-1/2, 1/2] in double precision and only then rounded to fp32, off
+// by 1e-7 rad at most, as much as cosine and sine themselves are (a sine in
+// double takes several times the instructions).
 __device__ __forceinline__ void fill_angles(const RopeArgs &a, int r0, int nr, float2 *cs) {
   const int P = a.R / 2;
   for (int u = threadIdx.x; u < nr * P; u += kRotThreads) {
