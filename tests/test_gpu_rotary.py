@@ -318,3 +318,64 @@ def test_write_equals_append():
     assert a.error_bits() == 0 and b.error_bits() == 0
     for name in ("k_pool", "v_pool", "block_table", "lengths", "free_top"):
         assert torch.equal(getattr(a, name), getattr(b, name)), name
+
+
+# Input of 64 to 256 MB is read past the last-level cache, by kernels of its own.
+PAST = 64 << 20
+LARGE = [
+    # dtype, heads, D, R, layout
+    (BF, 16, 128, 128, "half"), (BF, 24, 64, 32, "interleaved"), (F32, 8, 128, 64, "half"), (F32, 5, 96, 20, "interleaved"),
+]
+
+
+@pytest.mark.parametrize("case", range(len(LARGE)))
+def test_rotary_of_large_input(case):
+    dt, H, D, R, layout = LARGE[case]
+    rows = -(-PAST // (H * D * dt.itemsize)) + 9
+    a = dict(rot_dim=R, layout=layout, attn_scale=0.75)
+    x = _rand((rows, H, D), dt, case)
+    pos = torch.randint(0, 100000, (rows,), generator=torch.Generator().manual_seed(case)).int()
+    ref, slack = turned(x, pos, a, case % 2 == 1)
+    out = torch.full_like(x, float("nan"))
+    say("large rotary", dt, (rows, H, D, R), layout)
+    sm.rotary(x, pos.to(dev()), sm.rope_params(**a), out, transpose=case % 2 == 1)
+    assert_near(out, ref, slack, dt)
+    sm.rotary(x, pos.to(dev()), sm.rope_params(**a), x, transpose=case % 2 == 1)
+    assert torch.equal(x, out)
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("dt", [BF, F32], ids=str)
+def test_write_of_large_input(dt, layout):
+    Hq, Hkv, D, bs = (8, 4, 128, 16) if dt == BF else (5, 3, 64, 32)
+    rows = -(-PAST // ((Hq + 2 * Hkv) * D * dt.itemsize)) + 9
+    rng = np.random.RandomState(len(layout))
+    lens = [rows // 2 - 1, 1, 700, rows - rows // 2 - 700]
+    nb = sum(-(-x // bs) + 1 for x in lens)
+    c = _cache(dt, Hkv, D, bs, nb)
+    slots = _runs(rng, nb, bs, lens)
+    slots[rng.choice(rows, 100, replace=False)] = -1
+    pos = torch.from_numpy(rng.randint(0, 40000, rows).astype(np.int32))
+    a = dict(rot_dim=64, layout=layout) if dt == F32 else dict(rot_dim=128, layout=layout)
+    buf = _rand((rows, (Hq + 2 * Hkv) * D), dt, 7)
+    q, k, v = (t.unflatten(1, (-1, D)) for t in buf.split([Hq * D, Hkv * D, Hkv * D], 1))
+    k0, v0 = c.k_pool.double().cpu(), c.v_pool.double().cpu()
+    q_out = torch.full((rows, Hq, D), float("nan"), dtype=dt, device=dev())
+    say("large write", dt, layout, "rows", rows)
+    sm.kv_write_rotary(c, pos.to(dev()), i32(slots), q, k, v, sm.rope_params(**a), q_out)
+    torch.cuda.synchronize()
+    assert c.error_bits() == 0
+    assert_near(q_out, *turned(q, pos, a), dt)
+    ref, slack = turned(k, pos, a)
+    there = torch.from_numpy(slots >= 0)
+    s = torch.from_numpy(slots[slots >= 0].astype(np.int64))
+    # unwritten slots hold values of the type: exact
+    sk = torch.zeros_like(k0)
+    k0[s // bs, :, s % bs], sk[s // bs, :, s % bs] = ref[there], slack[there]
+    v0[s // bs, :, :, s % bs] = v.double().cpu()[there]
+    untouched = torch.ones(nb * bs, dtype=torch.bool)
+    untouched[s] = False
+    untouched = untouched.view(nb, 1, bs, 1).expand_as(k0)
+    assert torch.equal(c.k_pool.double().cpu()[untouched], k0[untouched])
+    assert torch.equal(c.v_pool.double().cpu(), v0)
+    assert_near(c.k_pool, k0, sk, dt)
