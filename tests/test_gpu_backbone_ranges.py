@@ -8,6 +8,7 @@ import torch
 
 from gpu_util import dev, i32, say
 from paper_2609_27233_amd import lib as sm
+from test_gpu_rotary import assert_near, turned
 
 pytestmark = pytest.mark.gpu
 
@@ -211,3 +212,30 @@ def test_captured_decode_step():
         assert a.c.error_bits() == 0 and b.c.error_bits() == 0
         for x, y in zip(a.state(), b.state()):
             assert torch.equal(x, y)
+
+
+def test_rows_past_32_bits_match_the_formula():
+    """Rows on both sides of 2^31 elements and the last ones, against the formula in 64 bits; the others are zeros."""
+    rows, d = 600_000, 4096                                              # 2.5 x 10^9 elements
+    first = (1 << 31) // d
+    some = torch.cat([torch.arange(3), torch.arange(first - 3, first + 4), torch.arange(rows - 5, rows)]).to(dev())
+    h = torch.zeros((rows, d), dtype=BF, device=dev())
+    h[some] = _rand((some.numel(), d), BF, 11)
+    out = torch.full_like(h, 7.0)
+    say("far rows", h.numel())
+    sm.block_norm(h, None, None, out, pre=sm.norm_params("rms", None))
+    x = h[some].double()
+    want = x / (x.square().mean(1, keepdim=True) + float(np.float32(1e-5))).sqrt()
+    got = out[some].double()
+    # 40 additions of the mean square, halved by the root, with that, the mean and the product: 26 x 2^-24; then half a step
+    assert ((got - want).abs() <= want.abs() * (26 * 2.0 ** -24 + 2.0 ** -8)).all()
+    out[some] = 0
+    assert not out.any()
+    pos = torch.zeros(rows, dtype=torch.int32, device=dev())
+    pos[some] = torch.arange(some.numel(), dtype=torch.int32, device=dev()) * 1013
+    x = h.view(rows, 32, 128)
+    want, slack = turned(x[some], pos[some], dict(rot_dim=128))
+    sm.rotary(x, pos, sm.rope_params(128), out.view(rows, 32, 128))
+    assert_near(out[some].view(-1, 32, 128), want, slack, BF)
+    out[some] = 0
+    assert not out.any()
