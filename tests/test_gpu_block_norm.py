@@ -1,4 +1,6 @@
 """The residual sum with the norms around it against the formula in 64 bits."""
+import sys
+
 import pytest
 import torch
 
@@ -206,3 +208,22 @@ def test_sums_past_the_largest_number(dt, d):
         assert torch.equal(layer[0], want)
         assert layer[1].isnan().all()                                    # (512 x 3e38 is past the largest number)
         assert torch.equal(layer[2], want)                               # equal features: no difference, as the formula has it
+
+
+@pytest.mark.parametrize("dt", [BF, F32], ids=str)
+@pytest.mark.parametrize("d", [64, 1111, 4096, 5120, 16384])
+def test_sums_to_their_counted_roundings(monkeypatch, dt, d):
+    """The same reference with the additions that a feature passes: 16 features of a thread, 6 steps over a wave, 16 waves,
+    and its square or the mean's product."""
+    monkeypatch.setattr(sys.modules[__name__], "SUM", (16 + 6 + 16 + 2) * U)
+    for k, (post, gate, pre) in enumerate(FORMS):
+        h, y = _rand((9, d), dt, 3 * d + k, 2.0, 0.5), _rand((9, d), dt, d + k + 5, 1.0, -0.3)
+        g = None if gate is None else _rand((d,) if gate == "channel" else (9, d), dt, k, 0.5)
+        p, p_ref = _make(post, d, dt, 70 + k)
+        q, q_ref = _make(pre, d, dt, 80 + k)
+        ho, no = (torch.full_like(h, float("nan")) for _ in range(2))
+        say("counted", dt, "d", d, post, gate, pre)
+        sm.block_norm(h, y, ho, no, post=p, gate=g, scale=0.75, pre=q)
+        r = reference(h, y, p_ref, g, 0.75, q_ref)
+        assert_near(ho, r[0], dt)
+        assert_near(no, r[1], dt)

@@ -300,3 +300,40 @@ def test_signaling_nan(dt, rows, V, k):
         _, _, order = reference(x[some], 1.0)
         assert torch.equal(ids[some].long(), order[:, :k])
         assert lp[some].isnan().all() and h[some].isnan().all() and tlp[some].isnan().all()
+
+
+@pytest.mark.parametrize("dt", [BF, F32], ids=str)
+@pytest.mark.parametrize("rows,V", [(3, 262144), (600, 262144), (4096, 65536)])
+def test_sums_to_their_counted_roundings(dt, rows, V):
+    """Log probabilities and entropy of long rows, by the additions that a term of the sums passes."""
+    n = 16 // dt.itemsize
+    x = _rand((rows, V), dt, V, 2.5)
+    x[1] = -0.5                                                         # sums of equal terms that are no power of two
+    x[1, 0] = 0.0
+    tokens = torch.arange(rows, dtype=torch.int32, device=dev()) * 7 % V
+    say("counted", dt, rows, V)
+    got = call(x, tokens, 4)
+    some = torch.tensor([0, 1, 2, rows - 1], device=dev())
+    z = x[some].double()
+    d = (z - z.amax(1, keepdim=True)).abs()
+    logp, H, order = reference(x[some], 1.0)
+    p = logp.exp()
+    # M and Q: the mean of |z - r| and its square under p; the reference r is within 3 of the maximum
+    M, Q = (p * d).sum(1) + 3, (p * (d + 3).square()).sum(1)
+    # A term passes a chunk's 4 vectors, at most V / (256 n) chunks and four joins of 6 steps.  The references that were
+    # left (a factor each, with an exponential of their difference) lie in a range of 15, at least 2.7 apart: 3 of each and
+    # 3 for every unit of the range, 60.  Its own exponent (difference, scale, product) is off by 3 |z - r|, the exponential by 2.
+    depth = 4 * n + V / (256 * n) + 24 + 60
+    err_s = (depth + 3 * M + 2) * U
+    # the logarithm is off by a unit of itself and of the factor behind it, the difference, product and sum by one each
+    def tol_lp(v):
+        return err_s[:, None] + 6 * U * (v.abs() + math.log(V) + 3)
+    lp, h, ids, tlp = (t[some] for t in got)
+    assert torch.equal(ids.long(), order[:, :4])
+    ref = logp.gather(1, tokens[some].long()[:, None])
+    assert ((lp[:, None].double() - ref).abs() <= tol_lp(ref)).all()
+    top = logp.gather(1, order[:, :4])
+    assert ((tlp.double() - top).abs() <= tol_lp(top)).all()
+    # E / S: the terms |p d| come to M, each off by what a term of S is and d's and the product's rounding
+    tol = (M * (depth + 4) + 3 * Q) * U + (M + 1) * err_s + 6 * U * (math.log(V) + M)
+    assert ((h.double() - H).abs() <= tol).all(), ((h.double() - H).abs() / tol).tolist()
