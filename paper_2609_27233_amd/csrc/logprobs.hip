@@ -628,21 +628,29 @@ struct LogprobPlan {
 constexpr int kLpFill = 512;
 // Rows of up to kLpShort vectors are one wave's, longer ones where there are
 // many rows: a wave alone has less to do once a row, and waits at no barrier.
-// Four waves and one, us: 8192 x 16,000 bf16 logits 76 and 54, 8192 x 50,257
-// 166 and 146, 4096 x 128,256 214 and 214; 1536 x 128,256 77 and 83.
+// Four waves and one, us, bf16 logits, 20 alternatives:
+//   9000 (1125 vectors) 1300 rows 15.9, 14.2; 5000 rows 44.1, 27.9
+//   16,000 (2000)       1300 17.9, 18.6; 1536 19.7, 18.8; 5000 50.4, 42.0
+//   32,000 (4000)       1536 25.9, 30.6; 1700 28.7, 31.1; 1850 32.8, 31.3; 5000 77.7, 72.0
+//   50,257 (6282)       1536 36.8, 42.3; 1700 41.1, 42.4; 1850 44.6, 42.5; 8192 169, 156
+//   128,256 (16,032)    2000 91, 95; 4096 179, 178 (two full rounds of 2048 waves; 201, 195 with likely
+//                       tokens); 4150 204, 213; 6000 258, 278; 8192 346, 363
+// (without alternatives one wave gains less, and loses up to 15% for 2000 to
+// 8192 vectors.)  Four waves take 1024 vectors at a time: 66,000 logits, 8250
+// vectors, would be one wave's by 9%, 65,000 and 70,000 are not.
 constexpr int kLpShort = 1024;
-constexpr int kLpMany = 1536, kLpManyVectors = 8192;  // this many rows of up to so many vectors,
-constexpr int kLpAll = 4096;                          // or this many of any length
+constexpr int kLpMiddle = 2048, kLpManyMiddle = 1536;  // up to so many vectors: from this many rows on
+constexpr int kLpLong = 8192, kLpManyLong = 1792;
 
 static bool one_wave_rows(int rows, int nvec) {
-  return nvec <= kLpShort || (rows >= kLpMany && nvec <= kLpManyVectors) || rows >= kLpAll;
+  return nvec <= kLpShort || (nvec <= kLpMiddle && rows >= kLpManyMiddle) || (nvec <= kLpLong && rows >= kLpManyLong);
 }
 
 // (no row is cut beyond kLpFill rows, so its counter is within the first 64 KiB)
 static_assert(kLpFill * kCounterStep * sizeof(int) <= 65536, "counters");
 
-// Rows of a launch: its threads are counted in 32 bits, 64 a row where there are many.
-constexpr int64_t kLpLaunchRows = 1 << 24;
+// Rows of a launch: its threads are counted in 32 bits, 256 a row at most.
+constexpr int64_t kLpLaunchRows = 1 << 23;
 
 static LogprobPlan plan_logprobs(int rows, int vocab, int k) {
   const int nvec = vocab / 4 + 1;  // (of fp32; bf16 rows have half as many)
