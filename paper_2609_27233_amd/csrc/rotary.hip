@@ -101,11 +101,16 @@ template <> struct Piece<uint16_t, 8> {
 };
 
 // Input that would fill the 256 MB of last-level cache with what is made of it
-// is read past it (STREAM), as nothing reads it again: beside what writes the
-// rows and what reads the result, 6000 rows of 12 KB take 25 us so and 31 with
-// plain loads, 20,000 rows 102 and 108; 4000 rows, which the cache holds
-// anyway, 20.4 and 18.4.  What the cache could not hold by itself is read
-// plainly: 268 MB of fp32 rows 117 us past it, 111 so.
+// is read past it (STREAM), as nothing reads it again.  Past it and plainly,
+// beside what writes the rows and what reads the result, us:
+//   about MiB         48          56          64          72          128         240
+//   rotary, bf16, 32  17.4, 15.9  19.7, 20.9  21.2, 25.7  23.1, 26.4  41.9, 55.0  93, 104
+//   write, bf16, 32+8 18.5, 20.1  25.0, 24.6  27.5, 28.3  25.1, 30.0  55.2, 64.0  105, 111
+//   write, bf16, 28+4 21.9, 18.2  27.5, 23.8  27.3, 27.6  28.2, 33.4  52.5, 62.4  99, 108
+//   write, fp32, 4+4  22.7, 20.7  25.7, 20.6  29.4, 26.0  31.6, 28.4  56.5, 59.7  96, 96
+// (heads of 128, the last of 64: such rows, 3 KB, gain nothing below 80 MiB;
+// fp32 writes of heads of 128 gain 8% and more from 56 on).  What the cache could not
+// hold by itself is read plainly: 268 MB of fp32 rows 117 us past it, 111 so.
 constexpr int64_t kStreamFrom = 64 << 20, kStreamTo = 256 << 20;
 
 template <bool STREAM, typename R>
