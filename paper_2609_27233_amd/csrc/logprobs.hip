@@ -309,7 +309,8 @@ __device__ __forceinline__ void put_row(const LogprobArgs &a, int64_t r, Sums s,
   const float log_s = __builtin_amdgcn_logf(s.S) * kLn2;
   auto logprob = [&](float f) {
     if (s.S == 0.f) return -INFINITY;  // nothing but -infinity
-    const float lp = fmaf(f - s.r, a.scale, -log_s);
+    // (logits further apart than the largest number are scaled first)
+    const float d = f - s.r, lp = d >= kLowest ? fmaf(d, a.scale, -log_s) : fmaf(f, a.scale, -a.scale * s.r) - log_s;
     return lp > 0.f ? 0.f : lp;
   };
   if (lane == 0) {

@@ -337,3 +337,30 @@ def test_sums_to_their_counted_roundings(dt, rows, V):
     # E / S: the terms |p d| come to M, each off by what a term of S is and d's and the product's rounding
     tol = (M * (depth + 4) + 3 * Q) * U + (M + 1) * err_s + 6 * U * (math.log(V) + M)
     assert ((h.double() - H).abs() <= tol).all(), ((h.double() - H).abs() / tol).tolist()
+
+
+@pytest.mark.parametrize("dt", [BF, F32], ids=str)
+@pytest.mark.parametrize("rows,V", [(3, 900), (3, 40000), (2000, 9000)])
+@pytest.mark.parametrize("scale", [1e-20, 1e-3, 0.4])
+def test_differences_past_the_largest_number(dt, rows, V, scale):
+    """Logits more than 3.4e38 apart: the scale brings their log probabilities back."""
+    x = torch.linspace(-3.3e38, 3.3e38, V, dtype=torch.float64, device=dev()).to(dt).expand(rows, V).contiguous()
+    x[1] = x[1].flip(0)
+    x[2, 5] = -math.inf
+    tokens = torch.arange(rows, dtype=torch.int32, device=dev()) % V
+    tokens[2] = 5
+    say("far apart", dt, rows, V, scale)
+    lp, h, ids, tlp = call(x, tokens, 8, scale)
+    some = torch.tensor([0, 1, 2, rows - 1], device=dev())
+    logp, H, order = reference(x[some], scale)
+    assert torch.equal(ids[some].long(), order[:, :8])
+    ref = logp.gather(1, tokens[some].long()[:, None])[:, 0]
+    top = logp.gather(1, order[:, :8])
+    assert lp[2] == -math.inf and torch.equal(ref.isfinite(), some != 2)
+    # a product with the scale and its rounding or a difference and its product, a sum: 4 units, of terms up to twice the
+    # value (one of 6.6e38 x scale of two of 3.3e38 x scale); beside them the logarithm counts for the near ones
+    for got, want in ((lp[some], ref), (tlp[some], top)):
+        fin = want.isfinite()
+        assert got.isfinite().eq(fin).all()
+        assert ((got.double() - want).abs() <= 8 * U * (want.abs() + 20))[fin].all()
+    assert ((h[some].double() - H).abs() <= 1e-4).all()
