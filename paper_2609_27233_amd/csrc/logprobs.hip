@@ -23,12 +23,13 @@
 // its slices are several ones', joined by the last to arrive at the row's
 // counter.
 //
-// Many rows are bound by the read: 4096 rows of 128,256 bf16 logits (1.05 GB)
-// take 169 us without alternatives, 6.2 TB/s, 176 with one, and 174 to 205 with
-// 20, where the vector instructions of a compute unit are busy nine tenths of
-// the time; fp32 rows of the same size 167 us with 20.  Few rows are bound by
-// latency: 16 rows 5.3 us without alternatives and 9.4 with 8 (bound, look,
-// sort, then the same of the slices' keys).
+// Many rows are bound by the read and, in bf16, by the vector instructions,
+// which a compute unit issues all the time: 4096 rows of 128,256 bf16 logits
+// (1.05 GB) take 167 us without alternatives, 6.3 TB/s, and 169 with one or with
+// 20 (one call after another, as the clock falls, 177, 188 and 201); fp32 rows
+// of the same size 169 us with 20.  Few rows are bound by latency: 16 rows 5.3 us
+// without alternatives and 9.4 with 8 (bound, look, sort, then the same of the
+// slices' keys), 300 rows 17.9 and 22.9 of the 11.4 that their read takes.
 #include <algorithm>
 #include <cmath>
 
