@@ -624,9 +624,10 @@ struct LogprobPlan {
 };
 
 // Slices of a row: about kLpFill workgroups in all.  128,256 bf16 logits and
-// 20 alternatives, us, with about 256, 512 and 1024 workgroups: 64 rows 16.4,
-// 15.4, 17.8; 130 rows 21.3, 19.8, 20.3; 200 rows 26.1, 23.1, 23.8; 500 rows
-// (one slice, one, two) 33.2, 32.5, 33.5.
+// 20 alternatives, us, with about 256, 512 and 1024 workgroups: 64 rows 14.6,
+// 13.5, 15.4; 130 rows 19.4, 17.5, 19.0; 200 rows 23.0, 20.5, 21.1; 300 rows
+// 27.6, 24.6, 24.4 (of 32,000 logits 12.7, 14.0, 13.9); 500 rows (one slice,
+// one, two) 28.5, 28.4, 31.7.
 constexpr int kLpFill = 512;
 // Rows of up to kLpShort vectors are one wave's, longer ones where there are
 // many rows: a wave alone has less to do once a row, and waits at no barrier.
