@@ -1,0 +1,644 @@
+"""The operators of a paged cache in 8 bits, of attention behind a shared prompt, and of choosing a token, as cases that
+can be timed and compared.
+
+  write    a packed projection's rows: q and K turned, K and V quantised into e4m3 pages by slot
+  read     cached entries of e4m3 pages read back as bf16 rows
+  decode   one query a sequence over its e4m3 pages
+  prefill  causal attention of a prompt's rows over e4m3 pages
+  shared   one query a sequence over the entries that its group shares, then its own (bf16 or e4m3 pages)
+  sample   tokens from rows of logits under temperature, top-k, min-p and top-p, by one given random number a row
+
+An e4m3 page holds, for each entry and kv head, D values of e4m3 and one exponent byte b: feature i is value[i] 2^(b - 127).
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+BF16, E4M3 = torch.bfloat16, torch.float8_e4m3fn
+DTYPES = {"bf16": BF16, "f32": torch.float32, "e4m3": E4M3}
+THETA = 500000.0
+
+
+# --------------------------------------------------------------------------
+# the cases
+
+def listed():
+    return [
+        # one decode step of the benchmark batch, 8B-shaped layer: the smallest write
+        dict(name="write-step", kind="write", n=16, lo=1, hi=1, past=2650, Hq=32, Hkv=8, D=128, R=128, bs=16, layout="half",
+             attn=1.0, pad=0),
+        # prefill of the benchmark's compacted prompt batch
+        dict(name="write-prompts", kind="write", n=16, lo=2458, hi=2458, past=0, Hq=32, Hkv=8, D=128, R=128, bs=16,
+             layout="half", attn=1.0, pad=0),
+        # the last entries of 33 ragged sessions of the small layer, from mid-page
+        dict(name="read-ragged", kind="read", n=33, lo=1, hi=61, start=517, Hkv=4, D=64, bs=32),
+        # the benchmark's prompt batch taken out of the cache
+        dict(name="read-prompts", kind="read", n=16, lo=2458, hi=2458, start=0, Hkv=8, D=128, bs=16),
+        # one short session of the small layer: the smallest attention
+        dict(name="decode-one", kind="decode", n=1, lo=307, hi=307, Hq=16, Hkv=4, D=64, bs=16),
+        # one decode step of the benchmark batch
+        dict(name="decode-step", kind="decode", n=16, lo=2458, hi=2842, Hq=32, Hkv=8, D=128, bs=16),
+        # a chunk of a long document's prompt behind the chunks before it
+        dict(name="prefill-chunk", kind="prefill", n=1, lo=250, hi=250, past=8192, Hq=32, Hkv=8, D=128, bs=16),
+        # the benchmark's compacted prompt batch
+        dict(name="prefill-prompts", kind="prefill", n=16, lo=2458, hi=2458, past=0, Hq=32, Hkv=8, D=128, bs=16),
+        # the benchmark batch's sessions behind one system prompt, a few hundred entries of their own
+        dict(name="shared-step", kind="shared", dtype="bf16", groups=1, mlo=16, mhi=16, plo=2048, phi=2048, lo=1, hi=640, Hq=32,
+             Hkv=8, D=128, bs=16),
+        # the 7B-shaped serving batch behind four long prompts, 8-bit pages
+        dict(name="shared-prompts", kind="shared", dtype="e4m3", groups=4, mlo=20, mhi=44, plo=6000, phi=8192, lo=128, hi=1024,
+             Hq=28, Hkv=4, D=128, bs=16),
+        # one decode step of the benchmark batch: a creative setting for all
+        dict(name="sample-step", kind="sample", dtype="bf16", rows=16, V=128256, settings="top-p", greedy=0.0),
+        # a large serving batch, each session with settings of its own, a tenth of them greedy
+        dict(name="sample-batch", kind="sample", dtype="bf16", rows=1024, V=128256, settings="mixed", greedy=0.1),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+# (query heads, kv heads, head dim) of the layers the library is configured and tested with
+_LAYERS = ((32, 8, 128), (28, 4, 128), (64, 8, 128), (16, 4, 64), (4, 4, 64))
+
+
+def draw(rng):
+    kind = rng.choice(("write", "read", "decode", "prefill", "shared", "sample"))
+    Hq, Hkv, D = rng.choice(_LAYERS)
+    bs = rng.choice((16, 16, 32, 64, 256))
+    if kind == "write":
+        n = _log_int(rng, 1, 256)
+        hi = _log_int(rng, 1, max(1, min(8192, 39328 * 32 // (n * max(Hq, 16)))))
+        return dict(kind=kind, n=n, lo=rng.choice((1, hi)), hi=hi, past=rng.choice((0, _log_int(rng, 1, 2048))), Hq=Hq, Hkv=Hkv,
+                    D=D, R=rng.choice((D, D, D // 2)), bs=bs, layout=rng.choice(("half", "half", "interleaved")),
+                    attn=rng.choice((1.0, 1.0, 1.25)), pad=rng.choice((0, 0, 5, 64)))
+    if kind == "read":
+        n = _log_int(rng, 1, 256)
+        hi = _log_int(rng, 1, max(1, min(8192, 39328 * 8 // (n * Hkv))))
+        return dict(kind=kind, n=n, lo=rng.choice((0 if n > 4 else 1, 1, hi)), hi=hi,
+                    start=rng.choice((0, 0, _log_int(rng, 1, 1000))), Hkv=Hkv, D=D, bs=bs)
+    if kind == "decode":
+        n = _log_int(rng, 1, 256)
+        hi = _log_int(rng, 1, max(1, min(65536, (1 << 18) // n)))
+        return dict(kind=kind, n=n, lo=rng.choice((0, 1, max(1, hi // 2), hi)), hi=hi, Hq=Hq, Hkv=Hkv, D=D, bs=bs)
+    if kind == "prefill":
+        n = _log_int(rng, 1, 32)
+        hi = _log_int(rng, 1, max(1, min(4096, 32768 // n)))
+        past = rng.choice((0, _log_int(rng, 1, 8192)))
+        while n * hi * (past + hi) * Hq * D > 16 * 2458 * 1229 * 32 * 128:
+            hi, past = max(1, hi // 2), past // 2
+        return dict(kind=kind, n=n, lo=rng.choice((1, hi)), hi=hi, past=past, Hq=Hq, Hkv=Hkv, D=D, bs=bs)
+    if kind == "shared":
+        groups = rng.choice((1, 1, 2, 5, 16))
+        mhi = _log_int(rng, 1, max(1, 128 // groups))
+        phi, hi = _log_int(rng, 1, 32768 // groups), _log_int(rng, 1, 1024)
+        return dict(kind=kind, dtype=rng.choice(("bf16", "e4m3")), groups=groups, mlo=rng.choice((1, mhi)), mhi=mhi,
+                    plo=rng.choice((0, phi)), phi=phi, lo=rng.choice((0, 1, hi)), hi=hi, Hq=Hq, Hkv=Hkv, D=D, bs=bs)
+    dtype = rng.choice(("bf16", "bf16", "f32"))
+    V = rng.choice((1000, 32000, 50257, 128256, 152064, _log_int(rng, 64, 262144)))
+    return dict(kind=kind, dtype=dtype, rows=_log_int(rng, 1, min(2048, (1 << (27 if dtype == "bf16" else 26)) // V)), V=V,
+                settings=rng.choice(("plain", "top-k", "top-p", "min-p", "mixed", "mixed")), greedy=rng.choice((0.0, 0.0, 0.1)))
+
+
+# --------------------------------------------------------------------------
+# inputs (plain torch and numpy)
+
+def _gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def _randn(g, shape, dtype, std=1.0):
+    return torch.empty(shape, dtype=dtype, device="cuda").normal_(0.0, std, generator=g)
+
+
+def _i32(a):
+    return torch.as_tensor(np.array(a, dtype=np.int32, order="C")).cuda()
+
+
+def _rope_args(c):
+    return dict(rot_dim=c["R"], theta=THETA, layout=c["layout"], attn_scale=c["attn"])
+
+
+def _tables(rng, lens, bs, spare=4):
+    """Block table of sequences of these lengths on pages in any order."""
+    blocks = -(-np.asarray(lens) // bs)
+    order = rng.permutation(int(blocks.sum()) + spare).astype(np.int32)
+    table = np.full((len(lens), max(1, int(blocks.max()))), -1, np.int32)
+    at = 0
+    for i, b in enumerate(blocks):
+        table[i, :b] = order[at:at + b]
+        at += int(b)
+    return table, len(order)
+
+
+def _pools(g, nb, Hkv, D, bs, dtype):
+    """Pages of features of about unit size; e4m3 rows with exponents of their own."""
+    shapes = dict(k_pool=(nb, Hkv, bs, D), v_pool=(nb, Hkv, D, bs))
+    if dtype != E4M3:
+        return {name: _randn(g, shape, dtype) for name, shape in shapes.items()}
+    t = {name: _randn(g, shape, BF16, 64.0).to(E4M3) for name, shape in shapes.items()}
+    for name in ("k_exp", "v_exp"):
+        t[name] = torch.randint(127 - 8, 127 - 4, (nb, Hkv, bs), device="cuda", generator=g, dtype=torch.uint8)
+    return t
+
+
+def _cached(s, c, table, nb, lens, dtype, g):
+    """Pages, block table and lengths, as the framework's cache where its calls are made."""
+    s.update(_pools(g, nb, c["Hkv"], c["D"], c["bs"], dtype), block_table=_i32(table), lengths=_i32(lens), bs=c["bs"])
+    if own:
+        from paper_2609_27233_amd import lib as sm
+        s["cache"] = sm.PagedCache(dtype=dtype, num_kv_heads=c["Hkv"], head_dim=c["D"], block_size=c["bs"], num_blocks=nb,
+                                   max_seqs=len(lens), max_blocks_per_seq=table.shape[1])
+        for name in ("k_pool", "v_pool", "k_exp", "v_exp", "block_table", "lengths"):
+            if name in s:
+                s[name] = getattr(s["cache"], name).copy_(s[name])
+    return s
+
+
+def _prepare_write(c, seed):
+    g, rng = _gen(seed), np.random.RandomState(seed % (1 << 32))
+    n, bs, Hq, Hkv, D = c["n"], c["bs"], c["Hq"], c["Hkv"], c["D"]
+    sizes = np.random.RandomState(n)  # lengths are the case's own, pages and order the seed's
+    new = sizes.randint(c["lo"], c["hi"] + 1, n)
+    past = sizes.randint(c["past"] // 2, c["past"] + 1, n) if c["past"] else np.zeros(n, np.int64)
+    table, nb = _tables(rng, past + new, bs)
+    pos = np.concatenate([np.arange(p, p + m) for p, m in zip(past, new)])
+    req = np.repeat(np.arange(n), new)
+    slots = table[req, pos // bs] * bs + pos % bs
+    pos, slots = np.concatenate([pos, np.zeros(c["pad"], int)]), np.concatenate([slots, np.full(c["pad"], -1)])
+    rows = len(pos)
+    qkv = _randn(g, (rows, (Hq + 2 * Hkv) * D), BF16)
+    s = dict(kind="write", q=qkv[:, :Hq * D].view(rows, Hq, D), k=qkv[:, Hq * D:(Hq + Hkv) * D].view(rows, Hkv, D),
+             v=qkv[:, (Hq + Hkv) * D:].view(rows, Hkv, D), pos=_i32(pos), slots=_i32(slots), args=_rope_args(c),
+             q_out=torch.empty((rows, Hq, D), dtype=BF16, device="cuda"))
+    _cached(s, c, table, nb, past + new, E4M3, g)
+    if own:
+        from paper_2609_27233_amd import lib as sm
+        s["rope"] = sm.rope_params(**s["args"])
+    return s
+
+
+def _prepare_read(c, seed):
+    rng, n = np.random.RandomState(seed % (1 << 32)), c["n"]
+    rows = np.random.RandomState(n).randint(c["lo"], c["hi"] + 1, n)
+    table, nb = _tables(rng, c["start"] + rows, c["bs"])
+    ids = rng.permutation(n)
+    total = int(rows.sum())
+    s = dict(kind="read", ids=_i32(ids), start=_i32(np.full(n, c["start"])), offs=_i32(np.concatenate([[0], np.cumsum(rows[ids])])),
+             K=torch.empty((total, c["Hkv"], c["D"]), dtype=BF16, device="cuda"),
+             V=torch.empty((total, c["Hkv"], c["D"]), dtype=BF16, device="cuda"))
+    return _cached(s, c, table, nb, c["start"] + rows, E4M3, _gen(seed))
+
+
+def _prepare_decode(c, seed):
+    g, rng, n = _gen(seed), np.random.RandomState(seed % (1 << 32)), c["n"]
+    lens = np.random.RandomState(n).randint(c["lo"], c["hi"] + 1, n)
+    table, nb = _tables(rng, lens, c["bs"])
+    s = dict(kind="decode", ids=_i32(rng.permutation(n)), q=_randn(g, (n, c["Hq"], c["D"]), BF16), max_len=c["hi"],
+             out=torch.empty((n, c["Hq"], c["D"]), dtype=BF16, device="cuda"))
+    _cached(s, c, table, nb, lens, E4M3, g)
+    if own:
+        from paper_2609_27233_amd import lib as sm
+        s["ws"] = torch.zeros(sm.decode_workspace_bytes(n, c["Hq"], c["D"], c["hi"]), dtype=torch.uint8, device="cuda")
+    return s
+
+
+def _prepare_prefill(c, seed):
+    g, rng, n = _gen(seed), np.random.RandomState(seed % (1 << 32)), c["n"]
+    rows = np.random.RandomState(n).randint(c["lo"], c["hi"] + 1, n)
+    table, nb = _tables(rng, c["past"] + rows, c["bs"])
+    total = int(rows.sum())
+    s = dict(kind="prefill", ids=_i32(np.arange(n)), q=_randn(g, (total, c["Hq"], c["D"]), BF16), max_rows=c["hi"],
+             offs=_i32(np.concatenate([[0], np.cumsum(rows)])),
+             out=torch.empty((total, c["Hq"], c["D"]), dtype=BF16, device="cuda"))
+    return _cached(s, c, table, nb, c["past"] + rows, E4M3, g)
+
+
+def _prepare_shared(c, seed):
+    g, rng, P = _gen(seed), np.random.RandomState(seed % (1 << 32)), c["groups"]
+    sizes = np.random.RandomState(P)
+    members = sizes.randint(c["mlo"], c["mhi"] + 1, P)
+    n = int(members.sum())
+    # sequences 0 .. P - 1 hold the prefixes, the others the sessions' own entries
+    lens = np.concatenate([sizes.randint(c["plo"], c["phi"] + 1, P), sizes.randint(c["lo"], c["hi"] + 1, n)])
+    table, nb = _tables(rng, lens, c["bs"])
+    dtype = DTYPES[c["dtype"]]
+    s = dict(kind="shared", ids=_i32(P + rng.permutation(n)), prefixes=_i32(np.arange(P)),
+             groups=_i32(np.concatenate([[0], np.cumsum(members)])), most=int(members.max()), max_len=c["hi"], max_prefix=c["phi"],
+             q=_randn(g, (n, c["Hq"], c["D"]), BF16), out=torch.empty((n, c["Hq"], c["D"]), dtype=BF16, device="cuda"))
+    _cached(s, c, table, nb, lens, dtype, g)
+    if own:
+        from paper_2609_27233_amd import lib as sm
+        s["ws"] = torch.zeros(sm.decode_shared_workspace_bytes(n, c["Hq"], c["D"], c["hi"], c["phi"]), dtype=torch.uint8,
+                              device="cuda")
+    return s
+
+
+def _prepare_sample(c, seed):
+    g, dt, rows, V = _gen(seed), DTYPES[c["dtype"]], c["rows"], c["V"]
+    x = _randn(g, (rows, V), dt, 2.5)
+    # a few likely tokens in each row, as a trained model has
+    peak = torch.randint(V, (rows, 8), device="cuda", generator=g)
+    x.scatter_add_(1, peak, (6.0 + 6.0 * torch.rand((rows, 8), device="cuda", generator=g)).to(dt))
+    f32 = dict(dtype=torch.float32, device="cuda")
+    rng = np.random.RandomState(seed % (1 << 32))
+    names = ("plain", "top-k", "top-p", "min-p")  # and 4: all three
+    how = rng.randint(0, 5, rows) if c["settings"] == "mixed" else np.full(rows, names.index(c["settings"]))
+    t = rng.uniform(0.5, 1.5, rows)
+    t[rng.uniform(size=rows) < c["greedy"]] = 0.0
+    k = np.where((how == 1) | (how == 4), rng.choice((1, 5, 20, 50, 200), rows), 0)
+    p = np.where((how == 2) | (how == 4), rng.choice((0.5, 0.9, 0.95, 0.99), rows), 1.0)
+    m = np.where((how == 3) | (how == 4), rng.choice((0.02, 0.05, 0.1), rows), 0.0)
+    s = dict(kind="sample", x=x, u=torch.rand(rows, generator=g, **f32), temperature=torch.as_tensor(t).to(**f32),
+             top_k=_i32(k), top_p=torch.as_tensor(p).to(**f32), min_p=torch.as_tensor(m).to(**f32),
+             tokens=torch.empty(rows, dtype=torch.int32, device="cuda"), logprob=torch.empty(rows, **f32))
+    if own:
+        from paper_2609_27233_amd import lib as sm
+        s["ws"] = torch.zeros(sm.sample_workspace_bytes(rows, V), dtype=torch.uint8, device="cuda")
+    return s
+
+
+_PREPARE = dict(write=_prepare_write, read=_prepare_read, decode=_prepare_decode, prefill=_prepare_prefill,
+                shared=_prepare_shared, sample=_prepare_sample)
+
+
+def prepare(case, seed):
+    return _PREPARE[case["kind"]](case, seed)
+
+
+# --------------------------------------------------------------------------
+# the framework's calls
+
+def _run_own(s):
+    from paper_2609_27233_amd import lib as sm
+    if s["kind"] == "write":
+        sm.kv_write_rotary(s["cache"], s["pos"], s["slots"], s["q"], s["k"], s["v"], s["rope"], s["q_out"])
+        return dict(q=s["q_out"], k_pool=s["k_pool"], v_pool=s["v_pool"], k_exp=s["k_exp"], v_exp=s["v_exp"])
+    if s["kind"] == "read":
+        sm.kv_read(s["cache"], s["ids"], s["offs"], s["K"], s["V"], start=s["start"])
+        return dict(K=s["K"], V=s["V"])
+    if s["kind"] == "decode":
+        sm.decode_attention(s["cache"], s["ids"], s["q"], s["out"], s["ws"], s["max_len"])
+        return s["out"]
+    if s["kind"] == "prefill":
+        sm.prefill_attention(s["cache"], s["ids"], s["offs"], s["q"], s["out"], s["max_rows"])
+        return s["out"]
+    if s["kind"] == "shared":
+        sm.decode_attention_shared(s["cache"], s["ids"], s["prefixes"], s["groups"], s["q"], s["out"], s["ws"], s["max_len"],
+                                   s["max_prefix"])
+        return s["out"]
+    sm.sample_tokens(s["x"], s["u"], s["tokens"], s["ws"], temperature=s["temperature"], top_k=s["top_k"], top_p=s["top_p"],
+                     min_p=s["min_p"], logprob=s["logprob"])
+    return dict(tokens=s["tokens"], logprob=s["logprob"])
+
+
+# --------------------------------------------------------------------------
+# the plain forms
+
+def _turned(x, pos, a):
+    R = a["rot_dim"]
+    j = torch.arange(R // 2, dtype=torch.float64, device="cuda")
+    ang = pos.double()[:, None] * a["theta"] ** (-2.0 * j / R)
+    cos, sin = ((a["attn_scale"] * f(ang)).float()[:, None] for f in (torch.cos, torch.sin))
+    x32 = x.float()
+    out = x32.clone()
+    u, v = (x32[..., :R // 2], x32[..., R // 2:R]) if a["layout"] == "half" else (x32[..., 0:R:2], x32[..., 1:R:2])
+    one, two = u * cos - v * sin, u * sin + v * cos
+    if a["layout"] == "half":
+        out[..., :R // 2], out[..., R // 2:R] = one, two
+    else:
+        out[..., 0:R:2], out[..., 1:R:2] = one, two
+    return out
+
+
+def _quantised(y, x, factor):
+    """e4m3 values of rows y with the exponent byte of their inputs x: the least e with factor max|x| <= 2^(e + 8)."""
+    mant, ex = torch.frexp(x.float().abs().amax(-1) * factor)
+    e = (torch.where(mant > 0.5, ex, ex - 1) - 8).clamp_(-100, 119)
+    return torch.ldexp(y, -e[..., None]).to(E4M3), (e + 127).to(torch.uint8)
+
+
+def _plain_write(s):
+    a, bs, slots = s["args"], s["bs"], s["slots"].long()
+    s["q_out"].copy_(_turned(s["q"], s["pos"], a))
+    k, k_exp = _quantised(_turned(s["k"], s["pos"], a), s["k"], max(1.0, abs(a["attn_scale"])))
+    v, v_exp = _quantised(s["v"].float(), s["v"], 1.0)
+    # a padded row writes the first row once more
+    src = torch.where(slots >= 0, torch.arange(slots.numel(), device="cuda"), 0)
+    page, at = slots[src] // bs, slots[src] % bs
+    byte = torch.uint8
+    s["k_pool"].view(byte)[page, :, at] = k.view(byte)[src]
+    s["v_pool"].view(byte)[page, :, :, at] = v.view(byte)[src]
+    s["k_exp"][page, :, at] = k_exp[src]
+    s["v_exp"][page, :, at] = v_exp[src]
+    return dict(q=s["q_out"], k_pool=s["k_pool"], v_pool=s["v_pool"], k_exp=s["k_exp"], v_exp=s["v_exp"])
+
+
+def _features(s, pages, name):
+    """fp32 features of the pages [...] of K (entries, then features) or V (features, then entries)."""
+    pool = s[name + "_pool"]
+    if pool.dtype != E4M3:
+        return pool[pages].float()
+    x = pool.view(torch.uint8)[pages].view(E4M3).float()
+    scale = torch.ldexp(torch.ones((), device="cuda"), s[name + "_exp"][pages].int() - 127)
+    return x * (scale[..., None] if name == "k" else scale[..., None, :])
+
+
+def _rows_of(s, ids):
+    """K, V [sequences, Hkv, entries, D] in fp32 and the lengths of the listed sequences."""
+    lens = s["lengths"][ids].long()
+    pages = s["block_table"][ids].long().clamp(min=0)
+    K = _features(s, pages, "k").transpose(1, 2).flatten(2, 3)
+    V = _features(s, pages, "v").permute(0, 2, 1, 4, 3).flatten(2, 3)
+    there = torch.arange(K.shape[2], device="cuda") < lens[:, None]
+    return K, V, there
+
+
+def _plain_read(s):
+    r = torch.arange(s["K"].shape[0], device="cuda")
+    offs, bs = s["offs"].long(), s["bs"]
+    i = torch.searchsorted(offs[1:], r, right=True)
+    p = r - offs[i] + s["start"][i].long()
+    page, at = s["block_table"][s["ids"][i].long(), p // bs].long(), p % bs
+    byte = torch.uint8
+    for name, out in (("k", s["K"]), ("v", s["V"])):
+        pool = s[name + "_pool"].view(byte)
+        x = (pool[page, :, at] if name == "k" else pool[page, :, :, at]).view(E4M3).float()
+        out.copy_(torch.ldexp(x, (s[name + "_exp"][page, :, at].int() - 127)[..., None]))
+    return dict(K=s["K"], V=s["V"])
+
+
+def _softmax_parts(score, there):
+    """(largest, exponentials) of scores where entries are there; rows of none: -inf, zeros."""
+    score = score.masked_fill(~there, -math.inf)
+    m = score.amax(-1, keepdim=True)
+    return m, score
+
+
+def _weights(score, m):
+    return torch.exp(score - torch.where(torch.isfinite(m), m, 0.0))
+
+
+def _plain_decode(s):
+    n, Hq, D = s["q"].shape
+    K, V, there = _rows_of(s, s["ids"].long())
+    q = s["q"].float().view(n, K.shape[1], -1, D)
+    m, score = _softmax_parts(q @ K.transpose(2, 3) * D ** -0.5, there[:, None, None])
+    w = _weights(score, m)
+    total = w.sum(-1, keepdim=True)
+    s["out"].copy_(((w @ V) / torch.where(total > 0, total, 1.0)).view(n, Hq, D))
+    return s["out"]
+
+
+def _plain_prefill(s):
+    rows, Hq, D = s["q"].shape
+    offs, n = s["offs"].long(), s["ids"].numel()
+    K, V, there = _rows_of(s, s["ids"].long())
+    Hkv, most = K.shape[1], s["max_rows"]
+    r = torch.arange(rows, device="cuda")
+    i = torch.searchsorted(offs[1:], r, right=True)
+    at = r - offs[i]
+    q = torch.zeros((n, most, Hq, D), device="cuda")
+    q[i, at] = s["q"].float()
+    q = q.view(n, most, Hkv, -1, D).permute(0, 2, 3, 1, 4).flatten(2, 3)             # [n, Hkv, heads x rows, D]
+    G = Hq // Hkv
+    m = offs[1:] - offs[:-1]
+    pos = (s["lengths"][s["ids"].long()].long() - m)[:, None] + torch.arange(most, device="cuda")
+    seen = torch.arange(K.shape[2], device="cuda") <= pos[..., None]                     # [n, rows, entries]
+    seen = seen[:, None, None].expand(n, 1, G, -1, -1).flatten(2, 3) & there[:, None, None]
+    m, score = _softmax_parts(q @ K.transpose(2, 3) * D ** -0.5, seen)
+    w = _weights(score, m)
+    out = (w @ V) / w.sum(-1, keepdim=True)
+    out = out.unflatten(2, (G, most)).permute(0, 3, 1, 2, 4).flatten(2, 3)
+    s["out"].copy_(out[i, at])
+    return s["out"]
+
+
+def _plain_shared(s):
+    n, Hq, D = s["q"].shape
+    K, V, there = _rows_of(s, s["ids"].long())
+    Kp, Vp, there_p = _rows_of(s, s["prefixes"].long())
+    P, Hkv, most = Kp.shape[0], Kp.shape[1], s["most"]
+    groups = s["groups"].long()
+    r = torch.arange(n, device="cuda")
+    grp = torch.searchsorted(groups[1:], r, right=True)
+    at = r - groups[grp]
+    q = s["q"].float().view(n, Hkv, -1, D)
+    G = q.shape[2]
+    qp = torch.zeros((P, most, Hkv, G, D), device="cuda")
+    qp[grp, at] = q
+    qp = qp.transpose(1, 2).flatten(2, 3)                                               # [P, Hkv, members x G, D]
+    m1, score1 = _softmax_parts(qp @ Kp.transpose(2, 3) * D ** -0.5, there_p[:, None, None])
+    m2, score2 = _softmax_parts(q @ K.transpose(2, 3) * D ** -0.5, there[:, None, None])
+
+    def by_group(x):  # [n, Hkv, G, k] of a request to [P, Hkv, members x G, k]
+        full = torch.full((P, most, Hkv, G, x.shape[-1]), -math.inf, device="cuda")
+        full[grp, at] = x
+        return full.transpose(1, 2).flatten(2, 3)
+
+    def by_request(x):
+        return x.unflatten(2, (most, G)).transpose(1, 2)[grp, at]
+    m = torch.maximum(by_request(m1), m2)
+    w1, w2 = _weights(score1, by_group(m)), _weights(score2, m)
+    total = by_request(w1.sum(-1, keepdim=True)) + w2.sum(-1, keepdim=True)
+    s["out"].copy_(((by_request(w1 @ Vp) + w2 @ V) / torch.where(total > 0, total, 1.0)).view(n, Hq, D))
+    return s["out"]
+
+
+def _plain_sample(s):
+    x, V = s["x"].float(), s["x"].shape[1]
+    greedy = s["temperature"] == 0
+    scale = torch.where(greedy, 1.0, 1.0 / s["temperature"].double())[:, None]
+    k = torch.where(greedy, 1, torch.where(s["top_k"] > 0, s["top_k"], V))[:, None]
+    top_p, min_p, u = (s[name].double()[:, None] for name in ("top_p", "min_p", "u"))
+    vals, order = torch.sort(x, dim=1, descending=True, stable=True)
+    top = vals[:, :1].double()
+    w = torch.exp((vals.double() - top) * scale)
+    rank = torch.arange(V, device="cuda")
+    keep = (rank < k) & (w >= min_p)
+    w = torch.where(keep, w, 0.0)
+    total = w.sum(1, keepdim=True)
+    keep &= ((w.cumsum(1) - w) < top_p * total) | (rank == 0) | (top_p >= 1)
+    kept = torch.zeros_like(keep).scatter_(1, order, keep)
+    w = torch.where(kept, torch.exp((x.double() - top) * scale), 0.0)
+    cum = w.cumsum(1)
+    total = cum[:, -1:]
+    token = (cum <= u * total).sum(1, keepdim=True).clamp_(max=V - 1)
+    s["tokens"].copy_(token[:, 0])
+    s["logprob"].copy_(torch.log(w.gather(1, token) / total)[:, 0])
+    return dict(tokens=s["tokens"], logprob=s["logprob"])
+
+
+_PLAIN = dict(write=_plain_write, read=_plain_read, decode=_plain_decode, prefill=_plain_prefill, shared=_plain_shared,
+              sample=_plain_sample)
+
+
+def run(state):
+    if own:
+        return _run_own(state)
+    return _PLAIN[state["kind"]](state)
+
+
+# --------------------------------------------------------------------------
+# what a pass cannot do without
+
+def work(case):
+    c = case
+    if c["kind"] == "sample":
+        return dict(bytes=c["rows"] * (c["V"] * (2 if c["dtype"] == "bf16" else 4) + 28), flops=5 * c["rows"] * c["V"])
+    D, Hkv = c["D"], c["Hkv"]
+    entry = 2 * Hkv * ((D + 1) if c.get("dtype", "e4m3") == "e4m3" else 2 * D)  # bytes of a cached entry
+    if c["kind"] == "write":
+        rows = c["n"] * (c["lo"] + c["hi"]) / 2
+        return dict(bytes=rows * (4 * (c["Hq"] + Hkv) * D + entry + 8) + c["pad"] * (4 * c["Hq"] * D + 8),
+                    flops=rows * (3 * (c["Hq"] + Hkv) * c["R"] + 4 * Hkv * D))
+    if c["kind"] == "read":
+        rows = c["n"] * (c["lo"] + c["hi"]) / 2
+        return dict(bytes=rows * (entry + 4 * Hkv * D) + 12 * c["n"], flops=2 * rows * Hkv * D)
+    Hq = c["Hq"]
+    if c["kind"] == "decode":
+        entries = c["n"] * (c["lo"] + c["hi"]) / 2
+        return dict(bytes=entries * entry + 4 * c["n"] * Hq * D, flops=4 * entries * Hq * D)
+    if c["kind"] == "prefill":
+        rows = c["n"] * (c["lo"] + c["hi"]) / 2
+        return dict(bytes=(rows + c["n"] * c["past"]) * entry + 4 * rows * Hq * D,
+                    flops=4 * rows * (c["past"] + (c["lo"] + c["hi"]) / 4) * Hq * D)
+    n, prefix, mine = c["groups"] * (c["mlo"] + c["mhi"]) / 2, (c["plo"] + c["phi"]) / 2, (c["lo"] + c["hi"]) / 2
+    return dict(bytes=(c["groups"] * prefix + n * mine) * entry + 4 * n * Hq * D, flops=4 * n * (prefix + mine) * Hq * D)
+
+
+# --------------------------------------------------------------------------
+# the definitions, in 64 bits
+
+def _exact_turn(x, pos, a):
+    """Each pair as a complex number, times attn_scale e^(i angle)."""
+    R, j = a["rot_dim"], np.arange(a["rot_dim"] // 2)
+    w = torch.from_numpy(np.exp(-2.0 * j / R * np.log(a["theta"]))).cuda()
+    turn = a["attn_scale"] * torch.exp(1j * pos.double()[:, None] * w)[:, None]
+    out = x.double()
+    head = out[..., :R]
+    pairs = head.unflatten(-1, (2, R // 2)).transpose(-1, -2) if a["layout"] == "half" else head.unflatten(-1, (R // 2, 2))
+    z = torch.view_as_real(torch.view_as_complex(pairs.contiguous()) * turn)
+    z = z.transpose(-1, -2).flatten(-2) if a["layout"] == "half" else z.flatten(-2)
+    return torch.cat([z, out[..., R:]], -1)
+
+
+def _exact_quantised(y, x, factor):
+    """The same by logarithms and steps: the step of a value in [2^k, 2^(k+1)) is 2^(k-3), the least 2^-9."""
+    e = (torch.ceil(torch.log2(x.double().abs().amax(-1) * factor)) - 8).clamp(-100, 119)
+    z = y * torch.exp2(-e)[..., None]
+    step = torch.exp2((torch.floor(torch.log2(z.abs().clamp(min=2.0 ** -6))) - 3))
+    return torch.round(z / step) * step, (e + 127).long()
+
+
+def _exact_write(c, s):
+    a, bs = s["args"], s["bs"]
+    at = torch.nonzero(s["slots"] >= 0)[:, 0]
+    slots = s["slots"][at].long()
+    k, ke = _exact_quantised(_exact_turn(s["k"], s["pos"], a)[at], s["k"][at], max(1.0, abs(a["attn_scale"])))
+    v, ve = _exact_quantised(s["v"][at].double(), s["v"][at], 1.0)
+    flat = s["k_pool"].double().transpose(1, 2).flatten(0, 1).index_copy(0, slots, k)
+    k_pool = flat.unflatten(0, (-1, bs)).transpose(1, 2)
+    flat = s["v_pool"].double().permute(0, 3, 1, 2).flatten(0, 1).index_copy(0, slots, v)
+    v_pool = flat.unflatten(0, (-1, bs)).permute(0, 2, 3, 1)
+    exps = []
+    for name, e in (("k_exp", ke), ("v_exp", ve)):
+        flat = s[name].long().transpose(1, 2).flatten(0, 1).index_copy(0, slots, e)
+        exps.append(flat.unflatten(0, (-1, bs)).transpose(1, 2))
+    return dict(q=_exact_turn(s["q"], s["pos"], a), k_pool=k_pool, v_pool=v_pool, k_exp=exps[0], v_exp=exps[1])
+
+
+def _exact_entries(s, seq, first, last):
+    """K, V [entries, Hkv, D] in 64 bits of one sequence's entries, by their slots."""
+    bs = s["bs"]
+    p = torch.arange(first, last, device="cuda")
+    page, at = s["block_table"][seq].long()[p // bs], p % bs
+    if s["k_pool"].dtype != E4M3:
+        return s["k_pool"][page, :, at].double(), s["v_pool"][page, :, :, at].double()
+    byte = torch.uint8
+    K = s["k_pool"].view(byte)[page, :, at].view(E4M3).double() * torch.exp2(s["k_exp"][page, :, at].double() - 127)[..., None]
+    V = s["v_pool"].view(byte)[page, :, :, at].view(E4M3).double() * torch.exp2(s["v_exp"][page, :, at].double() - 127)[..., None]
+    return K, V
+
+
+def _exact_read(c, s):
+    parts = []
+    offs, ids = s["offs"].tolist(), s["ids"].tolist()
+    for i, seq in enumerate(ids):
+        parts.append(_exact_entries(s, seq, c["start"], c["start"] + offs[i + 1] - offs[i]))
+    return dict(K=torch.cat([p[0] for p in parts]), V=torch.cat([p[1] for p in parts]))
+
+
+def _exact_attend(q, K, V, seen=None):
+    """q [rows, Hq, D] over entries K, V [entries, Hkv, D]; seen [rows, entries]."""
+    rows, Hq, D = q.shape
+    out = torch.zeros((rows, Hq, D), dtype=torch.float64, device="cuda")
+    if K.shape[0]:
+        G = Hq // K.shape[1]
+        for h in range(Hq):
+            score = q[:, h].double() @ K[:, h // G].T / math.sqrt(D)
+            if seen is not None:
+                score = torch.where(seen, score, -math.inf)
+            out[:, h] = torch.softmax(score, 1) @ V[:, h // G]
+    return out
+
+
+def _exact_decode(c, s):
+    lens = s["lengths"].tolist()
+    return torch.cat([_exact_attend(s["q"][i:i + 1], *_exact_entries(s, seq, 0, lens[seq]))
+                      for i, seq in enumerate(s["ids"].tolist())])
+
+
+def _exact_prefill(c, s):
+    offs, lens = s["offs"].tolist(), s["lengths"].tolist()
+    parts = []
+    for i, seq in enumerate(s["ids"].tolist()):
+        m, L = offs[i + 1] - offs[i], lens[seq]
+        seen = torch.ones((m, L), dtype=torch.bool, device="cuda").tril_(L - m)
+        parts.append(_exact_attend(s["q"][offs[i]:offs[i + 1]], *_exact_entries(s, seq, 0, L), seen))
+    return torch.cat(parts)
+
+
+def _exact_shared(c, s):
+    lens, groups, ids = s["lengths"].tolist(), s["groups"].tolist(), s["ids"].tolist()
+    parts = []
+    for p, prefix in enumerate(s["prefixes"].tolist()):
+        Kp, Vp = _exact_entries(s, prefix, 0, lens[prefix])
+        for i in range(groups[p], groups[p + 1]):
+            K, V = _exact_entries(s, ids[i], 0, lens[ids[i]])
+            parts.append(_exact_attend(s["q"][i:i + 1], torch.cat([Kp, K]), torch.cat([Vp, V])))
+    return torch.cat(parts)
+
+
+def _exact_sample(c, s):
+    """Row by row: the kept set is the start of the tokens in order, then the inverse of its cumulative mass."""
+    settings = [s[name].double().tolist() for name in ("temperature", "top_k", "top_p", "min_p", "u")]
+    tokens, logprobs = [], []
+    for x, T, k, p, m, u in zip(s["x"], *settings):
+        x = x.double()
+        order = torch.sort(x, descending=True, stable=True).indices[:1 if T == 0 else int(k) or None]
+        z = (x[order] - x[order[0]]) / (T or 1.0)
+        order = order[:max(1, int((z.exp() >= m).sum()))]
+        w = torch.exp(z[:order.numel()])
+        if p < 1:
+            mass = torch.cumsum(w, 0)
+            order = order[:1 + int((mass[:-1] < p * mass[-1]).sum())]
+        order = order.sort().values
+        w = torch.exp((x[order] - x.max()) / (T or 1.0))
+        mass = torch.cumsum(w, 0)
+        at = min(int(torch.searchsorted(mass, u * mass[-1], right=True)), order.numel() - 1)
+        tokens.append(order[at])
+        logprobs.append(torch.log(w[at]) - torch.log(mass[-1]))
+    return dict(tokens=torch.stack(tokens), logprob=torch.stack(logprobs))
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    return dict(write=_exact_write, read=_exact_read, decode=_exact_decode, prefill=_exact_prefill, shared=_exact_shared,
+                sample=_exact_sample)[case["kind"]](case, s)
