@@ -35,7 +35,8 @@
  *                       for all layers at once
  *   sm_rotary           rotary positions of rows of heads
  *   sm_kv_write_rotary  one layer's q, K and V rows: q and K turned, K and V
- *                       into the reserved slots
+ *                       into the reserved slots (in 8 bits where pages are)
+ *   sm_kv_read          cached entries back as rows of K and V
  *   sm_block_norm       residual sum with the norms after one block and
  *                       before the next
  *   sm_token_logprobs   log probabilities, entropy and top alternatives of
@@ -65,7 +66,8 @@
  *    memory is ever used to address memory before it has been range-checked.
  *
  * Dtypes: SM_F32 (fp32 storage, fp32 arithmetic) and SM_BF16 (bf16 storage,
- * fp32 accumulation, outputs rounded to nearest-even bf16).
+ * fp32 accumulation, outputs rounded to nearest-even bf16).  Pages of a cache
+ * may also be SM_E4M3 (see sm_paged_cache), for the calls that say so.
  */
 #ifndef SPANMERGE_H
 #define SPANMERGE_H
@@ -78,7 +80,7 @@
 extern "C" {
 #endif
 
-typedef enum { SM_F32 = 0, SM_BF16 = 1 } sm_dtype;
+typedef enum { SM_F32 = 0, SM_BF16 = 1, SM_E4M3 = 2 /* cache pages only */ } sm_dtype;
 
 typedef enum {
   SM_OK = 0,
@@ -135,6 +137,16 @@ typedef struct {
  * slot j % block_size.  head_dim must be 64 or 128; block_size must be a
  * power of two in [16, 512]; num_kv_heads * head_dim <= 2048.  Pools must
  * be 16-byte aligned.
+ *
+ * SM_E4M3: pages in 8 bits.  A pool holds its values as above, one e4m3 byte
+ * each (sign, 4 bits of exponent, 3 of the fraction, largest 448), and behind
+ * them one exponent byte for each entry and head,
+ *   [num_blocks][num_kv_heads][block_size]  b: feature = value x 2^(b - 127)
+ * (num_blocks x num_kv_heads x block_size x (head_dim + 1) bytes a pool).
+ * Rows going in and out, queries and results are bf16.  sm_kv_write_rotary
+ * fills such pages (positions of 0 turn nothing), sm_kv_read reads them, and
+ * sm_kv_reserve, sm_kv_rollback and sm_match_decode's crop move their tables.
+ * The other calls refuse them.
  */
 typedef struct {
   sm_dtype dtype;
@@ -805,6 +817,16 @@ sm_status sm_rotary(const void *x, int64_t x_stride, const int32_t *pos,
  * [-1, num_blocks x block_size); that row is not written to the pages, the
  * others are.  The call goes by its slots alone and does not look at the
  * error word (a reserve that failed gives no slots).
+ *
+ * SM_E4M3 pages: rows are bf16.  A K or V row of one head with features x is
+ * stored as round(y 2^-e), y the turned K (fp32) or V itself, under the least
+ * e with M <= 2^(e + 8), M = max |x| over its finite features (K: times
+ * |attn_scale| where that is above 1), -100 <= e <= 119; the exponent byte is
+ * e + 127.  The rounding is to the nearest e4m3 value, ties to even: off by at
+ * most 2^-4 of the value, or 2^-10 x 2^e where that is more, which is below
+ * 2^-17 M unless M < 2^-92.  Below e = 119 no value leaves the
+ * range; under it (M > 2^127) what does is +-448.  NaN and infinities are
+ * stored as NaN.
  */
 sm_status sm_kv_write_rotary(const sm_paged_cache *c, const int32_t *pos,
                              const int32_t *slots, int rows, const void *q,
@@ -812,6 +834,32 @@ sm_status sm_kv_write_rotary(const sm_paged_cache *c, const int32_t *pos,
                              int64_t k_stride, const void *v, int64_t v_stride,
                              const sm_rope_params *p, void *q_out,
                              int64_t q_out_stride, hipStream_t stream);
+
+/*
+ * sm_kv_read -- cached entries back as rows, the other way round from
+ * sm_kv_append and sm_kv_write_rotary: to move a sequence to another cache or
+ * to the host, or to go on with it in another type.
+ *   K[r], V[r] = entry start[i] + r - row_offsets[i] of sequence seq_ids[i],
+ *   row_offsets[i] <= r < row_offsets[i+1]
+ *
+ *  c            (host) any page type
+ *  seq_ids      [n] ids in [0, max_seqs) (repeats allowed), n <= SM_MAX_REQUESTS
+ *  start        [n] first entry of each request, or null for 0
+ *  row_offsets  [n + 1] as in sm_kv_append, row_offsets[0] = 0
+ *  total_rows   (host) room in K and V; rows from row_offsets[n] on are left
+ *               as they are
+ *  K, V         [total_rows][num_kv_heads][head_dim] out, row strides in
+ *               elements; either may be null.  Pages of SM_E4M3 are read as
+ *               bf16, which holds their features exactly; others as they are
+ * num_blocks x block_size must be below 2^31.  The error word does not stop
+ * it.  Device errors (into c->err): EINVAL when the offsets are out of order
+ * or range (then nothing is written), or for a bad id or block id, ERANGE for
+ * an entry outside its sequence; such rows are zero.
+ */
+sm_status sm_kv_read(const sm_paged_cache *c, const int32_t *seq_ids,
+                     const int32_t *start, const int32_t *row_offsets, int n,
+                     int total_rows, void *K, int64_t k_stride, void *V,
+                     int64_t v_stride, hipStream_t stream);
 
 /*
  * The norms around a block of the backbone:

@@ -130,9 +130,10 @@ static inline int ilog2_pow2(int v) {
   return l;
 }
 
-static inline bool cache_ok(const sm_paged_cache *c, sm::CacheArgs &a) {
+// eight: the call takes e4m3 pages, or does not touch the pools
+static inline bool cache_ok(const sm_paged_cache *c, sm::CacheArgs &a, bool eight = false) {
   if (!c) return false;
-  if (c->dtype != SM_F32 && c->dtype != SM_BF16) return false;
+  if (c->dtype != SM_F32 && c->dtype != SM_BF16 && !(eight && c->dtype == SM_E4M3)) return false;
   if (c->head_dim != 64 && c->head_dim != 128) return false;
   const int l = ilog2_pow2(c->block_size);
   if (l < 4 || l > 9) return false;

@@ -753,7 +753,7 @@ using namespace sm;
 SM_API sm_status sm_kv_rollback(const sm_paged_cache *c, const int32_t *seq_ids, const int32_t *k, int n,
                                 hipStream_t stream) {
   CacheArgs a;
-  if (!cache_ok(c, a) || n < 0 || n > SM_MAX_REQUESTS || n > c->max_seqs) return SM_EINVAL;
+  if (!cache_ok(c, a, true) || n < 0 || n > SM_MAX_REQUESTS || n > c->max_seqs) return SM_EINVAL;
   if (n == 0) return SM_OK;
   if (!seq_ids || !k) return SM_EINVAL;
   hipLaunchKernelGGL(rollback_kernel, dim3(1), dim3(kMetaThreads), 0, stream, a, seq_ids, k, n);

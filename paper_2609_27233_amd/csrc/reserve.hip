@@ -292,7 +292,7 @@ SM_API sm_status sm_kv_reserve(const sm_paged_cache *c, const int32_t *seq_ids, 
                                int n, int max_rows, int32_t *row_offsets, int32_t *pos, int32_t *slots,
                                hipStream_t stream) {
   CacheArgs a;
-  if (!cache_ok(c, a) || n < 0 || n > SM_MAX_REQUESTS || n > c->max_seqs || max_rows < 0) return SM_EINVAL;
+  if (!cache_ok(c, a, true) || n < 0 || n > SM_MAX_REQUESTS || n > c->max_seqs || max_rows < 0) return SM_EINVAL;
   if ((int64_t)c->num_blocks * c->block_size > INT32_MAX) return SM_EINVAL;
   if (!row_offsets || (n > 0 && (!seq_ids || !rows)) || (max_rows > 0 && (!pos || !slots))) return SM_EINVAL;
   const ReserveArgs r{seq_ids, crop, rows, n, max_rows, row_offsets, pos, slots};

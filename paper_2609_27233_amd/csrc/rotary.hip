@@ -25,6 +25,7 @@
 #include <cmath>
 
 #include "cache_meta.hpp"
+#include "e4m3.hpp"
 #include "vec16.hpp"
 
 namespace sm {
@@ -233,6 +234,7 @@ struct WriteArgs {
   Rows q, k, v;
   const int32_t *slots;
   void *k_pool, *v_pool;
+  uint8_t *k_exp, *v_exp;  // e4m3 pages
   int32_t *err;
   int bs_log2, dh_log2, num_slots;
 };
@@ -261,9 +263,155 @@ __device__ __forceinline__ T *page_of(T *pool, int s, const WriteArgs &w, int *i
   return pool + (((int64_t)(s >> w.bs_log2) * w.k.heads) << (w.bs_log2 + w.dh_log2));
 }
 
-template <typename T, bool HALF, bool STREAM>
+// e4m3 pages (rows of bf16).  A head's row is held by the D / 8 neighbouring
+// lanes of its 16-byte chunks, which share its largest input feature.
+
+// The turned features of chunk c of row x, and the largest of them before the turn.
+template <bool HALF, bool STREAM>
+__device__ __forceinline__ float turned_chunk(const uint16_t *x, int c, int R, const float2 *cs, float (&y)[8]) {
+  const int at = 8 * c;
+  Vec16<uint16_t>::open(load_as<STREAM, u32x4_t>(x + at), y);
+  const float most = largest(y);
+  if (at >= R) return most;
+  if constexpr (HALF) {
+    const bool first = at < R / 2;
+    float z[8];
+    Vec16<uint16_t>::open(load_as<STREAM, u32x4_t>(x + (first ? at + R / 2 : at - R / 2)), z);
+    cs += first ? at : at - R / 2;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float2 t = first ? turned(y[e], z[e], cs[e]) : turned(z[e], y[e], cs[e]);
+      y[e] = first ? t.x : t.y;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+      const float2 t = turned(y[e], y[e + 1], cs[at / 2 + e / 2]);
+      y[e] = t.x;
+      y[e + 1] = t.y;
+    }
+  }
+  return most;
+}
+// The same, a feature at a time: any R, any address.
+template <bool HALF>
+__device__ __forceinline__ float turned_features(const uint16_t *x, int c, int R, const float2 *cs, float (&y)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) y[e] = bf16_to_f32(x[8 * c + e]);
+  const float most = largest(y);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int i = 8 * c + e, j = HALF ? (i < R / 2 ? i : i - R / 2) : i / 2;  // its pair
+    if (i >= R) continue;
+    const bool first = HALF ? i < R / 2 : i % 2 == 0;
+    const float other = bf16_to_f32(x[HALF ? (first ? i + R / 2 : j) : i ^ 1]);
+    const float2 t = first ? turned(y[e], other, cs[j]) : turned(other, y[e], cs[j]);
+    y[e] = first ? t.x : t.y;
+  }
+  return most;
+}
+
+__device__ __forceinline__ uint2 quantised(const float (&y)[8], int byte) {
+  const float inv = exp_inverse(byte);
+  return make_uint2(pack_e4m3(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv),
+                    pack_e4m3(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv));
+}
+
+// Maximum over a head's lanes, 8 (D = 64) or 16.
+__device__ __forceinline__ float over_head(float m, int dh_log2) { return dh_log2 == 7 ? head_max<16>(m) : head_max<8>(m); }
+
+// K heads [k0, k1) of rows [r0, r0 + nr) into their pages, slots slot[0 .. nr).
+// chunk(x, c, row's cosines and sines, y): turned_chunk or turned_features.
+template <class F>
+__device__ __forceinline__ void write_k_e4m3(const RopeArgs &a, const WriteArgs &w, int64_t r0, int nr, int k0, int k1,
+                                             const int *slot, const float2 *cs, F chunk) {
+  const int lanes_log2 = w.dh_log2 - 3, D = 1 << w.dh_log2;
+  const float factor = fmaxf(1.f, fabsf(a.scale)), inv = 1.f / nr;
+  for (int u = threadIdx.x; u < (nr * (k1 - k0)) << lanes_log2; u += kRotThreads) {
+    const int c = u & ((1 << lanes_log2) - 1), hr = u >> lanes_log2;
+    const int hh = (int)((hr + 0.5f) * inv), r = hr - hh * nr, h = k0 + hh;  // (exact below 2^21)
+    float y[8];
+    const float most = over_head(chunk((const uint16_t *)w.k.in + (r0 + r) * w.k.in_stride + h * D, c, cs + r * (a.R / 2), y),
+                                 w.dh_log2);
+    const int byte = exp_byte(most * factor), sl = slot[r];
+    if (sl < 0) continue;
+    int at;
+    uint8_t *page = page_of((uint8_t *)w.k_pool, sl, w, &at) + ((int64_t)h << (w.bs_log2 + w.dh_log2));
+    *(uint2 *)(page + at * D + 8 * c) = quantised(y, byte);
+    if (c == 0) w.k_exp[(((int64_t)(sl >> w.bs_log2) * w.k.heads + h) << w.bs_log2) + at] = (uint8_t)byte;
+  }
+}
+
+// One row's V chunk, stored a byte at a time.
+__device__ __forceinline__ void store_v_e4m3(const WriteArgs &w, int sl, int h, int c, int byte, uint2 q) {
+  int at;
+  uint8_t *out = page_of((uint8_t *)w.v_pool, sl, w, &at) + ((((int64_t)h << w.dh_log2) + 8 * c) << w.bs_log2) + at;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) out[(int64_t)e << w.bs_log2] = (uint8_t)((e < 4 ? q.x : q.y) >> (8 * (e & 3)));
+  if (c == 0) w.v_exp[(((int64_t)(sl >> w.bs_log2) * w.v.heads + h) << w.bs_log2) + at] = (uint8_t)byte;
+}
+
+// V heads [g0, g1): a thread takes the 8 features of a chunk for a group of
+// rows that fill consecutive slots of 16 aligned ones; a whole group leaves as
+// 16 bytes a feature.
+template <bool STREAM>
+__device__ __forceinline__ void write_v_e4m3(const WriteArgs &w, int64_t r0, int g0, int g1, int groups, const int *group,
+                                             const int *slot) {
+  const int lanes_log2 = w.dh_log2 - 3, D = 1 << w.dh_log2;
+  const float inv = 1.f / groups;
+  for (int u = threadIdx.x; u < ((g1 - g0) * groups) << lanes_log2; u += kRotThreads) {
+    const int c = u & ((1 << lanes_log2) - 1), hg = u >> lanes_log2;
+    const int hh = (int)((hg + 0.5f) * inv), g = hg - hh * groups, h = g0 + hh;
+    const int f = group[g], n = group[g + 1] - f, sl = slot[f];
+    if (sl < 0) continue;
+    const uint16_t *in = (const uint16_t *)w.v.in + (r0 + f) * w.v.in_stride + h * D + 8 * c;
+    if (n < 16) {
+      for (int i = 0; i < n; ++i) {
+        float y[8];
+        Vec16<uint16_t>::open(load_as<STREAM, u32x4_t>(in + i * w.v.in_stride), y);
+        const int byte = exp_byte(over_head(largest(y), w.dh_log2));
+        store_v_e4m3(w, sl + i, h, c, byte, quantised(y, byte));
+      }
+      continue;
+    }
+    u32x4_t v[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = load_as<STREAM, u32x4_t>(in + i * w.v.in_stride);
+    u32x4_t out[8], bytes;
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4) {  // four rows: four bytes of each feature's 16
+      uint32_t lo[4], hi[4], tlo[4], thi[4], b4 = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float y[8];
+        Vec16<uint16_t>::open(v[4 * q4 + i], y);
+        const int byte = exp_byte(over_head(largest(y), w.dh_log2));
+        b4 |= (uint32_t)byte << (8 * i);
+        const uint2 q = quantised(y, byte);
+        lo[i] = q.x;
+        hi[i] = q.y;
+      }
+      bytes[q4] = b4;
+      transpose4(lo, tlo);
+      transpose4(hi, thi);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        out[e][q4] = tlo[e];
+        out[4 + e][q4] = thi[e];
+      }
+    }
+    int at;
+    uint8_t *to = page_of((uint8_t *)w.v_pool, sl, w, &at) + ((((int64_t)h << w.dh_log2) + 8 * c) << w.bs_log2) + at;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) *(u32x4_t *)(to + ((int64_t)e << w.bs_log2)) = out[e];
+    if (c == 0) *(u32x4_t *)(w.v_exp + (((int64_t)(sl >> w.bs_log2) * w.v.heads + h) << w.bs_log2) + at) = bytes;
+  }
+}
+
+// EIGHT: e4m3 pages, T = uint16_t
+template <typename T, bool HALF, bool STREAM, bool EIGHT = false>
 __global__ __launch_bounds__(kRotThreads) void kv_write_kernel(RopeArgs a, WriteArgs w, int heads_per) {
-  constexpr int VEC = 16 / sizeof(T);
+  constexpr int VEC = 16 / sizeof(T), FILL = EIGHT ? 16 : VEC;
   extern __shared__ float2 cs[];
   __shared__ int slot[kMostRows + 1], group[kMostRows + 1];
   const int t = threadIdx.x, lane = t & 63, D = 1 << w.dh_log2, bs = 1 << w.bs_log2;
@@ -278,13 +426,13 @@ __global__ __launch_bounds__(kRotThreads) void kv_write_kernel(RopeArgs a, Write
   const int before = __shfl_up(s, 1, kWave);
   const bool end = mine >= a.rows;
   const uint64_t first = __ballot(s < 0 || before != s - 1 || s % kTileRows == 0 || mine == 0 || end) >> 1;
-  const uint64_t fill = __ballot(s < 0 || before != s - 1 || s % VEC == 0 || mine == 0 || end) >> 1;  // group starts
+  const uint64_t fill = __ballot(s < 0 || before != s - 1 || s % FILL == 0 || mine == 0 || end) >> 1;  // group starts
   const int b0 = __builtin_ctzll(first), b1 = kTileRows + __builtin_ctzll(first >> kTileRows);
   const int r0 = (int)(base + b0), nr = (int)min((int64_t)a.rows, base + b1) - r0;
   if (nr <= 0) return;
   const int h0 = blockIdx.y * heads_per, h1 = min(h0 + heads_per, w.q.heads + 2 * w.k.heads);
   const int me = lane - 1 - b0;  // this lane's row of the tile
-  // groups of rows that fill consecutive slots of VEC aligned ones
+  // groups of rows that fill consecutive slots of FILL aligned ones
   const uint64_t mask = fill >> b0 & ((1ull << nr) - 1);
   const int groups = __popcll(mask);
   if (t < 64 && me >= 0 && me < nr) {
@@ -297,7 +445,9 @@ __global__ __launch_bounds__(kRotThreads) void kv_write_kernel(RopeArgs a, Write
   __syncthreads();
   // V: unit = (head, VEC dims, group), the groups of a segment side by side
   const int g0 = max(h0 - w.q.heads - w.k.heads, 0), g1 = h1 - w.q.heads - w.k.heads;
-  if (g1 > g0) {
+  if constexpr (EIGHT) {
+    if (g1 > g0) write_v_e4m3<STREAM>(w, r0, g0, g1, groups, group, slot);
+  } else if (g1 > g0) {
     const int dgs = D / VEC, units = (g1 - g0) * dgs * groups;
     const float inv = 1.f / groups;
     for (int u = t; u < units; u += kRotThreads) {
@@ -336,7 +486,12 @@ __global__ __launch_bounds__(kRotThreads) void kv_write_kernel(RopeArgs a, Write
       T *out = (T *)w.q.out + (r0 + r) * w.q.out_stride;
       unit.template run<STREAM>(h0 + part, hq1, share, [&](int h) { return q + h * D; }, [&](int h) { return out + h * D; });
     });
-  if (k1 > k0)
+  if constexpr (EIGHT) {
+    if (k1 > k0)
+      write_k_e4m3(a, w, r0, nr, k0, k1, slot, cs, [&](const uint16_t *x, int c, const float2 *row_cs, float (&y)[8]) {
+        return turned_chunk<HALF, STREAM>(x, c, a.R, row_cs, y);
+      });
+  } else if (k1 > k0)
     each_unit<false>(nr, a.per_head, k1 - k0, [&](int r, int j, int part, int share) {
       const int sl = slot[r];
       if (sl < 0) return;
@@ -351,7 +506,7 @@ __global__ __launch_bounds__(kRotThreads) void kv_write_kernel(RopeArgs a, Write
 }
 
 // Rows or strides that 16 bytes do not divide: a feature at a time.
-template <typename T, bool HALF>
+template <typename T, bool HALF, bool EIGHT = false>
 __global__ __launch_bounds__(kRotThreads) void kv_write_any_kernel(RopeArgs a, WriteArgs w, int heads_per) {
   extern __shared__ float2 cs[];
   __shared__ int slot[kTileRows];
@@ -369,6 +524,18 @@ __global__ __launch_bounds__(kRotThreads) void kv_write_any_kernel(RopeArgs a, W
   const int hq1 = min(h1, w.q.heads), k0 = max(h0 - w.q.heads, 0), k1 = min(h1 - w.q.heads, w.k.heads);
   const int g0 = max(h0 - w.q.heads - w.k.heads, 0), g1 = h1 - w.q.heads - w.k.heads;
   int at;
+  if constexpr (EIGHT) {
+    const int lanes_log2 = w.dh_log2 - 3;
+    for (int u = t; g1 > g0 && u < (nr * (g1 - g0)) << lanes_log2; u += kRotThreads) {
+      const int c = u & ((1 << lanes_log2) - 1), hr = u >> lanes_log2, h = g0 + hr / nr, r = hr % nr;
+      const uint16_t *in = (const uint16_t *)w.v.in + (r0 + r) * w.v.in_stride + h * D + 8 * c;
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = bf16_to_f32(in[e]);
+      const int byte = exp_byte(over_head(largest(y), w.dh_log2));
+      if (slot[r] >= 0) store_v_e4m3(w, slot[r], h, c, byte, quantised(y, byte));
+    }
+  } else
   for (int r = 0; r < nr && g1 > g0; ++r) {
     if (slot[r] < 0) continue;
     const T *in = (const T *)w.v.in + (r0 + r) * w.v.in_stride;
@@ -383,7 +550,12 @@ __global__ __launch_bounds__(kRotThreads) void kv_write_any_kernel(RopeArgs a, W
       T *out = (T *)w.q.out + (r0 + r) * w.q.out_stride;
       unit.template run<false>(h0 + part, hq1, share, [&](int h) { return q + h * D; }, [&](int h) { return out + h * D; });
     });
-  if (k1 > k0)
+  if constexpr (EIGHT) {
+    if (k1 > k0)
+      write_k_e4m3(a, w, r0, nr, k0, k1, slot, cs, [&](const uint16_t *x, int c, const float2 *row_cs, float (&y)[8]) {
+        return turned_features<HALF>(x, c, a.R, row_cs, y);
+      });
+  } else if (k1 > k0)
     each_unit<true>(nr, a.per_head, k1 - k0, [&](int r, int j, int part, int share) {
       if (slot[r] < 0) return;
       Unit<T, HALF, 1> unit;
@@ -533,16 +705,16 @@ SM_API sm_status sm_rotary(const void *x, int64_t x_stride, const int32_t *pos, 
   return SM_OK;
 }
 
-template <typename T>
+template <typename T, bool EIGHT = false>
 static void launch_write(const RopeArgs &a, const WriteArgs &w, bool half, bool wide, hipStream_t stream) {
   const int64_t tiles = ((int64_t)a.rows + kTileRows - 1) / kTileRows;
   const int heads = w.q.heads + 2 * w.k.heads, per = heads_per_wg(heads, tiles);
   const dim3 grid((unsigned)tiles, (heads + per - 1) / per);
   const size_t lds = kMostRows * (a.R / 2) * sizeof(float2);
   const bool past = streams(a, 1 << w.dh_log2, sizeof(T), half, heads);
-  const auto kernel = !wide  ? (half ? kv_write_any_kernel<T, true> : kv_write_any_kernel<T, false>)
-                      : past ? (half ? kv_write_kernel<T, true, true> : kv_write_kernel<T, false, true>)
-                             : (half ? kv_write_kernel<T, true, false> : kv_write_kernel<T, false, false>);
+  const auto kernel = !wide  ? (half ? kv_write_any_kernel<T, true, EIGHT> : kv_write_any_kernel<T, false, EIGHT>)
+                      : past ? (half ? kv_write_kernel<T, true, true, EIGHT> : kv_write_kernel<T, false, true, EIGHT>)
+                             : (half ? kv_write_kernel<T, true, false, EIGHT> : kv_write_kernel<T, false, false, EIGHT>);
   hipLaunchKernelGGL(kernel, grid, dim3(kRotThreads), lds, stream, a, w, per);
 }
 
@@ -551,7 +723,7 @@ SM_API sm_status sm_kv_write_rotary(const sm_paged_cache *c, const int32_t *pos,
                                     const void *v, int64_t v_stride, const sm_rope_params *p, void *q_out,
                                     int64_t q_out_stride, hipStream_t stream) {
   CacheArgs ca;
-  if (!cache_ok(c, ca) || rows < 0 || num_q_heads < 0 || num_q_heads > 1024 || c->num_kv_heads > 1024) return SM_EINVAL;
+  if (!cache_ok(c, ca, true) || rows < 0 || num_q_heads < 0 || num_q_heads > 1024 || c->num_kv_heads > 1024) return SM_EINVAL;
   if ((int64_t)c->num_blocks * c->block_size > INT32_MAX || !rope_ok(p, c->head_dim)) return SM_EINVAL;
   const int D = c->head_dim;
   const int64_t kv_width = (int64_t)c->num_kv_heads * D, q_width = (int64_t)num_q_heads * D;
@@ -560,7 +732,9 @@ SM_API sm_status sm_kv_write_rotary(const sm_paged_cache *c, const int32_t *pos,
   if (rows == 0) return SM_OK;
   if (!pos || !slots || !k || !v) return SM_EINVAL;
   if (num_q_heads > 0 && (!q || !q_out || !placed(q, q_stride, q_out, q_out_stride, rows))) return SM_EINVAL;
-  const int es = c->dtype == SM_BF16 ? 2 : 4;
+  const bool eight = c->dtype == SM_E4M3;
+  if (eight && !(aligned(c->k_pool, 0, 16, 1) && aligned(c->v_pool, 0, 16, 1))) return SM_EINVAL;
+  const int es = c->dtype == SM_F32 ? 4 : 2;
   const bool wide = divides(p, D, 16 / es) && aligned(k, k_stride, 16, es) && aligned(v, v_stride, 16, es) &&
                     aligned(c->k_pool, 0, 16, es) && aligned(c->v_pool, 0, 16, es) &&
                     (num_q_heads == 0 || (aligned(q, q_stride, 16, es) && aligned(q_out, q_out_stride, 16, es)));
@@ -572,8 +746,11 @@ SM_API sm_status sm_kv_write_rotary(const sm_paged_cache *c, const int32_t *pos,
     const WriteArgs w{Rows{row_at(q, r, q_stride, es), row_at(q_out, r, q_out_stride, es), q_stride, q_out_stride, num_q_heads},
                       Rows{row_at(k, r, k_stride, es), nullptr, k_stride, 0, hkv},
                       Rows{row_at(v, r, v_stride, es), nullptr, v_stride, 0, hkv},
-                      slots + r, c->k_pool, c->v_pool, c->err, ca.bs_log2, ca.dh_log2, c->num_blocks * c->block_size};
-    if (c->dtype == SM_BF16) launch_write<uint16_t>(a, w, p->layout == SM_ROPE_HALF, wide, stream);
+                      slots + r, c->k_pool, c->v_pool,
+                      eight ? pool_exps((uint8_t *)c->k_pool, c->num_blocks, hkv, c->block_size, D) : nullptr,
+                      eight ? pool_exps((uint8_t *)c->v_pool, c->num_blocks, hkv, c->block_size, D) : nullptr, c->err, ca.bs_log2, ca.dh_log2, c->num_blocks * c->block_size};
+    if (eight) launch_write<uint16_t, true>(a, w, p->layout == SM_ROPE_HALF, wide, stream);
+    else if (c->dtype == SM_BF16) launch_write<uint16_t>(a, w, p->layout == SM_ROPE_HALF, wide, stream);
     else launch_write<float>(a, w, p->layout == SM_ROPE_HALF, wide, stream);
     if (hipGetLastError() != hipSuccess) return SM_EHIP;
   }

@@ -783,7 +783,7 @@ SM_API sm_status sm_match_decode(const sm_rule_table *t, int32_t *state, int max
   if (n == 0) return SM_OK;
   if (!state || !seq_ids || !new_tokens || !k_out || !rule_out) return SM_EINVAL;
   CacheArgs ca = {};
-  if (cache && cache_ok(cache, ca))  // (checked above)
+  if (cache && cache_ok(cache, ca, true))  // (checked above)
     hipLaunchKernelGGL(match_decode_kernel<true>, dim3(1), dim3(kDecThreads), 0, stream, (const i32x4_t *)t->keys,
                        t->ids, (uint32_t)(t->capacity - 1), (i32x4_t *)state, max_seqs, seq_ids, new_tokens, n, k_out,
                        rule_out, t->err, ca);

@@ -19,7 +19,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libspanmerge.so")
 
-SM_F32, SM_BF16 = 0, 1
+SM_F32, SM_BF16, SM_E4M3 = 0, 1, 2
 SM_OK, SM_EINVAL, SM_ERANGE, SM_ENOMEM, SM_EHIP = 0, 1, 2, 3, 4
 ERR_EINVAL, ERR_ERANGE, ERR_ENOMEM = 1, 2, 4
 MAX_REQUESTS = 1024
@@ -39,7 +39,7 @@ EXPORTED = ("sm_status_string", "sm_merge_workspace_bytes", "sm_merge_spans",
             "sm_rules_lookup", "sm_match_prompt_workspace_bytes", "sm_match_prompt",
             "sm_match_decode", "sm_gather_surrogates", "sm_span_dedupe_workspace_bytes", "sm_span_dedupe",
             "sm_kv_project_workspace_bytes", "sm_kv_project", "sm_kv_append_projected",
-            "sm_kv_reserve", "sm_rotary", "sm_kv_write_rotary", "sm_block_norm",
+            "sm_kv_reserve", "sm_rotary", "sm_kv_write_rotary", "sm_kv_read", "sm_block_norm",
             "sm_token_logprobs_workspace_bytes", "sm_token_logprobs")
 
 
@@ -161,6 +161,8 @@ def load(path: str = LIB_PATH):
     L.sm_kv_write_rotary.argtypes = [C.POINTER(PagedCacheDesc), _P, _P, _I, _P, _L, _I, _P, _L, _P, _L,
                                      C.POINTER(RopeParams), _P, _L, _P]
     L.sm_kv_write_rotary.restype = _I
+    L.sm_kv_read.argtypes = [C.POINTER(PagedCacheDesc), _P, _P, _P, _I, _I, _P, _L, _P, _L, _P]
+    L.sm_kv_read.restype = _I
     L.sm_block_norm.argtypes = [_P, _L, _P, _L, _I, _I, C.POINTER(NormParams), _P, _L, _F, C.POINTER(NormParams), _I,
                                 _P, _L, _P, _L, _P]
     L.sm_block_norm.restype = _I
@@ -294,7 +296,11 @@ class PagedCache:
     pools are its own.  kv_reserve (or kv_rollback) moves the shared lengths
     once for all layers and kv_write_rotary fills each layer's pages; the calls
     that append to one cache (kv_append, decode_step and their like) would
-    move them once a layer."""
+    move them once a layer.
+
+    dtype torch.float8_e4m3fn: pages in 8 bits, with an exponent byte for each
+    entry and head (k_exp, v_exp [NB, Hkv, bs]: feature = value * 2^(byte - 127)).
+    kv_write_rotary fills them, kv_read reads them; rows (row_dtype) are bf16."""
 
     def __init__(self, *, dtype: torch.dtype, num_kv_heads: int, head_dim: int,
                  block_size: int, num_blocks: int, max_seqs: int,
@@ -303,8 +309,13 @@ class PagedCache:
         self.dtype = dtype
         self.H, self.D, self.bs = num_kv_heads, head_dim, block_size
         self.num_blocks, self.max_seqs, self.max_blocks = num_blocks, max_seqs, max_blocks_per_seq
-        self.k_pool = torch.zeros((num_blocks, num_kv_heads, block_size, head_dim), dtype=dtype, device=device)
-        self.v_pool = torch.zeros((num_blocks, num_kv_heads, head_dim, block_size), dtype=dtype, device=device)
+        self.row_dtype, self.k_exp, self.v_exp = dtype, None, None
+        shapes = (num_blocks, num_kv_heads, block_size, head_dim), (num_blocks, num_kv_heads, head_dim, block_size)
+        if dtype == torch.float8_e4m3fn:
+            self.row_dtype = torch.bfloat16
+            (self.k_pool, self.k_exp), (self.v_pool, self.v_exp) = (self._eight_bits(s, block_size, device) for s in shapes)
+        else:
+            self.k_pool, self.v_pool = (torch.zeros(s, dtype=dtype, device=device) for s in shapes)
         if tables is not None:
             if ((tables.bs, tables.num_blocks, tables.max_seqs, tables.max_blocks) !=
                     (block_size, num_blocks, max_seqs, max_blocks_per_seq) or free_order is not None
@@ -321,11 +332,18 @@ class PagedCache:
             self.free_stack = order.flip(0).contiguous().to(device)
             self.free_top = torch.tensor([num_blocks], dtype=torch.int32, device=device)
             self.err = torch.zeros(1, dtype=torch.int32, device=device)
-        self.desc = PagedCacheDesc(dtype_code(dtype), num_kv_heads, head_dim, block_size,
+        self.desc = PagedCacheDesc(SM_E4M3 if self.k_exp is not None else dtype_code(dtype), num_kv_heads, head_dim, block_size,
                                    num_blocks, max_seqs, max_blocks_per_seq,
                                    _ptr(self.k_pool), _ptr(self.v_pool), _ptr(self.block_table),
                                    _ptr(self.lengths), _ptr(self.free_stack), _ptr(self.free_top),
                                    _ptr(self.err))
+
+    @staticmethod
+    def _eight_bits(shape, bs: int, device):
+        """A pool of e4m3 values and, behind them in the same memory, its exponent bytes."""
+        values = shape[0] * shape[1] * shape[2] * shape[3]
+        buf = torch.zeros(values + shape[0] * shape[1] * bs, dtype=torch.uint8, device=device)
+        return buf[:values].view(torch.float8_e4m3fn).view(shape), buf[values:].view(shape[0], shape[1], bs)
 
     def error_bits(self) -> int:
         return int(self.err.item())
@@ -609,7 +627,7 @@ def kv_write_rotary(cache: PagedCache, pos, slots, q, k, v, rope: bytes, q_out, 
     cache's pages (-1: not written).  q, q_out [rows, Hq, D] or both None; k, v
     [rows, Hkv, D]; each row contiguous, so the three may be views of one buffer."""
     b = _calls()
-    row_stride, dt, H, D = b.row_stride, cache.dtype, cache.H, cache.D
+    row_stride, dt, H, D = b.row_stride, cache.row_dtype, cache.H, cache.D
     rows = _shape(k, 3, "k")[0]
     sk, sv = row_stride(k, dt, "k", rows, H, D), row_stride(v, dt, "v", rows, H, D)
     b.need(pos, rows, "pos")
@@ -625,6 +643,26 @@ def kv_write_rotary(cache: PagedCache, pos, slots, q, k, v, rope: bytes, q_out, 
     st = b.sm_kv_write_rotary(cache.desc, pos, slots, rows, _rows(q), sq, hq, (k,), sk, (v,), sv, rope, _rows(q_out), so,
                               handle, dev)
     _check(st, "sm_kv_write_rotary")
+
+
+def kv_read(cache: PagedCache, seq_ids, row_offsets, K, V, start=None, stream=None):
+    """Entries start[i], start[i] + 1, ... (None: from 0) of each listed sequence
+    as rows row_offsets[i] .. row_offsets[i + 1] - 1 of K and V [rows, Hkv, D]
+    (the cache's row_dtype; each row contiguous; either may be None)."""
+    b = _calls()
+    n, out = seq_ids.numel(), K if K is not None else V
+    if out is None:
+        raise SpanMergeError("kv_read: neither K nor V")
+    rows = _shape(out, 3, "K" if K is not None else "V")[0]
+    sk = 0 if K is None else b.row_stride(K, cache.row_dtype, "K", rows, cache.H, cache.D)
+    sv = 0 if V is None else b.row_stride(V, cache.row_dtype, "V", rows, cache.H, cache.D)
+    b.need(row_offsets, n + 1, "row_offsets")
+    if start is not None:
+        b.need(start, n, "start")
+    handle, dev = _here(stream)
+    _cache_here(cache, dev)
+    st = b.sm_kv_read(cache.desc, seq_ids, start, row_offsets, n, rows, _rows(K), sk, _rows(V), sv, handle, dev)
+    _check(st, "sm_kv_read")
 
 
 class Norm:
