@@ -144,9 +144,10 @@ typedef struct {
  *   [num_blocks][num_kv_heads][block_size]  b: feature = value x 2^(b - 127)
  * (num_blocks x num_kv_heads x block_size x (head_dim + 1) bytes a pool).
  * Rows going in and out, queries and results are bf16.  sm_kv_write_rotary
- * fills such pages (positions of 0 turn nothing), sm_kv_read reads them, and
- * sm_kv_reserve, sm_kv_rollback and sm_match_decode's crop move their tables.
- * The other calls refuse them.
+ * fills such pages (positions of 0 turn nothing); sm_decode_attention,
+ * sm_prefill_attention and sm_kv_read read them; sm_kv_reserve,
+ * sm_kv_rollback and sm_match_decode's crop move their tables.  The other
+ * calls refuse them.
  */
 typedef struct {
   sm_dtype dtype;
@@ -351,6 +352,8 @@ size_t sm_decode_workspace_bytes(int n, int num_q_heads, int head_dim,
  * partials over chunks of the cache, combined exactly by the last workgroup
  * of each (sequence, kv head) to finish.
  *
+ *  c            (host) any page type; SM_E4M3 pages stand for the features
+ *               above, to all of their bits, and q and out are bf16
  *  seq_ids      [n] ids in [0, max_seqs) (repeats allowed)
  *  q            [n][num_q_heads][head_dim] (cache dtype)
  *  num_q_heads  (host) multiple of num_kv_heads, group size <= 16
@@ -498,9 +501,11 @@ sm_status sm_decode_step_noalloc(const sm_paged_cache *c,
  *  scale        (host) any finite value; 0 gives the mean of V[s, 0..p]
  *  max_rows     (host) upper bound on every m_i; sizes the grid
  *  out          [total_rows][num_q_heads][head_dim], bf16
- * bf16 caches only, head_dim 64 or 128, block_size a power of two >= 16,
- * max_blocks_per_seq <= 4096, one page of all kv heads (num_kv_heads x
- * block_size x head_dim x 2 bytes) < 4 GiB.  No workspace.
+ * bf16 and SM_E4M3 caches only, head_dim 64 or 128, block_size a power of two
+ * >= 16, max_blocks_per_seq <= 4096, one page of all kv heads (num_kv_heads x
+ * block_size x head_dim x 2 bytes) < 4 GiB.  No workspace.  A NaN or an
+ * infinity in V can reach rows up to 256 positions before it, whose weight of
+ * it is 0, as 0 times it.
  * Device errors (into c->err; the request's rows are zero): EINVAL (bad id,
  * bad row range, m_i > L or > max_rows, block id out of range).
  */

@@ -32,8 +32,10 @@
 // tokens 8q .. 8q+7 of the tile for head r.
 #include <atomic>
 #include <mutex>
+#include <type_traits>
 
 #include "common.hpp"
+#include "e4m3.hpp"
 
 namespace sm {
 
@@ -76,6 +78,8 @@ struct DecodeArgs {
   // decode-time merge step only (sm_decode_merge_step): entries cropped
   // from each request's cache before its row is appended, request order
   const int32_t *crop;
+  // e4m3 pages only: the pools' exponent bytes
+  const uint8_t *k_exp, *v_exp;
 };
 
 // Chunking of a sequence of L cached entries: nc non-empty chunks of
@@ -951,12 +955,30 @@ struct KVTile {
   u32x4_t v[DH / 16];   // V^T: 16 dims x 8 tokens per lane
 };
 
+// e4m3 pages: 64 tokens a tile, 16 bytes of 16 features (K) or 16 tokens (V) a
+// lane, so that a tile has as many loads in flight as one of bf16.
+template <int DH>
+struct KVTile8 {
+  u32x4_t k[4][DH / 64];  // K rows of score tile j: token 16 (r >> 2) + 4 j + (r & 3), features 64 cc + 16 q4 .. +15
+  u32x4_t v[DH / 16];     // V^T: 16 dims x 16 tokens per lane
+  u32x4_t ke, ve;         // exponent bytes of the 16 tokens that K's rows, and V's tokens, lie among
+};
+
+// 2^(b - 127) of byte i of a word of exponent bytes
+__device__ __forceinline__ float byte_scale(uint32_t w, int i) {
+  const uint32_t x = i == 3 ? w >> 1 : w << (23 - 8 * i);
+  return __uint_as_float(x & 0x7f800000u);
+}
+
 // ORD: the grid takes the (request, kv head) pairs in length order (see
 // order_pick); a separate instantiation, so that the grid-order kernels
 // carry none of its code.
 // CROP (with STEP): the decode-time merge step; the crops and the append
 // are planned before the streaming loop, since they decide what is read.
-template <int DH, bool STEP, bool ORD, bool CROP = false>
+// EIGHT (without STEP): e4m3 pages.  Their values become bf16 on the way to the
+// matrix cores, K's with their exponents (a lane's K values are of one token);
+// V's exponents go into the probabilities before those are rounded to bf16.
+template <int DH, bool STEP, bool ORD, bool CROP = false, bool EIGHT = false>
 __global__ __launch_bounds__(kDecThreads, 2) void decode_split_bf16(DecodeArgs a) {
   __shared__ int pages[kMaxChunkPages];
   __shared__ int flag;
@@ -1203,13 +1225,14 @@ __global__ __launch_bounds__(kDecThreads, 2) void decode_split_bf16(DecodeArgs a
     const int q4 = lane >> 4;  // k-slot group of the MFMA operands
     const int G = a.G;
 
-    // Q^T operand: lane (r, q4) holds q[head r][32*kk + 8*q4 .. +7]
+    // Q^T operand: lane (r, q4) holds q[head r][32*kk + 8*q4 .. +7] (e4m3
+    // pages: [32*(kk - kk%2) + 8*(kk%2) + 16*q4 .. +7], as K's 16 bytes lie)
     u32x4_t qreg[DH / 32];
     {
-      const uint16_t *qb = (const uint16_t *)a.q + ((int64_t)i * a.Hq + g * G + r) * DH + 8 * q4;
+      const uint16_t *qb = (const uint16_t *)a.q + ((int64_t)i * a.Hq + g * G + r) * DH + (EIGHT ? 16 : 8) * q4;
 #pragma unroll
       for (int kk = 0; kk < DH / 32; ++kk)
-        qreg[kk] = (r < G) ? *(const u32x4_t *)(qb + 32 * kk) : u32x4_t{0u, 0u, 0u, 0u};
+        qreg[kk] = (r < G) ? *(const u32x4_t *)(qb + (EIGHT ? 32 * (kk & ~1) + 8 * (kk & 1) : 32 * kk)) : u32x4_t{0u, 0u, 0u, 0u};
     }
 
     const uint16_t *kp = (const uint16_t *)a.k_pool;
@@ -1218,9 +1241,35 @@ __global__ __launch_bounds__(kDecThreads, 2) void decode_split_bf16(DecodeArgs a
     const int offA = 8 * (r >> 2) + (r & 3);      // token of score-tile A row r
     const int offB = offA + 4;                     // token of score-tile B row r
     const int offV = 8 * q4;                       // first of this lane's 8 tokens
-    const int ntiles = t1p > t0 ? (t1p - t0 + 31) >> 5 : 0;
+    constexpr int TOK = EIGHT ? 64 : 32;           // tokens of a tile
+    const int ntiles = t1p > t0 ? (t1p - t0 + TOK - 1) / TOK : 0;
+    typedef std::conditional_t<EIGHT, KVTile8<DH>, KVTile<DH>> Tile;
 
-    auto load = [&](KVTile<DH> &T, int tile) {
+    auto load8 = [&](KVTile8<DH> &T, int tile) {
+      const int T0 = t0 + 64 * tile;
+      // tokens past the pool range read the chunk's first entries instead
+      const int tK = (T0 + 16 * (r >> 2) < t1p) ? T0 + 16 * (r >> 2) : t0;
+      const int tV = (T0 + 16 * q4 < t1p) ? T0 + 16 * q4 : t0;
+      const int64_t pK = (int64_t)pages[(tK >> bs_log2) - lp0] * a.Hkv + g, pV = (int64_t)pages[(tV >> bs_log2) - lp0] * a.Hkv + g;
+      const int atK = tK & (bs - 1), atV = tV & (bs - 1);
+      const uint8_t *k = (const uint8_t *)a.k_pool + pK * page_elems + (atK + (r & 3)) * DH + 16 * q4;
+      const uint8_t *v = (const uint8_t *)a.v_pool + pV * page_elems + (int64_t)r * bs + atV;
+      T.ke = *(const u32x4_t *)(a.k_exp + pK * bs + atK);
+      T.ve = *(const u32x4_t *)(a.v_exp + pV * bs + atV);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int cc = 0; cc < DH / 64; ++cc)
+          T.k[j][cc] = __builtin_nontemporal_load((const u32x4_t *)(k + 4 * j * DH + 64 * cc));
+#pragma unroll
+      for (int dt = 0; dt < DH / 16; ++dt)
+        T.v[dt] = __builtin_nontemporal_load((const u32x4_t *)(v + (int64_t)16 * dt * bs));
+    };
+    auto load = [&](auto &T, int tile) {
+      if constexpr (EIGHT) {
+        load8(T, tile);
+        return;
+      } else {
       const int T0 = t0 + 32 * tile;
       // tokens past the pool range read the chunk's first entry instead
       // (their scores are masked and their V lanes zeroed below)
@@ -1241,6 +1290,7 @@ __global__ __launch_bounds__(kDecThreads, 2) void decode_split_bf16(DecodeArgs a
 #pragma unroll
       for (int dt = 0; dt < DH / 16; ++dt)
         T.v[dt] = __builtin_nontemporal_load((const u32x4_t *)(pV + (int64_t)16 * dt * bs));
+      }
     };
 
     f32x4_t o[DH / 16];
@@ -1249,7 +1299,76 @@ __global__ __launch_bounds__(kDecThreads, 2) void decode_split_bf16(DecodeArgs a
     float m_run = -INFINITY, l_run = 0.f;
     const float sl2 = a.scale_log2e;
 
-    auto compute = [&](KVTile<DH> &T, int tile) {
+    auto compute8 = [&](KVTile8<DH> &T, int tile) {
+      const int T0 = t0 + 64 * tile;
+      float sc[16];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float scale = __uint_as_float((T.ke[j] >> (8 * (r & 3)) & 0xffu) << 23);
+        f32x4_t x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int cc = 0; cc < DH / 64; ++cc) {
+          const u32x4_t w = T.k[j][cc];
+          x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(e4m3_to_bf16(w[0], w[1], scale)), as_bf16x8(qreg[2 * cc]), x, 0, 0, 0);
+          x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(e4m3_to_bf16(w[2], w[3], scale)), as_bf16x8(qreg[2 * cc + 1]), x, 0, 0, 0);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc[4 * j + e] = x[e];
+      }
+      // lane (r, q4) now holds head r's scores of tokens T0 + 16*q4 + 0..15
+      const int nvalid = min(16, max(0, t1p - (T0 + 16 * q4)));
+      float mx = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        sc[j] = (j < nvalid) ? sc[j] * sl2 : -INFINITY;
+        mx = fmaxf(mx, sc[j]);
+      }
+      {
+        float a, b;
+        swap16(mx, a, b);
+        swap32(fmaxf(a, b), a, b);
+        mx = fmaxf(a, b);
+      }
+      const float m_new = fmaxf(m_run, mx);  // finite: every tile has a valid token
+      const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+      if (nvalid < 16) {  // stale slots past the end may hold anything
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int left = nvalid - 4 * e;
+          const uint32_t keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+          T.ve[e] &= keep;
+#pragma unroll
+          for (int dt = 0; dt < DH / 16; ++dt) T.v[dt][e] &= keep;
+        }
+      }
+      float ps = 0.f;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const float p = __builtin_amdgcn_exp2f(sc[j] - m_new);
+        ps += p;
+        sc[j] = p * byte_scale(T.ve[j >> 2], j & 3);
+      }
+      l_run = l_run * alpha + ps;
+      m_run = m_new;
+#pragma unroll
+      for (int dt = 0; dt < DH / 16; ++dt) o[dt] *= alpha;
+      u32x4_t pp[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        pp[h] = u32x4_t{pack_bf16x2(sc[8 * h], sc[8 * h + 1]), pack_bf16x2(sc[8 * h + 2], sc[8 * h + 3]),
+                        pack_bf16x2(sc[8 * h + 4], sc[8 * h + 5]), pack_bf16x2(sc[8 * h + 6], sc[8 * h + 7])};
+#pragma unroll
+      for (int dt = 0; dt < DH / 16; ++dt)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(e4m3_to_bf16(T.v[dt][2 * h], T.v[dt][2 * h + 1], 1.f)),
+                                                          as_bf16x8(pp[h]), o[dt], 0, 0, 0);
+    };
+    auto compute = [&](auto &T, int tile) {
+      if constexpr (EIGHT) {
+        compute8(T, tile);
+        return;
+      } else {
       const int T0 = t0 + 32 * tile;
       f32x4_t sa = {0.f, 0.f, 0.f, 0.f}, sb = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -1300,11 +1419,12 @@ __global__ __launch_bounds__(kDecThreads, 2) void decode_split_bf16(DecodeArgs a
 #pragma unroll
       for (int dt = 0; dt < DH / 16; ++dt)
         o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(T.v[dt]), as_bf16x8(pp), o[dt], 0, 0, 0);
+      }
     };
 
     // two register buffers, alternating without copies: while one tile is
     // multiplied the next one's 16 loads are in flight
-    KVTile<DH> bufA, bufB;
+    Tile bufA, bufB;
     constexpr int step = kDecWaves;
     if (w < ntiles) load(bufA, w);
     for (int tile = w; tile < ntiles; tile += 2 * step) {
@@ -1621,13 +1741,13 @@ SM_API size_t sm_decode_workspace_bytes(int n, int num_q_heads, int head_dim, in
 // sm_decode_workspace_bytes for these sizes, as documented.
 static sm_status decode_setup(const sm_paged_cache *c, const int32_t *seq_ids, int n, const void *q,
                               int num_q_heads, float scale, int max_len, void *out, void *ws, size_t ws_bytes,
-                              int64_t max_pairs, DecodeArgs &a, bool exact_ws = false) {
+                              int64_t max_pairs, DecodeArgs &a, bool exact_ws = false, bool eight = false) {
   if (!c || n < 0 || max_len < 0) return SM_EINVAL;
   if (n == 0) return SM_OK;
   if (!seq_ids || !q || !out || !ws || !c->k_pool || !c->v_pool || !c->block_table ||
       !c->lengths || !c->err)
     return SM_EINVAL;
-  if (c->dtype != SM_F32 && c->dtype != SM_BF16) return SM_EINVAL;
+  if (c->dtype != SM_F32 && c->dtype != SM_BF16 && !(eight && c->dtype == SM_E4M3)) return SM_EINVAL;
   if (c->head_dim != 64 && c->head_dim != 128) return SM_EINVAL;
   const int bs_log2 = ilog2_exact(c->block_size);
   if (bs_log2 < 4 || bs_log2 > 9) return SM_EINVAL;
@@ -1656,7 +1776,11 @@ static sm_status decode_setup(const sm_paged_cache *c, const int32_t *seq_ids, i
   a.max_seqs = c->max_seqs;
   a.max_blocks = c->max_blocks_per_seq;
   a.max_len = max_len;
-  a.chunk_nominal = (c->dtype == SM_BF16) ? chunk_policy_bf16(n, c->num_kv_heads, max_len)
+  if (c->dtype == SM_E4M3) {
+    a.k_exp = pool_exps((const uint8_t *)c->k_pool, c->num_blocks, c->num_kv_heads, c->block_size, c->head_dim);
+    a.v_exp = pool_exps((const uint8_t *)c->v_pool, c->num_blocks, c->num_kv_heads, c->block_size, c->head_dim);
+  }
+  a.chunk_nominal = (c->dtype != SM_F32) ? chunk_policy_bf16(n, c->num_kv_heads, max_len)
                                           : kF32ChunkTokens;
   a.max_chunks = max_len > 0 ? (max_len + a.chunk_nominal - 1) / a.chunk_nominal : 1;
   a.scale_log2e = scale * kLog2e;
@@ -1684,11 +1808,11 @@ static int device_cus() {
 }
 
 // Workgroups of a bf16 decode kernel resident on one compute unit at once.
-template <int DH, bool STEP, bool CROP>
+template <int DH, bool STEP, bool CROP, bool EIGHT = false>
 static int bf16_occupancy() {
   static const int occ = [] {
     int nb = 0;
-    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&nb, decode_split_bf16<DH, STEP, true, CROP>, kDecThreads, 0) !=
+    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&nb, decode_split_bf16<DH, STEP, true, CROP, EIGHT>, kDecThreads, 0) !=
         hipSuccess)
       nb = 1;
     return nb > 0 ? nb : 1;
@@ -1703,20 +1827,29 @@ static sm_status decode_launch(const sm_paged_cache *c, DecodeArgs a, int n, hip
   // a fused bf16 step adds one grid row: its first workgroup commits the append
   const int rows = n + ((STEP && c->dtype == SM_BF16) ? 1 : 0);
   const dim3 grid(a.max_chunks, c->num_kv_heads, rows);
-  if (c->dtype == SM_BF16 && a.max_chunks == 1 && n <= kDecThreads) {
+  if (c->dtype != SM_F32 && a.max_chunks == 1 && n <= kDecThreads) {
     // more single-chunk pairs than compute units: deal them longest first
     const int cus = device_cus();
     if (cus > 0 && (int64_t)n * c->num_kv_heads > cus) {
       a.order_n = n;
       a.order_cus = cus;
       const bool d128 = c->head_dim == 128;
-      if (STEP && a.crop)
+      if (c->dtype == SM_E4M3)
+        a.order_occ = d128 ? bf16_occupancy<128, false, false, true>() : bf16_occupancy<64, false, false, true>();
+      else if (STEP && a.crop)
         a.order_occ = d128 ? bf16_occupancy<128, STEP, STEP>() : bf16_occupancy<64, STEP, STEP>();
       else
         a.order_occ = d128 ? bf16_occupancy<128, STEP, false>() : bf16_occupancy<64, STEP, false>();
     }
   }
-  if (c->dtype == SM_BF16 && STEP && a.crop) {
+  if (c->dtype == SM_E4M3) {  // (never a step)
+    const bool ord = a.order_n > 0;
+    const auto kernel = c->head_dim == 128 ? (ord ? decode_split_bf16<128, false, true, false, true>
+                                                  : decode_split_bf16<128, false, false, false, true>)
+                                           : (ord ? decode_split_bf16<64, false, true, false, true>
+                                                  : decode_split_bf16<64, false, false, false, true>);
+    hipLaunchKernelGGL(kernel, grid, dim3(kDecThreads), 0, stream, a);
+  } else if (c->dtype == SM_BF16 && STEP && a.crop) {
     const bool ord = a.order_n > 0;
     if (c->head_dim == 128) {
       if (ord)
@@ -1756,7 +1889,7 @@ SM_API sm_status sm_decode_attention(const sm_paged_cache *c, const int32_t *seq
                                      void *out, void *ws, size_t ws_bytes, hipStream_t stream) {
   DecodeArgs a;
   const sm_status st = decode_setup(c, seq_ids, n, q, num_q_heads, scale, max_len, out, ws, ws_bytes,
-                                    kMaxPairs, a);
+                                    kMaxPairs, a, false, true);
   if (st != SM_OK || n == 0) return st;
   return decode_launch<false>(c, a, n, stream);
 }

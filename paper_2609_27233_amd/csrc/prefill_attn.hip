@@ -30,8 +30,16 @@
 // (a running maximum) moved only when a tile's maximum exceeds it by more
 // than 2^8.  Any reference gives the same ratios; keeping it mostly fixed
 // skips the rescale of the accumulators on almost every tile.
+//
+// e4m3 pages (EIGHT): 16 bytes of a page are 16 features of an entry (K) or 16
+// entries of a feature (V).  They become bf16 on the way to LDS, K with its
+// exponents, V without: those go into the probabilities before they are
+// rounded, as floats that a tile's buffer holds beside its rows.
 #include "common.hpp"
+#include "e4m3.hpp"
 #include "prefill_plan.hpp"
+
+#include <type_traits>
 
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
@@ -51,8 +59,9 @@ constexpr int kPfMaxPages = 4096;
 constexpr float kPfLog2e = 1.4426950408889634f;
 
 struct PrefillArgs {
-  const uint16_t *k_pool;
-  const uint16_t *v_pool;
+  const void *k_pool;
+  const void *v_pool;
+  const uint8_t *k_exp, *v_exp;  // e4m3 pages
   const int32_t *block_table;
   const int32_t *lengths;
   const int32_t *seq_ids;
@@ -117,15 +126,15 @@ __device__ __forceinline__ PfBlock pf_block(const PrefillArgs &a) {
 
 // LDS of a workgroup: the ring of K and V buffers, which the merge of the wave
 // groups uses again, then the page ids and a flag.
-template <int DH, int KS>
+template <int DH, int KS, bool EIGHT = false>
 constexpr int pf_lds_bytes() {
   const int keys = KS == 4 ? 32 : 64, vp = keys == 32 ? 32 : keys + 8;
-  const int ring = 4 * (KS * keys * (DH + 8) + KS * DH * vp);
+  const int ring = 4 * (KS * keys * (DH + 8) + KS * DH * vp) + (EIGHT ? 8 * KS * keys : 0);
   const int merge = KS > 1 ? (kPfWaves * 32 * (DH + 4) + kPfWaves * 64) * 4 : 0;
   return (ring > merge ? ring : merge) + kPfMaxPages * 4 + 16;
 }
 
-template <int DH, int KS>
+template <int DH, int KS, bool EIGHT = false>
 __device__ __forceinline__ void prefill_body(const PrefillArgs &a, const PfBlock &wg, uint8_t *lds) {
   constexpr int KEYS = KS == 4 ? 32 : 64;  // keys per tile
   constexpr int SUB = KEYS / 32;           // 32-key score blocks per tile
@@ -140,19 +149,21 @@ __device__ __forceinline__ void prefill_body(const PrefillArgs &a, const PfBlock
   auto v_at = [](int row, int chunk) { return row * VP + 8 * (KEYS == 32 ? chunk ^ ((row >> 2) & 3) : chunk); };
   constexpr int NKS = DH / 16;      // k steps of S^T
   constexpr int NRB = DH / 32;      // 32-dim row blocks of O^T
-  constexpr int KCH = DH / 8;       // 16-byte chunks of a K row
-  constexpr int VCH = KEYS / 8;     // 16-byte chunks of a V row (one dim) in a tile
+  constexpr int PER = EIGHT ? 16 : 8;  // values of 16 bytes of a page
+  constexpr int KCH = DH / PER;     // 16-byte chunks of a K row
+  constexpr int VCH = KEYS / PER;   // 16-byte chunks of a V row (one dim) in a tile
   constexpr int KTOT = SPAN * KCH, VTOT = KS * DH * VCH;  // 16-byte chunks per pass
   constexpr int KU = (KTOT + kPfThreads - 1) / kPfThreads;  // K chunks per thread and tile
   constexpr int VU = (VTOT + kPfThreads - 1) / kPfThreads;  // V chunks per thread and tile
   constexpr int KBUF = SPAN * KP, VBUF = KS * DH * VP;  // elements of one buffer
-  constexpr int RING = 2 * (KBUF + VBUF) * 2;
+  constexpr int RING = 2 * (KBUF + VBUF) * 2 + (EIGHT ? 2 * SPAN * 4 : 0);
   constexpr int OPITCH = DH + 4;                        // floats of one vector's outputs in the merge of the groups
   constexpr int MERGE = KS > 1 ? (kPfWaves * 32 * OPITCH + kPfWaves * 64) * 4 : 0;
   constexpr int PAGES = RING > MERGE ? RING : MERGE;
-  static_assert(PAGES + kPfMaxPages * 4 + 16 == pf_lds_bytes<DH, KS>(), "LDS of the workgroup");
+  static_assert(PAGES + kPfMaxPages * 4 + 16 == pf_lds_bytes<DH, KS, EIGHT>(), "LDS of the workgroup");
   int *pages = (int *)(lds + PAGES), *bad_flag = pages + kPfMaxPages;
   uint16_t *k_lds = (uint16_t *)lds, *v_lds = k_lds + 2 * KBUF;  // [2][KBUF], [2][KS][DH * VP]
+  float *vs_lds = (float *)(v_lds + 2 * VBUF);  // e4m3: [2][SPAN] scales of V's entries
 
   const int g = wg.g, qb = wg.qb, r0 = wg.r0, m = wg.m, s = wg.s, L = wg.L;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
@@ -228,34 +239,44 @@ __device__ __forceinline__ void prefill_body(const PrefillArgs &a, const PfBlock
   // A chunk's offset within its page is fixed per thread; a tile adds a
   // uniform (t0 mod bs) and its page id.  Tokens past kend re-read page 0.
   const uint64_t page_bytes = a.page_bytes;
-  const char *kbase = (const char *)a.k_pool + (int64_t)g * bs * DH * 2;
-  const char *vbase = (const char *)a.v_pool + (int64_t)g * bs * DH * 2;
+  constexpr int ES = EIGHT ? 1 : 2;  // bytes of a value
+  const char *kbase = (const char *)a.k_pool + (int64_t)g * bs * DH * ES;
+  const char *vbase = (const char *)a.v_pool + (int64_t)g * bs * DH * ES;
+  const uint32_t exp_page = (uint32_t)a.Hkv * bs;  // exponent bytes of a page
+  const uint8_t *kebase = a.k_exp + g * bs, *vebase = a.v_exp + g * bs;
   int ktk[KU], koff[KU], vtk[VU], voff[VU];
 #pragma unroll
   for (int u = 0; u < KU; ++u) {
     const int id = min(tid + kPfThreads * u, KTOT - 1);
     ktk[u] = id / KCH;
-    koff[u] = ((ktk[u] & (bs - 1)) * DH + (id % KCH) * 8) * 2;
+    koff[u] = ((ktk[u] & (bs - 1)) * DH + (id % KCH) * PER) * ES;
   }
 #pragma unroll
   for (int u = 0; u < VU; ++u) {
     const int id = min(tid + kPfThreads * u, VTOT - 1);
-    vtk[u] = id / (DH * VCH) * KEYS + 8 * (id % VCH);
-    voff[u] = (id / VCH % DH * bs + (vtk[u] & (bs - 1))) * 2;
+    vtk[u] = id / (DH * VCH) * KEYS + PER * (id % VCH);
+    voff[u] = (id / VCH % DH * bs + (vtk[u] & (bs - 1))) * ES;
   }
-  auto fetch = [&](int t0, u32x4_t (&kv)[KU + VU]) {
+  // e4m3: exponent bytes of this thread's K chunks, and of entry tid's V
+  struct Exps { int k[EIGHT ? KU : 1], v; };
+  auto fetch = [&](int t0, u32x4_t (&kv)[KU + VU], Exps &ex) {
     const int tin = t0 & (bs - 1);  // 0 when a page is no longer than a pass
 #pragma unroll
     for (int u = 0; u < KU; ++u) {
       const int tok = t0 + ktk[u];
       const uint32_t blk = pages[tok < kend ? tok >> bs_log2 : 0];
-      kv[u] = *(const u32x4_t *)(kbase + blk * page_bytes + (koff[u] + tin * DH * 2));
+      kv[u] = *(const u32x4_t *)(kbase + blk * page_bytes + (koff[u] + tin * DH * ES));
+      if constexpr (EIGHT) ex.k[u] = kebase[(uint64_t)blk * exp_page + (ktk[u] & (bs - 1)) + tin];
+    }
+    if constexpr (EIGHT) {
+      const int tok = t0 + tid;
+      ex.v = tid < SPAN && tok < kend ? vebase[(uint64_t)pages[tok >> bs_log2] * exp_page + (tok & (bs - 1))] : 0;
     }
 #pragma unroll
     for (int u = 0; u < VU; ++u) {
       const int tok = t0 + vtk[u];
       const uint32_t blk = pages[tok < kend ? tok >> bs_log2 : 0];
-      kv[KU + u] = *(const u32x4_t *)(vbase + blk * page_bytes + (voff[u] + tin * 2));
+      kv[KU + u] = *(const u32x4_t *)(vbase + blk * page_bytes + (voff[u] + tin * ES));
     }
     if (t0 + SPAN > L) {  // the last tile: V entries past the length may hold anything
 #pragma unroll
@@ -263,13 +284,40 @@ __device__ __forceinline__ void prefill_body(const PrefillArgs &a, const PfBlock
         const int nvalid = L - (t0 + vtk[u]);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          if (2 * e >= nvalid) kv[KU + u][e] = 0u;
-          else if (2 * e + 1 >= nvalid) kv[KU + u][e] &= 0xffffu;
+          if constexpr (EIGHT) {
+            const int left = nvalid - 4 * e;
+            kv[KU + u][e] &= left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+          } else {
+            if (2 * e >= nvalid) kv[KU + u][e] = 0u;
+            else if (2 * e + 1 >= nvalid) kv[KU + u][e] &= 0xffffu;
+          }
         }
       }
     }
   };
-  auto stash = [&](int buf, const u32x4_t (&kv)[KU + VU]) {
+  auto stash = [&](int buf, const u32x4_t (&kv)[KU + VU], const Exps &ex) {
+    if constexpr (EIGHT) {
+#pragma unroll
+      for (int u = 0; u < KU; ++u) {
+        const int id = tid + kPfThreads * u;
+        const float scale = exp_scale(ex.k[u]);
+        uint16_t *to = &k_lds[buf * KBUF + (id / KCH) * KP + (id % KCH) * 16];
+        if (KTOT % kPfThreads == 0 || id < KTOT) {
+          *(u32x4_t *)to = e4m3_to_bf16(kv[u][0], kv[u][1], scale);
+          *(u32x4_t *)(to + 8) = e4m3_to_bf16(kv[u][2], kv[u][3], scale);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < VU; ++u) {
+        const int id = tid + kPfThreads * u, row = id / VCH, chunk = id % VCH * 2;
+        if (VTOT % kPfThreads == 0 || id < VTOT) {
+          *(u32x4_t *)(&v_lds[buf * VBUF + v_at(row, chunk)]) = e4m3_to_bf16(kv[KU + u][0], kv[KU + u][1], 1.f);
+          *(u32x4_t *)(&v_lds[buf * VBUF + v_at(row, chunk + 1)]) = e4m3_to_bf16(kv[KU + u][2], kv[KU + u][3], 1.f);
+        }
+      }
+      if (tid < SPAN) vs_lds[buf * SPAN + tid] = exp_scale(ex.v);  // (an entry past the end: 0)
+      return;
+    }
 #pragma unroll
     for (int u = 0; u < KU; ++u) {
       const int id = tid + kPfThreads * u;
@@ -293,12 +341,13 @@ __device__ __forceinline__ void prefill_body(const PrefillArgs &a, const PfBlock
 
   const int ntiles = (kend + SPAN - 1) / SPAN;
   u32x4_t stage[KU + VU];
-  fetch(0, stage);
-  stash(0, stage);
+  Exps exps;
+  fetch(0, stage, exps);
+  stash(0, stage, exps);
   __syncthreads();
   for (int t = 0; t < ntiles; ++t) {
     const int buf = t & 1, t0 = t * SPAN + kg * KEYS;  // this group's tile
-    if (t + 1 < ntiles) fetch((t + 1) * SPAN, stage);  // in flight during this pass
+    if (t + 1 < ntiles) fetch((t + 1) * SPAN, stage, exps);  // in flight during this pass
 
     if (t0 <= wave_hi) {
       // S^T = K . Q^T, one 32-key block at a time: its fragment reads first,
@@ -376,6 +425,18 @@ __device__ __forceinline__ void prefill_body(const PrefillArgs &a, const PfBlock
           sc[sb][r] = __builtin_amdgcn_exp2f(fmaf(sc[sb][r], sl2, -mb));
           ps += sc[sb][r];
         }
+        if constexpr (EIGHT) {  // V's exponents: register 8 kst + i is entry 16 kst + 8 h2 + i of the block
+#pragma unroll
+          for (int kst = 0; kst < 2; ++kst) {
+            const float *vs = &vs_lds[buf * SPAN + kg * KEYS + 32 * sb + 16 * kst + 8 * h2];
+            const f32x4_t s0 = *(const f32x4_t *)vs, s1 = *(const f32x4_t *)(vs + 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              sc[sb][8 * kst + i] *= s0[i];
+              sc[sb][8 * kst + 4 + i] *= s1[i];
+            }
+          }
+        }
         const f32x16_t &x = sc[sb];
 #pragma unroll
         for (int kst = 0; kst < 2; ++kst)
@@ -402,7 +463,7 @@ __device__ __forceinline__ void prefill_body(const PrefillArgs &a, const PfBlock
       }
     }
 
-    if (t + 1 < ntiles) stash(buf ^ 1, stage);
+    if (t + 1 < ntiles) stash(buf ^ 1, stage, exps);
     __syncthreads();
   }
 
@@ -465,10 +526,10 @@ __device__ __forceinline__ void prefill_body(const PrefillArgs &a, const PfBlock
                                                      cvt_bf16x2(o[rb][4 * gg + 2] * inv, o[rb][4 * gg + 3] * inv));
 }
 
-template <int DH, int KS>
+template <int DH, int KS, bool EIGHT = false>
 __global__ __launch_bounds__(kPfThreads, 2) void prefill_bf16(PrefillArgs a) {
-  __shared__ __attribute__((aligned(16))) uint8_t lds[pf_lds_bytes<DH, KS>()];
-  prefill_body<DH, KS>(a, pf_block(a), lds);
+  __shared__ __attribute__((aligned(16))) uint8_t lds[pf_lds_bytes<DH, KS, EIGHT>()];
+  prefill_body<DH, KS, EIGHT>(a, pf_block(a), lds);
 }
 
 // For calls of few rows: blocks of KS = 4, but a request of up to kPfFewKeys
@@ -480,13 +541,13 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_bf16(PrefillArgs a) {
 // 6.9, 7.1; 301 7.6, 7.7; 401 9.3, 8.8.
 constexpr int kPfFewKeys = 320;
 
-template <int DH>
+template <int DH, bool EIGHT = false>
 __global__ __launch_bounds__(kPfThreads, 2) void prefill_few_bf16(PrefillArgs a) {
-  __shared__ __attribute__((aligned(16))) uint8_t lds[pf_lds_bytes<DH, 4>()];
-  static_assert(pf_lds_bytes<DH, 1>() <= pf_lds_bytes<DH, 4>(), "one LDS for both");
+  __shared__ __attribute__((aligned(16))) uint8_t lds[pf_lds_bytes<DH, 4, EIGHT>()];
+  static_assert(pf_lds_bytes<DH, 1, EIGHT>() <= pf_lds_bytes<DH, 4, EIGHT>(), "one LDS for both");
   const PfBlock wg = pf_block(a);
-  if (wg.L <= kPfFewKeys) prefill_body<DH, 1>(a, wg, lds);
-  else prefill_body<DH, 4>(a, wg, lds);
+  if (wg.L <= kPfFewKeys) prefill_body<DH, 1, EIGHT>(a, wg, lds);
+  else prefill_body<DH, 4, EIGHT>(a, wg, lds);
 }
 
 }  // namespace sm
@@ -501,7 +562,8 @@ SM_API sm_status sm_prefill_attention(const sm_paged_cache *c, const int32_t *se
   if (!seq_ids || !q_offsets || !q || !out || !c->k_pool || !c->v_pool || !c->block_table || !c->lengths ||
       !c->err)
     return SM_EINVAL;
-  if (c->dtype != SM_BF16 || !(fabsf(scale) <= 3.0e38f)) return SM_EINVAL;  // a finite scale
+  const bool eight = c->dtype == SM_E4M3;
+  if ((c->dtype != SM_BF16 && !eight) || !(fabsf(scale) <= 3.0e38f)) return SM_EINVAL;  // a finite scale
   const int H = c->num_kv_heads, D = c->head_dim, bs = c->block_size;
   if (H <= 0 || num_q_heads <= 0 || num_q_heads % H != 0) return SM_EINVAL;
   const int G = num_q_heads / H;
@@ -511,8 +573,10 @@ SM_API sm_status sm_prefill_attention(const sm_paged_cache *c, const int32_t *se
     return SM_EINVAL;
   if (n > 65535 || (uint64_t)H * bs * D * 2 > 0xffffffffull) return SM_EINVAL;
   PrefillArgs a;
-  a.k_pool = (const uint16_t *)c->k_pool;
-  a.v_pool = (const uint16_t *)c->v_pool;
+  a.k_pool = c->k_pool;
+  a.v_pool = c->v_pool;
+  a.k_exp = eight ? pool_exps((const uint8_t *)c->k_pool, c->num_blocks, H, bs, D) : nullptr;
+  a.v_exp = eight ? pool_exps((const uint8_t *)c->v_pool, c->num_blocks, H, bs, D) : nullptr;
   a.block_table = c->block_table;
   a.lengths = c->lengths;
   a.seq_ids = seq_ids;
@@ -535,7 +599,7 @@ SM_API sm_status sm_prefill_attention(const sm_paged_cache *c, const int32_t *se
   a.num_blocks = c->num_blocks;
   a.max_seqs = c->max_seqs;
   a.max_blocks = c->max_blocks_per_seq;
-  a.page_bytes = (uint32_t)((uint64_t)H * bs * D * 2);
+  a.page_bytes = (uint32_t)((uint64_t)H * bs * D * (eight ? 1 : 2));
   // A positive multiplier keeps exp2(-inf) = 0 for masked keys.  Below 1e-30
   // every weight rounds to 1 in fp32 either way (|q . k| stays far below 1e30).
   a.scale_log2e = fmaxf(fabsf(scale) * kPfLog2e, 1e-30f);
@@ -544,10 +608,18 @@ SM_API sm_status sm_prefill_attention(const sm_paged_cache *c, const int32_t *se
   if ((int64_t)nqb * n * H > 0x7fffffff) return SM_EINVAL;
   a.nqb = nqb;
   const dim3 grid(nqb * n * H);
-  const auto kernel = D == 128 ? (plan.few ? prefill_few_bf16<128> : ks == 4 ? prefill_bf16<128, 4>
-                                  : ks == 2 ? prefill_bf16<128, 2> : prefill_bf16<128, 1>)
-                               : (plan.few ? prefill_few_bf16<64> : ks == 4 ? prefill_bf16<64, 4>
-                                  : ks == 2 ? prefill_bf16<64, 2> : prefill_bf16<64, 1>);
-  hipLaunchKernelGGL(kernel, grid, dim3(kPfThreads), 0, stream, a);
+  const auto kernel = [&](auto dh, auto e) {
+    constexpr int DH = decltype(dh)::value;
+    constexpr bool EIGHT = decltype(e)::value;
+    return plan.few  ? prefill_few_bf16<DH, EIGHT>
+           : ks == 4 ? prefill_bf16<DH, 4, EIGHT>
+           : ks == 2 ? prefill_bf16<DH, 2, EIGHT>
+                     : prefill_bf16<DH, 1, EIGHT>;
+  };
+  const std::integral_constant<int, 128> d128{};
+  const std::integral_constant<int, 64> d64{};
+  const auto chosen = D == 128 ? (eight ? kernel(d128, std::true_type()) : kernel(d128, std::false_type()))
+                               : (eight ? kernel(d64, std::true_type()) : kernel(d64, std::false_type()));
+  hipLaunchKernelGGL(chosen, grid, dim3(kPfThreads), 0, stream, a);
   return hipGetLastError() == hipSuccess ? SM_OK : SM_EHIP;
 }

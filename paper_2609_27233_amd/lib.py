@@ -300,7 +300,8 @@ class PagedCache:
 
     dtype torch.float8_e4m3fn: pages in 8 bits, with an exponent byte for each
     entry and head (k_exp, v_exp [NB, Hkv, bs]: feature = value * 2^(byte - 127)).
-    kv_write_rotary fills them, kv_read reads them; rows (row_dtype) are bf16."""
+    kv_write_rotary fills them; decode_attention, prefill_attention and kv_read
+    read them; rows, queries and results (row_dtype) are bf16."""
 
     def __init__(self, *, dtype: torch.dtype, num_kv_heads: int, head_dim: int,
                  block_size: int, num_blocks: int, max_seqs: int,
@@ -368,9 +369,16 @@ def decode_workspace_bytes(n: int, num_q_heads: int, head_dim: int, max_len: int
     return load().sm_decode_workspace_bytes(n, num_q_heads, head_dim, max_len)
 
 
+def _row_types(cache: PagedCache, q, out):
+    """Queries and results of 8-bit pages are bf16 (other pages': their own type)."""
+    if cache.k_exp is not None and not q.dtype == out.dtype == cache.row_dtype:
+        raise SpanMergeError(f"q, out: expected {cache.row_dtype}, got {q.dtype} and {out.dtype}")
+
+
 def decode_attention(cache: PagedCache, seq_ids, q, out, ws, max_len: int,
                      scale: Optional[float] = None, stream=None):
     n, Hq, D = q.shape
+    _row_types(cache, q, out)
     sc = D ** -0.5 if scale is None else scale
     st = _calls().sm_decode_attention(cache.desc, seq_ids, n, q, Hq, sc, max_len, out, ws, ws.nbytes, _stream(stream))
     _check(st, "sm_decode_attention")
@@ -416,6 +424,7 @@ def prefill_attention(cache: PagedCache, seq_ids, q_offsets, q, out, max_rows: i
     """Causal attention of each request's last m_i cached positions:
     q, out [rows, Hq, D] bf16; q_offsets [n + 1] int32 row ranges."""
     rows, Hq, D = q.shape
+    _row_types(cache, q, out)
     sc = D ** -0.5 if scale is None else scale
     st = _calls().sm_prefill_attention(cache.desc, seq_ids, seq_ids.numel(), q_offsets, rows, q, Hq, sc, max_rows,
                                        out, _stream(stream))
