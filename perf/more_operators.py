@@ -275,6 +275,11 @@ def prepare(case, seed):
 # --------------------------------------------------------------------------
 # the framework's calls
 
+def _bound(s, name):
+    """A bound on lengths that no sequence of the cache passes."""
+    return min(s[name], s["cache"].max_blocks * s["bs"])
+
+
 def _run_own(s):
     from paper_2609_27233_amd import lib as sm
     if s["kind"] == "write":
@@ -284,14 +289,14 @@ def _run_own(s):
         sm.kv_read(s["cache"], s["ids"], s["offs"], s["K"], s["V"], start=s["start"])
         return dict(K=s["K"], V=s["V"])
     if s["kind"] == "decode":
-        sm.decode_attention(s["cache"], s["ids"], s["q"], s["out"], s["ws"], s["max_len"])
+        sm.decode_attention(s["cache"], s["ids"], s["q"], s["out"], s["ws"], _bound(s, "max_len"))
         return s["out"]
     if s["kind"] == "prefill":
         sm.prefill_attention(s["cache"], s["ids"], s["offs"], s["q"], s["out"], s["max_rows"])
         return s["out"]
     if s["kind"] == "shared":
-        sm.decode_attention_shared(s["cache"], s["ids"], s["prefixes"], s["groups"], s["q"], s["out"], s["ws"], s["max_len"],
-                                   s["max_prefix"])
+        sm.decode_attention_shared(s["cache"], s["ids"], s["prefixes"], s["groups"], s["q"], s["out"], s["ws"], _bound(s, "max_len"),
+                                   _bound(s, "max_prefix"))
         return s["out"]
     sm.sample_tokens(s["x"], s["u"], s["tokens"], s["ws"], temperature=s["temperature"], top_k=s["top_k"], top_p=s["top_p"],
                      min_p=s["min_p"], logprob=s["logprob"])
