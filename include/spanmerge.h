@@ -18,6 +18,7 @@
  *   sm_kv_rollback      crop k entries from the tail of each listed sequence
  *   sm_kv_append        append K/V rows (one surrogate state, or a prompt)
  *   sm_decode_attention one query per sequence over its whole paged cache
+ *   sm_decode_attention_shared the same behind entries that a group shares
  *   sm_prefill_attention causal attention of a prompt's positions over the
  *                       paged cache (the prefill pass over the compressed
  *                       sequence)
@@ -145,9 +146,9 @@ typedef struct {
  * (num_blocks x num_kv_heads x block_size x (head_dim + 1) bytes a pool).
  * Rows going in and out, queries and results are bf16.  sm_kv_write_rotary
  * fills such pages (positions of 0 turn nothing); sm_decode_attention,
- * sm_prefill_attention and sm_kv_read read them; sm_kv_reserve,
- * sm_kv_rollback and sm_match_decode's crop move their tables.  The other
- * calls refuse them.
+ * sm_decode_attention_shared, sm_prefill_attention and sm_kv_read read them;
+ * sm_kv_reserve, sm_kv_rollback and sm_match_decode's crop move their tables.
+ * The other calls refuse them.
  */
 typedef struct {
   sm_dtype dtype;
@@ -372,6 +373,51 @@ sm_status sm_decode_attention(const sm_paged_cache *c, const int32_t *seq_ids,
                               int n, const void *q, int num_q_heads,
                               float scale, int max_len, void *out, void *ws,
                               size_t ws_bytes, hipStream_t stream);
+
+/* Bytes of workspace sm_decode_attention_shared needs for these sizes. */
+size_t sm_decode_shared_workspace_bytes(int n, int num_q_heads, int head_dim,
+                                        int max_len, int max_prefix);
+
+/*
+ * sm_decode_attention_shared -- sm_decode_attention for requests whose first
+ * entries are the same (a system prompt, a document that many ask about): a
+ * group's prefix is cached once, as a sequence of its own, and read once for
+ * all of its requests.  Request i of group p attends over the entries of
+ * sequence prefix_ids[p], then over those of its own sequence:
+ *
+ *   out[i, h] = sum_j softmax_j(scale * q[i, h] . K[j, g]) V[j, g],
+ *   j over lengths[prefix_ids[p]] + lengths[seq_ids[i]] entries
+ *
+ * (K is cached turned, so a sequence's own positions start past its prefix:
+ * add the prefix's length to the positions that sm_kv_reserve gives, before
+ * sm_kv_write_rotary.)  Nothing at all to attend to gives zeros.  Two
+ * launches; the result does not depend on the order in which work is done.
+ *
+ *  c              (host) bf16 or SM_E4M3 pages, as sm_prefill_attention
+ *  seq_ids, n, q, num_q_heads, max_len, out: as sm_decode_attention; the
+ *                 lengths count a sequence's own entries, which may be none
+ *  prefix_ids     [num_groups] ids in [0, max_seqs) (repeats allowed), or -1
+ *                 for a group without a prefix
+ *  group_offsets  [num_groups + 1] group p's requests are
+ *                 [group_offsets[p], group_offsets[p+1]) of the list;
+ *                 group_offsets[0] = 0, group_offsets[num_groups] = n
+ *  num_groups     (host) 1 to 65535
+ *  scale          (host) finite
+ *  max_prefix     (host) upper bound on the prefixes' lengths; sizes the grid
+ *  ws, ws_bytes   at least sm_decode_shared_workspace_bytes(...); its first
+ *                 256 KiB as sm_decode_attention's, which it can serve too
+ * Device errors (into c->err; the affected requests' rows are zero): EINVAL
+ * (bad id or block id; group offsets out of order: every row), ERANGE (length
+ * > max_len, prefix > max_prefix).
+ */
+sm_status sm_decode_attention_shared(const sm_paged_cache *c,
+                                     const int32_t *seq_ids, int n,
+                                     const int32_t *prefix_ids,
+                                     const int32_t *group_offsets,
+                                     int num_groups, const void *q,
+                                     int num_q_heads, float scale, int max_len,
+                                     int max_prefix, void *out, void *ws,
+                                     size_t ws_bytes, hipStream_t stream);
 
 /*
  * sm_decode_step -- one decode step of a batch in a single launch: the new

@@ -36,6 +36,7 @@
 
 #include "common.hpp"
 #include "e4m3.hpp"
+#include "shared_prefix.hpp"
 
 namespace sm {
 
@@ -80,6 +81,8 @@ struct DecodeArgs {
   const int32_t *crop;
   // e4m3 pages only: the pools' exponent bytes
   const uint8_t *k_exp, *v_exp;
+  // sm_decode_attention_shared only: the requests' shares over their prefixes
+  PrefixParts prefix;
 };
 
 // Chunking of a sequence of L cached entries: nc non-empty chunks of
@@ -214,6 +217,46 @@ __device__ void write_zero_rows(const DecodeArgs &a, int i, int g, int DH, int s
   if (st != 0 && threadIdx.x == 0 && esink) set_err(esink, st);  // (no sink: reported elsewhere)
 }
 
+// sm_decode_attention_shared: the parts that request i's query head hq has of
+// its group's prefix (written by the launch before this one), joined to
+// dimension dd of what it has of its own entries.
+constexpr int kPrefixBatch = 4;
+template <int DH>
+__device__ __forceinline__ void join_prefix(const DecodeArgs &a, int i, int hq, int dd, float &M, float &acc, float &ls, bool &bad) {
+  const PrefixParts &p = a.prefix;
+  const int64_t base = ((int64_t)i * a.Hq + hq) * p.chunks;
+  if (p.chunks > 0 && *p.flag) bad = true;
+  for (int c0 = 0; c0 < p.chunks; c0 += kPrefixBatch) {
+    float pm[kPrefixBatch], pl[kPrefixBatch], po[kPrefixBatch];
+#pragma unroll
+    for (int c = 0; c < kPrefixBatch; ++c) {
+      const bool there = c0 + c < p.chunks;
+      const int64_t at = base + min(c0 + c, p.chunks - 1);
+      pm[c] = p.ml[2 * at];
+      pl[c] = there ? p.ml[2 * at + 1] : 0.f;
+      po[c] = p.o[at * DH + dd];
+    }
+#pragma unroll
+    for (int c = 0; c < kPrefixBatch; ++c) {
+      bad |= pl[c] < 0.f;
+      if (pl[c] == 0.f) continue;  // no entries (its output is not written); a NaN goes on
+      const float Mb = fmaxf(M, pm[c]);
+      const float f = M == -INFINITY ? 0.f : exp2f(M - Mb), fc = pm[c] == -INFINITY ? 0.f : exp2f(pm[c] - Mb);
+      acc = acc * f + po[c] * fc;
+      ls = ls * f + pl[c] * fc;
+      M = Mb;
+    }
+  }
+}
+
+// A row's result.  A NaN among its scores is its result over e4m3 pages and
+// behind a shared prefix; over bf16 pages alone such a row is zero.
+template <bool NANS>
+__device__ __forceinline__ float row_value(float acc, float ls) {
+  if constexpr (NANS) return ls == 0.f ? 0.f : acc / ls;
+  else return ls > 0.f ? acc / ls : 0.f;
+}
+
 // Every workgroup calls this once its partial is stored.  The last of the
 // nc workgroups of (sequence i, kv head g) to arrive rescales and sums all
 // partials of the group, writes the output rows and re-arms the counter.
@@ -224,8 +267,8 @@ __device__ void write_zero_rows(const DecodeArgs &a, int i, int g, int DH, int s
 // is exactly max-then-sum over all chunks.
 constexpr int kCombineBatch = 4;
 
-template <typename OutT>
-__device__ void finish_group(const DecodeArgs &a, int i, int g, int nc, int DH, int *last) {
+template <typename OutT, bool NANS = false, bool PREFIX = false, int D = 128>
+__device__ __forceinline__ void finish_group(const DecodeArgs &a, int i, int g, int nc, int DH, int *last) {
   int32_t *ctr = a.counters + (int64_t)i * a.Hkv + g;
   __builtin_amdgcn_s_waitcnt(0);  // this thread's partial stores are done
   __syncthreads();
@@ -298,8 +341,9 @@ __device__ void finish_group(const DecodeArgs &a, int i, int g, int nc, int DH, 
       const int e = e0 + threadIdx.x + kDecThreads * k;
       if (e < ne) {
         const int hh = e / DH, dd = e - hh * DH;
+        if constexpr (PREFIX) join_prefix<D>(a, i, g * a.G + hh, dd, M[k], acc[k], ls[k], bad[k]);
         out[((int64_t)i * a.Hq + g * a.G + hh) * DH + dd] =
-            Elem<OutT>::to_store(bad[k] || !(ls[k] > 0.f) ? 0.f : acc[k] / ls[k]);
+            Elem<OutT>::to_store(bad[k] ? 0.f : row_value<NANS>(acc[k], ls[k]));
       }
     }
   }
@@ -978,7 +1022,8 @@ __device__ __forceinline__ float byte_scale(uint32_t w, int i) {
 // EIGHT (without STEP): e4m3 pages.  Their values become bf16 on the way to the
 // matrix cores, K's with their exponents (a lane's K values are of one token);
 // V's exponents go into the probabilities before those are rounded to bf16.
-template <int DH, bool STEP, bool ORD, bool CROP = false, bool EIGHT = false>
+// PREFIX (without STEP): the requests' shares over a prefix are joined.
+template <int DH, bool STEP, bool ORD, bool CROP = false, bool EIGHT = false, bool PREFIX = false>
 __global__ __launch_bounds__(kDecThreads, 2) void decode_split_bf16(DecodeArgs a) {
   __shared__ int pages[kMaxChunkPages];
   __shared__ int flag;
@@ -1210,6 +1255,19 @@ __global__ __launch_bounds__(kDecThreads, 2) void decode_split_bf16(DecodeArgs a
         step_finish();
       }
     }
+    constexpr bool NANS = EIGHT || PREFIX;
+    if constexpr (PREFIX) {
+      if (st == 0 && L == 0) {  // nothing of its own
+        for (int e = tid; c == 0 && e < a.G * DH; e += kDecThreads) {
+          const int hh = e / DH, dd = e - hh * DH, hq = g * a.G + hh;
+          float M = -INFINITY, acc = 0.f, ls = 0.f;
+          bool bad = false;
+          join_prefix<DH>(a, i, hq, dd, M, acc, ls, bad);
+          ((uint16_t *)a.out)[((int64_t)i * a.Hq + hq) * DH + dd] = f32_to_bf16(bad ? 0.f : row_value<NANS>(acc, ls));
+        }
+        return;
+      }
+    }
     if (st != 0 || L == 0) {
       if (c == 0) write_zero_rows<uint16_t>(a, i, g, DH, st, esink);
       return;
@@ -1217,7 +1275,7 @@ __global__ __launch_bounds__(kDecThreads, 2) void decode_split_bf16(DecodeArgs a
     if (!work) return;
     if (!pages_ok) {
       write_bad_partial(a, i, g, c, esink);
-      finish_group<uint16_t>(a, i, g, nc, DH, &flag);
+      finish_group<uint16_t, NANS, PREFIX, DH>(a, i, g, nc, DH, &flag);
       return;
     }
     const int t1p = min(t1, L_pool);  // pool entries of this chunk: [t0, t1p)
@@ -1493,7 +1551,9 @@ __global__ __launch_bounds__(kDecThreads, 2) void decode_split_bf16(DecodeArgs a
         }
       }
       if (nc == 1) {  // the only chunk: write the result directly
-        ((uint16_t *)a.out)[((int64_t)i * a.Hq + g * G + hh) * DH + dd] = f32_to_bf16(ls > 0.f ? acc / ls : 0.f);
+        bool bad = false;
+        if constexpr (PREFIX) join_prefix<DH>(a, i, g * G + hh, dd, M, acc, ls, bad);
+        ((uint16_t *)a.out)[((int64_t)i * a.Hq + g * G + hh) * DH + dd] = f32_to_bf16(bad ? 0.f : row_value<NANS>(acc, ls));
         continue;
       }
       const int64_t pidx = ((int64_t)i * a.Hq + g * G + hh) * a.max_chunks + c;
@@ -1503,7 +1563,7 @@ __global__ __launch_bounds__(kDecThreads, 2) void decode_split_bf16(DecodeArgs a
         put_partial(&a.ws_ml[pidx * 2 + 1], ls);
       }
     }
-    if (nc > 1) finish_group<uint16_t>(a, i, g, nc, DH, &flag);
+    if (nc > 1) finish_group<uint16_t, NANS, PREFIX, DH>(a, i, g, nc, DH, &flag);
   };
   body();
 }
@@ -1808,11 +1868,11 @@ static int device_cus() {
 }
 
 // Workgroups of a bf16 decode kernel resident on one compute unit at once.
-template <int DH, bool STEP, bool CROP, bool EIGHT = false>
+template <int DH, bool STEP, bool CROP, bool EIGHT = false, bool PREFIX = false>
 static int bf16_occupancy() {
   static const int occ = [] {
     int nb = 0;
-    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&nb, decode_split_bf16<DH, STEP, true, CROP, EIGHT>, kDecThreads, 0) !=
+    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&nb, decode_split_bf16<DH, STEP, true, CROP, EIGHT, PREFIX>, kDecThreads, 0) !=
         hipSuccess)
       nb = 1;
     return nb > 0 ? nb : 1;
@@ -1834,7 +1894,9 @@ static sm_status decode_launch(const sm_paged_cache *c, DecodeArgs a, int n, hip
       a.order_n = n;
       a.order_cus = cus;
       const bool d128 = c->head_dim == 128;
-      if (c->dtype == SM_E4M3)
+      if (a.prefix.flag)  // (one more that is resident or not only changes the order)
+        a.order_occ = d128 ? bf16_occupancy<128, false, false, true, true>() : bf16_occupancy<64, false, false, true, true>();
+      else if (c->dtype == SM_E4M3)
         a.order_occ = d128 ? bf16_occupancy<128, false, false, true>() : bf16_occupancy<64, false, false, true>();
       else if (STEP && a.crop)
         a.order_occ = d128 ? bf16_occupancy<128, STEP, STEP>() : bf16_occupancy<64, STEP, STEP>();
@@ -1842,7 +1904,20 @@ static sm_status decode_launch(const sm_paged_cache *c, DecodeArgs a, int n, hip
         a.order_occ = d128 ? bf16_occupancy<128, STEP, false>() : bf16_occupancy<64, STEP, false>();
     }
   }
-  if (c->dtype == SM_E4M3) {  // (never a step)
+  if (a.prefix.flag) {  // (never a step)
+    const auto kernel = [&](auto dh, auto e) {
+      constexpr int DH = decltype(dh)::value;
+      constexpr bool EIGHT = decltype(e)::value;
+      return a.order_n > 0 ? decode_split_bf16<DH, false, true, false, EIGHT, true>
+                           : decode_split_bf16<DH, false, false, false, EIGHT, true>;
+    };
+    const std::integral_constant<int, 128> d128{};
+    const std::integral_constant<int, 64> d64{};
+    const bool eight = c->dtype == SM_E4M3;
+    const auto chosen = c->head_dim == 128 ? (eight ? kernel(d128, std::true_type()) : kernel(d128, std::false_type()))
+                                           : (eight ? kernel(d64, std::true_type()) : kernel(d64, std::false_type()));
+    hipLaunchKernelGGL(chosen, grid, dim3(kDecThreads), 0, stream, a);
+  } else if (c->dtype == SM_E4M3) {  // (never a step)
     const bool ord = a.order_n > 0;
     const auto kernel = c->head_dim == 128 ? (ord ? decode_split_bf16<128, false, true, false, true>
                                                   : decode_split_bf16<128, false, false, false, true>)
@@ -1896,6 +1971,55 @@ SM_API sm_status sm_decode_attention(const sm_paged_cache *c, const int32_t *seq
 
 // Polls of the fused step's commit wait (kCommitSpinLimit unless a test
 // lowers it to exercise the give-up path).
+// Workspace of a shared call: that of sm_decode_attention, then one line for
+// the flag, then the prefixes' parts.
+constexpr int64_t kSharedLine = 256;
+static int64_t decode_part_bytes(int n, int num_q_heads, int head_dim, int max_len) {
+  return ((int64_t)sm_decode_workspace_bytes(n, num_q_heads, head_dim, max_len) + kSharedLine - 1) / kSharedLine * kSharedLine;
+}
+
+SM_API size_t sm_decode_shared_workspace_bytes(int n, int num_q_heads, int head_dim, int max_len, int max_prefix) {
+  if (n <= 0 || num_q_heads <= 0 || head_dim <= 0 || max_len < 0 || max_prefix < 0) return 0;
+  const int64_t vectors = (int64_t)n * num_q_heads;
+  return (size_t)(decode_part_bytes(n, num_q_heads, head_dim, max_len) + kSharedLine +
+                  vectors * shared_most_chunks(vectors, max_prefix) * (head_dim + 2) * (int64_t)sizeof(float));
+}
+
+SM_API sm_status sm_decode_attention_shared(const sm_paged_cache *c, const int32_t *seq_ids, int n, const int32_t *prefix_ids,
+                                            const int32_t *group_offsets, int num_groups, const void *q, int num_q_heads,
+                                            float scale, int max_len, int max_prefix, void *out, void *ws, size_t ws_bytes,
+                                            hipStream_t stream) {
+  if (c && c->dtype == SM_F32) return SM_EINVAL;
+  DecodeArgs a;
+  const sm_status st = decode_setup(c, seq_ids, n, q, num_q_heads, scale, max_len, out, ws, ws_bytes, kMaxPairs, a, false, true);
+  if (st != SM_OK) return st;
+  if (max_prefix < 0 || num_groups < 0 || num_groups > 65535 || !(fabsf(scale) <= 3.0e38f)) return SM_EINVAL;
+  if (n == 0) return SM_OK;
+  if (num_groups == 0) return SM_EINVAL;
+  if (!prefix_ids || !group_offsets) return SM_EINVAL;
+  if ((int64_t)max_prefix > (int64_t)c->max_blocks_per_seq * c->block_size ||
+      (uint64_t)c->num_kv_heads * c->block_size * c->head_dim * 2 > 0xffffffffull)
+    return SM_EINVAL;
+  if (ws_bytes < sm_decode_shared_workspace_bytes(n, num_q_heads, c->head_dim, max_len, max_prefix)) return SM_EINVAL;
+  PrefixArgs p;
+  p.prefix_ids = prefix_ids;
+  p.group_offsets = group_offsets;
+  p.n = n;
+  p.groups = num_groups;
+  p.max_prefix = max_prefix;
+  p.plan = plan_shared(n, c->num_kv_heads, a.G, num_groups, max_prefix);
+  // one chunk at least: the launch that checks the groups
+  const int64_t chunks = p.plan.chunks > 0 ? p.plan.chunks : 1, vectors = (int64_t)n * num_q_heads;
+  char *at = (char *)ws + decode_part_bytes(n, num_q_heads, c->head_dim, max_len);
+  p.parts.flag = (int32_t *)at;
+  p.parts.ml = (float *)(at + kSharedLine);
+  p.parts.o = p.parts.ml + 2 * vectors * chunks;
+  p.parts.chunks = (int)chunks;
+  a.prefix = p.parts;
+  const sm_status first = launch_prefix(c, p, q, num_q_heads, scale, stream);
+  return first != SM_OK ? first : decode_launch<false>(c, a, n, stream);
+}
+
 static std::atomic<int> g_commit_spin_limit{kCommitSpinLimit};
 
 SM_API void sm_set_commit_wait_limit(int polls) {

@@ -35,9 +35,15 @@
 // entries of a feature (V).  They become bf16 on the way to LDS, K with its
 // exponents, V without: those go into the probabilities before they are
 // rounded, as floats that a tile's buffer holds beside its rows.
+//
+// The prefix of a group of requests (SHARED) is attended to by the same
+// tiles: the vectors are the G query heads of every request of the group, all
+// of them see all of a chunk of the prefix, and what they make of it goes to
+// the workspace unnormalised, for the decode kernel to join.
 #include "common.hpp"
 #include "e4m3.hpp"
 #include "prefill_plan.hpp"
+#include "shared_prefix.hpp"
 
 #include <type_traits>
 
@@ -73,6 +79,7 @@ struct PrefillArgs {
   uint32_t page_bytes;  // bytes of one page over all kv heads
   float scale_log2e;    // |scale| log2(e), at least 1e-30
   uint32_t q_sign;      // 0x80008000 when scale < 0: q enters with its sign flipped
+  PrefixArgs p;         // SHARED
 };
 
 // Score-block row rho (0..31) holds token tau(rho) of the block: within each
@@ -90,6 +97,7 @@ __device__ __forceinline__ int pf_token_of_row(int rho) {
 struct PfBlock {
   int g, qb, r0, m, s, L;
   bool ok;
+  int k0, c;  // SHARED: first entry and number of the chunk; r0, m: the group's requests, qb: a block of their vectors
 };
 
 __device__ __forceinline__ PfBlock pf_block(const PrefillArgs &a) {
@@ -121,7 +129,96 @@ __device__ __forceinline__ PfBlock pf_block(const PrefillArgs &a) {
     L = a.lengths[s];
     ok = L >= 0 && L <= (a.max_blocks << a.bs_log2) && m <= L;
   }
-  return PfBlock{g, qb, r0, m, s, L, ok};
+  return PfBlock{g, qb, r0, m, s, L, ok, 0, 0};
+}
+
+// SHARED: workgroup -> (chunk, kv head, block of vectors of a group).  The
+// blocks of one chunk and head land on one XCD, as above.  m = 0: nothing to do.
+template <int KS>
+__device__ __forceinline__ PfBlock prefix_block(const PrefillArgs &a) {
+  __shared__ int red[16], found[4];
+  constexpr int COLS = kPfVec / KS;
+  const PrefixArgs &p = a.p;
+  const int nb = a.nqb, P = p.parts.chunks * a.Hkv, Pfull = P & ~7, b = blockIdx.x;
+  int pair, j;
+  if (b < Pfull * nb) {
+    const int k = b >> 3;
+    pair = (k / nb) * 8 + (b & 7);
+    j = k - (k / nb) * nb;
+  } else {
+    const int b2 = b - Pfull * nb;
+    pair = Pfull + b2 / nb;
+    j = b2 - (b2 / nb) * nb;
+  }
+  PfBlock wg{pair % a.Hkv, 0, 0, 0, -1, 0, true, 0, pair / a.Hkv};
+  // the group that block j falls into, and whether the offsets list the requests in order
+  if (threadIdx.x == 0) found[0] = -1;
+  int before = 0, wrong = 0;
+  for (int base = 0; base < p.groups; base += kPfThreads) {
+    const int t = base + threadIdx.x;
+    int lo = 0, hi = 0, blocks = 0;
+    if (t < p.groups) {
+      lo = p.group_offsets[t];
+      hi = p.group_offsets[t + 1];
+      wrong |= lo < 0 || hi < lo || hi > p.n || (t == 0 && lo != 0) || (t == p.groups - 1 && hi != p.n);
+      if (!wrong) blocks = ((hi - lo) * a.G + COLS - 1) / COLS;
+    }
+    int total;
+    const int end = before + block_inclusive_scan(blocks, red, &total);
+    if (j >= end - blocks && j < end) {
+      found[0] = t;
+      found[1] = lo;
+      found[2] = hi - lo;
+      found[3] = j - (end - blocks);
+    }
+    before += total;
+    __syncthreads();  // (the next scan writes what this one reads)
+  }
+  wrong = __syncthreads_or(wrong);
+  if (b == 0 && threadIdx.x == 0) {
+    *p.parts.flag = wrong != 0;
+    if (wrong) set_err(a.err, SM_ERR_EINVAL);
+  }
+  const int grp = found[0];
+  if (wrong || grp < 0) return wg;
+  wg.r0 = found[1];
+  wg.m = found[2];
+  wg.qb = found[3];
+  wg.s = p.prefix_ids[grp];
+  wg.k0 = wg.c * p.plan.chunk;
+  if (wg.s != -1) {  // (-1: a group without a prefix)
+    int status = 0;
+    if (wg.s < -1 || wg.s >= a.max_seqs) status = SM_ERR_EINVAL;
+    else {
+      wg.L = a.lengths[wg.s];
+      if (wg.L < 0 || (int64_t)wg.L > (int64_t)a.max_blocks << a.bs_log2) status = SM_ERR_EINVAL;
+      else if (wg.L > p.max_prefix) status = SM_ERR_ERANGE;
+    }
+    wg.ok = status == 0;
+    if (status && wg.g == 0 && wg.c == 0 && wg.qb == 0 && threadIdx.x == 0) set_err(a.err, status);
+  }
+  return wg;
+}
+
+// The chunk's sums of this workgroup's vectors where it has no entries (0) or is unusable (-1).
+template <int KS>
+__device__ __forceinline__ void prefix_none(const PrefillArgs &a, const PfBlock &wg, float sum) {
+  constexpr int COLS = kPfVec / KS;
+  for (int v = threadIdx.x; v < COLS; v += kPfThreads) {
+    const int col = wg.qb * COLS + v, member = col / a.G;
+    if (member >= wg.m) break;
+    const int64_t at = ((int64_t)(wg.r0 + member) * a.Hq + wg.g * a.G + col - member * a.G) * a.p.parts.chunks + wg.c;
+    a.p.parts.ml[2 * at] = sum < 0.f ? 0.f : -INFINITY;
+    a.p.parts.ml[2 * at + 1] = sum;
+  }
+}
+
+// 1 / the sum of a row's weights.  A NaN among a row's scores is its result over
+// e4m3 pages; over bf16 pages such a row is zero.
+template <bool EIGHT>
+__device__ __forceinline__ float inverse_sum(float l) {
+  if constexpr (EIGHT) return l == 0.f ? 0.f : 1.0f / l;
+  else return l > 0.f ? 1.0f / l : 0.f;
 }
 
 // LDS of a workgroup: the ring of K and V buffers, which the merge of the wave
@@ -134,7 +231,7 @@ constexpr int pf_lds_bytes() {
   return (ring > merge ? ring : merge) + kPfMaxPages * 4 + 16;
 }
 
-template <int DH, int KS, bool EIGHT = false>
+template <int DH, int KS, bool EIGHT = false, bool SHARED = false>
 __device__ __forceinline__ void prefill_body(const PrefillArgs &a, const PfBlock &wg, uint8_t *lds) {
   constexpr int KEYS = KS == 4 ? 32 : 64;  // keys per tile
   constexpr int SUB = KEYS / 32;           // 32-key score blocks per tile
@@ -171,7 +268,12 @@ __device__ __forceinline__ void prefill_body(const PrefillArgs &a, const PfBlock
   const int vg = w % VG, kg = w / VG;  // this wave's vectors and its group's share of the keys
   const int bs_log2 = a.bs_log2, bs = 1 << bs_log2;
 
-  if (!wg.ok) {  // block 0 reports the request and zeroes its rows
+  if constexpr (SHARED) {
+    if (!wg.ok || wg.k0 >= L) {
+      prefix_none<KS>(a, wg, wg.ok ? 0.f : -1.f);
+      return;
+    }
+  } else if (!wg.ok) {  // block 0 reports the request and zeroes its rows
     if (qb != 0) return;
     if (tid == 0) set_err(a.err, SM_ERR_EINVAL);
     const int per_row = a.G * DH;  // this kv head's query heads
@@ -181,18 +283,20 @@ __device__ __forceinline__ void prefill_body(const PrefillArgs &a, const PfBlock
     }
     return;
   }
-  const int q_lo = qb * a.BQ;  // first row of this block within the request
-  if (q_lo >= m) return;
+  const int q_lo = SHARED ? 0 : qb * a.BQ;  // first row of this block within the request
+  if (!SHARED && q_lo >= m) return;
   const int nq = min(a.BQ, m - q_lo);
   const int pos0 = L - m + q_lo;  // position of row q_lo
-  const int kend = pos0 + nq;     // keys [0, kend) are needed
+  const int k0 = SHARED ? wg.k0 : 0;
+  const int kend = SHARED ? min(L, k0 + a.p.plan.chunk) : pos0 + nq;  // keys [k0, kend) are needed
+  const int lp0 = SHARED ? k0 >> bs_log2 : 0;  // page of key k0
 
   // ---- page ids of keys [0, kend) into LDS, range-checked ----
   if (tid == 0) *bad_flag = 0;
   __syncthreads();
-  const int npg = (kend + bs - 1) >> bs_log2;
+  const int npg = ((kend + bs - 1) >> bs_log2) - lp0;
   for (int p = tid; p < npg; p += kPfThreads) {
-    int blk = a.block_table[(int64_t)s * a.max_blocks + p];
+    int blk = a.block_table[(int64_t)s * a.max_blocks + lp0 + p];
     if (blk < 0 || blk >= a.num_blocks) {
       *bad_flag = 1;
       blk = 0;
@@ -202,6 +306,10 @@ __device__ __forceinline__ void prefill_body(const PrefillArgs &a, const PfBlock
   __syncthreads();
   if (*bad_flag) {  // a corrupt block table: this block's rows are zero
     if (tid == 0) set_err(a.err, SM_ERR_EINVAL);
+    if constexpr (SHARED) {
+      prefix_none<KS>(a, wg, -1.f);
+      return;
+    }
     const int per_row = a.G * DH;
     for (int e = tid; e < nq * per_row; e += kPfThreads) {
       const int rr = e / per_row, k = e - rr * per_row;
@@ -211,12 +319,13 @@ __device__ __forceinline__ void prefill_body(const PrefillArgs &a, const PfBlock
   }
 
   // ---- this wave's 32 query vectors: v = 32 vg + c32 -> query head g G + v / BQ, row q_lo + v % BQ ----
-  const int v = 32 * vg + c32;
-  const int hh = v / a.BQ, rr = v - hh * a.BQ;
-  const bool vok = hh < a.G && rr < nq;
+  // (SHARED: vector v of the group's -> request v / G, query head v % G; all keys)
+  const int v = 32 * vg + c32 + (SHARED ? qb * (kPfVec / KS) : 0);
+  const int rr = SHARED ? v / a.G : v % a.BQ, hh = SHARED ? v - rr * a.G : v / a.BQ;
+  const bool vok = SHARED ? rr < m : hh < a.G && rr < nq;
   const int vhead = g * a.G + (vok ? hh : 0);
   const int vrow = r0 + q_lo + (vok ? rr : 0);
-  const int vpos = vok ? pos0 + rr : -1;  // an idle vector sees no key
+  const int vpos = !vok ? -1 : SHARED ? kend - 1 : pos0 + rr;  // an idle vector sees no key
   u32x4_t qf[NKS];
   {
     const uint16_t *qp = a.q + ((int64_t)vrow * a.Hq + vhead) * DH + 8 * h2;
@@ -264,18 +373,18 @@ __device__ __forceinline__ void prefill_body(const PrefillArgs &a, const PfBlock
 #pragma unroll
     for (int u = 0; u < KU; ++u) {
       const int tok = t0 + ktk[u];
-      const uint32_t blk = pages[tok < kend ? tok >> bs_log2 : 0];
+      const uint32_t blk = pages[tok < kend ? (tok >> bs_log2) - lp0 : 0];
       kv[u] = *(const u32x4_t *)(kbase + blk * page_bytes + (koff[u] + tin * DH * ES));
       if constexpr (EIGHT) ex.k[u] = kebase[(uint64_t)blk * exp_page + (ktk[u] & (bs - 1)) + tin];
     }
     if constexpr (EIGHT) {
       const int tok = t0 + tid;
-      ex.v = tid < SPAN && tok < kend ? vebase[(uint64_t)pages[tok >> bs_log2] * exp_page + (tok & (bs - 1))] : 0;
+      ex.v = tid < SPAN && tok < kend ? vebase[(uint64_t)pages[(tok >> bs_log2) - lp0] * exp_page + (tok & (bs - 1))] : 0;
     }
 #pragma unroll
     for (int u = 0; u < VU; ++u) {
       const int tok = t0 + vtk[u];
-      const uint32_t blk = pages[tok < kend ? tok >> bs_log2 : 0];
+      const uint32_t blk = pages[tok < kend ? (tok >> bs_log2) - lp0 : 0];
       kv[KU + u] = *(const u32x4_t *)(vbase + blk * page_bytes + (voff[u] + tin * ES));
     }
     if (t0 + SPAN > L) {  // the last tile: V entries past the length may hold anything
@@ -339,15 +448,15 @@ __device__ __forceinline__ void prefill_body(const PrefillArgs &a, const PfBlock
   const float sl2 = a.scale_log2e;
   const int krow = pf_token_of_row(c32);  // this lane's K row in the S^T operand
 
-  const int ntiles = (kend + SPAN - 1) / SPAN;
+  const int ntiles = (kend - k0 + SPAN - 1) / SPAN;  // (SHARED: k0 is a multiple of SPAN)
   u32x4_t stage[KU + VU];
   Exps exps;
-  fetch(0, stage, exps);
+  fetch(k0, stage, exps);
   stash(0, stage, exps);
   __syncthreads();
   for (int t = 0; t < ntiles; ++t) {
-    const int buf = t & 1, t0 = t * SPAN + kg * KEYS;  // this group's tile
-    if (t + 1 < ntiles) fetch((t + 1) * SPAN, stage, exps);  // in flight during this pass
+    const int buf = t & 1, t0 = k0 + t * SPAN + kg * KEYS;  // this group's tile
+    if (t + 1 < ntiles) fetch(k0 + (t + 1) * SPAN, stage, exps);  // in flight during this pass
 
     if (t0 <= wave_hi) {
       // S^T = K . Q^T, one 32-key block at a time: its fragment reads first,
@@ -477,7 +586,7 @@ __device__ __forceinline__ void prefill_body(const PrefillArgs &a, const PfBlock
     // scaled to the common reference, its output columns; then wave kg of a
     // group's KS waves adds the KS partials of its DH / KS dims.
     float *ml = (float *)lds, *po = ml + kPfWaves * 64;  // [wave][32 m, 32 l], [wave][32][OPITCH]
-    const int live = min(KS, (kend + KEYS - 1) / KEYS);   // groups that had a tile at all
+    const int live = min(KS, (kend - k0 + KEYS - 1) / KEYS);   // groups that had a tile at all
     if (h2 == 0) {
       ml[w * 64 + c32] = m_run;
       ml[w * 64 + 32 + c32] = l_tot;
@@ -498,7 +607,6 @@ __device__ __forceinline__ void prefill_body(const PrefillArgs &a, const PfBlock
           *(f32x4_t *)&po[(w * 32 + c32) * OPITCH + 32 * rb + 8 * gg + 4 * h2] =
               f32x4_t{o[rb][4 * gg] * mine, o[rb][4 * gg + 1] * mine, o[rb][4 * gg + 2] * mine, o[rb][4 * gg + 3] * mine};
     __syncthreads();
-    const float inv = l_tot > 0.f ? 1.0f / l_tot : 0.f;
     if (!vok) return;
     // lane (c32, h2) takes dims d0 .. d0 + DH / KS / 2 - 1 of its column
     constexpr int DW = DH / KS / 2;
@@ -509,14 +617,33 @@ __device__ __forceinline__ void prefill_body(const PrefillArgs &a, const PfBlock
     for (int k = 0; k < live; ++k)
 #pragma unroll
       for (int c = 0; c < DW / 4; ++c) y[c] += *(const f32x4_t *)&po[((k * VG + vg) * 32 + c32) * OPITCH + d0 + 4 * c];
+    if constexpr (SHARED) {
+      const int64_t at = ((int64_t)vrow * a.Hq + vhead) * a.p.parts.chunks + wg.c;
+#pragma unroll
+      for (int c = 0; c < DW / 4; ++c) *(f32x4_t *)&a.p.parts.o[at * DH + d0 + 4 * c] = y[c];
+      if (kg == 0 && h2 == 0) *(float2 *)&a.p.parts.ml[2 * at] = make_float2(mb, l_tot);
+      return;
+    }
+    const float inv = inverse_sum<EIGHT>(l_tot);
     uint16_t *op = a.out + ((int64_t)vrow * a.Hq + vhead) * DH + d0;
 #pragma unroll
     for (int c = 0; c < DW / 4; ++c)
       *(uint2 *)(op + 4 * c) = make_uint2(cvt_bf16x2(y[c][0] * inv, y[c][1] * inv), cvt_bf16x2(y[c][2] * inv, y[c][3] * inv));
     return;
   }
-  const float inv = l_tot > 0.f ? 1.0f / l_tot : 0.f;
   if (!vok) return;
+  if constexpr (SHARED) {
+    const int64_t at = ((int64_t)vrow * a.Hq + vhead) * a.p.parts.chunks + wg.c;
+#pragma unroll
+    for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+      for (int gg = 0; gg < 4; ++gg)
+        *(f32x4_t *)&a.p.parts.o[at * DH + 32 * rb + 8 * gg + 4 * h2] =
+            f32x4_t{o[rb][4 * gg], o[rb][4 * gg + 1], o[rb][4 * gg + 2], o[rb][4 * gg + 3]};
+    if (h2 == 0) *(float2 *)&a.p.parts.ml[2 * at] = make_float2(m_run, l_tot);
+    return;
+  }
+  const float inv = inverse_sum<EIGHT>(l_tot);
   uint16_t *op = a.out + ((int64_t)vrow * a.Hq + vhead) * DH + 4 * h2;
 #pragma unroll
   for (int rb = 0; rb < NRB; ++rb)
@@ -550,6 +677,71 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_few_bf16(PrefillArgs a)
   else prefill_body<DH, 4, EIGHT>(a, wg, lds);
 }
 
+template <int DH, int KS, bool EIGHT>
+__global__ __launch_bounds__(kPfThreads, 2) void prefix_kernel(PrefillArgs a) {
+  __shared__ __attribute__((aligned(16))) uint8_t lds[pf_lds_bytes<DH, KS, EIGHT>()];
+  const PfBlock wg = prefix_block<KS>(a);
+  if (wg.m > 0) prefill_body<DH, KS, EIGHT, true>(a, wg, lds);
+}
+
+// The cache and the queries, as both calls have them (checked by them).
+static PrefillArgs pf_args(const sm_paged_cache *c, const void *q, int num_q_heads, float scale) {
+  const int H = c->num_kv_heads, D = c->head_dim, bs = c->block_size;
+  const bool eight = c->dtype == SM_E4M3;
+  PrefillArgs a = {};
+  a.k_pool = c->k_pool;
+  a.v_pool = c->v_pool;
+  if (eight) {
+    a.k_exp = pool_exps((const uint8_t *)c->k_pool, c->num_blocks, H, bs, D);
+    a.v_exp = pool_exps((const uint8_t *)c->v_pool, c->num_blocks, H, bs, D);
+  }
+  a.block_table = c->block_table;
+  a.lengths = c->lengths;
+  a.q = (const uint16_t *)q;
+  a.err = c->err;
+  a.Hkv = H;
+  a.Hq = num_q_heads;
+  a.G = num_q_heads / H;
+  int bl = 0;
+  while ((1 << bl) < bs) ++bl;
+  a.bs_log2 = bl;
+  a.num_blocks = c->num_blocks;
+  a.max_seqs = c->max_seqs;
+  a.max_blocks = c->max_blocks_per_seq;
+  a.page_bytes = (uint32_t)((uint64_t)H * bs * D * (eight ? 1 : 2));
+  // A positive multiplier keeps exp2(-inf) = 0 for masked keys.  Below 1e-30
+  // every weight rounds to 1 in fp32 either way (|q . k| stays far below 1e30).
+  a.scale_log2e = fmaxf(fabsf(scale) * kPfLog2e, 1e-30f);
+  a.q_sign = scale < 0.f ? 0x80008000u : 0u;
+  return a;
+}
+
+sm_status launch_prefix(const sm_paged_cache *c, const PrefixArgs &p, const void *q, int num_q_heads, float scale,
+                        hipStream_t stream) {
+  PrefillArgs a = pf_args(c, q, num_q_heads, scale);
+  a.p = p;
+  a.BQ = 1;
+  const int cols = kPfVec / p.plan.splits;
+  // blocks of vectors: at most this many over all groups
+  const int64_t nb = (int64_t)p.n * a.G / cols + p.groups;
+  a.nqb = (int)nb;
+  if (nb * a.Hkv * p.parts.chunks > 0x7fffffff) return SM_EINVAL;
+  const dim3 grid((unsigned)(nb * a.Hkv * p.parts.chunks));
+  const auto kernel = [&](auto dh, auto e) {
+    constexpr int DH = decltype(dh)::value;
+    constexpr bool EIGHT = decltype(e)::value;
+    return p.plan.splits == 4 ? prefix_kernel<DH, 4, EIGHT> : p.plan.splits == 2 ? prefix_kernel<DH, 2, EIGHT>
+                                                                               : prefix_kernel<DH, 1, EIGHT>;
+  };
+  const std::integral_constant<int, 128> d128{};
+  const std::integral_constant<int, 64> d64{};
+  const bool eight = c->dtype == SM_E4M3;
+  const auto chosen = c->head_dim == 128 ? (eight ? kernel(d128, std::true_type()) : kernel(d128, std::false_type()))
+                                         : (eight ? kernel(d64, std::true_type()) : kernel(d64, std::false_type()));
+  hipLaunchKernelGGL(chosen, grid, dim3(kPfThreads), 0, stream, a);
+  return hipGetLastError() == hipSuccess ? SM_OK : SM_EHIP;
+}
+
 }  // namespace sm
 
 using namespace sm;
@@ -572,38 +764,16 @@ SM_API sm_status sm_prefill_attention(const sm_paged_cache *c, const int32_t *se
       c->num_blocks <= 0 || c->max_seqs <= 0)
     return SM_EINVAL;
   if (n > 65535 || (uint64_t)H * bs * D * 2 > 0xffffffffull) return SM_EINVAL;
-  PrefillArgs a;
-  a.k_pool = c->k_pool;
-  a.v_pool = c->v_pool;
-  a.k_exp = eight ? pool_exps((const uint8_t *)c->k_pool, c->num_blocks, H, bs, D) : nullptr;
-  a.v_exp = eight ? pool_exps((const uint8_t *)c->v_pool, c->num_blocks, H, bs, D) : nullptr;
-  a.block_table = c->block_table;
-  a.lengths = c->lengths;
+  PrefillArgs a = pf_args(c, q, num_q_heads, scale);
   a.seq_ids = seq_ids;
   a.q_offsets = q_offsets;
-  a.q = (const uint16_t *)q;
   a.out = (uint16_t *)out;
-  a.err = c->err;
   a.n = n;
   a.total_rows = total_rows;
   a.max_rows = max_rows;
-  a.Hkv = H;
-  a.Hq = num_q_heads;
-  a.G = G;
   const PrefillPlan plan = plan_prefill(n, H, G, total_rows, max_rows, (int64_t)c->max_blocks_per_seq * bs);
   const int ks = plan.splits;
   a.BQ = kPfVec / ks / G;
-  int bl = 0;
-  while ((1 << bl) < bs) ++bl;
-  a.bs_log2 = bl;
-  a.num_blocks = c->num_blocks;
-  a.max_seqs = c->max_seqs;
-  a.max_blocks = c->max_blocks_per_seq;
-  a.page_bytes = (uint32_t)((uint64_t)H * bs * D * (eight ? 1 : 2));
-  // A positive multiplier keeps exp2(-inf) = 0 for masked keys.  Below 1e-30
-  // every weight rounds to 1 in fp32 either way (|q . k| stays far below 1e30).
-  a.scale_log2e = fmaxf(fabsf(scale) * kPfLog2e, 1e-30f);
-  a.q_sign = scale < 0.f ? 0x80008000u : 0u;
   const int nqb = max_rows > 0 ? (max_rows + a.BQ - 1) / a.BQ : 1;  // block 0 reports bad requests
   if ((int64_t)nqb * n * H > 0x7fffffff) return SM_EINVAL;
   a.nqb = nqb;

@@ -35,6 +35,7 @@ EXPORTED = ("sm_status_string", "sm_merge_workspace_bytes", "sm_merge_spans",
             "sm_pack_spans", "sm_kv_rollback", "sm_kv_append",
             "sm_decode_workspace_bytes", "sm_decode_attention", "sm_decode_step", "sm_decode_merge_step",
             "sm_decode_step_noalloc_max_bytes", "sm_decode_step_noalloc", "sm_set_commit_wait_limit",
+            "sm_decode_shared_workspace_bytes", "sm_decode_attention_shared",
             "sm_prefill_attention", "sm_rules_build_workspace_bytes", "sm_rules_build",
             "sm_rules_lookup", "sm_match_prompt_workspace_bytes", "sm_match_prompt",
             "sm_match_decode", "sm_gather_surrogates", "sm_span_dedupe_workspace_bytes", "sm_span_dedupe",
@@ -115,6 +116,10 @@ def load(path: str = LIB_PATH):
     L.sm_decode_attention.argtypes = [C.POINTER(PagedCacheDesc), _P, _I, _P, _I, _F,
                                       _I, _P, _P, _Z, _P]
     L.sm_decode_attention.restype = _I
+    L.sm_decode_shared_workspace_bytes.argtypes = [_I, _I, _I, _I, _I]
+    L.sm_decode_shared_workspace_bytes.restype = _Z
+    L.sm_decode_attention_shared.argtypes = [C.POINTER(PagedCacheDesc), _P, _I, _P, _P, _I, _P, _I, _F, _I, _I, _P, _P, _Z, _P]
+    L.sm_decode_attention_shared.restype = _I
     L.sm_decode_step.argtypes = [C.POINTER(PagedCacheDesc), _P, _I, _P, _P, _P, _I, _F,
                                  _I, _P, _P, _Z, _P]
     L.sm_decode_step.restype = _I
@@ -300,8 +305,8 @@ class PagedCache:
 
     dtype torch.float8_e4m3fn: pages in 8 bits, with an exponent byte for each
     entry and head (k_exp, v_exp [NB, Hkv, bs]: feature = value * 2^(byte - 127)).
-    kv_write_rotary fills them; decode_attention, prefill_attention and kv_read
-    read them; rows, queries and results (row_dtype) are bf16."""
+    kv_write_rotary fills them; decode_attention, decode_attention_shared,
+    prefill_attention and kv_read read them; rows, queries and results (row_dtype) are bf16."""
 
     def __init__(self, *, dtype: torch.dtype, num_kv_heads: int, head_dim: int,
                  block_size: int, num_blocks: int, max_seqs: int,
@@ -382,6 +387,31 @@ def decode_attention(cache: PagedCache, seq_ids, q, out, ws, max_len: int,
     sc = D ** -0.5 if scale is None else scale
     st = _calls().sm_decode_attention(cache.desc, seq_ids, n, q, Hq, sc, max_len, out, ws, ws.nbytes, _stream(stream))
     _check(st, "sm_decode_attention")
+
+
+def decode_shared_workspace_bytes(n: int, num_q_heads: int, head_dim: int, max_len: int, max_prefix: int) -> int:
+    return load().sm_decode_shared_workspace_bytes(n, num_q_heads, head_dim, max_len, max_prefix)
+
+
+def decode_attention_shared(cache: PagedCache, seq_ids, prefix_ids, group_offsets, q, out, ws, max_len: int, max_prefix: int,
+                            scale: Optional[float] = None, stream=None):
+    """decode_attention of requests behind shared entries: the requests
+    group_offsets[p] .. group_offsets[p + 1] - 1 attend over the entries of
+    sequence prefix_ids[p] (-1: none), then over their own.  q, out [n, Hq, D]
+    bf16; max_len and max_prefix bound the sequences' and the prefixes' lengths."""
+    b = _calls()
+    n, Hq, D = _shape(q, 3, "q")
+    for t, name in ((q, "q"), (out, "out")):
+        b.row_stride(t, torch.bfloat16, name, n, Hq, cache.D)
+    groups = prefix_ids.numel()
+    b.need(seq_ids, n, "seq_ids")
+    b.need(group_offsets, groups + 1, "group_offsets")
+    handle, dev = _here(stream)
+    _cache_here(cache, dev)
+    sc = D ** -0.5 if scale is None else scale
+    st = b.sm_decode_attention_shared(cache.desc, seq_ids, n, prefix_ids, group_offsets, groups, q, Hq, sc, max_len, max_prefix,
+                                      out, ws, ws.nbytes, handle, dev)
+    _check(st, "sm_decode_attention_shared")
 
 
 def decode_step(cache: PagedCache, seq_ids, K, V, q, out, ws, max_len: int,
