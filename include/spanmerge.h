@@ -42,6 +42,7 @@
  *                       before the next
  *   sm_token_logprobs   log probabilities, entropy and top alternatives of
  *                       rows of logits
+ *   sm_sample_tokens    tokens drawn from rows of logits
  *
  * General rules for every call
  * ----------------------------
@@ -1001,6 +1002,52 @@ sm_status sm_token_logprobs(const void *logits, int64_t stride, int rows,
                             float *entropy, int k, int32_t *top_ids,
                             float *top_logprobs, void *ws, size_t ws_bytes,
                             int32_t *err, hipStream_t stream);
+
+/* Bytes of workspace sm_sample_tokens needs for these sizes. */
+size_t sm_sample_workspace_bytes(int rows, int vocab);
+
+/*
+ * sm_sample_tokens -- one token from each row of logits, by one given random
+ * number u in [0, 1).  With M the largest logit, token v weighs
+ *   w_v = exp((x_v - M) / temperature)
+ * and of the tokens in descending order of x, the lower index first among
+ * equal ones, those are kept that pass in turn
+ *   top_k   the first k
+ *   min_p   w_v >= min_p (a part of the likeliest token's probability)
+ *   top_p   less than top_p of the mass of what is left lies before it (one
+ *           token always stays)
+ * tokens[r] is then the first token, in the order of the vocabulary, at which
+ * the cumulative mass of the kept ones passes u times all of it.  The same
+ * inputs give the same tokens; the next, sm_match_decode, takes them.
+ *
+ *  logits, stride  [rows][vocab] (dtype dt), row stride in elements (>=
+ *               vocab), any element-aligned address
+ *  rows, vocab  (host) 1 <= vocab <= 524288
+ *  u            [rows] fp32, 0 <= u < 1
+ *  temperature  [rows] fp32, finite, >= 0 (0: the likeliest token); null: 1
+ *  top_k        [rows] int32 >= 0 (0, or vocab and above: all); null: all
+ *  top_p        [rows] fp32 >= 0 (1 and above: all); null: all
+ *  min_p        [rows] fp32, 0 <= min_p <= 1 (0: all); null: all
+ *  tokens       [rows] int32 out
+ *  logprob      [rows] fp32 out, or null: log of the token's share of the kept
+ *               mass (sm_token_logprobs gives its share of everything)
+ *  ws, ws_bytes at least sm_sample_workspace_bytes(rows, vocab), 16-byte
+ *               aligned; its first 64 KiB as sm_token_logprobs's (zero before
+ *               the first call and after every one).  Calls that may run
+ *               concurrently must not share a workspace
+ * Weights are formed in double precision and added as whole multiples of
+ * 2^-44, so that a token below 2^-45 of the likeliest one weighs nothing, and a
+ * share is right to 2^-27 at worst, 2^-37 as a rule.  A logit of -infinity is
+ * never drawn.  Device errors (into err, unless it is null): EINVAL for a
+ * setting out of its range, or a row that holds a NaN or +infinity or nothing
+ * but -infinity; its token is -1 and its log probability NaN.
+ */
+sm_status sm_sample_tokens(const void *logits, int64_t stride, int rows,
+                           int vocab, sm_dtype dt, const float *u,
+                           const float *temperature, const int32_t *top_k,
+                           const float *top_p, const float *min_p,
+                           int32_t *tokens, float *logprob, void *ws,
+                           size_t ws_bytes, int32_t *err, hipStream_t stream);
 
 #ifdef __cplusplus
 }

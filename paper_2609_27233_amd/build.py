@@ -20,7 +20,8 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libspanmerge.so")
 SOURCES = ["block_norm.hip", "decode_attn.hip", "kv_paged.hip", "kv_read.hip", "kvproj.hip", "logprobs.hip", "lut.hip", "merge_spans.hip",
-           "prefill_attn.hip", "reserve.hip", "rotary.hip", "rules.hip"]
+           "prefill_attn.hip", "reserve.hip", "rotary.hip", "rules.hip",
+           "sample.hip"]
 BINDING = os.path.join(HERE, "_binding" + sysconfig.get_config_var("EXT_SUFFIX"))
 ARCH = "gfx950"
 

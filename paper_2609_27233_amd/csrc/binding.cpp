@@ -37,7 +37,7 @@ namespace {
 // one argument more, the current device's index, comes last.
 #define SM_CHECKED(X) \
   X(sm_kv_reserve) X(sm_rotary) X(sm_kv_write_rotary) X(sm_kv_read) X(sm_block_norm) X(sm_token_logprobs)     \
-  X(sm_decode_attention_shared)
+  X(sm_decode_attention_shared) X(sm_sample_tokens)
 #define SM_SLOT(name) decltype(&::name) p_##name;
 SM_ENTRIES(SM_SLOT)
 SM_CHECKED(SM_SLOT)

@@ -41,7 +41,7 @@ EXPORTED = ("sm_status_string", "sm_merge_workspace_bytes", "sm_merge_spans",
             "sm_match_decode", "sm_gather_surrogates", "sm_span_dedupe_workspace_bytes", "sm_span_dedupe",
             "sm_kv_project_workspace_bytes", "sm_kv_project", "sm_kv_append_projected",
             "sm_kv_reserve", "sm_rotary", "sm_kv_write_rotary", "sm_kv_read", "sm_block_norm",
-            "sm_token_logprobs_workspace_bytes", "sm_token_logprobs")
+            "sm_token_logprobs_workspace_bytes", "sm_token_logprobs", "sm_sample_workspace_bytes", "sm_sample_tokens")
 
 
 class MergeParams(C.Structure):
@@ -175,6 +175,10 @@ def load(path: str = LIB_PATH):
     L.sm_token_logprobs_workspace_bytes.restype = _Z
     L.sm_token_logprobs.argtypes = [_P, _L, _I, _I, _I, _F, _P, _P, _P, _I, _P, _P, _P, _Z, _P, _P]
     L.sm_token_logprobs.restype = _I
+    L.sm_sample_workspace_bytes.argtypes = [_I, _I]
+    L.sm_sample_workspace_bytes.restype = _Z
+    L.sm_sample_tokens.argtypes = [_P, _L, _I, _I, _I, _P, _P, _P, _P, _P, _P, _P, _P, _Z, _P, _P]
+    L.sm_sample_tokens.restype = _I
     try:
         fast = importlib.import_module("._binding", __package__)
     except ImportError as e:
@@ -786,3 +790,29 @@ def token_logprobs(logits, tokens, logprob, entropy, top_ids, top_logprobs, ws, 
     st = b.sm_token_logprobs((logits,), sl, rows, vocab, dtype_code(dt), scale, tokens, logprob, entropy, k, top_ids,
                              top_logprobs, ws, ws.nbytes, err, handle, dev)
     _check(st, "sm_token_logprobs")
+
+
+def sample_workspace_bytes(rows: int, vocab: int) -> int:
+    return load().sm_sample_workspace_bytes(rows, vocab)
+
+
+def sample_tokens(logits, u, tokens, ws, temperature=None, top_k=None, top_p=None, min_p=None, logprob=None, err=None,
+                  stream=None):
+    """tokens[r] drawn from the row logits[r] by the random number u[r]: weights
+    exp(logits / temperature), of which top_k, then min_p, then top_p keep the
+    likeliest (each [rows], or None: 1 and no filter; a temperature of 0 takes
+    the likeliest token).  logprob: log of the token's share of what is kept."""
+    b = _calls()
+    (rows, vocab), dt, need = _shape(logits, 2, "logits"), logits.dtype, b.need
+    sl = b.row_stride(logits, dt, "logits", rows, vocab)
+    need(u, rows, "u")
+    need(tokens, rows, "tokens")
+    for t, name in ((temperature, "temperature"), (top_k, "top_k"), (top_p, "top_p"), (min_p, "min_p"), (logprob, "logprob")):
+        if t is not None:
+            need(t, rows, name)
+    if err is not None:
+        need(err, 1, "err")
+    handle, dev = _here(stream)
+    st = b.sm_sample_tokens((logits,), sl, rows, vocab, dtype_code(dt), u, temperature, top_k, top_p, min_p, tokens, logprob, ws,
+                            ws.nbytes, err, handle, dev)
+    _check(st, "sm_sample_tokens")
