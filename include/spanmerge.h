@@ -1032,9 +1032,9 @@ size_t sm_sample_workspace_bytes(int rows, int vocab);
  *  logprob      [rows] fp32 out, or null: log of the token's share of the kept
  *               mass (sm_token_logprobs gives its share of everything)
  *  ws, ws_bytes at least sm_sample_workspace_bytes(rows, vocab), 16-byte
- *               aligned; its first 64 KiB as sm_token_logprobs's (zero before
- *               the first call and after every one).  Calls that may run
- *               concurrently must not share a workspace
+ *               aligned: zero-fill all of it once before the first call; every
+ *               call leaves it ready for the next, whatever its sizes.  Calls
+ *               that may run concurrently must not share a workspace
  * Weights are formed in double precision and added as whole multiples of
  * 2^-44, so that a token below 2^-45 of the likeliest one weighs nothing, and a
  * share is right to 2^-27 at worst, 2^-37 as a rule.  A logit of -infinity is

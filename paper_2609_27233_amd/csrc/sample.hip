@@ -10,19 +10,25 @@
 // kept mass passes u times the whole of it.
 //
 // A token is a whole number: masses have to be right to far less than a
-// token's share.  A weight is formed in double precision (a table of 64 and a
-// polynomial, off by 2^-50) and rounded to a multiple of 2^-44; masses are
+// token's share.  A weight is formed in double precision (a table of 128 and a
+// polynomial, off by 2^-49) and rounded to a multiple of 2^-44; masses are
 // 64-bit integers.  Their sums are exact and the same in any order, so that
 // workgroups, waves and atomics may add them as they come.  Over 128,256
 // tokens the roundings come to about 2^-37 of the largest weight.
 //
-// One workgroup takes a row.  It finds M.  A filter looks for the value at
-// which its start of the tokens ends: a histogram over M - x in 32-bit
-// integers, of counts (top-k, exact) or of masses to 2^-14 of themselves
-// (top-p), names a bin or two; one pass in full precision takes the mass above
-// them, and their tokens into a list, which is cut by its values until one is
-// left.  The kept masses of the pieces of 512 tokens are scanned, and the piece
-// that the random number falls into is looked at token by token.
+// Three launches, none of which waits inside:
+//   scan    M, and a histogram over the logits (2048 bins of 1/23): counts for
+//           top-k; for top-p masses in 32-bit integers, right to 2^-14 or so
+//   weigh   the histogram names the bin or two in which the filter's last token
+//           lies; their tokens are listed, and what is above is weighed in full
+//           precision, by pieces of 512 tokens
+//   choose  a workgroup a row: the list is cut by its values until one is left,
+//           the pieces' masses are scanned, and the piece that the random
+//           number falls into is looked at token by token
+// A row is read twice, in slices dealt over the device, four 16-byte loads a
+// lane in flight.  A row whose list does not suffice (thousands of equal logits
+// where the filter ends, a k of thousands, logits hundreds apart) is cut by
+// passes over the whole row, in `choose`, to the same result.
 #include <algorithm>
 #include <cmath>
 
@@ -30,16 +36,36 @@
 
 namespace sm {
 
-constexpr int kSampThreads = 1024, kSampWaves = kSampThreads / 64;
+constexpr int kSampThreads = 256, kSampWaves = kSampThreads / 64;
 constexpr int kPiece = 512;                    // tokens of a piece: 8 a lane
 constexpr int kMostVocab = 1 << 19;            // a mass of 2^44 times this many fits 63 bits
 constexpr int kMostPieces = kMostVocab / kPiece;
-constexpr int kBins = 2048;
-constexpr float kBinsPerLog2 = 16.f;           // bins of a factor of 2
-constexpr int kList = 4096;                    // tokens that are cut in LDS
+constexpr int kInFlight = 4;                   // pieces that a wave loads at a time
 constexpr int kUnit = 44;                      // a weight of 1 is 2^44
 constexpr double kLeast = -46.0;               // exponents from here down weigh nothing
 constexpr double kLog2eD = 1.4426950408889634073599246810019;
+
+// The histogram: bins of 1/23 in the logits, the first 512 above the largest
+// of the row's first piece.
+constexpr int kBins = 2048, kBinsAbove = 512;
+constexpr float kBinsPerUnit = 16.f * 1.44269504f;
+constexpr float kSharpest = 0.25f;             // temperatures below go by a list of all that weighs anything
+constexpr int kList = 4096;                    // tokens that are cut in LDS
+constexpr int kCutBins = 1024;
+
+// What a row has in the workspace.  The first part is zero between calls.
+struct RowState {
+  uint32_t top;       // key of M
+  uint32_t bad;       // a NaN
+  uint32_t listed;    // tokens listed; more than kList: not all of them
+  uint32_t unused;
+  uint64_t mass;      // of all tokens (MASS)
+  uint32_t bins[kBins];
+  // not cleared
+  uint64_t pieces[kMostPieces];  // ties << 54 | mass
+  uint64_t list[kList];          // key << 32 | token
+};
+constexpr int kRowsAtATime = 1024;  // rows that the workspace holds
 
 struct SampleArgs {
   const void *logits;
@@ -50,7 +76,8 @@ struct SampleArgs {
   int32_t *tokens;
   float *logprob;
   int32_t *err;
-  int64_t first;  // row of the launch's first workgroup
+  RowState *state;
+  int slices, per_slice;  // per_slice: pieces
 };
 
 // Ascends with x; -0 counts as 0.
@@ -77,17 +104,20 @@ __device__ __forceinline__ uint64_t unit_weight(double t, const double *table) {
   const double w = ldexp(table[k & 127] * p, (k >> 7) + kUnit) + 4503599627370496.0;  // to nearest
   return t < kLeast ? 0 : __double_as_longlong(w) & 0xfffffffffffffll;
 }
-
-__device__ __forceinline__ uint64_t shfl_xor64(uint64_t v, int m) {
-  const uint32_t lo = __shfl_xor((uint32_t)v, m, kWave), hi = __shfl_xor((uint32_t)(v >> 32), m, kWave);
-  return (uint64_t)hi << 32 | lo;
+__device__ __forceinline__ void fill_table(double *table) {
+  if (threadIdx.x < 128) table[threadIdx.x] = exp2(threadIdx.x / 128.0);
 }
+
+// ---- sums ------------------------------------------------------------------
 __device__ __forceinline__ uint64_t wave_sum64(uint64_t v) {
 #pragma unroll
-  for (int m = 1; m < 64; m <<= 1) v += shfl_xor64(v, m);
+  for (int m = 1; m < 64; m <<= 1) {
+    const uint32_t lo = __shfl_xor((uint32_t)v, m, kWave), hi = __shfl_xor((uint32_t)(v >> 32), m, kWave);
+    v += (uint64_t)hi << 32 | lo;
+  }
   return v;
 }
-__device__ __forceinline__ uint64_t wave_scan64(uint64_t v) {
+__device__ __forceinline__ uint64_t wave_scan(uint64_t v) {
   const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
@@ -96,13 +126,23 @@ __device__ __forceinline__ uint64_t wave_scan64(uint64_t v) {
   }
   return v;
 }
+__device__ __forceinline__ float wave_scan(float v) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const float u = __shfl_up(v, d, kWave);
+    if (lane >= d) v += u;
+  }
+  return v;
+}
 // Inclusive over the workgroup; red: one value a wave.  The last barrier lets red be used again.
-__device__ __forceinline__ uint64_t block_scan64(uint64_t v, uint64_t *red, uint64_t *total) {
+template <typename V>
+__device__ __forceinline__ V block_scan(V v, V *red, V *total) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  v = wave_scan64(v);
+  v = wave_scan(v);
   if (lane == 63) red[w] = v;
   __syncthreads();
-  uint64_t before = 0, all = 0;
+  V before = 0, all = 0;
   for (int i = 0; i < kSampWaves; ++i) {
     if (i < w) before += red[i];
     all += red[i];
@@ -112,394 +152,495 @@ __device__ __forceinline__ uint64_t block_scan64(uint64_t v, uint64_t *red, uint
   return v + before;
 }
 
-__device__ __forceinline__ double block_scan_f64(double v, double *red) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+// (An atomic minimum of every lane's own value at one place would be taken lane
+// by lane: 64 rounds.  These leave one a wave.)
+__device__ __forceinline__ uint32_t wave_min_u32(uint32_t v) {
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const double u = __shfl_up(v, d, kWave);
-    if (lane >= d) v += u;
-  }
-  if (lane == 63) red[w] = v;
+  for (int m = 1; m < 64; m <<= 1) v = min(v, (uint32_t)__shfl_xor((int)v, m, kWave));
+  return v;
+}
+// The least value over the workgroup of the threads that have one, kNone of
+// none; values ascend with the thread.  red: one value a wave.
+constexpr int kNone = 0x7fffffff;
+__device__ __forceinline__ int block_first(bool has, int value, int *red) {
+  const int w = threadIdx.x >> 6;
+  const uint64_t who = __ballot(has);
+  const int first = __shfl(value, who ? __builtin_ctzll(who) : 0, kWave);
+  if ((threadIdx.x & 63) == 0) red[w] = who ? first : kNone;
   __syncthreads();
-  double before = 0;
-  for (int i = 0; i < w; ++i) before += red[i];
+  int least = kNone;
+  for (int i = kSampWaves - 1; i >= 0; --i)
+    if (red[i] != kNone) least = red[i];
   __syncthreads();
-  return v + before;
+  return least;
 }
 
-struct SampleShared {
-  uint64_t mass[kBins];          // of a cut's bins, or of the pieces
-  uint32_t count[kBins];         // of a cut's bins, or of the pieces' ties
-  uint64_t list[kList];          // key << 32 | token
-  double table[128];
-  uint64_t red[kSampWaves];
-  float fred[kSampWaves];
-  uint64_t before;               // mass (or count) above the bin
-  int bin, last, bad, listed;
-  uint32_t klo, khi;
-  uint64_t above;
-};
-static_assert(kMostPieces <= kSampThreads && kMostPieces <= kBins, "a piece a thread");
+// ---- a row -----------------------------------------------------------------
 
-// A row, or what is left of it: tokens with keys above `tie`, and `ties` of those equal to it.
+// Tokens with keys above `tie`, and `ties` of those equal to it.
 struct Kept {
   uint32_t tie;
-  uint64_t ties;
+  uint32_t ties;
 };
 
+enum Mode {
+  kPlain,  // the pieces' masses, of the tokens that min_p keeps (greedy: of the largest alone)
+  kListK,  // list the bins that hold the first k
+  kListM,  // list the tokens that min_p keeps, or that weigh anything
+  kMass,   // top-p over everything: list the bins in which it ends, weigh what is above
+};
+
+struct Settings {
+  bool fine;
+  Mode mode;
+  int k;        // 0: all
+  float p, u;
+  double c;     // log2 e / temperature
+  double lm;    // least exponent that min_p keeps
+  bool greedy;
+};
+
+__device__ __forceinline__ Settings settings_of(const SampleArgs &a, int64_t r) {
+  const float t = a.temperature ? a.temperature[r] : 1.f, p = a.top_p ? a.top_p[r] : 1.f, m = a.min_p ? a.min_p[r] : 0.f;
+  const int k = a.top_k ? a.top_k[r] : 0;
+  Settings s;
+  s.u = a.u[r];
+  s.fine = t >= 0.f && t < INFINITY && p >= 0.f && m >= 0.f && m <= 1.f && s.u >= 0.f && s.u < 1.f && k >= 0;
+  s.greedy = t == 0.f || k == 1;
+  s.k = k < a.vocab ? k : 0;
+  s.p = p;
+  s.c = t > 0.f ? kLog2eD / (double)t : kLog2eD;
+  s.lm = m > 0.f ? log2((double)m) : -INFINITY;
+  s.mode = s.greedy ? kPlain : s.k > 0 ? kListK : p >= 1.f ? kPlain : m > 0.f || t < kSharpest ? kListM : kMass;
+  return s;
+}
+
+// A row's logits.
 template <typename T>
 struct Row {
   const T *x;
   int vocab;
   float M;
-  double c;    // log2 e / temperature
-  double lm;   // log2 min_p (least exponent that is kept)
-  float bin_scale;
+  double c;
+  float origin;  // of the bins
 
-  // The eight logits of this lane in piece p, -infinity behind the last.
-  __device__ __forceinline__ void load(int p, float (&f)[8]) const {
+  __device__ __forceinline__ Row(const SampleArgs &a, int64_t r) : x((const T *)a.logits + r * a.stride), vocab(a.vocab) {}
+
+  // The eight logits of this lane in piece p, -infinity behind the last, as they
+  // lie in memory, and as floats.
+  struct Eight {
+    T t[8];
+    __device__ __forceinline__ float operator[](int e) const { return Elem<T>::load(t + e); }
+  };
+  __device__ __forceinline__ Eight raw(int p) const {
     const int at = p * kPiece + 8 * (threadIdx.x & 63);
+    Eight f;
     if (at + 8 <= vocab) {
-      T t[8];
-      __builtin_memcpy(t, x + at, sizeof t);  // (any element-aligned address)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] = Elem<T>::load(t + e);
+      __builtin_memcpy(f.t, x + at, sizeof f.t);  // (any element-aligned address)
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] = at + e < vocab ? Elem<T>::load(x + at + e) : -INFINITY;
+      for (int e = 0; e < 8; ++e) f.t[e] = at + e < vocab ? x[at + e] : Elem<T>::to_store(-INFINITY);
+    }
+    return f;
+  }
+  __device__ __forceinline__ int pieces() const { return (vocab + kPiece - 1) / kPiece; }
+  // g(eight logits, piece) of this wave's pieces among [p0, p1).
+  template <class G>
+  __device__ __forceinline__ void each_piece(int p0, int p1, G g) const {
+    for (int p = p0 + (threadIdx.x >> 6); p < p1; p += kInFlight * kSampWaves) {
+      Eight f[kInFlight];
+#pragma unroll
+      for (int i = 0; i < kInFlight; ++i) f[i] = raw(min(p + i * kSampWaves, p1 - 1));
+#pragma unroll 1
+      for (int i = 0; i < kInFlight; ++i) {
+        if (p + i * kSampWaves < p1) g(f[0], p + i * kSampWaves);
+#pragma unroll
+        for (int j = 1; j < kInFlight; ++j) f[j - 1] = f[j];
+      }
     }
   }
   __device__ __forceinline__ double exponent(float v) const { return ((double)v - (double)M) * c; }
-  __device__ __forceinline__ int pieces() const { return (vocab + kPiece - 1) / kPiece; }
-  // How far below M, in bins; descends as v ascends.
-  __device__ __forceinline__ float depth(float v) const { return (M - v) * bin_scale; }
-  __device__ __forceinline__ int bin(float v) const {
-    const float d = depth(v);
-    return d < (float)(kBins - 1) ? (int)d : kBins - 1;
-  }
-  // The masses of this lane's tokens in piece p above the tie, and which are equal to it.
-  __device__ __forceinline__ void weights(int p, const Kept &kept, const double *table, uint64_t (&m)[8], uint32_t &tied) const {
-    float f[8];
-    load(p, f);
-    tied = 0;
+
+  // The bins descend as the logits ascend.
+  __device__ __forceinline__ void set_origin() {
+    float top = -INFINITY;
+    const Eight f = raw(0);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t key = order_key(f[e]);
-      m[e] = 0;
-      if (f[e] > -INFINITY && key > kept.tie) {
-        const double ex = exponent(f[e]);
-        if (ex >= lm) m[e] = unit_weight(ex, table);
-      }
-      tied |= (uint32_t)(kept.ties > 0 && key == kept.tie && f[e] > -INFINITY) << e;
-    }
+    for (int e = 0; e < 8; ++e) top = fmaxf(top, f[e]);
+    top = wave_max(top);
+    origin = fabsf(top) < INFINITY ? top : 0.f;
   }
-  // f(value, token) of the tokens of this wave's pieces
-  template <class F>
-  __device__ __forceinline__ void each(F f) const {
-    for (int p = threadIdx.x >> 6; p < pieces(); p += kSampWaves) {
-      float v[8];
-      load(p, v);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) f(v[e], p * kPiece + 8 * (int)(threadIdx.x & 63) + e);
-    }
+  __device__ __forceinline__ float depth(float v) const {
+    return fmaxf((origin - v) * kBinsPerUnit + (float)kBinsAbove, 0.f);
   }
+  __device__ __forceinline__ int bin(float v) const { return (int)fminf(depth(v), (float)(kBins - 1)); }
 };
 
-// What a cut looks at: the tokens of a row with keys above the tie, or those of
-// them that are listed (a range of bins, complete).
+// ---- scan ------------------------------------------------------------------
+
+// A bin's masses are parts of its largest, 2^(-its depth's exponent), in whole
+// numbers of which all the tokens together stay below 2^32.
+__device__ __forceinline__ float mass_one(int vocab) { return (float)(1 << (31 - (32 - __clz((vocab - 1) | 1)))); }
+__device__ __forceinline__ float log2_per_bin(const Settings &s) { return (float)(s.c * (1.0 / (16.0 * kLog2eD))); }
+
+template <typename T>
+__global__ __launch_bounds__(kSampThreads) void sample_scan_kernel(SampleArgs a) {
+  __shared__ uint32_t bins[kBins];
+  const int t = threadIdx.x, lane = t & 63;
+  const int64_t r = blockIdx.x / a.slices;
+  const int p0 = (int)(blockIdx.x % a.slices) * a.per_slice;
+  Row<T> row(a, r);
+  const int p1 = min(p0 + a.per_slice, row.pieces());
+  RowState &st = a.state[r];
+  const Settings s = settings_of(a, r);
+  if (!s.fine) return;
+  const bool counts = s.mode == kListK, masses = s.mode == kMass;
+  float M = -INFINITY;
+  bool nan = false;
+  if (counts || masses) {
+    for (int i = t; i < kBins; i += kSampThreads) bins[i] = 0;
+    row.set_origin();
+    const float one = mass_one(a.vocab), slope = log2_per_bin(s);
+    __syncthreads();
+    row.each_piece(p0, p1, [&](const typename Row<T>::Eight &f, int) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float v = f[e];
+        nan |= v != v;
+        M = fmaxf(M, v);
+        const float d = row.depth(v), b = floorf(fminf(d, (float)(kBins - 1)));
+        const uint32_t part = masses ? (uint32_t)fmaf(__builtin_amdgcn_exp2f((b - d) * slope), one, 0.5f) : 1u;
+        if (v > -INFINITY) atomicAdd(&bins[(int)b], part);
+      }
+    });
+    __syncthreads();
+    for (int i = t; i < kBins; i += kSampThreads)
+      if (bins[i]) atomicAdd(&st.bins[i], bins[i]);
+  } else {
+    row.each_piece(p0, p1, [&](const typename Row<T>::Eight &f, int) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        nan |= f[e] != f[e];
+        M = fmaxf(M, f[e]);
+      }
+    });
+  }
+  M = wave_max(M);
+  const bool any = __ballot(nan) != 0;
+  if (lane == 0) {
+    if (M > -INFINITY) atomicMax(&st.top, order_key(M));
+    if (any) atomicOr(&st.bad, 1u);
+  }
+}
+
+// ---- weigh -----------------------------------------------------------------
+
+// A range of bins: [first, last] are listed, what is above counts as it is.
+struct Range {
+  int first, last;
+};
+
+// The bins in which the first k tokens, or the masses' first part p, end (all,
+// if there are no more than k; none: masses that came to nothing).  All threads.
+__device__ __forceinline__ Range end_bins(const RowState &st, const Settings &s, float top_depth, int vocab, uint64_t *red) {
+  constexpr int N = kBins / kSampThreads;
+  const int t = threadIdx.x;
+  u32x4_t raw[N / 4];
+#pragma unroll
+  for (int i = 0; i < N / 4; ++i) raw[i] = *(const u32x4_t *)(st.bins + N * t + 4 * i);
+  if (s.mode == kListK) {
+    uint64_t n = 0, total;
+#pragma unroll
+    for (int i = 0; i < N; ++i) n += raw[i / 4][i % 4];
+    uint64_t at = block_scan(n, red, &total) - n;
+    const bool here = at < (uint64_t)s.k && at + n >= (uint64_t)s.k;
+    int b = 0;
+#pragma unroll
+    for (int i = N - 1; i >= 0; --i) {  // the first bin at which k are reached
+      if (at + n >= (uint64_t)s.k) b = i;
+      n -= raw[i / 4][i % 4];
+    }
+    const int last = block_first(here, N * t + b, (int *)red);
+    return Range{0, min(last, kBins - 1)};
+  }
+  // masses relative to the bin of M, in fp32: the slack takes the roundings of
+  // these sums and, as a rule, those of the histogram; where they come to more,
+  // the masses of full precision tell
+  const float one = mass_one(vocab), per_bin = log2_per_bin(s), from = floorf(fminf(top_depth, (float)(kBins - 1)));
+  float m[N], sum = 0.f, total;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint32_t n = raw[i / 4][i % 4];  // (none above M's bin)
+    m[i] = n ? (float)n * (1.f / one) * __builtin_amdgcn_exp2f((from - (float)(N * t + i)) * per_bin) : 0.f;
+    sum += m[i];
+  }
+  float at = block_scan(sum, (float *)red, &total);
+  const float slack = (0.5f / one + 2e-6f) * total, lo = s.p * total - slack, hi = s.p * total + slack;
+  int b1 = kNone, b2 = kNone;
+#pragma unroll
+  for (int i = N - 1; i >= 0; --i) {
+    if (at >= lo) b1 = N * t + i;
+    if (at >= hi) b2 = N * t + i;
+    at -= m[i];
+  }
+  b1 = block_first(b1 != kNone, b1, (int *)red);
+  b2 = block_first(b2 != kNone, b2, (int *)red);
+  return Range{b1, min(b2, kBins - 1)};
+}
+
+// tokens that a workgroup of `weigh` gathers before it takes their places in the row's list
+constexpr int kSliceList = 1024;
+
+template <typename T>
+__global__ __launch_bounds__(kSampThreads) void sample_weigh_kernel(SampleArgs a) {
+  __shared__ double table[128];
+  __shared__ uint64_t list[kSliceList], red[kSampWaves];
+  __shared__ int listed, place;
+  const int t = threadIdx.x, lane = t & 63;
+  const int64_t r = blockIdx.x / a.slices;
+  const int p0 = (int)(blockIdx.x % a.slices) * a.per_slice;
+  Row<T> row(a, r);
+  const int p1 = min(p0 + a.per_slice, row.pieces());
+  RowState &st = a.state[r];
+  const Settings s = settings_of(a, r);
+  const uint32_t top = st.top;
+  row.M = value_of_key(top);
+  if (!s.fine || st.bad || top == 0 || !(row.M < INFINITY)) return;
+  row.c = s.c;
+  fill_table(table);
+  if (t == 0) listed = 0;
+  Range range{0, -1};
+  if (s.mode == kListK || s.mode == kMass) {
+    row.set_origin();
+    range = end_bins(st, s, row.depth(row.M), a.vocab, red);
+    if (range.first == kNone) {  // (masses that came to nothing)
+      if (t == 0 && p0 == 0) atomicAdd(&st.listed, kList + 1);
+      return;
+    }
+  }
+  __syncthreads();
+  const auto add = [&](float v, int token) {
+    const int at = atomicAdd(&listed, 1);
+    if (at < kSliceList) list[at] = (uint64_t)order_key(v) << 32 | (uint32_t)token;
+  };
+  const double lm = s.mode == kListM ? fmax(s.lm, kLeast) : s.lm;
+  if (s.mode == kListK) {
+    row.each_piece(p0, p1, [&](const typename Row<T>::Eight &f, int p) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (f[e] > -INFINITY && row.bin(f[e]) <= range.last) add(f[e], p * kPiece + 8 * lane + e);
+    });
+  } else if (s.mode == kListM) {
+    row.each_piece(p0, p1, [&](const typename Row<T>::Eight &f, int p) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (f[e] > -INFINITY && row.exponent(f[e]) >= lm) add(f[e], p * kPiece + 8 * lane + e);
+    });
+  } else if (s.mode == kMass) {
+    uint64_t S = 0;
+    row.each_piece(p0, p1, [&](const typename Row<T>::Eight &f, int p) {
+      uint64_t above = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint64_t m = f[e] > -INFINITY ? unit_weight(row.exponent(f[e]), table) : 0;
+        const int b = row.bin(f[e]);
+        S += m;
+        above += b < range.first ? m : 0;
+        if (b >= range.first && b <= range.last && f[e] > -INFINITY) add(f[e], p * kPiece + 8 * lane + e);
+      }
+      above = wave_sum64(above);
+      if (lane == 0) st.pieces[p] = above;
+    });
+    S = wave_sum64(S);
+    if (lane == 0) atomicAdd((unsigned long long *)&st.mass, S);
+  } else if (s.greedy) {
+    row.each_piece(p0, p1, [&](const typename Row<T>::Eight &f, int p) {
+      int n = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) n += __popcll(__ballot(order_key(f[e]) == top));
+      if (lane == 0) st.pieces[p] = (uint64_t)n << 54;
+    });
+  } else {
+    row.each_piece(p0, p1, [&](const typename Row<T>::Eight &f, int p) {
+      uint64_t sum = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const double ex = row.exponent(f[e]);
+        if (f[e] > -INFINITY && ex >= lm) sum += unit_weight(ex, table);
+      }
+      sum = wave_sum64(sum);
+      if (lane == 0) st.pieces[p] = sum;
+    });
+  }
+  if (s.mode == kPlain) return;
+  __syncthreads();
+  if (t == 0) place = (int)atomicAdd(&st.listed, listed <= kSliceList ? (uint32_t)listed : kList + 1u);
+  __syncthreads();
+  const int at = place;
+  for (int i = t; i < min(listed, kSliceList) && at + i < kList; i += kSampThreads) st.list[at + i] = list[i];
+}
+
+// ---- choose ----------------------------------------------------------------
+
+struct ChooseShared {
+  uint64_t mass[kCutBins];       // of a cut's bins, or of the pieces
+  uint32_t count[kCutBins];      // of a cut's bins, or of the pieces' ties
+  uint64_t list[kList];
+  double table[128];
+  uint64_t red[kSampWaves];
+  uint64_t before;               // mass (or count) above the bin
+  int bin, left;
+  uint32_t klo, khi;
+};
+static_assert(kMostPieces <= kCutBins, "the pieces in the bins' place");
+constexpr int kPer = kCutBins / kSampThreads;  // bins, or pieces, of a thread
+
+// f(value, key, token) of the row's list, as it is in LDS, or of all its
+// tokens above -infinity.
 template <typename T>
 struct Tokens {
   const Row<T> &row;
-  const SampleShared &sh;
-  Kept kept;
-  bool listed;
+  const ChooseShared &sh;
+  int listed;  // below 0: the whole row
   template <class F>
-  __device__ __forceinline__ void each(F f) const {  // f(value, key)
-    if (listed) {
-      for (int i = threadIdx.x; i < sh.listed; i += kSampThreads) {
+  __device__ __forceinline__ void each(F f) const {
+    if (listed >= 0) {
+      for (int i = threadIdx.x; i < listed; i += kSampThreads) {
         const uint32_t key = (uint32_t)(sh.list[i] >> 32);
-        f(value_of_key(key), key);
+        f(value_of_key(key), key, (int)(uint32_t)sh.list[i]);
       }
     } else {
-      row.each([&](float v, int) {
-        const uint32_t key = order_key(v);
-        if (v > -INFINITY && key > kept.tie && row.exponent(v) >= row.lm) f(v, key);
-      });
+      for (int p = threadIdx.x >> 6; p < row.pieces(); p += kSampWaves) {
+        const typename Row<T>::Eight v = row.raw(p);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (v[e] > -INFINITY) f(v[e], order_key(v[e]), p * kPiece + 8 * (int)(threadIdx.x & 63) + e);
+      }
     }
   }
 };
 
-// The smallest start of these tokens in descending order at which `before`
-// plus their amount (MASS: of their masses; else their number) reaches the
-// target; ties: how many more of the tie's value there are (the last of all).
-// All threads; returns the same in each.  Rounds of 2048 bins, the first by
-// M - x, the others by keys, until a single value is left.
+// The smallest start of the kept ones of these tokens, in descending order, at
+// which `before` plus their amount (MASS: of their masses; else their number)
+// reaches the target.  All threads; returns the same in each.  Rounds of 1024
+// bins over keys from the largest down, until a single value is left.
 template <bool MASS, typename T>
-__device__ Kept cut(const Row<T> &row, const Tokens<T> &tokens, uint64_t before, double target, bool tie_in, SampleShared &sh) {
+__device__ __noinline__ Kept cut(const Row<T> &row, const Tokens<T> &tokens, Kept kept, double lm, uint64_t before, double target,
+                                 ChooseShared &sh) {
   const int t = threadIdx.x;
-  const Kept kept = tokens.kept;
   const auto amount = [&](float v) { return MASS ? unit_weight(row.exponent(v), sh.table) : (uint64_t)1; };
   const float tie_value = value_of_key(kept.tie);
-  uint32_t klo = 0, khi = 0;
-  int shift = -1, bin = 0;
+  const bool tie_in = kept.ties > 0 && row.exponent(tie_value) >= lm;
+  uint32_t klo = 0, khi = 0xffffffffu;
   for (;;) {
-    for (int i = t; i < kBins; i += kSampThreads) sh.mass[i] = sh.count[i] = 0;
-    if (t == 0) sh.bin = kBins;
-    __syncthreads();
-    const auto place = [&](float v, uint32_t key) { return shift < 0 ? row.bin(v) : (int)((khi - key) >> shift); };
-    const auto inside = [&](float v, uint32_t key) { return shift < 0 || (key >= klo && key <= khi && row.bin(v) == bin); };
-    tokens.each([&](float v, uint32_t key) {
-      if (!inside(v, key)) return;
-      const int b = place(v, key);
-      atomicAdd(&sh.count[b], 1u);
-      if constexpr (MASS) atomicAdd((unsigned long long *)&sh.mass[b], amount(v));
-    });
-    if (t == 0 && tie_in && inside(tie_value, kept.tie)) {
-      const int b = place(tie_value, kept.tie);
-      atomicAdd(&sh.count[b], (uint32_t)kept.ties);
-      if constexpr (MASS) atomicAdd((unsigned long long *)&sh.mass[b], kept.ties * amount(tie_value));
-    }
-    __syncthreads();
-    uint64_t mine[2], total;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) mine[i] = MASS ? sh.mass[2 * t + i] : sh.count[2 * t + i];
-    const uint64_t end = block_scan64(mine[0] + mine[1], sh.red, &total) + before;
-    total += before;
-    // the first bin with a token at which the target is reached, or the last with one
-    const uint64_t ends[2] = {end - mine[1], end};
-#pragma unroll
-    for (int i = 1; i >= 0; --i)
-      if (sh.count[2 * t + i] && ((double)ends[i] >= target || ends[i] == total)) atomicMin(&sh.bin, 2 * t + i);
+    // ---- least and largest key ----
     if (t == 0) {
       sh.klo = 0xffffffffu;
       sh.khi = 0;
     }
+    for (int i = t; i < kCutBins; i += kSampThreads) sh.mass[i] = sh.count[i] = 0;
     __syncthreads();
-    const int b = sh.bin;
-    if (b >= kBins) return kept;  // no tokens
-    if (b >> 1 == t) sh.before = ends[b & 1] - mine[b & 1];
-    const uint32_t n = sh.count[b];
-    const uint64_t sum = MASS ? sh.mass[b] : n;
-    // its least and largest key
     uint32_t lo = 0xffffffffu, hi = 0;
-    const auto see = [&](float v, uint32_t key) {
-      if (!inside(v, key) || place(v, key) != b) return;
+    tokens.each([&](float v, uint32_t key, int) {
+      if (key <= kept.tie || key < klo || key > khi || row.exponent(v) < lm) return;
       lo = min(lo, key);
       hi = max(hi, key);
-    };
-    tokens.each(see);
-    if (t == 0 && tie_in) see(tie_value, kept.tie);
-    if (hi) {
+    });
+    if (t == 0 && tie_in && kept.tie >= klo && kept.tie <= khi) {
+      lo = min(lo, kept.tie);
+      hi = max(hi, kept.tie);
+    }
+    lo = wave_min_u32(lo);
+    hi = ~wave_min_u32(~hi);
+    if ((t & 63) == 0 && hi) {
       atomicMin(&sh.klo, lo);
       atomicMax(&sh.khi, hi);
     }
     __syncthreads();
     klo = sh.klo;
     khi = sh.khi;
+    if (khi == 0) return kept;  // no tokens
+    int shift = 0;
+    while ((khi - klo) >> shift >= (uint32_t)kCutBins) ++shift;
+    // ---- amounts by bins ----
+    tokens.each([&](float v, uint32_t key, int) {
+      if (key <= kept.tie || key < klo || key > khi || row.exponent(v) < lm) return;
+      const int b = (khi - key) >> shift;
+      atomicAdd(&sh.count[b], 1u);
+      if constexpr (MASS) atomicAdd((unsigned long long *)&sh.mass[b], amount(v));
+    });
+    if (t == 0 && tie_in && kept.tie >= klo && kept.tie <= khi) {
+      const int b = (khi - kept.tie) >> shift;
+      atomicAdd(&sh.count[b], kept.ties);
+      if constexpr (MASS) atomicAdd((unsigned long long *)&sh.mass[b], kept.ties * amount(tie_value));
+    }
+    __syncthreads();
+    uint64_t mine[kPer], sum = 0, total;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      mine[i] = MASS ? sh.mass[kPer * t + i] : sh.count[kPer * t + i];
+      sum += mine[i];
+    }
+    uint64_t at = block_scan(sum, sh.red, &total) + before - sum;
+    total += before;
+    // the first bin with a token at which the target is reached, or the last with one
+    int mine_first = kNone;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      at += mine[i];
+      if (mine_first == kNone && sh.count[kPer * t + i] && ((double)at >= target || at == total)) mine_first = kPer * t + i;
+    }
+    const int b = block_first(mine_first != kNone, mine_first, (int *)sh.red);
+    if (b / kPer == t) {
+      uint64_t end = at;
+#pragma unroll
+      for (int i = kPer - 1; i >= 0; --i)
+        if (i >= b % kPer) end -= mine[i];
+      sh.before = end;
+    }
+    __syncthreads();
     before = sh.before;
-    if (klo == khi) {  // one value: its first few
-      const double each = (double)(sum / n), need = (target - (double)before) / each;
-      const uint64_t few = each > 0 && need < (double)n ? (need > 1.0 ? (uint64_t)ceil(need) : 1) : n;
-      return Kept{klo, few};
+    const uint32_t n = sh.count[b];
+    const uint64_t amounts = MASS ? sh.mass[b] : n;
+    const uint32_t lower = khi - min(khi - klo, ((uint32_t)(b + 1) << shift) - 1), upper = khi - ((uint32_t)b << shift);
+    if (lower == upper) {  // one value: its first few
+      const double each = (double)(amounts / n), need = (target - (double)before) / each;
+      const uint32_t few = each > 0 && need < (double)n ? (need > 1.0 ? (uint32_t)ceil(need) : 1u) : n;
+      return Kept{lower, few};
     }
-    if (shift < 0) bin = b;
-    shift = 0;
-    while ((khi - klo) >> shift >= (uint32_t)kBins) ++shift;
+    klo = lower;
+    khi = upper;
     __syncthreads();
-  }
-}
-
-// Adds token (key, index) to the list; past its end only the count goes on.
-__device__ __forceinline__ void list_token(SampleShared &sh, uint32_t key, int token) {
-  const int at = atomicAdd(&sh.listed, 1);
-  if (at < kList) sh.list[at] = (uint64_t)key << 32 | (uint32_t)token;
-}
-
-// The first k tokens (lower index first among equal ones).
-template <typename T>
-__device__ Kept first_k(const Row<T> &row, int k, SampleShared &sh) {
-  const int t = threadIdx.x;
-  const Kept all{0, 0};
-  for (int i = t; i < kBins; i += kSampThreads) sh.count[i] = 0;
-  if (t == 0) {
-    sh.bin = kBins;
-    sh.listed = 0;
-  }
-  __syncthreads();
-  row.each([&](float v, int) {
-    if (v > -INFINITY) atomicAdd(&sh.count[row.bin(v)], 1u);
-  });
-  __syncthreads();
-  const uint32_t c0 = sh.count[2 * t], c1 = sh.count[2 * t + 1];
-  uint64_t total;
-  const uint64_t end = block_scan64(c0 + c1, sh.red, &total);
-  if (total <= (uint64_t)k) return all;  // (-infinity has no place)
-  if (end >= (uint64_t)k && end - c0 - c1 < (uint64_t)k) {
-    const bool second = end - c1 < (uint64_t)k;
-    sh.bin = 2 * t + second;
-    sh.before = end - c1 - (second ? 0 : c0);
-  }
-  __syncthreads();
-  const int b = sh.bin;
-  const uint64_t before = sh.before;
-  row.each([&](float v, int token) {
-    if (v > -INFINITY && row.bin(v) == b) list_token(sh, order_key(v), token);
-  });
-  __syncthreads();
-  const bool listed = sh.listed <= kList;
-  return cut<false>(row, Tokens<T>{row, sh, all, listed}, listed ? before : 0, (double)k, false, sh);
-}
-
-// The start of the kept tokens before whose last lies less than `part` of their
-// mass.  True: the pieces' kept masses and ties are in sh.mass and sh.count.
-template <typename T>
-__device__ bool first_mass(const Row<T> &row, Kept &kept, double part, SampleShared &sh) {
-  const int t = threadIdx.x, w = t >> 6, lane = t & 63, pieces = row.pieces();
-  const float tie_value = value_of_key(kept.tie);
-  const uint64_t tie_each = kept.ties > 0 ? unit_weight(row.exponent(tie_value), sh.table) : 0;
-  // a bin's masses as parts of its largest, in whole numbers of `bits` bits: no sum of them passes 32
-  int bits = 31;
-  while (bits > 0 && (row.vocab - 1) >> (31 - bits)) --bits;
-  const float one = (float)(1 << bits), least = -(float)kLeast * kBinsPerLog2;
-  for (int i = t; i < kBins; i += kSampThreads) sh.count[i] = 0;
-  if (t == 0) {
-    sh.bin = sh.last = kBins;
-    sh.listed = 0;
-    sh.above = 0;
-  }
-  __syncthreads();
-  const float floor_depth = row.lm > -INFINITY ? (float)-row.lm * kBinsPerLog2 : INFINITY;
-  const auto approximate = [&](float v) {
-    const float d = row.depth(v), b = floorf(d);
-    if (d < least && d <= floor_depth)
-      atomicAdd(&sh.count[(int)b], (uint32_t)(__builtin_amdgcn_exp2f((b - d) * (1.f / kBinsPerLog2)) * one + 0.5f));
-  };
-  row.each([&](float v, int) {
-    if (order_key(v) > kept.tie) approximate(v);  // (-infinity is too deep)
-  });
-  __syncthreads();
-  // Bin b's largest weight is 2^(-b / 16).  The slack is what the roundings come
-  // to as a rule; where they come to more, the masses below tell.
-  double mine[2];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) mine[i] = (double)sh.count[2 * t + i] * exp2((double)-(2 * t + i) / kBinsPerLog2) / one;
-  if (kept.ties > 0) {
-    const float d = row.depth(tie_value);
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      if (d < least && (int)d == 2 * t + i) mine[i] += (double)(kept.ties * tie_each) * 0x1p-44;
-  }
-  const double end = block_scan_f64(mine[0] + mine[1], (double *)sh.red);
-  if (t == kSampThreads - 1) *(double *)&sh.before = end;
-  __syncthreads();
-  const double all = *(double *)&sh.before, slack = 0.5 / one + 1e-6, target_a = part * all;
-  const double ends[2] = {end - mine[1], end};
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    if (ends[i] >= target_a - slack * all) atomicMin(&sh.bin, 2 * t + i);
-    if (ends[i] >= target_a + slack * all) atomicMin(&sh.last, 2 * t + i);
-  }
-  __syncthreads();
-  // ---- the masses above the bins in which the end lies, and their tokens ----
-  const int b1 = sh.bin, b2 = sh.last;
-  uint64_t S = 0;
-  for (int p = w; p < pieces; p += kSampWaves) {
-    uint64_t m[8], above = 0;
-    float f[8];
-    row.load(p, f);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t key = order_key(f[e]);
-      m[e] = 0;
-      if (f[e] > -INFINITY && key > kept.tie) {
-        const double ex = row.exponent(f[e]);
-        if (ex >= row.lm) {
-          m[e] = unit_weight(ex, sh.table);
-          const int b = row.bin(f[e]);
-          if (b < b1) above += m[e];
-          else if (b <= b2) list_token(sh, key, p * kPiece + 8 * lane + e);
-        }
-      }
-      S += m[e];
-    }
-    above = wave_sum64(above);
-    if (lane == 0) sh.mass[p] = above;
-  }
-  S = wave_sum64(S);
-  if (lane == 0) atomicAdd((unsigned long long *)&sh.above, S);
-  __syncthreads();
-  S = sh.above + kept.ties * tie_each;
-  uint64_t above;
-  {
-    const uint64_t a = t < pieces ? sh.mass[t] : 0;
-    block_scan64(a, sh.red, &above);
-    __syncthreads();
-    // (the cut's bins take the place of the pieces)
-    const double target = part * (double)S;
-    const int tie_bin = kept.ties > 0 ? row.bin(tie_value) : kBins;
-    const bool tie_above = tie_bin < b1, tie_in = tie_bin >= b1 && tie_bin <= b2;
-    if (tie_above) above += kept.ties * tie_each;
-    uint64_t inside = 0, rest;
-    const bool whole = sh.listed <= kList;
-    if (whole)
-      for (int i = t; i < sh.listed; i += kSampThreads)
-        inside += unit_weight(row.exponent(value_of_key((uint32_t)(sh.list[i] >> 32))), sh.table);
-    if (t == 0 && tie_in) inside += kept.ties * tie_each;
-    block_scan64(inside, sh.red, &rest);
-    if (!whole || (double)above >= target || (double)(above + rest) < target) {
-      kept = cut<true>(row, Tokens<T>{row, sh, kept, false}, 0, target, kept.ties > 0, sh);
-      return false;
-    }
-    const Kept was = kept;
-    kept = cut<true>(row, Tokens<T>{row, sh, was, true}, above, target, tie_in, sh);
-    __syncthreads();
-    for (int i = t; i < kBins; i += kSampThreads) sh.count[i] = 0;
-    sh.mass[t] = a;
-    __syncthreads();
-    for (int i = t; i < sh.listed; i += kSampThreads) {
-      const uint32_t key = (uint32_t)(sh.list[i] >> 32), token = (uint32_t)sh.list[i];
-      if (key > kept.tie)
-        atomicAdd((unsigned long long *)&sh.mass[token / kPiece], unit_weight(row.exponent(value_of_key(key)), sh.table));
-      else if (key == kept.tie) atomicAdd(&sh.count[token / kPiece], 1u);
-    }
-    __syncthreads();
-    return kept.tie != was.tie;  // (the tokens of the tie itself are not listed)
   }
 }
 
 template <typename T>
-__global__ __launch_bounds__(kSampThreads) void sample_kernel(SampleArgs a) {
-  __shared__ SampleShared sh;
+__global__ __launch_bounds__(kSampThreads) void sample_choose_kernel(SampleArgs a) {
+  __shared__ ChooseShared sh;
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
-  const int64_t r = a.first + blockIdx.x;
-  Row<T> row;
-  row.x = (const T *)a.logits + r * a.stride;
-  row.vocab = a.vocab;
-  if (t < 128) sh.table[t] = exp2(t / 128.0);
-  if (t == 0) sh.bad = 0;
-  // ---- the largest logit ----
-  float M = -INFINITY;
-  bool nan = false;
-  for (int p = w; p < row.pieces(); p += kSampWaves) {
-    float f[8];
-    row.load(p, f);
+  const int64_t r = blockIdx.x;
+  Row<T> row(a, r);
+  RowState &st = a.state[r];
+  Settings s = settings_of(a, r);
+  const uint32_t top = st.top;
+  const int listed = (int)min(st.listed, kList + 1u);
+  const uint64_t mass = st.mass;
+  row.M = value_of_key(top);
+  row.c = s.c;
+  const bool fine = s.fine && !st.bad && top != 0 && row.M < INFINITY;
+  fill_table(sh.table);
+  if (fine && listed <= kList)
+    for (int i = t; i < listed; i += kSampThreads) sh.list[i] = st.list[i];
+  const int pieces = row.pieces();
+  uint64_t mine[kPer];  // the pieces of this thread: ties << 54 | mass
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      nan |= f[e] != f[e];
-      M = fmaxf(M, f[e]);
-    }
-  }
-  M = wave_max(M);
-  if (lane == 0) sh.fred[w] = M;
+  for (int i = 0; i < kPer; ++i)
+    mine[i] = fine && (s.mode == kPlain || s.mode == kMass) && kPer * t + i < pieces ? st.pieces[kPer * t + i] : 0;
   __syncthreads();
-  for (int i = 0; i < kSampWaves; ++i) M = fmaxf(M, sh.fred[i]);
-  if (__ballot(nan) != 0 && lane == 0) sh.bad = 1;
-  __syncthreads();
-  const float temp = a.temperature ? a.temperature[r] : 1.f, top_p = a.top_p ? a.top_p[r] : 1.f;
-  const float min_p = a.min_p ? a.min_p[r] : 0.f, u = a.u[r];
-  const int top_k = a.top_k ? a.top_k[r] : 0;
-  const bool fine = temp >= 0.f && temp < INFINITY && top_p >= 0.f && min_p >= 0.f && min_p <= 1.f && u >= 0.f && u < 1.f &&
-                    top_k >= 0 && !sh.bad && M < INFINITY && M > -INFINITY;
+  // ---- the row's state is zero again ----
+  if (t < 4) (&st.top)[t] = 0;
+  if (t == 4) st.mass = 0;
+  for (int i = t; i < kBins / 4; i += kSampThreads) *(u32x4_t *)(st.bins + 4 * i) = u32x4_t{0u, 0u, 0u, 0u};
   if (!fine) {
     if (t == 0) {
       a.tokens[r] = -1;
@@ -508,78 +649,132 @@ __global__ __launch_bounds__(kSampThreads) void sample_kernel(SampleArgs a) {
     }
     return;
   }
-  row.M = M;
-  row.c = temp > 0.f ? kLog2eD / (double)temp : kLog2eD;
-  row.bin_scale = kBinsPerLog2 * (float)row.c;
   // ---- the filters ----
   Kept kept{0, 0};  // (no finite logit has key 0)
-  const double lm = min_p > 0.f ? log2((double)min_p) : -INFINITY;
-  row.lm = -INFINITY;  // (the first k whatever they weigh)
-  if (temp == 0.f || top_k == 1) kept = Kept{order_key(M), 1};
-  else if (top_k > 0 && top_k < a.vocab) kept = first_k(row, top_k, sh);
-  row.lm = lm;
-  if (kept.ties > 0 && row.exponent(value_of_key(kept.tie)) < row.lm) kept.ties = 0;
-  bool have_pieces = false;
-  if (top_p < 1.f && temp > 0.f && top_k != 1) have_pieces = first_mass(row, kept, (double)top_p, sh);
-  // ---- kept masses of the pieces ----
-  const float tie_value = value_of_key(kept.tie);
-  const uint64_t each = kept.ties > 0 ? unit_weight(row.exponent(tie_value), sh.table) : 0;
-  const int pieces = row.pieces();
-  __syncthreads();
-  if (!have_pieces) {
-    for (int p = w; p < pieces; p += kSampWaves) {
-      uint64_t m[8], sum = 0;
-      uint32_t tied;
-      row.weights(p, kept, sh.table, m, tied);
+  if (s.greedy) {
+    kept = Kept{top, 1};
+  } else if (s.mode != kPlain) {
+    Tokens<T> tokens{row, sh, listed <= kList ? listed : -1};
+    if (s.k > 0) kept = cut<false>(row, tokens, kept, -INFINITY, 0, (double)s.k, sh);
+    if (kept.ties > 0 && row.exponent(value_of_key(kept.tie)) < s.lm) kept.ties = 0;
+    if (s.p < 1.f) {
+      uint64_t before = 0, all = 0;
+      if (s.mode == kMass && tokens.listed >= 0) {
+        uint64_t sum = 0, rest = 0;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum += m[e];
-      // the number of tied tokens rides above the mass: 2^9 tokens of at most 2^44 each
-      sum = wave_sum64(sum + ((uint64_t)__popc(tied) << 54));
-      if (lane == 0) {
-        sh.mass[p] = sum & ((1ull << 54) - 1);
-        sh.count[p] = (uint32_t)(sum >> 54);
+        for (int i = 0; i < kPer; ++i) sum += mine[i];
+        block_scan(sum, sh.red, &before);
+        tokens.each([&](float v, uint32_t, int) { rest += unit_weight(row.exponent(v), sh.table); });
+        block_scan(rest, sh.red, &rest);
+        all = mass;
+        const double target = (double)s.p * (double)all;
+        if (((double)before >= target && before > 0) || (double)(before + rest) < target) tokens.listed = -1;  // it ends elsewhere
       }
+      if (!(s.mode == kMass && tokens.listed >= 0)) {
+        uint64_t sum = 0;
+        before = 0;
+        tokens.each([&](float v, uint32_t key, int) {
+          if (key > kept.tie && row.exponent(v) >= s.lm) sum += unit_weight(row.exponent(v), sh.table);
+        });
+        if (t == 0 && kept.ties > 0) sum += kept.ties * unit_weight(row.exponent(value_of_key(kept.tie)), sh.table);
+        block_scan(sum, sh.red, &all);
+      }
+      kept = cut<true>(row, tokens, kept, s.lm, before, (double)s.p * (double)all, sh);
+    }
+    // ---- the pieces' masses and ties, above the list and in it ----
+    const bool add = s.mode == kMass && tokens.listed >= 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      sh.mass[kPer * t + i] = add ? mine[i] : 0;
+      sh.count[kPer * t + i] = 0;
     }
     __syncthreads();
+    tokens.each([&](float v, uint32_t key, int token) {
+      const double ex = row.exponent(v);
+      if (key > kept.tie && ex >= s.lm)
+        atomicAdd((unsigned long long *)&sh.mass[token / kPiece], unit_weight(ex, sh.table));
+      else if (key == kept.tie && kept.ties > 0) atomicAdd(&sh.count[token / kPiece], 1u);
+    });
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) mine[i] = sh.mass[kPer * t + i] | (uint64_t)sh.count[kPer * t + i] << 54;
   }
-  uint64_t all_ties, S;
-  const uint64_t tied = t < pieces ? sh.count[t] : 0;
-  const uint64_t tied_before = block_scan64(tied, sh.red, &all_ties) - tied;
-  const uint64_t mine_ties = tied_before >= kept.ties ? 0 : min(tied, kept.ties - tied_before);
-  const uint64_t mine = t < pieces ? sh.mass[t] + mine_ties * each : 0;
-  const uint64_t end = block_scan64(mine, sh.red, &S);
-  const uint64_t target = (uint64_t)((double)u * (double)S);  // passed by the first cumulative mass above it
-  // ---- the piece, then its token ----
-  if (end > target && end - mine <= target) {
-    sh.bin = t;
-    sh.before = end - mine;
-    sh.count[0] = (uint32_t)(kept.ties - min(kept.ties, tied_before));  // ties that are left for it
+  // ---- the piece: the first at which the cumulative mass passes u times all of it ----
+  const float tie_value = value_of_key(kept.tie);
+  const uint64_t each = kept.ties > 0 ? unit_weight(row.exponent(tie_value), sh.table) : 0;
+  uint64_t ties = 0, sum = 0, unused, S;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) ties += mine[i] >> 54;
+  uint64_t ties_before = block_scan(ties, sh.red, &unused) - ties, first_ties = ties_before;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const uint64_t n = mine[i] >> 54;
+    mine[i] &= (1ull << 54) - 1;
+    mine[i] += (ties_before >= kept.ties ? 0 : min(n, kept.ties - ties_before)) * each;
+    ties_before += n;
+    sum += mine[i];
+  }
+  const uint64_t start = block_scan(sum, sh.red, &S) - sum;
+  const uint64_t target = (uint64_t)((double)s.u * (double)S);
+  if (start <= target && target < start + sum) {
+    uint64_t at = start;
+    bool found = false;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      if (!found && at + mine[i] > target) {
+        found = true;
+        sh.bin = kPer * t + i;
+        sh.before = at;
+      }
+      at += mine[i];
+    }
+    // ties that are left for it: those of its thread's pieces before it are counted below
+    sh.left = (int)min<uint64_t>(kept.ties, first_ties);
   }
   __syncthreads();
   if (w != 0) return;
-  uint64_t m[8], sum = 0;
-  uint32_t ties;
-  row.weights(sh.bin, kept, sh.table, m, ties);
-  int ties_before = (int)(wave_scan64(__popc(ties)) - __popc(ties));
-  const int left = (int)min(sh.count[0], (uint32_t)kPiece);
+  // ---- its token, by one wave ----
+  const int piece = sh.bin;
+  const typename Row<T>::Eight f = row.raw(piece);
+  const uint64_t goal = target - sh.before;
+  uint64_t m[8];
+  uint32_t tied = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    if (ties >> e & 1) {
-      if (ties_before < left) m[e] = each;
-      ++ties_before;
+    const uint32_t key = order_key(f[e]);
+    const double ex = row.exponent(f[e]);
+    m[e] = f[e] > -INFINITY && key > kept.tie && ex >= s.lm && !s.greedy ? unit_weight(ex, sh.table) : 0;
+    tied |= (uint32_t)(kept.ties > 0 && key == kept.tie) << e;
+  }
+  // the ties of the pieces before this one: `left` up to the first piece of its thread, the others looked at again
+  int seen = sh.left;
+  if (kept.ties > 0)
+    for (int q = piece / kPer * kPer; q < piece; ++q) {
+      const typename Row<T>::Eight g = row.raw(q);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) seen += __popcll(__ballot(order_key(g[e]) == kept.tie));
+    }
+  int rank = seen + (int)wave_scan((uint64_t)__popc(tied)) - __popc(tied);
+  sum = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    if (tied >> e & 1) {
+      if (rank < (int)kept.ties) m[e] = each;
+      ++rank;
     }
     sum += m[e];
   }
-  uint64_t cum = sh.before + wave_scan64(sum) - sum;
-  if (!(cum <= target && target < cum + sum)) return;
-  int at = 7;  // (the last one with a mass, at the latest)
+  const uint64_t before = wave_scan(sum) - sum;
+  if (!(before <= goal && goal < before + sum)) return;
+  int at = 7;
 #pragma unroll
   for (int e = 7; e >= 0; --e)
-    if (cum + sum > target) {  // sum: the masses up to e
+    if (before + sum > goal) {  // sum: the masses up to e
       at = e;
       sum -= m[e];
     }
-  const int token = sh.bin * kPiece + 8 * lane + at;
+  const int token = piece * kPiece + 8 * lane + at;
   a.tokens[r] = token;
   if (a.logprob) {
     const double ex = row.exponent(Elem<T>::load(row.x + token));
@@ -592,7 +787,16 @@ __global__ __launch_bounds__(kSampThreads) void sample_kernel(SampleArgs a) {
 using namespace sm;
 
 SM_API size_t sm_sample_workspace_bytes(int rows, int vocab) {
-  return rows > 0 && vocab > 0 ? 256 : 0;
+  return rows > 0 && vocab > 0 ? sizeof(RowState) * std::min(rows, kRowsAtATime) : 0;
+}
+
+template <typename T>
+static sm_status launch_sample(const SampleArgs &a, hipStream_t stream) {
+  const dim3 grid((unsigned)(a.rows * a.slices)), threads(kSampThreads);
+  hipLaunchKernelGGL(sample_scan_kernel<T>, grid, threads, 0, stream, a);
+  hipLaunchKernelGGL(sample_weigh_kernel<T>, grid, threads, 0, stream, a);
+  hipLaunchKernelGGL(sample_choose_kernel<T>, dim3(a.rows), threads, 0, stream, a);
+  return hipGetLastError() == hipSuccess ? SM_OK : SM_EHIP;
 }
 
 SM_API sm_status sm_sample_tokens(const void *logits, int64_t stride, int rows, int vocab, sm_dtype dt, const float *u,
@@ -601,13 +805,17 @@ SM_API sm_status sm_sample_tokens(const void *logits, int64_t stride, int rows, 
   if ((dt != SM_F32 && dt != SM_BF16) || rows < 0 || vocab < 1 || vocab > kMostVocab || stride < vocab) return SM_EINVAL;
   if (rows == 0) return SM_OK;
   if (!logits || !u || !tokens || !ws || (uintptr_t)ws % 16 || ws_bytes < sm_sample_workspace_bytes(rows, vocab)) return SM_EINVAL;
-  SampleArgs a{logits, stride, rows, vocab, u, temperature, top_p, min_p, top_k, tokens, logprob, err, 0};
-  constexpr int kLaunchRows = 1 << 20;  // a launch's threads are counted in 32 bits
-  for (; a.first < rows; a.first += kLaunchRows) {
-    const dim3 grid(std::min<int64_t>(rows - a.first, kLaunchRows));
-    if (dt == SM_BF16) hipLaunchKernelGGL(sample_kernel<uint16_t>, grid, dim3(kSampThreads), 0, stream, a);
-    else hipLaunchKernelGGL(sample_kernel<float>, grid, dim3(kSampThreads), 0, stream, a);
-    if (hipGetLastError() != hipSuccess) return SM_EHIP;
+  const int pieces = (vocab + kPiece - 1) / kPiece, es = dt == SM_BF16 ? 2 : 4;
+  // Slices of 16 pieces, all loaded at once, until there are plenty of
+  // workgroups; then of 64.
+  const int per = (int64_t)std::min(rows, kRowsAtATime) * ((pieces + 15) / 16) <= 4096 ? 16 : 64;
+  for (int first = 0; first < rows; first += kRowsAtATime) {
+    const SampleArgs a{(const char *)logits + first * stride * es, stride, std::min(rows - first, kRowsAtATime), vocab, u + first,
+                       temperature ? temperature + first : nullptr, top_p ? top_p + first : nullptr,
+                       min_p ? min_p + first : nullptr, top_k ? top_k + first : nullptr, tokens + first,
+                       logprob ? logprob + first : nullptr, err, (RowState *)ws, (pieces + per - 1) / per, per};
+    const sm_status st = dt == SM_BF16 ? launch_sample<uint16_t>(a, stream) : launch_sample<float>(a, stream);
+    if (st != SM_OK) return st;
   }
   return SM_OK;
 }
