@@ -42,7 +42,7 @@ constexpr int kMostVocab = 1 << 19;            // a mass of 2^44 times this many
 constexpr int kMostPieces = kMostVocab / kPiece;
 constexpr int kInFlight = 4;                   // pieces that a wave loads at a time
 constexpr int kUnit = 44;                      // a weight of 1 is 2^44
-constexpr double kLeast = -46.0;               // exponents from here down weigh nothing
+constexpr double kLeast = -46.0;               // exponents from here down weigh nothing (2^-45 and its half on)
 constexpr double kLog2eD = 1.4426950408889634073599246810019;
 
 // The histogram: bins of 1/23 in the logits, the first 512 above the largest
@@ -87,13 +87,16 @@ __device__ __forceinline__ uint32_t order_key(float x) {
 }
 __device__ __forceinline__ float value_of_key(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o); }
 
-// 2^t for t <= 0 in multiples of 2^-44; 0 from 2^-46 on.  table: 2^(j / 128).
-// t = k / 128 + r, |r| <= 2^-8, 2^r = e^(r ln 2) to its fourth power: the next
-// term is below 2^-49.
-__device__ __forceinline__ uint64_t unit_weight(double t, const double *table) {
+// 2^t for t <= 0 in multiples of 2^-44, to nearest (so 0 from 2^-45 on), as the
+// low bits of a double of 2^52 and that many; table: 2^(44 + j / 128).  t = k /
+// 128 + r, |r| <= 2^-8, 2^r = e^(r ln 2) to its fourth power: the next term is
+// below 2^-49.  The binary exponent goes into the table's entry.
+constexpr uint64_t kZeroWeight = 0x4330000000000000ull;  // 2^52 as bits
+__device__ __forceinline__ uint64_t weight_bits(double t, const double *table) {
   constexpr double ln2 = 0.69314718055994530941723212145818;
   constexpr double c1 = ln2, c2 = c1 * ln2 / 2, c3 = c2 * ln2 / 3, c4 = c3 * ln2 / 4;
   constexpr double magic = 6755399441055744.0;  // 1.5 x 2^52: a sum with it is a whole number in its low bits
+  t = fmax(t, -100.0);                          // (and -infinity)
   const double sum = fma(t, 128.0, magic);
   const int k = (int)__double_as_longlong(sum);
   const double r = fma(sum - magic, -0.0078125, t);
@@ -101,77 +104,120 @@ __device__ __forceinline__ uint64_t unit_weight(double t, const double *table) {
   p = fma(r, p, c2);
   p = fma(r, p, c1);
   p = fma(r, p, 1.0);
-  const double w = ldexp(table[k & 127] * p, (k >> 7) + kUnit) + 4503599627370496.0;  // to nearest
-  return t < kLeast ? 0 : __double_as_longlong(w) & 0xfffffffffffffll;
+  const double entry = table[k & 127];
+  const double power = __hiloint2double(__double2hiint(entry) + ((k & ~127) << 13), __double2loint(entry));
+  return __double_as_longlong(fma(power, p, 4503599627370496.0));
 }
+__device__ __forceinline__ uint64_t unit_weight(double t, const double *table) { return weight_bits(t, table) - kZeroWeight; }
+
+// 2^(j / 128), rounded to double precision
+__constant__ double kPowers[128] = {
+    0x1.0000000000000p+0, 0x1.0163da9fb3335p+0, 0x1.02c9a3e778061p+0, 0x1.04315e86e7f85p+0,
+    0x1.059b0d3158574p+0, 0x1.0706b29ddf6dep+0, 0x1.0874518759bc8p+0, 0x1.09e3ecac6f383p+0,
+    0x1.0b5586cf9890fp+0, 0x1.0cc922b7247f7p+0, 0x1.0e3ec32d3d1a2p+0, 0x1.0fb66affed31bp+0,
+    0x1.11301d0125b51p+0, 0x1.12abdc06c31ccp+0, 0x1.1429aaea92de0p+0, 0x1.15a98c8a58e51p+0,
+    0x1.172b83c7d517bp+0, 0x1.18af9388c8deap+0, 0x1.1a35beb6fcb75p+0, 0x1.1bbe084045cd4p+0,
+    0x1.1d4873168b9aap+0, 0x1.1ed5022fcd91dp+0, 0x1.2063b88628cd6p+0, 0x1.21f49917ddc96p+0,
+    0x1.2387a6e756238p+0, 0x1.251ce4fb2a63fp+0, 0x1.26b4565e27cddp+0, 0x1.284dfe1f56381p+0,
+    0x1.29e9df51fdee1p+0, 0x1.2b87fd0dad990p+0, 0x1.2d285a6e4030bp+0, 0x1.2ecafa93e2f56p+0,
+    0x1.306fe0a31b715p+0, 0x1.32170fc4cd831p+0, 0x1.33c08b26416ffp+0, 0x1.356c55f929ff1p+0,
+    0x1.371a7373aa9cbp+0, 0x1.38cae6d05d866p+0, 0x1.3a7db34e59ff7p+0, 0x1.3c32dc313a8e5p+0,
+    0x1.3dea64c123422p+0, 0x1.3fa4504ac801cp+0, 0x1.4160a21f72e2ap+0, 0x1.431f5d950a897p+0,
+    0x1.44e086061892dp+0, 0x1.46a41ed1d0057p+0, 0x1.486a2b5c13cd0p+0, 0x1.4a32af0d7d3dep+0,
+    0x1.4bfdad5362a27p+0, 0x1.4dcb299fddd0dp+0, 0x1.4f9b2769d2ca7p+0, 0x1.516daa2cf6642p+0,
+    0x1.5342b569d4f82p+0, 0x1.551a4ca5d920fp+0, 0x1.56f4736b527dap+0, 0x1.58d12d497c7fdp+0,
+    0x1.5ab07dd485429p+0, 0x1.5c9268a5946b7p+0, 0x1.5e76f15ad2148p+0, 0x1.605e1b976dc09p+0,
+    0x1.6247eb03a5585p+0, 0x1.6434634ccc320p+0, 0x1.6623882552225p+0, 0x1.68155d44ca973p+0,
+    0x1.6a09e667f3bcdp+0, 0x1.6c012750bdabfp+0, 0x1.6dfb23c651a2fp+0, 0x1.6ff7df9519484p+0,
+    0x1.71f75e8ec5f74p+0, 0x1.73f9a48a58174p+0, 0x1.75feb564267c9p+0, 0x1.780694fde5d3fp+0,
+    0x1.7a11473eb0187p+0, 0x1.7c1ed0130c132p+0, 0x1.7e2f336cf4e62p+0, 0x1.80427543e1a12p+0,
+    0x1.82589994cce13p+0, 0x1.8471a4623c7adp+0, 0x1.868d99b4492edp+0, 0x1.88ac7d98a6699p+0,
+    0x1.8ace5422aa0dbp+0, 0x1.8cf3216b5448cp+0, 0x1.8f1ae99157736p+0, 0x1.9145b0b91ffc6p+0,
+    0x1.93737b0cdc5e5p+0, 0x1.95a44cbc8520fp+0, 0x1.97d829fde4e50p+0, 0x1.9a0f170ca07bap+0,
+    0x1.9c49182a3f090p+0, 0x1.9e86319e32323p+0, 0x1.a0c667b5de565p+0, 0x1.a309bec4a2d33p+0,
+    0x1.a5503b23e255dp+0, 0x1.a799e1330b358p+0, 0x1.a9e6b5579fdbfp+0, 0x1.ac36bbfd3f37ap+0,
+    0x1.ae89f995ad3adp+0, 0x1.b0e07298db666p+0, 0x1.b33a2b84f15fbp+0, 0x1.b59728de5593ap+0,
+    0x1.b7f76f2fb5e47p+0, 0x1.ba5b030a1064ap+0, 0x1.bcc1e904bc1d2p+0, 0x1.bf2c25bd71e09p+0,
+    0x1.c199bdd85529cp+0, 0x1.c40ab5fffd07ap+0, 0x1.c67f12e57d14bp+0, 0x1.c8f6d9406e7b5p+0,
+    0x1.cb720dcef9069p+0, 0x1.cdf0b555dc3fap+0, 0x1.d072d4a07897cp+0, 0x1.d2f87080d89f2p+0,
+    0x1.d5818dcfba487p+0, 0x1.d80e316c98398p+0, 0x1.da9e603db3285p+0, 0x1.dd321f301b460p+0,
+    0x1.dfc97337b9b5fp+0, 0x1.e264614f5a129p+0, 0x1.e502ee78b3ff6p+0, 0x1.e7a51fbc74c83p+0,
+    0x1.ea4afa2a490dap+0, 0x1.ecf482d8e67f1p+0, 0x1.efa1bee615a27p+0, 0x1.f252b376bba97p+0,
+    0x1.f50765b6e4540p+0, 0x1.f7bfdad9cbe14p+0, 0x1.fa7c1819e90d8p+0, 0x1.fd3c22b8f71f1p+0,
+};
 __device__ __forceinline__ void fill_table(double *table) {
-  if (threadIdx.x < 128) table[threadIdx.x] = exp2(threadIdx.x / 128.0);
+  if (threadIdx.x < 128) table[threadIdx.x] = kPowers[threadIdx.x] * (double)(1ull << kUnit);
 }
 
 // ---- sums ------------------------------------------------------------------
-__device__ __forceinline__ uint64_t wave_sum64(uint64_t v) {
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) {
-    const uint32_t lo = __shfl_xor((uint32_t)v, m, kWave), hi = __shfl_xor((uint32_t)(v >> 32), m, kWave);
-    v += (uint64_t)hi << 32 | lo;
-  }
-  return v;
+// Scans by lane permutations in the vector ALU: shifts by 1, 2, 4 and 8 within
+// rows of 16 lanes, then each row's last lane to the rows behind it.  (Through
+// LDS, as __shfl does it, a scan of 64 bits took 0.4 us of a call's chain.)
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t lane_moved(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, true);  // 0 where nothing moves in
 }
-__device__ __forceinline__ uint64_t wave_scan(uint64_t v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t lo = __shfl_up((uint32_t)v, d, kWave), hi = __shfl_up((uint32_t)(v >> 32), d, kWave);
-    if (lane >= d) v += (uint64_t)hi << 32 | lo;
-  }
-  return v;
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ uint64_t moved(uint64_t v) {
+  return (uint64_t)lane_moved<CTRL, ROWS>((uint32_t)(v >> 32)) << 32 | lane_moved<CTRL, ROWS>((uint32_t)v);
 }
-__device__ __forceinline__ float wave_scan(float v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const float u = __shfl_up(v, d, kWave);
-    if (lane >= d) v += u;
-  }
-  return v;
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ float moved(float v) {
+  return __uint_as_float(lane_moved<CTRL, ROWS>(__float_as_uint(v)));
 }
-// Inclusive over the workgroup; red: one value a wave.  The last barrier lets red be used again.
 template <typename V>
-__device__ __forceinline__ V block_scan(V v, V *red, V *total) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+__device__ __forceinline__ V wave_scan(V v) {
+  v += moved<0x111>(v);       // row_shr:1, 2, 4, 8
+  v += moved<0x112>(v);
+  v += moved<0x114>(v);
+  v += moved<0x118>(v);
+  v += moved<0x142, 0xa>(v);  // row_bcast:15 into rows 1 and 3
+  v += moved<0x143, 0xc>(v);  // row_bcast:31 into rows 2 and 3
+  return v;
+}
+__device__ __forceinline__ uint64_t last_lane(uint64_t v) {
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), 63) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+__device__ __forceinline__ float last_lane(float v) {
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+__device__ __forceinline__ uint64_t wave_sum64(uint64_t v) { return last_lane(wave_scan(v)); }
+// Inclusive over the workgroup.  red: one value a wave, in turn two places, so
+// that one barrier a scan does.
+struct Red {
+  uint64_t v[2][kSampWaves];
+};
+template <typename V>
+__device__ __forceinline__ V block_scan(V v, Red &red, int &turn, V *total) {
+  const int w = threadIdx.x >> 6;
   v = wave_scan(v);
-  if (lane == 63) red[w] = v;
+  V *r = (V *)red.v[turn ^= 1];
+  if ((threadIdx.x & 63) == 63) r[w] = v;
   __syncthreads();
   V before = 0, all = 0;
+#pragma unroll
   for (int i = 0; i < kSampWaves; ++i) {
-    if (i < w) before += red[i];
-    all += red[i];
+    if (i < w) before += r[i];
+    all += r[i];
   }
-  __syncthreads();
   *total = all;
   return v + before;
 }
-
-// (An atomic minimum of every lane's own value at one place would be taken lane
-// by lane: 64 rounds.  These leave one a wave.)
-__device__ __forceinline__ uint32_t wave_min_u32(uint32_t v) {
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) v = min(v, (uint32_t)__shfl_xor((int)v, m, kWave));
-  return v;
-}
 // The least value over the workgroup of the threads that have one, kNone of
-// none; values ascend with the thread.  red: one value a wave.
+// none; values ascend with the thread.  (An atomic minimum of every lane's own
+// value at one place would be taken lane by lane.)
 constexpr int kNone = 0x7fffffff;
-__device__ __forceinline__ int block_first(bool has, int value, int *red) {
+__device__ __forceinline__ int block_first(bool has, int value, Red &red, int &turn) {
   const int w = threadIdx.x >> 6;
   const uint64_t who = __ballot(has);
-  const int first = __shfl(value, who ? __builtin_ctzll(who) : 0, kWave);
-  if ((threadIdx.x & 63) == 0) red[w] = who ? first : kNone;
+  int *r = (int *)red.v[turn ^= 1];
+  const int first = __builtin_amdgcn_readlane(value, who ? __builtin_ctzll(who) : 0);
+  if ((threadIdx.x & 63) == 0) r[w] = who ? first : kNone;
   __syncthreads();
   int least = kNone;
+#pragma unroll
   for (int i = kSampWaves - 1; i >= 0; --i)
-    if (red[i] != kNone) least = red[i];
-  __syncthreads();
+    if (r[i] != kNone) least = r[i];
   return least;
 }
 
@@ -201,10 +247,14 @@ struct Settings {
 };
 
 __device__ __forceinline__ Settings settings_of(const SampleArgs &a, int64_t r) {
-  const float t = a.temperature ? a.temperature[r] : 1.f, p = a.top_p ? a.top_p[r] : 1.f, m = a.min_p ? a.min_p[r] : 0.f;
-  const int k = a.top_k ? a.top_k[r] : 0;
+  // (loaded at once: what is not given from where u is)
+  const float u = a.u[r], t0 = (a.temperature ? a.temperature : a.u)[r], p0 = (a.top_p ? a.top_p : a.u)[r];
+  const float m0 = (a.min_p ? a.min_p : a.u)[r];
+  const int k0 = (a.top_k ? a.top_k : (const int32_t *)a.u)[r];
+  const float t = a.temperature ? t0 : 1.f, p = a.top_p ? p0 : 1.f, m = a.min_p ? m0 : 0.f;
+  const int k = a.top_k ? k0 : 0;
   Settings s;
-  s.u = a.u[r];
+  s.u = u;
   s.fine = t >= 0.f && t < INFINITY && p >= 0.f && m >= 0.f && m <= 1.f && s.u >= 0.f && s.u < 1.f && k >= 0;
   s.greedy = t == 0.f || k == 1;
   s.k = k < a.vocab ? k : 0;
@@ -342,7 +392,7 @@ struct Range {
 
 // The bins in which the first k tokens, or the masses' first part p, end (all,
 // if there are no more than k; none: masses that came to nothing).  All threads.
-__device__ __forceinline__ Range end_bins(const RowState &st, const Settings &s, float top_depth, int vocab, uint64_t *red) {
+__device__ __forceinline__ Range end_bins(const RowState &st, const Settings &s, float top_depth, int vocab, Red &red, int &turn) {
   constexpr int N = kBins / kSampThreads;
   const int t = threadIdx.x;
   u32x4_t raw[N / 4];
@@ -352,7 +402,7 @@ __device__ __forceinline__ Range end_bins(const RowState &st, const Settings &s,
     uint64_t n = 0, total;
 #pragma unroll
     for (int i = 0; i < N; ++i) n += raw[i / 4][i % 4];
-    uint64_t at = block_scan(n, red, &total) - n;
+    uint64_t at = block_scan(n, red, turn, &total) - n;
     const bool here = at < (uint64_t)s.k && at + n >= (uint64_t)s.k;
     int b = 0;
 #pragma unroll
@@ -360,7 +410,7 @@ __device__ __forceinline__ Range end_bins(const RowState &st, const Settings &s,
       if (at + n >= (uint64_t)s.k) b = i;
       n -= raw[i / 4][i % 4];
     }
-    const int last = block_first(here, N * t + b, (int *)red);
+    const int last = block_first(here, N * t + b, red, turn);
     return Range{0, min(last, kBins - 1)};
   }
   // masses relative to the bin of M, in fp32: the slack takes the roundings of
@@ -374,7 +424,7 @@ __device__ __forceinline__ Range end_bins(const RowState &st, const Settings &s,
     m[i] = n ? (float)n * (1.f / one) * __builtin_amdgcn_exp2f((from - (float)(N * t + i)) * per_bin) : 0.f;
     sum += m[i];
   }
-  float at = block_scan(sum, (float *)red, &total);
+  float at = block_scan(sum, red, turn, &total);
   const float slack = (0.5f / one + 2e-6f) * total, lo = s.p * total - slack, hi = s.p * total + slack;
   int b1 = kNone, b2 = kNone;
 #pragma unroll
@@ -383,8 +433,8 @@ __device__ __forceinline__ Range end_bins(const RowState &st, const Settings &s,
     if (at >= hi) b2 = N * t + i;
     at -= m[i];
   }
-  b1 = block_first(b1 != kNone, b1, (int *)red);
-  b2 = block_first(b2 != kNone, b2, (int *)red);
+  b1 = block_first(b1 != kNone, b1, red, turn);
+  b2 = block_first(b2 != kNone, b2, red, turn);
   return Range{b1, min(b2, kBins - 1)};
 }
 
@@ -394,7 +444,9 @@ constexpr int kSliceList = 1024;
 template <typename T>
 __global__ __launch_bounds__(kSampThreads) void sample_weigh_kernel(SampleArgs a) {
   __shared__ double table[128];
-  __shared__ uint64_t list[kSliceList], red[kSampWaves];
+  __shared__ uint64_t list[kSliceList];
+  __shared__ Red red;
+  int turn = 0;
   __shared__ int listed, place;
   const int t = threadIdx.x, lane = t & 63;
   const int64_t r = blockIdx.x / a.slices;
@@ -412,44 +464,68 @@ __global__ __launch_bounds__(kSampThreads) void sample_weigh_kernel(SampleArgs a
   Range range{0, -1};
   if (s.mode == kListK || s.mode == kMass) {
     row.set_origin();
-    range = end_bins(st, s, row.depth(row.M), a.vocab, red);
+    range = end_bins(st, s, row.depth(row.M), a.vocab, red, turn);
     if (range.first == kNone) {  // (masses that came to nothing)
       if (t == 0 && p0 == 0) atomicAdd(&st.listed, kList + 1);
       return;
     }
   }
   __syncthreads();
-  const auto add = [&](float v, int token) {
-    const int at = atomicAdd(&listed, 1);
-    if (at < kSliceList) list[at] = (uint64_t)order_key(v) << 32 | (uint32_t)token;
+  // takes the marked ones of a lane's eight tokens into the list: one place in it a wave and piece
+  const auto add = [&](const typename Row<T>::Eight &f, int p, const bool (&take)[8]) {
+    int at[8], n = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint64_t who = __ballot(take[e]);
+      at[e] = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+      n += __popcll(who);
+    }
+    if (n == 0) return;
+    int base = 0;
+    if (lane == 0) base = atomicAdd(&listed, n);
+    base = __builtin_amdgcn_readfirstlane(base);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (take[e] && base + at[e] < kSliceList)
+        list[base + at[e]] = (uint64_t)order_key(f[e]) << 32 | (uint32_t)(p * kPiece + 8 * lane + e);
   };
   const double lm = s.mode == kListM ? fmax(s.lm, kLeast) : s.lm;
+  // a depth below these lies in a bin above the range, or in it or above
+  const float above_range = (float)range.first, in_range = range.last < kBins - 1 ? (float)(range.last + 1) : INFINITY;
   if (s.mode == kListK) {
     row.each_piece(p0, p1, [&](const typename Row<T>::Eight &f, int p) {
+      bool take[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (f[e] > -INFINITY && row.bin(f[e]) <= range.last) add(f[e], p * kPiece + 8 * lane + e);
+      for (int e = 0; e < 8; ++e) take[e] = f[e] > -INFINITY && row.depth(f[e]) < in_range;
+      add(f, p, take);
     });
   } else if (s.mode == kListM) {
     row.each_piece(p0, p1, [&](const typename Row<T>::Eight &f, int p) {
+      bool take[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (f[e] > -INFINITY && row.exponent(f[e]) >= lm) add(f[e], p * kPiece + 8 * lane + e);
+      for (int e = 0; e < 8; ++e) take[e] = f[e] > -INFINITY && row.exponent(f[e]) >= lm;
+      add(f, p, take);
     });
   } else if (s.mode == kMass) {
     uint64_t S = 0;
     row.each_piece(p0, p1, [&](const typename Row<T>::Eight &f, int p) {
-      uint64_t above = 0;
+      uint64_t above = 0, all = 0;
+      int n = 0;
+      bool take[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const uint64_t m = f[e] > -INFINITY ? unit_weight(row.exponent(f[e]), table) : 0;
-        const int b = row.bin(f[e]);
-        S += m;
-        above += b < range.first ? m : 0;
-        if (b >= range.first && b <= range.last && f[e] > -INFINITY) add(f[e], p * kPiece + 8 * lane + e);
+        const uint64_t m = weight_bits(row.exponent(f[e]), table);
+        const float d = row.depth(f[e]);
+        const bool over = d < above_range;
+        all += m;
+        above += over ? m : 0;
+        n += over;
+        take[e] = !over && d < in_range && f[e] > -INFINITY;
       }
-      above = wave_sum64(above);
+      S += all - 8 * kZeroWeight;
+      above = wave_sum64(above - n * kZeroWeight);
       if (lane == 0) st.pieces[p] = above;
+      add(f, p, take);
     });
     S = wave_sum64(S);
     if (lane == 0) atomicAdd((unsigned long long *)&st.mass, S);
@@ -460,15 +536,23 @@ __global__ __launch_bounds__(kSampThreads) void sample_weigh_kernel(SampleArgs a
       for (int e = 0; e < 8; ++e) n += __popcll(__ballot(order_key(f[e]) == top));
       if (lane == 0) st.pieces[p] = (uint64_t)n << 54;
     });
-  } else {
+  } else if (lm > -INFINITY) {
     row.each_piece(p0, p1, [&](const typename Row<T>::Eight &f, int p) {
       uint64_t sum = 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const double ex = row.exponent(f[e]);
-        if (f[e] > -INFINITY && ex >= lm) sum += unit_weight(ex, table);
+        if (ex >= lm) sum += unit_weight(ex, table);
       }
       sum = wave_sum64(sum);
+      if (lane == 0) st.pieces[p] = sum;
+    });
+  } else {
+    row.each_piece(p0, p1, [&](const typename Row<T>::Eight &f, int p) {
+      uint64_t sum = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum += weight_bits(row.exponent(f[e]), table);
+      sum = wave_sum64(sum - 8 * kZeroWeight);
       if (lane == 0) st.pieces[p] = sum;
     });
   }
@@ -487,10 +571,10 @@ struct ChooseShared {
   uint32_t count[kCutBins];      // of a cut's bins, or of the pieces' ties
   uint64_t list[kList];
   double table[128];
-  uint64_t red[kSampWaves];
-  uint64_t before;               // mass (or count) above the bin
+  Red red;
+  uint32_t lo[kSampWaves], hi[kSampWaves];
+  uint64_t before, amount;       // mass (or count) above the bin, and in it
   int bin, left;
-  uint32_t klo, khi;
 };
 static_assert(kMostPieces <= kCutBins, "the pieces in the bins' place");
 constexpr int kPer = kCutBins / kSampThreads;  // bins, or pieces, of a thread
@@ -512,67 +596,95 @@ struct Tokens {
     } else {
       for (int p = threadIdx.x >> 6; p < row.pieces(); p += kSampWaves) {
         const typename Row<T>::Eight v = row.raw(p);
+#pragma unroll 1
+        for (int e = 0; e < 8; ++e) {
+          float x = v[0];
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (v[e] > -INFINITY) f(v[e], order_key(v[e]), p * kPiece + 8 * (int)(threadIdx.x & 63) + e);
+          for (int i = 1; i < 8; ++i) x = e == i ? v[i] : x;
+          if (x > -INFINITY) f(x, order_key(x), p * kPiece + 8 * (int)(threadIdx.x & 63) + e);
+        }
       }
     }
   }
 };
 
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+  v = max(v, lane_moved<0x111, 0xf>(v));
+  v = max(v, lane_moved<0x112, 0xf>(v));
+  v = max(v, lane_moved<0x114, 0xf>(v));
+  v = max(v, lane_moved<0x118, 0xf>(v));
+  v = max(v, lane_moved<0x142, 0xa>(v));
+  v = max(v, lane_moved<0x143, 0xc>(v));
+  return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+
 // The smallest start of the kept ones of these tokens, in descending order, at
 // which `before` plus their amount (MASS: of their masses; else their number)
-// reaches the target.  All threads; returns the same in each.  Rounds of 1024
-// bins over keys from the largest down, until a single value is left.
+// reaches the target, or all of them.  All threads; returns the same in each.
+// Rounds of 1024 bins over the keys from the largest down (of bf16 the upper
+// halves, which are all there is to them): one for a list of bf16, two or
+// three for fp32.  false: the target lies before these tokens or behind them.
 template <bool MASS, typename T>
-__device__ __noinline__ Kept cut(const Row<T> &row, const Tokens<T> &tokens, Kept kept, double lm, uint64_t before, double target,
-                                 ChooseShared &sh) {
-  const int t = threadIdx.x;
+__device__ __noinline__ bool cut(const Row<T> &row, const Tokens<T> &tokens, Kept &kept, double lm, uint64_t before, uint64_t target,
+                                 ChooseShared &sh, int &turn) {
+  constexpr int DROP = 32 - 8 * sizeof(T);  // bits of a key that say nothing
+  const int t = threadIdx.x, w = t >> 6;
   const auto amount = [&](float v) { return MASS ? unit_weight(row.exponent(v), sh.table) : (uint64_t)1; };
-  const float tie_value = value_of_key(kept.tie);
-  const bool tie_in = kept.ties > 0 && row.exponent(tie_value) >= lm;
-  uint32_t klo = 0, khi = 0xffffffffu;
+  const bool tie_in = kept.ties > 0 && row.exponent(value_of_key(kept.tie)) >= lm;
+  const Kept was = kept;
+  // ---- least and largest key ----
+  uint32_t lo = 0xffffffffu, hi = 0;
+  tokens.each([&](float v, uint32_t key, int) {
+    if (key <= was.tie || row.exponent(v) < lm) return;
+    lo = min(lo, key >> DROP);
+    hi = max(hi, key >> DROP);
+  });
+  if (tie_in) lo = was.tie >> DROP;  // (the others are above it)
+  hi = max(hi, tie_in ? was.tie >> DROP : 0u);
+  hi = wave_max_u32(hi);
+  lo = ~wave_max_u32(~lo);
+  if ((t & 63) == 0) {
+    sh.lo[w] = lo;
+    sh.hi[w] = hi;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kSampWaves; ++i) {
+    lo = min(lo, sh.lo[i]);
+    hi = max(hi, sh.hi[i]);
+  }
+  if (hi == 0) return before >= target;  // no tokens
   for (;;) {
-    // ---- least and largest key ----
-    if (t == 0) {
-      sh.klo = 0xffffffffu;
-      sh.khi = 0;
-    }
+    int shift = 0;
+    while ((hi - lo) >> shift >= (uint32_t)kCutBins) ++shift;
     for (int i = t; i < kCutBins; i += kSampThreads) sh.mass[i] = sh.count[i] = 0;
     __syncthreads();
-    uint32_t lo = 0xffffffffu, hi = 0;
-    tokens.each([&](float v, uint32_t key, int) {
-      if (key <= kept.tie || key < klo || key > khi || row.exponent(v) < lm) return;
-      lo = min(lo, key);
-      hi = max(hi, key);
-    });
-    if (t == 0 && tie_in && kept.tie >= klo && kept.tie <= khi) {
-      lo = min(lo, kept.tie);
-      hi = max(hi, kept.tie);
-    }
-    lo = wave_min_u32(lo);
-    hi = ~wave_min_u32(~hi);
-    if ((t & 63) == 0 && hi) {
-      atomicMin(&sh.klo, lo);
-      atomicMax(&sh.khi, hi);
-    }
-    __syncthreads();
-    klo = sh.klo;
-    khi = sh.khi;
-    if (khi == 0) return kept;  // no tokens
-    int shift = 0;
-    while ((khi - klo) >> shift >= (uint32_t)kCutBins) ++shift;
     // ---- amounts by bins ----
     tokens.each([&](float v, uint32_t key, int) {
-      if (key <= kept.tie || key < klo || key > khi || row.exponent(v) < lm) return;
-      const int b = (khi - key) >> shift;
+      const uint32_t k = key >> DROP;
+      if (key <= was.tie || k < lo || k > hi || row.exponent(v) < lm) return;
+      const int b = (hi - k) >> shift;
+      const uint64_t each = amount(v);
+      // the commonest values of a wave's tokens are counted first: a bin takes one add of each, not one of every token
+      bool left = true;
+      for (int i = 0; i < 4 && left; ++i) {
+        const uint32_t first = __builtin_amdgcn_readfirstlane(k);
+        const uint64_t who = __ballot(k == first);
+        if (k != first) continue;
+        left = false;
+        if ((t & 63) == __builtin_ctzll(who)) {
+          atomicAdd(&sh.count[b], (uint32_t)__popcll(who));
+          if constexpr (MASS) atomicAdd((unsigned long long *)&sh.mass[b], each * __popcll(who));
+        }
+      }
+      if (!left) return;
       atomicAdd(&sh.count[b], 1u);
-      if constexpr (MASS) atomicAdd((unsigned long long *)&sh.mass[b], amount(v));
+      if constexpr (MASS) atomicAdd((unsigned long long *)&sh.mass[b], each);
     });
-    if (t == 0 && tie_in && kept.tie >= klo && kept.tie <= khi) {
-      const int b = (khi - kept.tie) >> shift;
-      atomicAdd(&sh.count[b], kept.ties);
-      if constexpr (MASS) atomicAdd((unsigned long long *)&sh.mass[b], kept.ties * amount(tie_value));
+    if (t == 0 && tie_in && was.tie >> DROP >= lo) {
+      const int b = (hi - (was.tie >> DROP)) >> shift;
+      atomicAdd(&sh.count[b], was.ties);
+      if constexpr (MASS) atomicAdd((unsigned long long *)&sh.mass[b], was.ties * amount(value_of_key(was.tie)));
     }
     __syncthreads();
     uint64_t mine[kPer], sum = 0, total;
@@ -581,35 +693,45 @@ __device__ __noinline__ Kept cut(const Row<T> &row, const Tokens<T> &tokens, Kep
       mine[i] = MASS ? sh.mass[kPer * t + i] : sh.count[kPer * t + i];
       sum += mine[i];
     }
-    uint64_t at = block_scan(sum, sh.red, &total) + before - sum;
+    const uint64_t end = block_scan(sum, sh.red, turn, &total) + before;
     total += before;
-    // the first bin with a token at which the target is reached, or the last with one
-    int mine_first = kNone;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      at += mine[i];
-      if (mine_first == kNone && sh.count[kPer * t + i] && ((double)at >= target || at == total)) mine_first = kPer * t + i;
+    if (before >= target && before > 0) return false;
+    if (total < target) {
+      if (MASS) return false;
+      target = total;  // fewer than k: all of them
     }
-    const int b = block_first(mine_first != kNone, mine_first, (int *)sh.red);
-    if (b / kPer == t) {
-      uint64_t end = at;
+    // the first bin at which the target is reached; one token at least
+    const uint64_t aim = max(target, before + 1);
+    if (end >= aim && end - sum < aim) {
+      uint64_t at = end - sum;
+      int b = 0;
 #pragma unroll
-      for (int i = kPer - 1; i >= 0; --i)
-        if (i >= b % kPer) end -= mine[i];
-      sh.before = end;
+      for (int i = 0; i < kPer; ++i)
+        if (at < aim) {
+          b = i;
+          at += mine[i];
+        }
+      uint64_t in = mine[0];
+#pragma unroll
+      for (int i = 1; i < kPer; ++i) in = b == i ? mine[i] : in;
+      sh.bin = kPer * t + b;
+      sh.before = at - in;
+      sh.amount = in;
     }
     __syncthreads();
+    const int b = sh.bin;
     before = sh.before;
+    const uint64_t in = sh.amount;
     const uint32_t n = sh.count[b];
-    const uint64_t amounts = MASS ? sh.mass[b] : n;
-    const uint32_t lower = khi - min(khi - klo, ((uint32_t)(b + 1) << shift) - 1), upper = khi - ((uint32_t)b << shift);
-    if (lower == upper) {  // one value: its first few
-      const double each = (double)(amounts / n), need = (target - (double)before) / each;
-      const uint32_t few = each > 0 && need < (double)n ? (need > 1.0 ? (uint32_t)ceil(need) : 1u) : n;
-      return Kept{lower, few};
+    const uint32_t lower = hi - min(hi - lo, ((uint32_t)(b + 1) << shift) - 1), upper = hi - ((uint32_t)b << shift);
+    if (shift == 0) {  // one value: its first few
+      const uint64_t each = in / n, few = (aim - before + each - 1) / each;
+      kept = Kept{upper << DROP, (uint32_t)min<uint64_t>(few, n)};
+      if (DROP > 0 && !(kept.tie & 0x80000000u)) kept.tie |= (1u << DROP) - 1;  // (a negative number's bits are turned round)
+      return true;
     }
-    klo = lower;
-    khi = upper;
+    lo = lower;
+    hi = upper;
     __syncthreads();
   }
 }
@@ -617,13 +739,14 @@ __device__ __noinline__ Kept cut(const Row<T> &row, const Tokens<T> &tokens, Kep
 template <typename T>
 __global__ __launch_bounds__(kSampThreads) void sample_choose_kernel(SampleArgs a) {
   __shared__ ChooseShared sh;
-  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+  const int t = threadIdx.x;
   const int64_t r = blockIdx.x;
   Row<T> row(a, r);
   RowState &st = a.state[r];
   Settings s = settings_of(a, r);
   const uint32_t top = st.top;
   const int listed = (int)min(st.listed, kList + 1u);
+  int turn = 0;
   const uint64_t mass = st.mass;
   row.M = value_of_key(top);
   row.c = s.c;
@@ -655,31 +778,29 @@ __global__ __launch_bounds__(kSampThreads) void sample_choose_kernel(SampleArgs 
     kept = Kept{top, 1};
   } else if (s.mode != kPlain) {
     Tokens<T> tokens{row, sh, listed <= kList ? listed : -1};
-    if (s.k > 0) kept = cut<false>(row, tokens, kept, -INFINITY, 0, (double)s.k, sh);
+    if (s.k > 0) cut<false>(row, tokens, kept, -INFINITY, 0, (uint64_t)s.k, sh, turn);
     if (kept.ties > 0 && row.exponent(value_of_key(kept.tie)) < s.lm) kept.ties = 0;
     if (s.p < 1.f) {
-      uint64_t before = 0, all = 0;
+      const auto reached = [&](uint64_t all) { return (uint64_t)ceil((double)s.p * (double)all); };
+      bool found = false;
       if (s.mode == kMass && tokens.listed >= 0) {
-        uint64_t sum = 0, rest = 0;
+        uint64_t sum = 0, above;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) sum += mine[i];
-        block_scan(sum, sh.red, &before);
-        tokens.each([&](float v, uint32_t, int) { rest += unit_weight(row.exponent(v), sh.table); });
-        block_scan(rest, sh.red, &rest);
-        all = mass;
-        const double target = (double)s.p * (double)all;
-        if (((double)before >= target && before > 0) || (double)(before + rest) < target) tokens.listed = -1;  // it ends elsewhere
+        block_scan(sum, sh.red, turn, &above);
+        found = cut<true>(row, tokens, kept, s.lm, above, reached(mass), sh, turn);
+        if (!found) tokens.listed = -1;  // it ends elsewhere
+        __syncthreads();
       }
-      if (!(s.mode == kMass && tokens.listed >= 0)) {
-        uint64_t sum = 0;
-        before = 0;
+      if (!found) {
+        uint64_t sum = 0, all;
         tokens.each([&](float v, uint32_t key, int) {
           if (key > kept.tie && row.exponent(v) >= s.lm) sum += unit_weight(row.exponent(v), sh.table);
         });
         if (t == 0 && kept.ties > 0) sum += kept.ties * unit_weight(row.exponent(value_of_key(kept.tie)), sh.table);
-        block_scan(sum, sh.red, &all);
+        block_scan(sum, sh.red, turn, &all);
+        cut<true>(row, tokens, kept, s.lm, 0, reached(all), sh, turn);
       }
-      kept = cut<true>(row, tokens, kept, s.lm, before, (double)s.p * (double)all, sh);
     }
     // ---- the pieces' masses and ties, above the list and in it ----
     const bool add = s.mode == kMass && tokens.listed >= 0;
@@ -706,7 +827,7 @@ __global__ __launch_bounds__(kSampThreads) void sample_choose_kernel(SampleArgs 
   uint64_t ties = 0, sum = 0, unused, S;
 #pragma unroll
   for (int i = 0; i < kPer; ++i) ties += mine[i] >> 54;
-  uint64_t ties_before = block_scan(ties, sh.red, &unused) - ties, first_ties = ties_before;
+  uint64_t ties_before = block_scan(ties, sh.red, turn, &unused) - ties, first_ties = ties_before;
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
     const uint64_t n = mine[i] >> 54;
@@ -715,7 +836,7 @@ __global__ __launch_bounds__(kSampThreads) void sample_choose_kernel(SampleArgs 
     ties_before += n;
     sum += mine[i];
   }
-  const uint64_t start = block_scan(sum, sh.red, &S) - sum;
+  const uint64_t start = block_scan(sum, sh.red, turn, &S) - sum;
   const uint64_t target = (uint64_t)((double)s.u * (double)S);
   if (start <= target && target < start + sum) {
     uint64_t at = start;
@@ -733,48 +854,34 @@ __global__ __launch_bounds__(kSampThreads) void sample_choose_kernel(SampleArgs 
     sh.left = (int)min<uint64_t>(kept.ties, first_ties);
   }
   __syncthreads();
-  if (w != 0) return;
-  // ---- its token, by one wave ----
-  const int piece = sh.bin;
-  const typename Row<T>::Eight f = row.raw(piece);
+  // ---- its token, by two a thread ----
+  const int piece = sh.bin, first = piece * kPiece + 2 * t;
   const uint64_t goal = target - sh.before;
-  uint64_t m[8];
-  uint32_t tied = 0;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const uint32_t key = order_key(f[e]);
-    const double ex = row.exponent(f[e]);
-    m[e] = f[e] > -INFINITY && key > kept.tie && ex >= s.lm && !s.greedy ? unit_weight(ex, sh.table) : 0;
-    tied |= (uint32_t)(kept.ties > 0 && key == kept.tie) << e;
-  }
-  // the ties of the pieces before this one: `left` up to the first piece of its thread, the others looked at again
   int seen = sh.left;
-  if (kept.ties > 0)
-    for (int q = piece / kPer * kPer; q < piece; ++q) {
-      const typename Row<T>::Eight g = row.raw(q);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) seen += __popcll(__ballot(order_key(g[e]) == kept.tie));
-    }
-  int rank = seen + (int)wave_scan((uint64_t)__popc(tied)) - __popc(tied);
-  sum = 0;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    if (tied >> e & 1) {
-      if (rank < (int)kept.ties) m[e] = each;
-      ++rank;
-    }
-    sum += m[e];
+  // the ties of the pieces before this one: `left` up to the first piece of its thread, the others looked at again
+  if (kept.ties > 0 && piece % kPer != 0) {
+    int n = 0;
+    for (int i = piece / kPer * kPer * kPiece + t; i < piece * kPiece; i += kSampThreads)
+      n += order_key(Elem<T>::load(row.x + i)) == kept.tie;
+    block_scan((uint64_t)n, sh.red, turn, &unused);
+    seen += (int)unused;
   }
-  const uint64_t before = wave_scan(sum) - sum;
-  if (!(before <= goal && goal < before + sum)) return;
-  int at = 7;
+  uint64_t m[2];
+  int tied[2];
 #pragma unroll
-  for (int e = 7; e >= 0; --e)
-    if (before + sum > goal) {  // sum: the masses up to e
-      at = e;
-      sum -= m[e];
-    }
-  const int token = piece * kPiece + 8 * lane + at;
+  for (int e = 0; e < 2; ++e) {
+    const float v = first + e < row.vocab ? Elem<T>::load(row.x + first + e) : -INFINITY;
+    const uint32_t key = order_key(v);
+    const double ex = row.exponent(v);
+    m[e] = v > -INFINITY && key > kept.tie && ex >= s.lm && !s.greedy ? unit_weight(ex, sh.table) : 0;
+    tied[e] = kept.ties > 0 && key == kept.tie;
+  }
+  const int rank = seen + (int)block_scan((uint64_t)(tied[0] + tied[1]), sh.red, turn, &unused) - tied[0] - tied[1];
+  if (tied[0]) m[0] = rank < (int)kept.ties ? each : 0;
+  if (tied[1]) m[1] = rank + tied[0] < (int)kept.ties ? each : 0;
+  const uint64_t before = block_scan(m[0] + m[1], sh.red, turn, &unused) - m[0] - m[1];
+  if (!(before <= goal && goal < before + m[0] + m[1])) return;
+  const int token = first + (goal >= before + m[0]);
   a.tokens[r] = token;
   if (a.logprob) {
     const double ex = row.exponent(Elem<T>::load(row.x + token));
