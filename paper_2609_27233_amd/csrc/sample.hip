@@ -625,7 +625,7 @@ __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
 // halves, which are all there is to them): one for a list of bf16, two or
 // three for fp32.  false: the target lies before these tokens or behind them.
 template <bool MASS, typename T>
-__device__ __noinline__ bool cut(const Row<T> &row, const Tokens<T> &tokens, Kept &kept, double lm, uint64_t before, uint64_t target,
+__device__ __forceinline__ bool cut(const Row<T> &row, const Tokens<T> &tokens, Kept &kept, double lm, uint64_t before, uint64_t target,
                                  ChooseShared &sh, int &turn) {
   constexpr int DROP = 32 - 8 * sizeof(T);  // bits of a key that say nothing
   const int t = threadIdx.x, w = t >> 6;
@@ -782,24 +782,22 @@ __global__ __launch_bounds__(kSampThreads) void sample_choose_kernel(SampleArgs 
     if (kept.ties > 0 && row.exponent(value_of_key(kept.tie)) < s.lm) kept.ties = 0;
     if (s.p < 1.f) {
       const auto reached = [&](uint64_t all) { return (uint64_t)ceil((double)s.p * (double)all); };
-      bool found = false;
-      if (s.mode == kMass && tokens.listed >= 0) {
-        uint64_t sum = 0, above;
+      for (;;) {
+        uint64_t sum = 0, above = 0, all = mass;
+        if (s.mode == kMass && tokens.listed >= 0) {
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) sum += mine[i];
-        block_scan(sum, sh.red, turn, &above);
-        found = cut<true>(row, tokens, kept, s.lm, above, reached(mass), sh, turn);
-        if (!found) tokens.listed = -1;  // it ends elsewhere
+          for (int i = 0; i < kPer; ++i) sum += mine[i];
+          block_scan(sum, sh.red, turn, &above);
+        } else {
+          tokens.each([&](float v, uint32_t key, int) {
+            if (key > kept.tie && row.exponent(v) >= s.lm) sum += unit_weight(row.exponent(v), sh.table);
+          });
+          if (t == 0 && kept.ties > 0) sum += kept.ties * unit_weight(row.exponent(value_of_key(kept.tie)), sh.table);
+          block_scan(sum, sh.red, turn, &all);
+        }
+        if (cut<true>(row, tokens, kept, s.lm, above, reached(all), sh, turn) || tokens.listed < 0) break;
+        tokens.listed = -1;  // it ends elsewhere
         __syncthreads();
-      }
-      if (!found) {
-        uint64_t sum = 0, all;
-        tokens.each([&](float v, uint32_t key, int) {
-          if (key > kept.tie && row.exponent(v) >= s.lm) sum += unit_weight(row.exponent(v), sh.table);
-        });
-        if (t == 0 && kept.ties > 0) sum += kept.ties * unit_weight(row.exponent(value_of_key(kept.tie)), sh.table);
-        block_scan(sum, sh.red, turn, &all);
-        cut<true>(row, tokens, kept, s.lm, 0, reached(all), sh, turn);
       }
     }
     // ---- the pieces' masses and ties, above the list and in it ----
