@@ -36,7 +36,7 @@
 
 #include "common.hpp"
 #include "e4m3.hpp"
-#include "shared_prefix.hpp"
+#include "prefill_tiles.hpp"
 
 namespace sm {
 
@@ -81,8 +81,6 @@ struct DecodeArgs {
   const int32_t *crop;
   // e4m3 pages only: the pools' exponent bytes
   const uint8_t *k_exp, *v_exp;
-  // sm_decode_attention_shared only: the requests' shares over their prefixes
-  PrefixParts prefix;
 };
 
 // Chunking of a sequence of L cached entries: nc non-empty chunks of
@@ -217,38 +215,6 @@ __device__ void write_zero_rows(const DecodeArgs &a, int i, int g, int DH, int s
   if (st != 0 && threadIdx.x == 0 && esink) set_err(esink, st);  // (no sink: reported elsewhere)
 }
 
-// sm_decode_attention_shared: the parts that request i's query head hq has of
-// its group's prefix (written by the launch before this one), joined to
-// dimension dd of what it has of its own entries.
-constexpr int kPrefixBatch = 4;
-template <int DH>
-__device__ __forceinline__ void join_prefix(const DecodeArgs &a, int i, int hq, int dd, float &M, float &acc, float &ls, bool &bad) {
-  const PrefixParts &p = a.prefix;
-  const int64_t base = ((int64_t)i * a.Hq + hq) * p.chunks;
-  if (p.chunks > 0 && *p.flag) bad = true;
-  for (int c0 = 0; c0 < p.chunks; c0 += kPrefixBatch) {
-    float pm[kPrefixBatch], pl[kPrefixBatch], po[kPrefixBatch];
-#pragma unroll
-    for (int c = 0; c < kPrefixBatch; ++c) {
-      const bool there = c0 + c < p.chunks;
-      const int64_t at = base + min(c0 + c, p.chunks - 1);
-      pm[c] = p.ml[2 * at];
-      pl[c] = there ? p.ml[2 * at + 1] : 0.f;
-      po[c] = p.o[at * DH + dd];
-    }
-#pragma unroll
-    for (int c = 0; c < kPrefixBatch; ++c) {
-      bad |= pl[c] < 0.f;
-      if (pl[c] == 0.f) continue;  // no entries (its output is not written); a NaN goes on
-      const float Mb = fmaxf(M, pm[c]);
-      const float f = M == -INFINITY ? 0.f : exp2f(M - Mb), fc = pm[c] == -INFINITY ? 0.f : exp2f(pm[c] - Mb);
-      acc = acc * f + po[c] * fc;
-      ls = ls * f + pl[c] * fc;
-      M = Mb;
-    }
-  }
-}
-
 // A row's result.  A NaN among its scores is its result over e4m3 pages and
 // behind a shared prefix; over bf16 pages alone such a row is zero.
 template <bool NANS>
@@ -267,7 +233,7 @@ __device__ __forceinline__ float row_value(float acc, float ls) {
 // is exactly max-then-sum over all chunks.
 constexpr int kCombineBatch = 4;
 
-template <typename OutT, bool NANS = false, bool PREFIX = false, int D = 128>
+template <typename OutT, bool NANS = false>
 __device__ __forceinline__ void finish_group(const DecodeArgs &a, int i, int g, int nc, int DH, int *last) {
   int32_t *ctr = a.counters + (int64_t)i * a.Hkv + g;
   __builtin_amdgcn_s_waitcnt(0);  // this thread's partial stores are done
@@ -341,7 +307,6 @@ __device__ __forceinline__ void finish_group(const DecodeArgs &a, int i, int g, 
       const int e = e0 + threadIdx.x + kDecThreads * k;
       if (e < ne) {
         const int hh = e / DH, dd = e - hh * DH;
-        if constexpr (PREFIX) join_prefix<D>(a, i, g * a.G + hh, dd, M[k], acc[k], ls[k], bad[k]);
         out[((int64_t)i * a.Hq + g * a.G + hh) * DH + dd] =
             Elem<OutT>::to_store(bad[k] ? 0.f : row_value<NANS>(acc[k], ls[k]));
       }
@@ -1022,29 +987,45 @@ __device__ __forceinline__ float byte_scale(uint32_t w, int i) {
 // EIGHT (without STEP): e4m3 pages.  Their values become bf16 on the way to the
 // matrix cores, K's with their exponents (a lane's K values are of one token);
 // V's exponents go into the probabilities before those are rounded to bf16.
-// PREFIX (without STEP): the requests' shares over a prefix are joined.
-template <int DH, bool STEP, bool ORD, bool CROP = false, bool EIGHT = false, bool PREFIX = false>
-__global__ __launch_bounds__(kDecThreads, 2) void decode_split_bf16(DecodeArgs a) {
-  __shared__ int pages[kMaxChunkPages];
-  __shared__ int flag;
-  __shared__ float red_m[kDecWaves][16];
-  __shared__ float red_l[kDecWaves][16];
-  __shared__ float red_o[kDecWaves][16][DH];
-  __shared__ float step_sn[16];       // fused step: scaled score of the new token per query head
-  __shared__ float step_vn[DH];       // ... and its V row
-  __shared__ int step_bad_page[kDecWaves];
-  __shared__ int step_plan_sh[3];     // ... the append commits; block popped for this request; its crop
-  __shared__ uint32_t dup_bm[STEP ? kDupBitmapWords : 1];  // the plan's duplicate-id check (one wave)
+// PARTS (without STEP): every chunk's partial stays in the workspace, for a
+// launch behind this one to join.
+template <int DH, bool STEP, bool ORD>
+struct DecodeLds {
+  float red_o[kDecWaves][16][DH];
+  int64_t ord_key[ORD ? kDecThreads : 1];
+  int pages[kMaxChunkPages];
+  int flag;
+  float red_m[kDecWaves][16];
+  float red_l[kDecWaves][16];
+  float step_sn[16];       // fused step: scaled score of the new token per query head
+  float step_vn[DH];       // ... and its V row
+  int step_bad_page[kDecWaves];
+  int step_plan_sh[3];     // ... the append commits; block popped for this request; its crop
+  uint32_t dup_bm[STEP ? kDupBitmapWords : 1];  // the plan's duplicate-id check (one wave)
+  int ord_sid[ORD ? kDecThreads : 1], ord_pick[1];
+};
 
-  const int c = blockIdx.x;
-  int g = blockIdx.y, i = blockIdx.z;  // (request, kv head): grid position, or by length order
+// c: chunk; (i, g): request and kv head, or their place in the length order
+template <int DH, bool STEP, bool ORD, bool CROP, bool EIGHT, bool PARTS>
+__device__ __forceinline__ void decode_split_body(const DecodeArgs &a, int c, int g, int i, DecodeLds<DH, STEP, ORD> &lds) {
+  auto &pages = lds.pages;
+  auto &flag = lds.flag;
+  auto &red_m = lds.red_m;
+  auto &red_l = lds.red_l;
+  auto &red_o = lds.red_o;
+  auto &step_sn = lds.step_sn;
+  auto &step_vn = lds.step_vn;
+  auto &step_bad_page = lds.step_bad_page;
+  auto &step_plan_sh = lds.step_plan_sh;
+  auto &dup_bm = lds.dup_bm;
+  auto &ord_key = lds.ord_key;
+  auto &ord_sid = lds.ord_sid;
+  auto &ord_pick = lds.ord_pick;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const int bs_log2 = a.bs_log2, bs = 1 << bs_log2;
   int s = 0, L = 0, st = 0, L_pool = 0;  // chunking covers [0, L), the pool holds [0, L_pool)
   const bool ordered = ORD && i < a.order_n;  // (the step's commit row is not)
   int s_ord = 0, L_ord = 0;
-  __shared__ int64_t ord_key[ORD ? kDecThreads : 1];
-  __shared__ int ord_sid[ORD ? kDecThreads : 1], ord_pick[1];
   int nc = 0, chunk = 0, t0 = 0, t1 = 0, lp0 = 0, npages = 0;
   bool work = false, pages_ok = true;
 
@@ -1255,27 +1236,18 @@ __global__ __launch_bounds__(kDecThreads, 2) void decode_split_bf16(DecodeArgs a
         step_finish();
       }
     }
-    constexpr bool NANS = EIGHT || PREFIX;
-    if constexpr (PREFIX) {
-      if (st == 0 && L == 0) {  // nothing of its own
-        for (int e = tid; c == 0 && e < a.G * DH; e += kDecThreads) {
-          const int hh = e / DH, dd = e - hh * DH, hq = g * a.G + hh;
-          float M = -INFINITY, acc = 0.f, ls = 0.f;
-          bool bad = false;
-          join_prefix<DH>(a, i, hq, dd, M, acc, ls, bad);
-          ((uint16_t *)a.out)[((int64_t)i * a.Hq + hq) * DH + dd] = f32_to_bf16(bad ? 0.f : row_value<NANS>(acc, ls));
-        }
-        return;
-      }
-    }
     if (st != 0 || L == 0) {
-      if (c == 0) write_zero_rows<uint16_t>(a, i, g, DH, st, esink);
+      if constexpr (PARTS) {
+        if (c == 0 && g == 0 && tid == 0 && st != 0) set_err(esink, st);
+      } else {
+        if (c == 0) write_zero_rows<uint16_t>(a, i, g, DH, st, esink);
+      }
       return;
     }
     if (!work) return;
     if (!pages_ok) {
       write_bad_partial(a, i, g, c, esink);
-      finish_group<uint16_t, NANS, PREFIX, DH>(a, i, g, nc, DH, &flag);
+      if constexpr (!PARTS) finish_group<uint16_t, EIGHT>(a, i, g, nc, DH, &flag);
       return;
     }
     const int t1p = min(t1, L_pool);  // pool entries of this chunk: [t0, t1p)
@@ -1550,10 +1522,14 @@ __global__ __launch_bounds__(kDecThreads, 2) void decode_split_bf16(DecodeArgs a
           ls = -1.f;  // marks the chunk as unusable: the group's rows become zero
         }
       }
+      if constexpr (PARTS) {
+        const int64_t pidx = ((int64_t)i * a.Hq + g * G + hh) * a.max_chunks + c;
+        a.ws_o[pidx * DH + dd] = acc;
+        if (dd == 0) *(float2 *)&a.ws_ml[pidx * 2] = make_float2(M, ls);
+        continue;
+      }
       if (nc == 1) {  // the only chunk: write the result directly
-        bool bad = false;
-        if constexpr (PREFIX) join_prefix<DH>(a, i, g * G + hh, dd, M, acc, ls, bad);
-        ((uint16_t *)a.out)[((int64_t)i * a.Hq + g * G + hh) * DH + dd] = f32_to_bf16(bad ? 0.f : row_value<NANS>(acc, ls));
+        ((uint16_t *)a.out)[((int64_t)i * a.Hq + g * G + hh) * DH + dd] = f32_to_bf16(row_value<EIGHT>(acc, ls));
         continue;
       }
       const int64_t pidx = ((int64_t)i * a.Hq + g * G + hh) * a.max_chunks + c;
@@ -1563,9 +1539,95 @@ __global__ __launch_bounds__(kDecThreads, 2) void decode_split_bf16(DecodeArgs a
         put_partial(&a.ws_ml[pidx * 2 + 1], ls);
       }
     }
-    if (nc > 1) finish_group<uint16_t, NANS, PREFIX, DH>(a, i, g, nc, DH, &flag);
+    if constexpr (!PARTS)
+      if (nc > 1) finish_group<uint16_t, EIGHT>(a, i, g, nc, DH, &flag);
   };
   body();
+}
+
+template <int DH, bool STEP, bool ORD, bool CROP = false, bool EIGHT = false>
+__global__ __launch_bounds__(kDecThreads, 2) void decode_split_bf16(DecodeArgs a) {
+  __shared__ DecodeLds<DH, STEP, ORD> lds;
+  decode_split_body<DH, STEP, ORD, CROP, EIGHT, false>(a, blockIdx.x, blockIdx.y, blockIdx.z, lds);
+}
+
+// ---------------------------------------------------------------------------
+// Behind a shared prefix (sm_decode_attention_shared): one launch for the
+// prefixes' chunks, each for all the vectors of its group, and for the
+// requests' own chunks, side by side; a second joins a row's partials.
+
+struct SharedArgs {
+  DecodeArgs own;
+  PrefillArgs prefix;
+  int prefix_wgs;
+};
+
+template <int DH, int KS, bool EIGHT>
+__global__ __launch_bounds__(kDecThreads, 2) void shared_parts_kernel(SharedArgs a) {
+  static_assert(kDecThreads == 64 * kPrefixWaves, "one workgroup size for both");
+  constexpr int OWN = sizeof(DecodeLds<DH, false, false>), PREFIX = pf_lds_bytes<DH, KS, EIGHT, true>();
+  __shared__ __attribute__((aligned(16))) uint8_t lds[OWN > PREFIX ? OWN : PREFIX];
+  const int b = blockIdx.x;
+  if (b < a.prefix_wgs) {
+    const PfBlock wg = prefix_block<KS>(a.prefix, b);
+    if (wg.m > 0) prefill_body<DH, KS, EIGHT, true>(a.prefix, wg, lds);
+    return;
+  }
+  const int u = b - a.prefix_wgs, pair = u / a.own.max_chunks, i = pair / a.own.Hkv;
+  decode_split_body<DH, false, false, false, EIGHT, true>(a.own, u - pair * a.own.max_chunks, pair - i * a.own.Hkv, i,
+                                                          *(DecodeLds<DH, false, false> *)lds);
+}
+
+// A workgroup for each request and kv head, four dimensions a thread: own
+// chunks, then the prefix's.  kJoinBatch chunks' loads are in flight at a time.
+constexpr int kJoinBatch = 8;
+template <int DH>
+__global__ __launch_bounds__(kDecThreads) void shared_join_kernel(DecodeArgs a, PrefixParts p) {
+  const int i = blockIdx.x / a.Hkv, g = blockIdx.x - i * a.Hkv, per = DH / 4;
+  int L;
+  const int st = seq_status(a, a.seq_ids[i], L);
+  int nc = 0, chunk;
+  if (st == 0) chunking(L, a.chunk_nominal, nc, chunk);
+  const bool none = st != 0 || *p.flag != 0;
+  for (int u = threadIdx.x; u < a.G * per; u += kDecThreads) {
+    const int hq = g * a.G + u / per, d = u % per * 4;
+    float M = -INFINITY, ls = 0.f;
+    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+    bool bad = none;
+    const auto join = [&](const float *o, const float *ml, int chunks) {
+      for (int c0 = 0; c0 < chunks; c0 += kJoinBatch) {
+        float2 m[kJoinBatch];
+        f32x4_t x[kJoinBatch];
+#pragma unroll
+        for (int c = 0; c < kJoinBatch; ++c) {
+          const int at = min(c0 + c, chunks - 1);
+          m[c] = *(const float2 *)(ml + 2 * at);
+          x[c] = *(const f32x4_t *)(o + (int64_t)at * DH);
+        }
+#pragma unroll
+        for (int c = 0; c < kJoinBatch; ++c) {
+          if (c0 + c >= chunks) break;
+          bad |= m[c].y < 0.f;
+          if (m[c].y == 0.f) continue;  // no entries (its output is not written); a NaN goes on
+          const float Mb = fmaxf(M, m[c].x);
+          const float f = M == -INFINITY ? 0.f : exp2f(M - Mb), fc = m[c].x == -INFINITY ? 0.f : exp2f(m[c].x - Mb);
+          acc = acc * f + x[c] * fc;
+          ls = ls * f + m[c].y * fc;
+          M = Mb;
+        }
+      }
+    };
+    if (!none) {
+      const int64_t own = ((int64_t)i * a.Hq + hq) * a.max_chunks, pre = ((int64_t)i * a.Hq + hq) * p.chunks;
+      join(a.ws_o + own * DH + d, a.ws_ml + own * 2, nc);
+      join(p.o + pre * DH + d, p.ml + pre * 2, p.chunks);
+    }
+    uint2 out = make_uint2(0u, 0u);
+    if (!bad)
+      out = make_uint2(pack_bf16x2(row_value<true>(acc[0], ls), row_value<true>(acc[1], ls)),
+                       pack_bf16x2(row_value<true>(acc[2], ls), row_value<true>(acc[3], ls)));
+    *(uint2 *)((uint16_t *)a.out + ((int64_t)i * a.Hq + hq) * DH + d) = out;
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -1868,11 +1930,11 @@ static int device_cus() {
 }
 
 // Workgroups of a bf16 decode kernel resident on one compute unit at once.
-template <int DH, bool STEP, bool CROP, bool EIGHT = false, bool PREFIX = false>
+template <int DH, bool STEP, bool CROP, bool EIGHT = false>
 static int bf16_occupancy() {
   static const int occ = [] {
     int nb = 0;
-    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&nb, decode_split_bf16<DH, STEP, true, CROP, EIGHT, PREFIX>, kDecThreads, 0) !=
+    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&nb, decode_split_bf16<DH, STEP, true, CROP, EIGHT>, kDecThreads, 0) !=
         hipSuccess)
       nb = 1;
     return nb > 0 ? nb : 1;
@@ -1894,9 +1956,7 @@ static sm_status decode_launch(const sm_paged_cache *c, DecodeArgs a, int n, hip
       a.order_n = n;
       a.order_cus = cus;
       const bool d128 = c->head_dim == 128;
-      if (a.prefix.flag)  // (one more that is resident or not only changes the order)
-        a.order_occ = d128 ? bf16_occupancy<128, false, false, true, true>() : bf16_occupancy<64, false, false, true, true>();
-      else if (c->dtype == SM_E4M3)
+      if (c->dtype == SM_E4M3)
         a.order_occ = d128 ? bf16_occupancy<128, false, false, true>() : bf16_occupancy<64, false, false, true>();
       else if (STEP && a.crop)
         a.order_occ = d128 ? bf16_occupancy<128, STEP, STEP>() : bf16_occupancy<64, STEP, STEP>();
@@ -1904,20 +1964,7 @@ static sm_status decode_launch(const sm_paged_cache *c, DecodeArgs a, int n, hip
         a.order_occ = d128 ? bf16_occupancy<128, STEP, false>() : bf16_occupancy<64, STEP, false>();
     }
   }
-  if (a.prefix.flag) {  // (never a step)
-    const auto kernel = [&](auto dh, auto e) {
-      constexpr int DH = decltype(dh)::value;
-      constexpr bool EIGHT = decltype(e)::value;
-      return a.order_n > 0 ? decode_split_bf16<DH, false, true, false, EIGHT, true>
-                           : decode_split_bf16<DH, false, false, false, EIGHT, true>;
-    };
-    const std::integral_constant<int, 128> d128{};
-    const std::integral_constant<int, 64> d64{};
-    const bool eight = c->dtype == SM_E4M3;
-    const auto chosen = c->head_dim == 128 ? (eight ? kernel(d128, std::true_type()) : kernel(d128, std::false_type()))
-                                           : (eight ? kernel(d64, std::true_type()) : kernel(d64, std::false_type()));
-    hipLaunchKernelGGL(chosen, grid, dim3(kDecThreads), 0, stream, a);
-  } else if (c->dtype == SM_E4M3) {  // (never a step)
+  if (c->dtype == SM_E4M3) {  // (never a step)
     const bool ord = a.order_n > 0;
     const auto kernel = c->head_dim == 128 ? (ord ? decode_split_bf16<128, false, true, false, true>
                                                   : decode_split_bf16<128, false, false, false, true>)
@@ -2015,9 +2062,28 @@ SM_API sm_status sm_decode_attention_shared(const sm_paged_cache *c, const int32
   p.parts.ml = (float *)(at + kSharedLine);
   p.parts.o = p.parts.ml + 2 * vectors * chunks;
   p.parts.chunks = (int)chunks;
-  a.prefix = p.parts;
-  const sm_status first = launch_prefix(c, p, q, num_q_heads, scale, stream);
-  return first != SM_OK ? first : decode_launch<false>(c, a, n, stream);
+  // the launch of the parts: at most `blocks` blocks of vectors over all groups
+  const int64_t blocks = (int64_t)n * a.G / (kSharedVec / p.plan.splits) + num_groups;
+  const int64_t prefix_wgs = blocks * a.Hkv * chunks, own_wgs = (int64_t)n * a.Hkv * a.max_chunks;
+  if (prefix_wgs + own_wgs > (1 << 24)) return SM_EINVAL;  // (a launch's threads are counted in 32 bits)
+  SharedArgs sa{a, pf_args(c, q, num_q_heads, scale), (int)prefix_wgs};
+  sa.prefix.p = p;
+  sa.prefix.BQ = 1;
+  sa.prefix.nqb = (int)blocks;
+  const auto kernel = [&](auto dh, auto e) {
+    constexpr int DH = decltype(dh)::value;
+    constexpr bool EIGHT = decltype(e)::value;
+    return p.plan.splits == 2 ? shared_parts_kernel<DH, 2, EIGHT> : shared_parts_kernel<DH, 1, EIGHT>;
+  };
+  const std::integral_constant<int, 128> d128{};
+  const std::integral_constant<int, 64> d64{};
+  const bool eight = c->dtype == SM_E4M3;
+  const auto chosen = c->head_dim == 128 ? (eight ? kernel(d128, std::true_type()) : kernel(d128, std::false_type()))
+                                         : (eight ? kernel(d64, std::true_type()) : kernel(d64, std::false_type()));
+  hipLaunchKernelGGL(chosen, dim3((unsigned)(prefix_wgs + own_wgs)), dim3(kDecThreads), 0, stream, sa);
+  const auto join = c->head_dim == 128 ? shared_join_kernel<128> : shared_join_kernel<64>;
+  hipLaunchKernelGGL(join, dim3((unsigned)(n * a.Hkv)), dim3(kDecThreads), 0, stream, a, p.parts);
+  return hipGetLastError() == hipSuccess ? SM_OK : SM_EHIP;
 }
 
 static std::atomic<int> g_commit_spin_limit{kCommitSpinLimit};

@@ -7,10 +7,11 @@
 
 namespace sm {
 
-constexpr int kSharedVec = 256;        // query vectors of a workgroup whose waves do not split the keys
+constexpr int kSharedVec = 128;        // query vectors of a workgroup whose waves do not split the keys
 constexpr int kSharedStep = 128;       // entries that a chunk is a multiple of
 constexpr int kSharedMostChunk = 8192;
-constexpr int64_t kSharedVectors = 1 << 16;  // vectors x chunks that the cut aims at: 256 for each compute unit
+constexpr int kSharedWgs = 512;        // workgroups that the cut aims at: two for each compute unit
+constexpr int64_t kSharedVectors = (int64_t)kSharedWgs * kSharedVec;  // vectors x chunks, at most
 
 struct SharedPlan {
   int splits;  // groups into which a workgroup's waves split its keys: 256 / splits vectors a workgroup
@@ -29,13 +30,12 @@ inline int64_t shared_most_chunks(int64_t vectors, int max_prefix) {
 
 // n requests of G query heads on each of H kv heads, in `groups` groups.
 inline SharedPlan plan_shared(int n, int H, int G, int groups, int max_prefix) {
-  if (max_prefix <= 0) return SharedPlan{4, kSharedStep, 0};
+  if (max_prefix <= 0) return SharedPlan{2, kSharedStep, 0};
   const int64_t per = ((int64_t)n + groups - 1) / groups * G;  // vectors of a group and kv head
   const int64_t most = shared_most_chunks((int64_t)n * G * H, max_prefix);
-  int ks = 4;
-  while (ks > 1 && per > kSharedVec / ks) ks /= 2;
+  const int ks = per > kSharedVec / 2 ? 1 : 2;
   const int64_t blocks = (per + kSharedVec / ks - 1) / (kSharedVec / ks) * groups * H;
-  int64_t chunks = 256 / blocks;
+  int64_t chunks = kSharedWgs / blocks;
   if (chunks > most) chunks = most;
   if (chunks < 1) chunks = 1;
   int64_t chunk = ((int64_t)max_prefix + chunks - 1) / chunks;

@@ -22,8 +22,4 @@ struct PrefixArgs {
   PrefixParts parts;
 };
 
-// Enqueues the attention of every group's vectors over its prefix.
-sm_status launch_prefix(const sm_paged_cache *c, const PrefixArgs &p, const void *q, int num_q_heads, float scale,
-                        hipStream_t stream);
-
 }  // namespace sm

@@ -46,6 +46,6 @@ def test_the_chunks_cover_any_prefix_and_fit_the_workspace(plan, H, G):
         for groups in (1, 2, 5, 100, 65535):
             for longest in (0, 1, 127, 128, 129, 1000, 8192, 32768, 1000000, 2 ** 31 - 1):
                 splits, chunk, chunks, most = plan(n, H, G, groups, longest)
-                assert splits in (1, 2, 4) and chunk % 128 == 0 and 128 <= chunk <= 8192
+                assert splits in (1, 2) and chunk % 128 == 0 and 128 <= chunk <= 8192
                 assert chunks * chunk >= longest and (chunks - 1) * chunk < max(1, longest)
                 assert max(1, chunks) <= most, (n, groups, longest)
