@@ -1562,15 +1562,15 @@ struct SharedArgs {
   int prefix_wgs;
 };
 
-template <int DH, int KS, bool EIGHT>
+template <int DH, bool EIGHT>
 __global__ __launch_bounds__(kDecThreads, 2) void shared_parts_kernel(SharedArgs a) {
   static_assert(kDecThreads == 64 * kPrefixWaves, "one workgroup size for both");
-  constexpr int OWN = sizeof(DecodeLds<DH, false, false>), PREFIX = pf_lds_bytes<DH, KS, EIGHT, true>();
+  constexpr int OWN = sizeof(DecodeLds<DH, false, false>), PREFIX = pf_lds_bytes<DH, 1, EIGHT, true>();
   __shared__ __attribute__((aligned(16))) uint8_t lds[OWN > PREFIX ? OWN : PREFIX];
   const int b = blockIdx.x;
   if (b < a.prefix_wgs) {
-    const PfBlock wg = prefix_block<KS>(a.prefix, b);
-    if (wg.m > 0) prefill_body<DH, KS, EIGHT, true>(a.prefix, wg, lds);
+    const PfBlock wg = prefix_block(a.prefix, b);
+    if (wg.m > 0) prefill_body<DH, 1, EIGHT, true>(a.prefix, wg, lds);
     return;
   }
   const int u = b - a.prefix_wgs, pair = u / a.own.max_chunks, i = pair / a.own.Hkv;
@@ -2063,7 +2063,7 @@ SM_API sm_status sm_decode_attention_shared(const sm_paged_cache *c, const int32
   p.parts.o = p.parts.ml + 2 * vectors * chunks;
   p.parts.chunks = (int)chunks;
   // the launch of the parts: at most `blocks` blocks of vectors over all groups
-  const int64_t blocks = (int64_t)n * a.G / (kSharedVec / p.plan.splits) + num_groups;
+  const int64_t blocks = (int64_t)n * a.G / kSharedVec + num_groups;
   const int64_t prefix_wgs = blocks * a.Hkv * chunks, own_wgs = (int64_t)n * a.Hkv * a.max_chunks;
   if (prefix_wgs + own_wgs > (1 << 24)) return SM_EINVAL;  // (a launch's threads are counted in 32 bits)
   SharedArgs sa{a, pf_args(c, q, num_q_heads, scale), (int)prefix_wgs};
@@ -2073,7 +2073,7 @@ SM_API sm_status sm_decode_attention_shared(const sm_paged_cache *c, const int32
   const auto kernel = [&](auto dh, auto e) {
     constexpr int DH = decltype(dh)::value;
     constexpr bool EIGHT = decltype(e)::value;
-    return p.plan.splits == 2 ? shared_parts_kernel<DH, 2, EIGHT> : shared_parts_kernel<DH, 1, EIGHT>;
+    return shared_parts_kernel<DH, EIGHT>;
   };
   const std::integral_constant<int, 128> d128{};
   const std::integral_constant<int, 64> d64{};

@@ -141,9 +141,8 @@ __device__ __forceinline__ PfBlock pf_block(const PrefillArgs &a) {
 // SHARED: workgroup b -> (chunk, kv head, block of vectors of a group).  The
 // blocks of one chunk and head land on one XCD, as above.  m = 0: nothing to
 // do.  Every wave finds the group by itself, 64 of them at a time.
-template <int KS>
 __device__ __forceinline__ PfBlock prefix_block(const PrefillArgs &a, int b) {
-  constexpr int COLS = kSharedVec / KS;
+  constexpr int COLS = kSharedVec;
   const PrefixArgs &p = a.p;
   const int nb = a.nqb, P = p.parts.chunks * a.Hkv, Pfull = P & ~7, lane = threadIdx.x & 63;
   int pair, j;
@@ -214,9 +213,8 @@ __device__ __forceinline__ PfBlock prefix_block(const PrefillArgs &a, int b) {
 }
 
 // The chunk's sums of this workgroup's vectors where it has no entries (0) or is unusable (-1).
-template <int KS>
 __device__ __forceinline__ void prefix_none(const PrefillArgs &a, const PfBlock &wg, float sum) {
-  constexpr int COLS = kSharedVec / KS;
+  constexpr int COLS = kSharedVec;
   for (int v = threadIdx.x; v < COLS; v += 64 * kPrefixWaves) {
     const int col = wg.qb * COLS + v, member = col / a.G;
     if (member >= wg.m) break;
@@ -239,7 +237,7 @@ __device__ __forceinline__ float inverse_sum(float l) {
 template <int DH, int KS, bool EIGHT = false, bool SHARED = false>
 constexpr int pf_lds_bytes() {
   const int W = SHARED ? kPrefixWaves : kPfWaves;
-  const int keys = SHARED ? 64 / KS : KS == 4 ? 32 : 64, vp = keys == 32 ? 32 : keys + 8;
+  const int keys = KS == 4 ? 32 : 64, vp = keys == 32 ? 32 : keys + 8;
   const int ring = 4 * (KS * keys * (DH + 8) + KS * DH * vp) + (EIGHT ? 8 * KS * keys : 0);
   const int merge = KS > 1 ? (W * 32 * (DH + 4) + W * 64) * 4 : 0;
   return (ring > merge ? ring : merge) + (SHARED ? kPrefixPages : kPfMaxPages) * 4 + 16;
@@ -248,7 +246,8 @@ constexpr int pf_lds_bytes() {
 template <int DH, int KS, bool EIGHT = false, bool SHARED = false>
 __device__ __forceinline__ void prefill_body(const PrefillArgs &a, const PfBlock &wg, uint8_t *lds) {
   constexpr int W = SHARED ? kPrefixWaves : kPfWaves, THREADS = 64 * W;
-  constexpr int KEYS = SHARED ? 64 / KS : KS == 4 ? 32 : 64;  // keys per tile
+  constexpr int KEYS = KS == 4 ? 32 : 64;  // keys per tile
+  static_assert(!SHARED || KS == 1, "the waves over a prefix do not split its keys");
   constexpr int SUB = KEYS / 32;           // 32-key score blocks per tile
   constexpr int SPAN = KS * KEYS;          // keys per pass: one tile for each of the KS wave groups
   constexpr int VG = W / KS;        // waves per group: 32 VG query vectors per workgroup
@@ -286,7 +285,7 @@ __device__ __forceinline__ void prefill_body(const PrefillArgs &a, const PfBlock
 
   if constexpr (SHARED) {
     if (!wg.ok || wg.k0 >= L) {
-      prefix_none<KS>(a, wg, wg.ok ? 0.f : -1.f);
+      prefix_none(a, wg, wg.ok ? 0.f : -1.f);
       return;
     }
   } else if (!wg.ok) {  // block 0 reports the request and zeroes its rows
@@ -323,7 +322,7 @@ __device__ __forceinline__ void prefill_body(const PrefillArgs &a, const PfBlock
   if (*bad_flag) {  // a corrupt block table: this block's rows are zero
     if (tid == 0) set_err(a.err, SM_ERR_EINVAL);
     if constexpr (SHARED) {
-      prefix_none<KS>(a, wg, -1.f);
+      prefix_none(a, wg, -1.f);
       return;
     }
     const int per_row = a.G * DH;
@@ -336,7 +335,7 @@ __device__ __forceinline__ void prefill_body(const PrefillArgs &a, const PfBlock
 
   // ---- this wave's 32 query vectors: v = 32 vg + c32 -> query head g G + v / BQ, row q_lo + v % BQ ----
   // (SHARED: vector v of the group's -> request v / G, query head v % G; all keys)
-  const int v = 32 * vg + c32 + (SHARED ? qb * (kSharedVec / KS) : 0);
+  const int v = 32 * vg + c32 + (SHARED ? qb * kSharedVec : 0);
   const int rr = SHARED ? v / a.G : v % a.BQ, hh = SHARED ? v - rr * a.G : v / a.BQ;
   const bool vok = SHARED ? rr < m : hh < a.G && rr < nq;
   const int vhead = g * a.G + (vok ? hh : 0);
@@ -633,13 +632,6 @@ __device__ __forceinline__ void prefill_body(const PrefillArgs &a, const PfBlock
     for (int k = 0; k < live; ++k)
 #pragma unroll
       for (int c = 0; c < DW / 4; ++c) y[c] += *(const f32x4_t *)&po[((k * VG + vg) * 32 + c32) * OPITCH + d0 + 4 * c];
-    if constexpr (SHARED) {
-      const int64_t at = ((int64_t)vrow * a.Hq + vhead) * a.p.parts.chunks + wg.c;
-#pragma unroll
-      for (int c = 0; c < DW / 4; ++c) *(f32x4_t *)&a.p.parts.o[at * DH + d0 + 4 * c] = y[c];
-      if (kg == 0 && h2 == 0) *(float2 *)&a.p.parts.ml[2 * at] = make_float2(mb, l_tot);
-      return;
-    }
     const float inv = inverse_sum<EIGHT>(l_tot);
     uint16_t *op = a.out + ((int64_t)vrow * a.Hq + vhead) * DH + d0;
 #pragma unroll

@@ -7,14 +7,13 @@
 
 namespace sm {
 
-constexpr int kSharedVec = 128;        // query vectors of a workgroup whose waves do not split the keys
+constexpr int kSharedVec = 128;        // query vectors of a workgroup
 constexpr int kSharedStep = 128;       // entries that a chunk is a multiple of
 constexpr int kSharedMostChunk = 8192;
-constexpr int kSharedWgs = 512;        // workgroups that the cut aims at: two for each compute unit
+constexpr int kSharedWgs = 256;        // workgroups that the cut aims at: one for each compute unit
 constexpr int64_t kSharedVectors = (int64_t)kSharedWgs * kSharedVec;  // vectors x chunks, at most
 
 struct SharedPlan {
-  int splits;  // groups into which a workgroup's waves split its keys: 256 / splits vectors a workgroup
   int chunk;   // entries of a chunk, a multiple of kSharedStep
   int chunks;  // chunks of the longest prefix
 };
@@ -30,18 +29,17 @@ inline int64_t shared_most_chunks(int64_t vectors, int max_prefix) {
 
 // n requests of G query heads on each of H kv heads, in `groups` groups.
 inline SharedPlan plan_shared(int n, int H, int G, int groups, int max_prefix) {
-  if (max_prefix <= 0) return SharedPlan{2, kSharedStep, 0};
+  if (max_prefix <= 0) return SharedPlan{kSharedStep, 0};
   const int64_t per = ((int64_t)n + groups - 1) / groups * G;  // vectors of a group and kv head
   const int64_t most = shared_most_chunks((int64_t)n * G * H, max_prefix);
-  const int ks = per > kSharedVec / 2 ? 1 : 2;
-  const int64_t blocks = (per + kSharedVec / ks - 1) / (kSharedVec / ks) * groups * H;
+  const int64_t blocks = (per + kSharedVec - 1) / kSharedVec * groups * H;
   int64_t chunks = kSharedWgs / blocks;
   if (chunks > most) chunks = most;
   if (chunks < 1) chunks = 1;
   int64_t chunk = ((int64_t)max_prefix + chunks - 1) / chunks;
   chunk = (chunk + kSharedStep - 1) / kSharedStep * kSharedStep;
   if (chunk > kSharedMostChunk) chunk = kSharedMostChunk;
-  return SharedPlan{ks, (int)chunk, (int)(((int64_t)max_prefix + chunk - 1) / chunk)};
+  return SharedPlan{(int)chunk, (int)(((int64_t)max_prefix + chunk - 1) / chunk)};
 }
 
 }  // namespace sm

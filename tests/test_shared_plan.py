@@ -13,17 +13,16 @@ SHIM = """
 #include "shared_plan.hpp"
 extern "C" void plan(int n, int H, int G, int groups, int max_prefix, int *out) {
   const sm::SharedPlan p = sm::plan_shared(n, H, G, groups, max_prefix);
-  out[0] = p.splits;
-  out[1] = p.chunk;
-  out[2] = p.chunks;
-  out[3] = (int)sm::shared_most_chunks((long long)n * G * H, max_prefix);
+  out[0] = p.chunk;
+  out[1] = p.chunks;
+  out[2] = (int)sm::shared_most_chunks((long long)n * G * H, max_prefix);
 }
 """
 
 
 @pytest.fixture(scope="session")
 def plan(tmp_path_factory):
-    """plan(requests, kv heads, group, groups, longest prefix): (splits, chunk, chunks, chunks that the workspace holds)"""
+    """plan(requests, kv heads, group, groups, longest prefix): (chunk, chunks, chunks that the workspace holds)"""
     if shutil.which("g++") is None:
         pytest.skip("g++ not available")
     d = tmp_path_factory.mktemp("plan")
@@ -34,7 +33,7 @@ def plan(tmp_path_factory):
     f = C.CDLL(str(d / "plan.so")).plan
 
     def call(*a):
-        out = (C.c_int * 4)()
+        out = (C.c_int * 3)()
         f(*a, out)
         return tuple(out)
     return call
@@ -45,7 +44,7 @@ def test_the_chunks_cover_any_prefix_and_fit_the_workspace(plan, H, G):
     for n in (1, 2, 3, 16, 33, 128, 1000, 4096, 65535 // H):
         for groups in (1, 2, 5, 100, 65535):
             for longest in (0, 1, 127, 128, 129, 1000, 8192, 32768, 1000000, 2 ** 31 - 1):
-                splits, chunk, chunks, most = plan(n, H, G, groups, longest)
-                assert splits in (1, 2) and chunk % 128 == 0 and 128 <= chunk <= 8192
+                chunk, chunks, most = plan(n, H, G, groups, longest)
+                assert chunk % 128 == 0 and 128 <= chunk <= 8192
                 assert chunks * chunk >= longest and (chunks - 1) * chunk < max(1, longest)
                 assert max(1, chunks) <= most, (n, groups, longest)
