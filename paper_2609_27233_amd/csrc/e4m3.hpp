@@ -30,18 +30,17 @@ __device__ __forceinline__ int exp_byte(float most) {
 __device__ __forceinline__ float exp_scale(int byte) { return __uint_as_float((uint32_t)byte << 23); }     // 2^(byte - 127)
 __device__ __forceinline__ float exp_inverse(int byte) { return __uint_as_float((uint32_t)(254 - byte) << 23); }
 
-// A quotient as e4m3 takes it: above 448 (only under the largest exponent) the
-// largest value, an infinity NaN.
+// Four quotients -> four e4m3 values, the first in the low byte (to nearest,
+// ties to even; NaN and infinities become NaN).
+__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+  return (uint32_t)w;
+}
+// Under the largest exponent a finite quotient may be above 448: the largest value then.
 __device__ __forceinline__ float in_e4m3(float z) {
   const float size = fabsf(z);
-  return size <= kMostE4m3 ? z : size < INFINITY ? copysignf(kMostE4m3, z) : NAN;
-}
-
-// Four quotients -> four e4m3 values, the first in the low byte (to nearest, ties to even).
-__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(in_e4m3(a), in_e4m3(b), 0, false);
-  w = __builtin_amdgcn_cvt_pk_fp8_f32(in_e4m3(c), in_e4m3(d), w, true);
-  return (uint32_t)w;
+  return size > kMostE4m3 && size < INFINITY ? copysignf(kMostE4m3, z) : z;
 }
 
 // Four e4m3 values times 2^(scale's exponent) -> two pairs of bf16, exact.
@@ -56,26 +55,45 @@ __device__ __forceinline__ u32x4_t e4m3_to_bf16(uint32_t a, uint32_t b, float sc
   return u32x4_t{e4m3_lo(a, scale), e4m3_hi(a, scale), e4m3_lo(b, scale), e4m3_hi(b, scale)};
 }
 
-// Largest |feature| of 16 bytes of bf16, infinities and NaN left out.
-__device__ __forceinline__ float largest(const float (&f)[8]) {
-  float m = fmaxf(fmaxf(fabsf(f[0]), fabsf(f[1])), fmaxf(fabsf(f[2]), fabsf(f[3])));  // (fmaxf leaves NaN out)
-  m = fmaxf(m, fmaxf(fmaxf(fabsf(f[4]), fabsf(f[5])), fmaxf(fabsf(f[6]), fabsf(f[7]))));
-  if (m == INFINITY) {
-    m = 0.f;
+typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+
+// Largest |feature| of 16 bytes of bf16, as bf16's bits.  (Without its sign it
+// ascends as the 16-bit integer: two features to an instruction.)
+__device__ __forceinline__ uint32_t largest_bits(u32x4_t v) {
+  u16x2_t m = __builtin_bit_cast(u16x2_t, v[0] & 0x7fff7fffu);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) m = fabsf(f[e]) < INFINITY ? fmaxf(m, fabsf(f[e])) : m;
+  for (int i = 1; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2_t, v[i] & 0x7fff7fffu));
+  return max((uint32_t)m[0], (uint32_t)m[1]);
+}
+// A row whose largest feature passes these bits (2^126) has an infinity or NaN
+// in it, which its maximum leaves out, or the largest exponent, under which a
+// feature may have to be cut to 448.
+constexpr uint32_t kPlainBits = 0x7e80u;
+__device__ __forceinline__ float largest(u32x4_t v) {
+  uint32_t most = largest_bits(v);
+  if (most >= 0x7f80u) {
+    most = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t x = v[i / 2] >> (16 * (i % 2)) & 0x7fffu;
+      if (x < 0x7f80u) most = max(most, x);
+    }
   }
-  return m >= 0.f ? m : 0.f;  // (nothing but NaN)
+  return __uint_as_float(most << 16);
 }
 
-// Maximum over the 8 or 16 neighbouring lanes of a head (8 features each).
-template <int LANES>
-__device__ __forceinline__ float head_max(float v) {
-  v = fmaxf(v, dpp_f32<kDppXor1>(v));
-  v = fmaxf(v, dpp_f32<kDppXor2>(v));
-  v = fmaxf(v, dpp_f32<kDppHalfMirror>(v));
-  if constexpr (LANES == 16) v = fmaxf(v, dpp_f32<kDppMirror>(v));
-  return v;
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_bits(uint32_t v) {
+  return __float_as_uint(dpp_f32<CTRL>(__uint_as_float(v)));
+}
+// Maximum (of values >= 0, by their bits) over the lanes of a head, 8 features
+// each: 16 neighbours, or 8 where the head has 64.
+__device__ __forceinline__ uint32_t head_max(uint32_t v, bool wide) {
+  v = max(v, dpp_bits<kDppXor1>(v));
+  v = max(v, dpp_bits<kDppXor2>(v));
+  v = max(v, dpp_bits<kDppHalfMirror>(v));
+  const uint32_t both = max(v, dpp_bits<kDppMirror>(v));
+  return wide ? both : v;
 }
 
 // Bytes i of four words: in[r] byte d -> out[d] byte r.

@@ -266,79 +266,130 @@ __device__ __forceinline__ T *page_of(T *pool, int s, const WriteArgs &w, int *i
 // e4m3 pages (rows of bf16).  A head's row is held by the D / 8 neighbouring
 // lanes of its 16-byte chunks, which share its largest input feature.
 
-// The turned features of chunk c of row x, and the largest of them before the turn.
-template <bool HALF, bool STREAM>
-__device__ __forceinline__ float turned_chunk(const uint16_t *x, int c, int R, const float2 *cs, float (&y)[8]) {
-  const int at = 8 * c;
-  Vec16<uint16_t>::open(load_as<STREAM, u32x4_t>(x + at), y);
-  const float most = largest(y);
-  if (at >= R) return most;
-  if constexpr (HALF) {
-    const bool first = at < R / 2;
-    float z[8];
-    Vec16<uint16_t>::open(load_as<STREAM, u32x4_t>(x + (first ? at + R / 2 : at - R / 2)), z);
-    cs += first ? at : at - R / 2;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float2 t = first ? turned(y[e], z[e], cs[e]) : turned(z[e], y[e], cs[e]);
-      y[e] = first ? t.x : t.y;
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; e += 2) {
-      const float2 t = turned(y[e], y[e + 1], cs[at / 2 + e / 2]);
-      y[e] = t.x;
-      y[e + 1] = t.y;
-    }
+// Chunk c of a row: its features and, in the half layout, the other halves of
+// their pairs, with the sign to be added to them: (a, b) -> a cos - b sin
+// where a lies, b cos + a sin where b does.
+template <bool HALF>
+struct Chunk {
+  u32x4_t own, other;
+  template <bool STREAM>
+  __device__ __forceinline__ void load(const uint16_t *x, int c, int R) {
+    const int at = 8 * c;
+    own = load_as<STREAM, u32x4_t>(x + at);
+    if (HALF && at < R)
+      other = load_as<STREAM, u32x4_t>(x + (at < R / 2 ? at + R / 2 : at - R / 2)) ^ (at < R / 2 ? 0x80008000u : 0u);
   }
-  return most;
+  __device__ __forceinline__ float turn(int c, int R, const float2 *cs, float (&y)[8]) const {
+    const int at = 8 * c;
+    Vec16<uint16_t>::open(own, y);
+    if (at < R) {
+      if constexpr (HALF) {
+        float z[8];
+        Vec16<uint16_t>::open(other, z);
+        cs += at < R / 2 ? at : at - R / 2;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = y[e] * cs[e].x + z[e] * cs[e].y;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+          const float2 t = turned(y[e], y[e + 1], cs[at / 2 + e / 2]);
+          y[e] = t.x;
+          y[e + 1] = t.y;
+        }
+      }
+    }
+    return largest(own);
+  }
+};
+// Eight features from any element's address, one by one.
+__device__ __forceinline__ u32x4_t features8(const uint16_t *x) {
+  u32x4_t v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = (uint32_t)x[2 * i] | (uint32_t)x[2 * i + 1] << 16;
+  return v;
 }
 // The same, a feature at a time: any R, any address.
 template <bool HALF>
-__device__ __forceinline__ float turned_features(const uint16_t *x, int c, int R, const float2 *cs, float (&y)[8]) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e) y[e] = bf16_to_f32(x[8 * c + e]);
-  const float most = largest(y);
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const int i = 8 * c + e, j = HALF ? (i < R / 2 ? i : i - R / 2) : i / 2;  // its pair
-    if (i >= R) continue;
-    const bool first = HALF ? i < R / 2 : i % 2 == 0;
-    const float other = bf16_to_f32(x[HALF ? (first ? i + R / 2 : j) : i ^ 1]);
-    const float2 t = first ? turned(y[e], other, cs[j]) : turned(other, y[e], cs[j]);
-    y[e] = first ? t.x : t.y;
+struct Features {
+  const uint16_t *x;
+  template <bool STREAM>
+  __device__ __forceinline__ void load(const uint16_t *row, int, int) {
+    x = row;
   }
-  return most;
-}
+  __device__ __forceinline__ float turn(int c, int R, const float2 *cs, float (&y)[8]) const {
+    const u32x4_t own = features8(x + 8 * c);
+    Vec16<uint16_t>::open(own, y);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int i = 8 * c + e, j = HALF ? (i < R / 2 ? i : i - R / 2) : i / 2;  // its pair
+      if (i >= R) continue;
+      const bool first = HALF ? i < R / 2 : i % 2 == 0;
+      const float pair = bf16_to_f32(x[HALF ? (first ? i + R / 2 : j) : i ^ 1]);
+      const float2 t = first ? turned(y[e], pair, cs[j]) : turned(pair, y[e], cs[j]);
+      y[e] = first ? t.x : t.y;
+    }
+    return largest(own);
+  }
+};
 
-__device__ __forceinline__ uint2 quantised(const float (&y)[8], int byte) {
+__device__ __forceinline__ uint2 quantised(float (&y)[8], int byte) {
   const float inv = exp_inverse(byte);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) y[e] *= inv;
+  if (byte == kMostExp + kExpBias) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = in_e4m3(y[e]);
+  }
+  return make_uint2(pack_e4m3(y[0], y[1], y[2], y[3]), pack_e4m3(y[4], y[5], y[6], y[7]));
+}
+// 16 bytes of a row as they lie in memory, none to be cut
+__device__ __forceinline__ uint2 scaled(u32x4_t v, float inv) {
+  float y[8];
+  Vec16<uint16_t>::open(v, y);
   return make_uint2(pack_e4m3(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv),
                     pack_e4m3(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv));
 }
+__device__ __forceinline__ uint2 quantised(u32x4_t v, int byte) {
+  float y[8];
+  Vec16<uint16_t>::open(v, y);
+  return quantised(y, byte);
+}
 
-// Maximum over a head's lanes, 8 (D = 64) or 16.
-__device__ __forceinline__ float over_head(float m, int dh_log2) { return dh_log2 == 7 ? head_max<16>(m) : head_max<8>(m); }
+// The exponent byte of a row from its lanes' largest features.
+__device__ __forceinline__ int head_byte(float most, float factor, int dh_log2) {
+  return exp_byte(__uint_as_float(head_max(__float_as_uint(most), dh_log2 == 7)) * factor);
+}
 
-// K heads [k0, k1) of rows [r0, r0 + nr) into their pages, slots slot[0 .. nr).
-// chunk(x, c, row's cosines and sines, y): turned_chunk or turned_features.
-template <class F>
+// K heads [k0, k1) of rows [r0, r0 + nr) into their pages, slots slot[0 .. nr):
+// a thread takes one chunk of a row for HEADS heads, all of them loaded before
+// the first is turned.  CHUNK: Chunk or Features.
+template <class CHUNK, int HEADS, bool STREAM>
 __device__ __forceinline__ void write_k_e4m3(const RopeArgs &a, const WriteArgs &w, int64_t r0, int nr, int k0, int k1,
-                                             const int *slot, const float2 *cs, F chunk) {
-  const int lanes_log2 = w.dh_log2 - 3, D = 1 << w.dh_log2;
+                                             const int *slot, const float2 *cs) {
+  const int lanes_log2 = w.dh_log2 - 3, D = 1 << w.dh_log2, parts = (k1 - k0 + HEADS - 1) / HEADS;
   const float factor = fmaxf(1.f, fabsf(a.scale)), inv = 1.f / nr;
-  for (int u = threadIdx.x; u < (nr * (k1 - k0)) << lanes_log2; u += kRotThreads) {
-    const int c = u & ((1 << lanes_log2) - 1), hr = u >> lanes_log2;
-    const int hh = (int)((hr + 0.5f) * inv), r = hr - hh * nr, h = k0 + hh;  // (exact below 2^21)
-    float y[8];
-    const float most = over_head(chunk((const uint16_t *)w.k.in + (r0 + r) * w.k.in_stride + h * D, c, cs + r * (a.R / 2), y),
-                                 w.dh_log2);
-    const int byte = exp_byte(most * factor), sl = slot[r];
+  for (int u = threadIdx.x; u < (nr * parts) << lanes_log2; u += kRotThreads) {
+    const int c = u & ((1 << lanes_log2) - 1), pr = u >> lanes_log2;
+    const int part = (int)((pr + 0.5f) * inv), r = pr - part * nr, h0 = k0 + part * HEADS;  // (exact below 2^21)
+    const uint16_t *x = (const uint16_t *)w.k.in + (r0 + r) * w.k.in_stride;
+    CHUNK chunk[HEADS];
+#pragma unroll
+    for (int i = 0; i < HEADS; ++i) chunk[i].template load<STREAM>(x + min(h0 + i, k1 - 1) * D, c, a.R);
+    const int sl = slot[r];
     if (sl < 0) continue;
     int at;
-    uint8_t *page = page_of((uint8_t *)w.k_pool, sl, w, &at) + ((int64_t)h << (w.bs_log2 + w.dh_log2));
-    *(uint2 *)(page + at * D + 8 * c) = quantised(y, byte);
-    if (c == 0) w.k_exp[(((int64_t)(sl >> w.bs_log2) * w.k.heads + h) << w.bs_log2) + at] = (uint8_t)byte;
+    const int64_t head = (int64_t)1 << (w.bs_log2 + w.dh_log2);
+    uint8_t *page = page_of((uint8_t *)w.k_pool, sl, w, &at) + at * D + 8 * c;
+    uint8_t *exps = w.k_exp + (((int64_t)(sl >> w.bs_log2) * w.k.heads) << w.bs_log2) + at;
+#pragma unroll
+    for (int i = 0; i < HEADS; ++i) {
+      float y[8];
+      const float most = chunk[i].turn(c, a.R, cs + r * (a.R / 2), y);
+      const int byte = head_byte(most, factor, w.dh_log2), h = h0 + i;
+      if (h >= k1) continue;
+      *(uint2 *)(page + h * head) = quantised(y, byte);
+      if (c == 0) exps[h << w.bs_log2] = (uint8_t)byte;
+    }
   }
 }
 
@@ -352,8 +403,12 @@ __device__ __forceinline__ void store_v_e4m3(const WriteArgs &w, int sl, int h, 
 }
 
 // V heads [g0, g1): a thread takes the 8 features of a chunk for a group of
-// rows that fill consecutive slots of 16 aligned ones; a whole group leaves as
-// 16 bytes a feature.
+// rows that fill consecutive slots of 8 aligned ones; a whole group leaves as
+// 8 bytes a feature.  (Groups of 16 rows, 16 bytes a feature, held 154
+// registers, three waves to a SIMD: 39,328 rows of 8 heads x 128 took 96 us
+// for keys and values where groups of 8 take 80, and bf16 pages 63.  The
+// largest features go as integers and the rare rows apart: with a branch for
+// each row the same took 115.)
 template <bool STREAM>
 __device__ __forceinline__ void write_v_e4m3(const WriteArgs &w, int64_t r0, int g0, int g1, int groups, const int *group,
                                              const int *slot) {
@@ -365,53 +420,62 @@ __device__ __forceinline__ void write_v_e4m3(const WriteArgs &w, int64_t r0, int
     const int f = group[g], n = group[g + 1] - f, sl = slot[f];
     if (sl < 0) continue;
     const uint16_t *in = (const uint16_t *)w.v.in + (r0 + f) * w.v.in_stride + h * D + 8 * c;
-    if (n < 16) {
+    const auto one_by_one = [&] {
+#pragma unroll 1
       for (int i = 0; i < n; ++i) {
-        float y[8];
-        Vec16<uint16_t>::open(load_as<STREAM, u32x4_t>(in + i * w.v.in_stride), y);
-        const int byte = exp_byte(over_head(largest(y), w.dh_log2));
-        store_v_e4m3(w, sl + i, h, c, byte, quantised(y, byte));
+        const u32x4_t v = load_as<STREAM, u32x4_t>(in + i * w.v.in_stride);
+        const int byte = head_byte(largest(v), 1.f, w.dh_log2);
+        store_v_e4m3(w, sl + i, h, c, byte, quantised(v, byte));
       }
+    };
+    u32x4_t v[8];
+    uint32_t most[8], worst = 0;
+    if (n == 8) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = load_as<STREAM, u32x4_t>(in + i * w.v.in_stride);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        most[i] = head_max(largest_bits(v[i]), w.dh_log2 == 7);
+        worst = max(worst, most[i]);
+      }
+    }
+    if (n < 8 || worst > kPlainBits) {
+      one_by_one();
       continue;
     }
-    u32x4_t v[16];
+    uint2 out[8], bytes;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = load_as<STREAM, u32x4_t>(in + i * w.v.in_stride);
-    u32x4_t out[8], bytes;
-#pragma unroll
-    for (int q4 = 0; q4 < 4; ++q4) {  // four rows: four bytes of each feature's 16
+    for (int q4 = 0; q4 < 2; ++q4) {  // four rows: four bytes of each feature's 8
       uint32_t lo[4], hi[4], tlo[4], thi[4], b4 = 0;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        float y[8];
-        Vec16<uint16_t>::open(v[4 * q4 + i], y);
-        const int byte = exp_byte(over_head(largest(y), w.dh_log2));
+        const int byte = exp_byte(__uint_as_float(most[4 * q4 + i] << 16));
         b4 |= (uint32_t)byte << (8 * i);
-        const uint2 q = quantised(y, byte);
+        const uint2 q = scaled(v[4 * q4 + i], exp_inverse(byte));
         lo[i] = q.x;
         hi[i] = q.y;
       }
-      bytes[q4] = b4;
+      (q4 ? bytes.y : bytes.x) = b4;
       transpose4(lo, tlo);
       transpose4(hi, thi);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        out[e][q4] = tlo[e];
-        out[4 + e][q4] = thi[e];
+        (q4 ? out[e].y : out[e].x) = tlo[e];
+        (q4 ? out[4 + e].y : out[4 + e].x) = thi[e];
       }
     }
     int at;
     uint8_t *to = page_of((uint8_t *)w.v_pool, sl, w, &at) + ((((int64_t)h << w.dh_log2) + 8 * c) << w.bs_log2) + at;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) *(u32x4_t *)(to + ((int64_t)e << w.bs_log2)) = out[e];
-    if (c == 0) *(u32x4_t *)(w.v_exp + (((int64_t)(sl >> w.bs_log2) * w.v.heads + h) << w.bs_log2) + at) = bytes;
+    for (int e = 0; e < 8; ++e) *(uint2 *)(to + ((int64_t)e << w.bs_log2)) = out[e];
+    if (c == 0) *(uint2 *)(w.v_exp + (((int64_t)(sl >> w.bs_log2) * w.v.heads + h) << w.bs_log2) + at) = bytes;
   }
 }
 
 // EIGHT: e4m3 pages, T = uint16_t
 template <typename T, bool HALF, bool STREAM, bool EIGHT = false>
 __global__ __launch_bounds__(kRotThreads) void kv_write_kernel(RopeArgs a, WriteArgs w, int heads_per) {
-  constexpr int VEC = 16 / sizeof(T), FILL = EIGHT ? 16 : VEC;
+  constexpr int VEC = 16 / sizeof(T), FILL = EIGHT ? 8 : VEC;
   extern __shared__ float2 cs[];
   __shared__ int slot[kMostRows + 1], group[kMostRows + 1];
   const int t = threadIdx.x, lane = t & 63, D = 1 << w.dh_log2, bs = 1 << w.bs_log2;
@@ -487,10 +551,7 @@ __global__ __launch_bounds__(kRotThreads) void kv_write_kernel(RopeArgs a, Write
       unit.template run<STREAM>(h0 + part, hq1, share, [&](int h) { return q + h * D; }, [&](int h) { return out + h * D; });
     });
   if constexpr (EIGHT) {
-    if (k1 > k0)
-      write_k_e4m3(a, w, r0, nr, k0, k1, slot, cs, [&](const uint16_t *x, int c, const float2 *row_cs, float (&y)[8]) {
-        return turned_chunk<HALF, STREAM>(x, c, a.R, row_cs, y);
-      });
+    if (k1 > k0) write_k_e4m3<Chunk<HALF>, 4, STREAM>(a, w, r0, nr, k0, k1, slot, cs);
   } else if (k1 > k0)
     each_unit<false>(nr, a.per_head, k1 - k0, [&](int r, int j, int part, int share) {
       const int sl = slot[r];
@@ -529,11 +590,9 @@ __global__ __launch_bounds__(kRotThreads) void kv_write_any_kernel(RopeArgs a, W
     for (int u = t; g1 > g0 && u < (nr * (g1 - g0)) << lanes_log2; u += kRotThreads) {
       const int c = u & ((1 << lanes_log2) - 1), hr = u >> lanes_log2, h = g0 + hr / nr, r = hr % nr;
       const uint16_t *in = (const uint16_t *)w.v.in + (r0 + r) * w.v.in_stride + h * D + 8 * c;
-      float y[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = bf16_to_f32(in[e]);
-      const int byte = exp_byte(over_head(largest(y), w.dh_log2));
-      if (slot[r] >= 0) store_v_e4m3(w, slot[r], h, c, byte, quantised(y, byte));
+      const u32x4_t v = features8(in);
+      const int byte = head_byte(largest(v), 1.f, w.dh_log2);
+      if (slot[r] >= 0) store_v_e4m3(w, slot[r], h, c, byte, quantised(v, byte));
     }
   } else
   for (int r = 0; r < nr && g1 > g0; ++r) {
@@ -551,10 +610,7 @@ __global__ __launch_bounds__(kRotThreads) void kv_write_any_kernel(RopeArgs a, W
       unit.template run<false>(h0 + part, hq1, share, [&](int h) { return q + h * D; }, [&](int h) { return out + h * D; });
     });
   if constexpr (EIGHT) {
-    if (k1 > k0)
-      write_k_e4m3(a, w, r0, nr, k0, k1, slot, cs, [&](const uint16_t *x, int c, const float2 *row_cs, float (&y)[8]) {
-        return turned_features<HALF>(x, c, a.R, row_cs, y);
-      });
+    if (k1 > k0) write_k_e4m3<Features<HALF>, 1, false>(a, w, r0, nr, k0, k1, slot, cs);
   } else if (k1 > k0)
     each_unit<true>(nr, a.per_head, k1 - k0, [&](int r, int j, int part, int share) {
       if (slot[r] < 0) return;
