@@ -220,3 +220,38 @@ def test_the_draws_follow_the_weights():
     counts = np.bincount(tokens, minlength=V)
     assert set(np.nonzero(counts)[0]) <= set(ids)
     assert np.abs(counts[ids] - n * w / w.sum()).max() <= 1.0
+
+
+@pytest.mark.parametrize("dt", [BF, F32], ids=str)
+def test_lists_that_do_not_suffice(dt):
+    """A k of thousands and ends of the mass among thousands of near-equal logits: cut by passes over the row."""
+    rng = np.random.RandomState(11)
+    x = logits(128256, 8, dt, 12)
+    x[4:6] *= 1e-3                                               # all in a bin or two
+    x[6:] = torch.from_numpy(rng.choice([0.0, 0.5, 1.0], (2, 128256))).to(dt).to(dev())
+    u = rng.uniform(size=8)
+    check(x, u, k=[5000, 20000, 60000, 128255, 4097, 100000, 50000, 1])
+    check(x, u, k=[5000, 20000, 60000, 128255, 4097, 100000, 50000, 9], p=np.full(8, 0.7), m=np.full(8, 1e-5))
+    check(x, u, p=np.linspace(0.05, 0.9999, 8), T=[1.0, 0.3, 9.0, 1e-45, 1.0, 0.5, 1.0, 2.0])
+
+
+def test_many_rows_each_with_its_own_settings():
+    """More rows than the workspace holds at a time."""
+    rng = np.random.RandomState(13)
+    say("rows", 1500)
+    check(logits(1030, 1500, BF, 14), rng.uniform(size=1500), *settings(rng, 1500))
+
+
+def test_refused_rows_leave_the_workspace_as_any_do():
+    rng = np.random.RandomState(15)
+    x = logits(3000, 40, BF, 16)
+    u, s = rng.uniform(size=40), settings(rng, 40)
+    ws = torch.zeros(sm.sample_workspace_bytes(40, 3000), dtype=torch.uint8, device=dev())
+    want = sample(x, u, *s, ws=ws)
+    bad = x.clone()
+    bad[::3, ::7] = float("nan")
+    bad[1::3] = -INF
+    for T in (s[0], np.full(40, -1.0)):
+        assert sample(bad, u, T, *s[1:], ws=ws)[2] == sm.ERR_EINVAL
+        got = sample(x, u, *s, ws=ws)
+        assert got[2] == 0 and np.array_equal(got[0], want[0]) and np.array_equal(got[1], want[1])
