@@ -1,6 +1,6 @@
 // Prefill attention over the paged cache (gfx950): the kernels and their host
 // side; the tiles they work by are in prefill_tiles.hpp.
-#include "prefill_tiles.hpp"
+#include "prefill_apart.hpp"
 
 namespace sm {
 
@@ -26,6 +26,12 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_few_bf16(PrefillArgs a)
   const PfBlock wg = pf_block(a);
   if (wg.L <= kPfFewKeys) prefill_body<DH, 1, EIGHT>(a, wg, lds);
   else prefill_body<DH, 4, EIGHT>(a, wg, lds);
+}
+
+template <int DH>
+__global__ __launch_bounds__(kPfThreads, 2) void prefill_apart_e4m3(PrefillArgs a) {
+  __shared__ __attribute__((aligned(16))) uint8_t lds[apart_lds_bytes<DH>()];
+  prefill_apart_body<DH>(a, pf_block(a), lds);
 }
 
 }  // namespace sm
@@ -58,7 +64,8 @@ SM_API sm_status sm_prefill_attention(const sm_paged_cache *c, const int32_t *se
   a.total_rows = total_rows;
   a.max_rows = max_rows;
   const PrefillPlan plan = plan_prefill(n, H, G, total_rows, max_rows, (int64_t)c->max_blocks_per_seq * bs);
-  const int ks = plan.splits;
+  const bool apart = eight && prefill_apart(n, H, G, total_rows, max_rows);
+  const int ks = apart ? 8 : plan.splits;
   a.BQ = kPfVec / ks / G;
   const int nqb = max_rows > 0 ? (max_rows + a.BQ - 1) / a.BQ : 1;  // block 0 reports bad requests
   if ((int64_t)nqb * n * H > 0x7fffffff) return SM_EINVAL;
@@ -67,6 +74,8 @@ SM_API sm_status sm_prefill_attention(const sm_paged_cache *c, const int32_t *se
   const auto kernel = [&](auto dh, auto e) {
     constexpr int DH = decltype(dh)::value;
     constexpr bool EIGHT = decltype(e)::value;
+    if constexpr (EIGHT)
+      if (apart) return prefill_apart_e4m3<DH>;
     return plan.few  ? prefill_few_bf16<DH, EIGHT>
            : ks == 4 ? prefill_bf16<DH, 4, EIGHT>
            : ks == 2 ? prefill_bf16<DH, 2, EIGHT>

@@ -49,4 +49,18 @@ inline PrefillPlan plan_prefill(int n, int H, int G, int total_rows, int max_row
   return PrefillPlan{1, false};
 }
 
+// Over e4m3 pages, whether the waves work apart (KS = 8, prefill_apart.hpp):
+// where that leaves a workgroup for each compute unit, or a request's rows are
+// one workgroup's either way.  Us apart and as above, 32/8 heads, D = 128: one
+// row 5.5, 6.1; after 8192 entries 46, 107; 250 rows (256 workgroups) 8.7, 10.8
+// and 54, 111; 64 requests of 2 rows after 1000 32, 77.  With more workgroups
+// it loses what it gains in a tile: 400 rows (400) 15.0, 15.3; after 300 19.1,
+// 17.1; 1024 (1024) 37, 26.  16/4 heads, D = 64: 250 rows after 4000 21, 42.
+inline bool prefill_apart(int n, int H, int G, int total_rows, int max_rows) {
+  const int bq = kPfVec / 8 / G;
+  const int64_t avg = ((int64_t)total_rows + n - 1) / n;
+  auto wgs = [&](int64_t rows) { return (rows + bq - 1) / bq * n * H; };
+  return max_rows <= bq || (wgs(avg) <= kPfCus && wgs(max_rows) <= 8 * kPfCus);
+}
+
 }  // namespace sm

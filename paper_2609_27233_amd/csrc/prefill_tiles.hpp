@@ -40,7 +40,7 @@
 // The prefix of a group of requests (SHARED) is attended to by the same
 // tiles: the vectors are the G query heads of every request of the group, all
 // of them see all of a chunk of the prefix, and what they make of it goes to
-// the workspace unnormalised, for the decode kernel to join.
+// the workspace unnormalised, for a second launch to join.
 #pragma once
 
 #include "common.hpp"
@@ -232,6 +232,68 @@ __device__ __forceinline__ float inverse_sum(float l) {
   else return l > 0.f ? 1.0f / l : 0.f;
 }
 
+// Rows [first, first + rows) of the request come out as zeros, this kv head's query heads.
+template <int DH, int THREADS>
+__device__ __forceinline__ void zero_rows(const PrefillArgs &a, const PfBlock &wg, int first, int rows) {
+  const int per_row = a.G * DH;
+  for (int64_t e = threadIdx.x; e < (int64_t)rows * per_row; e += THREADS) {
+    const int rr = (int)(e / per_row), k = (int)(e - (int64_t)rr * per_row);
+    a.out[((int64_t)(wg.r0 + first + rr) * a.Hq + wg.g * a.G) * DH + k] = 0;
+  }
+}
+
+// Softmax states of KS wave groups over the same vectors, merged through LDS
+// and stored; wave w holds vectors 32 (w % VG) .. + 31 and group w / VG's keys.
+// Every wave leaves its reference and sum and, scaled to the common reference,
+// its output columns (register 4 gg + e of block rb = dim 32 rb + 8 gg + 4 h2 +
+// e); then wave kg of a group's KS waves adds the KS partials of its DH / KS
+// dims.  live: groups that had a tile at all; row: this lane's vector's output.
+template <int DH, int KS, int W>
+constexpr int join_bytes() {
+  return KS > 1 ? (W * 32 * (DH + 4) + W * 64) * 4 : 0;
+}
+template <int DH, int KS, int W, bool EIGHT>
+__device__ __forceinline__ void join_groups(uint8_t *lds, const f32x16_t (&o)[DH / 32], float m_run, float l_tot, int live,
+                                            bool vok, uint16_t *row) {
+  constexpr int VG = W / KS, OPITCH = DH + 4;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, c32 = lane & 31, h2 = lane >> 5, vg = w % VG, kg = w / VG;
+  float *ml = (float *)lds, *po = ml + W * 64;  // [wave][32 m, 32 l], [wave][32][OPITCH]
+  if (h2 == 0) {
+    ml[w * 64 + c32] = m_run;
+    ml[w * 64 + 32 + c32] = l_tot;
+  }
+  __syncthreads();
+  float m_all = -INFINITY;
+  for (int k = 0; k < live; ++k) m_all = fmaxf(m_all, ml[(k * VG + vg) * 64 + c32]);
+  const float mb = m_all == -INFINITY ? 0.f : m_all;  // an idle column
+  l_tot = 0.f;
+  for (int k = 0; k < live; ++k)
+    l_tot += ml[(k * VG + vg) * 64 + 32 + c32] * __builtin_amdgcn_exp2f(ml[(k * VG + vg) * 64 + c32] - mb);
+  const float mine = __builtin_amdgcn_exp2f(m_run - mb);
+  if (kg < live)
+#pragma unroll
+    for (int rb = 0; rb < DH / 32; ++rb)
+#pragma unroll
+      for (int gg = 0; gg < 4; ++gg)
+        *(f32x4_t *)&po[(w * 32 + c32) * OPITCH + 32 * rb + 8 * gg + 4 * h2] =
+            f32x4_t{o[rb][4 * gg] * mine, o[rb][4 * gg + 1] * mine, o[rb][4 * gg + 2] * mine, o[rb][4 * gg + 3] * mine};
+  __syncthreads();
+  if (!vok) return;
+  // lane (c32, h2) takes dims d0 .. d0 + DH / KS / 2 - 1 of its column
+  constexpr int DW = DH / KS / 2;
+  const int d0 = kg * (DH / KS) + h2 * DW;
+  f32x4_t y[DW / 4];
+#pragma unroll
+  for (int c = 0; c < DW / 4; ++c) y[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  for (int k = 0; k < live; ++k)
+#pragma unroll
+    for (int c = 0; c < DW / 4; ++c) y[c] += *(const f32x4_t *)&po[((k * VG + vg) * 32 + c32) * OPITCH + d0 + 4 * c];
+  const float inv = inverse_sum<EIGHT>(l_tot);
+#pragma unroll
+  for (int c = 0; c < DW / 4; ++c)
+    *(uint2 *)(row + d0 + 4 * c) = make_uint2(cvt_bf16x2(y[c][0] * inv, y[c][1] * inv), cvt_bf16x2(y[c][2] * inv, y[c][3] * inv));
+}
+
 // LDS of a workgroup: the ring of K and V buffers, which the merge of the wave
 // groups uses again, then the page ids and a flag.
 template <int DH, int KS, bool EIGHT = false, bool SHARED = false>
@@ -239,7 +301,7 @@ constexpr int pf_lds_bytes() {
   const int W = SHARED ? kPrefixWaves : kPfWaves;
   const int keys = KS == 4 ? 32 : 64, vp = keys == 32 ? 32 : keys + 8;
   const int ring = 4 * (KS * keys * (DH + 8) + KS * DH * vp) + (EIGHT ? 8 * KS * keys : 0);
-  const int merge = KS > 1 ? (W * 32 * (DH + 4) + W * 64) * 4 : 0;
+  const int merge = join_bytes<DH, KS, W>();
   return (ring > merge ? ring : merge) + (SHARED ? kPrefixPages : kPfMaxPages) * 4 + 16;
 }
 
@@ -268,8 +330,7 @@ __device__ __forceinline__ void prefill_body(const PrefillArgs &a, const PfBlock
   constexpr int VU = (VTOT + THREADS - 1) / THREADS;  // V chunks per thread and tile
   constexpr int KBUF = SPAN * KP, VBUF = KS * DH * VP;  // elements of one buffer
   constexpr int RING = 2 * (KBUF + VBUF) * 2 + (EIGHT ? 2 * SPAN * 4 : 0);
-  constexpr int OPITCH = DH + 4;                        // floats of one vector's outputs in the merge of the groups
-  constexpr int MERGE = KS > 1 ? (W * 32 * OPITCH + W * 64) * 4 : 0;
+  constexpr int MERGE = join_bytes<DH, KS, W>();
   constexpr int MAXPAGES = SHARED ? kPrefixPages : kPfMaxPages;
   constexpr int PAGES = RING > MERGE ? RING : MERGE;
   static_assert(PAGES + MAXPAGES * 4 + 16 == pf_lds_bytes<DH, KS, EIGHT, SHARED>(), "LDS of the workgroup");
@@ -291,11 +352,7 @@ __device__ __forceinline__ void prefill_body(const PrefillArgs &a, const PfBlock
   } else if (!wg.ok) {  // block 0 reports the request and zeroes its rows
     if (qb != 0) return;
     if (tid == 0) set_err(a.err, SM_ERR_EINVAL);
-    const int per_row = a.G * DH;  // this kv head's query heads
-    for (int64_t e = tid; e < (int64_t)m * per_row; e += THREADS) {
-      const int rr = (int)(e / per_row), k = (int)(e - (int64_t)rr * per_row);
-      a.out[((int64_t)(r0 + rr) * a.Hq + g * a.G) * DH + k] = 0;
-    }
+    zero_rows<DH, THREADS>(a, wg, 0, m);
     return;
   }
   const int q_lo = SHARED ? 0 : qb * a.BQ;  // first row of this block within the request
@@ -325,11 +382,7 @@ __device__ __forceinline__ void prefill_body(const PrefillArgs &a, const PfBlock
       prefix_none(a, wg, -1.f);
       return;
     }
-    const int per_row = a.G * DH;
-    for (int e = tid; e < nq * per_row; e += THREADS) {
-      const int rr = e / per_row, k = e - rr * per_row;
-      a.out[((int64_t)(r0 + q_lo + rr) * a.Hq + g * a.G) * DH + k] = 0;
-    }
+    zero_rows<DH, THREADS>(a, wg, q_lo, nq);
     return;
   }
 
@@ -596,47 +649,9 @@ __device__ __forceinline__ void prefill_body(const PrefillArgs &a, const PfBlock
   swap32(l_run, a0, b0);
   float l_tot = a0 + b0;
   if constexpr (KS > 1) {
-    // The groups' softmax states, merged through LDS (the ring is free: the
-    // loop ends on a barrier).  Every wave leaves its reference and sum and,
-    // scaled to the common reference, its output columns; then wave kg of a
-    // group's KS waves adds the KS partials of its DH / KS dims.
-    float *ml = (float *)lds, *po = ml + W * 64;  // [wave][32 m, 32 l], [wave][32][OPITCH]
-    const int live = min(KS, (kend - k0 + KEYS - 1) / KEYS);   // groups that had a tile at all
-    if (h2 == 0) {
-      ml[w * 64 + c32] = m_run;
-      ml[w * 64 + 32 + c32] = l_tot;
-    }
-    __syncthreads();
-    float m_all = -INFINITY;
-    for (int k = 0; k < live; ++k) m_all = fmaxf(m_all, ml[(k * VG + vg) * 64 + c32]);
-    const float mb = m_all == -INFINITY ? 0.f : m_all;  // an idle column
-    l_tot = 0.f;
-    for (int k = 0; k < live; ++k)
-      l_tot += ml[(k * VG + vg) * 64 + 32 + c32] * __builtin_amdgcn_exp2f(ml[(k * VG + vg) * 64 + c32] - mb);
-    const float mine = __builtin_amdgcn_exp2f(m_run - mb);
-    if (kg < live)
-#pragma unroll
-      for (int rb = 0; rb < NRB; ++rb)
-#pragma unroll
-        for (int gg = 0; gg < 4; ++gg)
-          *(f32x4_t *)&po[(w * 32 + c32) * OPITCH + 32 * rb + 8 * gg + 4 * h2] =
-              f32x4_t{o[rb][4 * gg] * mine, o[rb][4 * gg + 1] * mine, o[rb][4 * gg + 2] * mine, o[rb][4 * gg + 3] * mine};
-    __syncthreads();
-    if (!vok) return;
-    // lane (c32, h2) takes dims d0 .. d0 + DH / KS / 2 - 1 of its column
-    constexpr int DW = DH / KS / 2;
-    const int d0 = kg * (DH / KS) + h2 * DW;
-    f32x4_t y[DW / 4];
-#pragma unroll
-    for (int c = 0; c < DW / 4; ++c) y[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < live; ++k)
-#pragma unroll
-      for (int c = 0; c < DW / 4; ++c) y[c] += *(const f32x4_t *)&po[((k * VG + vg) * 32 + c32) * OPITCH + d0 + 4 * c];
-    const float inv = inverse_sum<EIGHT>(l_tot);
-    uint16_t *op = a.out + ((int64_t)vrow * a.Hq + vhead) * DH + d0;
-#pragma unroll
-    for (int c = 0; c < DW / 4; ++c)
-      *(uint2 *)(op + 4 * c) = make_uint2(cvt_bf16x2(y[c][0] * inv, y[c][1] * inv), cvt_bf16x2(y[c][2] * inv, y[c][3] * inv));
+    // (the ring is free: the loop ends on a barrier)
+    join_groups<DH, KS, W, EIGHT>(lds, o, m_run, l_tot, min(KS, (kend - k0 + KEYS - 1) / KEYS), vok,
+                                  a.out + ((int64_t)vrow * a.Hq + vhead) * DH);
     return;
   }
   if (!vok) return;

@@ -154,9 +154,28 @@ PREFILLS = [
 ]
 
 
-@pytest.mark.parametrize("case", range(len(PREFILLS)))
+# The same with the form that the call takes: the waves apart, or the groups that they split a tile's keys into.
+FORMS = [
+    (32, 8, 128, 16, [(250, 700)], "apart"),
+    (28, 4, 128, 64, [(61, 0), (3, 900), (1, 0), (17, 100)], "apart"),     # 4 rows of 7 heads, 4 vectors idle
+    (16, 1, 64, 512, [(5, 1000), (0, 3), (2, 511)], "apart"),
+    (4, 4, 128, 16, [(33, 31), (32, 32), (31, 33), (1, 255), (1, 256), (1, 257)], "apart"),
+    (32, 8, 128, 32, [(8, 3 * i) for i in range(40)], "apart"),            # a request's rows are one workgroup's
+    (32, 8, 128, 16, [(20, 100)] * 12, "few"),
+    (32, 8, 128, 16, [(400, 50)], 4),
+    (32, 8, 128, 64, [(1024, 0)], 2),
+    (32, 8, 128, 16, [(700, 10)] * 3, 1),
+    (16, 4, 64, 16, [(250, 100)], "apart"),
+    (16, 4, 64, 16, [(20, 100)] * 23, "few"),
+    (16, 4, 64, 32, [(1000, 20)], 4),
+    (16, 4, 64, 16, [(2000, 0)], 2),
+    (16, 4, 64, 16, [(1300, 0)] * 4, 1),
+]
+
+
+@pytest.mark.parametrize("case", range(len(PREFILLS) + len(FORMS)))
 def test_prefill_matches_formula(case):
-    Hq, Hkv, D, bs, reqs, scale = PREFILLS[case]
+    Hq, Hkv, D, bs, reqs, scale = (PREFILLS + [(*f[:5], None) for f in FORMS])[case]
     lens = [m + past for m, past in reqs]
     c = filled(E4, Hkv, D, bs, sum(-(-x // bs) for x in lens) + 1, max_seqs=len(lens),
                max_blocks_per_seq=-(-max(lens) // bs))
