@@ -7,11 +7,29 @@
 
 namespace sm {
 
-constexpr int kSharedVec = 128;        // query vectors of a workgroup
+// Query vectors of a workgroup: 32 for each of its four waves, which share the
+// tiles of its keys.  (Waves over different keys, merged through LDS, and e4m3
+// fragments straight from the pages, as for few prefill rows, measured slower:
+// 128 requests behind 16,000 e4m3 entries 99 us for 87.)
+constexpr int kSharedVec = 128;
 constexpr int kSharedStep = 128;       // entries that a chunk is a multiple of
 constexpr int kSharedMostChunk = 8192;
-constexpr int kSharedWgs = 256;        // workgroups that the cut aims at: one for each compute unit
-constexpr int64_t kSharedVectors = (int64_t)kSharedWgs * kSharedVec;  // vectors x chunks, at most
+// Workgroups that the cut aims at: one for each compute unit, or two where that
+// leaves their chunks long.  A second one hides the first's waits and its
+// softmax; a chunk more costs the join a read of every row.  Us at 128, 256 and
+// 512, 32/8 heads, D = 128, bf16 and e4m3 pages (chunk in entries at 256):
+//   128 requests behind 4096 (512)    -, 47, 57 and -, 42, 49
+//   behind 8192 (1024)                -, 57, 66 and -, 56, 59
+//   behind 12,000 (1536)              -, 69, 73 and -, 72, 65
+//   behind 16,000 (2048)              105, 82, 81 and 118, 86, 73
+//   behind 32,000 (4096)              -, 143, 115 and -, 153, 108
+//   64 behind 32,000 (2048)           -, 81, 73 and -, 87, 69
+//   128 behind four of 6000 to 8192, 28/4 heads (1024)  74, 66, 78 and 74, 56, 63
+//   8 behind each of 16 of 2000, 16/4 heads, D = 64 (512)  29, 22, 23 and 29, 21, 19
+// Many requests' own chunks are the second workgroup anyway: 500 behind 4096
+// (2048) -, 124, 140 and -, 103, 111.
+constexpr int kSharedWgs = 256, kSharedLongChunk = 896, kSharedFewPairs = 2048;
+constexpr int64_t kSharedVectors = 2 * (int64_t)kSharedWgs * kSharedVec;  // vectors x chunks, at most
 
 struct SharedPlan {
   int chunk;   // entries of a chunk, a multiple of kSharedStep
@@ -33,7 +51,8 @@ inline SharedPlan plan_shared(int n, int H, int G, int groups, int max_prefix) {
   const int64_t per = ((int64_t)n + groups - 1) / groups * G;  // vectors of a group and kv head
   const int64_t most = shared_most_chunks((int64_t)n * G * H, max_prefix);
   const int64_t blocks = (per + kSharedVec - 1) / kSharedVec * groups * H;
-  int64_t chunks = kSharedWgs / blocks;
+  int64_t chunks = 2 * kSharedWgs / blocks;
+  if (chunks * kSharedLongChunk > max_prefix || (int64_t)n * H > kSharedFewPairs) chunks = kSharedWgs / blocks;
   if (chunks > most) chunks = most;
   if (chunks < 1) chunks = 1;
   int64_t chunk = ((int64_t)max_prefix + chunks - 1) / chunks;

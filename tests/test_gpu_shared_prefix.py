@@ -49,6 +49,7 @@ CASES = [
     (32, 8, 128, 16, [300], [3], [5000, 1, 2600], 0.0),          # own entries in several chunks; scale 0
     (8, 8, 64, 16, [20, 50], [300, 260], (1, 3), None),
     (4, 2, 128, 16, [70] * 600, [0, 1, 0] * 200, (1, 20), None),  # more groups than threads of a workgroup
+    (16, 1, 64, 16, [3700], [1000], (0, 2), None),               # chunks long enough for two workgroups a compute unit
 ]
 
 

@@ -48,3 +48,11 @@ def test_the_chunks_cover_any_prefix_and_fit_the_workspace(plan, H, G):
                 assert chunk % 128 == 0 and 128 <= chunk <= 8192
                 assert chunks * chunk >= longest and (chunks - 1) * chunk < max(1, longest)
                 assert max(1, chunks) <= most, (n, groups, longest)
+
+
+def test_the_forms_of_the_gpu_tests(plan):
+    """Two workgroups a compute unit where their chunks stay long, one otherwise."""
+    assert plan(1000, 1, 16, 1, 3700)[:2] == (1024, 4)           # 125 blocks of vectors
+    assert plan(1000, 1, 16, 1, 3500)[:2] == (1792, 2)
+    assert plan(16, 8, 4, 1, 2048)[:2] == (128, 16)
+    assert plan(500, 8, 4, 1, 4096)[:2] == (2048, 2)             # many requests' own entries beside them
