@@ -9,6 +9,11 @@
 // pages are dim-major, and a thread takes one 16-byte piece of 8 (fp32: 4)
 // features' slots, turns them round in registers and stores whole 16-byte
 // pieces of rows.
+//
+// HBM bounds it: 39,328 entries of 8 heads x 128 out of e4m3 pages 57 us over
+// several caches in turn (4.3 TB/s of values, exponents and rows), 41 over one
+// whose pages stay in the last-level cache; out of bf16 pages 67.  A step's few
+// rows take a launch, 5 us.
 #include <algorithm>
 
 #include "cache_meta.hpp"

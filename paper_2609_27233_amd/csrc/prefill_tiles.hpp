@@ -41,6 +41,12 @@
 // tiles: the vectors are the G query heads of every request of the group, all
 // of them see all of a chunk of the prefix, and what they make of it goes to
 // the workspace unnormalised, for a second launch to join.
+//
+// e4m3 pages become bf16 on the way into LDS, K with its exponents; V's
+// exponents go into the probabilities.  16 x 2458 rows of 32/8 heads, D = 128:
+// 1010 us (0.78 PFLOP/s) where bf16 pages take 920 to 945: 64 conversions and
+// as many products with exponents for each 64 keys and wave are added to a loop
+// whose vector ALU bounds it.
 #pragma once
 
 #include "common.hpp"
