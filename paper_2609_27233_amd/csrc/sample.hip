@@ -305,15 +305,18 @@ struct Row {
   // g(eight logits, piece) of this wave's pieces among [p0, p1).
   template <class G>
   __device__ __forceinline__ void each_piece(int p0, int p1, G g) const {
-    for (int p = p0 + (threadIdx.x >> 6); p < p1; p += kInFlight * kSampWaves) {
-      Eight f[kInFlight];
+    int p = p0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (p >= p1) return;
+    Eight f[kInFlight];
 #pragma unroll
-      for (int i = 0; i < kInFlight; ++i) f[i] = raw(min(p + i * kSampWaves, p1 - 1));
-#pragma unroll 1
+    for (int i = 0; i < kInFlight; ++i) f[i] = raw(min(p + i * kSampWaves, p1 - 1));
+    while (true) {
+#pragma unroll
       for (int i = 0; i < kInFlight; ++i) {
-        if (p + i * kSampWaves < p1) g(f[0], p + i * kSampWaves);
-#pragma unroll
-        for (int j = 1; j < kInFlight; ++j) f[j - 1] = f[j];
+        g(f[i], p);
+        if (p + kInFlight * kSampWaves < p1) f[i] = raw(p + kInFlight * kSampWaves);
+        p += kSampWaves;
+        if (p >= p1) return;
       }
     }
   }
