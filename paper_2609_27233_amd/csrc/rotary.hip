@@ -269,19 +269,26 @@ __device__ __forceinline__ T *page_of(T *pool, int s, const WriteArgs &w, int *i
 // Chunk c of a row: its features and, in the half layout, the other halves of
 // their pairs, with the sign to be added to them: (a, b) -> a cos - b sin
 // where a lies, b cos + a sin where b does.
-template <bool HALF>
+// LANES: of 128 features, all turned, the other half lies eight lanes on.
+// (39,328 rows of 8 heads, keys and values: 62 us, loading it 80; bf16 pages 63.)
+template <bool HALF, bool LANES = false>
 struct Chunk {
   u32x4_t own, other;
   template <bool STREAM>
   __device__ __forceinline__ void load(const uint16_t *x, int c, int R) {
     const int at = 8 * c;
     own = load_as<STREAM, u32x4_t>(x + at);
+    if constexpr (LANES) return;
     if (HALF && at < R)
       other = load_as<STREAM, u32x4_t>(x + (at < R / 2 ? at + R / 2 : at - R / 2)) ^ (at < R / 2 ? 0x80008000u : 0u);
   }
-  __device__ __forceinline__ float turn(int c, int R, const float2 *cs, float (&y)[8]) const {
+  __device__ __forceinline__ float turn(int c, int R, const float2 *cs, float (&y)[8]) {
     const int at = 8 * c;
     Vec16<uint16_t>::open(own, y);
+    if constexpr (LANES) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) other[i] = dpp_bits<0x128>(own[i]) ^ (c < 8 ? 0x80008000u : 0u);  // row_ror:8
+    }
     if (at < R) {
       if constexpr (HALF) {
         float z[8];
@@ -406,9 +413,8 @@ __device__ __forceinline__ void store_v_e4m3(const WriteArgs &w, int sl, int h, 
 // rows that fill consecutive slots of 8 aligned ones; a whole group leaves as
 // 8 bytes a feature.  (Groups of 16 rows, 16 bytes a feature, held 154
 // registers, three waves to a SIMD: 39,328 rows of 8 heads x 128 took 96 us
-// for keys and values where groups of 8 take 80, and bf16 pages 63.  The
-// largest features go as integers and the rare rows apart: with a branch for
-// each row the same took 115.)
+// for keys and values where groups of 8 took 80.  The largest features go as
+// integers and the rare rows apart: with a branch for each row it took 115.)
 template <bool STREAM>
 __device__ __forceinline__ void write_v_e4m3(const WriteArgs &w, int64_t r0, int g0, int g1, int groups, const int *group,
                                              const int *slot) {
@@ -551,7 +557,10 @@ __global__ __launch_bounds__(kRotThreads) void kv_write_kernel(RopeArgs a, Write
       unit.template run<STREAM>(h0 + part, hq1, share, [&](int h) { return q + h * D; }, [&](int h) { return out + h * D; });
     });
   if constexpr (EIGHT) {
-    if (k1 > k0) write_k_e4m3<Chunk<HALF>, 4, STREAM>(a, w, r0, nr, k0, k1, slot, cs);
+    if (k1 > k0) {
+      if (HALF && w.dh_log2 == 7 && a.R == 128) write_k_e4m3<Chunk<HALF, HALF>, 4, STREAM>(a, w, r0, nr, k0, k1, slot, cs);
+      else write_k_e4m3<Chunk<HALF>, 4, STREAM>(a, w, r0, nr, k0, k1, slot, cs);
+    }
   } else if (k1 > k0)
     each_unit<false>(nr, a.per_head, k1 - k0, [&](int r, int j, int part, int share) {
       const int sl = slot[r];
