@@ -355,7 +355,8 @@ size_t sm_decode_workspace_bytes(int n, int num_q_heads, int head_dim,
  * of each (sequence, kv head) to finish.
  *
  *  c            (host) any page type; SM_E4M3 pages stand for the features
- *               above, to all of their bits, and q and out are bf16
+ *               above, to all of their bits, and q and out are bf16; a NaN
+ *               that a row attends to is then its result
  *  seq_ids      [n] ids in [0, max_seqs) (repeats allowed)
  *  q            [n][num_q_heads][head_dim] (cache dtype)
  *  num_q_heads  (host) multiple of num_kv_heads, group size <= 16
@@ -391,7 +392,8 @@ size_t sm_decode_shared_workspace_bytes(int n, int num_q_heads, int head_dim,
  *
  * (K is cached turned, so a sequence's own positions start past its prefix:
  * add the prefix's length to the positions that sm_kv_reserve gives, before
- * sm_kv_write_rotary.)  Nothing at all to attend to gives zeros.  Two
+ * sm_kv_write_rotary.)  Nothing at all to attend to gives zeros, a NaN that a
+ * row attends to is its result (over pages of either type).  Two
  * launches; the result does not depend on the order in which work is done.
  *
  *  c              (host) bf16 or SM_E4M3 pages, as sm_prefill_attention
@@ -404,7 +406,9 @@ size_t sm_decode_shared_workspace_bytes(int n, int num_q_heads, int head_dim,
  *                 group_offsets[0] = 0, group_offsets[num_groups] = n
  *  num_groups     (host) 1 to 65535
  *  scale          (host) finite
- *  max_prefix     (host) upper bound on the prefixes' lengths; sizes the grid
+ *  max_prefix     (host) upper bound on the prefixes' lengths; sizes the grid,
+ *                 which is refused past 2^24 workgroups (tens of thousands of
+ *                 groups or requests with bounds of hundreds of thousands)
  *  ws, ws_bytes   at least sm_decode_shared_workspace_bytes(...); its first
  *                 256 KiB as sm_decode_attention's, which it can serve too
  * Device errors (into c->err; the affected requests' rows are zero): EINVAL
