@@ -30,8 +30,9 @@
 // where the filter ends, a k of thousands, logits hundreds apart) is cut by
 // passes over the whole row, in `choose`, to the same result.
 //
-// 1024 rows of 128,256 bf16 logits, mixed filters: scan 71 us, weigh 118,
-// choose 24.  The vector ALU bounds the first two (22 and 37 instructions a
+// 1024 rows of 128,256 bf16 logits, mixed filters: scan 71 us, weigh 112,
+// choose 24; all greedy, which are read once, 70 in all (123 with their ties
+// counted by weigh).  The vector ALU bounds the first two (22 and 37 instructions a
 // logit; a read alone would take 39): LDS atomics and an exponential, and the
 // nine products in double precision of a weight.  (Weights from a table of the
 // bf16 values in LDS: 222 for 207 in all, for the waves that its 32 KB displace.)  16 rows: 7, 11 and 14 us, a
@@ -68,7 +69,7 @@ struct RowState {
   uint32_t bad;       // a NaN
   uint32_t listed;    // tokens listed; more than kList: not all of them
   uint32_t unused;
-  uint64_t mass;      // of all tokens (MASS)
+  uint64_t mass;      // of all tokens (kMass); greedy: key of M << 32 | ~its first token
   uint32_t bins[kBins];
   // not cleared
   uint64_t pieces[kMostPieces];  // ties << 54 | mass
@@ -190,6 +191,15 @@ __device__ __forceinline__ uint64_t last_lane(uint64_t v) {
 __device__ __forceinline__ float last_lane(float v) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+  v = max(v, lane_moved<0x111, 0xf>(v));
+  v = max(v, lane_moved<0x112, 0xf>(v));
+  v = max(v, lane_moved<0x114, 0xf>(v));
+  v = max(v, lane_moved<0x118, 0xf>(v));
+  v = max(v, lane_moved<0x142, 0xa>(v));
+  v = max(v, lane_moved<0x143, 0xc>(v));
+  return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
 __device__ __forceinline__ uint64_t wave_sum64(uint64_t v) { return last_lane(wave_scan(v)); }
 // Inclusive over the workgroup.  red: one value a wave, in turn two places, so
 // that one barrier a scan does.
@@ -239,7 +249,7 @@ struct Kept {
 };
 
 enum Mode {
-  kPlain,  // the pieces' masses, of the tokens that min_p keeps (greedy: of the largest alone)
+  kPlain,  // the pieces' masses, of the tokens that min_p keeps (greedy: `scan` has found the token)
   kListK,  // list the bins that hold the first k
   kListM,  // list the tokens that min_p keeps, or that weigh anything
   kMass,   // top-p over everything: list the bins in which it ends, weigh what is above
@@ -378,6 +388,20 @@ __global__ __launch_bounds__(kSampThreads) void sample_scan_kernel(SampleArgs a)
     __syncthreads();
     for (int i = t; i < kBins; i += kSampThreads)
       if (bins[i]) atomicAdd(&st.bins[i], bins[i]);
+  } else if (s.greedy) {
+    int at = 0;  // the first token of M: a lane's ascend
+    row.each_piece(p0, p1, [&](const typename Row<T>::Eight &f, int p) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float v = f[e];
+        nan |= v != v;
+        at = v > M ? p * kPiece + 8 * lane + e : at;
+        M = v > M ? v : M;
+      }
+    });
+    const float most = wave_max(M);
+    const uint32_t first = wave_max_u32(M == most ? ~(uint32_t)at : 0u);
+    if (lane == 0 && most > -INFINITY) atomicMax((unsigned long long *)&st.mass, (uint64_t)order_key(most) << 32 | first);
   } else {
     row.each_piece(p0, p1, [&](const typename Row<T>::Eight &f, int) {
 #pragma unroll
@@ -469,7 +493,7 @@ __global__ __launch_bounds__(kSampThreads) void sample_weigh_kernel(SampleArgs a
   const Settings s = settings_of(a, r);
   const uint32_t top = st.top;
   row.M = value_of_key(top);
-  if (!s.fine || st.bad || top == 0 || !(row.M < INFINITY)) return;
+  if (!s.fine || s.greedy || st.bad || top == 0 || !(row.M < INFINITY)) return;
   row.c = s.c;
   fill_table(table);
   if (t == 0) listed = 0;
@@ -541,13 +565,6 @@ __global__ __launch_bounds__(kSampThreads) void sample_weigh_kernel(SampleArgs a
     });
     S = wave_sum64(S);
     if (lane == 0) atomicAdd((unsigned long long *)&st.mass, S);
-  } else if (s.greedy) {
-    row.each_piece(p0, p1, [&](const typename Row<T>::Eight &f, int p) {
-      int n = 0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) n += __popcll(__ballot(order_key(f[e]) == top));
-      if (lane == 0) st.pieces[p] = (uint64_t)n << 54;
-    });
   } else if (lm > -INFINITY) {
     row.each_piece(p0, p1, [&](const typename Row<T>::Eight &f, int p) {
       uint64_t sum = 0;
@@ -619,16 +636,6 @@ struct Tokens {
     }
   }
 };
-
-__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
-  v = max(v, lane_moved<0x111, 0xf>(v));
-  v = max(v, lane_moved<0x112, 0xf>(v));
-  v = max(v, lane_moved<0x114, 0xf>(v));
-  v = max(v, lane_moved<0x118, 0xf>(v));
-  v = max(v, lane_moved<0x142, 0xa>(v));
-  v = max(v, lane_moved<0x143, 0xc>(v));
-  return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
-}
 
 // The smallest start of the kept ones of these tokens, in descending order, at
 // which `before` plus their amount (MASS: of their masses; else their number)
@@ -784,11 +791,16 @@ __global__ __launch_bounds__(kSampThreads) void sample_choose_kernel(SampleArgs 
     }
     return;
   }
+  if (s.greedy) {
+    if (t == 0) {
+      a.tokens[r] = (int)~(uint32_t)mass;
+      if (a.logprob) a.logprob[r] = 0.f;
+    }
+    return;
+  }
   // ---- the filters ----
   Kept kept{0, 0};  // (no finite logit has key 0)
-  if (s.greedy) {
-    kept = Kept{top, 1};
-  } else if (s.mode != kPlain) {
+  if (s.mode != kPlain) {
     Tokens<T> tokens{row, sh, listed <= kList ? listed : -1};
     if (s.k > 0) cut<false>(row, tokens, kept, -INFINITY, 0, (uint64_t)s.k, sh, turn);
     if (kept.ties > 0 && row.exponent(value_of_key(kept.tie)) < s.lm) kept.ties = 0;
@@ -883,7 +895,7 @@ __global__ __launch_bounds__(kSampThreads) void sample_choose_kernel(SampleArgs 
     const float v = first + e < row.vocab ? Elem<T>::load(row.x + first + e) : -INFINITY;
     const uint32_t key = order_key(v);
     const double ex = row.exponent(v);
-    m[e] = v > -INFINITY && key > kept.tie && ex >= s.lm && !s.greedy ? unit_weight(ex, sh.table) : 0;
+    m[e] = v > -INFINITY && key > kept.tie && ex >= s.lm ? unit_weight(ex, sh.table) : 0;
     tied[e] = kept.ties > 0 && key == kept.tie;
   }
   const int rank = seen + (int)block_scan((uint64_t)(tied[0] + tied[1]), sh.red, turn, &unused) - tied[0] - tied[1];
