@@ -266,6 +266,13 @@ __device__ __forceinline__ T *page_of(T *pool, int s, const WriteArgs &w, int *i
 // e4m3 pages (rows of bf16).  A head's row is held by the D / 8 neighbouring
 // lanes of its 16-byte chunks, which share its largest input feature.
 
+// A feature turned with the other of its pair (the sign its sine has to it in
+// other), rounded twice in whatever form a row comes, so that its bits in a
+// page do not go by addresses or sizes.  (The larger product of the slow pairs
+// is rounded by itself, as where nothing is fused: one that comes to lie on a
+// tie between two e4m3 values goes the same way.)
+__device__ __forceinline__ float turned_one(float own, float other, float2 cs) { return fmaf(other, cs.y, own * cs.x); }
+
 // Chunk c of a row: its features and, in the half layout, the other halves of
 // their pairs, with the sign to be added to them: (a, b) -> a cos - b sin
 // where a lies, b cos + a sin where b does.
@@ -295,13 +302,13 @@ struct Chunk {
         Vec16<uint16_t>::open(other, z);
         cs += at < R / 2 ? at : at - R / 2;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = y[e] * cs[e].x + z[e] * cs[e].y;
+        for (int e = 0; e < 8; ++e) y[e] = turned_one(y[e], z[e], cs[e]);
       } else {
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
-          const float2 t = turned(y[e], y[e + 1], cs[at / 2 + e / 2]);
-          y[e] = t.x;
-          y[e + 1] = t.y;
+          const float a = y[e], b = y[e + 1];
+          y[e] = turned_one(a, -b, cs[at / 2 + e / 2]);
+          y[e + 1] = turned_one(b, a, cs[at / 2 + e / 2]);
         }
       }
     }
@@ -332,8 +339,7 @@ struct Features {
       if (i >= R) continue;
       const bool first = HALF ? i < R / 2 : i % 2 == 0;
       const float pair = bf16_to_f32(x[HALF ? (first ? i + R / 2 : j) : i ^ 1]);
-      const float2 t = first ? turned(y[e], pair, cs[j]) : turned(pair, y[e], cs[j]);
-      y[e] = first ? t.x : t.y;
+      y[e] = turned_one(y[e], first ? -pair : pair, cs[j]);
     }
     return largest(own);
   }

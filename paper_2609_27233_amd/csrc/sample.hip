@@ -30,15 +30,15 @@
 // where the filter ends, a k of thousands, logits hundreds apart) is cut by
 // passes over the whole row, in `choose`, to the same result.
 //
-// 1024 rows of 128,256 bf16 logits, mixed filters: scan 71 us, weigh 112,
-// choose 24; all greedy, which are read once, 70 in all (123 with their ties
-// counted by weigh).  The vector ALU bounds the first two (22 and 37 instructions a
-// logit; a read alone would take 39): LDS atomics and an exponential, and the
-// nine products in double precision of a weight.  (Weights from a table of the
-// bf16 values in LDS: 222 for 207 in all, for the waves that its 32 KB displace.)  16 rows: 7, 11 and 14 us, a
-// chain of dependent reads and barriers.  Rows a thousand at a time are still
-// in the last-level cache when weigh reads them; fewer at a time, or a slice's
-// loads before the bins are known, took longer.
+// 1024 rows of 128,256 bf16 logits, mixed filters: scan 72 us, weigh 109,
+// choose 23; all greedy, which are read once, 70 in all (123 with their ties
+// counted by weigh).  The vector ALU and the two reads bound it (22 and 37
+// instructions a logit; a read alone would take 39 us): LDS atomics and an
+// exponential, and the nine products in double precision of a weight.  (Weights
+// from a table of the bf16 values in LDS: 222 for 207 in all, for the waves that
+// its 32 KB displace.)  16 rows: 7, 11 and 14 us, a chain of dependent reads and
+// barriers.  Rows fewer at a time, or a slice's loads before the bins are known,
+// took longer.
 #include <algorithm>
 #include <cmath>
 

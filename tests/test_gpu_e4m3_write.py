@@ -179,6 +179,30 @@ def test_slots_out_of_range_are_refused_alone():
     check_write(c, before, slots, pos, k, v, dict(rot_dim=64))
 
 
+@pytest.mark.parametrize("D,R,layout", [(128, 128, "half"), (64, 64, "half"), (128, 64, "half"), (128, 128, "interleaved")])
+def test_a_row_has_the_same_bits_however_it_comes(D, R, layout):
+    """Rows one element off a 16-byte address, alone and in full tiles, with and without neighbours."""
+    rows, H = 70, 5
+    k, v = (_rand((rows, H, D), BF, s).to(dev()) for s in (5, 6))
+    pos, slots = i32(np.arange(rows) * 37 + 1000), i32(np.random.RandomState(2).permutation(96)[:rows])
+    rope = sm.rope_params(R, layout=layout)
+    caches = [filled(E4, H, D, 16, 6) for _ in range(4)]
+    odd = [torch.empty((rows, H * D + 8), dtype=BF, device=dev())[:, 1:1 + H * D].unflatten(1, (H, D)) for _ in range(2)]
+    for o, x in zip(odd, (k, v)):
+        o.copy_(x)
+    say("same bits", D, R, layout)
+    sm.kv_write_rotary(caches[0], pos, slots, None, k, v, rope, None)
+    sm.kv_write_rotary(caches[1], pos, slots, None, *odd, rope, None)
+    order = slots.argsort()
+    sm.kv_write_rotary(caches[2], pos[order], slots[order], None, k[order], v[order], rope, None)
+    for r in range(rows):
+        sm.kv_write_rotary(caches[3], pos[r:r + 1], slots[r:r + 1], None, k[r:r + 1], v[r:r + 1], rope, None)
+    torch.cuda.synchronize()
+    for c in caches[1:]:
+        for name in ("k_pool", "v_pool", "k_exp", "v_exp"):
+            assert torch.equal(getattr(c, name).view(torch.uint8), getattr(caches[0], name).view(torch.uint8)), name
+
+
 # --------------------------------------------------------------------------
 # entries read back
 
