@@ -129,3 +129,20 @@ def test_sizes_that_no_int_holds_are_refused(L):
         bad[at] += many
         with pytest.raises(sm.SpanMergeError, match="argument"):
             b.sm_sample_tokens(*bad)
+
+
+def test_shared_wrapper_refuses_what_does_not_lie_in_one_piece(monkeypatch, L):
+    monkeypatch.setattr(sm, "_here", lambda stream: (0, -1))
+    monkeypatch.setattr(sm, "_ptr", lambda t: t.data_ptr())
+    c = sm.PagedCache(dtype=torch.float8_e4m3fn, num_kv_heads=2, head_dim=64, block_size=16, num_blocks=8, max_seqs=2,
+                      max_blocks_per_seq=4, device="cpu")
+    i32, wide = torch.int32, torch.zeros((3, 4, 128), dtype=torch.bfloat16)
+    q, two = torch.zeros((3, 4, 64), dtype=torch.bfloat16), torch.zeros(4, dtype=i32)
+    ws = torch.zeros(sm.decode_shared_workspace_bytes(3, 4, 64, 64, 64), dtype=torch.uint8)
+    good = dict(ids=two[:3], prefixes=two[:1], offs=two[:2], q=q, out=q, ws=ws)
+    for kw in (dict(q=wide[..., :64]), dict(out=wide[..., 64:]), dict(q=torch.zeros((3, 8, 64), dtype=q.dtype)[:, :4]),
+               dict(q=q.expand(3, 4, 64)[:1].expand(3, 4, 64)), dict(q=q.float()), dict(out=q[:2]), dict(ids=two[::2]),
+               dict(offs=torch.zeros(4, dtype=i32)[::2]), dict(prefixes=two[:2]), dict(ws=ws[::2]), dict(ws=ws[:100])):
+        a = {**good, **kw}
+        with pytest.raises(sm.SpanMergeError):
+            sm.decode_attention_shared(c, a["ids"], a["prefixes"], a["offs"], a["q"], a["out"], a["ws"], 64, 64)

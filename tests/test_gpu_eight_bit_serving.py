@@ -302,3 +302,36 @@ def test_the_same_sequence_more_than_once():
     at = slots_of(s.c.block_table.cpu().numpy(), BS, 2, np.arange(int(s.c.lengths[2])))
     at = np.concatenate([at, at])
     assert_within(sh[:1], *attended(q[:1].double().cpu(), Kf[at], Vf[at], D ** -0.5))
+
+
+def test_layers_of_both_page_types_share_their_tables():
+    """One reservation a step for a bf16 layer and an 8-bit one of other head counts; a span's crop moves both."""
+    kw = dict(head_dim=D, block_size=BS, num_blocks=20, max_seqs=3, max_blocks_per_seq=8)
+    a = sm.PagedCache(dtype=BF, num_kv_heads=2, **kw)
+    b = sm.PagedCache(dtype=E4, num_kv_heads=1, tables=a, **kw)
+    rng, ids, rope = np.random.RandomState(6), i32([2, 0]), sm.rope_params(D, **ROPE)
+    ws = torch.zeros(sm.decode_workspace_bytes(2, 4, D, 128), dtype=torch.uint8, device=dev())
+    say("both page types")
+    for counts, crop in (([30, 17], [0, 0]), ([1, 1], [0, 0]), ([1, 2], [3, 0]), ([1, 0], [2, 17])):
+        total = sum(counts)
+        offs, pos, slots = to_ints(3), to_ints(total), to_ints(total)
+        sm.kv_reserve(a, ids, i32(counts), offs, pos, slots, crop=i32(crop))
+        for c in (a, b):
+            k, v = (_rand((total, c.H, D), BF, int(rng.randint(1000))).to(dev()) for _ in "kv")
+            sm.kv_write_rotary(c, pos, slots, None, k, v, rope, None)
+    sm.kv_rollback(a, i32([0]), i32([1]))
+    torch.cuda.synchronize()
+    lens = a.lengths.cpu().numpy()
+    assert lens.tolist() == [17 + 1 + 2 - 17 - 1, 0, 30 + 1 - 3 + 1 - 2 + 1]
+    table = a.block_table.cpu().numpy()
+    assert a.error_bits() == 0 and torch.equal(a.lengths, b.lengths)
+    q = _rand((2, 4, D), BF, 9).to(dev())
+    for c in (a, b):
+        out = torch.empty_like(q)
+        sm.decode_attention(c, ids, q, out, ws, 128)
+        torch.cuda.synchronize()
+        K, V = features(c)
+        for i, s in enumerate((2, 0)):
+            at = slots_of(table, BS, s, np.arange(lens[s]))
+            assert_within(out[i:i + 1], *attended(q[i:i + 1].double().cpu(), K[at], V[at], D ** -0.5))
+    assert a.error_bits() == 0
