@@ -30,17 +30,18 @@
 // where the filter ends, a k of thousands, logits hundreds apart) is cut by
 // passes over the whole row, in `choose`, to the same result.
 //
-// 1024 rows of 128,256 bf16 logits, mixed filters: scan 72 us, weigh 109,
+// 1024 rows of 128,256 bf16 logits, mixed filters: scan 69 us, weigh 108,
 // choose 23; all greedy, which are read once, 70 in all (123 with their ties
-// counted by weigh).  The vector ALU and the two reads bound it (22 and 37
+// counted by weigh).  The vector ALU and the two reads bound it (20 and 37
 // instructions a logit; a read alone would take 39 us): LDS atomics and an
 // exponential, and the nine products in double precision of a weight.  (Weights
 // from a table of the bf16 values in LDS: 222 for 207 in all, for the waves that
-// its 32 KB displace.)  16 rows: 7, 11 and 14 us, a chain of dependent reads and
+// its 32 KB displace.)  16 rows: 6, 11 and 14 us, a chain of dependent reads and
 // barriers.  Rows fewer at a time, or a slice's loads before the bins are known,
 // took longer.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "common.hpp"
 
@@ -357,7 +358,7 @@ __device__ __forceinline__ float log2_per_bin(const Settings &s) { return (float
 
 template <typename T>
 __global__ __launch_bounds__(kSampThreads) void sample_scan_kernel(SampleArgs a) {
-  __shared__ uint32_t bins[kBins];
+  __shared__ uint32_t bins[kBins + 64];  // and a place a lane for what is masked, so that no lane has to leave
   const int t = threadIdx.x, lane = t & 63;
   const int64_t r = blockIdx.x / a.slices;
   const int p0 = (int)(blockIdx.x % a.slices) * a.per_slice;
@@ -374,17 +375,22 @@ __global__ __launch_bounds__(kSampThreads) void sample_scan_kernel(SampleArgs a)
     row.set_origin();
     const float one = mass_one(a.vocab), slope = log2_per_bin(s);
     __syncthreads();
-    row.each_piece(p0, p1, [&](const typename Row<T>::Eight &f, int) {
+    const auto fill = [&](auto of_masses) {
+      row.each_piece(p0, p1, [&](const typename Row<T>::Eight &f, int) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float v = f[e];
-        nan |= v != v;
-        M = fmaxf(M, v);
-        const float d = row.depth(v), b = floorf(fminf(d, (float)(kBins - 1)));
-        const uint32_t part = masses ? (uint32_t)fmaf(__builtin_amdgcn_exp2f((b - d) * slope), one, 0.5f) : 1u;
-        if (v > -INFINITY) atomicAdd(&bins[(int)b], part);
-      }
-    });
+        for (int e = 0; e < 8; ++e) {
+          const float v = f[e];
+          nan |= v != v;
+          M = fmaxf(M, v);
+          const float d = row.depth(v), b = floorf(fminf(d, (float)(kBins - 1)));
+          uint32_t part = 1;
+          if constexpr (of_masses) part = (uint32_t)fmaf(__builtin_amdgcn_exp2f((b - d) * slope), one, 0.5f);
+          atomicAdd(&bins[v > -INFINITY ? (int)b : kBins + lane], part);
+        }
+      });
+    };
+    if (masses) fill(std::true_type());
+    else fill(std::false_type());
     __syncthreads();
     for (int i = t; i < kBins; i += kSampThreads)
       if (bins[i]) atomicAdd(&st.bins[i], bins[i]);
