@@ -27,7 +27,8 @@
 //           number falls into is looked at token by token
 // A row is read twice, in slices dealt over the device, four 16-byte loads a
 // lane in flight.  A row whose list does not suffice (thousands of equal logits
-// where the filter ends, a k of thousands, logits hundreds apart) is cut by
+// where the filter ends, a k of thousands, logits hundreds apart, or all of them
+// so far below the bins' origin that the histogram holds no mass) is cut by
 // passes over the whole row, in `choose`, to the same result.
 //
 // 1024 rows of 128,256 bf16 logits, mixed filters: scan 69 us, weigh 108,
@@ -467,6 +468,7 @@ __device__ __forceinline__ Range end_bins(const RowState &st, const Settings &s,
     sum += m[i];
   }
   float at = block_scan(sum, red, turn, &total);
+  if (!(total > 0.f)) return Range{kNone, kNone};
   const float slack = (0.5f / one + 2e-6f) * total, lo = s.p * total - slack, hi = s.p * total + slack;
   int b1 = kNone, b2 = kNone;
 #pragma unroll
@@ -648,7 +650,8 @@ struct Tokens {
 // reaches the target, or all of them.  All threads; returns the same in each.
 // Rounds of 1024 bins over the keys from the largest down (of bf16 the upper
 // halves, which are all there is to them): one for a list of bf16, two or
-// three for fp32.  false: the target lies before these tokens or behind them.
+// three for fp32.  false: the target lies before these tokens or behind them, or
+// there are none.
 template <bool MASS, typename T>
 __device__ __forceinline__ bool cut(const Row<T> &row, const Tokens<T> &tokens, Kept &kept, double lm, uint64_t before, uint64_t target,
                                  ChooseShared &sh, int &turn) {
@@ -678,7 +681,7 @@ __device__ __forceinline__ bool cut(const Row<T> &row, const Tokens<T> &tokens, 
     lo = min(lo, sh.lo[i]);
     hi = max(hi, sh.hi[i]);
   }
-  if (hi == 0) return before >= target;  // no tokens
+  if (hi == 0) return false;  // no tokens
   for (;;) {
     int shift = 0;
     while ((hi - lo) >> shift >= (uint32_t)kCutBins) ++shift;
@@ -807,7 +810,8 @@ __global__ __launch_bounds__(kSampThreads) void sample_choose_kernel(SampleArgs 
   // ---- the filters ----
   Kept kept{0, 0};  // (no finite logit has key 0)
   if (s.mode != kPlain) {
-    Tokens<T> tokens{row, sh, listed <= kList ? listed : -1};
+    // (a filter ends at a token: a list of none does not suffice)
+    Tokens<T> tokens{row, sh, listed > 0 && listed <= kList ? listed : -1};
     if (s.k > 0) cut<false>(row, tokens, kept, -INFINITY, 0, (uint64_t)s.k, sh, turn);
     if (kept.ties > 0 && row.exponent(value_of_key(kept.tie)) < s.lm) kept.ties = 0;
     if (s.p < 1.f) {
