@@ -534,13 +534,15 @@ __global__ __launch_bounds__(kSampThreads) void sample_weigh_kernel(SampleArgs a
         list[base + at[e]] = (uint64_t)order_key(f[e]) << 32 | (uint32_t)(p * kPiece + 8 * lane + e);
   };
   const double lm = s.mode == kListM ? fmax(s.lm, kLeast) : s.lm;
-  // a depth below these lies in a bin above the range, or in it or above
-  const float above_range = (float)range.first, in_range = range.last < kBins - 1 ? (float)(range.last + 1) : INFINITY;
+  // a depth below the first lies in a bin above the range, one up to the second in it or above (the last bin's
+  // logits may lie at an infinite depth)
+  const float above_range = (float)range.first;
+  const float in_range = range.last < kBins - 1 ? __uint_as_float(__float_as_uint((float)(range.last + 1)) - 1) : INFINITY;
   if (s.mode == kListK) {
     row.each_piece(p0, p1, [&](const typename Row<T>::Eight &f, int p) {
       bool take[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) take[e] = f[e] > -INFINITY && row.depth(f[e]) < in_range;
+      for (int e = 0; e < 8; ++e) take[e] = f[e] > -INFINITY && row.depth(f[e]) <= in_range;
       add(f, p, take);
     });
   } else if (s.mode == kListM) {
@@ -564,7 +566,7 @@ __global__ __launch_bounds__(kSampThreads) void sample_weigh_kernel(SampleArgs a
         all += m;
         above += over ? m : 0;
         n += over;
-        take[e] = !over && d < in_range && f[e] > -INFINITY;
+        take[e] = !over && d <= in_range && f[e] > -INFINITY;
       }
       S += all - 8 * kZeroWeight;
       above = wave_sum64(above - n * kZeroWeight);

@@ -57,3 +57,26 @@ def test_no_mass_is_kept_but_the_likeliest_token(dt):
         assert np.array_equal(tokens, x.float().cpu().numpy().argmax(1))
     x[:] = -INF
     assert sample(x, np.full(n, 0.5), p=np.zeros(n))[2] == sm.ERR_EINVAL
+
+
+@pytest.mark.parametrize("dt", [BF, F32], ids=str)
+@pytest.mark.parametrize("V", [2000, 30000])
+def test_a_wide_k_takes_logits_past_the_largest_depth(V, dt):
+    """Finite logits so low that their depth below the others passes fp32's range weigh like any others at a temperature as
+    high: a k that reaches into them keeps its first."""
+    rng = np.random.RandomState(V)
+    big = torch.finfo(dt).max
+    x = np.full((6, V), -big, np.float32)
+    near = [600, 40, 1500, 600, 600, 3]
+    for r, n in enumerate(near):
+        x[r, rng.permutation(V)[:n]] = rng.randn(n)
+    x[3, 0] = 0.0                                                # the bins' origin, with and without a near logit
+    x[4, :512] = -big
+    x = torch.from_numpy(x).to(dt).to(dev())
+    u = np.array([0.99, 0.5, 0.9, 0.999, 0.7, 0.8])
+    say("wide k", dt, V)
+    for T in (3e38, 1e38):
+        tokens = check(x, u, T=np.full(6, T), k=[V - 1, 1500, 1600, V - 1, 1900, 10])
+        assert (x[torch.arange(6), torch.from_numpy(tokens).long()] < -1e30).any()
+        check(x, u, T=np.full(6, T), k=np.full(6, 1700), p=np.full(6, 0.9))
+        check(x, u, T=np.full(6, T), p=np.linspace(0.1, 0.95, 6))
