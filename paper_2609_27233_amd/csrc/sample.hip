@@ -42,6 +42,7 @@
 // took longer.
 #include <algorithm>
 #include <cmath>
+#include <cstddef>
 #include <type_traits>
 
 #include "common.hpp"
@@ -65,18 +66,20 @@ constexpr float kSharpest = 0.25f;             // temperatures below go by a lis
 constexpr int kList = 4096;                    // tokens that are cut in LDS
 constexpr int kCutBins = 1024;
 
-// What a row has in the workspace.  The first part is zero between calls.
-struct RowState {
+// What a row has in the workspace.  The first part is zero between calls.  The
+// bins are read and cleared 16 bytes at a time.
+struct alignas(16) RowState {
   uint32_t top;       // key of M
   uint32_t bad;       // a NaN
   uint32_t listed;    // tokens listed; more than kList: not all of them
   uint32_t unused;
   uint64_t mass;      // of all tokens (kMass); greedy: key of M << 32 | ~its first token
-  uint32_t bins[kBins];
+  alignas(16) uint32_t bins[kBins];
   // not cleared
   uint64_t pieces[kMostPieces];  // ties << 54 | mass
   uint64_t list[kList];          // key << 32 | token
 };
+static_assert(offsetof(RowState, bins) % 16 == 0 && sizeof(RowState) % 16 == 0, "16-byte accesses to the bins of any row");
 constexpr int kRowsAtATime = 1024;  // rows that the workspace holds
 
 struct SampleArgs {
