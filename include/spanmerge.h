@@ -409,8 +409,9 @@ size_t sm_decode_shared_workspace_bytes(int n, int num_q_heads, int head_dim,
  *  max_prefix     (host) upper bound on the prefixes' lengths; sizes the grid,
  *                 which is refused past 2^24 workgroups (tens of thousands of
  *                 groups or requests with bounds of hundreds of thousands)
- *  ws, ws_bytes   at least sm_decode_shared_workspace_bytes(...); its first
- *                 256 KiB as sm_decode_attention's, which it can serve too
+ *  ws, ws_bytes   at least sm_decode_shared_workspace_bytes(...), 16-byte
+ *                 aligned; its first 256 KiB as sm_decode_attention's, which
+ *                 it can serve too
  * Device errors (into c->err; the affected requests' rows are zero): EINVAL
  * (bad id or block id; group offsets out of order: every row), ERANGE (length
  * > max_len, prefix > max_prefix).

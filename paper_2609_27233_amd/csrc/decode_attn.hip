@@ -2027,9 +2027,8 @@ SM_API sm_status sm_decode_attention(const sm_paged_cache *c, const int32_t *seq
 
 // Polls of the fused step's commit wait (kCommitSpinLimit unless a test
 // lowers it to exercise the give-up path).
-// Workspace of a shared call: that of sm_decode_attention, then one line for
-// the flag, then the prefixes' parts.
-constexpr int64_t kSharedLine = 256;
+// Workspace of a shared call: that of sm_decode_attention, then the prefixes'
+// parts.
 static int64_t decode_part_bytes(int n, int num_q_heads, int head_dim, int max_len) {
   return ((int64_t)sm_decode_workspace_bytes(n, num_q_heads, head_dim, max_len) + kSharedLine - 1) / kSharedLine * kSharedLine;
 }
@@ -2037,8 +2036,8 @@ static int64_t decode_part_bytes(int n, int num_q_heads, int head_dim, int max_l
 SM_API size_t sm_decode_shared_workspace_bytes(int n, int num_q_heads, int head_dim, int max_len, int max_prefix) {
   if (n <= 0 || num_q_heads <= 0 || head_dim <= 0 || max_len < 0 || max_prefix < 0) return 0;
   const int64_t vectors = (int64_t)n * num_q_heads;
-  return (size_t)(decode_part_bytes(n, num_q_heads, head_dim, max_len) + kSharedLine +
-                  vectors * shared_most_chunks(vectors, max_prefix) * (head_dim + 2) * (int64_t)sizeof(float));
+  return (size_t)(decode_part_bytes(n, num_q_heads, head_dim, max_len) +
+                  shared_parts(vectors, shared_most_chunks(vectors, max_prefix), head_dim).end);
 }
 
 SM_API sm_status sm_decode_attention_shared(const sm_paged_cache *c, const int32_t *seq_ids, int n, const int32_t *prefix_ids,
@@ -2052,7 +2051,7 @@ SM_API sm_status sm_decode_attention_shared(const sm_paged_cache *c, const int32
   if (max_prefix < 0 || num_groups < 0 || num_groups > 65535 || !(fabsf(scale) <= 3.0e38f)) return SM_EINVAL;
   if (n == 0) return SM_OK;
   if (num_groups == 0) return SM_EINVAL;
-  if (!prefix_ids || !group_offsets) return SM_EINVAL;
+  if (!prefix_ids || !group_offsets || (uintptr_t)ws % 16) return SM_EINVAL;
   if ((int64_t)max_prefix > (int64_t)c->max_blocks_per_seq * c->block_size ||
       (uint64_t)c->num_kv_heads * c->block_size * c->head_dim * 2 > 0xffffffffull)
     return SM_EINVAL;
@@ -2067,9 +2066,10 @@ SM_API sm_status sm_decode_attention_shared(const sm_paged_cache *c, const int32
   // one chunk at least: the launch that checks the groups
   const int64_t chunks = p.plan.chunks > 0 ? p.plan.chunks : 1, vectors = (int64_t)n * num_q_heads;
   char *at = (char *)ws + decode_part_bytes(n, num_q_heads, c->head_dim, max_len);
-  p.parts.flag = (int32_t *)at;
-  p.parts.ml = (float *)(at + kSharedLine);
-  p.parts.o = p.parts.ml + 2 * vectors * chunks;
+  const SharedParts parts = shared_parts(vectors, chunks, c->head_dim);
+  p.parts.flag = (int32_t *)(at + parts.flag);
+  p.parts.o = (float *)(at + parts.o);
+  p.parts.ml = (float *)(at + parts.ml);
   p.parts.chunks = (int)chunks;
   // the launch of the parts: at most `blocks` blocks of vectors over all groups
   const int64_t blocks = (int64_t)n * a.G / kSharedVec + num_groups;

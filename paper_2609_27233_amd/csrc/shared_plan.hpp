@@ -45,6 +45,19 @@ inline int64_t shared_most_chunks(int64_t vectors, int max_prefix) {
   return got > 1 ? got : 1;
 }
 
+// Where the prefixes' parts lie in the workspace, in bytes from the end of the
+// requests' own: the flag in a line of its own, then each vector's and chunk's
+// unnormalised output, read and written 16 bytes at a time (the statistics
+// behind it: their 8 bytes come in any number).
+constexpr int64_t kSharedLine = 256;
+struct SharedParts {
+  int64_t flag, o, ml, end;
+};
+inline SharedParts shared_parts(int64_t vectors, int64_t chunks, int head_dim) {
+  const int64_t o = kSharedLine, ml = o + vectors * chunks * head_dim * 4;
+  return SharedParts{0, o, ml, ml + vectors * chunks * 8};
+}
+
 // n requests of G query heads on each of H kv heads, in `groups` groups.
 inline SharedPlan plan_shared(int n, int H, int G, int groups, int max_prefix) {
   if (max_prefix <= 0) return SharedPlan{kSharedStep, 0};
