@@ -407,7 +407,7 @@ size_t sm_decode_shared_workspace_bytes(int n, int num_q_heads, int head_dim,
  *  num_groups     (host) 1 to 65535
  *  scale          (host) finite
  *  max_prefix     (host) upper bound on the prefixes' lengths; sizes the grid,
- *                 which is refused past 2^24 workgroups (tens of thousands of
+ *                 which is refused from 2^24 workgroups on (tens of thousands of
  *                 groups or requests with bounds of hundreds of thousands)
  *  ws, ws_bytes   at least sm_decode_shared_workspace_bytes(...), 16-byte
  *                 aligned; its first 256 KiB as sm_decode_attention's, which

@@ -2074,7 +2074,7 @@ SM_API sm_status sm_decode_attention_shared(const sm_paged_cache *c, const int32
   // the launch of the parts: at most `blocks` blocks of vectors over all groups
   const int64_t blocks = (int64_t)n * a.G / kSharedVec + num_groups;
   const int64_t prefix_wgs = blocks * a.Hkv * chunks, own_wgs = (int64_t)n * a.Hkv * a.max_chunks;
-  if (prefix_wgs + own_wgs > (1 << 24)) return SM_EINVAL;  // (a launch's threads are counted in 32 bits)
+  if (prefix_wgs + own_wgs >= (1 << 24)) return SM_EINVAL;  // (a launch's threads are counted in 32 bits)
   SharedArgs sa{a, pf_args(c, q, num_q_heads, scale), (int)prefix_wgs};
   sa.prefix.p = p;
   sa.prefix.BQ = 1;
@@ -2090,6 +2090,7 @@ SM_API sm_status sm_decode_attention_shared(const sm_paged_cache *c, const int32
   const auto chosen = c->head_dim == 128 ? (eight ? kernel(d128, std::true_type()) : kernel(d128, std::false_type()))
                                          : (eight ? kernel(d64, std::true_type()) : kernel(d64, std::false_type()));
   hipLaunchKernelGGL(chosen, dim3((unsigned)(prefix_wgs + own_wgs)), dim3(kDecThreads), 0, stream, sa);
+  if (hipGetLastError() != hipSuccess) return SM_EHIP;  // (nothing to join)
   const auto join = c->head_dim == 128 ? shared_join_kernel<128> : shared_join_kernel<64>;
   hipLaunchKernelGGL(join, dim3((unsigned)(n * a.Hkv)), dim3(kDecThreads), 0, stream, a, p.parts);
   return hipGetLastError() == hipSuccess ? SM_OK : SM_EHIP;

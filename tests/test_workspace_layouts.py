@@ -68,3 +68,12 @@ def test_the_parts_of_shared_prefixes_are_aligned(parts, D):
 def test_a_shared_workspace_off_16_bytes_is_refused(ws):
     d = _desc(dtype=sm.SM_E4M3, k_pool=16, v_pool=32)
     assert sm.load().sm_decode_attention_shared(C.byref(d), 1, 4, 1, 1, 1, 1, 32, 1.0, 16, 16, 1, ws, 1 << 40, None) == sm.SM_EINVAL
+
+
+def test_a_shared_grid_of_two_to_the_24_is_refused():
+    """4095 groups x 4097 chunks of 8192 entries, and one workgroup for the request's own: 2^32 threads, one more than a
+    launch counts."""
+    d = _desc(dtype=sm.SM_E4M3, k_pool=16, v_pool=32, num_kv_heads=1, block_size=512, max_blocks_per_seq=4097 * 16)
+    longest = 4097 * 8192
+    need = sm.load().sm_decode_shared_workspace_bytes(1, 1, 128, 0, longest)
+    assert sm.load().sm_decode_attention_shared(C.byref(d), 1, 1, 1, 1, 4095, 1, 1, 1.0, 0, longest, 1, 16, need, None) == sm.SM_EINVAL
