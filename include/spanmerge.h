@@ -1042,10 +1042,11 @@ size_t sm_sample_workspace_bytes(int rows, int vocab);
  *               that may run concurrently must not share a workspace
  * Weights are formed in double precision and added as whole multiples of
  * 2^-44, so that a token below 2^-45 of the likeliest one weighs nothing, and a
- * share is right to 2^-27 at worst, 2^-37 as a rule.  A logit of -infinity is
- * never drawn.  Device errors (into err, unless it is null): EINVAL for a
- * setting out of its range, or a row that holds a NaN or +infinity or nothing
- * but -infinity; its token is -1 and its log probability NaN.
+ * share is right to vocab x 2^-45 at worst (2^-28 for 128,256 tokens, 2^-26 for
+ * 524,288), 2^-37 as a rule.  A logit of -infinity is never drawn.  Device
+ * errors (into err, unless it is null): EINVAL for a setting out of its range,
+ * or a row that holds a NaN or +infinity or nothing but -infinity; its token is
+ * -1 and its log probability NaN.
  */
 sm_status sm_sample_tokens(const void *logits, int64_t stride, int rows,
                            int vocab, sm_dtype dt, const float *u,

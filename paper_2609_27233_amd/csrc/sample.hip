@@ -13,8 +13,9 @@
 // token's share.  A weight is formed in double precision (a table of 128 and a
 // polynomial, off by 2^-49) and rounded to a multiple of 2^-44; masses are
 // 64-bit integers.  Their sums are exact and the same in any order, so that
-// workgroups, waves and atomics may add them as they come.  Over 128,256
-// tokens the roundings come to about 2^-37 of the largest weight.
+// workgroups, waves and atomics may add them as they come.  Of V tokens the
+// roundings come to V x 2^-45 of the largest weight at most (2^-28 for 128,256,
+// 2^-26 for the most that a row may have); as a rule, over 128,256, to 2^-37.
 //
 // Three launches, none of which waits inside:
 //   scan    M, and a histogram over the logits (2048 bins of 1/23): counts for
@@ -51,7 +52,7 @@ namespace sm {
 
 constexpr int kSampThreads = 256, kSampWaves = kSampThreads / 64;
 constexpr int kPiece = 512;                    // tokens of a piece: 8 a lane
-constexpr int kMostVocab = 1 << 19;            // a mass of 2^44 times this many fits 63 bits
+constexpr int kMostVocab = 1 << 19;            // 2^44 times this many is 2^63: a mass fits 64 bits
 constexpr int kMostPieces = kMostVocab / kPiece;
 constexpr int kInFlight = 4;                   // pieces that a wave loads at a time
 constexpr int kUnit = 44;                      // a weight of 1 is 2^44
