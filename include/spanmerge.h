@@ -396,6 +396,14 @@ size_t sm_decode_shared_workspace_bytes(int n, int num_q_heads, int head_dim,
  * row attends to is its result (over pages of either type).  Two
  * launches; the result does not depend on the order in which work is done.
  *
+ * This is a form for single tokens.  sm_prefill_attention attends over the
+ * entries of one sequence, so a request's prompt rows that are to attend to the
+ * prefix go through a sequence that holds its entries too: sm_kv_read the
+ * prefix and sm_kv_write_rotary it there (positions of 0, attn_scale 1), then
+ * write the prompt's K and V rows twice, behind that copy and into the request's
+ * own sequence, at the same positions; queries attend over the copy, whose
+ * prompt rows sm_kv_rollback takes away for the next request.
+ *
  *  c              (host) bf16 or SM_E4M3 pages, as sm_prefill_attention
  *  seq_ids, n, q, num_q_heads, max_len, out: as sm_decode_attention; the
  *                 lengths count a sequence's own entries, which may be none

@@ -402,7 +402,9 @@ def decode_attention_shared(cache: PagedCache, seq_ids, prefix_ids, group_offset
     """decode_attention of requests behind shared entries: the requests
     group_offsets[p] .. group_offsets[p + 1] - 1 attend over the entries of
     sequence prefix_ids[p] (-1: none), then over their own.  q, out [n, Hq, D]
-    bf16; max_len and max_prefix bound the sequences' and the prefixes' lengths."""
+    bf16; max_len and max_prefix bound the sequences' and the prefixes' lengths.
+    For single tokens: a prompt's rows attend to a prefix through a sequence
+    that holds a copy of its entries (prefill_attention sees one sequence)."""
     b = _calls()
     n, Hq, D = _shape(q, 3, "q")
     for t, name in ((q, "q"), (out, "out")):
