@@ -50,8 +50,8 @@ METRIC = "decode-attention tokens/s + achieved HBM GB/s over span-compacted KV c
 # WRITE_SIZE runs (see profiles/decode_step_llama3-8b-layer.md): scaled
 # measured bytes per launch divided by the algorithmic bytes of the same
 # launches.  Valid only for the kernel source it was measured on.
-TRAFFIC_RATIO = 1.0155
-TRAFFIC_SOURCE_SHA256 = {"decode_attn.hip": "da751894d7af571acc712013394b24d0a0e22c3c9ad1704637bd9d57c7187b78", "common.hpp": "3a781c03722dbc429c51a46492495ab49231891a56fcc322a70bd2033200c04d"}
+TRAFFIC_RATIO = 1.0154
+TRAFFIC_SOURCE_SHA256 = {"decode_attn.hip": "d3cdb5ce2bf32660e80f2109e5d6d1e91eebd22c9b2a331e630e15c39eeff265", "common.hpp": "3a781c03722dbc429c51a46492495ab49231891a56fcc322a70bd2033200c04d"}
 
 
 def log(*a):

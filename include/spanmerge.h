@@ -70,6 +70,9 @@
  * Dtypes: SM_F32 (fp32 storage, fp32 arithmetic) and SM_BF16 (bf16 storage,
  * fp32 accumulation, outputs rounded to nearest-even bf16).  Pages of a cache
  * may also be SM_E4M3 (see sm_paged_cache), for the calls that say so.
+ * Attention over bf16 and SM_E4M3 pages rounds each entry's weight (SM_E4M3:
+ * times the power of two of its V) to bf16 before the product with V; the
+ * weights' sum is taken of the unrounded ones, in fp32.
  */
 #ifndef SPANMERGE_H
 #define SPANMERGE_H
@@ -355,8 +358,8 @@ size_t sm_decode_workspace_bytes(int n, int num_q_heads, int head_dim,
  * of each (sequence, kv head) to finish.
  *
  *  c            (host) any page type; SM_E4M3 pages stand for the features
- *               above, to all of their bits, and q and out are bf16; a NaN
- *               that a row attends to is then its result
+ *               of sm_paged_cache, which are read without loss, and q and out
+ *               are bf16; a NaN that a row attends to is then its result
  *  seq_ids      [n] ids in [0, max_seqs) (repeats allowed)
  *  q            [n][num_q_heads][head_dim] (cache dtype)
  *  num_q_heads  (host) multiple of num_kv_heads, group size <= 16

@@ -986,7 +986,11 @@ __device__ __forceinline__ float byte_scale(uint32_t w, int i) {
 // are planned before the streaming loop, since they decide what is read.
 // EIGHT (without STEP): e4m3 pages.  Their values become bf16 on the way to the
 // matrix cores, K's with their exponents (a lane's K values are of one token);
-// V's exponents go into the probabilities before those are rounded to bf16.
+// V's exponents go into the probabilities before those are rounded to bf16, the
+// matrix cores' type for an operand beside V (2^-8 of a weight at most; their
+// sum is of the unrounded ones).  The reference is the largest score, whose
+// weight of 1 loses nothing: at 16 sequences of 2458 to 2842 the result is off
+// by 1.7e-3 of its size, which is its own rounding to bf16.
 // Half the bytes in as many loads (16 bytes a lane, tiles of 64 tokens).  Us,
 // e4m3 and bf16, 32/8 heads, D = 128: 16 x 2842 21.4, 33.5; 128 x 4096 179, 325
 // (6.0 and 6.6 TB/s); 4 x 32,768 49, 87.  A batch's step is bound by what one
@@ -1560,8 +1564,9 @@ __global__ __launch_bounds__(kDecThreads, 2) void decode_split_bf16(DecodeArgs a
 // prefixes' chunks, each for all the vectors of its group, and for the
 // requests' own chunks, side by side; a second joins a row's partials.  (Own
 // chunks in a launch of their own, which joined as the last workgroup of a row
-// arrived: 16 requests behind 2048 entries 33 us for 21.5, 128 behind four of
-// 6000 to 8192 87 for 62.)  The prefixes' products bound it where groups are
+// arrived, took 33 us where this took 21.5 for 16 requests behind 2048 entries,
+// and 87 for 62 for 128 behind four of 6000 to 8192; the cut of the prefixes has
+// brought those to 52 since.)  The prefixes' products bound it where groups are
 // large, 0.35 to 0.6 PFLOP/s; a batch's step is 14 us of parts, for one chunk
 // of 128 entries a workgroup, and 6 of joins: launches and dependent reads.
 
@@ -2025,8 +2030,6 @@ SM_API sm_status sm_decode_attention(const sm_paged_cache *c, const int32_t *seq
   return decode_launch<false>(c, a, n, stream);
 }
 
-// Polls of the fused step's commit wait (kCommitSpinLimit unless a test
-// lowers it to exercise the give-up path).
 // Workspace of a shared call: that of sm_decode_attention, then the prefixes'
 // parts.
 static int64_t decode_part_bytes(int n, int num_q_heads, int head_dim, int max_len) {
@@ -2096,6 +2099,8 @@ SM_API sm_status sm_decode_attention_shared(const sm_paged_cache *c, const int32
   return hipGetLastError() == hipSuccess ? SM_OK : SM_EHIP;
 }
 
+// Polls of the fused step's commit wait (kCommitSpinLimit unless a test
+// lowers it to exercise the give-up path).
 static std::atomic<int> g_commit_spin_limit{kCommitSpinLimit};
 
 SM_API void sm_set_commit_wait_limit(int polls) {

@@ -12,7 +12,9 @@
 //   * Row rho of the score block is the token at which register r of lane half
 //     h2 has token 16 h2 + r: a half's 16 probabilities are a run of 16 tokens,
 //     and so are its bytes of V, the 16 of one dim in a page.
-// V's exponents go into the probabilities after their sum is taken.
+// V's exponents go into the probabilities after their sum is taken and before
+// they are rounded to bf16, the matrix cores' type beside V (2.2e-3 of the
+// result's size with its own rounding of 1.65e-3).
 //
 // The two products and the softmax of a tile bound it: 0.7 PFLOP/s at 250 rows
 // of 32/8 heads, D = 128, behind 8192 entries (54 us; with the loads left out

@@ -277,7 +277,11 @@ __device__ __forceinline__ float turned_one(float own, float other, float2 cs) {
 // their pairs, with the sign to be added to them: (a, b) -> a cos - b sin
 // where a lies, b cos + a sin where b does.
 // LANES: of 128 features, all turned, the other half lies eight lanes on.
-// (39,328 rows of 8 heads, keys and values: 62 us, loading it 80; bf16 pages 63.)
+// (39,328 rows of 8 heads, keys and values, over several caches in turn: 57 to 62
+// us, loading it 80.  What loads it: 64 of 128 features turned 65, head dim 64 37
+// where the interleaved layout, which has its pairs in a lane, takes 31; bf16
+// pages 68, 71, 39 and 34.  Rows off 16 bytes, a feature at a time, 177; bf16
+// pages 360.)
 template <bool HALF, bool LANES = false>
 struct Chunk {
   u32x4_t own, other;

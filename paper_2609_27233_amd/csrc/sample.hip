@@ -32,15 +32,26 @@
 // so far below the bins' origin that the histogram holds no mass) is cut by
 // passes over the whole row, in `choose`, to the same result.
 //
+// Such a row is slow: one workgroup passes over it several times.  Us for 16
+// rows of 128,256 bf16 logits: k = 50 22, 5000 687; p = 0.9 28, of nearly equal
+// logits 960, of equal ones 506; p = 0.9 and min-p 1e-4 at T = 4 1020; k = 50000
+// and p = 0.9 1190.  1024 rows: k = 50 162, 5000 1690; p = 0.9 269, of nearly
+// equal logits 2650.  So is one whose first 512 logits lie more than 22 below the
+// rest without being -infinity (a mask of -1e4 or of the type's lowest value):
+// all of the rest falls into the first bin, and k = 50 takes 533, p = 0.9 1020
+// (masked by -infinity 22 and 28).
+//
 // 1024 rows of 128,256 bf16 logits, mixed filters: scan 69 us, weigh 108,
-// choose 23; all greedy, which are read once, 70 in all (123 with their ties
-// counted by weigh).  The vector ALU and the two reads bound it (20 and 37
-// instructions a logit; a read alone would take 39 us): LDS atomics and an
-// exponential, and the nine products in double precision of a weight.  (Weights
-// from a table of the bf16 values in LDS: 222 for 207 in all, for the waves that
-// its 32 KB displace.)  16 rows: 6, 11 and 14 us, a chain of dependent reads and
-// barriers.  Rows fewer at a time, or a slice's loads before the bins are known,
-// took longer.
+// choose 23; all greedy, which are read once, 70 in all (scan 58 at 4.5 TB/s, 12
+// of two launches that find nothing to do; 123 with their ties counted by
+// weigh).  By filter: none 183, top-k 153, top-p 277, min-p 137; 400 rows of
+// fp32 95, 94, 147, 83, greedy 50; 16 rows of bf16 14, 22, 31, 14, greedy 11.
+// The vector ALU and the two reads bound it (20 and 37 instructions a logit; a
+// read alone would take 39 us): LDS atomics and an exponential, and the nine
+// products in double precision of a weight.  (Weights from a table of the bf16
+// values in LDS: 222 for 207 in all, for the waves that its 32 KB displace.)  16
+// rows: 6, 11 and 14 us, a chain of dependent reads and barriers.  Rows fewer at
+// a time, or a slice's loads before the bins are known, took longer.
 #include <algorithm>
 #include <cmath>
 #include <cstddef>
